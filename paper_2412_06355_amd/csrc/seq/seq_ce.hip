@@ -1,0 +1,582 @@
+// Softmax cross entropy of a linear readout over a vocabulary.
+//
+//   z = s H W^T,  lse = log sum_v exp z_v,  loss = lse - z_target
+//   dz = r s (softmax(z) - onehot(target)),  dH = dz W,  dW = dz^T H
+//
+// The rows go through in pieces whose logits fit a bounded scratch.  Of a piece, the
+// first product leaves each row's maximum and sum of exponentials over every tile of
+// the vocabulary (and, for the gradient, its fp32 logits); the tiles' statistics are
+// joined into lse; the gradient of the logits is rounded to bf16 once and enters the
+// two other products, dW summed over the pieces in fp32.  The three products carry
+// the time: 2 N V D operations each.
+#include "seq_gemm.h"
+
+namespace dendsn_seq {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int64_t kPieceBytes = int64_t(4) << 30;  // of the logits and their gradient of a piece
+
+__device__ __forceinline__ int64_t target_of(const void* t, int wide, int64_t i) {
+  return wide ? static_cast<const int64_t*>(t)[i] : int64_t(static_cast<const int32_t*>(t)[i]);
+}
+
+// ---------------------------------------------------------------------------
+// Operands as bf16 planes
+// ---------------------------------------------------------------------------
+struct PackArgs {
+  const void* src;
+  uint16_t* dst;
+  const void* targets;  // rows without a target become zero (NULL: none)
+  int64_t rows, cols, ld, cols_p, plane, V;
+  int wide, planes;
+};
+
+// v as three bf16 that add up to it (two for the bits below the first eight): cut off,
+// not rounded, so that no part overflows.  Infinities and NaN are in the first alone, and
+// not in its finite copy.
+__device__ __forceinline__ void split3(float v, uint16_t& a, uint16_t& finite, uint16_t& b, uint16_t& c) {
+  const uint32_t u = __float_as_uint(v);
+  a = finite = uint16_t(u >> 16);
+  if ((u & 0x7F800000u) == 0x7F800000u) {
+    if (u & 0x7FFFFFu) a |= 0x40;  // a NaN stays one without its low bits
+    finite = b = c = 0;
+    return;
+  }
+  const float r1 = v - __uint_as_float(u & 0xFFFF0000u);
+  const uint32_t u1 = __float_as_uint(r1);
+  b = uint16_t(u1 >> 16);
+  const float r2 = r1 - __uint_as_float(u1 & 0xFFFF0000u);
+  c = uint16_t(__float_as_uint(r2) >> 16);
+}
+
+template <typename IO>
+__global__ void __launch_bounds__(kThreads) ce_pack_kernel(PackArgs p) {
+  const int64_t row = blockIdx.x;
+  bool keep = true;
+  if (p.targets) {
+    const int64_t t = target_of(p.targets, p.wide, row);
+    keep = t >= 0 && t < p.V;
+  }
+  const IO* src = static_cast<const IO*>(p.src) + row * p.ld;
+  uint16_t* dst = p.dst + row * p.cols_p;
+  for (int64_t d = threadIdx.x; d < p.cols_p; d += kThreads) {
+    const float v = keep && d < p.cols ? widen(src[d]) : 0.0f;
+    if (p.planes == 1) {
+      dst[d] = bf16_bits(v);
+    } else {
+      uint16_t a, f, b, c;
+      split3(v, a, f, b, c);
+      dst[d] = a;
+      dst[p.plane + d] = b;
+      dst[2 * p.plane + d] = c;
+      dst[kFinite * p.plane + d] = f;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The products
+// ---------------------------------------------------------------------------
+struct LogitArgs {
+  GemmArgs g;
+  float scale;
+  float2* stats;   // [M][tiles_n] maximum and sum of exponentials
+  float* z;        // [M][ldz] logits, NULL: not kept
+  float* chosen;   // [M] the target's logit (where z is not kept)
+  const void* targets;
+  int64_t ldz;
+  int wide;
+};
+
+template <int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(WM * WN * 64) ce_logits_kernel(LogitArgs p) {
+  using G = Gemm<BM, BN, WM, WN, false, false>;
+  __shared__ __align__(1024) char lds[2 * G::kStage];
+  int tm, tn;
+  tile_of(p.g, blockIdx.x, tm, tn);
+  f32x4 acc[G::FN][G::FM];
+  G::run(p.g, lds, tm, tn, 0, acc);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int wm = w / WN, wn = w % WN;
+  float2* part = reinterpret_cast<float2*>(lds);  // [WN][BM]
+  const int64_t n0 = int64_t(tn) * BN + wn * G::TN + 4 * (lane >> 4);
+#pragma unroll
+  for (int j = 0; j < G::FM; ++j) {
+    const int64_t m = int64_t(tm) * BM + wm * G::TM + 16 * j + (lane & 15);
+    const bool row = m < p.g.M;
+    int64_t target = -1;
+    if (p.chosen && row) target = target_of(p.targets, p.wide, m);
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < G::FN; ++i) {
+      const int64_t n = n0 + 16 * i;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float z = acc[i][j][r] * p.scale;
+        acc[i][j][r] = z;
+        if (n + r < p.g.N) top = fmaxf(top, z);
+        if (p.chosen && n + r == target) p.chosen[m] = z;
+      }
+      if (p.z && row && n < p.ldz) *reinterpret_cast<f32x4*>(p.z + m * p.ldz + n) = acc[i][j];
+    }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < G::FN; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (n0 + 16 * i + r < p.g.N) sum += __expf(acc[i][j][r] - ref);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (lane < 16) part[wn * BM + wm * G::TM + 16 * j + lane] = make_float2(top, sum);
+  }
+  __syncthreads();
+  for (int r = threadIdx.x; r < BM; r += WM * WN * 64) {
+    const int64_t m = int64_t(tm) * BM + r;
+    if (m >= p.g.M) continue;
+    float2 a = part[r];
+#pragma unroll
+    for (int q = 1; q < WN; ++q) {
+      const float2 b = part[q * BM + r];
+      const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.0f : top;
+      a = make_float2(top, a.y * __expf(a.x - ref) + b.y * __expf(b.x - ref));
+    }
+    p.stats[m * p.g.tiles_n + tn] = a;
+  }
+}
+
+enum Out { kOutIo = 0, kOutPartial = 1, kOutSum = 2 };
+
+struct GradArgs {
+  GemmArgs g;
+  void* out;             // io (kOutIo)
+  float* part;           // [splits][M][N] (kOutPartial) or [M][N] (kOutSum)
+  const void* targets;   // rows without a target are +0 (NULL: none)
+  int64_t ld, V;
+  int wide, io;          // io: dendsn_io
+  int add, keep;         // kOutSum: add what is there; write fp32 (else io, the last piece)
+};
+
+__device__ __forceinline__ void store4(void* out, int io, int64_t at, int64_t n, int64_t N, f32x4 v) {
+  // rows of any alignment: element by element unless 4 fit and lie aligned
+  if (io == DENDSN_IO_BF16) {
+    uint16_t* o = static_cast<uint16_t*>(out) + at;
+    if (n + 4 <= N && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
+      const uint64_t q = uint64_t(bf16_bits(v[0])) | uint64_t(bf16_bits(v[1])) << 16 |
+                         uint64_t(bf16_bits(v[2])) << 32 | uint64_t(bf16_bits(v[3])) << 48;
+      *reinterpret_cast<uint64_t*>(o) = q;
+      return;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (n + r < N) o[r] = bf16_bits(v[r]);
+  } else {
+    float* o = static_cast<float*>(out) + at;
+    if (n + 4 <= N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
+      *reinterpret_cast<f32x4*>(o) = v;
+      return;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (n + r < N) o[r] = v[r];
+  }
+}
+
+template <int BM, int BN, int WM, int WN, bool XCOL>
+__global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs p) {
+  using G = Gemm<BM, BN, WM, WN, XCOL, true>;
+  __shared__ __align__(1024) char lds[2 * G::kStage];
+  int tm, tn;
+  tile_of(p.g, blockIdx.x, tm, tn);
+  f32x4 acc[G::FN][G::FM];
+  const int split = blockIdx.y;
+  G::run(p.g, lds, tm, tn, split, acc);
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int64_t N = p.g.N;
+#pragma unroll
+  for (int j = 0; j < G::FM; ++j) {
+    const int64_t m = int64_t(tm) * BM + w / WN * G::TM + 16 * j + (lane & 15);
+    if (m >= p.g.M) continue;
+    bool zero = false;
+    if (p.targets) {
+      const int64_t t = target_of(p.targets, p.wide, m);
+      zero = t < 0 || t >= p.V;
+    }
+#pragma unroll
+    for (int i = 0; i < G::FN; ++i) {
+      const int64_t n = int64_t(tn) * BN + w % WN * G::TN + 16 * i + 4 * (lane >> 4);
+      if (n >= N) continue;
+      f32x4 v = acc[i][j];
+      if (zero) v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (p.g.splits > 1) {
+        store4(p.part, DENDSN_IO_F32, (int64_t(split) * p.g.M + m) * N + n, n, N, v);
+        continue;
+      }
+      if (p.add) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (n + r < N) v[r] += p.part[m * N + n + r];
+      }
+      if (p.keep) store4(p.part, DENDSN_IO_F32, m * N + n, n, N, v);
+      else store4(p.out, p.io, m * p.ld + n, n, N, v);
+    }
+  }
+}
+
+// The splits of a product joined, in their order.
+struct JoinArgs {
+  const float* part;
+  void* out;
+  int64_t M, N, ld;
+  int splits, io;
+};
+
+__global__ void __launch_bounds__(kThreads) ce_join_splits_kernel(JoinArgs p) {
+  const int64_t m = blockIdx.x;
+  for (int64_t n = threadIdx.x; n < p.N; n += kThreads) {
+    float s = 0.0f;
+    for (int k = 0; k < p.splits; ++k) s += p.part[(int64_t(k) * p.M + m) * p.N + n];
+    if (p.io == DENDSN_IO_BF16) static_cast<uint16_t*>(p.out)[m * p.ld + n] = bf16_bits(s);
+    else static_cast<float*>(p.out)[m * p.ld + n] = s;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Rows
+// ---------------------------------------------------------------------------
+struct LossArgs {
+  const float2* stats;
+  const float* z;       // kept logits, or
+  const float* chosen;  // the target's
+  const void* targets;
+  float *loss, *lse;    // lse: also what the gradient reads
+  int64_t M, ldz, V;
+  int tiles, wide;
+};
+
+// A wave a row: joins the tiles' statistics.
+__global__ void __launch_bounds__(kThreads) ce_loss_kernel(LossArgs p) {
+  const int lane = threadIdx.x & 63;
+  const int64_t m = int64_t(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
+  if (m >= p.M) return;
+  const int64_t t = target_of(p.targets, p.wide, m);
+  const bool keep = t >= 0 && t < p.V;
+  float top = -INFINITY;
+  for (int i = lane; i < p.tiles; i += 64) top = fmaxf(top, p.stats[m * p.tiles + i].x);
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f;
+  for (int i = lane; i < p.tiles; i += 64) {
+    const float2 s = p.stats[m * p.tiles + i];
+    sum += s.y * __expf((s.x == -INFINITY ? 0.0f : s.x) - ref);
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
+  if (lane == 0) {
+    const float lse = ref + logf(sum);
+    const float z = !keep ? 0.0f : p.z ? p.z[m * p.ldz + t] : p.chosen[m];
+    p.loss[m] = keep ? lse - z : 0.0f;
+    if (p.lse) p.lse[m] = keep ? lse : 0.0f;
+  }
+}
+
+struct DzArgs {
+  const float *z, *lse, *row_weight;
+  const void* targets;
+  uint16_t* dz;
+  int64_t ldz, plane, V;
+  float scale;
+  int wide, planes;
+};
+
+// dz = r s (exp(z - lse) - onehot), +0 in rows without a target and past V.
+__global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
+  const int64_t m = blockIdx.y;
+  const int64_t v0 = (int64_t(blockIdx.x) * kThreads + threadIdx.x) * 8;
+  if (v0 >= p.ldz) return;
+  const int64_t t = target_of(p.targets, p.wide, m);
+  const bool keep = t >= 0 && t < p.V;
+  const float c = keep ? p.scale * (p.row_weight ? p.row_weight[m] : 1.0f) : 0.0f;
+  const float lse = keep ? p.lse[m] : 0.0f;
+  const f32x4* z = reinterpret_cast<const f32x4*>(p.z + m * p.ldz + v0);
+  const f32x4 za = z[0], zb = z[1];
+  uint16_t a[8], f, b[8], d[8];  // (dz is finite wherever the loss is: no copy)
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float zk = k < 4 ? za[k & 3] : zb[k & 3];
+    float g = 0.0f;
+    if (keep && v0 + k < p.V) {
+      g = __expf(zk - lse);
+      if (v0 + k == t) g -= 1.0f;
+      g *= c;
+    }
+    if (p.planes == 1) a[k] = bf16_bits(g);
+    else split3(g, a[k], f, b[k], d[k]);
+  }
+  auto put = [&](uint16_t* to, const uint16_t (&x)[8]) {
+    uint4 q;
+    q.x = x[0] | uint32_t(x[1]) << 16;
+    q.y = x[2] | uint32_t(x[3]) << 16;
+    q.z = x[4] | uint32_t(x[5]) << 16;
+    q.w = x[6] | uint32_t(x[7]) << 16;
+    *reinterpret_cast<uint4*>(to + m * p.ldz + v0) = q;
+  };
+  put(p.dz, a);
+  if (p.planes == 3) put(p.dz + p.plane, b), put(p.dz + 2 * p.plane, d);
+}
+
+__global__ void __launch_bounds__(kThreads) ce_zero_kernel(void* out, int64_t rows, int64_t cols, int64_t ld, int io) {
+  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  if (i >= rows * cols) return;
+  const int64_t at = i / cols * ld + i % cols;
+  if (io == DENDSN_IO_BF16) static_cast<uint16_t*>(out)[at] = 0;
+  else static_cast<float*>(out)[at] = 0.0f;
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+dendsn_status check_cfg(const dendsn_ce_cfg* c) {
+  if (!c) return fail(DENDSN_E_INVALID, "cfg is NULL");
+  if (c->N < 0 || c->N > (int64_t(1) << 26)) return fail(DENDSN_E_INVALID, "N must be in [0, 2^26]");
+  if (c->V < 1 || c->V > (int64_t(1) << 24)) return fail(DENDSN_E_INVALID, "V must be in [1, 2^24]");
+  if (c->D < 1 || c->D > (int64_t(1) << 20)) return fail(DENDSN_E_INVALID, "D must be in [1, 2^20]");
+  const int64_t ld[4] = {c->ld_hidden, c->ld_grad_hidden, c->ld_weight, c->ld_grad_weight};
+  for (int i = 0; i < 4; ++i) {
+    if (ld[i] < c->D) return fail(DENDSN_E_INVALID, "every stride must be >= D");
+    if (!small_product(i < 2 ? c->N : c->V, ld[i])) return fail(DENDSN_E_INVALID, "a stride is too large");
+  }
+  if (c->io != DENDSN_IO_F32 && c->io != DENDSN_IO_BF16) return fail(DENDSN_E_INVALID, "bad io");
+  if (c->index != DENDSN_INDEX_I32 && c->index != DENDSN_INDEX_I64) return fail(DENDSN_E_INVALID, "bad index");
+  if (!isfinite(c->logit_scale)) return fail(DENDSN_E_INVALID, "logit_scale must be finite");
+  return DENDSN_OK;
+}
+
+constexpr int kBig = 256;  // tile of a product, both ways
+
+struct Plan {
+  int planes;
+  int64_t Dp, Vp;      // rows of packed operands, of logits
+  int64_t piece, pieces;
+  bool big;            // 256 x 256 tiles (else 128 x 128)
+  int tile;
+  int splits;          // of dH
+  size_t h, w, stats, z, dz, chosen, lse, dh, dw, total;
+};
+
+// Operands that the DMA can take as they lie: bf16, 16-byte chunks.
+bool direct(const dendsn_ce_cfg* c, const void* p, int64_t ld) {
+  return c->io == DENDSN_IO_BF16 && aligned(p, 16) && c->D % 8 == 0 && ld % 8 == 0 && ld <= kMaxLd;
+}
+
+Plan make_plan(const dendsn_ce_cfg* c, bool train) {
+  Plan p{};
+  p.planes = c->io == DENDSN_IO_BF16 ? 1 : 3;
+  p.Dp = round_up(c->D, kStep);
+  p.Vp = round_up(c->V, kStep);
+  const int64_t per_row = train ? p.Vp * (4 + 2 * p.planes) : ceil_div(c->V, 64) * 8;
+  int64_t most = kPieceBytes / per_row / kBig * kBig;
+  if (most < kBig) most = kBig;
+  const int64_t N = c->N > 0 ? c->N : 1;
+  p.pieces = ceil_div(N, most);
+  p.piece = p.pieces > 1 ? round_up(ceil_div(N, p.pieces), kBig) : N;
+  p.pieces = ceil_div(N, p.piece);
+  p.big = ceil_div(p.piece, kBig) * ceil_div(c->V, kBig) >= 256;
+  p.tile = p.big ? kBig : 128;
+  Carve cv;
+  p.h = cv.take(size_t(p.planes == 3 ? 4 : 1) * size_t(p.piece) * size_t(p.Dp) * 2);
+  p.w = cv.take(size_t(p.planes == 3 ? 4 : 1) * size_t(c->V) * size_t(p.Dp) * 2);
+  p.stats = cv.take(size_t(p.piece) * size_t(ceil_div(c->V, 64)) * 8);
+  p.lse = cv.take(size_t(p.piece) * 4);
+  p.chosen = cv.take(size_t(p.piece) * 4);
+  p.splits = 1;
+  if (train) {
+    p.z = cv.take(size_t(p.piece) * size_t(p.Vp) * 4);
+    p.dz = cv.take(size_t(p.planes) * size_t(p.piece) * size_t(p.Vp) * 2);
+    const int64_t tiles = ceil_div(p.piece, p.tile) * ceil_div(c->D, p.tile);
+    const int64_t steps = ceil_div(c->V, kStep) * (p.planes == 3 ? 6 : 1);
+    int64_t s = (p.big ? 256 : 512) / tiles;
+    if (s > steps / 8) s = steps / 8;
+    if (s > 32) s = 32;
+    p.splits = s < 1 ? 1 : int(s);
+    p.splits = int(ceil_div(steps, ceil_div(steps, p.splits)));
+    p.dh = cv.take(p.splits > 1 ? size_t(p.splits) * size_t(p.piece) * size_t(c->D) * 4 : 0);
+    p.dw = cv.take(p.pieces > 1 ? size_t(c->V) * size_t(c->D) * 4 : 0);
+  }
+  p.total = cv.at;
+  return p;
+}
+
+void finish(GemmArgs& g, int planes, int tile, int splits) {
+  g.planes = planes;
+  g.tiles_m = int(ceil_div(g.M, tile));
+  g.tiles_n = int(ceil_div(g.N, tile));
+  g.splits = splits;
+  g.steps = ceil_div(g.K, kStep) * (planes == 3 ? 6 : 1);
+}
+
+dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const void* weight, const void* targets,
+                  const float* row_weight, float* loss, float* lse, void* grad_hidden, void* grad_weight,
+                  char* ws, const Plan& p, hipStream_t stream) {
+  const size_t esz = c->io == DENDSN_IO_BF16 ? 2 : 4;
+  const int wide = c->index == DENDSN_INDEX_I64;
+  const size_t isz = wide ? 8 : 4;
+  const bool bf = c->io == DENDSN_IO_BF16;
+  Operand w{};
+  if (direct(c, weight, c->ld_weight)) {
+    w = Operand{static_cast<const uint16_t*>(weight), c->ld_weight, 0, 0, c->V, c->D};
+  } else {
+    PackArgs a{weight, reinterpret_cast<uint16_t*>(ws + p.w), nullptr, c->V, c->D, c->ld_weight, p.Dp, c->V * p.Dp, c->V, wide, p.planes};
+    if (bf) ce_pack_kernel<bf16_t><<<dim3(unsigned(c->V)), dim3(kThreads), 0, stream>>>(a);
+    else ce_pack_kernel<float><<<dim3(unsigned(c->V)), dim3(kThreads), 0, stream>>>(a);
+    w = Operand{a.dst, p.Dp, a.plane, kFinite * a.plane, c->V, p.Dp};
+  }
+  for (int64_t r0 = 0; r0 < c->N; r0 += p.piece) {
+    const int64_t M = c->N - r0 < p.piece ? c->N - r0 : p.piece;
+    const void* hp = static_cast<const char*>(hidden) + size_t(r0) * size_t(c->ld_hidden) * esz;
+    const void* tp = static_cast<const char*>(targets) + size_t(r0) * isz;
+    Operand h{};
+    if (!train && direct(c, hp, c->ld_hidden)) {
+      h = Operand{static_cast<const uint16_t*>(hp), c->ld_hidden, 0, 0, M, c->D};
+    } else {
+      PackArgs a{hp, reinterpret_cast<uint16_t*>(ws + p.h), tp, M, c->D, c->ld_hidden, p.Dp, M * p.Dp, c->V, wide, p.planes};
+      if (bf) ce_pack_kernel<bf16_t><<<dim3(unsigned(M)), dim3(kThreads), 0, stream>>>(a);
+      else ce_pack_kernel<float><<<dim3(unsigned(M)), dim3(kThreads), 0, stream>>>(a);
+      h = Operand{a.dst, p.Dp, a.plane, kFinite * a.plane, M, p.Dp};
+    }
+    LogitArgs l{};
+    l.g.x = h; l.g.y = w;
+    l.g.M = M; l.g.N = c->V; l.g.K = c->D;
+    finish(l.g, p.planes, p.tile, 1);
+    l.scale = c->logit_scale;
+    l.stats = reinterpret_cast<float2*>(ws + p.stats);
+    l.z = train ? reinterpret_cast<float*>(ws + p.z) : nullptr;
+    l.chosen = train ? nullptr : reinterpret_cast<float*>(ws + p.chosen);
+    l.targets = tp; l.ldz = p.Vp; l.wide = wide;
+    const dim3 lg(unsigned(int64_t(l.g.tiles_m) * l.g.tiles_n));
+    if (p.big) ce_logits_kernel<256, 256, 2, 4><<<lg, dim3(512), 0, stream>>>(l);
+    else ce_logits_kernel<128, 128, 2, 2><<<lg, dim3(256), 0, stream>>>(l);
+
+    LossArgs s{};
+    s.stats = l.stats; s.z = l.z; s.chosen = l.chosen; s.targets = tp;
+    s.loss = loss + r0;
+    float* own_lse = reinterpret_cast<float*>(ws + p.lse);
+    s.lse = lse ? lse + r0 : train ? own_lse : nullptr;
+    s.M = M; s.ldz = p.Vp; s.V = c->V; s.tiles = l.g.tiles_n; s.wide = wide;
+    ce_loss_kernel<<<dim3(unsigned(ceil_div(M, kThreads / 64))), dim3(kThreads), 0, stream>>>(s);
+    if (!train) continue;
+
+    DzArgs z{};
+    z.z = l.z; z.lse = s.lse; z.row_weight = row_weight ? row_weight + r0 : nullptr; z.targets = tp;
+    z.dz = reinterpret_cast<uint16_t*>(ws + p.dz);
+    z.ldz = p.Vp; z.plane = M * p.Vp; z.V = c->V; z.scale = c->logit_scale; z.wide = wide; z.planes = p.planes;
+    // rows along y: at most 2^15 a launch
+    for (int64_t y0 = 0; y0 < M; y0 += 32768) {
+      DzArgs q = z;
+      const int64_t rows = M - y0 < 32768 ? M - y0 : 32768;
+      q.z += y0 * p.Vp; q.lse += y0; q.dz += y0 * p.Vp;
+      if (q.row_weight) q.row_weight += y0;
+      q.targets = static_cast<const char*>(tp) + size_t(y0) * isz;
+      ce_dz_kernel<<<dim3(unsigned(ceil_div(p.Vp, 8 * kThreads)), unsigned(rows)), dim3(kThreads), 0, stream>>>(q);
+    }
+
+    GradArgs gh{};
+    gh.g.x = Operand{z.dz, p.Vp, z.plane, 0, M, p.Vp};
+    gh.g.y = w;
+    gh.g.M = M; gh.g.N = c->D; gh.g.K = c->V;
+    finish(gh.g, p.planes, p.tile, p.splits);
+    gh.out = static_cast<char*>(grad_hidden) + size_t(r0) * size_t(c->ld_grad_hidden) * esz;
+    gh.part = reinterpret_cast<float*>(ws + p.dh);
+    gh.targets = tp; gh.ld = c->ld_grad_hidden; gh.V = c->V; gh.wide = wide; gh.io = c->io;
+    const dim3 hg(unsigned(int64_t(gh.g.tiles_m) * gh.g.tiles_n), unsigned(p.splits));
+    if (p.big) ce_grad_kernel<256, 256, 2, 4, false><<<hg, dim3(512), 0, stream>>>(gh);
+    else ce_grad_kernel<128, 128, 2, 2, false><<<hg, dim3(256), 0, stream>>>(gh);
+    if (p.splits > 1) {
+      JoinArgs j{gh.part, gh.out, M, c->D, c->ld_grad_hidden, p.splits, c->io};
+      ce_join_splits_kernel<<<dim3(unsigned(M)), dim3(kThreads), 0, stream>>>(j);
+    }
+
+    GradArgs gw{};
+    gw.g.x = Operand{z.dz, p.Vp, z.plane, 0, M, p.Vp};
+    gw.g.y = h;
+    gw.g.M = c->V; gw.g.N = c->D; gw.g.K = M;
+    finish(gw.g, p.planes, p.tile, 1);
+    gw.out = grad_weight; gw.ld = c->ld_grad_weight; gw.io = c->io;
+    gw.part = reinterpret_cast<float*>(ws + p.dw);
+    gw.add = r0 > 0; gw.keep = r0 + M < c->N;
+    const dim3 wg(unsigned(int64_t(gw.g.tiles_m) * gw.g.tiles_n));
+    if (p.big) ce_grad_kernel<256, 256, 2, 4, true><<<wg, dim3(512), 0, stream>>>(gw);
+    else ce_grad_kernel<128, 128, 2, 2, true><<<wg, dim3(256), 0, stream>>>(gw);
+  }
+  return launched("linear cross entropy");
+}
+
+dendsn_status check_args(const dendsn_ce_cfg* c, const void* hidden, const void* weight, const void* targets,
+                         const float* loss, const float* lse) {
+  const size_t isz = c->index == DENDSN_INDEX_I64 ? 8 : 4, esz = c->io == DENDSN_IO_BF16 ? 2 : 4;
+  if (c->N > 0 && (!hidden || !targets || !loss)) return fail(DENDSN_E_INVALID, "hidden, targets or loss is NULL");
+  if (!weight) return fail(DENDSN_E_INVALID, "weight is NULL");
+  if (!aligned(hidden, esz) || !aligned(weight, esz) || !aligned(targets, isz) || !aligned(loss, 4) || !aligned(lse, 4))
+    return fail(DENDSN_E_INVALID, "hidden, weight, targets, loss or lse misaligned");
+  return DENDSN_OK;
+}
+
+}  // namespace
+}  // namespace dendsn_seq
+
+using namespace dendsn_seq;
+
+extern "C" {
+
+dendsn_status dendsn_ce_workspace_bytes(const dendsn_ce_cfg* cfg, int32_t train, size_t* bytes) {
+  clear_error();
+  const dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  if (!bytes) return fail(DENDSN_E_INVALID, "bytes is NULL");
+  *bytes = make_plan(cfg, train != 0).total;
+  return DENDSN_OK;
+}
+
+dendsn_status dendsn_ce_forward(const dendsn_ce_cfg* cfg, const void* hidden, const void* weight,
+                                const void* targets, float* loss, float* lse, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream) {
+  clear_error();
+  dendsn_status st = check_cfg(cfg);
+  if (st == DENDSN_OK) st = check_args(cfg, hidden, weight, targets, loss, lse);
+  if (st != DENDSN_OK) return st;
+  const Plan p = make_plan(cfg, false);
+  st = check_workspace(workspace, workspace_bytes, p.total, "dendsn_ce_workspace_bytes");
+  if (st != DENDSN_OK || cfg->N == 0) return st;
+  return run(cfg, false, hidden, weight, targets, nullptr, loss, lse, nullptr, nullptr, static_cast<char*>(workspace),
+             p, stream);
+}
+
+dendsn_status dendsn_ce_train(const dendsn_ce_cfg* cfg, const void* hidden, const void* weight,
+                              const void* targets, const float* row_weight, float* loss, float* lse,
+                              void* grad_hidden, void* grad_weight, void* workspace, size_t workspace_bytes,
+                              hipStream_t stream) {
+  clear_error();
+  dendsn_status st = check_cfg(cfg);
+  if (st == DENDSN_OK) st = check_args(cfg, hidden, weight, targets, loss, lse);
+  if (st != DENDSN_OK) return st;
+  const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
+  if ((cfg->N > 0 && !grad_hidden) || !grad_weight) return fail(DENDSN_E_INVALID, "grad_hidden or grad_weight is NULL");
+  if (!aligned(grad_hidden, esz) || !aligned(grad_weight, esz) || !aligned(row_weight, 4))
+    return fail(DENDSN_E_INVALID, "grad_hidden, grad_weight or row_weight misaligned");
+  const Plan p = make_plan(cfg, true);
+  st = check_workspace(workspace, workspace_bytes, p.total, "dendsn_ce_workspace_bytes");
+  if (st != DENDSN_OK) return st;
+  if (cfg->N == 0) {
+    const int64_t n = cfg->V * cfg->D;
+    ce_zero_kernel<<<dim3(unsigned(ceil_div(n, kThreads))), dim3(kThreads), 0, stream>>>(grad_weight, cfg->V, cfg->D, cfg->ld_grad_weight, cfg->io);
+    return launched("linear cross entropy");
+  }
+  return run(cfg, true, hidden, weight, targets, row_weight, loss, lse, grad_hidden, grad_weight,
+             static_cast<char*>(workspace), p, stream);
+}
+
+}  // extern "C"

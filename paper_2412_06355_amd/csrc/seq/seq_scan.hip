@@ -1,0 +1,654 @@
+// Gated leaky scan: forward, backward and one-token step.
+//
+//   a = sigmoid(g) or g,  w = 1 - a or 1,  h[t] = a[t] h[t-1] + w[t] x[t]
+//   lam[t] = dh[t] + c[t],  c[t-1] = a[t] lam[t],  c[T] = dh_last
+//   dx = w lam,  da = lam (h[t-1] - (leaky ? x : 0)),  dg = da a (1 - a) or da,  dh0 = c[0]
+//
+// Both recurrences are linear, so a run of steps acts on what enters it as
+// (A, B): out = A in + B, A the product of the run's a.  A block owns 64 lanes of
+// VEC channels of one sequence and walks its steps tile by tile; a tile is W waves
+// of L steps, each wave's run composed in registers, the waves' runs joined
+// through LDS (one barrier a tile), the state carried in registers.  Every input
+// is read once.  With few channels the steps are also split over S blocks: a first
+// kernel composes each block's run, and the scan starts from the runs before it.
+#include "seq_common.h"
+
+namespace dendsn_seq {
+namespace {
+
+constexpr int kW = 8;          // waves of a block
+constexpr int kL = 8;          // steps of a wave in a tile
+constexpr int kTile = kW * kL; // steps between checkpoints
+constexpr int kMaxSplit = 64;  // most blocks along the steps
+
+struct ScanArgs {
+  const void *x, *g, *gh;
+  const float *h0, *ckpt_in, *gh_last;
+  const int32_t* lengths;
+  void *h, *gx, *gg;
+  float *h_last, *ckpt, *gh0;
+  float2* runs;  // [S][batch][D] composed runs of the split
+  int64_t D, x_t, x_b, g_t, g_b, h_t, h_b, gh_t, gh_b, gx_t, gx_b, gg_t, gg_b;
+  int32_t T, batch, ntiles, per;  // per: tiles of a block of the split
+};
+
+// The decay and its complement, each with full relative accuracy.
+template <bool SIG>
+__device__ __forceinline__ void decay(float g, float& a, float& na) {
+  if (SIG) {
+    // e = exp(-|g|), in [0, 1]; the exponential instruction flushes results below 2^-126,
+    // which a gate's gradient would lose: there its argument is raised and the result lowered
+    const float y = -1.44269504f * fabsf(g);
+    const bool low = y < -126.0f;
+    const float e = __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(low ? y + 64.0f : y), low ? -64 : 0);
+    const float s = 1.0f + e;
+    float r = __builtin_amdgcn_rcpf(s);
+    r = fmaf(fmaf(-s, r, 1.0f), r, r);  // a long memory multiplies the decay's rounding
+    const float q = e * r;
+    a = g >= 0.0f ? r : q;
+    na = g >= 0.0f ? q : r;
+  } else {
+    a = g;
+    na = 1.0f - g;
+  }
+}
+
+template <typename IO, int VEC>
+__device__ __forceinline__ Pack<IO, VEC> load_row(const void* base, int64_t off) {
+  return *reinterpret_cast<const Pack<IO, VEC>*>(static_cast<const IO*>(base) + off);
+}
+
+__device__ __forceinline__ int seq_length(const ScanArgs& p, int b) {
+  if (!p.lengths) return p.T;
+  return max(0, min(p.T, p.lengths[b]));
+}
+
+// Composes the run of one block of the split: (A, B) over its steps, forward
+// (u = w x) or backward (c[t-1] = a[t] (dh[t] + c[t])).
+template <typename IO, int VEC, bool SIG, bool LEAKY, bool BWD>
+__global__ void __launch_bounds__(kW * 64) scan_runs_kernel(ScanArgs p) {
+  __shared__ float2 sh[kW][64 * VEC];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int b = blockIdx.y;
+  const int seg = BWD ? int(blockIdx.z) + 1 : int(blockIdx.z);  // the first (last) block's run feeds nobody
+  const int64_t d0 = (int64_t(blockIdx.x) * 64 + lane) * VEC;
+  const bool on = d0 < p.D;
+  const int64_t d = on ? d0 : 0;
+  const int len = seq_length(p, b);
+  const int lo = seg * p.per * kTile, hi = min(min(lo + p.per * kTile, p.T), len);
+  // wave w composes the steps [s0, s1)
+  const int each = p.per * kL;
+  const int s0 = lo + w * each, s1 = min(s0 + each, hi);
+  const int64_t xb = b * (BWD ? p.gh_b : p.x_b) + d, gb = b * p.g_b + d;
+  const void* xs = BWD ? p.gh : p.x;
+  const int64_t xt = BWD ? p.gh_t : p.x_t;
+  float A[VEC], B[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) A[v] = 1.0f, B[v] = 0.0f;
+  const int n = s1 - s0;
+  for (int j0 = 0; j0 < n; j0 += kL) {
+    Pack<IO, VEC> rx[kL], rg[kL];
+#pragma unroll
+    for (int j = 0; j < kL; ++j) {
+      const int i = min(j0 + j, n - 1);
+      const int64_t t = BWD ? s1 - 1 - i : s0 + i;
+      rx[j] = load_row<IO, VEC>(xs, t * xt + xb);
+      rg[j] = load_row<IO, VEC>(p.g, t * p.g_t + gb);
+    }
+#pragma unroll
+    for (int j = 0; j < kL; ++j) {
+      if (j0 + j < n) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          float a, na;
+          decay<SIG>(widen(rg[j].v[v]), a, na);
+          const float xv = widen(rx[j].v[v]);
+          if (BWD)
+            B[v] = a * (xv + B[v]);
+          else
+            B[v] = fmaf(a, B[v], LEAKY ? na * xv : xv);
+          A[v] *= a;
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) sh[w][v * 64 + lane] = make_float2(A[v], B[v]);
+  __syncthreads();
+  if (w == 0 && on) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      float2 c = sh[BWD ? kW - 1 : 0][v * 64 + lane];
+      for (int k = 1; k < kW; ++k) {
+        const float2 r = sh[BWD ? kW - 1 - k : k][v * 64 + lane];
+        c = make_float2(r.x * c.x, fmaf(r.x, c.y, r.y));
+      }
+      p.runs[(int64_t(seg) * p.batch + b) * p.D + d + v] = c;
+    }
+  }
+}
+
+template <typename IO, int VEC, bool SIG, bool LEAKY>
+__global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
+  __shared__ float2 sh[2][kW][64 * VEC];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int b = blockIdx.y, seg = blockIdx.z;
+  const int64_t d0 = (int64_t(blockIdx.x) * 64 + lane) * VEC;
+  const bool on = d0 < p.D;
+  const int64_t d = on ? d0 : 0;
+  const int len = seq_length(p, b);
+  const int64_t xb = b * p.x_b + d, gb = b * p.g_b + d, hb = b * p.h_b + d;
+  const int64_t bd = int64_t(b) * p.D + d, lanes = int64_t(p.batch) * p.D;
+
+  float carry[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) carry[v] = p.h0 ? p.h0[bd + v] : 0.0f;
+  for (int s = 0; s < seg; ++s) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      const float2 r = p.runs[s * lanes + bd + v];
+      carry[v] = fmaf(r.x, carry[v], r.y);
+    }
+  }
+
+  const int k1 = min((seg + 1) * p.per, p.ntiles);
+  Pack<IO, VEC> rx[kL], rg[kL];
+  auto fetch = [&](int k) {  // rows past the end read the last row again
+    const int t0 = k * kTile + w * kL;
+    if (t0 < len) {
+#pragma unroll
+      for (int j = 0; j < kL; ++j) {
+        const int64_t t = min(t0 + j, p.T - 1);
+        rx[j] = load_row<IO, VEC>(p.x, t * p.x_t + xb);
+        rg[j] = load_row<IO, VEC>(p.g, t * p.g_t + gb);
+      }
+    }
+  };
+  fetch(seg * p.per);
+  for (int k = seg * p.per; k < k1; ++k) {
+    const int t0 = k * kTile + w * kL;
+    float P[kL][VEC], H[kL][VEC];  // the run of the wave's first j + 1 steps
+#pragma unroll
+    for (int j = 0; j < kL; ++j) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float pp = j ? P[j - 1][v] : 1.0f, hp = j ? H[j - 1][v] : 0.0f;
+        P[j][v] = pp;
+        H[j][v] = hp;
+        if (t0 + j < len) {
+          float a, na;
+          decay<SIG>(widen(rg[j].v[v]), a, na);
+          const float xv = widen(rx[j].v[v]);
+          P[j][v] = pp * a;
+          H[j][v] = fmaf(a, hp, LEAKY ? na * xv : xv);
+        }
+      }
+    }
+    if (k + 1 < k1) fetch(k + 1);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) sh[k & 1][w][v * 64 + lane] = make_float2(P[kL - 1][v], H[kL - 1][v]);
+    __syncthreads();
+    float in[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      if (w == 0 && on && p.ckpt) p.ckpt[int64_t(k) * lanes + bd + v] = carry[v];
+      in[v] = carry[v];
+#pragma unroll
+      for (int q = 0; q < kW; ++q) {
+        const float2 r = sh[k & 1][q][v * 64 + lane];
+        if (q == w) in[v] = carry[v];
+        carry[v] = fmaf(r.x, carry[v], r.y);
+      }
+    }
+    if (on) {
+#pragma unroll
+      for (int j = 0; j < kL; ++j) {
+        const int t = t0 + j;
+        if (t < p.T) {
+          Pack<IO, VEC> o;
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) o.v[v] = narrow<IO>(t < len ? fmaf(P[j][v], in[v], H[j][v]) : 0.0f);
+          *reinterpret_cast<Pack<IO, VEC>*>(static_cast<IO*>(p.h) + t * p.h_t + hb) = o;
+        }
+      }
+    }
+  }
+  if (w == 0 && on && p.h_last && k1 == p.ntiles && seg * p.per < k1) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) p.h_last[bd + v] = carry[v];
+  }
+}
+
+template <typename IO, int VEC, bool SIG, bool LEAKY>
+__global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
+  __shared__ float shA[2][kW][64 * VEC], shH[2][kW][64 * VEC], shC[2][kW][64 * VEC];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int b = blockIdx.y, seg = blockIdx.z;
+  const int64_t d0 = (int64_t(blockIdx.x) * 64 + lane) * VEC;
+  const bool on = d0 < p.D;
+  const int64_t d = on ? d0 : 0;
+  const int len = seq_length(p, b);
+  const int64_t xb = b * p.x_b + d, gb = b * p.g_b + d, ghb = b * p.gh_b + d;
+  const int64_t gxb = b * p.gx_b + d, ggb = b * p.gg_b + d;
+  const int64_t bd = int64_t(b) * p.D + d, lanes = int64_t(p.batch) * p.D;
+
+  float carry[VEC];  // c of the tile's last step
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) carry[v] = p.gh_last ? p.gh_last[bd + v] : 0.0f;
+  for (int s = gridDim.z - 1; s > seg; --s) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      const float2 r = p.runs[s * lanes + bd + v];
+      carry[v] = fmaf(r.x, carry[v], r.y);
+    }
+  }
+
+  const int k0 = seg * p.per, k1 = min(k0 + p.per, p.ntiles);
+  Pack<IO, VEC> rx[kL], rg[kL], rh[kL];
+  float start[VEC];
+  auto fetch = [&](int k) {
+    const int t0 = k * kTile + w * kL;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) start[v] = p.ckpt_in[int64_t(k) * lanes + bd + v];
+    if (t0 < len) {
+#pragma unroll
+      for (int j = 0; j < kL; ++j) {
+        const int64_t t = min(t0 + j, p.T - 1);
+        rx[j] = load_row<IO, VEC>(p.x, t * p.x_t + xb);
+        rg[j] = load_row<IO, VEC>(p.g, t * p.g_t + gb);
+        rh[j] = load_row<IO, VEC>(p.gh, t * p.gh_t + ghb);
+      }
+    }
+  };
+  if (k0 < k1) fetch(k1 - 1);
+  for (int k = k1 - 1; k >= k0; --k) {
+    const int t0 = k * kTile + w * kL;
+    float a[kL][VEC], na[kL][VEC], x[kL][VEC], dh[kL][VEC];
+    float A[VEC], H[VEC], C[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) A[v] = 1.0f, H[v] = 0.0f, C[v] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kL; ++j) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        a[j][v] = 1.0f;
+        na[j][v] = x[j][v] = dh[j][v] = 0.0f;
+        if (t0 + j < len) {
+          decay<SIG>(widen(rg[j].v[v]), a[j][v], na[j][v]);
+          x[j][v] = widen(rx[j].v[v]);
+          dh[j][v] = widen(rh[j].v[v]);
+        }
+        A[v] *= a[j][v];
+        H[v] = fmaf(a[j][v], H[v], LEAKY ? na[j][v] * x[j][v] : x[j][v]);
+      }
+    }
+#pragma unroll
+    for (int j = kL - 1; j >= 0; --j) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) C[v] = a[j][v] * (dh[j][v] + C[v]);
+    }
+    const int buf = k & 1;
+    float hin[VEC], cin[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      hin[v] = start[v];
+      shA[buf][w][v * 64 + lane] = A[v];
+      shH[buf][w][v * 64 + lane] = H[v];
+      shC[buf][w][v * 64 + lane] = C[v];
+    }
+    if (k > k0) fetch(k - 1);
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+#pragma unroll
+      for (int q = 0; q < kW - 1; ++q)
+        if (q < w) hin[v] = fmaf(shA[buf][q][v * 64 + lane], hin[v], shH[buf][q][v * 64 + lane]);
+      cin[v] = carry[v];
+#pragma unroll
+      for (int q = kW - 1; q >= 0; --q) {
+        if (q == w) cin[v] = carry[v];
+        carry[v] = fmaf(shA[buf][q][v * 64 + lane], carry[v], shC[buf][q][v * 64 + lane]);
+      }
+    }
+    float before[kL][VEC];
+#pragma unroll
+    for (int j = 0; j < kL; ++j) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        before[j][v] = hin[v];
+        hin[v] = fmaf(a[j][v], hin[v], LEAKY ? na[j][v] * x[j][v] : x[j][v]);
+      }
+    }
+#pragma unroll
+    for (int j = kL - 1; j >= 0; --j) {
+      const int t = t0 + j;
+      Pack<IO, VEC> ox, og;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        const float lam = dh[j][v] + cin[v];
+        cin[v] = a[j][v] * lam;
+        float da = lam * (LEAKY ? before[j][v] - x[j][v] : before[j][v]);
+        if (SIG) da *= a[j][v] * na[j][v];
+        ox.v[v] = narrow<IO>(t < len ? (LEAKY ? na[j][v] * lam : lam) : 0.0f);
+        og.v[v] = narrow<IO>(t < len ? da : 0.0f);
+      }
+      if (on && t < p.T) {
+        *reinterpret_cast<Pack<IO, VEC>*>(static_cast<IO*>(p.gx) + t * p.gx_t + gxb) = ox;
+        *reinterpret_cast<Pack<IO, VEC>*>(static_cast<IO*>(p.gg) + t * p.gg_t + ggb) = og;
+      }
+    }
+  }
+  if (w == 0 && on && p.gh0 && seg == 0) {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) p.gh0[bd + v] = carry[v];
+  }
+}
+
+struct StepArgs {
+  const void *x, *g;
+  const int32_t* slots;
+  float* state;
+  void* h;
+  int64_t D, x_b, g_b, h_b, n_slots;
+};
+
+// One token of each request: VEC channels a thread, the state read and written
+// where it lies.
+template <typename IO, int VEC, bool SIG, bool LEAKY>
+__global__ void __launch_bounds__(256) scan_step_kernel(StepArgs p) {
+  const int64_t d = (int64_t(blockIdx.x) * 256 + threadIdx.x) * VEC;
+  const int b = blockIdx.y;
+  if (d >= p.D) return;
+  const int64_t slot = p.slots ? int64_t(p.slots[b]) : b;
+  const bool live = slot >= 0 && slot < p.n_slots;
+  Pack<IO, VEC> o;
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) o.v[v] = narrow<IO>(0.0f);
+  if (live) {
+    const Pack<IO, VEC> rx = load_row<IO, VEC>(p.x, b * p.x_b + d), rg = load_row<IO, VEC>(p.g, b * p.g_b + d);
+    auto* st = reinterpret_cast<Pack<float, VEC>*>(p.state + slot * p.D + d);
+    Pack<float, VEC> s = *st;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      float a, na;
+      decay<SIG>(widen(rg.v[v]), a, na);
+      const float xv = widen(rx.v[v]);
+      s.v[v] = fmaf(a, s.v[v], LEAKY ? na * xv : xv);
+      o.v[v] = narrow<IO>(s.v[v]);
+    }
+    *st = s;
+  }
+  *reinterpret_cast<Pack<IO, VEC>*>(static_cast<IO*>(p.h) + b * p.h_b + d) = o;
+}
+
+// T = 0: the state passes through.
+__global__ void __launch_bounds__(256) scan_copy_kernel(const float* from, float* to, int64_t n) {
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (i < n) to[i] = from ? from[i] : 0.0f;
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+bool rows_apart(const dendsn_scan_cfg* c, int64_t st, int64_t sb) {
+  // every two rows of [T, batch] are at least D apart
+  if (c->T > 1 && st < c->D) return false;
+  if (c->batch > 1 && sb < c->D) return false;
+  if (c->T <= 1 || c->batch <= 1) return true;
+  return st >= (c->batch - 1) * sb + c->D || sb >= (c->T - 1) * st + c->D;
+}
+
+bool strides_fit(const dendsn_scan_cfg* c, int64_t st, int64_t sb) {
+  return st >= 0 && sb >= 0 && st <= kMaxElems && sb <= kMaxElems && small_product(c->T, st) &&
+         small_product(c->batch, sb);
+}
+
+bool empty(const dendsn_scan_cfg* c) { return c->T == 0 || c->batch == 0 || c->D == 0; }
+
+dendsn_status check_cfg(const dendsn_scan_cfg* c) {
+  if (!c) return fail(DENDSN_E_INVALID, "cfg is NULL");
+  if (c->T < 0 || c->T > (int64_t(1) << 30)) return fail(DENDSN_E_INVALID, "T must be in [0, 2^30]");
+  if (c->batch < 0 || c->batch > 65535) return fail(DENDSN_E_INVALID, "batch must be in [0, 65535]");
+  // a launch has fewer than 2^32 threads along the channels: eight of them each
+  if (c->D < 0 || c->D > (int64_t(1) << 27)) return fail(DENDSN_E_INVALID, "D must be in [0, 2^27]");
+  if (c->io != DENDSN_IO_F32 && c->io != DENDSN_IO_BF16) return fail(DENDSN_E_INVALID, "bad io");
+  if (c->gate != DENDSN_GATE_SIGMOID && c->gate != DENDSN_GATE_DECAY) return fail(DENDSN_E_INVALID, "bad gate");
+  if (c->leaky != 0 && c->leaky != 1) return fail(DENDSN_E_INVALID, "leaky must be 0 or 1");
+  if (!small_product(c->batch * c->D, c->T)) return fail(DENDSN_E_INVALID, "T * batch * D too large");
+  const int64_t s[12] = {c->x_t, c->x_b, c->g_t, c->g_b, c->h_t, c->h_b, c->grad_h_t, c->grad_h_b,
+                         c->grad_x_t, c->grad_x_b, c->grad_g_t, c->grad_g_b};
+  for (int i = 0; i < 12; i += 2)
+    if (!strides_fit(c, s[i], s[i + 1])) return fail(DENDSN_E_INVALID, "a stride is negative or too large");
+  return DENDSN_OK;
+}
+
+struct Plan {
+  int vec;
+  int64_t groups;  // blocks along the channels
+  int ntiles, per, S;
+};
+
+// Lanes of two channels where every row allows it (4 or 8 bytes a lane).  The
+// steps are split while the chip is not full: kFill blocks of eight waves.
+constexpr int64_t kFill = 1024;
+
+Plan make_plan(const dendsn_scan_cfg* c, bool wide) {
+  Plan p;
+  p.vec = wide ? 2 : 1;
+  p.groups = ceil_div(c->D, 64 * p.vec);
+  p.ntiles = int(ceil_div(c->T, kTile));
+  const int64_t blocks = p.groups * c->batch;
+  int64_t S = blocks >= kFill / 2 ? 1 : ceil_div(kFill, blocks);
+  S = S < kMaxSplit ? S : kMaxSplit;
+  // a block of the split has two tiles at least
+  S = S < p.ntiles / 2 ? S : p.ntiles / 2;
+  if (S < 1) S = 1;
+  p.per = int(ceil_div(p.ntiles, S));
+  p.S = int(ceil_div(p.ntiles, p.per));
+  return p;
+}
+
+// The split of narrow lanes is never finer than that of wide ones, whose blocks
+// are half as many: the scratch is sized for the most blocks.
+size_t runs_bytes(const dendsn_scan_cfg* c) {
+  const Plan a = make_plan(c, false), b = make_plan(c, true);
+  const int S = a.S > b.S ? a.S : b.S;
+  return S > 1 ? size_t(S) * size_t(c->batch) * size_t(c->D) * sizeof(float2) : 0;
+}
+
+size_t ckpt_bytes(const dendsn_scan_cfg* c) {
+  return empty(c) ? 0 : size_t(ceil_div(c->T, kTile)) * size_t(c->batch) * size_t(c->D) * sizeof(float);
+}
+
+template <typename F>
+void dispatch(const dendsn_scan_cfg* c, bool wide, F&& f) {
+  auto flags = [&](auto io, auto vec) {
+    using IO = decltype(io);
+    constexpr int V = decltype(vec)::value;
+    if (c->gate == DENDSN_GATE_SIGMOID) {
+      if (c->leaky) f.template operator()<IO, V, true, true>();
+      else f.template operator()<IO, V, true, false>();
+    } else {
+      if (c->leaky) f.template operator()<IO, V, false, true>();
+      else f.template operator()<IO, V, false, false>();
+    }
+  };
+  auto width = [&](auto io) {
+    if (wide) flags(io, std::integral_constant<int, 2>{});
+    else flags(io, std::integral_constant<int, 1>{});
+  };
+  if (c->io == DENDSN_IO_BF16) width(bf16_t{});
+  else width(float{});
+}
+
+struct LaunchFwd {
+  ScanArgs a;
+  Plan p;
+  hipStream_t stream;
+  template <typename IO, int V, bool SIG, bool LEAKY>
+  void operator()() const {
+    const dim3 block(kW * 64);
+    if (p.S > 1)
+      scan_runs_kernel<IO, V, SIG, LEAKY, false><<<dim3(unsigned(p.groups), a.batch, p.S - 1), block, 0, stream>>>(a);
+    scan_fwd_kernel<IO, V, SIG, LEAKY><<<dim3(unsigned(p.groups), a.batch, p.S), block, 0, stream>>>(a);
+  }
+};
+
+struct LaunchBwd {
+  ScanArgs a;
+  Plan p;
+  hipStream_t stream;
+  template <typename IO, int V, bool SIG, bool LEAKY>
+  void operator()() const {
+    const dim3 block(kW * 64);
+    if (p.S > 1)
+      scan_runs_kernel<IO, V, SIG, LEAKY, true><<<dim3(unsigned(p.groups), a.batch, p.S - 1), block, 0, stream>>>(a);
+    scan_bwd_kernel<IO, V, SIG, LEAKY><<<dim3(unsigned(p.groups), a.batch, p.S), block, 0, stream>>>(a);
+  }
+};
+
+struct LaunchStep {
+  StepArgs a;
+  int64_t batch;
+  hipStream_t stream;
+  template <typename IO, int V, bool SIG, bool LEAKY>
+  void operator()() const {
+    scan_step_kernel<IO, V, SIG, LEAKY>
+        <<<dim3(unsigned(ceil_div(a.D, 256 * V)), unsigned(batch)), dim3(256), 0, stream>>>(a);
+  }
+};
+
+bool even(int64_t a, int64_t b) { return a % 2 == 0 && b % 2 == 0; }
+
+}  // namespace
+}  // namespace dendsn_seq
+
+using namespace dendsn_seq;
+
+extern "C" {
+
+dendsn_status dendsn_scan_ckpt_bytes(const dendsn_scan_cfg* cfg, size_t* bytes) {
+  clear_error();
+  const dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  if (!bytes) return fail(DENDSN_E_INVALID, "bytes is NULL");
+  *bytes = ckpt_bytes(cfg);
+  return DENDSN_OK;
+}
+
+dendsn_status dendsn_scan_workspace_bytes(const dendsn_scan_cfg* cfg, int32_t backward, size_t* bytes) {
+  clear_error();
+  const dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  if (!bytes) return fail(DENDSN_E_INVALID, "bytes is NULL");
+  (void)backward;  // both directions split alike
+  *bytes = empty(cfg) ? 0 : runs_bytes(cfg);
+  return DENDSN_OK;
+}
+
+dendsn_status dendsn_scan_forward(const dendsn_scan_cfg* cfg, const void* x, const void* g, const float* h0,
+                                  const int32_t* lengths, void* h, float* h_last, float* ckpt, void* workspace,
+                                  size_t workspace_bytes, hipStream_t stream) {
+  clear_error();
+  dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  const bool none = empty(cfg);
+  const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
+  if (!none && (!x || !g || !h)) return fail(DENDSN_E_INVALID, "x, g or h is NULL");
+  if (!aligned(x, esz) || !aligned(g, esz) || !aligned(h, esz)) return fail(DENDSN_E_INVALID, "x, g or h misaligned");
+  if (!aligned(h0, 4) || !aligned(lengths, 4) || !aligned(h_last, 4))
+    return fail(DENDSN_E_INVALID, "h0, lengths or h_last misaligned");
+  if (!aligned(ckpt, 16)) return fail(DENDSN_E_INVALID, "ckpt must be 16-byte aligned");
+  if (!none && !rows_apart(cfg, cfg->h_t, cfg->h_b)) return fail(DENDSN_E_INVALID, "rows of h overlap");
+  if (none) {
+    const int64_t lanes = cfg->batch * cfg->D;
+    if (h_last && lanes) {
+      scan_copy_kernel<<<dim3(unsigned(ceil_div(lanes, 256))), dim3(256), 0, stream>>>(h0, h_last, lanes);
+      return launched("scan forward");
+    }
+    return DENDSN_OK;
+  }
+  st = check_workspace(workspace, workspace_bytes, runs_bytes(cfg), "dendsn_scan_workspace_bytes");
+  if (st != DENDSN_OK) return st;
+  const bool wide = cfg->D % 2 == 0 && aligned(x, 2 * esz) && aligned(g, 2 * esz) && aligned(h, 2 * esz) &&
+                    even(cfg->x_t, cfg->x_b) && even(cfg->g_t, cfg->g_b) && even(cfg->h_t, cfg->h_b);
+  LaunchFwd f{{}, make_plan(cfg, wide), stream};
+  ScanArgs& a = f.a;
+  a.x = x; a.g = g; a.h0 = h0; a.lengths = lengths; a.h = h; a.h_last = h_last; a.ckpt = ckpt;
+  a.runs = static_cast<float2*>(workspace);
+  a.D = cfg->D; a.T = int32_t(cfg->T); a.batch = int32_t(cfg->batch); a.ntiles = f.p.ntiles; a.per = f.p.per;
+  a.x_t = cfg->x_t; a.x_b = cfg->x_b; a.g_t = cfg->g_t; a.g_b = cfg->g_b; a.h_t = cfg->h_t; a.h_b = cfg->h_b;
+  dispatch(cfg, wide, f);
+  return launched("scan forward");
+}
+
+dendsn_status dendsn_scan_backward(const dendsn_scan_cfg* cfg, const void* x, const void* g,
+                                   const int32_t* lengths, const float* ckpt, const void* grad_h,
+                                   const float* grad_h_last, void* grad_x, void* grad_g, float* grad_h0,
+                                   void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  clear_error();
+  dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  const bool none = empty(cfg);
+  const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
+  if (!none && (!x || !g || !grad_h || !grad_x || !grad_g))
+    return fail(DENDSN_E_INVALID, "x, g, grad_h, grad_x or grad_g is NULL");
+  if (!none && !ckpt) return fail(DENDSN_E_INVALID, "ckpt is NULL");
+  if (!aligned(x, esz) || !aligned(g, esz) || !aligned(grad_h, esz) || !aligned(grad_x, esz) || !aligned(grad_g, esz))
+    return fail(DENDSN_E_INVALID, "x, g, grad_h, grad_x or grad_g misaligned");
+  if (!aligned(grad_h_last, 4) || !aligned(lengths, 4) || !aligned(grad_h0, 4))
+    return fail(DENDSN_E_INVALID, "grad_h_last, lengths or grad_h0 misaligned");
+  if (!aligned(ckpt, 16)) return fail(DENDSN_E_INVALID, "ckpt must be 16-byte aligned");
+  if (!none && (!rows_apart(cfg, cfg->grad_x_t, cfg->grad_x_b) || !rows_apart(cfg, cfg->grad_g_t, cfg->grad_g_b)))
+    return fail(DENDSN_E_INVALID, "rows of grad_x or of grad_g overlap");
+  if (none) {
+    const int64_t lanes = cfg->batch * cfg->D;
+    if (grad_h0 && lanes) {
+      scan_copy_kernel<<<dim3(unsigned(ceil_div(lanes, 256))), dim3(256), 0, stream>>>(grad_h_last, grad_h0, lanes);
+      return launched("scan backward");
+    }
+    return DENDSN_OK;
+  }
+  st = check_workspace(workspace, workspace_bytes, runs_bytes(cfg), "dendsn_scan_workspace_bytes");
+  if (st != DENDSN_OK) return st;
+  const bool wide = cfg->D % 2 == 0 && aligned(x, 2 * esz) && aligned(g, 2 * esz) && aligned(grad_h, 2 * esz) &&
+                    aligned(grad_x, 2 * esz) && aligned(grad_g, 2 * esz) && even(cfg->x_t, cfg->x_b) &&
+                    even(cfg->g_t, cfg->g_b) && even(cfg->grad_h_t, cfg->grad_h_b) &&
+                    even(cfg->grad_x_t, cfg->grad_x_b) && even(cfg->grad_g_t, cfg->grad_g_b);
+  LaunchBwd f{{}, make_plan(cfg, wide), stream};
+  ScanArgs& a = f.a;
+  a.x = x; a.g = g; a.gh = grad_h; a.lengths = lengths; a.ckpt_in = ckpt; a.gh_last = grad_h_last;
+  a.gx = grad_x; a.gg = grad_g; a.gh0 = grad_h0;
+  a.runs = static_cast<float2*>(workspace);
+  a.D = cfg->D; a.T = int32_t(cfg->T); a.batch = int32_t(cfg->batch); a.ntiles = f.p.ntiles; a.per = f.p.per;
+  a.x_t = cfg->x_t; a.x_b = cfg->x_b; a.g_t = cfg->g_t; a.g_b = cfg->g_b;
+  a.gh_t = cfg->grad_h_t; a.gh_b = cfg->grad_h_b; a.gx_t = cfg->grad_x_t; a.gx_b = cfg->grad_x_b;
+  a.gg_t = cfg->grad_g_t; a.gg_b = cfg->grad_g_b;
+  dispatch(cfg, wide, f);
+  return launched("scan backward");
+}
+
+dendsn_status dendsn_scan_step(const dendsn_scan_cfg* cfg, const void* x, const void* g, int64_t n_slots,
+                               const int32_t* slots, float* state, void* h, hipStream_t stream) {
+  clear_error();
+  dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  if (cfg->T != 1) return fail(DENDSN_E_INVALID, "T must be 1");
+  const bool none = empty(cfg);
+  const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
+  if (n_slots < 0 || !small_product(n_slots, cfg->D)) return fail(DENDSN_E_INVALID, "n_slots negative or too large");
+  if (!slots && n_slots < cfg->batch) return fail(DENDSN_E_INVALID, "without slots, n_slots must be >= batch");
+  if (!none && (!x || !g || !h)) return fail(DENDSN_E_INVALID, "x, g or h is NULL");
+  if (!none && n_slots > 0 && !state) return fail(DENDSN_E_INVALID, "state is NULL");
+  if (!aligned(x, esz) || !aligned(g, esz) || !aligned(h, esz)) return fail(DENDSN_E_INVALID, "x, g or h misaligned");
+  if (!aligned(slots, 4) || !aligned(state, 4)) return fail(DENDSN_E_INVALID, "slots or state misaligned");
+  if (!none && !rows_apart(cfg, cfg->h_t, cfg->h_b)) return fail(DENDSN_E_INVALID, "rows of h overlap");
+  if (none) return DENDSN_OK;
+  const bool wide = cfg->D % 2 == 0 && aligned(x, 2 * esz) && aligned(g, 2 * esz) && aligned(h, 2 * esz) &&
+                    aligned(state, 8) && cfg->x_b % 2 == 0 && cfg->g_b % 2 == 0 && cfg->h_b % 2 == 0;
+  LaunchStep f{{x, g, slots, state, h, cfg->D, cfg->x_b, cfg->g_b, cfg->h_b, n_slots}, cfg->batch, stream};
+  dispatch(cfg, wide, f);
+  return launched("scan step");
+}
+
+}  // extern "C"

@@ -1,0 +1,210 @@
+"""Linear cross entropy on the GPU against float64."""
+
+import pytest
+import torch
+
+import paper_2412_06355_amd as dendsn
+from tests import seq_ref
+from tests.parity import announce
+
+pytestmark = pytest.mark.gpu
+
+
+def make(N, V, D, io, dev, seed=0, ignored=0.2, index=torch.int64, spread=2.0):
+    gen = torch.Generator(device=dev).manual_seed(seed)
+    dt = seq_ref.io_dtype(io)
+    n = lambda *s: torch.randn(s, generator=gen, device=dev)
+    hidden, weight = n(N, D).to(dt), (spread * D ** -0.5 * n(V, D)).to(dt)
+    targets = torch.randint(0, V, (N,), generator=gen, device=dev)
+    gone = torch.rand((N,), generator=gen, device=dev) < ignored
+    targets = torch.where(gone, torch.where(targets % 2 == 0, -100, V), targets).to(index)
+    return hidden, weight, targets, torch.rand((N,), generator=gen, device=dev)
+
+
+def check(cfg, hidden, weight, targets, row_weight):
+    ref = seq_ref.ce(hidden, weight, targets, cfg.logit_scale, cfg.io, row_weight)
+    norms = ref.pop("norms")
+    loss, lse = dendsn.linear_ce(cfg, hidden, weight, targets)
+    got = dendsn.linear_ce_train(cfg, hidden, weight, targets, row_weight)
+    again = dendsn.linear_ce_train(cfg, hidden, weight, targets, row_weight)
+    seq_ref.assert_within(loss, *ref["loss"], "loss alone")
+    seq_ref.assert_within(lse, *ref["lse"], "lse alone")
+    for k, (value, bound) in ref.items():
+        seq_ref.assert_within(got[k], value, bound, k)
+        assert torch.equal(got[k].view(torch.uint8), again[k].view(torch.uint8)), k
+    for k, most in norms.items():
+        value = ref[k][0]
+        # (beside the storage roundings of ``most``, fp32 sums: of the result's own size)
+        off = float((got[k].double() - value).norm())
+        extra = seq_ref.U * (cfg.D + 64) * float(value.norm()) + seq_ref.TINY
+        assert off <= most + extra, (k, off, most)
+    return got
+
+
+# rows, classes and features around tiles of 128 and 256, stages of 64 and chunks of 8
+SHAPES = [(1, 1, 1), (1, 2, 64), (2, 63, 8), (3, 64, 7), (15, 65, 65), (16, 129, 32), (17, 257, 64), (127, 1000, 128),
+          (129, 500, 96), (300, 1003, 72), (257, 130, 200), (64, 5003, 264), (511, 2000, 100), (200, 3001, 513)]
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V,D", SHAPES)
+def test_against_definition(gpu_device, N, V, D, io):
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io, logit_scale=1.0 if N % 2 else 0.7)
+    cfg = cfg.with_(logit_scale=float(torch.tensor(cfg.logit_scale, dtype=torch.float32)))
+    index = torch.int32 if V % 2 else torch.int64
+    announce(f"ce {cfg} {index}")
+    check(cfg, *make(N, V, D, io, gpu_device, N + V, index=index))
+
+
+@pytest.mark.parametrize("N,V,D,io", [(2048, 9000, 256, "bf16"), (1100, 17000, 520, "bf16"), (4099, 4100, 64, "bf16"),
+                                      (1024, 20000, 128, "f32")])
+def test_large_tiles(gpu_device, N, V, D, io):
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    announce(f"ce {cfg}")
+    check(cfg, *make(N, V, D, io, gpu_device, N))
+
+
+def test_pieces_of_rows(gpu_device):
+    """More rows than the scratch holds logits of: the pieces' gradients of the weights add up."""
+    N, V, D = 6000, 131072, 16
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io="bf16")
+    one = dendsn.dendsn_ce_workspace_bytes(cfg.with_(N=2000), True)
+    assert dendsn.dendsn_ce_workspace_bytes(cfg, True) < 3 * one   # fewer rows than 6000 at a time
+    announce(f"ce pieces {cfg}")
+    check(cfg, *make(N, V, D, "bf16", gpu_device, 4))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_row_weights(gpu_device, io):
+    """No weights are weights of one; rows of weight zero have no gradient; signs count."""
+    cfg = dendsn.LinearCEConfig(N=70, V=300, D=48, io=io)
+    h, w, t, _ = make(70, 300, 48, io, gpu_device, 1)
+    announce(f"ce row weights {cfg}")
+    a = dendsn.linear_ce_train(cfg, h, w, t)
+    b = dendsn.linear_ce_train(cfg, h, w, t, torch.ones(70, device=gpu_device))
+    for k in a:
+        assert torch.equal(a[k], b[k]), k
+    r = torch.linspace(-1, 1, 70, device=gpu_device)
+    r[::3] = 0.0
+    got = check(cfg, h, w, t, r)
+    assert not got["grad_hidden"][::3].any()
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_ignored_rows_hold_anything(gpu_device, io):
+    """Rows without a target: NaN and infinities in them reach nothing; a batch of only such
+    rows has zero loss and +0 gradients."""
+    N, V, D = 140, 333, 40
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    h, w, t, r = make(N, V, D, io, gpu_device, 7, ignored=0.4)
+    announce(f"ce ignored rows {cfg}")
+    want = check(cfg, h, w, t, r)
+    gone = (t < 0) | (t >= V)
+    for bad in (float("nan"), float("inf"), torch.finfo(h.dtype).min):
+        hb, rb = h.clone(), r.clone()
+        hb[gone] = bad
+        rb[gone] = bad
+        got = dendsn.linear_ce_train(cfg, hb, w, t, rb)
+        loss, lse = dendsn.linear_ce(cfg, hb, w, t)
+        for k in want:
+            assert torch.equal(got[k], want[k]), (k, bad)
+        assert not loss[gone].any() and not lse[gone].any() and not want["loss"][gone].any()
+    assert not want["grad_hidden"][gone].view(torch.int16).any()
+    none = dendsn.linear_ce_train(cfg, h, w, torch.full_like(t, -1), r)
+    for k in none:
+        assert not none[k].contiguous().view(torch.uint8).any(), k
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_extreme_logits(gpu_device, io):
+    """Logits of +-40000, of one class far above the rest, and classes at minus infinity."""
+    N, V, D = 20, 200, 64
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    h, w, t, r = make(N, V, D, io, gpu_device, 3, ignored=0.0)
+    announce(f"ce extreme logits {cfg}")
+    check(cfg, 200 * h, 100 * w, t, r)
+    sharp = w.clone()
+    sharp[5] = 64 * h[0]
+    check(cfg, h, sharp, t, r)
+    # classes that every row puts at minus infinity: no part in the statistics
+    hp, wp = h.clone(), w.clone()
+    hp[:, 0] = 1.0
+    wp[100:, 0] = -float("inf")
+    ref = seq_ref.ce(hp, wp, t % 100, 1.0, io, train=False)
+    loss, lse = dendsn.linear_ce(cfg, hp, wp, t % 100)
+    seq_ref.assert_within(loss, *ref["loss"], "loss")
+    seq_ref.assert_within(lse, *ref["lse"], "lse")
+    got = dendsn.linear_ce_train(cfg, hp, wp, t % 100, r)
+    seq_ref.assert_within(got["loss"], *ref["loss"], "loss of the training call")
+    # a NaN in a row that counts is seen in its loss, and in no other's
+    hn = h.clone()
+    hn[3, 1] = float("nan")
+    loss, _ = dendsn.linear_ce(cfg, hn, w, t)
+    assert torch.equal(torch.isnan(loss), torch.arange(N, device=gpu_device) == 3)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_rows_that_lie_apart(gpu_device, io):
+    """Operands as slices of wider buffers of NaN, aligned and odd, give the same bits."""
+    N, V, D = 90, 400, 64
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    h, w, t, r = make(N, V, D, io, gpu_device, 11)
+    want, want_loss = dendsn.linear_ce_train(cfg, h, w, t, r), dendsn.linear_ce(cfg, h, w, t)
+    for pad, at in ((8, 0), (16, 8), (3, 1)):
+        announce(f"ce strided {io} pad {pad} at {at}")
+        hw = torch.full((N, D + pad), float("nan"), dtype=h.dtype, device=gpu_device)
+        ww = torch.full((V, D + pad), float("nan"), dtype=h.dtype, device=gpu_device)
+        hw[:, at:at + D], ww[:, at:at + D] = h, w
+        got = dendsn.linear_ce_train(cfg, hw[:, at:at + D], ww[:, at:at + D], t, r)
+        for k in want:
+            assert torch.equal(got[k], want[k]), k
+        for a, b in zip(dendsn.linear_ce(cfg, hw[:, at:at + D], ww[:, at:at + D], t), want_loss):
+            assert torch.equal(a, b)
+
+
+def test_gradients_with_strides(gpu_device):
+    """The entry point with the C name writes gradients into slices, and nothing beside them."""
+    N, V, D = 50, 70, 20
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, ld_grad_hidden=D + 3, ld_grad_weight=D + 1)
+    h, w, t, r = make(N, V, D, "f32", gpu_device, 12)
+    want = dendsn.linear_ce_train(cfg, h, w, t, r)
+    gh = torch.full((N, D + 3), 7.0, device=gpu_device)
+    gw = torch.full((V, D + 1), 7.0, device=gpu_device)
+    loss = torch.empty(N, device=gpu_device)
+    ws = torch.empty(dendsn.dendsn_ce_workspace_bytes(cfg, True), dtype=torch.uint8, device=gpu_device)
+    announce(f"ce strided gradients {cfg}")
+    dendsn.dendsn_ce_train(cfg, h, w, t, r, loss, None, gh, gw, ws)
+    assert torch.equal(gh[:, :D], want["grad_hidden"]) and torch.equal(gw[:, :D], want["grad_weight"])
+    assert bool((gh[:, D:] == 7.0).all()) and bool((gw[:, D:] == 7.0).all()) and torch.equal(loss, want["loss"])
+
+
+def test_gradient_against_differences(gpu_device):
+    """Directional derivatives by central differences of the float64 loss, step 1e-4 (cubic
+    remainder below 1e-7 of the derivative's scale), fp32 gradients within 1e-5 of the summed
+    sizes."""
+    N, V, D = 30, 77, 20
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, logit_scale=0.5)
+    h, w, t, r = make(N, V, D, "f32", gpu_device, 13)
+    announce(f"ce differences {cfg}")
+    got = dendsn.linear_ce_train(cfg, h, w, t, r)
+    h, w, r = (a.double().cpu() for a in (h, w, r))
+    t = t.cpu()
+    gen = torch.Generator().manual_seed(1)
+    for name in ("grad_hidden", "grad_weight"):
+        for _ in range(3):
+            v = torch.randn(got[name].shape, generator=gen, dtype=torch.float64)
+            at = lambda s: seq_ref.ce_loss(h + s * v if name == "grad_hidden" else h,
+                                           w + s * v if name == "grad_weight" else w, t, 0.5, r)
+            diff = (at(1e-4) - at(-1e-4)) / 2e-4
+            terms = got[name].double().cpu() * v
+            assert abs(float(terms.sum()) - diff) <= 1e-5 * float(terms.abs().sum()), name
+
+
+def test_nothing(gpu_device):
+    cfg = dendsn.LinearCEConfig(N=0, V=9, D=5)
+    h, t = torch.zeros((0, 5), device=gpu_device), torch.zeros((0,), dtype=torch.int64, device=gpu_device)
+    announce("ce N = 0")
+    loss, lse = dendsn.linear_ce(cfg, h, torch.ones((9, 5), device=gpu_device), t)
+    got = dendsn.linear_ce_train(cfg, h, torch.ones((9, 5), device=gpu_device), t)
+    assert loss.numel() == 0 and lse.numel() == 0 and got["grad_weight"].shape == (9, 5)
+    assert not got["grad_weight"].view(torch.int32).any()

@@ -1,0 +1,293 @@
+"""Host-side checks of include/dendsn_seq.h: exports, sizes, and every refusal.
+
+Nothing here touches a GPU: each call queries a size, is of no elements, or fails the
+argument checks, which run on the host before any launch.  Pointers are integers that
+the library never dereferences.
+"""
+
+import ctypes
+import os
+import re
+
+import pytest
+
+import paper_2412_06355_amd as dendsn
+from paper_2412_06355_amd.sequence import dendsn_ce_cfg, dendsn_embed_cfg, dendsn_scan_cfg
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+OK, INVALID, UNSUPPORTED, WORKSPACE = 0, 1, 2, 3
+A = 0x10000          # an aligned address
+BIG = 1 << 46
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return dendsn.seq_lib()
+
+
+def ref(cfg):
+    return ctypes.byref(cfg) if cfg is not None else None
+
+
+def p(v):
+    return None if v is None else ctypes.c_void_p(v)
+
+
+def z(v):
+    return ctypes.c_size_t(v)
+
+
+def test_every_declared_function_is_exported(lib):
+    text = open(os.path.join(ROOT, "include", "dendsn_seq.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    declared = set(re.findall(r"\b(dendsn_[a-z_]+)\s*\(", text))
+    assert declared == set(dendsn.SEQ_EXPORTS)
+    for name in declared:
+        assert hasattr(lib, name)
+
+
+# -- embedding ---------------------------------------------------------------
+def embed_cfg(**kw):
+    c = dict(n=100, V=1000, D=64, ld_table=64, ld_out=64, io=0, index=1, scale=1.0)
+    c.update(kw)
+    return dendsn_embed_cfg(**c)
+
+
+def embed_fwd(lib, c, ids=A, table=2 * A, out=3 * A):
+    return lib.dendsn_embed_forward(ref(c), p(ids), p(table), p(out), None)
+
+
+def embed_bwd(lib, c, ids=A, grad=2 * A, table=3 * A, ws=4 * A, nbytes=1 << 40):
+    return lib.dendsn_embed_backward(ref(c), p(ids), p(grad), p(table), p(ws), z(nbytes), None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(n=-1), dict(n=(1 << 25) + 1), dict(V=-1), dict(V=(1 << 27) + 1), dict(D=-1), dict(D=1 << 22, ld_table=1 << 22),
+    dict(ld_table=63), dict(ld_table=BIG + 1), dict(ld_table=1 << 40), dict(ld_out=-1), dict(ld_out=1 << 45),
+    dict(io=2), dict(io=-1), dict(index=2), dict(scale=float("nan")), dict(scale=float("inf"))])
+def test_embed_bad_cfg(lib, kw):
+    c, out = embed_cfg(**kw), ctypes.c_size_t(77)
+    assert lib.dendsn_embed_workspace_bytes(ref(c), ctypes.byref(out)) == INVALID and out.value == 77
+    assert embed_fwd(lib, c) == INVALID and embed_bwd(lib, c) == INVALID
+    assert dendsn.dendsn_seq_last_error() != ""
+
+
+def test_embed_arguments(lib):
+    c = embed_cfg()
+    assert embed_fwd(lib, None) == INVALID and embed_bwd(lib, None) == INVALID
+    assert lib.dendsn_embed_workspace_bytes(ref(c), None) == INVALID
+    for k in ("ids", "table", "out"):
+        assert embed_fwd(lib, c, **{k: None}) == INVALID
+        assert embed_fwd(lib, c, **{k: A + 2}) == INVALID
+    assert embed_fwd(lib, c, ids=A + 4) == INVALID            # int64 ids
+    assert embed_fwd(lib, embed_cfg(ld_out=63)) == INVALID    # rows of out overlap
+    for k in ("ids", "grad", "table"):
+        assert embed_bwd(lib, c, **{k: None}) == INVALID
+        assert embed_bwd(lib, c, **{k: A + 2}) == INVALID
+    need = ctypes.c_size_t(0)
+    assert lib.dendsn_embed_workspace_bytes(ref(c), ctypes.byref(need)) == OK and need.value > 0
+    assert embed_bwd(lib, c, ws=None) == WORKSPACE
+    assert embed_bwd(lib, c, ws=A + 8) == WORKSPACE
+    assert embed_bwd(lib, c, nbytes=need.value - 1) == WORKSPACE
+    assert "dendsn_embed_workspace_bytes" in dendsn.dendsn_seq_last_error()
+
+
+def test_embed_nothing(lib):
+    assert embed_fwd(lib, embed_cfg(n=0), ids=None, table=None, out=None) == OK
+    assert embed_fwd(lib, embed_cfg(D=0, ld_table=0, ld_out=0), ids=None, out=None) == OK
+    assert embed_bwd(lib, embed_cfg(V=0), ids=None, grad=None, table=None) == OK
+    assert dendsn.dendsn_seq_last_error() == ""
+
+
+# -- scan --------------------------------------------------------------------
+def scan_cfg(**kw):
+    c = dict(T=100, batch=3, D=64, io=0, gate=0, leaky=1)
+    c.update({k: v for k, v in kw.items() if k in c})
+    lanes = c["batch"] * c["D"]
+    for k in ("x", "g", "h", "grad_h", "grad_x", "grad_g"):
+        c[k + "_t"], c[k + "_b"] = max(lanes, 0), max(c["D"], 0)
+    c.update(kw)
+    return dendsn_scan_cfg(**c)
+
+
+def scan_fwd(lib, c, x=A, g=2 * A, h0=None, lengths=None, h=3 * A, last=None, ckpt=4 * A, ws=5 * A, nbytes=1 << 40):
+    return lib.dendsn_scan_forward(ref(c), p(x), p(g), p(h0), p(lengths), p(h), p(last), p(ckpt), p(ws), z(nbytes), None)
+
+
+def scan_bwd(lib, c, x=A, g=2 * A, lengths=None, ckpt=3 * A, gh=4 * A, gl=None, gx=5 * A, gg=6 * A, g0=None, ws=7 * A,
+             nbytes=1 << 40):
+    return lib.dendsn_scan_backward(ref(c), p(x), p(g), p(lengths), p(ckpt), p(gh), p(gl), p(gx), p(gg), p(g0), p(ws),
+                                    z(nbytes), None)
+
+
+def scan_step(lib, c, x=A, g=2 * A, n=8, slots=None, state=3 * A, h=4 * A):
+    return lib.dendsn_scan_step(ref(c), p(x), p(g), n, p(slots), p(state), p(h), None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(T=-1), dict(T=(1 << 30) + 1), dict(batch=-1), dict(batch=65536), dict(D=-1), dict(D=(1 << 27) + 1),
+    dict(T=1 << 30, D=1 << 20), dict(io=2), dict(gate=2), dict(gate=-1), dict(leaky=2), dict(x_t=-1), dict(g_b=-5),
+    dict(h_t=BIG + 1), dict(grad_g_b=BIG), dict(x_t=1 << 45)])
+def test_scan_bad_cfg(lib, kw):
+    c, out = scan_cfg(**kw), ctypes.c_size_t(77)
+    assert lib.dendsn_scan_ckpt_bytes(ref(c), ctypes.byref(out)) == INVALID
+    assert lib.dendsn_scan_workspace_bytes(ref(c), 0, ctypes.byref(out)) == INVALID and out.value == 77
+    assert scan_fwd(lib, c) == INVALID and scan_bwd(lib, c) == INVALID and scan_step(lib, c) == INVALID
+    assert dendsn.dendsn_seq_last_error() != ""
+
+
+def test_scan_arguments(lib):
+    c = scan_cfg()
+    assert scan_fwd(lib, None) == INVALID and scan_bwd(lib, None) == INVALID and scan_step(lib, None) == INVALID
+    for k in ("x", "g", "h"):
+        assert scan_fwd(lib, c, **{k: None}) == INVALID
+        assert scan_fwd(lib, c, **{k: A + 2}) == INVALID
+    for k in ("h0", "lengths", "last"):
+        assert scan_fwd(lib, c, **{k: A + 2}) == INVALID
+    assert scan_fwd(lib, c, ckpt=A + 8) == INVALID
+    assert scan_fwd(lib, scan_cfg(h_t=32)) == INVALID and "overlap" in dendsn.dendsn_seq_last_error()
+    assert scan_fwd(lib, scan_cfg(h_b=32)) == INVALID
+    assert scan_fwd(lib, scan_cfg(h_t=64, h_b=64)) == INVALID      # each row apart, yet they meet
+    for k in ("x", "g", "ckpt", "gh", "gx", "gg"):
+        assert scan_bwd(lib, c, **{k: None}) == INVALID
+        assert scan_bwd(lib, c, **{k: A + 2}) == INVALID
+    for k in ("lengths", "gl", "g0"):
+        assert scan_bwd(lib, c, **{k: A + 2}) == INVALID
+    assert scan_bwd(lib, scan_cfg(grad_x_t=63)) == INVALID and scan_bwd(lib, scan_cfg(grad_g_b=0)) == INVALID
+
+
+def test_scan_sizes(lib):
+    out = ctypes.c_size_t(0)
+    for T in (0, 1, 64, 65, 1000):
+        c = scan_cfg(T=T)
+        assert lib.dendsn_scan_ckpt_bytes(ref(c), ctypes.byref(out)) == OK
+        assert out.value == -(-T // 64) * 3 * 64 * 4
+    c = scan_cfg(T=100000)
+    for backward in (0, 1):
+        assert lib.dendsn_scan_workspace_bytes(ref(c), backward, ctypes.byref(out)) == OK and out.value > 0
+        call = scan_bwd if backward else scan_fwd
+        assert call(lib, c, ws=None) == WORKSPACE
+        assert call(lib, c, ws=A + 8) == WORKSPACE
+        assert call(lib, c, nbytes=out.value - 1) == WORKSPACE
+
+
+def test_scan_step_arguments(lib):
+    c = scan_cfg(T=1)
+    for k in ("x", "g", "state", "h"):
+        assert scan_step(lib, c, **{k: None}) == INVALID
+        assert scan_step(lib, c, **{k: A + 2}) == INVALID
+    assert scan_step(lib, scan_cfg(T=2)) == INVALID
+    assert scan_step(lib, c, n=-1) == INVALID
+    assert scan_step(lib, c, n=2) == INVALID                        # three requests, no slots
+    assert scan_step(lib, c, slots=A + 1) == INVALID
+    assert scan_step(lib, scan_cfg(T=1, h_b=60)) == INVALID
+
+
+def test_scan_nothing(lib):
+    for kw in (dict(T=0), dict(batch=0), dict(D=0)):
+        c = scan_cfg(**kw)
+        assert scan_fwd(lib, c, x=None, g=None, h=None, ckpt=None, ws=None) == OK
+        assert scan_bwd(lib, c, x=None, g=None, ckpt=None, gh=None, gx=None, gg=None, ws=None) == OK
+    assert scan_step(lib, scan_cfg(T=1, batch=0), x=None, g=None, state=None, h=None) == OK
+
+
+# -- linear cross entropy ----------------------------------------------------
+def ce_cfg(**kw):
+    c = dict(N=100, V=1000, D=64, ld_hidden=64, ld_weight=64, ld_grad_hidden=64, ld_grad_weight=64, io=0, index=1,
+             logit_scale=1.0)
+    c.update(kw)
+    return dendsn_ce_cfg(**c)
+
+
+def ce_fwd(lib, c, h=A, w=2 * A, t=3 * A, loss=4 * A, lse=None, ws=5 * A, nbytes=1 << 50):
+    return lib.dendsn_ce_forward(ref(c), p(h), p(w), p(t), p(loss), p(lse), p(ws), z(nbytes), None)
+
+
+def ce_train(lib, c, h=A, w=2 * A, t=3 * A, r=None, loss=4 * A, lse=None, gh=5 * A, gw=6 * A, ws=7 * A, nbytes=1 << 50):
+    return lib.dendsn_ce_train(ref(c), p(h), p(w), p(t), p(r), p(loss), p(lse), p(gh), p(gw), p(ws), z(nbytes), None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(N=-1), dict(N=(1 << 26) + 1), dict(V=0), dict(V=(1 << 24) + 1), dict(D=0), dict(D=(1 << 20) + 1),
+    dict(ld_hidden=63), dict(ld_weight=63), dict(ld_grad_hidden=63), dict(ld_grad_weight=0), dict(ld_weight=1 << 40),
+    dict(io=2), dict(index=-1), dict(logit_scale=float("inf")), dict(logit_scale=float("nan"))])
+def test_ce_bad_cfg(lib, kw):
+    c, out = ce_cfg(**kw), ctypes.c_size_t(77)
+    assert lib.dendsn_ce_workspace_bytes(ref(c), 1, ctypes.byref(out)) == INVALID and out.value == 77
+    assert ce_fwd(lib, c) == INVALID and ce_train(lib, c) == INVALID
+    assert dendsn.dendsn_seq_last_error() != ""
+
+
+def test_ce_arguments(lib):
+    c = ce_cfg()
+    assert ce_fwd(lib, None) == INVALID and ce_train(lib, None) == INVALID
+    for call in (ce_fwd, ce_train):
+        for k in ("h", "w", "t", "loss"):
+            assert call(lib, c, **{k: None}) == INVALID
+            assert call(lib, c, **{k: A + 2}) == INVALID
+        assert call(lib, c, t=A + 4) == INVALID                     # int64 targets
+        assert call(lib, c, lse=A + 2) == INVALID
+        assert call(lib, c, ws=None) == WORKSPACE
+        assert call(lib, c, ws=A + 8) == WORKSPACE
+        need = ctypes.c_size_t(0)
+        assert lib.dendsn_ce_workspace_bytes(ref(c), int(call is ce_train), ctypes.byref(need)) == OK
+        assert call(lib, c, nbytes=need.value - 1) == WORKSPACE
+    for k in ("gh", "gw"):
+        assert ce_train(lib, c, **{k: None}) == INVALID
+        assert ce_train(lib, c, **{k: A + 2}) == INVALID
+    assert ce_train(lib, c, r=A + 2) == INVALID
+
+
+def test_ce_scratch_is_bounded(lib):
+    """The scratch stops growing with the rows."""
+    size = []
+    for N in (1 << 14, 1 << 17, 1 << 20):
+        out = ctypes.c_size_t(0)
+        assert lib.dendsn_ce_workspace_bytes(ref(ce_cfg(N=N, V=128000, D=1024, ld_hidden=1024, ld_weight=1024,
+                                                        ld_grad_hidden=1024, ld_grad_weight=1024, io=1)), 1,
+                                             ctypes.byref(out)) == OK
+        size.append(out.value)
+    assert max(size) < 8 << 30 and size[2] <= 1.1 * size[1]
+
+
+def test_ce_nothing(lib):
+    c = ce_cfg(N=0)
+    assert ce_fwd(lib, c, h=None, t=None, loss=None) == OK
+
+
+# -- the calls that allocate their outputs -----------------------------------
+def test_python_checks():
+    import torch
+
+    e = dendsn.EmbeddingConfig(n=4, V=8, D=6)
+    ids, table = torch.zeros(4, dtype=torch.int64), torch.zeros(8, 6)
+    with pytest.raises(ValueError, match="shape"):
+        dendsn.embedding(e, ids[:3], table)
+    with pytest.raises(ValueError, match="dtype"):
+        dendsn.embedding(e, ids.to(torch.int16), table)
+    with pytest.raises(ValueError, match="dtype"):
+        dendsn.embedding(e, ids, table.to(torch.bfloat16))
+    with pytest.raises(ValueError, match="adjacent"):
+        dendsn.embedding(e, ids, torch.zeros(6, 8).t())
+    with pytest.raises(ValueError, match="overlap"):
+        dendsn.embedding(e, ids, torch.zeros(6).expand(8, 6))
+    s = dendsn.GatedScanConfig(T=3, batch=2, D=4)
+    x = torch.zeros(3, 2, 4)
+    with pytest.raises(ValueError, match="shape"):
+        dendsn.gated_scan(s, x, x[:2])
+    with pytest.raises(ValueError, match="lengths"):
+        dendsn.gated_scan(s, x, x, lengths=torch.zeros(2))
+    with pytest.raises(ValueError, match="ckpt"):
+        dendsn.gated_scan_backward(s, x, x, None, None, x)
+    with pytest.raises(ValueError, match="state"):
+        dendsn.gated_scan_step(s.with_(T=1), x[0], x[0], torch.zeros(2, 4, dtype=torch.float64))
+    c = dendsn.LinearCEConfig(N=3, V=5, D=4)
+    h, w, t = torch.zeros(3, 4), torch.zeros(5, 4), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError, match="weight"):
+        dendsn.linear_ce(c, h, w[:4], t)
+    with pytest.raises(ValueError, match="targets"):
+        dendsn.linear_ce(c, h, w, t.float())
+    with pytest.raises(ValueError, match="row_weight"):
+        dendsn.linear_ce_train(c, h, w, t, torch.ones(2))
+    with pytest.raises(ValueError, match="overlap"):
+        dendsn.linear_ce(c, torch.zeros(4).expand(3, 4), w, t)
