@@ -2,25 +2,24 @@
 //
 //   out[i] = s table[id_i],   grad_table[v] = s sum over {i : id_i = v} of grad_out[i]
 //
-// The gradient adds each row's positions in ascending order, so that it does not
-// depend on scheduling: positions are sorted by id (a stable radix sort of up to 9
-// bits a pass), rows of 64 sorted positions that all hold one id are summed first
-// (frequent tokens), and then every row of the table is written once, +0 or the sum
-// of its first loose positions, its whole rows of 64 and its last loose positions.
-// Both directions are bound by memory: the gradient writes all V rows.
+// The gradient adds each row's positions in an order that the ids alone fix: positions
+// are sorted by id (a stable radix sort of up to 9 bits a pass), every wave sums the
+// runs of equal ids among kRun sorted positions, whatever their rows, so that frequent
+// tokens cost no more than rare ones, and the sums of ids that go on past a wave's
+// positions are joined by a second kernel.  Rows that no token names are cleared beside
+// the sums.  Both directions are bound by memory: the gradient writes all V rows.
 #include "seq_common.h"
 
 namespace dendsn_seq {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kBits = 9, kRadix = 1 << kBits;  // most bits of a pass
-constexpr int kChunk = 2048;                   // positions of a sorting block, at least
 constexpr int kMaxTiles = 512;                 // sorting blocks, at most
-constexpr int kRun = 64;                       // sorted positions of a partial sum
-constexpr int kRows = 32;                      // table rows of a block
-constexpr int kRowWaves = 8;
-constexpr int kLight = 16;  // a row of at most so many positions is one wave's
+constexpr int kOneBlock = 4096;                // positions that one block sorts alone
+constexpr int kRun = 32;                       // sorted positions of a wave
+constexpr int kRows = 32;                      // table rows of a clearing block
 
 template <typename ID>
 __device__ __forceinline__ uint32_t key_of(const ID* ids, int64_t i, uint32_t V) {
@@ -61,9 +60,9 @@ struct SortArgs {
   const uint32_t *key_in, *at_in;
   uint32_t *key_out, *at_out;
   uint32_t* hist;               // [tiles][kRadix]
-  int64_t n, tile;              // tile: positions of a block, a multiple of kThreads
+  int64_t n, tile;              // tile: positions of a block, a multiple of kSortThreads
   uint32_t V, ntiles;
-  int shift, bits;
+  int shift, bits, passes;
 };
 
 template <typename ID, bool FIRST>
@@ -71,52 +70,52 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs& p, int64_t i) {
   return FIRST ? key_of(static_cast<const ID*>(p.ids), i, p.V) : p.key_in[i];
 }
 
+// A pass's counts of each tile.  (Counted by the pass before as it places the keys,
+// with global atomics, frequent ids made that pass 11 us slower; this launch is 3 us.)
 template <typename ID, bool FIRST>
-__global__ void __launch_bounds__(kThreads) embed_hist_kernel(SortArgs p) {
+__global__ void __launch_bounds__(kSortThreads) embed_hist_kernel(SortArgs p) {
   __shared__ uint32_t h[kRadix];
-  for (int d = threadIdx.x; d < kRadix; d += kThreads) h[d] = 0;
+  const int tid = threadIdx.x;
+  if (tid < kRadix) h[tid] = 0;
   __syncthreads();
   const int64_t lo = blockIdx.x * p.tile, hi = min(lo + p.tile, p.n);
   const uint32_t mask = (1u << p.bits) - 1;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads)
-    atomicAdd(&h[(sort_key<ID, FIRST>(p, i) >> p.shift) & mask], 1u);
+  for (int64_t i = lo + tid; i < hi; i += kSortThreads) atomicAdd(&h[(sort_key<ID, FIRST>(p, i) >> p.shift) & mask], 1u);
   __syncthreads();
-  for (int d = threadIdx.x; d < kRadix; d += kThreads) p.hist[int64_t(blockIdx.x) * kRadix + d] = h[d];
+  if (tid < kRadix) p.hist[int64_t(blockIdx.x) * kRadix + tid] = h[tid];
 }
 
-template <typename ID, bool FIRST>
-__global__ void __launch_bounds__(kThreads) embed_scatter_kernel(SortArgs p) {
-  constexpr int W = kThreads / 64;
-  __shared__ uint32_t base[kRadix], count[W][kRadix], sums[kThreads];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  // where this block's first position of each digit goes: digits before it in all
-  // blocks, and the digit itself in the blocks before
-  uint32_t total[2] = {0, 0}, before[2] = {0, 0};
-  for (uint32_t t = 0; t < p.ntiles; ++t) {
-    const uint2 c = *reinterpret_cast<const uint2*>(p.hist + int64_t(t) * kRadix + 2 * tid);
-    total[0] += c.x;
-    total[1] += c.y;
-    if (t < blockIdx.x) before[0] += c.x, before[1] += c.y;
-  }
-  sums[tid] = total[0] + total[1];
+struct SortShared {
+  uint32_t base[kRadix], count[kSortWaves][kRadix], sums[kRadix], part[4][2][kRadix];
+};
+
+// base[d] = positions before this tile's first of digit d, from the digits' totals and
+// their counts in the tiles before.  total, before: of digit tid < kRadix.
+__device__ __forceinline__ void sort_bases(SortShared& s, uint32_t total, uint32_t before) {
+  const int tid = threadIdx.x;
+  if (tid < kRadix) s.sums[tid] = total;
   __syncthreads();
-  for (int s = 1; s < kThreads; s <<= 1) {
-    const uint32_t add = tid >= s ? sums[tid - s] : 0;
+  for (int d = 1; d < kRadix; d <<= 1) {
+    const uint32_t add = tid < kRadix && tid >= d ? s.sums[tid - d] : 0;
     __syncthreads();
-    sums[tid] += add;
+    if (tid < kRadix) s.sums[tid] += add;
     __syncthreads();
   }
-  const uint32_t first = sums[tid] - total[0] - total[1];
-  base[2 * tid] = first + before[0];
-  base[2 * tid + 1] = first + total[0] + before[1];
+  if (tid < kRadix) s.base[tid] = s.sums[tid] - total + before;
+}
+
+// Moves the positions [lo, hi) to their places, in their order.
+template <typename ID, bool FIRST>
+__device__ __forceinline__ void sort_move(const SortArgs& p, SortShared& s, int64_t lo, int64_t hi) {
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const uint32_t mask = (1u << p.bits) - 1;
-  const int64_t lo = blockIdx.x * p.tile, hi = min(lo + p.tile, p.n);
-  for (int64_t i0 = lo; i0 < hi; i0 += kThreads) {
-    for (int d = tid; d < W * kRadix; d += kThreads) (&count[0][0])[d] = 0;
+  for (int64_t i0 = lo; i0 < hi; i0 += kSortThreads) {
+    for (int d = tid; d < kSortWaves * kRadix; d += kSortThreads) (&s.count[0][0])[d] = 0;
     __syncthreads();
     const int64_t i = i0 + tid;
     const bool in = i < hi;
     const uint32_t key = in ? sort_key<ID, FIRST>(p, i) : 0;
+    const uint32_t at = in ? (FIRST ? uint32_t(i) : p.at_in[i]) : 0;
     const uint32_t digit = (key >> p.shift) & mask;
     uint64_t same = __ballot(in);
     for (int b = 0; b < p.bits; ++b) {
@@ -125,22 +124,76 @@ __global__ void __launch_bounds__(kThreads) embed_scatter_kernel(SortArgs p) {
       same &= set ? votes : ~votes;
     }
     const uint32_t rank = __popcll(same & ((uint64_t(1) << lane) - 1));
-    if (in && rank == 0) count[w][digit] = __popcll(same);
+    if (in && rank == 0) s.count[w][digit] = __popcll(same);
+    __syncthreads();
+    if (tid < kRadix) {  // a digit's counts become the places of the waves' first
+      uint32_t sum = s.base[tid];
+#pragma unroll
+      for (int q = 0; q < kSortWaves; ++q) {
+        const uint32_t c = s.count[q][tid];
+        s.count[q][tid] = sum;
+        sum += c;
+      }
+      s.base[tid] = sum;
+    }
     __syncthreads();
     if (in) {
-      uint32_t to = base[digit] + rank;
-      for (int q = 0; q < w; ++q) to += count[q][digit];
+      const uint32_t to = s.count[w][digit] + rank;
       p.key_out[to] = key;
-      p.at_out[to] = FIRST ? uint32_t(i) : p.at_in[i];
+      p.at_out[to] = at;
     }
     __syncthreads();
-    for (int d = tid; d < kRadix; d += kThreads) {
-      uint32_t add = 0;
+  }
+}
+
+template <typename ID, bool FIRST>
+__global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(SortArgs p) {
+  __shared__ SortShared s;
+  const int tid = threadIdx.x, q = tid >> 8, d = (tid & 255) * 2;
+  uint2 total = make_uint2(0, 0), before = make_uint2(0, 0);
+#pragma unroll 8
+  for (uint32_t t = q; t < p.ntiles; t += 4) {
+    const uint2 c = *reinterpret_cast<const uint2*>(p.hist + int64_t(t) * kRadix + d);
+    total.x += c.x, total.y += c.y;
+    if (t < blockIdx.x) before.x += c.x, before.y += c.y;
+  }
+  *reinterpret_cast<uint2*>(&s.part[q][0][d]) = total;
+  *reinterpret_cast<uint2*>(&s.part[q][1][d]) = before;
+  __syncthreads();
+  uint32_t tt = 0, bb = 0;
+  if (tid < kRadix) {
 #pragma unroll
-      for (int q = 0; q < W; ++q) add += count[q][d];
-      base[d] += add;
+    for (int k = 0; k < 4; ++k) tt += s.part[k][0][tid], bb += s.part[k][1][tid];
+  }
+  sort_bases(s, tt, bb);
+  const int64_t lo = blockIdx.x * p.tile;
+  sort_move<ID, FIRST>(p, s, lo, min(lo + p.tile, p.n));
+}
+
+// Few positions: one block makes all passes.  buf: the two buffers in turn.
+template <typename ID>
+__global__ void __launch_bounds__(kSortThreads) embed_sort_kernel(SortArgs p, uint32_t* key0, uint32_t* at0,
+                                                                  uint32_t* key1, uint32_t* at1) {
+  __shared__ SortShared s;
+  const int tid = threadIdx.x;
+  const uint32_t mask = (1u << p.bits) - 1;
+  for (int k = 0; k < p.passes; ++k) {
+    p.shift = k * p.bits;
+    p.key_in = k & 1 ? key1 : key0;
+    p.at_in = k & 1 ? at1 : at0;
+    p.key_out = k & 1 ? key0 : key1;
+    p.at_out = k & 1 ? at0 : at1;
+    __syncthreads();  // the last pass's places are written (a block's barrier orders its memory)
+    if (tid < kRadix) s.part[0][0][tid] = 0;
+    __syncthreads();
+    for (int64_t i = tid; i < p.n; i += kSortThreads) {
+      const uint32_t key = k ? sort_key<ID, false>(p, i) : sort_key<ID, true>(p, i);
+      atomicAdd(&s.part[0][0][(key >> p.shift) & mask], 1u);
     }
     __syncthreads();
+    sort_bases(s, tid < kRadix ? s.part[0][0][tid] : 0, 0);
+    if (k) sort_move<ID, false>(p, s, 0, p.n);
+    else sort_move<ID, true>(p, s, 0, p.n);
   }
 }
 
@@ -151,63 +204,17 @@ struct SumArgs {
   const uint32_t *key, *at;  // sorted
   const void* grad;
   void* table;
-  float* part;               // [n / kRun][D]
+  float* part;               // [runs][2][D]: sums of the ids that a run begins and ends in the middle of
   int64_t n, D, ldg, ldt;
+  int64_t runs, sum_blocks;
+  int chunks;                // waves along a row
   uint32_t V;
   float scale;
 };
 
-template <typename IO, int VEC>
-__device__ __forceinline__ void add_rows(float (&acc)[VEC], const SumArgs& p, int64_t from, int64_t to, int64_t d) {
-  const IO* grad = static_cast<const IO*>(p.grad);
-  constexpr int U = 8;  // loads in flight
-  for (int64_t i = from; i < to; i += U) {
-    Pack<IO, VEC> v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u)  // past the end: the last row again, dropped below
-      v[u] = *reinterpret_cast<const Pack<IO, VEC>*>(grad + int64_t(p.at[min(i + u, to - 1)]) * p.ldg + d);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u < to)
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) acc[k] += widen(v[u].v[k]);
-  }
-}
-
-template <int VEC>
-__device__ __forceinline__ void add_parts(float (&acc)[VEC], const SumArgs& p, int64_t from, int64_t to, int64_t d) {
-  constexpr int U = 4;
-  for (int64_t i = from; i < to; i += U) {
-    Pack<float, VEC> v[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = *reinterpret_cast<const Pack<float, VEC>*>(p.part + min(i + u, to - 1) * p.D + d);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (i + u < to)
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) acc[k] += v[u].v[k];
-  }
-}
-
-// The sum of kRun sorted positions, where they all hold one id.
-template <typename IO, int VEC>
-__global__ void __launch_bounds__(64) embed_part_kernel(SumArgs p) {
-  const int64_t j = blockIdx.x;
-  const uint32_t key = p.key[j * kRun];
-  if (key >= p.V || key != p.key[j * kRun + kRun - 1]) return;
-  const int64_t d = (int64_t(blockIdx.y) * 64 + threadIdx.x) * VEC;
-  if (d >= p.D) return;
-  float acc[VEC] = {};
-  add_rows<IO, VEC>(acc, p, j * kRun, (j + 1) * kRun, d);
-  Pack<float, VEC> o;
-#pragma unroll
-  for (int k = 0; k < VEC; ++k) o.v[k] = acc[k];
-  *reinterpret_cast<Pack<float, VEC>*>(p.part + j * p.D + d) = o;
-}
-
-// First sorted position whose key is at least `key`, by one wave: 64 candidates a step.
-__device__ __forceinline__ int64_t lower_bound(const uint32_t* keys, int64_t n, uint32_t key, int lane) {
-  int64_t lo = 0, len = n;  // the answer lies in [lo, lo + len]
+// First sorted position in [lo, lo + len) whose key is at least `key` (lo + len: none), by
+// one wave: 64 candidates a step.
+__device__ __forceinline__ int64_t lower_bound(const uint32_t* keys, int64_t lo, int64_t len, uint32_t key, int lane) {
   while (len > 0) {
     const int64_t step = ceil_div(len, 64);
     const int64_t i = lo + int64_t(lane) * step;
@@ -231,67 +238,132 @@ __device__ __forceinline__ void store_row(const SumArgs& p, uint32_t v, int64_t 
   *reinterpret_cast<Pack<IO, VEC>*>(static_cast<IO*>(p.table) + int64_t(v) * p.ldt + d) = o;
 }
 
-// kRows rows of the table: a wave for a row of few positions, the whole block for a
-// row of many.
+// A wave: kRun sorted positions by 64 VEC values of a row.
 template <typename IO, int VEC>
-__global__ void __launch_bounds__(kRowWaves * 64) embed_rows_kernel(SumArgs p) {
+__device__ __forceinline__ void sum_run(const SumArgs& p, int64_t run, int chunk, int lane) {
+  constexpr int U = 8;  // loads in flight
+  const int64_t i0 = run * kRun;
+  const int count = int(min(int64_t(kRun), p.n - i0));
+  const int64_t mine = i0 + min(lane, count - 1);
+  const uint32_t key = p.key[mine], at = p.at[mine];
+  const uint32_t prev = i0 > 0 ? p.key[i0 - 1] : ~0u, next = i0 + count < p.n ? p.key[i0 + count] : ~0u;
+  const int64_t d0 = (int64_t(chunk) * 64 + lane) * VEC;
+  const bool on = d0 < p.D;
+  const int64_t d = on ? d0 : 0;
+  const IO* grad = static_cast<const IO*>(p.grad) + d;
+  const bool inside = __builtin_amdgcn_readlane(key, 0) == prev;  // the first id began before
+  bool first = true;
+  float acc[VEC] = {};
+  for (int j0 = 0; j0 < count; j0 += U) {
+    Pack<IO, VEC> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)  // past the end: the last position again, dropped below
+      v[u] = *reinterpret_cast<const Pack<IO, VEC>*>(grad + int64_t(__builtin_amdgcn_readlane(at, min(j0 + u, count - 1))) * p.ldg);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u;
+      if (j >= count) break;
+      const uint32_t k = __builtin_amdgcn_readlane(key, j);
+      if (k >= p.V) return;  // the rest name no row
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc[e] += widen(v[u].v[e]);
+      const uint32_t after = j + 1 < count ? __builtin_amdgcn_readlane(key, j + 1) : next;
+      const bool last = j + 1 == count;
+      if (k != after || last) {
+        const bool begun = first && inside, goes_on = last && k == after;
+        if (on) {
+          if (!begun && !goes_on) {
+            store_row<IO, VEC>(p, k, d, acc);
+          } else {
+            Pack<float, VEC> o;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) o.v[e] = acc[e];
+            *reinterpret_cast<Pack<float, VEC>*>(p.part + (run * 2 + (begun ? 0 : 1)) * p.D + d) = o;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) acc[e] = 0.0f;
+        first = false;
+      }
+    }
+  }
+}
+
+// The first sum_blocks blocks sum runs, the others clear the rows that no token names.
+template <typename IO, int VEC>
+__global__ void __launch_bounds__(kThreads) embed_sum_kernel(SumArgs p) {
   __shared__ int64_t bounds[2];
-  __shared__ int64_t start[kRows + 1];
-  __shared__ float join[kRowWaves][64 * VEC];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const uint32_t v0 = blockIdx.x * uint32_t(kRows);
+  __shared__ uint32_t named;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (blockIdx.x < p.sum_blocks) {
+    const int64_t unit = int64_t(blockIdx.x) * (kThreads / 64) + w;
+    if (unit < p.runs * p.chunks) sum_run<IO, VEC>(p, unit / p.chunks, int(unit % p.chunks), lane);
+    return;
+  }
+  const uint32_t v0 = uint32_t(blockIdx.x - p.sum_blocks) * kRows;
   const uint32_t rows = min(uint32_t(kRows), p.V - v0);
+  if (threadIdx.x == 0) named = 0;
   if (w < 2) {
-    const int64_t at = lower_bound(p.key, p.n, v0 + (w ? rows : 0), lane);
+    const int64_t at = lower_bound(p.key, 0, p.n, v0 + (w ? rows : 0), lane);
     if (lane == 0) bounds[w] = at;
   }
   __syncthreads();
-  const int64_t lo = bounds[0], hi = bounds[1];
-  if (threadIdx.x <= kRows) start[threadIdx.x] = hi;
-  __syncthreads();
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kRowWaves * 64) {
+  for (int64_t i = bounds[0] + threadIdx.x; i < bounds[1]; i += kThreads) {
     const uint32_t k = p.key[i];
-    uint32_t v = i > lo ? p.key[i - 1] + 1 : v0;  // rows up to k start here
-    for (; v <= k; ++v) start[v - v0] = i;
+    if (i == bounds[0] || p.key[i - 1] != k) atomicOr(&named, 1u << (k - v0));
   }
   __syncthreads();
-  for (uint32_t r = w; r < rows; r += kRowWaves) {
-    const int64_t s = start[r], e = start[r + 1];
-    if (e - s > kLight) continue;
-    for (int64_t d = lane * VEC; d < p.D; d += 64 * VEC) {
-      float acc[VEC] = {};
-      add_rows<IO, VEC>(acc, p, s, e, d);
-      store_row<IO, VEC>(p, v0 + r, d, acc);
+  const uint32_t have = named;
+  const float zero[VEC] = {};
+  for (uint32_t r = w; r < rows; r += kThreads / 64) {
+    if (have >> r & 1) continue;
+    for (int64_t d = lane * VEC; d < p.D; d += 64 * VEC) store_row<IO, VEC>(p, v0 + r, d, zero);
+  }
+}
+
+// Ids whose positions go on past a run: the block of the run that they begin in adds
+// the runs' sums, each of its waves a share.
+template <typename IO, int VEC>
+__global__ void __launch_bounds__(kThreads) embed_join_kernel(SumArgs p) {
+  constexpr int W = kThreads / 64, U = 4;
+  __shared__ float join[W][64 * VEC];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t run = blockIdx.x, i0 = run * kRun, i1 = i0 + kRun;  // (i1 < n: the last run has no block)
+  const uint32_t k = p.key[i1 - 1];
+  if (k >= p.V || p.key[i1] != k || (i0 > 0 && p.key[i0 - 1] == k)) return;
+  const int64_t end = lower_bound(p.key, i1, p.n - i1, k + 1, lane);
+  const int64_t runs = (end - 1) / kRun - run;  // that go on
+  const int64_t each = ceil_div(runs, W), lo = min(run + 1 + w * each, run + 1 + runs), hi = min(lo + each, run + 1 + runs);
+  const int64_t d = (int64_t(blockIdx.y) * 64 + lane) * VEC;
+  const bool on = d < p.D;
+  float acc[VEC] = {};
+  if (on) {
+    if (w == 0) {
+      const auto v = *reinterpret_cast<const Pack<float, VEC>*>(p.part + (run * 2 + 1) * p.D + d);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc[e] = v.v[e];
+    }
+    for (int64_t r = lo; r < hi; r += U) {
+      Pack<float, VEC> v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        v[u] = *reinterpret_cast<const Pack<float, VEC>*>(p.part + min(r + u, hi - 1) * 2 * p.D + d);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (r + u < hi)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) acc[e] += v[u].v[e];
     }
   }
-  for (uint32_t r = 0; r < rows; ++r) {
-    const int64_t s = start[r], e = start[r + 1];
-    if (e - s <= kLight) continue;
-    // whole runs [b0, b1) of kRun, loose positions before and after
-    const int64_t b0 = ceil_div(s, kRun), b1 = max(b0, e / kRun);
-    const int64_t head = min(b0 * kRun, e), tail = max(b1 * kRun, head);
-    const int64_t ph = ceil_div(head - s, kRowWaves), pp = ceil_div(b1 - b0, kRowWaves);
-    const int64_t pt = ceil_div(e - tail, kRowWaves);
-    for (int64_t c = 0; c < p.D; c += 64 * VEC) {
-      const int64_t d = c + lane * VEC;
-      float acc[VEC] = {};
-      if (d < p.D) {
-        add_rows<IO, VEC>(acc, p, min(s + w * ph, head), min(s + (w + 1) * ph, head), d);
-        if (b1 * kRun <= e) add_parts<VEC>(acc, p, min(b0 + w * pp, b1), min(b0 + (w + 1) * pp, b1), d);
-        add_rows<IO, VEC>(acc, p, min(tail + w * pt, e), min(tail + (w + 1) * pt, e), d);
-      }
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) join[w][k * 64 + lane] = acc[k];
-      __syncthreads();
-      if (w == 0 && d < p.D) {
+  for (int e = 0; e < VEC; ++e) join[w][e * 64 + lane] = acc[e];
+  __syncthreads();
+  if (w == 0 && on) {
 #pragma unroll
-        for (int q = 1; q < kRowWaves; ++q)
+    for (int q = 1; q < W; ++q)
 #pragma unroll
-          for (int k = 0; k < VEC; ++k) acc[k] += join[q][k * 64 + lane];
-        store_row<IO, VEC>(p, v0 + r, d, acc);
-      }
-      __syncthreads();
-    }
+      for (int e = 0; e < VEC; ++e) acc[e] += join[q][e * 64 + lane];
+    store_row<IO, VEC>(p, k, d, acc);
   }
 }
 
@@ -324,44 +396,72 @@ bool wide(const dendsn_embed_cfg* c, const void* a, const void* b) {
 
 struct Layout {
   size_t key[2], at[2], hist, part, total;
-  int64_t tile;
+  int64_t tile, runs;
   uint32_t ntiles;
+  int bits, passes;
 };
 
 Layout layout(const dendsn_embed_cfg* c) {
   Layout l;
   Carve cv;
-  l.tile = round_up(ceil_div(c->n > 0 ? c->n : 1, kMaxTiles), kThreads);
-  if (l.tile < kChunk) l.tile = kChunk;
-  l.ntiles = uint32_t(ceil_div(c->n > 0 ? c->n : 1, l.tile));
+  int bits = 1;  // of the keys 0 .. V
+  while (bits < 32 && (uint64_t(c->V) >> bits) != 0) ++bits;
+  l.passes = int(ceil_div(bits, kBits));
+  l.bits = int(ceil_div(bits, l.passes));
+  const int64_t n = c->n > 0 ? c->n : 1;
+  l.tile = round_up(ceil_div(n, kMaxTiles), kSortThreads);
+  l.ntiles = uint32_t(ceil_div(n, l.tile));
+  l.runs = ceil_div(n, kRun);
   for (int i = 0; i < 2; ++i) {
-    l.key[i] = cv.take(size_t(c->n) * 4);
-    l.at[i] = cv.take(size_t(c->n) * 4);
+    l.key[i] = cv.take(size_t(n) * 4);
+    l.at[i] = cv.take(size_t(n) * 4);
   }
   l.hist = cv.take(size_t(l.ntiles) * kRadix * 4);
-  l.part = cv.take(size_t(c->n / kRun) * size_t(c->D) * 4);
+  l.part = cv.take(size_t(l.runs) * 2 * size_t(c->D) * 4);
   l.total = cv.at;
   return l;
 }
 
+// Sorts the positions by id; returns which of the two buffers holds the result.
 template <typename ID>
-void sort_pass(const SortArgs& a, bool first, hipStream_t stream) {
-  const dim3 grid(a.ntiles), block(kThreads);
-  if (first) {
-    embed_hist_kernel<ID, true><<<grid, block, 0, stream>>>(a);
-    embed_scatter_kernel<ID, true><<<grid, block, 0, stream>>>(a);
-  } else {
-    embed_hist_kernel<ID, false><<<grid, block, 0, stream>>>(a);
-    embed_scatter_kernel<ID, false><<<grid, block, 0, stream>>>(a);
+int sort(const dendsn_embed_cfg* c, const Layout& l, const void* ids, char* ws, hipStream_t stream) {
+  uint32_t *key[2], *at[2];
+  for (int i = 0; i < 2; ++i) {
+    key[i] = reinterpret_cast<uint32_t*>(ws + l.key[i]);
+    at[i] = reinterpret_cast<uint32_t*>(ws + l.at[i]);
   }
+  SortArgs s{};
+  s.ids = ids; s.n = c->n; s.tile = l.tile; s.V = uint32_t(c->V); s.ntiles = l.ntiles;
+  s.bits = l.bits; s.passes = l.passes;
+  const dim3 grid(l.ntiles), block(kSortThreads);
+  if (c->n <= kOneBlock) {
+    embed_sort_kernel<ID><<<dim3(1), block, 0, stream>>>(s, key[0], at[0], key[1], at[1]);
+    return l.passes & 1;
+  }
+  s.hist = reinterpret_cast<uint32_t*>(ws + l.hist);
+  for (int k = 0; k < l.passes; ++k) {
+    s.shift = k * l.bits;
+    s.key_in = key[k & 1]; s.at_in = at[k & 1];
+    s.key_out = key[~k & 1]; s.at_out = at[~k & 1];
+    if (k == 0) {
+      embed_hist_kernel<ID, true><<<grid, block, 0, stream>>>(s);
+      embed_scatter_kernel<ID, true><<<grid, block, 0, stream>>>(s);
+    } else {
+      embed_hist_kernel<ID, false><<<grid, block, 0, stream>>>(s);
+      embed_scatter_kernel<ID, false><<<grid, block, 0, stream>>>(s);
+    }
+  }
+  return l.passes & 1;
 }
 
 template <typename IO, int VEC>
-void sums(const SumArgs& a, hipStream_t stream) {
-  if (a.n >= kRun)
-    embed_part_kernel<IO, VEC>
-        <<<dim3(unsigned(a.n / kRun), unsigned(ceil_div(a.D, 64 * VEC))), dim3(64), 0, stream>>>(a);
-  embed_rows_kernel<IO, VEC><<<dim3(unsigned(ceil_div(a.V, kRows))), dim3(kRowWaves * 64), 0, stream>>>(a);
+void sums(SumArgs a, hipStream_t stream) {
+  a.chunks = int(ceil_div(a.D, 64 * VEC));
+  a.sum_blocks = ceil_div(a.runs * a.chunks, kThreads / 64);
+  embed_sum_kernel<IO, VEC>
+      <<<dim3(unsigned(a.sum_blocks + ceil_div(a.V, kRows))), dim3(kThreads), 0, stream>>>(a);
+  if (a.runs > 1)
+    embed_join_kernel<IO, VEC><<<dim3(unsigned(a.runs - 1), unsigned(a.chunks)), dim3(kThreads), 0, stream>>>(a);
 }
 
 template <typename IO, typename ID>
@@ -431,28 +531,14 @@ dendsn_status dendsn_embed_backward(const dendsn_embed_cfg* cfg, const void* ids
   if (st != DENDSN_OK) return st;
   if (none) return DENDSN_OK;
 
+  if (l.runs * ceil_div(cfg->D, 64) > (int64_t(1) << 25))
+    return fail(DENDSN_E_UNSUPPORTED, "n * D must be below 2^36");
   char* ws = static_cast<char*>(workspace);
-  SortArgs s{};
-  s.ids = ids;
-  s.hist = reinterpret_cast<uint32_t*>(ws + l.hist);
-  s.n = cfg->n; s.tile = l.tile; s.V = uint32_t(cfg->V); s.ntiles = l.ntiles;
-  int bits = 1;  // of the keys 0 .. V
-  while (bits < 32 && (uint64_t(cfg->V) >> bits) != 0) ++bits;
-  const int passes = int(ceil_div(bits, kBits));
-  s.bits = int(ceil_div(bits, passes));
   int cur = 0;
-  if (cfg->n > 0) {
-    for (int k = 0; k < passes; ++k) {
-      s.shift = k * s.bits;
-      s.key_in = reinterpret_cast<const uint32_t*>(ws + l.key[cur]);
-      s.at_in = reinterpret_cast<const uint32_t*>(ws + l.at[cur]);
-      cur ^= 1;
-      s.key_out = reinterpret_cast<uint32_t*>(ws + l.key[cur]);
-      s.at_out = reinterpret_cast<uint32_t*>(ws + l.at[cur]);
-      cfg->index == DENDSN_INDEX_I64 ? sort_pass<int64_t>(s, k == 0, stream) : sort_pass<int32_t>(s, k == 0, stream);
-    }
-  }
+  if (cfg->n > 0)
+    cur = cfg->index == DENDSN_INDEX_I64 ? sort<int64_t>(cfg, l, ids, ws, stream) : sort<int32_t>(cfg, l, ids, ws, stream);
   SumArgs a{};
+  a.runs = cfg->n > 0 ? l.runs : 0;
   a.key = reinterpret_cast<const uint32_t*>(ws + l.key[cur]);
   a.at = reinterpret_cast<const uint32_t*>(ws + l.at[cur]);
   a.grad = grad_out; a.table = grad_table;
