@@ -82,16 +82,16 @@ struct LogitArgs {
   GemmArgs g;
   float scale;
   float2* stats;   // [M][tiles_n] maximum and sum of exponentials
-  float* z;        // [M][ldz] logits, NULL: not kept
+  float* z;        // logits in panels of 64 classes, NULL: not kept
   float* chosen;   // [M] the target's logit (where z is not kept)
   const void* targets;
-  int64_t ldz;
+  int64_t zrows, zcols;  // rows of a panel, classes of all
   int wide;
 };
 
 template <int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(WM * WN * 64) ce_logits_kernel(LogitArgs p) {
-  using G = Gemm<BM, BN, WM, WN, false, false>;
+  using G = Gemm<BM, BN, WM, WN, false, false, false>;
   __shared__ __align__(1024) char lds[2 * G::kStage];
   int tm, tn;
   tile_of(p.g, blockIdx.x, tm, tn);
@@ -118,7 +118,8 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_logits_kernel(LogitArgs p) {
         if (n + r < p.g.N) top = fmaxf(top, z);
         if (p.chosen && n + r == target) p.chosen[m] = z;
       }
-      if (p.z && row && n < p.ldz) *reinterpret_cast<f32x4*>(p.z + m * p.ldz + n) = acc[i][j];
+      if (p.z && row && n < p.zcols)
+        *reinterpret_cast<f32x4*>(p.z + (n / kStep * p.zrows + m) * kStep + n % kStep) = acc[i][j];
     }
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
@@ -187,7 +188,7 @@ __device__ __forceinline__ void store4(void* out, int io, int64_t at, int64_t n,
 
 template <int BM, int BN, int WM, int WN, bool XCOL>
 __global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs p) {
-  using G = Gemm<BM, BN, WM, WN, XCOL, true>;
+  using G = Gemm<BM, BN, WM, WN, XCOL, true, true>;  // X: dz, in panels
   __shared__ __align__(1024) char lds[2 * G::kStage];
   int tm, tn;
   tile_of(p.g, blockIdx.x, tm, tn);
@@ -253,7 +254,7 @@ struct LossArgs {
   const float* chosen;  // the target's
   const void* targets;
   float *loss, *lse;    // lse: also what the gradient reads
-  int64_t M, ldz, V;
+  int64_t M, zrows, V;
   int tiles, wide;
 };
 
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(kThreads) ce_loss_kernel(LossArgs p) {
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if (lane == 0) {
     const float lse = ref + logf(sum);
-    const float z = !keep ? 0.0f : p.z ? p.z[m * p.ldz + t] : p.chosen[m];
+    const float z = !keep ? 0.0f : p.z ? p.z[(t / kStep * p.zrows + m) * kStep + t % kStep] : p.chosen[m];
     p.loss[m] = keep ? lse - z : 0.0f;
     if (p.lse) p.lse[m] = keep ? lse : 0.0f;
   }
@@ -288,45 +289,53 @@ struct DzArgs {
   const float *z, *lse, *row_weight;
   const void* targets;
   uint16_t* dz;
-  int64_t ldz, plane, V;
+  int64_t M, rows, blocks, plane, V;  // rows of a panel; blocks along the rows
   float scale;
   int wide, planes;
 };
 
-// dz = r s (exp(z - lse) - onehot), +0 in rows without a target and past V.
+constexpr int kDzRows = 128;  // rows of a block, of one panel
+
+// dz = r s (exp(z - lse) - onehot); +0 in rows without a target, past V, and in the
+// rows past M that the last stage of dW's sum reads.
 __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
-  const int64_t m = blockIdx.y;
-  const int64_t v0 = (int64_t(blockIdx.x) * kThreads + threadIdx.x) * 8;
-  if (v0 >= p.ldz) return;
-  const int64_t t = target_of(p.targets, p.wide, m);
-  const bool keep = t >= 0 && t < p.V;
-  const float c = keep ? p.scale * (p.row_weight ? p.row_weight[m] : 1.0f) : 0.0f;
-  const float lse = keep ? p.lse[m] : 0.0f;
-  const f32x4* z = reinterpret_cast<const f32x4*>(p.z + m * p.ldz + v0);
-  const f32x4 za = z[0], zb = z[1];
-  uint16_t a[8], f, b[8], d[8];  // (dz is finite wherever the loss is: no copy)
+  const int64_t panel = blockIdx.x / p.blocks, r0 = blockIdx.x % p.blocks * kDzRows;
+  const int64_t v0 = panel * kStep + threadIdx.x % 8 * 8;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float zk = k < 4 ? za[k & 3] : zb[k & 3];
-    float g = 0.0f;
-    if (keep && v0 + k < p.V) {
-      g = __expf(zk - lse);
-      if (v0 + k == t) g -= 1.0f;
-      g *= c;
+  for (int it = 0; it < kDzRows / 32; ++it) {
+    const int64_t m = r0 + it * 32 + threadIdx.x / 8;
+    if (m >= round_up(p.M, kStep)) return;
+    const int64_t t = m < p.M ? target_of(p.targets, p.wide, m) : -1;
+    const bool keep = t >= 0 && t < p.V;
+    const float c = keep ? p.scale * (p.row_weight ? p.row_weight[m] : 1.0f) : 0.0f;
+    const float lse = keep ? p.lse[m] : 0.0f;
+    const int64_t at = (panel * p.rows + m) * kStep + threadIdx.x % 8 * 8;
+    const f32x4* z = reinterpret_cast<const f32x4*>(p.z + at);
+    const f32x4 za = z[0], zb = z[1];
+    uint16_t a[8], f, b[8], d[8];  // (dz is finite wherever the loss is: no copy)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float zk = k < 4 ? za[k & 3] : zb[k & 3];
+      float g = 0.0f;
+      if (keep && v0 + k < p.V) {
+        g = __expf(zk - lse);
+        if (v0 + k == t) g -= 1.0f;
+        g *= c;
+      }
+      if (p.planes == 1) a[k] = bf16_bits(g);
+      else split3(g, a[k], f, b[k], d[k]);
     }
-    if (p.planes == 1) a[k] = bf16_bits(g);
-    else split3(g, a[k], f, b[k], d[k]);
+    auto put = [&](uint16_t* to, const uint16_t (&x)[8]) {
+      uint4 q;
+      q.x = x[0] | uint32_t(x[1]) << 16;
+      q.y = x[2] | uint32_t(x[3]) << 16;
+      q.z = x[4] | uint32_t(x[5]) << 16;
+      q.w = x[6] | uint32_t(x[7]) << 16;
+      *reinterpret_cast<uint4*>(to + at) = q;
+    };
+    put(p.dz, a);
+    if (p.planes == 3) put(p.dz + p.plane, b), put(p.dz + 2 * p.plane, d);
   }
-  auto put = [&](uint16_t* to, const uint16_t (&x)[8]) {
-    uint4 q;
-    q.x = x[0] | uint32_t(x[1]) << 16;
-    q.y = x[2] | uint32_t(x[3]) << 16;
-    q.z = x[4] | uint32_t(x[5]) << 16;
-    q.w = x[6] | uint32_t(x[7]) << 16;
-    *reinterpret_cast<uint4*>(to + m * p.ldz + v0) = q;
-  };
-  put(p.dz, a);
-  if (p.planes == 3) put(p.dz + p.plane, b), put(p.dz + 2 * p.plane, d);
 }
 
 __global__ void __launch_bounds__(kThreads) ce_zero_kernel(void* out, int64_t rows, int64_t cols, int64_t ld, int io) {
@@ -361,7 +370,7 @@ constexpr int kBig = 256;  // tile of a product, both ways
 struct Plan {
   int planes;
   int64_t Dp, Vp;      // rows of packed operands, of logits
-  int64_t piece, pieces;
+  int64_t piece, pieces, rows;  // rows: of a panel
   bool big;            // 256 x 256 tiles (else 128 x 128)
   int tile;
   int splits;          // of dH
@@ -381,10 +390,12 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   const int64_t per_row = train ? p.Vp * (4 + 2 * p.planes) : ceil_div(c->V, 64) * 8;
   int64_t most = kPieceBytes / per_row / kBig * kBig;
   if (most < kBig) most = kBig;
+  if (most > kMaxPanelRows) most = kMaxPanelRows;
   const int64_t N = c->N > 0 ? c->N : 1;
   p.pieces = ceil_div(N, most);
   p.piece = p.pieces > 1 ? round_up(ceil_div(N, p.pieces), kBig) : N;
   p.pieces = ceil_div(N, p.piece);
+  p.rows = round_up(p.piece, kBig);
   p.big = ceil_div(p.piece, kBig) * ceil_div(c->V, kBig) >= 256;
   p.tile = p.big ? kBig : 128;
   Carve cv;
@@ -395,8 +406,8 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   p.chosen = cv.take(size_t(p.piece) * 4);
   p.splits = 1;
   if (train) {
-    p.z = cv.take(size_t(p.piece) * size_t(p.Vp) * 4);
-    p.dz = cv.take(size_t(p.planes) * size_t(p.piece) * size_t(p.Vp) * 2);
+    p.z = cv.take(size_t(p.rows) * size_t(p.Vp) * 4);
+    p.dz = cv.take(size_t(p.planes) * size_t(p.rows) * size_t(p.Vp) * 2);
     const int64_t tiles = ceil_div(p.piece, p.tile) * ceil_div(c->D, p.tile);
     const int64_t steps = ceil_div(c->V, kStep) * (p.planes == 3 ? 6 : 1);
     int64_t s = (p.big ? 256 : 512) / tiles;
@@ -416,7 +427,7 @@ void finish(GemmArgs& g, int planes, int tile, int splits) {
   g.tiles_m = int(ceil_div(g.M, tile));
   g.tiles_n = int(ceil_div(g.N, tile));
   g.splits = splits;
-  g.steps = ceil_div(g.K, kStep) * (planes == 3 ? 6 : 1);
+  g.steps = int(ceil_div(g.K, kStep) * (planes == 3 ? 6 : 1));
 }
 
 dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const void* weight, const void* targets,
@@ -456,7 +467,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     l.stats = reinterpret_cast<float2*>(ws + p.stats);
     l.z = train ? reinterpret_cast<float*>(ws + p.z) : nullptr;
     l.chosen = train ? nullptr : reinterpret_cast<float*>(ws + p.chosen);
-    l.targets = tp; l.ldz = p.Vp; l.wide = wide;
+    l.targets = tp; l.zrows = p.rows; l.zcols = p.Vp; l.wide = wide;
     const dim3 lg(unsigned(int64_t(l.g.tiles_m) * l.g.tiles_n));
     if (p.big) ce_logits_kernel<256, 256, 2, 4><<<lg, dim3(512), 0, stream>>>(l);
     else ce_logits_kernel<128, 128, 2, 2><<<lg, dim3(256), 0, stream>>>(l);
@@ -466,26 +477,19 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     s.loss = loss + r0;
     float* own_lse = reinterpret_cast<float*>(ws + p.lse);
     s.lse = lse ? lse + r0 : train ? own_lse : nullptr;
-    s.M = M; s.ldz = p.Vp; s.V = c->V; s.tiles = l.g.tiles_n; s.wide = wide;
+    s.M = M; s.zrows = p.rows; s.V = c->V; s.tiles = l.g.tiles_n; s.wide = wide;
     ce_loss_kernel<<<dim3(unsigned(ceil_div(M, kThreads / 64))), dim3(kThreads), 0, stream>>>(s);
     if (!train) continue;
 
     DzArgs z{};
     z.z = l.z; z.lse = s.lse; z.row_weight = row_weight ? row_weight + r0 : nullptr; z.targets = tp;
     z.dz = reinterpret_cast<uint16_t*>(ws + p.dz);
-    z.ldz = p.Vp; z.plane = M * p.Vp; z.V = c->V; z.scale = c->logit_scale; z.wide = wide; z.planes = p.planes;
-    // rows along y: at most 2^15 a launch
-    for (int64_t y0 = 0; y0 < M; y0 += 32768) {
-      DzArgs q = z;
-      const int64_t rows = M - y0 < 32768 ? M - y0 : 32768;
-      q.z += y0 * p.Vp; q.lse += y0; q.dz += y0 * p.Vp;
-      if (q.row_weight) q.row_weight += y0;
-      q.targets = static_cast<const char*>(tp) + size_t(y0) * isz;
-      ce_dz_kernel<<<dim3(unsigned(ceil_div(p.Vp, 8 * kThreads)), unsigned(rows)), dim3(kThreads), 0, stream>>>(q);
-    }
+    z.M = M; z.rows = p.rows; z.blocks = ceil_div(round_up(M, kStep), kDzRows);
+    z.plane = p.rows * p.Vp; z.V = c->V; z.scale = c->logit_scale; z.wide = wide; z.planes = p.planes;
+    ce_dz_kernel<<<dim3(unsigned(z.blocks * (p.Vp / kStep))), dim3(kThreads), 0, stream>>>(z);
 
     GradArgs gh{};
-    gh.g.x = Operand{z.dz, p.Vp, z.plane, 0, M, p.Vp};
+    gh.g.x = Operand{z.dz, p.rows, z.plane, 0, M, p.Vp};
     gh.g.y = w;
     gh.g.M = M; gh.g.N = c->D; gh.g.K = c->V;
     finish(gh.g, p.planes, p.tile, p.splits);
@@ -501,7 +505,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     }
 
     GradArgs gw{};
-    gw.g.x = Operand{z.dz, p.Vp, z.plane, 0, M, p.Vp};
+    gw.g.x = Operand{z.dz, p.rows, z.plane, 0, M, p.Vp};
     gw.g.y = h;
     gw.g.M = c->V; gw.g.N = c->D; gw.g.K = M;
     finish(gw.g, p.planes, p.tile, 1);

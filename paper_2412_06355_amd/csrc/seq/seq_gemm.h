@@ -3,7 +3,10 @@
 // Each operand lies in memory either with k adjacent ("K rows": X[m][k]) or with
 // its other index adjacent ("K columns": X[k][m]); both are staged in LDS as they
 // lie, by LDS-DMA of 16 bytes a lane, two stages deep, and reach the matrix
-// instructions through 16-byte reads or, for K columns, transposing reads.  The
+// instructions through 16-byte reads or, for K columns, transposing reads.  A wave holds
+// the fragments of half a stage while it reads those of the next half, and the block
+// meets once a stage, between the halves, with products on both sides of the barrier;
+// the products of a half go in rounds with its reads and fetches between them.  The
 // 16-byte chunks of a stage are permuted so that neither kind of read meets a bank
 // twice: the DMA writes LDS linearly, so each lane fetches the chunk that belongs at
 // its place.  Buffer descriptors bound every access: rows, columns and k past an
@@ -29,12 +32,16 @@ typedef __attribute__((address_space(3))) void lds_void_t;
 constexpr int kStep = 64;   // k of a stage
 constexpr int kFinite = 3;  // the first plane without infinities, as a plane's number
 
+// An operand as it lies: rows of cols elements, ld apart; or, in panels, columns in
+// groups of 64, each group a [ld][64] matrix of its own (ld: rows of a panel, of which
+// all exist; cols a multiple of 64).  Panels keep what a stage reads of a wide matrix
+// in a few pages, whichever way the product runs.
 struct Operand {
   const uint16_t* p;
-  int64_t ld;      // elements between rows as they lie
+  int64_t ld;
   int64_t plane;   // elements between planes
   int64_t finite;  // elements from the first plane to its copy without infinities
-  int64_t rows, cols;  // as they lie
+  int64_t rows, cols;
 };
 
 struct GemmArgs {
@@ -43,14 +50,15 @@ struct GemmArgs {
   int planes;       // 1 or 3
   int tiles_m, tiles_n;
   int splits;       // blocks along k of a tile
-  int64_t steps;    // stages of the whole sum
+  int steps;        // stages of the whole sum
 };
 
-// Rows of an operand may be this far apart: 256 of them lie within a descriptor.
+// Rows of an operand may be this far apart: a stage's 256 lie within a descriptor.
 constexpr int64_t kMaxLd = int64_t(1) << 21;
+constexpr int64_t kMaxPanelRows = int64_t(1) << 20;
 
-__device__ __forceinline__ void dma16(rsrc_t r, uint32_t off, void* lds) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)lds, 16, off, 0, 0, 0);
+__device__ __forceinline__ void dma16(rsrc_t r, uint32_t off, uint32_t soff, void* lds) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)lds, 16, off, soff, 0, 0);
 }
 
 // A barrier that leaves loads in flight; no memory access of the program moves across it.
@@ -60,58 +68,97 @@ __device__ __forceinline__ void block_barrier() {
   asm volatile("" ::: "memory");
 }
 
-// One operand's side of a block: R rows (K rows) or columns (K columns) of its stage.
-template <int R, int NW, bool KCOL>
+// Values that are the same in every lane, put where the compiler sees it (scalar
+// registers): results of divisions are not.
+__device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ const char* scalar(const char* p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(v)), hi = __builtin_amdgcn_readfirstlane(uint32_t(v >> 32));
+  return reinterpret_cast<const char*>(uint64_t(hi) << 32 | lo);
+}
+
+// One operand's side of a block: R rows (K rows) or columns (K columns) of its stages.
+// A stage is fetched through a descriptor that stays put while a scalar offset moves.
+template <int R, int NW, bool KCOL, bool PANEL>
 struct Side {
   static constexpr int kBytes = R * kStep * 2;
   static constexpr int kLoads = kBytes / (1024 * NW);  // DMA instructions of a wave
   static_assert(kLoads >= 1 && kBytes % (1024 * NW) == 0, "a stage is whole DMA instructions");
-  static constexpr int kRowBytes = KCOL ? R * 2 : kStep * 2;
+  static constexpr int kRowBytes = KCOL ? R * 2 : kStep * 2;  // in LDS
+  static constexpr uint32_t kRebase = 1u << 29;
 
-  const char* base;
-  int64_t left;          // bytes from base to the operand's end
-  int64_t ldb;           // bytes between rows
-  int64_t plane, finite; // bytes between planes, and to the copy of the first one
-  int64_t per_step;      // bytes from stage to stage
+  const char *first, *base;
+  int64_t plane, finite;  // bytes between planes, and to the copy of the first one
+  int64_t left, total;    // bytes from base, from first to the operand's end
+  uint32_t step, soff;    // bytes from stage to stage, from base to the stage
+  int records;
   uint32_t off[kLoads];
-  uint32_t tail;         // bit i: load i of a K-rows stage reads past the last k in the last step
+  uint32_t tail;          // bit i: load i of a K-rows stage is past the last k in the last stage
 
   __device__ __forceinline__ void init(const Operand& o, int64_t r0, int w, int lane) {
-    ldb = o.ld * 2;
+    const int64_t ldb = PANEL ? kStep * 2 : o.ld * 2, panel = o.ld * kStep * 2;
     plane = o.plane * 2;
     finite = o.finite * 2;
-    const int64_t at = KCOL ? r0 * 2 : r0 * ldb;
-    base = reinterpret_cast<const char*>(o.p) + at;
-    left = ((o.rows - 1) * o.ld + o.cols) * 2 - at;
-    per_step = KCOL ? kStep * ldb : kStep * 2;
+    const int64_t at = PANEL ? (KCOL ? r0 / kStep * panel : r0 * ldb) : KCOL ? r0 * 2 : r0 * ldb;
+    first = reinterpret_cast<const char*>(o.p) + at;
+    total = (PANEL ? o.cols / kStep * panel : ((o.rows - 1) * o.ld + o.cols) * 2) - at;
+    step = uint32_t(KCOL ? kStep * ldb : PANEL ? panel : kStep * 2);
     tail = 0;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int b = (w * kLoads + i) * 1024 + lane * 16;
-      const int row = b / kRowBytes, chunk = b % kRowBytes / 16;
-      const int logical = chunk ^ swizzle(row);
-      off[i] = uint32_t(row * ldb) + logical * 16;
-      if (!KCOL && logical * 8 >= int((o.cols - 1) % kStep + 1)) tail |= 1u << i;
+      const int row = b / kRowBytes, chunk = (b % kRowBytes / 16) ^ swizzle(row);
+      off[i] = uint32_t(row * ldb) + (PANEL && KCOL ? uint32_t(chunk / 8 * panel) + chunk % 8 * 16 : chunk * 16);
+      if (!KCOL && !PANEL && chunk * 8 >= int((o.cols - 1) % kStep + 1)) tail |= 1u << i;
     }
   }
   static __device__ __forceinline__ int swizzle(int row) {
     return KCOL ? 2 * ((row & 3) | ((row >> 3) & 1) << 2) : row & 7;
   }
-  // The stage of step `step` of plane `pl` (kFinite: of the first one's copy); `last`: the
-  // last step of a plane's k.
-  __device__ __forceinline__ void fetch(char* lds, int pl, int64_t step, bool last, int w) const {
-    const int64_t skip = (pl == kFinite ? finite : pl * plane) + step * per_step;
-    int64_t n = left - step * per_step;
-    n = n < 0 ? 0 : n > 0x7FFFFFF0 ? 0x7FFFFFF0 : n;
-    const rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base + skip), 0, int(n), 0x00020000);
+  __device__ __forceinline__ void place() {
+    const int hi = int(left >> 32);  // (a 64-bit comparison would be a vector instruction)
+    const uint32_t lo = uint32_t(left);
+    records = hi < 0 ? 0 : hi > 0 || lo > 0x7FFFFFF0u ? 0x7FFFFFF0 : int(lo);
+  }
+  // Goes to stage `s` of plane `pl` (kFinite: of the first one's copy).
+  __device__ __forceinline__ void seek(int pl, int64_t s) {
+    const int64_t skip = s * step;
+    base = first + (pl == kFinite ? finite : pl * plane) + skip;
+    left = total - skip;
+    soff = 0;
+    place();
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      uint32_t o = off[i];
-      if (!KCOL && last && (tail >> i & 1)) o = 0x80000000u;
-      dma16(r, o, lds + (w * kLoads + i) * 1024);
-    }
+    for (int i = 0; i < kLoads; ++i) off[i] &= 0x7FFFFFFFu;
+  }
+  __device__ __forceinline__ void next() { soff += step; }
+  __device__ __forceinline__ void rebase() {
+    base += soff;
+    left -= soff;
+    soff = 0;
+    place();
+  }
+  // The stage that comes is the last of its plane: what lies past the last k is out of
+  // every descriptor's reach.
+  __device__ __forceinline__ void last() {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+      if (!KCOL && !PANEL && (tail >> i & 1)) off[i] |= 0x80000000u;
+  }
+  __device__ __forceinline__ rsrc_t descriptor(bool live) const {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(scalar(base)), 0, scalar(live ? records : 0), 0x00020000);
+  }
+  __device__ __forceinline__ void fetch(rsrc_t r, char* lds, int i, int w) const {
+    dma16(r, off[i], soff, lds + (w * kLoads + i) * 1024);
   }
 };
+
+// Four rows of 16 elements, a lane's pointer at 4 of them, come as 16 columns of four.
+// (The qualifier is what tells the compiler which memory the builtin reads; without it
+// every such read waited for all DMA in flight, whatever it was writing.)
+__device__ __forceinline__ s16x4 read_transposed(const char* __restrict__ p) {
+  typedef __attribute__((address_space(3))) s16x4* ptr;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(p));
+}
 
 // A lane's addresses of its fragments in a stage: rows (or columns) r0 + 16 f + (lane & 15),
 // k = 32 s + 8 (lane >> 4) .. + 7.
@@ -133,9 +180,7 @@ struct Frags {
   __device__ __forceinline__ bf16x8 read(const char* lds, int f, int s) const {
     if (KCOL) {
       const char* p = lds + at[f] + s * (32 * R * 2);
-      typedef __attribute__((address_space(3))) s16x4* ptr;
-      const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(p));
-      const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr)(p + 4 * R * 2));
+      const s16x4 a = read_transposed(p), b = read_transposed(p + 4 * R * 2);
       typedef short s16x8 __attribute__((ext_vector_type(8)));
       const s16x8 v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
       return __builtin_bit_cast(bf16x8, v);
@@ -158,8 +203,8 @@ __device__ __forceinline__ void tile_of(const GemmArgs& g, int64_t id, int& tm, 
   const int first = int(grp) * kGroup;
   const int size = g.tiles_m - first < kGroup ? g.tiles_m - first : kGroup;
   const int64_t in = t - grp * width;
-  tm = first + int(in % size);
-  tn = int(in / size);
+  tm = scalar(first + int(in % size));
+  tn = scalar(int(in / size));
 }
 
 // The planes of the s-th product of an fp32 pair, smallest first.
@@ -171,12 +216,14 @@ __device__ __forceinline__ void planes_of(int s, int& px, int& py) {
 
 // The product of one tile.  acc[i][j]: lane l holds rows m = 16 j + (l & 15) and
 // columns n = 16 i + 4 (l >> 4) + 0..3 of the wave's tile.
-template <int BM, int BN, int WM, int WN, bool XCOL, bool YCOL>
+template <int BM, int BN, int WM, int WN, bool XCOL, bool XPANEL, bool YCOL>
 struct Gemm {
   static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
-  using SX = Side<BM, NW, XCOL>;
-  using SY = Side<BN, NW, YCOL>;
+  using SX = Side<BM, NW, XCOL, XPANEL>;
+  using SY = Side<BN, NW, YCOL, false>;
   static constexpr int kStage = SX::kBytes + SY::kBytes;
+  static constexpr int kLoads = SX::kLoads + SY::kLoads;
+  static_assert(FM % 2 == 0 && FN <= FM / 2 * 2, "half of a wave's rounds read all fragments");
 
   static __device__ __forceinline__ void run(const GemmArgs& g, char* lds, int tm, int tn, int split,
                                              f32x4 (&acc)[FN][FM]) {
@@ -195,43 +242,94 @@ struct Gemm {
 #pragma unroll
       for (int j = 0; j < FM; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    const int64_t per = ceil_div(g.K, kStep);  // stages of one product of planes
-    const int64_t each = ceil_div(g.steps, g.splits);
-    const int64_t s0 = split * each, s1 = s0 + each < g.steps ? s0 + each : g.steps;
-    int prod = int(s0 / per);
-    int64_t k = s0 % per;
-    auto fetch = [&](char* to) {
+    const int per = int(ceil_div(g.K, kStep));  // stages of one product of planes
+    const int each = scalar((g.steps + g.splits - 1) / g.splits);
+    const int s0 = split * each, s1 = min(s0 + each, g.steps);
+    int prod = scalar(s0 / per), k = scalar(s0 % per);
+    auto seek = [&]() {
       int px = 0, py = 0;
       if (g.planes == 3) planes_of(prod, px, py);
-      sx.fetch(to, px, k, k == per - 1, w);
-      sy.fetch(to + SX::kBytes, py, k, k == per - 1, w);
-      if (++k == per) k = 0, ++prod;
+      sx.seek(px, k);
+      sy.seek(py, k);
+      if (k == per - 1) sx.last(), sy.last();
     };
-    if (s0 < s1) fetch(lds);
-    for (int64_t s = s0; s < s1; ++s) {
-      const int buf = int(s - s0) & 1;
-      // this wave's part of the stage is there (vmcnt 0) and its reads of the other one are
-      // done (lgkmcnt 0); past the barrier, so are every wave's
+    auto next = [&]() {
+      ++k;
+      sx.next();
+      sy.next();
+      if (k >= per - 1 || max(sx.soff, sy.soff) >= SX::kRebase) {  // seldom
+        if (k == per) {
+          ++prod;
+          k = 0;
+          if (prod < 6) seek();
+        } else {
+          sx.rebase();
+          sy.rebase();
+          if (k == per - 1) sx.last(), sy.last();
+        }
+      }
+    };
+    // loads [lo, hi) of a stage
+    auto fetch = [&](rsrc_t rx, rsrc_t ry, char* to, int lo, int hi) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        if (i < lo || i >= hi) continue;
+        if (i < SX::kLoads) sx.fetch(rx, to, i, w);
+        else sy.fetch(ry, to + SX::kBytes, i - SX::kLoads, w);
+      }
+    };
+    bf16x8 xa[FM], ya[FN], xb[FM], yb[FN];  // fragments of a stage's first and second 32 k
+    // round j of FM: one row of products, and what the next half needs read
+    auto read = [&](const char* from, int h, int j, bf16x8 (&xf)[FM], bf16x8 (&yf)[FN]) {
+      if (j >= FM / 2) return;
+#pragma unroll
+      for (int i = 0; i < FN; ++i)
+        if (i / ((FN + FM / 2 - 1) / (FM / 2)) == j) yf[i] = fy.read(from + SX::kBytes, i, h);
+      xf[2 * j] = fx.read(from, 2 * j, h);
+      xf[2 * j + 1] = fx.read(from, 2 * j + 1, h);
+    };
+    auto multiply = [&](int j, const bf16x8 (&xf)[FM], const bf16x8 (&yf)[FN]) {
+#pragma unroll
+      for (int i = 0; i < FN; ++i)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yf[i], xf[j], acc[i][j], 0, 0, 0);
+    };
+    if (s0 < s1) {
+      seek();
+      fetch(sx.descriptor(true), sy.descriptor(true), lds, 0, kLoads);
+      next();
+      fetch(sx.descriptor(s0 + 1 < s1), sy.descriptor(s0 + 1 < s1), lds + kStage, 0, kLoads);
+      next();
+      __builtin_amdgcn_s_waitcnt(0x0F70 | kLoads);  // the first stage's loads are done
+      block_barrier();
+#pragma unroll
+      for (int j = 0; j < FM / 2; ++j) read(lds, 0, j, xa, ya);
+    }
+    for (int s = s0; s < s1; ++s) {
+      char* now = lds + ((s - s0) & 1) * kStage;
+      char* then = lds + (~(s - s0) & 1) * kStage;
+#pragma unroll
+      for (int j = 0; j < FM; ++j) {
+        read(now, 1, j, xb, yb);
+        multiply(j, xa, ya);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // the next stage is there (vmcnt 0) and this one is in registers (lgkmcnt 0); past the
+      // barrier that holds for every wave, so this stage's place takes the stage after next
+      // (past the last one: nothing, by an empty descriptor)
       __builtin_amdgcn_s_waitcnt(0x0070);
       block_barrier();
-      if (s + 1 < s1) fetch(lds + (buf ^ 1) * kStage);
-      const char* cx = lds + buf * kStage;
-      const char* cy = cx + SX::kBytes;
+      __builtin_amdgcn_sched_barrier(0);
+      const rsrc_t rx = sx.descriptor(s + 2 < s1), ry = sy.descriptor(s + 2 < s1);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        bf16x8 xf[FM], yf[FN];
-#pragma unroll
-        for (int i = 0; i < FN; ++i) yf[i] = fy.read(cy, i, h);
-#pragma unroll
-        for (int j = 0; j < FM; ++j) xf[j] = fx.read(cx, j, h);
-#pragma unroll
-        for (int j = 0; j < FM; ++j)
-#pragma unroll
-          for (int i = 0; i < FN; ++i)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yf[i], xf[j], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < FM; ++j) {
+        read(then, 0, j, xa, ya);
+        fetch(rx, ry, now, j * kLoads / FM, (j + 1) * kLoads / FM);
+        multiply(j, xb, yb);
+        __builtin_amdgcn_sched_barrier(0);
       }
+      next();
     }
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt 0: past the barrier, the stages may be reused
+    __builtin_amdgcn_s_waitcnt(0x0070);  // nothing is in flight: past the barrier, the stages may be reused
     block_barrier();
   }
 };
