@@ -78,87 +78,136 @@ __global__ void __launch_bounds__(kThreads) ce_pack_kernel(PackArgs p) {
 // ---------------------------------------------------------------------------
 // The products
 // ---------------------------------------------------------------------------
+// exp(a - b): the difference first, which is exact where it matters (a scaled maximum
+// would be rounded, by hundredths for logits of 10^4).
+__device__ __forceinline__ float exp_diff(float a, float b) {
+  return __builtin_amdgcn_exp2f(1.44269504f * (a - b));
+}
+
 struct LogitArgs {
   GemmArgs g;
   float scale;
   float2* stats;   // [M][tiles_n] maximum and sum of exponentials
-  float* z;        // logits in panels of 64 classes, NULL: not kept
-  float* chosen;   // [M] the target's logit (where z is not kept)
+  float* z;        // hidden weight^T in panels of 64 classes, NULL: not kept
+  float* chosen;   // [M] the target's (where z is not kept)
   const void* targets;
   int64_t zrows, zcols;  // rows of a panel, classes of all
   int wide;
 };
 
+// Over the four lane groups of a wave that hold one row.
+template <typename F>
+__device__ __forceinline__ float over_groups(float v, F f) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// A block takes tiles in turn: the next one's first stages are fetched while it works
+// out this one's statistics.  Where the logits are kept it has one tile: its fetches
+// would wait for its stores (vmcnt counts both, in order), which a new block's do not.
 template <int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(WM * WN * 64) ce_logits_kernel(LogitArgs p) {
+__global__ void __launch_bounds__(WM * WN * 64) ce_logits_kernel(LogitArgs) {
   using G = Gemm<BM, BN, WM, WN, false, false, false>;
-  __shared__ __align__(1024) char lds[2 * G::kStage];
+  // (one array: with two, the compiler tells reads of one from DMA into the other, and
+  // makes every read of a stage wait for all DMA in flight)
+  __shared__ __align__(1024) char lds[2 * G::kStage + G::kNotes];
+  float2(*part)[BM] = reinterpret_cast<float2(*)[BM]>(lds + 2 * G::kStage);
+  G gemm(lds);
+  const int lane = gemm.lane, wm = gemm.w / WN, wn = gemm.w % WN;
   int tm, tn;
-  tile_of(p.g, blockIdx.x, tm, tn);
-  f32x4 acc[G::FN][G::FM];
-  G::run(p.g, lds, tm, tn, 0, acc);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int wm = w / WN, wn = w % WN;
-  float2* part = reinterpret_cast<float2*>(lds);  // [WN][BM]
-  const int64_t n0 = int64_t(tn) * BN + wn * G::TN + 4 * (lane >> 4);
+  tile_of(arguments<GemmArgs>(), blockIdx.x, tm, tn);
+  gemm.begin(tm, tn, 0);
+  G::landed();
+  block_barrier();
+  for (uint32_t id = blockIdx.x;; ) {
+    f32x4 acc[G::FN][G::FM];
+    gemm.run(acc);
+    const LogitArgs& p = arguments<LogitArgs>();
+    const uint32_t tiles = scalar(p.g.tiles_m * p.g.tiles_n);
+    const float scale = p.scale;
+    const int64_t m0 = int64_t(tm) * BM, n0 = int64_t(tn) * BN + wn * G::TN + 4 * (lane >> 4);
+    const bool whole = int64_t(tn + 1) * BN <= p.g.N;
+    const int this_tn = tn;
+    id += gridDim.x;
+    if (id < tiles) {
+      tile_of(p.g, id, tm, tn);
+      gemm.begin(tm, tn, 0);
+    }
+    const int r0 = wm * G::TM + (lane & 15);
+    if (p.chosen) {
 #pragma unroll
-  for (int j = 0; j < G::FM; ++j) {
-    const int64_t m = int64_t(tm) * BM + wm * G::TM + 16 * j + (lane & 15);
-    const bool row = m < p.g.M;
-    int64_t target = -1;
-    if (p.chosen && row) target = target_of(p.targets, p.wide, m);
-    float top = -INFINITY;
+      for (int j = 0; j < G::FM; ++j) {
+        const int64_t m = m0 + r0 + 16 * j;
+        const int64_t at = (m < p.g.M ? target_of(p.targets, p.wide, m) : -1) - n0;
+        if (at < 0 || at >= p.g.N - n0) continue;
 #pragma unroll
-    for (int i = 0; i < G::FN; ++i) {
-      const int64_t n = n0 + 16 * i;
+        for (int i = 0; i < G::FN; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float z = acc[i][j][r] * p.scale;
-        acc[i][j][r] = z;
-        if (n + r < p.g.N) top = fmaxf(top, z);
-        if (p.chosen && n + r == target) p.chosen[m] = z;
+          for (int r = 0; r < 4; ++r)
+            if (at == 16 * i + r) p.chosen[m] = acc[i][j][r];
       }
-      if (p.z && row && n < p.zcols)
-        *reinterpret_cast<f32x4*>(p.z + (n / kStep * p.zrows + m) * kStep + n % kStep) = acc[i][j];
     }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float ref = top == -INFINITY ? 0.0f : top;
-    float sum = 0.0f;
+    if (p.z) {
+      // (a column past zcols is in no panel)
+      float* z = p.z + (n0 / kStep * p.zrows + m0 + r0) * kStep + n0 % kStep;
 #pragma unroll
-    for (int i = 0; i < G::FN; ++i)
+      for (int j = 0; j < G::FM; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (n0 + 16 * i + r < p.g.N) sum += __expf(acc[i][j][r] - ref);
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (lane < 16) part[wn * BM + wm * G::TM + 16 * j + lane] = make_float2(top, sum);
-  }
-  __syncthreads();
-  for (int r = threadIdx.x; r < BM; r += WM * WN * 64) {
-    const int64_t m = int64_t(tm) * BM + r;
-    if (m >= p.g.M) continue;
-    float2 a = part[r];
-#pragma unroll
-    for (int q = 1; q < WN; ++q) {
-      const float2 b = part[q * BM + r];
-      const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.0f : top;
-      a = make_float2(top, a.y * __expf(a.x - ref) + b.y * __expf(b.x - ref));
+        for (int i = 0; i < G::FN; ++i) {
+          static_assert(G::TN == kStep, "a wave's columns are one panel's");
+          if (n0 < p.zcols) *reinterpret_cast<f32x4*>(z + 16 * j * kStep + 16 * i) = acc[i][j];
+        }
     }
-    p.stats[m * p.g.tiles_n + tn] = a;
+#pragma unroll
+    for (int j = 0; j < G::FM; ++j) {
+      f32x4 t[G::FN];
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < G::FN; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          t[i][r] = acc[i][j][r] * scale;
+          if (!whole && n0 + 16 * i + r >= p.g.N) t[i][r] = -INFINITY;
+          top = fmaxf(top, t[i][r]);
+        }
+      top = over_groups(top, [](float a, float b) { return fmaxf(a, b); });
+      const float ref = top == -INFINITY ? 0.0f : top;
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < G::FN; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += exp_diff(t[i][r], ref);
+      sum = over_groups(sum, [](float a, float b) { return a + b; });
+      if (lane < 16) part[wn][r0 + 16 * j] = make_float2(top, sum);
+    }
+    if (id < tiles) G::landed();
+    else __builtin_amdgcn_s_waitcnt(0xC07F);  // (lgkmcnt 0: the logits need not have arrived)
+    block_barrier();
+    for (int r = threadIdx.x; r < BM; r += WM * WN * 64) {
+      if (m0 + r >= p.g.M) continue;
+      float2 a = part[0][r];
+#pragma unroll
+      for (int q = 1; q < WN; ++q) {
+        const float2 b = part[q][r];
+        const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.0f : top;
+        a = make_float2(top, a.y * exp_diff(a.x, ref) + b.y * exp_diff(b.x, ref));
+      }
+      p.stats[(m0 + r) * p.g.tiles_n + this_tn] = a;
+    }
+    if (id >= tiles) break;
   }
 }
 
-enum Out { kOutIo = 0, kOutPartial = 1, kOutSum = 2 };
-
 struct GradArgs {
   GemmArgs g;
-  void* out;             // io (kOutIo)
-  float* part;           // [splits][M][N] (kOutPartial) or [M][N] (kOutSum)
+  void* out;             // io
+  float* part;           // fp32: [splits][M][N] (splits > 1), or [M][N] summed over pieces
   const void* targets;   // rows without a target are +0 (NULL: none)
   int64_t ld, V;
   int wide, io;          // io: dendsn_io
-  int add, keep;         // kOutSum: add what is there; write fp32 (else io, the last piece)
+  int add, keep;         // add the sum of the pieces before; keep it (else the result is whole)
 };
 
 __device__ __forceinline__ void store4(void* out, int io, int64_t at, int64_t n, int64_t N, f32x4 v) {
@@ -187,43 +236,63 @@ __device__ __forceinline__ void store4(void* out, int io, int64_t at, int64_t n,
 }
 
 template <int BM, int BN, int WM, int WN, bool XCOL>
-__global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs p) {
+__global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs) {
   using G = Gemm<BM, BN, WM, WN, XCOL, true, true>;  // X: dz, in panels
   __shared__ __align__(1024) char lds[2 * G::kStage];
-  int tm, tn;
-  tile_of(p.g, blockIdx.x, tm, tn);
-  f32x4 acc[G::FN][G::FM];
-  const int split = blockIdx.y;
-  G::run(p.g, lds, tm, tn, split, acc);
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int64_t N = p.g.N;
+  G gemm(lds);
+  const int lane = gemm.lane, wm = gemm.w / WN, wn = gemm.w % WN;
+  int tm, tn, split;
+  auto begin = [&](const GemmArgs& g, uint32_t id) {
+    const uint32_t tiles = uint32_t(g.tiles_m) * uint32_t(g.tiles_n);
+    split = scalar(int(id / tiles));
+    tile_of(g, id % tiles, tm, tn);
+    gemm.begin(tm, tn, split);
+  };
+  begin(arguments<GemmArgs>(), blockIdx.x);
+  G::landed();
+  block_barrier();
+  for (uint32_t id = blockIdx.x;; ) {
+    f32x4 acc[G::FN][G::FM];
+    gemm.run(acc);
+    const GradArgs& p = arguments<GradArgs>();
+    const uint32_t units = scalar(p.g.tiles_m * p.g.tiles_n * p.g.splits);
+    const int64_t N = p.g.N;
+    const int64_t m0 = int64_t(tm) * BM + wm * G::TM + (lane & 15);
+    const int64_t n0 = int64_t(tn) * BN + wn * G::TN + 4 * (lane >> 4);
+    const int this_split = split;
+    id += gridDim.x;
+    if (id < units) begin(p.g, id);
+    G::landed();
+    block_barrier();
 #pragma unroll
-  for (int j = 0; j < G::FM; ++j) {
-    const int64_t m = int64_t(tm) * BM + w / WN * G::TM + 16 * j + (lane & 15);
-    if (m >= p.g.M) continue;
-    bool zero = false;
-    if (p.targets) {
-      const int64_t t = target_of(p.targets, p.wide, m);
-      zero = t < 0 || t >= p.V;
-    }
-#pragma unroll
-    for (int i = 0; i < G::FN; ++i) {
-      const int64_t n = int64_t(tn) * BN + w % WN * G::TN + 16 * i + 4 * (lane >> 4);
-      if (n >= N) continue;
-      f32x4 v = acc[i][j];
-      if (zero) v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-      if (p.g.splits > 1) {
-        store4(p.part, DENDSN_IO_F32, (int64_t(split) * p.g.M + m) * N + n, n, N, v);
-        continue;
+    for (int j = 0; j < G::FM; ++j) {
+      const int64_t m = m0 + 16 * j;
+      if (m >= p.g.M) continue;
+      bool zero = false;
+      if (p.targets) {
+        const int64_t t = target_of(p.targets, p.wide, m);
+        zero = t < 0 || t >= p.V;
       }
-      if (p.add) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (n + r < N) v[r] += p.part[m * N + n + r];
+      for (int i = 0; i < G::FN; ++i) {
+        const int64_t n = n0 + 16 * i;
+        if (n >= N) continue;
+        f32x4 v = acc[i][j];
+        if (zero) v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (p.g.splits > 1) {
+          store4(p.part, DENDSN_IO_F32, (int64_t(this_split) * p.g.M + m) * N + n, n, N, v);
+          continue;
+        }
+        if (p.add) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (n + r < N) v[r] += p.part[m * N + n + r];
+        }
+        if (p.keep) store4(p.part, DENDSN_IO_F32, m * N + n, n, N, v);
+        else store4(p.out, p.io, m * p.ld + n, n, N, v);
       }
-      if (p.keep) store4(p.part, DENDSN_IO_F32, m * N + n, n, N, v);
-      else store4(p.out, p.io, m * p.ld + n, n, N, v);
     }
+    if (id >= units) break;
   }
 }
 
@@ -255,6 +324,7 @@ struct LossArgs {
   const void* targets;
   float *loss, *lse;    // lse: also what the gradient reads
   int64_t M, zrows, V;
+  float scale;
   int tiles, wide;
 };
 
@@ -273,13 +343,13 @@ __global__ void __launch_bounds__(kThreads) ce_loss_kernel(LossArgs p) {
   float sum = 0.0f;
   for (int i = lane; i < p.tiles; i += 64) {
     const float2 s = p.stats[m * p.tiles + i];
-    sum += s.y * __expf((s.x == -INFINITY ? 0.0f : s.x) - ref);
+    sum += s.y * exp_diff(s.x == -INFINITY ? 0.0f : s.x, ref);
   }
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if (lane == 0) {
     const float lse = ref + logf(sum);
-    const float z = !keep ? 0.0f : p.z ? p.z[(t / kStep * p.zrows + m) * kStep + t % kStep] : p.chosen[m];
+    const float z = !keep ? 0.0f : p.scale * (p.z ? p.z[(t / kStep * p.zrows + m) * kStep + t % kStep] : p.chosen[m]);
     p.loss[m] = keep ? lse - z : 0.0f;
     if (p.lse) p.lse[m] = keep ? lse : 0.0f;
   }
@@ -290,6 +360,7 @@ struct DzArgs {
   const void* targets;
   uint16_t* dz;
   int64_t M, rows, blocks, plane, V;  // rows of a panel; blocks along the rows
+  int64_t ld;                         // dz: elements between rows of a panel
   float scale;
   int wide, planes;
 };
@@ -297,7 +368,9 @@ struct DzArgs {
 constexpr int kDzRows = 128;  // rows of a block, of one panel
 
 // dz = r s (exp(z - lse) - onehot); +0 in rows without a target, past V, and in the
-// rows past M that the last stage of dW's sum reads.
+// rows past M that the last stage of dW's sum reads.  In bf16 dz takes the place of the
+// logits (ld = 128: the first half of each row's 64 fp32): the eight lanes that write a
+// row are those that have read it, in one wave.
 __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
   const int64_t panel = blockIdx.x / p.blocks, r0 = blockIdx.x % p.blocks * kDzRows;
   const int64_t v0 = panel * kStep + threadIdx.x % 8 * 8;
@@ -309,8 +382,8 @@ __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
     const bool keep = t >= 0 && t < p.V;
     const float c = keep ? p.scale * (p.row_weight ? p.row_weight[m] : 1.0f) : 0.0f;
     const float lse = keep ? p.lse[m] : 0.0f;
-    const int64_t at = (panel * p.rows + m) * kStep + threadIdx.x % 8 * 8;
-    const f32x4* z = reinterpret_cast<const f32x4*>(p.z + at);
+    const int64_t row = panel * p.rows + m, at = row * p.ld + threadIdx.x % 8 * 8;
+    const f32x4* z = reinterpret_cast<const f32x4*>(p.z + row * kStep + threadIdx.x % 8 * 8);
     const f32x4 za = z[0], zb = z[1];
     uint16_t a[8], f, b[8], d[8];  // (dz is finite wherever the loss is: no copy)
 #pragma unroll
@@ -318,7 +391,7 @@ __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
       const float zk = k < 4 ? za[k & 3] : zb[k & 3];
       float g = 0.0f;
       if (keep && v0 + k < p.V) {
-        g = __expf(zk - lse);
+        g = exp_diff(p.scale * zk, lse);
         if (v0 + k == t) g -= 1.0f;
         g *= c;
       }
@@ -387,7 +460,8 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   p.planes = c->io == DENDSN_IO_BF16 ? 1 : 3;
   p.Dp = round_up(c->D, kStep);
   p.Vp = round_up(c->V, kStep);
-  const int64_t per_row = train ? p.Vp * (4 + 2 * p.planes) : ceil_div(c->V, 64) * 8;
+  // a row's logits, with their gradient in their place (fp32: beside them, in planes)
+  const int64_t per_row = train ? p.Vp * (p.planes == 1 ? 4 : 10) : ceil_div(c->V, 64) * 8;
   int64_t most = kPieceBytes / per_row / kBig * kBig;
   if (most < kBig) most = kBig;
   if (most > kMaxPanelRows) most = kMaxPanelRows;
@@ -407,7 +481,7 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   p.splits = 1;
   if (train) {
     p.z = cv.take(size_t(p.rows) * size_t(p.Vp) * 4);
-    p.dz = cv.take(size_t(p.planes) * size_t(p.rows) * size_t(p.Vp) * 2);
+    p.dz = p.planes == 1 ? p.z : cv.take(size_t(p.planes) * size_t(p.rows) * size_t(p.Vp) * 2);
     const int64_t tiles = ceil_div(p.piece, p.tile) * ceil_div(c->D, p.tile);
     const int64_t steps = ceil_div(c->V, kStep) * (p.planes == 3 ? 6 : 1);
     int64_t s = (p.big ? 256 : 512) / tiles;
@@ -427,7 +501,16 @@ void finish(GemmArgs& g, int planes, int tile, int splits) {
   g.tiles_m = int(ceil_div(g.M, tile));
   g.tiles_n = int(ceil_div(g.N, tile));
   g.splits = splits;
-  g.steps = int(ceil_div(g.K, kStep) * (planes == 3 ? 6 : 1));
+  g.per = int(ceil_div(g.K, kStep));
+  g.steps = g.per * (planes == 3 ? 6 : 1);
+  g.each = (g.steps + splits - 1) / splits;
+}
+
+// As many blocks as the 256 CUs hold at a time, a multiple of the eight XCDs: a block's
+// tiles then stay on its XCD.
+unsigned grid_of(const GemmArgs& g, bool big, bool all) {
+  const int64_t units = int64_t(g.tiles_m) * g.tiles_n * g.splits, most = big ? 256 : 512;
+  return unsigned(all || units < most ? units : most);
 }
 
 dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const void* weight, const void* targets,
@@ -468,7 +551,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     l.z = train ? reinterpret_cast<float*>(ws + p.z) : nullptr;
     l.chosen = train ? nullptr : reinterpret_cast<float*>(ws + p.chosen);
     l.targets = tp; l.zrows = p.rows; l.zcols = p.Vp; l.wide = wide;
-    const dim3 lg(unsigned(int64_t(l.g.tiles_m) * l.g.tiles_n));
+    const dim3 lg(grid_of(l.g, p.big, train));
     if (p.big) ce_logits_kernel<256, 256, 2, 4><<<lg, dim3(512), 0, stream>>>(l);
     else ce_logits_kernel<128, 128, 2, 2><<<lg, dim3(256), 0, stream>>>(l);
 
@@ -477,7 +560,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     s.loss = loss + r0;
     float* own_lse = reinterpret_cast<float*>(ws + p.lse);
     s.lse = lse ? lse + r0 : train ? own_lse : nullptr;
-    s.M = M; s.zrows = p.rows; s.V = c->V; s.tiles = l.g.tiles_n; s.wide = wide;
+    s.M = M; s.zrows = p.rows; s.V = c->V; s.scale = c->logit_scale; s.tiles = l.g.tiles_n; s.wide = wide;
     ce_loss_kernel<<<dim3(unsigned(ceil_div(M, kThreads / 64))), dim3(kThreads), 0, stream>>>(s);
     if (!train) continue;
 
@@ -485,18 +568,18 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     z.z = l.z; z.lse = s.lse; z.row_weight = row_weight ? row_weight + r0 : nullptr; z.targets = tp;
     z.dz = reinterpret_cast<uint16_t*>(ws + p.dz);
     z.M = M; z.rows = p.rows; z.blocks = ceil_div(round_up(M, kStep), kDzRows);
-    z.plane = p.rows * p.Vp; z.V = c->V; z.scale = c->logit_scale; z.wide = wide; z.planes = p.planes;
+    z.ld = p.planes == 1 ? 2 * kStep : kStep; z.plane = p.rows * p.Vp; z.V = c->V; z.scale = c->logit_scale; z.wide = wide; z.planes = p.planes;
     ce_dz_kernel<<<dim3(unsigned(z.blocks * (p.Vp / kStep))), dim3(kThreads), 0, stream>>>(z);
 
     GradArgs gh{};
-    gh.g.x = Operand{z.dz, p.rows, z.plane, 0, M, p.Vp};
+    gh.g.x = Operand{z.dz, z.ld, z.plane, 0, M, p.Vp, p.rows};
     gh.g.y = w;
     gh.g.M = M; gh.g.N = c->D; gh.g.K = c->V;
     finish(gh.g, p.planes, p.tile, p.splits);
     gh.out = static_cast<char*>(grad_hidden) + size_t(r0) * size_t(c->ld_grad_hidden) * esz;
     gh.part = reinterpret_cast<float*>(ws + p.dh);
     gh.targets = tp; gh.ld = c->ld_grad_hidden; gh.V = c->V; gh.wide = wide; gh.io = c->io;
-    const dim3 hg(unsigned(int64_t(gh.g.tiles_m) * gh.g.tiles_n), unsigned(p.splits));
+    const dim3 hg(grid_of(gh.g, p.big, false));
     if (p.big) ce_grad_kernel<256, 256, 2, 4, false><<<hg, dim3(512), 0, stream>>>(gh);
     else ce_grad_kernel<128, 128, 2, 2, false><<<hg, dim3(256), 0, stream>>>(gh);
     if (p.splits > 1) {
@@ -505,14 +588,14 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     }
 
     GradArgs gw{};
-    gw.g.x = Operand{z.dz, p.rows, z.plane, 0, M, p.Vp};
+    gw.g.x = Operand{z.dz, z.ld, z.plane, 0, M, p.Vp, p.rows};
     gw.g.y = h;
     gw.g.M = c->V; gw.g.N = c->D; gw.g.K = M;
     finish(gw.g, p.planes, p.tile, 1);
     gw.out = grad_weight; gw.ld = c->ld_grad_weight; gw.io = c->io;
     gw.part = reinterpret_cast<float*>(ws + p.dw);
     gw.add = r0 > 0; gw.keep = r0 + M < c->N;
-    const dim3 wg(unsigned(int64_t(gw.g.tiles_m) * gw.g.tiles_n));
+    const dim3 wg(grid_of(gw.g, p.big, false));
     if (p.big) ce_grad_kernel<256, 256, 2, 4, true><<<wg, dim3(512), 0, stream>>>(gw);
     else ce_grad_kernel<128, 128, 2, 2, true><<<wg, dim3(256), 0, stream>>>(gw);
   }

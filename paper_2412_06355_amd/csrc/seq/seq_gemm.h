@@ -33,15 +33,16 @@ constexpr int kStep = 64;   // k of a stage
 constexpr int kFinite = 3;  // the first plane without infinities, as a plane's number
 
 // An operand as it lies: rows of cols elements, ld apart; or, in panels, columns in
-// groups of 64, each group a [ld][64] matrix of its own (ld: rows of a panel, of which
-// all exist; cols a multiple of 64).  Panels keep what a stage reads of a wide matrix
-// in a few pages, whichever way the product runs.
+// groups of 64, each group a matrix of its own of `height` rows ld apart (all of which
+// exist; cols is a multiple of 64).  Panels keep what a stage reads of a wide matrix in a
+// few pages, whichever way the product runs.
 struct Operand {
   const uint16_t* p;
   int64_t ld;
   int64_t plane;   // elements between planes
   int64_t finite;  // elements from the first plane to its copy without infinities
   int64_t rows, cols;
+  int64_t height;
 };
 
 struct GemmArgs {
@@ -51,6 +52,7 @@ struct GemmArgs {
   int tiles_m, tiles_n;
   int splits;       // blocks along k of a tile
   int steps;        // stages of the whole sum
+  int per, each;    // stages of one product of planes, of a split
 };
 
 // Rows of an operand may be this far apart: a stage's 256 lie within a descriptor.
@@ -71,10 +73,22 @@ __device__ __forceinline__ void block_barrier() {
 // Values that are the same in every lane, put where the compiler sees it (scalar
 // registers): results of divisions are not.
 __device__ __forceinline__ int scalar(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t scalar(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(v)), hi = __builtin_amdgcn_readfirstlane(uint32_t(uint64_t(v) >> 32));
+  return int64_t(uint64_t(hi) << 32 | lo);
+}
 __device__ __forceinline__ const char* scalar(const char* p) {
-  const uint64_t v = reinterpret_cast<uint64_t>(p);
-  const uint32_t lo = __builtin_amdgcn_readfirstlane(uint32_t(v)), hi = __builtin_amdgcn_readfirstlane(uint32_t(v >> 32));
-  return reinterpret_cast<const char*>(uint64_t(hi) << 32 | lo);
+  return reinterpret_cast<const char*>(scalar(reinterpret_cast<int64_t>(p)));
+}
+
+// The kernel's arguments, read again where they are used.  Held from the start of a kernel
+// they would take the scalar registers that its main loop needs.
+template <typename T>
+__device__ __forceinline__ const T& arguments() {
+  typedef const __attribute__((address_space(4))) T* ptr;
+  ptr p = (ptr)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const T*)p;
 }
 
 // One operand's side of a block: R rows (K rows) or columns (K columns) of its stages.
@@ -87,22 +101,16 @@ struct Side {
   static constexpr int kRowBytes = KCOL ? R * 2 : kStep * 2;  // in LDS
   static constexpr uint32_t kRebase = 1u << 29;
 
-  const char *first, *base;
-  int64_t plane, finite;  // bytes between planes, and to the copy of the first one
-  int64_t left, total;    // bytes from base, from first to the operand's end
-  uint32_t step, soff;    // bytes from stage to stage, from base to the stage
+  const char* base;
+  int64_t left;         // bytes from base to the operand's end
+  uint32_t step, soff;  // bytes from stage to stage, from base to the stage
   int records;
   uint32_t off[kLoads];
-  uint32_t tail;          // bit i: load i of a K-rows stage is past the last k in the last stage
+  uint32_t tail;        // bit i: load i of a K-rows stage is past the last k in the last stage
 
-  __device__ __forceinline__ void init(const Operand& o, int64_t r0, int w, int lane) {
-    const int64_t ldb = PANEL ? kStep * 2 : o.ld * 2, panel = o.ld * kStep * 2;
-    plane = o.plane * 2;
-    finite = o.finite * 2;
-    const int64_t at = PANEL ? (KCOL ? r0 / kStep * panel : r0 * ldb) : KCOL ? r0 * 2 : r0 * ldb;
-    first = reinterpret_cast<const char*>(o.p) + at;
-    total = (PANEL ? o.cols / kStep * panel : ((o.rows - 1) * o.ld + o.cols) * 2) - at;
-    step = uint32_t(KCOL ? kStep * ldb : PANEL ? panel : kStep * 2);
+  __device__ __forceinline__ void init(const Operand& o, int w, int lane) {
+    const int64_t ldb = o.ld * 2, panel = o.height * ldb;
+    step = uint32_t(scalar(int(KCOL ? kStep * ldb : PANEL ? panel : kStep * 2)));
     tail = 0;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -118,13 +126,17 @@ struct Side {
   __device__ __forceinline__ void place() {
     const int hi = int(left >> 32);  // (a 64-bit comparison would be a vector instruction)
     const uint32_t lo = uint32_t(left);
-    records = hi < 0 ? 0 : hi > 0 || lo > 0x7FFFFFF0u ? 0x7FFFFFF0 : int(lo);
+    records = scalar(hi < 0 ? 0 : hi > 0 || lo > 0x7FFFFFF0u ? 0x7FFFFFF0 : int(lo));
   }
-  // Goes to stage `s` of plane `pl` (kFinite: of the first one's copy).
-  __device__ __forceinline__ void seek(int pl, int64_t s) {
-    const int64_t skip = s * step;
-    base = first + (pl == kFinite ? finite : pl * plane) + skip;
-    left = total - skip;
+  // Goes to stage `s` of plane `pl` (kFinite: of the first one's copy) at row or column r0.
+  __device__ __forceinline__ void seek(const Operand& o, int r0, int pl, int s) {
+    const int64_t ldb = o.ld * 2, panel = o.height * ldb;
+    const int64_t at = PANEL ? (KCOL ? r0 / kStep * panel : r0 * ldb) : KCOL ? r0 * 2 : r0 * ldb;
+    const int64_t total = PANEL ? (o.cols / kStep - 1) * panel + (o.height - 1) * ldb + kStep * 2
+                                : ((o.rows - 1) * o.ld + o.cols) * 2;
+    const int64_t skip = at + int64_t(s) * step;
+    base = scalar(reinterpret_cast<const char*>(o.p + (pl == kFinite ? o.finite : pl * o.plane)) + skip);
+    left = scalar(total - skip);
     soff = 0;
     place();
 #pragma unroll
@@ -140,15 +152,16 @@ struct Side {
   // The stage that comes is the last of its plane: what lies past the last k is out of
   // every descriptor's reach.
   __device__ __forceinline__ void last() {
+    // (no branch: lanes differ, and with one the loop's uniform state would go to vectors)
 #pragma unroll
     for (int i = 0; i < kLoads; ++i)
-      if (!KCOL && !PANEL && (tail >> i & 1)) off[i] |= 0x80000000u;
+      if (!KCOL && !PANEL) off[i] |= (tail >> i & 1) << 31;
   }
   __device__ __forceinline__ rsrc_t descriptor(bool live) const {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(scalar(base)), 0, scalar(live ? records : 0), 0x00020000);
   }
   __device__ __forceinline__ void fetch(rsrc_t r, char* lds, int i, int w) const {
-    dma16(r, off[i], soff, lds + (w * kLoads + i) * 1024);
+    dma16(r, off[i], scalar(int(soff)), lds + (w * kLoads + i) * 1024);
   }
 };
 
@@ -189,21 +202,20 @@ struct Frags {
   }
 };
 
-// Which tile a block works on: neighbours along the launch order go to the eight
-// XCDs in turn, so each XCD takes a contiguous run of tiles, in groups of eight
-// rows of tiles (the run's operands then fit its L2).
-__device__ __forceinline__ void tile_of(const GemmArgs& g, int64_t id, int& tm, int& tn) {
-  constexpr int kXcd = 8, kGroup = 8;
-  const int64_t tiles = int64_t(g.tiles_m) * g.tiles_n;
-  const int64_t q = tiles / kXcd, rem = tiles % kXcd;
-  const int64_t x = id % kXcd, k = id / kXcd;
-  const int64_t t = x * q + (x < rem ? x : rem) + k;
-  const int64_t width = int64_t(kGroup) * g.tiles_n;
-  const int64_t grp = t / width;
-  const int first = int(grp) * kGroup;
-  const int size = g.tiles_m - first < kGroup ? g.tiles_m - first : kGroup;
-  const int64_t in = t - grp * width;
-  tm = scalar(first + int(in % size));
+// The tile of a unit of work: neighbours go to the eight XCDs in turn, so each XCD takes
+// a contiguous run of tiles, in groups of eight rows of tiles (what the run reads at a
+// time then fits its L2).
+__device__ __forceinline__ void tile_of(const GemmArgs& g, uint32_t id, int& tm, int& tn) {
+  constexpr uint32_t kXcd = 8, kGroup = 8;
+  const uint32_t tiles = uint32_t(g.tiles_m) * uint32_t(g.tiles_n);
+  const uint32_t q = tiles / kXcd, rem = tiles % kXcd;
+  const uint32_t x = id % kXcd, k = id / kXcd;
+  const uint32_t t = x * q + (x < rem ? x : rem) + k;
+  const uint32_t width = kGroup * uint32_t(g.tiles_n);
+  const uint32_t grp = t / width, in = t - grp * width;
+  const uint32_t first = grp * kGroup, left = uint32_t(g.tiles_m) - first;
+  const uint32_t size = left < kGroup ? left : kGroup;
+  tm = scalar(int(first + in % size));
   tn = scalar(int(in / size));
 }
 
@@ -223,87 +235,103 @@ struct Gemm {
   using SY = Side<BN, NW, YCOL, false>;
   static constexpr int kStage = SX::kBytes + SY::kBytes;
   static constexpr int kLoads = SX::kLoads + SY::kLoads;
+  static constexpr int kNotes = WN * BM * 8;  // bytes past the stages for the kernel's own use
   static_assert(FM % 2 == 0 && FN <= FM / 2 * 2, "half of a wave's rounds read all fragments");
 
-  static __device__ __forceinline__ void run(const GemmArgs& g, char* lds, int tm, int tn, int split,
-                                             f32x4 (&acc)[FN][FM]) {
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm = w / WN, wn = w % WN;
-    SX sx;
-    SY sy;
-    sx.init(g.x, int64_t(tm) * BM, w, lane);
-    sy.init(g.y, int64_t(tn) * BN, w, lane);
-    Frags<BM, FM, XCOL> fx;
-    Frags<BN, FN, YCOL> fy;
-    fx.init(wm * TM, lane);
-    fy.init(wn * TN, lane);
+  // (the kernel's arguments begin with the GemmArgs)
+  char* lds;  // two stages
+  int lane, w, per, s0, s1, prod, k, m0, n0;
+  SX sx;
+  SY sy;
+  Frags<BM, FM, XCOL> fx;
+  Frags<BN, FN, YCOL> fy;
+
+  __device__ __forceinline__ explicit Gemm(char* stages) : lds(stages) {
+    const GemmArgs& g = arguments<GemmArgs>();
+    lane = threadIdx.x & 63;
+    w = scalar(int(threadIdx.x >> 6));
+    fx.init(w / WN * TM, lane);
+    fy.init(w % WN * TN, lane);
+    sx.init(g.x, w, lane);
+    sy.init(g.y, w, lane);
+    per = scalar(g.per);
+  }
+
+  // Starts on a tile: its first two stages are on their way.
+  __device__ __forceinline__ void begin(int tm, int tn, int split) {
+    const GemmArgs& g = arguments<GemmArgs>();
+    s0 = scalar(split * g.each);
+    s1 = scalar(min(s0 + g.each, g.steps));
+    prod = scalar(s0 / per);
+    k = s0 - prod * per;
+    m0 = tm * BM;
+    n0 = tn * BN;
+    seek();
+    fetch(sx.descriptor(s0 < s1), sy.descriptor(s0 < s1), lds, 0, kLoads);
+    next();
+    fetch(sx.descriptor(s0 + 1 < s1), sy.descriptor(s0 + 1 < s1), lds + kStage, 0, kLoads);
+    next();
+  }
+
+  __device__ __forceinline__ void seek() {
+    const GemmArgs& g = arguments<GemmArgs>();
+    int px = 0, py = 0;
+    if (g.planes == 3) planes_of(prod, px, py);
+    sx.seek(g.x, m0, px, k);
+    sy.seek(g.y, n0, py, k);
+    if (k == per - 1) sx.last(), sy.last();
+  }
+  __device__ __forceinline__ void next() {
+    ++k;
+    sx.next();
+    sy.next();
+    if (k >= per - 1 || max(sx.soff, sy.soff) >= SX::kRebase) {  // seldom
+      if (k == per) {
+        ++prod;
+        k = 0;
+        if (prod < 6) seek();
+      } else {
+        sx.rebase();
+        sy.rebase();
+        if (k == per - 1) sx.last(), sy.last();
+      }
+    }
+  }
+  // Loads [lo, hi) of a stage.
+  __device__ __forceinline__ void fetch(rsrc_t rx, rsrc_t ry, char* to, int lo, int hi) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if (i < lo || i >= hi) continue;
+      if (i < SX::kLoads) sx.fetch(rx, to, i, w);
+      else sy.fetch(ry, to + SX::kBytes, i - SX::kLoads, w);
+    }
+  }
+  // What round j of FM reads of a half: all of it in the first half of the rounds.
+  __device__ __forceinline__ void read(const char* from, int h, int j, bf16x8 (&xf)[FM], bf16x8 (&yf)[FN]) const {
+    if (j >= FM / 2) return;
 #pragma unroll
     for (int i = 0; i < FN; ++i)
-#pragma unroll
-      for (int j = 0; j < FM; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (i / ((FN + FM / 2 - 1) / (FM / 2)) == j) yf[i] = fy.read(from + SX::kBytes, i, h);
+    xf[2 * j] = fx.read(from, 2 * j, h);
+    xf[2 * j + 1] = fx.read(from, 2 * j + 1, h);
+  }
 
-    const int per = int(ceil_div(g.K, kStep));  // stages of one product of planes
-    const int each = scalar((g.steps + g.splits - 1) / g.splits);
-    const int s0 = split * each, s1 = min(s0 + each, g.steps);
-    int prod = scalar(s0 / per), k = scalar(s0 % per);
-    auto seek = [&]() {
-      int px = 0, py = 0;
-      if (g.planes == 3) planes_of(prod, px, py);
-      sx.seek(px, k);
-      sy.seek(py, k);
-      if (k == per - 1) sx.last(), sy.last();
-    };
-    auto next = [&]() {
-      ++k;
-      sx.next();
-      sy.next();
-      if (k >= per - 1 || max(sx.soff, sy.soff) >= SX::kRebase) {  // seldom
-        if (k == per) {
-          ++prod;
-          k = 0;
-          if (prod < 6) seek();
-        } else {
-          sx.rebase();
-          sy.rebase();
-          if (k == per - 1) sx.last(), sy.last();
-        }
-      }
-    };
-    // loads [lo, hi) of a stage
-    auto fetch = [&](rsrc_t rx, rsrc_t ry, char* to, int lo, int hi) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        if (i < lo || i >= hi) continue;
-        if (i < SX::kLoads) sx.fetch(rx, to, i, w);
-        else sy.fetch(ry, to + SX::kBytes, i - SX::kLoads, w);
-      }
-    };
+  // The tile's product.  Before: this wave's vmcnt was 0 after begin(), and the block met.
+  // After: the stages may be overwritten.
+  __device__ __forceinline__ void run(f32x4 (&acc)[FN][FM]) {
     bf16x8 xa[FM], ya[FN], xb[FM], yb[FN];  // fragments of a stage's first and second 32 k
-    // round j of FM: one row of products, and what the next half needs read
-    auto read = [&](const char* from, int h, int j, bf16x8 (&xf)[FM], bf16x8 (&yf)[FN]) {
-      if (j >= FM / 2) return;
-#pragma unroll
-      for (int i = 0; i < FN; ++i)
-        if (i / ((FN + FM / 2 - 1) / (FM / 2)) == j) yf[i] = fy.read(from + SX::kBytes, i, h);
-      xf[2 * j] = fx.read(from, 2 * j, h);
-      xf[2 * j + 1] = fx.read(from, 2 * j + 1, h);
-    };
     auto multiply = [&](int j, const bf16x8 (&xf)[FM], const bf16x8 (&yf)[FN]) {
 #pragma unroll
       for (int i = 0; i < FN; ++i)
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(yf[i], xf[j], acc[i][j], 0, 0, 0);
     };
-    if (s0 < s1) {
-      seek();
-      fetch(sx.descriptor(true), sy.descriptor(true), lds, 0, kLoads);
-      next();
-      fetch(sx.descriptor(s0 + 1 < s1), sy.descriptor(s0 + 1 < s1), lds + kStage, 0, kLoads);
-      next();
-      __builtin_amdgcn_s_waitcnt(0x0F70 | kLoads);  // the first stage's loads are done
-      block_barrier();
 #pragma unroll
-      for (int j = 0; j < FM / 2; ++j) read(lds, 0, j, xa, ya);
-    }
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+      for (int j = 0; j < FM; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < FM / 2; ++j) read(lds, 0, j, xa, ya);
+#pragma nounroll
     for (int s = s0; s < s1; ++s) {
       char* now = lds + ((s - s0) & 1) * kStage;
       char* then = lds + (~(s - s0) & 1) * kStage;
@@ -313,10 +341,11 @@ struct Gemm {
         multiply(j, xa, ya);
         __builtin_amdgcn_sched_barrier(0);
       }
-      // the next stage is there (vmcnt 0) and this one is in registers (lgkmcnt 0); past the
-      // barrier that holds for every wave, so this stage's place takes the stage after next
-      // (past the last one: nothing, by an empty descriptor)
-      __builtin_amdgcn_s_waitcnt(0x0070);
+      // the next stage is there (vmcnt 0; the tile's second one was before) and this one is
+      // in registers (lgkmcnt 0); past the barrier that holds for every wave, so this stage's
+      // place takes the stage after next (past the last one: nothing, by an empty descriptor)
+      if (s > s0) __builtin_amdgcn_s_waitcnt(0x0070);
+      else __builtin_amdgcn_s_waitcnt(0xC07F);
       block_barrier();
       __builtin_amdgcn_sched_barrier(0);
       const rsrc_t rx = sx.descriptor(s + 2 < s1), ry = sy.descriptor(s + 2 < s1);
@@ -329,9 +358,13 @@ struct Gemm {
       }
       next();
     }
-    __builtin_amdgcn_s_waitcnt(0x0070);  // nothing is in flight: past the barrier, the stages may be reused
+    __builtin_amdgcn_s_waitcnt(0x0070);
     block_barrier();
   }
+
+  // This wave's share of the stages that begin() fetched has landed, and what it wrote to
+  // LDS is there.
+  static __device__ __forceinline__ void landed() { __builtin_amdgcn_s_waitcnt(0x0070); }
 };
 
 }  // namespace dendsn_seq
