@@ -104,6 +104,34 @@ __device__ __forceinline__ float over_groups(float v, F f) {
   return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
+// Each row's maximum and sum of exponentials over a wave's columns n0 + 16 i + 0..3 of its
+// tile (those below N; WHOLE: all of them), times scale >= 0, to to[16 j].
+template <bool WHOLE, int FN, int FM>
+__device__ __forceinline__ void row_statistics(const f32x4 (&acc)[FN][FM], int64_t n0, int64_t N, float scale, float2* to,
+                                               int lane) {
+  const float c = 1.44269504f * scale;
+  const auto in = [&](int i, int r) { return WHOLE || n0 + 16 * i + r < N; };
+#pragma unroll
+  for (int j = 0; j < FM; ++j) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) top = fmaxf(top, in(i, r) ? acc[i][j][r] : -INFINITY);
+    top = over_groups(top, [](float a, float b) { return fmaxf(a, b); });
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        // (the difference first: see exp_diff)
+        sum += in(i, r) ? __builtin_amdgcn_exp2f(c * (acc[i][j][r] - ref)) : 0.0f;
+    sum = over_groups(sum, [](float a, float b) { return a + b; });
+    if (lane < 16) to[16 * j] = make_float2(scale * top, sum);
+  }
+}
+
 // A block takes tiles in turn: the next one's first stages are fetched while it works
 // out this one's statistics.  Where the logits are kept it has one tile: its fetches
 // would wait for its stores (vmcnt counts both, in order), which a new block's do not.
@@ -160,28 +188,14 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_logits_kernel(LogitArgs) {
           if (n0 < p.zcols) *reinterpret_cast<f32x4*>(z + 16 * j * kStep + 16 * i) = acc[i][j];
         }
     }
+    if (scale < 0.0f) {  // the largest logit belongs to the smallest product
 #pragma unroll
-    for (int j = 0; j < G::FM; ++j) {
-      f32x4 t[G::FN];
-      float top = -INFINITY;
+      for (int j = 0; j < G::FM; ++j)
 #pragma unroll
-      for (int i = 0; i < G::FN; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          t[i][r] = acc[i][j][r] * scale;
-          if (!whole && n0 + 16 * i + r >= p.g.N) t[i][r] = -INFINITY;
-          top = fmaxf(top, t[i][r]);
-        }
-      top = over_groups(top, [](float a, float b) { return fmaxf(a, b); });
-      const float ref = top == -INFINITY ? 0.0f : top;
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < G::FN; ++i)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) sum += exp_diff(t[i][r], ref);
-      sum = over_groups(sum, [](float a, float b) { return a + b; });
-      if (lane < 16) part[wn][r0 + 16 * j] = make_float2(top, sum);
+        for (int i = 0; i < G::FN; ++i) acc[i][j] = -acc[i][j];
     }
+    if (whole) row_statistics<true>(acc, n0, p.g.N, fabsf(scale), part[wn] + r0, lane);
+    else row_statistics<false>(acc, n0, p.g.N, fabsf(scale), part[wn] + r0, lane);
     if (id < tiles) G::landed();
     else __builtin_amdgcn_s_waitcnt(0xC07F);  // (lgkmcnt 0: the logits need not have arrived)
     block_barrier();
@@ -384,7 +398,7 @@ __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
     const float lse = keep ? p.lse[m] : 0.0f;
     const int64_t row = panel * p.rows + m, at = row * p.ld + threadIdx.x % 8 * 8;
     const f32x4* z = reinterpret_cast<const f32x4*>(p.z + row * kStep + threadIdx.x % 8 * 8);
-    const f32x4 za = z[0], zb = z[1];
+    const f32x4 za = __builtin_nontemporal_load(z), zb = __builtin_nontemporal_load(z + 1);
     uint16_t a[8], f, b[8], d[8];  // (dz is finite wherever the loss is: no copy)
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
