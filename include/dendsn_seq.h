@@ -173,8 +173,8 @@ dendsn_status dendsn_ce_forward(const dendsn_ce_cfg* cfg, const void* hidden, co
  *   row_weight  [N] fp32          NULL means 1
  *   grad_hidden [N,D] io, grad_weight [V,D] io   required outputs; rows of ignored
  *                                 rows, and of classes with no part, are +0
- * In bf16 the gradient of the logits is rounded to bf16 before the two products
- * that it enters; every sum is fp32.
+ * In bf16 the gradient of the logits, in units of the largest row weight, is
+ * rounded to bf16 before the two products that it enters; every sum is fp32.
  */
 dendsn_status dendsn_ce_train(const dendsn_ce_cfg* cfg, const void* hidden, const void* weight,
                               const void* targets, const float* row_weight, float* loss, float* lse,

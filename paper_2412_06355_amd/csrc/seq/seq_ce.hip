@@ -6,9 +6,9 @@
 // The rows go through in pieces whose logits fit a bounded scratch.  Of a piece, the
 // first product leaves each row's maximum and sum of exponentials over every tile of
 // the vocabulary (and, for the gradient, its fp32 logits); the tiles' statistics are
-// joined into lse; the gradient of the logits is rounded to bf16 once and enters the
-// two other products, dW summed over the pieces in fp32.  The three products carry
-// the time: 2 N V D operations each.
+// joined into lse; the gradient of the logits, without the rows' common factor (see
+// ce_unit_kernel), is rounded to bf16 once and enters the two other products, dW summed
+// over the pieces in fp32.  The three products carry the time: 2 N V D operations each.
 #include "seq_gemm.h"
 
 namespace dendsn_seq {
@@ -216,6 +216,8 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_logits_kernel(LogitArgs) {
 
 struct GradArgs {
   GemmArgs g;
+  const float* unit;     // what dz leaves out (NULL: 1), times scale
+  float scale;
   void* out;             // io
   float* part;           // fp32: [splits][M][N] (splits > 1), or [M][N] summed over pieces
   const void* targets;   // rows without a target are +0 (NULL: none)
@@ -271,6 +273,7 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs) {
     const GradArgs& p = arguments<GradArgs>();
     const uint32_t units = scalar(p.g.tiles_m * p.g.tiles_n * p.g.splits);
     const int64_t N = p.g.N;
+    const float unit = p.unit ? *p.unit * p.scale : p.scale;
     const int64_t m0 = int64_t(tm) * BM + wm * G::TM + (lane & 15);
     const int64_t n0 = int64_t(tn) * BN + wn * G::TN + 4 * (lane >> 4);
     const int this_split = split;
@@ -303,7 +306,7 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs) {
             if (n + r < N) v[r] += p.part[m * N + n + r];
         }
         if (p.keep) store4(p.part, DENDSN_IO_F32, m * N + n, n, N, v);
-        else store4(p.out, p.io, m * p.ld + n, n, N, v);
+        else store4(p.out, p.io, m * p.ld + n, n, N, zero ? v : unit * v);
       }
     }
     if (id >= units) break;
@@ -312,17 +315,20 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs) {
 
 // The splits of a product joined, in their order.
 struct JoinArgs {
-  const float* part;
+  const float *part, *unit;
   void* out;
   int64_t M, N, ld;
+  float scale;
   int splits, io;
 };
 
 __global__ void __launch_bounds__(kThreads) ce_join_splits_kernel(JoinArgs p) {
   const int64_t m = blockIdx.x;
+  const float unit = p.unit ? *p.unit * p.scale : p.scale;
   for (int64_t n = threadIdx.x; n < p.N; n += kThreads) {
     float s = 0.0f;
     for (int k = 0; k < p.splits; ++k) s += p.part[(int64_t(k) * p.M + m) * p.N + n];
+    s = s == 0.0f ? 0.0f : unit * s;
     if (p.io == DENDSN_IO_BF16) static_cast<uint16_t*>(p.out)[m * p.ld + n] = bf16_bits(s);
     else static_cast<float*>(p.out)[m * p.ld + n] = s;
   }
@@ -369,8 +375,36 @@ __global__ void __launch_bounds__(kThreads) ce_loss_kernel(LossArgs p) {
   }
 }
 
+// The largest weight of a row with a target: dz is formed in its units.  Rows of one
+// weight (a mean) would otherwise all carry that number's own rounding to bf16, up to
+// 0.4 % the same way in every sum; in units of it they carry none.
+struct UnitArgs {
+  const float* row_weight;
+  const void* targets;
+  float* unit;
+  int64_t N, V;
+  int wide;
+};
+
+__global__ void __launch_bounds__(1024) ce_unit_kernel(UnitArgs p) {
+  __shared__ float most[16];
+  float top = 0.0f;
+  for (int64_t i = threadIdx.x; i < p.N; i += 1024) {
+    const int64_t t = target_of(p.targets, p.wide, i);
+    if (t >= 0 && t < p.V) top = fmaxf(top, fabsf(p.row_weight[i]));
+  }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  if (threadIdx.x % 64 == 0) most[threadIdx.x / 64] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int q = 1; q < 16; ++q) top = fmaxf(top, most[q]);
+    *p.unit = top > 0.0f && top < INFINITY ? top : 1.0f;
+  }
+}
+
 struct DzArgs {
-  const float *z, *lse, *row_weight;
+  const float *z, *lse, *row_weight, *unit;
   const void* targets;
   uint16_t* dz;
   int64_t M, rows, blocks, plane, V;  // rows of a panel; blocks along the rows
@@ -381,7 +415,7 @@ struct DzArgs {
 
 constexpr int kDzRows = 128;  // rows of a block, of one panel
 
-// dz = r s (exp(z - lse) - onehot); +0 in rows without a target, past V, and in the
+// dz = (r / unit) (exp(s z - lse) - onehot); +0 in rows without a target, past V, and in the
 // rows past M that the last stage of dW's sum reads.  In bf16 dz takes the place of the
 // logits (ld = 128: the first half of each row's 64 fp32): the eight lanes that write a
 // row are those that have read it, in one wave.
@@ -394,7 +428,7 @@ __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
     if (m >= round_up(p.M, kStep)) return;
     const int64_t t = m < p.M ? target_of(p.targets, p.wide, m) : -1;
     const bool keep = t >= 0 && t < p.V;
-    const float c = keep ? p.scale * (p.row_weight ? p.row_weight[m] : 1.0f) : 0.0f;
+    const float c = keep && p.row_weight ? p.row_weight[m] / *p.unit : 1.0f;
     const float lse = keep ? p.lse[m] : 0.0f;
     const int64_t row = panel * p.rows + m, at = row * p.ld + threadIdx.x % 8 * 8;
     const f32x4* z = reinterpret_cast<const f32x4*>(p.z + row * kStep + threadIdx.x % 8 * 8);
@@ -461,7 +495,7 @@ struct Plan {
   bool big;            // 256 x 256 tiles (else 128 x 128)
   int tile;
   int splits;          // of dH
-  size_t h, w, stats, z, dz, chosen, lse, dh, dw, total;
+  size_t h, w, stats, z, dz, chosen, lse, unit, dh, dw, total;
 };
 
 // Operands that the DMA can take as they lie: bf16, 16-byte chunks.
@@ -492,6 +526,7 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   p.stats = cv.take(size_t(p.piece) * size_t(ceil_div(c->V, 64)) * 8);
   p.lse = cv.take(size_t(p.piece) * 4);
   p.chosen = cv.take(size_t(p.piece) * 4);
+  p.unit = cv.take(4);
   p.splits = 1;
   if (train) {
     p.z = cv.take(size_t(p.rows) * size_t(p.Vp) * 4);
@@ -543,6 +578,11 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     else ce_pack_kernel<float><<<dim3(unsigned(c->V)), dim3(kThreads), 0, stream>>>(a);
     w = Operand{a.dst, p.Dp, a.plane, kFinite * a.plane, c->V, p.Dp};
   }
+  float* unit = nullptr;
+  if (train && row_weight) {
+    unit = reinterpret_cast<float*>(ws + p.unit);
+    ce_unit_kernel<<<dim3(1), dim3(1024), 0, stream>>>(UnitArgs{row_weight, targets, unit, c->N, c->V, wide});
+  }
   for (int64_t r0 = 0; r0 < c->N; r0 += p.piece) {
     const int64_t M = c->N - r0 < p.piece ? c->N - r0 : p.piece;
     const void* hp = static_cast<const char*>(hidden) + size_t(r0) * size_t(c->ld_hidden) * esz;
@@ -579,7 +619,8 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     if (!train) continue;
 
     DzArgs z{};
-    z.z = l.z; z.lse = s.lse; z.row_weight = row_weight ? row_weight + r0 : nullptr; z.targets = tp;
+    z.z = l.z; z.lse = s.lse; z.row_weight = row_weight ? row_weight + r0 : nullptr;
+    z.unit = unit; z.targets = tp;
     z.dz = reinterpret_cast<uint16_t*>(ws + p.dz);
     z.M = M; z.rows = p.rows; z.blocks = ceil_div(round_up(M, kStep), kDzRows);
     z.ld = p.planes == 1 ? 2 * kStep : kStep; z.plane = p.rows * p.Vp; z.V = c->V; z.scale = c->logit_scale; z.wide = wide; z.planes = p.planes;
@@ -592,12 +633,13 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     finish(gh.g, p.planes, p.tile, p.splits);
     gh.out = static_cast<char*>(grad_hidden) + size_t(r0) * size_t(c->ld_grad_hidden) * esz;
     gh.part = reinterpret_cast<float*>(ws + p.dh);
+    gh.unit = unit; gh.scale = c->logit_scale;
     gh.targets = tp; gh.ld = c->ld_grad_hidden; gh.V = c->V; gh.wide = wide; gh.io = c->io;
     const dim3 hg(grid_of(gh.g, p.big, false));
     if (p.big) ce_grad_kernel<256, 256, 2, 4, false><<<hg, dim3(512), 0, stream>>>(gh);
     else ce_grad_kernel<128, 128, 2, 2, false><<<hg, dim3(256), 0, stream>>>(gh);
     if (p.splits > 1) {
-      JoinArgs j{gh.part, gh.out, M, c->D, c->ld_grad_hidden, p.splits, c->io};
+      JoinArgs j{gh.part, unit, gh.out, M, c->D, c->ld_grad_hidden, c->logit_scale, p.splits, c->io};
       ce_join_splits_kernel<<<dim3(unsigned(M)), dim3(kThreads), 0, stream>>>(j);
     }
 
@@ -606,6 +648,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     gw.g.y = h;
     gw.g.M = c->V; gw.g.N = c->D; gw.g.K = M;
     finish(gw.g, p.planes, p.tile, 1);
+    gw.unit = unit; gw.scale = c->logit_scale;
     gw.out = grad_weight; gw.ld = c->ld_grad_weight; gw.io = c->io;
     gw.part = reinterpret_cast<float*>(ws + p.dw);
     gw.add = r0 > 0; gw.keep = r0 + M < c->N;
