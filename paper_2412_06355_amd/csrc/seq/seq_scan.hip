@@ -53,9 +53,15 @@ __device__ __forceinline__ void decay(float g, float& a, float& na) {
   }
 }
 
+// VEC values at d of the row that starts `off` elements into an array (off is the same in
+// every lane, d a lane's).
 template <typename IO, int VEC>
-__device__ __forceinline__ Pack<IO, VEC> load_row(const void* base, int64_t off) {
-  return *reinterpret_cast<const Pack<IO, VEC>*>(static_cast<const IO*>(base) + off);
+__device__ __forceinline__ Pack<IO, VEC> load_row(const void* base, int64_t off, int d) {
+  return *reinterpret_cast<const Pack<IO, VEC>*>(static_cast<const IO*>(base) + off + d);
+}
+template <typename IO, int VEC>
+__device__ __forceinline__ void store_row(void* base, int64_t off, int d, const Pack<IO, VEC>& v) {
+  *reinterpret_cast<Pack<IO, VEC>*>(static_cast<IO*>(base) + off + d) = v;
 }
 
 __device__ __forceinline__ int seq_length(const ScanArgs& p, int b) {
@@ -63,52 +69,57 @@ __device__ __forceinline__ int seq_length(const ScanArgs& p, int b) {
   return max(0, min(p.T, p.lengths[b]));
 }
 
+// A barrier for what waves wrote to LDS: loads and stores of global memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt 0
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // Composes the run of one block of the split: (A, B) over its steps, forward
 // (u = w x) or backward (c[t-1] = a[t] (dh[t] + c[t])).
 template <typename IO, int VEC, bool SIG, bool LEAKY, bool BWD>
 __global__ void __launch_bounds__(kW * 64) scan_runs_kernel(ScanArgs p) {
   __shared__ float2 sh[kW][64 * VEC];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = blockIdx.y;
   const int seg = BWD ? int(blockIdx.z) + 1 : int(blockIdx.z);  // the first (last) block's run feeds nobody
-  const int64_t d0 = (int64_t(blockIdx.x) * 64 + lane) * VEC;
+  const int d0 = int((blockIdx.x * 64 + lane) * VEC);
   const bool on = d0 < p.D;
-  const int64_t d = on ? d0 : 0;
+  const int d = on ? d0 : 0;
   const int len = seq_length(p, b);
   const int lo = seg * p.per * kTile, hi = min(min(lo + p.per * kTile, p.T), len);
   // wave w composes the steps [s0, s1)
   const int each = p.per * kL;
   const int s0 = lo + w * each, s1 = min(s0 + each, hi);
-  const int64_t xb = b * (BWD ? p.gh_b : p.x_b) + d, gb = b * p.g_b + d;
+  const int64_t xb = b * (BWD ? p.gh_b : p.x_b), gb = b * p.g_b;
   const void* xs = BWD ? p.gh : p.x;
   const int64_t xt = BWD ? p.gh_t : p.x_t;
   float A[VEC], B[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) A[v] = 1.0f, B[v] = 0.0f;
   const int n = s1 - s0;
-  for (int j0 = 0; j0 < n; j0 += kL) {
+  for (int j0 = 0; j0 < n; j0 += kL) {  // (loads further ahead than this measured no faster)
     Pack<IO, VEC> rx[kL], rg[kL];
 #pragma unroll
     for (int j = 0; j < kL; ++j) {
       const int i = min(j0 + j, n - 1);
       const int64_t t = BWD ? s1 - 1 - i : s0 + i;
-      rx[j] = load_row<IO, VEC>(xs, t * xt + xb);
-      rg[j] = load_row<IO, VEC>(p.g, t * p.g_t + gb);
+      rx[j] = load_row<IO, VEC>(xs, t * xt + xb, d);
+      rg[j] = load_row<IO, VEC>(p.g, t * p.g_t + gb, d);
     }
 #pragma unroll
     for (int j = 0; j < kL; ++j) {
-      if (j0 + j < n) {
+      const bool in = j0 + j < n;
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          float a, na;
-          decay<SIG>(widen(rg[j].v[v]), a, na);
-          const float xv = widen(rx[j].v[v]);
-          if (BWD)
-            B[v] = a * (xv + B[v]);
-          else
-            B[v] = fmaf(a, B[v], LEAKY ? na * xv : xv);
-          A[v] *= a;
-        }
+      for (int v = 0; v < VEC; ++v) {
+        float a, na;
+        decay<SIG>(widen(rg[j].v[v]), a, na);
+        const float xv = widen(rx[j].v[v]);
+        const float next = BWD ? a * (xv + B[v]) : fmaf(a, B[v], LEAKY ? na * xv : xv);
+        B[v] = in ? next : B[v];
+        A[v] = in ? A[v] * a : A[v];
       }
     }
   }
@@ -128,66 +139,81 @@ __global__ void __launch_bounds__(kW * 64) scan_runs_kernel(ScanArgs p) {
   }
 }
 
+// What enters block `to` of the split, from what entered block `from`: the runs between,
+// in the order of `step`, sixteen at a time in flight.
+template <int VEC>
+__device__ __forceinline__ void enter(float (&carry)[VEC], const float2* runs, int64_t lanes, int from, int to, int step) {
+  constexpr int U = 16;
+  for (int s0 = from; s0 != to; s0 += step * min(U, (to - s0) * step)) {
+    float2 r[U][VEC];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = (to - s0) * step > u ? s0 + u * step : s0;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) r[u][v] = runs[s * lanes + v];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if ((to - s0) * step > u)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) carry[v] = fmaf(r[u][v].x, carry[v], r[u][v].y);
+  }
+}
+
 template <typename IO, int VEC, bool SIG, bool LEAKY>
 __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
   __shared__ float2 sh[2][kW][64 * VEC];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = blockIdx.y, seg = blockIdx.z;
-  const int64_t d0 = (int64_t(blockIdx.x) * 64 + lane) * VEC;
+  const int d0 = int((blockIdx.x * 64 + lane) * VEC);
   const bool on = d0 < p.D;
-  const int64_t d = on ? d0 : 0;
+  const int d = on ? d0 : 0;
   const int len = seq_length(p, b);
-  const int64_t xb = b * p.x_b + d, gb = b * p.g_b + d, hb = b * p.h_b + d;
+  const int64_t xb = b * p.x_b, gb = b * p.g_b, hb = b * p.h_b;
   const int64_t bd = int64_t(b) * p.D + d, lanes = int64_t(p.batch) * p.D;
 
   float carry[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) carry[v] = p.h0 ? p.h0[bd + v] : 0.0f;
-  for (int s = 0; s < seg; ++s) {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      const float2 r = p.runs[s * lanes + bd + v];
-      carry[v] = fmaf(r.x, carry[v], r.y);
-    }
-  }
+  enter<VEC>(carry, p.runs + bd, lanes, 0, seg, 1);
 
-  const int k1 = min((seg + 1) * p.per, p.ntiles);
-  Pack<IO, VEC> rx[kL], rg[kL];
-  auto fetch = [&](int k) {  // rows past the end read the last row again
+  const int k0 = seg * p.per, k1 = min(k0 + p.per, p.ntiles);
+  struct Raw {
+    Pack<IO, VEC> x[kL], g[kL];
+  };
+  auto fetch = [&](Raw& r, int k) {  // rows past the end read the last row again
     const int t0 = k * kTile + w * kL;
-    if (t0 < len) {
+    if (k < k1 && t0 < len) {
 #pragma unroll
       for (int j = 0; j < kL; ++j) {
         const int64_t t = min(t0 + j, p.T - 1);
-        rx[j] = load_row<IO, VEC>(p.x, t * p.x_t + xb);
-        rg[j] = load_row<IO, VEC>(p.g, t * p.g_t + gb);
+        r.x[j] = load_row<IO, VEC>(p.x, t * p.x_t + xb, d);
+        r.g[j] = load_row<IO, VEC>(p.g, t * p.g_t + gb, d);
       }
     }
   };
-  fetch(seg * p.per);
-  for (int k = seg * p.per; k < k1; ++k) {
+  // WHOLE: all of the wave's steps belong to the sequence
+  auto tile = [&](auto whole, Raw& raw, int k, int buf) {
+    constexpr bool WHOLE = decltype(whole)::value;
     const int t0 = k * kTile + w * kL;
     float P[kL][VEC], H[kL][VEC];  // the run of the wave's first j + 1 steps
 #pragma unroll
     for (int j = 0; j < kL; ++j) {
+      const bool in = WHOLE || t0 + j < len;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         const float pp = j ? P[j - 1][v] : 1.0f, hp = j ? H[j - 1][v] : 0.0f;
-        P[j][v] = pp;
-        H[j][v] = hp;
-        if (t0 + j < len) {
-          float a, na;
-          decay<SIG>(widen(rg[j].v[v]), a, na);
-          const float xv = widen(rx[j].v[v]);
-          P[j][v] = pp * a;
-          H[j][v] = fmaf(a, hp, LEAKY ? na * xv : xv);
-        }
+        float a, na;
+        decay<SIG>(widen(raw.g[j].v[v]), a, na);
+        const float xv = widen(raw.x[j].v[v]);
+        P[j][v] = in ? pp * a : pp;
+        H[j][v] = in ? fmaf(a, hp, LEAKY ? na * xv : xv) : hp;
       }
     }
-    if (k + 1 < k1) fetch(k + 1);
+    fetch(raw, k + 2);
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) sh[k & 1][w][v * 64 + lane] = make_float2(P[kL - 1][v], H[kL - 1][v]);
-    __syncthreads();
+    for (int v = 0; v < VEC; ++v) sh[buf][w][v * 64 + lane] = make_float2(P[kL - 1][v], H[kL - 1][v]);
+    lds_barrier();
     float in[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
@@ -195,7 +221,7 @@ __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
       in[v] = carry[v];
 #pragma unroll
       for (int q = 0; q < kW; ++q) {
-        const float2 r = sh[k & 1][q][v * 64 + lane];
+        const float2 r = sh[buf][q][v * 64 + lane];
         if (q == w) in[v] = carry[v];
         carry[v] = fmaf(r.x, carry[v], r.y);
       }
@@ -204,16 +230,25 @@ __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
 #pragma unroll
       for (int j = 0; j < kL; ++j) {
         const int t = t0 + j;
-        if (t < p.T) {
-          Pack<IO, VEC> o;
+        Pack<IO, VEC> o;
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) o.v[v] = narrow<IO>(t < len ? fmaf(P[j][v], in[v], H[j][v]) : 0.0f);
-          *reinterpret_cast<Pack<IO, VEC>*>(static_cast<IO*>(p.h) + t * p.h_t + hb) = o;
-        }
+        for (int v = 0; v < VEC; ++v) o.v[v] = narrow<IO>(WHOLE || t < len ? fmaf(P[j][v], in[v], H[j][v]) : 0.0f);
+        if (WHOLE || t < p.T) store_row<IO, VEC>(p.h, t * p.h_t + hb, d, o);
       }
     }
+  };
+  auto either = [&](Raw& raw, int k, int buf) {
+    if (k * kTile + (w + 1) * kL <= len) tile(std::true_type{}, raw, k, buf);
+    else tile(std::false_type{}, raw, k, buf);
+  };
+  Raw ra, rb;  // a tile's loads are two tiles ahead of its use
+  fetch(ra, k0);
+  fetch(rb, k0 + 1);
+  for (int k = k0; k < k1; k += 2) {
+    either(ra, k, 0);
+    if (k + 1 < k1) either(rb, k + 1, 1);
   }
-  if (w == 0 && on && p.h_last && k1 == p.ntiles && seg * p.per < k1) {
+  if (w == 0 && on && p.h_last && k1 == p.ntiles && k0 < k1) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) p.h_last[bd + v] = carry[v];
   }
@@ -222,46 +257,42 @@ __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
 template <typename IO, int VEC, bool SIG, bool LEAKY>
 __global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
   __shared__ float shA[2][kW][64 * VEC], shH[2][kW][64 * VEC], shC[2][kW][64 * VEC];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = blockIdx.y, seg = blockIdx.z;
-  const int64_t d0 = (int64_t(blockIdx.x) * 64 + lane) * VEC;
+  const int d0 = int((blockIdx.x * 64 + lane) * VEC);
   const bool on = d0 < p.D;
-  const int64_t d = on ? d0 : 0;
+  const int d = on ? d0 : 0;
   const int len = seq_length(p, b);
-  const int64_t xb = b * p.x_b + d, gb = b * p.g_b + d, ghb = b * p.gh_b + d;
-  const int64_t gxb = b * p.gx_b + d, ggb = b * p.gg_b + d;
+  const int64_t xb = b * p.x_b, gb = b * p.g_b, ghb = b * p.gh_b, gxb = b * p.gx_b, ggb = b * p.gg_b;
   const int64_t bd = int64_t(b) * p.D + d, lanes = int64_t(p.batch) * p.D;
 
   float carry[VEC];  // c of the tile's last step
 #pragma unroll
   for (int v = 0; v < VEC; ++v) carry[v] = p.gh_last ? p.gh_last[bd + v] : 0.0f;
-  for (int s = gridDim.z - 1; s > seg; --s) {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      const float2 r = p.runs[s * lanes + bd + v];
-      carry[v] = fmaf(r.x, carry[v], r.y);
-    }
-  }
+  enter<VEC>(carry, p.runs + bd, lanes, int(gridDim.z) - 1, seg, -1);
 
   const int k0 = seg * p.per, k1 = min(k0 + p.per, p.ntiles);
-  Pack<IO, VEC> rx[kL], rg[kL], rh[kL];
-  float start[VEC];
-  auto fetch = [&](int k) {
+  struct Raw {
+    Pack<IO, VEC> x[kL], g[kL], h[kL];
+    float start[VEC];
+  };
+  auto fetch = [&](Raw& r, int k) {
+    if (k < k0) return;
     const int t0 = k * kTile + w * kL;
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) start[v] = p.ckpt_in[int64_t(k) * lanes + bd + v];
+    for (int v = 0; v < VEC; ++v) r.start[v] = p.ckpt_in[int64_t(k) * lanes + bd + v];
     if (t0 < len) {
 #pragma unroll
       for (int j = 0; j < kL; ++j) {
         const int64_t t = min(t0 + j, p.T - 1);
-        rx[j] = load_row<IO, VEC>(p.x, t * p.x_t + xb);
-        rg[j] = load_row<IO, VEC>(p.g, t * p.g_t + gb);
-        rh[j] = load_row<IO, VEC>(p.gh, t * p.gh_t + ghb);
+        r.x[j] = load_row<IO, VEC>(p.x, t * p.x_t + xb, d);
+        r.g[j] = load_row<IO, VEC>(p.g, t * p.g_t + gb, d);
+        r.h[j] = load_row<IO, VEC>(p.gh, t * p.gh_t + ghb, d);
       }
     }
   };
-  if (k0 < k1) fetch(k1 - 1);
-  for (int k = k1 - 1; k >= k0; --k) {
+  auto tile = [&](auto whole, Raw& raw, int k, int buf) {
+    constexpr bool WHOLE = decltype(whole)::value;
     const int t0 = k * kTile + w * kL;
     float a[kL][VEC], na[kL][VEC], x[kL][VEC], dh[kL][VEC];
     float A[VEC], H[VEC], C[VEC];
@@ -271,13 +302,13 @@ __global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
     for (int j = 0; j < kL; ++j) {
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        a[j][v] = 1.0f;
-        na[j][v] = x[j][v] = dh[j][v] = 0.0f;
-        if (t0 + j < len) {
-          decay<SIG>(widen(rg[j].v[v]), a[j][v], na[j][v]);
-          x[j][v] = widen(rx[j].v[v]);
-          dh[j][v] = widen(rh[j].v[v]);
-        }
+        const bool in = WHOLE || t0 + j < len;
+        float av, nav;
+        decay<SIG>(widen(raw.g[j].v[v]), av, nav);
+        a[j][v] = in ? av : 1.0f;
+        na[j][v] = in ? nav : 0.0f;
+        x[j][v] = in ? widen(raw.x[j].v[v]) : 0.0f;
+        dh[j][v] = in ? widen(raw.h[j].v[v]) : 0.0f;
         A[v] *= a[j][v];
         H[v] = fmaf(a[j][v], H[v], LEAKY ? na[j][v] * x[j][v] : x[j][v]);
       }
@@ -287,17 +318,16 @@ __global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
 #pragma unroll
       for (int v = 0; v < VEC; ++v) C[v] = a[j][v] * (dh[j][v] + C[v]);
     }
-    const int buf = k & 1;
     float hin[VEC], cin[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      hin[v] = start[v];
+      hin[v] = raw.start[v];
       shA[buf][w][v * 64 + lane] = A[v];
       shH[buf][w][v * 64 + lane] = H[v];
       shC[buf][w][v * 64 + lane] = C[v];
     }
-    if (k > k0) fetch(k - 1);
-    __syncthreads();
+    fetch(raw, k - 1);
+    lds_barrier();
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
 #pragma unroll
@@ -329,15 +359,22 @@ __global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
         cin[v] = a[j][v] * lam;
         float da = lam * (LEAKY ? before[j][v] - x[j][v] : before[j][v]);
         if (SIG) da *= a[j][v] * na[j][v];
-        ox.v[v] = narrow<IO>(t < len ? (LEAKY ? na[j][v] * lam : lam) : 0.0f);
-        og.v[v] = narrow<IO>(t < len ? da : 0.0f);
+        ox.v[v] = narrow<IO>(WHOLE || t < len ? (LEAKY ? na[j][v] * lam : lam) : 0.0f);
+        og.v[v] = narrow<IO>(WHOLE || t < len ? da : 0.0f);
       }
-      if (on && t < p.T) {
-        *reinterpret_cast<Pack<IO, VEC>*>(static_cast<IO*>(p.gx) + t * p.gx_t + gxb) = ox;
-        *reinterpret_cast<Pack<IO, VEC>*>(static_cast<IO*>(p.gg) + t * p.gg_t + ggb) = og;
+      if (on && (WHOLE || t < p.T)) {
+        store_row<IO, VEC>(p.gx, t * p.gx_t + gxb, d, ox);
+        store_row<IO, VEC>(p.gg, t * p.gg_t + ggb, d, og);
       }
     }
-  }
+  };
+  auto either = [&](Raw& raw, int k, int buf) {
+    if (k * kTile + (w + 1) * kL <= len) tile(std::true_type{}, raw, k, buf);
+    else tile(std::false_type{}, raw, k, buf);
+  };
+  Raw raw;  // (two tiles ahead, as in the forward, the registers do not reach)
+  fetch(raw, k1 - 1);
+  for (int k = k1 - 1; k >= k0; --k) either(raw, k, k & 1);
   if (w == 0 && on && p.gh0 && seg == 0) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) p.gh0[bd + v] = carry[v];
@@ -365,7 +402,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(StepArgs p) {
 #pragma unroll
   for (int v = 0; v < VEC; ++v) o.v[v] = narrow<IO>(0.0f);
   if (live) {
-    const Pack<IO, VEC> rx = load_row<IO, VEC>(p.x, b * p.x_b + d), rg = load_row<IO, VEC>(p.g, b * p.g_b + d);
+    const Pack<IO, VEC> rx = load_row<IO, VEC>(p.x, b * p.x_b, int(d)), rg = load_row<IO, VEC>(p.g, b * p.g_b, int(d));
     auto* st = reinterpret_cast<Pack<float, VEC>*>(p.state + slot * p.D + d);
     Pack<float, VEC> s = *st;
 #pragma unroll
@@ -428,9 +465,9 @@ struct Plan {
   int ntiles, per, S;
 };
 
-// Lanes of two channels where every row allows it (4 or 8 bytes a lane).  The
-// steps are split while the chip is not full: kFill blocks of eight waves.
-constexpr int64_t kFill = 1024;
+// Lanes of two channels where every row allows it (4 or 8 bytes a lane).  With fewer
+// blocks than CUs the steps are split, to kFill blocks.
+constexpr int64_t kCus = 256, kFill = 512;
 
 Plan make_plan(const dendsn_scan_cfg* c, bool wide) {
   Plan p;
@@ -438,7 +475,7 @@ Plan make_plan(const dendsn_scan_cfg* c, bool wide) {
   p.groups = ceil_div(c->D, 64 * p.vec);
   p.ntiles = int(ceil_div(c->T, kTile));
   const int64_t blocks = p.groups * c->batch;
-  int64_t S = blocks >= kFill / 2 ? 1 : ceil_div(kFill, blocks);
+  int64_t S = blocks >= kCus ? 1 : ceil_div(kFill, blocks);
   S = S < kMaxSplit ? S : kMaxSplit;
   // a block of the split has two tiles at least
   S = S < p.ntiles / 2 ? S : p.ntiles / 2;

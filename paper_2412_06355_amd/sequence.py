@@ -15,7 +15,7 @@ import ctypes
 import dataclasses
 from dataclasses import dataclass
 
-from .binding import IO, DendSNError, _ptr, _stream
+from .binding import IO, DendSNError
 from .binding import lib as _lib
 
 GATE = {"sigmoid": 0, "decay": 1}
@@ -78,6 +78,19 @@ def seq_lib():
 def _check(status: int):
     if status != 0:
         raise DendSNError(status, seq_lib().dendsn_seq_last_error().decode())
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _stream(device):
+    """The current stream of the device: a serving step's calls are a few microseconds long, so
+    the handle is asked for without building a Stream object."""
+    import torch
+
+    return torch._C._cuda_getCurrentRawStream(device.index if device.index is not None else
+                                              torch.cuda.current_device())
 
 
 def dendsn_seq_last_error() -> str:
