@@ -214,6 +214,124 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_logits_kernel(LogitArgs) {
   }
 }
 
+// ---------------------------------------------------------------------------
+// Few rows: the weights are streamed once
+// ---------------------------------------------------------------------------
+struct ScoreArgs {
+  const void *h, *w;
+  const void* targets;
+  float2* stats;   // [M][gridDim.x]
+  float* chosen;   // [M]
+  int64_t ldh, ldw, M, V, K;
+  float scale;
+  int wide;
+};
+
+constexpr int kScoreWaves = 8;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes a lane of either operand: 32 k of bf16, or four times 4 k of fp32.
+template <typename IO>
+__device__ __forceinline__ f32x4 multiply16(u32x4 a, u32x4 b, f32x4 acc) {
+  if constexpr (sizeof(IO) == 2) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a[k]), __uint_as_float(b[k]), acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+// A block takes V / gridDim.x classes, sixteen at a time; wave w takes the k of its U
+// units of 64 (lane group q the 16 k from 16 q on, in both operands, so that whole lines of
+// the weights are read at once).  The rows of hidden, MF times sixteen, stay in
+// registers; the waves' sums meet in LDS, where wave f keeps the statistics of rows
+// 16 f .. 16 f + 15.  Bound by the weights' bytes: two groups of classes are in flight.
+template <typename IO, int MF, int U>
+__global__ void __launch_bounds__(kScoreWaves * 64) ce_score_kernel(ScoreArgs p) {
+  constexpr int E = 16 / sizeof(IO), L = 16 / E;  // values of a load, loads of a unit
+  __shared__ f32x4 part[2][kScoreWaves][MF][64];
+  const int lane = threadIdx.x & 63, w = scalar(int(threadIdx.x >> 6)), i = lane & 15, q = lane >> 4;
+  const int64_t n0 = p.V * blockIdx.x / gridDim.x, n1 = p.V * (blockIdx.x + 1) / gridDim.x;
+  const int k0 = w * U * kStep + q * 16;
+  u32x4 hf[MF][L * U];
+#pragma unroll
+  for (int f = 0; f < MF; ++f)
+#pragma unroll
+    for (int e = 0; e < L * U; ++e) {
+      const int k = k0 + e / L * kStep + e % L * E;
+      const int64_t m = 16 * f + i;
+      hf[f][e] = u32x4{0, 0, 0, 0};
+      if (m < p.M && k < p.K) hf[f][e] = *reinterpret_cast<const u32x4*>(static_cast<const IO*>(p.h) + m * p.ldh + k);
+    }
+  struct Group {
+    u32x4 v[L * U];
+  };
+  auto fetch = [&](Group& g, int64_t n) {  // classes n .. n + 15; past n1 and past K: zero
+    const int64_t rows = n1 - n;
+    const int64_t bytes = rows > 0 ? ((rows - 1) * p.ldw + p.K) * int64_t(sizeof(IO)) : 0;
+    const int records = scalar(int(bytes < 0x7FFFFFF0 ? bytes : 0x7FFFFFF0));
+    const rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<char*>(scalar(reinterpret_cast<const char*>(static_cast<const IO*>(p.w) + n * p.ldw))), 0, records, 0x00020000);
+#pragma unroll
+    for (int e = 0; e < L * U; ++e) {
+      const int k = k0 + e / L * kStep + e % L * E;
+      const uint32_t off = k < p.K && i < rows ? uint32_t(i * p.ldw + k) * uint32_t(sizeof(IO)) : 0x80000000u;
+      g.v[e] = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+    }
+  };
+  float top = -INFINITY, sum = 0.0f;
+  const int64_t m = 16 * w + i;  // (of a wave below MF)
+  const int64_t target = w < MF && m < p.M ? target_of(p.targets, p.wide, m) : -1;
+  auto group = [&](Group& g, int64_t n, int buf) {
+    f32x4 acc[MF];
+#pragma unroll
+    for (int f = 0; f < MF; ++f) acc[f] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int e = 0; e < L * U; ++e)
+#pragma unroll
+      for (int f = 0; f < MF; ++f) acc[f] = multiply16<IO>(g.v[e], hf[f][e], acc[f]);
+    fetch(g, n + 32);
+#pragma unroll
+    for (int f = 0; f < MF; ++f) part[buf][w][f][lane] = acc[f];
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt 0
+    block_barrier();
+    if (w < MF) {
+      f32x4 z = part[buf][0][w][lane];
+#pragma unroll
+      for (int o = 1; o < kScoreWaves; ++o) z += part[buf][o][w][lane];
+      float most = top;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t v = n + 4 * q + r;
+        if (v == target && v < n1) p.chosen[m] = z[r];  // (past n1: another block's)
+        z[r] = v < n1 ? p.scale * z[r] : -INFINITY;
+        most = fmaxf(most, z[r]);
+      }
+      const float ref = most == -INFINITY ? 0.0f : most;
+      sum *= exp_diff(top, ref);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) sum += exp_diff(z[r], ref);
+      top = most;
+    }
+  };
+  Group ga, gb;
+  fetch(ga, n0);
+  fetch(gb, n0 + 16);
+  for (int64_t n = n0; n < n1; n += 32) {
+    group(ga, n, 0);
+    if (n + 16 < n1) group(gb, n + 16, 1);
+  }
+  if (w < MF) {
+    const float most = over_groups(top, [](float a, float b) { return fmaxf(a, b); });
+    const float ref = most == -INFINITY ? 0.0f : most;
+    sum = over_groups(sum * exp_diff(top, ref), [](float a, float b) { return a + b; });
+    if (lane < 16 && m < p.M) p.stats[m * gridDim.x + blockIdx.x] = make_float2(most, sum);
+  }
+}
+
 struct GradArgs {
   GemmArgs g;
   const float* unit;     // what dz leaves out (NULL: 1), times scale
@@ -498,9 +616,15 @@ struct Plan {
   size_t h, w, stats, z, dz, chosen, lse, unit, dh, dw, total;
 };
 
-// Operands that the DMA can take as they lie: bf16, 16-byte chunks.
+// Rows that can be read in chunks of 16 bytes, near enough for a descriptor.
+bool rows16(const dendsn_ce_cfg* c, const void* p, int64_t ld) {
+  const int64_t m = c->io == DENDSN_IO_BF16 ? 8 : 4;
+  return aligned(p, 16) && c->D % m == 0 && ld % m == 0 && ld <= kMaxLd;
+}
+
+// Operands that the DMA can take as they lie.
 bool direct(const dendsn_ce_cfg* c, const void* p, int64_t ld) {
-  return c->io == DENDSN_IO_BF16 && aligned(p, 16) && c->D % 8 == 0 && ld % 8 == 0 && ld <= kMaxLd;
+  return c->io == DENDSN_IO_BF16 && rows16(c, p, ld);
 }
 
 Plan make_plan(const dendsn_ce_cfg* c, bool train) {
@@ -555,6 +679,30 @@ void finish(GemmArgs& g, int planes, int tile, int splits) {
   g.each = (g.steps + splits - 1) / splits;
 }
 
+// The kernel for few rows, if one is made for these sizes: MF times sixteen rows, U units
+// of 64 k a wave, as far as the registers reach.  2048 features, 50001 classes in bf16: 8
+// rows 33 us, 32 rows 35 us; the tiles, which split no sum over k, 53 and 41 us (and fp32
+// would be laid out in planes first).
+template <typename IO>
+bool launch_score(const ScoreArgs& a, unsigned grid, hipStream_t stream) {
+  constexpr bool BF = sizeof(IO) == 2;
+  const int64_t mf = ceil_div(a.M, 16), u = ceil_div(a.K, kStep * kScoreWaves);
+  const dim3 g(grid), b(kScoreWaves * 64);
+#define DENDSN_SCORE(MF, U)                                 \
+  if (mf <= MF && u <= U) {                                 \
+    ce_score_kernel<IO, MF, U><<<g, b, 0, stream>>>(a);     \
+    return true;                                            \
+  }
+  DENDSN_SCORE(1, 1) DENDSN_SCORE(1, 2) DENDSN_SCORE(1, 4)
+  DENDSN_SCORE(2, 1) DENDSN_SCORE(2, 2)
+  DENDSN_SCORE(4, 1)
+  if constexpr (BF) {
+    DENDSN_SCORE(1, 8) DENDSN_SCORE(2, 4) DENDSN_SCORE(4, 2)
+  }
+#undef DENDSN_SCORE
+  return false;
+}
+
 // As many blocks as the 256 CUs hold at a time, a multiple of the eight XCDs: a block's
 // tiles then stay on its XCD.
 unsigned grid_of(const GemmArgs& g, bool big, bool all) {
@@ -569,6 +717,19 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
   const int wide = c->index == DENDSN_INDEX_I64;
   const size_t isz = wide ? 8 : 4;
   const bool bf = c->io == DENDSN_IO_BF16;
+  if (!train && rows16(c, hidden, c->ld_hidden) && rows16(c, weight, c->ld_weight)) {
+    // at most as many blocks as there is room for statistics, a CU each
+    const int64_t blocks = ceil_div(c->V, kStep) < 256 ? ceil_div(c->V, kStep) : 256;
+    const ScoreArgs a{hidden, weight, targets, reinterpret_cast<float2*>(ws + p.stats), reinterpret_cast<float*>(ws + p.chosen),
+                      c->ld_hidden, c->ld_weight, c->N, c->V, c->D, c->logit_scale, wide};
+    if (bf ? launch_score<bf16_t>(a, unsigned(blocks), stream) : launch_score<float>(a, unsigned(blocks), stream)) {
+      LossArgs s{};
+      s.stats = a.stats; s.chosen = a.chosen; s.targets = targets; s.loss = loss; s.lse = lse;
+      s.M = c->N; s.V = c->V; s.scale = c->logit_scale; s.tiles = int(blocks); s.wide = wide;
+      ce_loss_kernel<<<dim3(unsigned(ceil_div(c->N, kThreads / 64))), dim3(kThreads), 0, stream>>>(s);
+      return launched("linear cross entropy");
+    }
+  }
   Operand w{};
   if (direct(c, weight, c->ld_weight)) {
     w = Operand{static_cast<const uint16_t*>(weight), c->ld_weight, 0, 0, c->V, c->D};

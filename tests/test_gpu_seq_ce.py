@@ -64,6 +64,28 @@ def test_large_tiles(gpu_device, N, V, D, io):
     check(cfg, *make(N, V, D, io, gpu_device, N))
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V,D", [(1, 1003, 520), (9, 700, 1024), (16, 65, 2048), (5, 517, 4096), (8, 300, 1504),
+                                   (17, 999, 512), (32, 1500, 904), (25, 640, 2000), (33, 2001, 512), (64, 1030, 1016),
+                                   (7, 350, 4608), (3, 20000, 128), (50, 90, 64)])
+def test_few_rows(gpu_device, N, V, D, io):
+    """The losses of few rows, around sixteens of rows, 512 features and shares of the classes;
+    rows that lie apart and, beside them, unaligned ones."""
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    h, w, t, _ = make(N, V, D, io, gpu_device, V)
+    announce(f"ce few rows {cfg}")
+    ref = seq_ref.ce(h, w, t, 1.0, io, train=False)
+    wide = torch.full((V, D + 16), float("nan"), dtype=w.dtype, device=gpu_device)
+    odd = torch.full((V, D + 1), float("nan"), dtype=w.dtype, device=gpu_device)
+    wide[:, 8:D + 8], odd[:, 1:] = w, w
+    for weight in (w, wide[:, 8:D + 8], odd[:, 1:]):
+        loss, lse = dendsn.linear_ce(cfg, h, weight, t)
+        seq_ref.assert_within(loss, *ref["loss"], "loss")
+        seq_ref.assert_within(lse, *ref["lse"], "lse")
+    again, _ = dendsn.linear_ce(cfg, h, odd[:, 1:], t)
+    assert torch.equal(again, loss)
+
+
 def test_pieces_of_rows(gpu_device):
     """More rows than the scratch holds logits of: the pieces' gradients of the weights add up."""
     N, V, D = 6000, 131072, 16
