@@ -50,28 +50,57 @@ __device__ __forceinline__ void split3(float v, uint16_t& a, uint16_t& finite, u
   c = uint16_t(__float_as_uint(r2) >> 16);
 }
 
-template <typename IO>
+__device__ __forceinline__ void store8(uint16_t* to, const uint16_t (&x)[8]) {
+  uint4 q;
+  q.x = x[0] | uint32_t(x[1]) << 16;
+  q.y = x[2] | uint32_t(x[3]) << 16;
+  q.z = x[4] | uint32_t(x[5]) << 16;
+  q.w = x[6] | uint32_t(x[7]) << 16;
+  *reinterpret_cast<uint4*>(to) = q;
+}
+
+// Eight values a thread; WIDE: 16-byte reads (the rows allow them).
+template <typename IO, bool WIDE>
 __global__ void __launch_bounds__(kThreads) ce_pack_kernel(PackArgs p) {
-  const int64_t row = blockIdx.x;
+  constexpr int E = 16 / sizeof(IO);
+  const int64_t chunks = p.cols_p / 8, id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  const int64_t row = id / chunks, d = id % chunks * 8;
+  if (row >= p.rows) return;
   bool keep = true;
   if (p.targets) {
     const int64_t t = target_of(p.targets, p.wide, row);
     keep = t >= 0 && t < p.V;
   }
-  const IO* src = static_cast<const IO*>(p.src) + row * p.ld;
-  uint16_t* dst = p.dst + row * p.cols_p;
-  for (int64_t d = threadIdx.x; d < p.cols_p; d += kThreads) {
-    const float v = keep && d < p.cols ? widen(src[d]) : 0.0f;
-    if (p.planes == 1) {
-      dst[d] = bf16_bits(v);
-    } else {
-      uint16_t a, f, b, c;
-      split3(v, a, f, b, c);
-      dst[d] = a;
-      dst[p.plane + d] = b;
-      dst[2 * p.plane + d] = c;
-      dst[kFinite * p.plane + d] = f;
+  const IO* src = static_cast<const IO*>(p.src) + row * p.ld + d;
+  float v[8] = {};
+  if (keep) {
+#pragma unroll
+    for (int e = 0; e < 8; e += E) {
+      if (WIDE) {  // (cols is a multiple of E)
+        if (d + e < p.cols) {
+          const auto x = *reinterpret_cast<const Pack<IO, E>*>(src + e);
+#pragma unroll
+          for (int k = 0; k < E; ++k) v[e + k] = widen(x.v[k]);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+          if (d + e + k < p.cols) v[e + k] = widen(src[e + k]);
+      }
     }
+  }
+  uint16_t* dst = p.dst + row * p.cols_p + d;
+  uint16_t a[8], f[8], b[8], c[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    if (p.planes == 1) a[k] = bf16_bits(v[k]);
+    else split3(v[k], a[k], f[k], b[k], c[k]);
+  }
+  store8(dst, a);
+  if (p.planes == 3) {
+    store8(dst + p.plane, b);
+    store8(dst + 2 * p.plane, c);
+    store8(dst + kFinite * p.plane, f);
   }
 }
 
@@ -440,15 +469,32 @@ struct JoinArgs {
   int splits, io;
 };
 
+// VEC: values of a thread (4 where N is a multiple of it).
+template <int VEC>
 __global__ void __launch_bounds__(kThreads) ce_join_splits_kernel(JoinArgs p) {
-  const int64_t m = blockIdx.x;
+  const int64_t at = (int64_t(blockIdx.x) * kThreads + threadIdx.x) * VEC;
+  if (at >= p.M * p.N) return;
   const float unit = p.unit ? *p.unit * p.scale : p.scale;
-  for (int64_t n = threadIdx.x; n < p.N; n += kThreads) {
-    float s = 0.0f;
-    for (int k = 0; k < p.splits; ++k) s += p.part[(int64_t(k) * p.M + m) * p.N + n];
-    s = s == 0.0f ? 0.0f : unit * s;
-    if (p.io == DENDSN_IO_BF16) static_cast<uint16_t*>(p.out)[m * p.ld + n] = bf16_bits(s);
-    else static_cast<float*>(p.out)[m * p.ld + n] = s;
+  const float* from = p.part + at;
+  float s[VEC] = {};
+  constexpr int U = 8;  // loads in flight
+  for (int k0 = 0; k0 < p.splits; k0 += U) {
+    Pack<float, VEC> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      v[u] = *reinterpret_cast<const Pack<float, VEC>*>(from + int64_t(min(k0 + u, p.splits - 1)) * p.M * p.N);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + u < p.splits)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s[e] += v[u].v[e];
+  }
+  const int64_t to = at / p.N * p.ld + at % p.N;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    const float g = s[e] == 0.0f ? 0.0f : unit * s[e];
+    if (p.io == DENDSN_IO_BF16) static_cast<uint16_t*>(p.out)[to + e] = bf16_bits(g);
+    else static_cast<float*>(p.out)[to + e] = g;
   }
 }
 
@@ -564,16 +610,8 @@ __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
       if (p.planes == 1) a[k] = bf16_bits(g);
       else split3(g, a[k], f, b[k], d[k]);
     }
-    auto put = [&](uint16_t* to, const uint16_t (&x)[8]) {
-      uint4 q;
-      q.x = x[0] | uint32_t(x[1]) << 16;
-      q.y = x[2] | uint32_t(x[3]) << 16;
-      q.z = x[4] | uint32_t(x[5]) << 16;
-      q.w = x[6] | uint32_t(x[7]) << 16;
-      *reinterpret_cast<uint4*>(to + at) = q;
-    };
-    put(p.dz, a);
-    if (p.planes == 3) put(p.dz + p.plane, b), put(p.dz + 2 * p.plane, d);
+    store8(p.dz + at, a);
+    if (p.planes == 3) store8(p.dz + p.plane + at, b), store8(p.dz + 2 * p.plane + at, d);
   }
 }
 
@@ -610,9 +648,8 @@ struct Plan {
   int planes;
   int64_t Dp, Vp;      // rows of packed operands, of logits
   int64_t piece, pieces, rows;  // rows: of a panel
-  bool big;            // 256 x 256 tiles (else 128 x 128)
-  int tile;
-  int splits;          // of dH
+  int logits, dh_tile, dw_tile;  // tiles of the products: 256 x 256 or 128 x 128
+  int splits;                    // of dH
   size_t h, w, stats, z, dz, chosen, lse, unit, dh, dw, total;
 };
 
@@ -625,6 +662,17 @@ bool rows16(const dendsn_ce_cfg* c, const void* p, int64_t ld) {
 // Operands that the DMA can take as they lie.
 bool direct(const dendsn_ce_cfg* c, const void* p, int64_t ld) {
   return c->io == DENDSN_IO_BF16 && rows16(c, p, ld);
+}
+
+// The tile of a product of M x N.  A CU works through a 256 tile at 0.6 of the time of
+// four 128 tiles (its fragments are read from LDS half as often): in units of one 256 tile
+// a CU, rounds of 256 tiles against 0.4 a round of 128 tiles.  Measured, 1024 x 10000 x
+// 512 in fp32 (160 tiles of 256 or 632 of 128): logits 78 us against 107; dW (80 or 316)
+// 138 us against 115.
+int tile_for(int64_t M, int64_t N) {
+  const int64_t big = ceil_div(ceil_div(M, 256) * ceil_div(N, 256), 256);
+  const int64_t small = ceil_div(ceil_div(M, 128) * ceil_div(N, 128), 256);
+  return 5 * big <= 2 * small ? 256 : 128;
 }
 
 Plan make_plan(const dendsn_ce_cfg* c, bool train) {
@@ -642,8 +690,7 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   p.piece = p.pieces > 1 ? round_up(ceil_div(N, p.pieces), kBig) : N;
   p.pieces = ceil_div(N, p.piece);
   p.rows = round_up(p.piece, kBig);
-  p.big = ceil_div(p.piece, kBig) * ceil_div(c->V, kBig) >= 256;
-  p.tile = p.big ? kBig : 128;
+  p.logits = tile_for(p.piece, c->V);
   Carve cv;
   p.h = cv.take(size_t(p.planes == 3 ? 4 : 1) * size_t(p.piece) * size_t(p.Dp) * 2);
   p.w = cv.take(size_t(p.planes == 3 ? 4 : 1) * size_t(c->V) * size_t(p.Dp) * 2);
@@ -655,11 +702,16 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   if (train) {
     p.z = cv.take(size_t(p.rows) * size_t(p.Vp) * 4);
     p.dz = p.planes == 1 ? p.z : cv.take(size_t(p.planes) * size_t(p.rows) * size_t(p.Vp) * 2);
-    const int64_t tiles = ceil_div(p.piece, p.tile) * ceil_div(c->D, p.tile);
+    p.dw_tile = tile_for(c->V, c->D);
+    // dH's sum over the classes is split until the chip is full, by 32 parts of eight
+    // stages at most: the larger tiles where those fill it (2048 x 30000 x 512 fp32: 353 us
+    // against 463; but 1024 x 10000 x 512 bf16, 152 blocks, 28 us against 25)
     const int64_t steps = ceil_div(c->V, kStep) * (p.planes == 3 ? 6 : 1);
-    int64_t s = (p.big ? 256 : 512) / tiles;
-    if (s > steps / 8) s = steps / 8;
-    if (s > 32) s = 32;
+    const int64_t parts = steps / 8 < 32 ? steps / 8 : 32;
+    p.dh_tile = ceil_div(p.piece, 256) * ceil_div(c->D, 256) * parts >= 256 ? 256 : 128;
+    const int64_t tiles = ceil_div(p.piece, p.dh_tile) * ceil_div(c->D, p.dh_tile);
+    int64_t s = (p.dh_tile == 256 ? 256 : 512) / tiles;
+    if (s > parts) s = parts;
     p.splits = s < 1 ? 1 : int(s);
     p.splits = int(ceil_div(steps, ceil_div(steps, p.splits)));
     p.dh = cv.take(p.splits > 1 ? size_t(p.splits) * size_t(p.piece) * size_t(c->D) * 4 : 0);
@@ -677,6 +729,12 @@ void finish(GemmArgs& g, int planes, int tile, int splits) {
   g.per = int(ceil_div(g.K, kStep));
   g.steps = g.per * (planes == 3 ? 6 : 1);
   g.each = (g.steps + splits - 1) / splits;
+}
+
+void pack(const PackArgs& a, bool bf, bool wide, hipStream_t stream) {
+  const dim3 g(unsigned(ceil_div(a.rows * (a.cols_p / 8), kThreads))), b(kThreads);
+  if (bf) wide ? ce_pack_kernel<bf16_t, true><<<g, b, 0, stream>>>(a) : ce_pack_kernel<bf16_t, false><<<g, b, 0, stream>>>(a);
+  else wide ? ce_pack_kernel<float, true><<<g, b, 0, stream>>>(a) : ce_pack_kernel<float, false><<<g, b, 0, stream>>>(a);
 }
 
 // The kernel for few rows, if one is made for these sizes: MF times sixteen rows, U units
@@ -705,8 +763,8 @@ bool launch_score(const ScoreArgs& a, unsigned grid, hipStream_t stream) {
 
 // As many blocks as the 256 CUs hold at a time, a multiple of the eight XCDs: a block's
 // tiles then stay on its XCD.
-unsigned grid_of(const GemmArgs& g, bool big, bool all) {
-  const int64_t units = int64_t(g.tiles_m) * g.tiles_n * g.splits, most = big ? 256 : 512;
+unsigned grid_of(const GemmArgs& g, int tile, bool all) {
+  const int64_t units = int64_t(g.tiles_m) * g.tiles_n * g.splits, most = tile == 256 ? 256 : 512;
   return unsigned(all || units < most ? units : most);
 }
 
@@ -735,8 +793,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     w = Operand{static_cast<const uint16_t*>(weight), c->ld_weight, 0, 0, c->V, c->D};
   } else {
     PackArgs a{weight, reinterpret_cast<uint16_t*>(ws + p.w), nullptr, c->V, c->D, c->ld_weight, p.Dp, c->V * p.Dp, c->V, wide, p.planes};
-    if (bf) ce_pack_kernel<bf16_t><<<dim3(unsigned(c->V)), dim3(kThreads), 0, stream>>>(a);
-    else ce_pack_kernel<float><<<dim3(unsigned(c->V)), dim3(kThreads), 0, stream>>>(a);
+    pack(a, bf, rows16(c, weight, c->ld_weight), stream);
     w = Operand{a.dst, p.Dp, a.plane, kFinite * a.plane, c->V, p.Dp};
   }
   float* unit = nullptr;
@@ -753,21 +810,20 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
       h = Operand{static_cast<const uint16_t*>(hp), c->ld_hidden, 0, 0, M, c->D};
     } else {
       PackArgs a{hp, reinterpret_cast<uint16_t*>(ws + p.h), tp, M, c->D, c->ld_hidden, p.Dp, M * p.Dp, c->V, wide, p.planes};
-      if (bf) ce_pack_kernel<bf16_t><<<dim3(unsigned(M)), dim3(kThreads), 0, stream>>>(a);
-      else ce_pack_kernel<float><<<dim3(unsigned(M)), dim3(kThreads), 0, stream>>>(a);
+      pack(a, bf, rows16(c, hp, c->ld_hidden), stream);
       h = Operand{a.dst, p.Dp, a.plane, kFinite * a.plane, M, p.Dp};
     }
     LogitArgs l{};
     l.g.x = h; l.g.y = w;
     l.g.M = M; l.g.N = c->V; l.g.K = c->D;
-    finish(l.g, p.planes, p.tile, 1);
+    finish(l.g, p.planes, p.logits, 1);
     l.scale = c->logit_scale;
     l.stats = reinterpret_cast<float2*>(ws + p.stats);
     l.z = train ? reinterpret_cast<float*>(ws + p.z) : nullptr;
     l.chosen = train ? nullptr : reinterpret_cast<float*>(ws + p.chosen);
     l.targets = tp; l.zrows = p.rows; l.zcols = p.Vp; l.wide = wide;
-    const dim3 lg(grid_of(l.g, p.big, train));
-    if (p.big) ce_logits_kernel<256, 256, 2, 4><<<lg, dim3(512), 0, stream>>>(l);
+    const dim3 lg(grid_of(l.g, p.logits, train));
+    if (p.logits == 256) ce_logits_kernel<256, 256, 2, 4><<<lg, dim3(512), 0, stream>>>(l);
     else ce_logits_kernel<128, 128, 2, 2><<<lg, dim3(256), 0, stream>>>(l);
 
     LossArgs s{};
@@ -791,30 +847,33 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     gh.g.x = Operand{z.dz, z.ld, z.plane, 0, M, p.Vp, p.rows};
     gh.g.y = w;
     gh.g.M = M; gh.g.N = c->D; gh.g.K = c->V;
-    finish(gh.g, p.planes, p.tile, p.splits);
+    finish(gh.g, p.planes, p.dh_tile, p.splits);
     gh.out = static_cast<char*>(grad_hidden) + size_t(r0) * size_t(c->ld_grad_hidden) * esz;
     gh.part = reinterpret_cast<float*>(ws + p.dh);
     gh.unit = unit; gh.scale = c->logit_scale;
     gh.targets = tp; gh.ld = c->ld_grad_hidden; gh.V = c->V; gh.wide = wide; gh.io = c->io;
-    const dim3 hg(grid_of(gh.g, p.big, false));
-    if (p.big) ce_grad_kernel<256, 256, 2, 4, false><<<hg, dim3(512), 0, stream>>>(gh);
+    const dim3 hg(grid_of(gh.g, p.dh_tile, false));
+    if (p.dh_tile == 256) ce_grad_kernel<256, 256, 2, 4, false><<<hg, dim3(512), 0, stream>>>(gh);
     else ce_grad_kernel<128, 128, 2, 2, false><<<hg, dim3(256), 0, stream>>>(gh);
     if (p.splits > 1) {
       JoinArgs j{gh.part, unit, gh.out, M, c->D, c->ld_grad_hidden, c->logit_scale, p.splits, c->io};
-      ce_join_splits_kernel<<<dim3(unsigned(M)), dim3(kThreads), 0, stream>>>(j);
+      const bool four = c->D % 4 == 0;
+      const dim3 jg(unsigned(ceil_div(M * c->D, kThreads * (four ? 4 : 1))));
+      if (four) ce_join_splits_kernel<4><<<jg, dim3(kThreads), 0, stream>>>(j);
+      else ce_join_splits_kernel<1><<<jg, dim3(kThreads), 0, stream>>>(j);
     }
 
     GradArgs gw{};
     gw.g.x = Operand{z.dz, z.ld, z.plane, 0, M, p.Vp, p.rows};
     gw.g.y = h;
     gw.g.M = c->V; gw.g.N = c->D; gw.g.K = M;
-    finish(gw.g, p.planes, p.tile, 1);
+    finish(gw.g, p.planes, p.dw_tile, 1);
     gw.unit = unit; gw.scale = c->logit_scale;
     gw.out = grad_weight; gw.ld = c->ld_grad_weight; gw.io = c->io;
     gw.part = reinterpret_cast<float*>(ws + p.dw);
     gw.add = r0 > 0; gw.keep = r0 + M < c->N;
-    const dim3 wg(grid_of(gw.g, p.big, false));
-    if (p.big) ce_grad_kernel<256, 256, 2, 4, true><<<wg, dim3(512), 0, stream>>>(gw);
+    const dim3 wg(grid_of(gw.g, p.dw_tile, false));
+    if (p.dw_tile == 256) ce_grad_kernel<256, 256, 2, 4, true><<<wg, dim3(512), 0, stream>>>(gw);
     else ce_grad_kernel<128, 128, 2, 2, true><<<wg, dim3(256), 0, stream>>>(gw);
   }
   return launched("linear cross entropy");
