@@ -62,10 +62,11 @@ __device__ __forceinline__ float narrow<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ bf16_t narrow<bf16_t>(float v) { return bf16_t{bf16_bits(v)}; }
 
-// V adjacent elements, moved by one load or store (the address is a multiple of
-// their size).
+// V adjacent elements, moved by one load or store.  The address need be no multiple of
+// more than an element's size: the memory pipe takes any, so odd rows go as wide as even
+// ones.
 template <typename IO, int V>
-struct alignas(sizeof(IO) * V) Pack {
+struct __attribute__((packed, aligned(sizeof(IO)))) Pack {
   IO v[V];
 };
 

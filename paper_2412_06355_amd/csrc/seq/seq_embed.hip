@@ -38,7 +38,8 @@ __global__ void __launch_bounds__(kThreads) embed_fwd_kernel(const ID* ids, cons
   const uint32_t key = __builtin_amdgcn_readfirstlane(key_of(ids, i, V));
   const IO* row = table + int64_t(key) * ldt;
   IO* to = out + i * ldo;
-  for (int64_t d = lane * VEC; d < D; d += 64 * VEC) {
+  for (int64_t d0 = lane * VEC; d0 < D; d0 += 64 * VEC) {
+    const int64_t d = min(d0, D - VEC);  // (a row's last lane shares values with the one before)
     Pack<IO, VEC> v;
     if (key < V) {
       v = *reinterpret_cast<const Pack<IO, VEC>*>(row + d);
@@ -249,7 +250,7 @@ __device__ __forceinline__ void sum_run(const SumArgs& p, int64_t run, int chunk
   const uint32_t prev = i0 > 0 ? p.key[i0 - 1] : ~0u, next = i0 + count < p.n ? p.key[i0 + count] : ~0u;
   const int64_t d0 = (int64_t(chunk) * 64 + lane) * VEC;
   const bool on = d0 < p.D;
-  const int64_t d = on ? d0 : 0;
+  const int64_t d = on ? min(d0, p.D - VEC) : 0;  // (a row's last lane shares values with the one before)
   const IO* grad = static_cast<const IO*>(p.grad) + d;
   const bool inside = __builtin_amdgcn_readlane(key, 0) == prev;  // the first id began before
   bool first = true;
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kThreads) embed_sum_kernel(SumArgs p) {
   const float zero[VEC] = {};
   for (uint32_t r = w; r < rows; r += kThreads / 64) {
     if (have >> r & 1) continue;
-    for (int64_t d = lane * VEC; d < p.D; d += 64 * VEC) store_row<IO, VEC>(p, v0 + r, d, zero);
+    for (int64_t d = lane * VEC; d < p.D; d += 64 * VEC) store_row<IO, VEC>(p, v0 + r, min(d, p.D - VEC), zero);
   }
 }
 
@@ -334,8 +335,8 @@ __global__ void __launch_bounds__(kThreads) embed_join_kernel(SumArgs p) {
   const int64_t end = lower_bound(p.key, i1, p.n - i1, k + 1, lane);
   const int64_t runs = (end - 1) / kRun - run;  // that go on
   const int64_t each = ceil_div(runs, W), lo = min(run + 1 + w * each, run + 1 + runs), hi = min(lo + each, run + 1 + runs);
-  const int64_t d = (int64_t(blockIdx.y) * 64 + lane) * VEC;
-  const bool on = d < p.D;
+  const int64_t d0 = (int64_t(blockIdx.y) * 64 + lane) * VEC, d = min(d0, p.D - VEC);
+  const bool on = d0 < p.D;
   float acc[VEC] = {};
   if (on) {
     if (w == 0) {
@@ -388,11 +389,8 @@ dendsn_status check_cfg(const dendsn_embed_cfg* c) {
 
 size_t esize(const dendsn_embed_cfg* c) { return c->io == DENDSN_IO_BF16 ? 2 : 4; }
 
-// 16 bytes a lane where every row allows it, else element by element.
-bool wide(const dendsn_embed_cfg* c, const void* a, const void* b) {
-  const int64_t m = int64_t(16 / esize(c));
-  return aligned(a, 16) && aligned(b, 16) && c->D % m == 0 && c->ld_table % m == 0 && c->ld_out % m == 0;
-}
+// 16 bytes a lane, but for rows that are shorter.
+bool wide(const dendsn_embed_cfg* c) { return c->D >= int64_t(16 / esize(c)); }
 
 struct Layout {
   size_t key[2], at[2], hist, part, total;
@@ -471,7 +469,7 @@ void forward(const dendsn_embed_cfg* c, const void* ids, const void* table, void
   const auto* i = static_cast<const ID*>(ids);
   const auto* t = static_cast<const IO*>(table);
   auto* o = static_cast<IO*>(out);
-  if (wide(c, table, out))
+  if (wide(c))
     embed_fwd_kernel<IO, ID, VEC><<<grid, block, 0, stream>>>(i, t, o, c->n, uint32_t(c->V), c->D, c->ld_table, c->ld_out, c->scale);
   else
     embed_fwd_kernel<IO, ID, 1><<<grid, block, 0, stream>>>(i, t, o, c->n, uint32_t(c->V), c->D, c->ld_table, c->ld_out, c->scale);
@@ -544,7 +542,7 @@ dendsn_status dendsn_embed_backward(const dendsn_embed_cfg* cfg, const void* ids
   a.grad = grad_out; a.table = grad_table;
   a.part = reinterpret_cast<float*>(ws + l.part);
   a.n = cfg->n; a.D = cfg->D; a.ldg = cfg->ld_out; a.ldt = cfg->ld_table; a.V = uint32_t(cfg->V); a.scale = cfg->scale;
-  const bool w = wide(cfg, grad_out, grad_table);
+  const bool w = wide(cfg);
   if (cfg->io == DENDSN_IO_BF16)
     w ? sums<bf16_t, 8>(a, stream) : sums<bf16_t, 1>(a, stream);
   else

@@ -87,7 +87,7 @@ __global__ void __launch_bounds__(kW * 64) scan_runs_kernel(ScanArgs p) {
   const int seg = BWD ? int(blockIdx.z) + 1 : int(blockIdx.z);  // the first (last) block's run feeds nobody
   const int d0 = int((blockIdx.x * 64 + lane) * VEC);
   const bool on = d0 < p.D;
-  const int d = on ? d0 : 0;
+  const int d = on ? min(d0, int(p.D) - VEC) : 0;  // (an odd row's last lane shares a channel)
   const int len = seq_length(p, b);
   const int lo = seg * p.per * kTile, hi = min(min(lo + p.per * kTile, p.T), len);
   // wave w composes the steps [s0, s1)
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
   const int b = blockIdx.y, seg = blockIdx.z;
   const int d0 = int((blockIdx.x * 64 + lane) * VEC);
   const bool on = d0 < p.D;
-  const int d = on ? d0 : 0;
+  const int d = on ? min(d0, int(p.D) - VEC) : 0;  // (an odd row's last lane shares a channel)
   const int len = seq_length(p, b);
   const int64_t xb = b * p.x_b, gb = b * p.g_b, hb = b * p.h_b;
   const int64_t bd = int64_t(b) * p.D + d, lanes = int64_t(p.batch) * p.D;
@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
   const int b = blockIdx.y, seg = blockIdx.z;
   const int d0 = int((blockIdx.x * 64 + lane) * VEC);
   const bool on = d0 < p.D;
-  const int d = on ? d0 : 0;
+  const int d = on ? min(d0, int(p.D) - VEC) : 0;  // (an odd row's last lane shares a channel)
   const int len = seq_length(p, b);
   const int64_t xb = b * p.x_b, gb = b * p.g_b, ghb = b * p.gh_b, gxb = b * p.gx_b, ggb = b * p.gg_b;
   const int64_t bd = int64_t(b) * p.D + d, lanes = int64_t(p.batch) * p.D;
@@ -465,13 +465,13 @@ struct Plan {
   int ntiles, per, S;
 };
 
-// Lanes of two channels where every row allows it (4 or 8 bytes a lane).  With fewer
+// Lanes of two channels (4 or 8 bytes a lane).  With fewer
 // blocks than CUs the steps are split, to kFill blocks.
 constexpr int64_t kCus = 256, kFill = 512;
 
-Plan make_plan(const dendsn_scan_cfg* c, bool wide) {
+Plan make_plan(const dendsn_scan_cfg* c) {
   Plan p;
-  p.vec = wide ? 2 : 1;
+  p.vec = c->D >= 2 ? 2 : 1;
   p.groups = ceil_div(c->D, 64 * p.vec);
   p.ntiles = int(ceil_div(c->T, kTile));
   const int64_t blocks = p.groups * c->batch;
@@ -485,12 +485,9 @@ Plan make_plan(const dendsn_scan_cfg* c, bool wide) {
   return p;
 }
 
-// The split of narrow lanes is never finer than that of wide ones, whose blocks
-// are half as many: the scratch is sized for the most blocks.
 size_t runs_bytes(const dendsn_scan_cfg* c) {
-  const Plan a = make_plan(c, false), b = make_plan(c, true);
-  const int S = a.S > b.S ? a.S : b.S;
-  return S > 1 ? size_t(S) * size_t(c->batch) * size_t(c->D) * sizeof(float2) : 0;
+  const Plan p = make_plan(c);
+  return p.S > 1 ? size_t(p.S) * size_t(c->batch) * size_t(c->D) * sizeof(float2) : 0;
 }
 
 size_t ckpt_bytes(const dendsn_scan_cfg* c) {
@@ -555,8 +552,6 @@ struct LaunchStep {
   }
 };
 
-bool even(int64_t a, int64_t b) { return a % 2 == 0 && b % 2 == 0; }
-
 }  // namespace
 }  // namespace dendsn_seq
 
@@ -607,15 +602,13 @@ dendsn_status dendsn_scan_forward(const dendsn_scan_cfg* cfg, const void* x, con
   }
   st = check_workspace(workspace, workspace_bytes, runs_bytes(cfg), "dendsn_scan_workspace_bytes");
   if (st != DENDSN_OK) return st;
-  const bool wide = cfg->D % 2 == 0 && aligned(x, 2 * esz) && aligned(g, 2 * esz) && aligned(h, 2 * esz) &&
-                    even(cfg->x_t, cfg->x_b) && even(cfg->g_t, cfg->g_b) && even(cfg->h_t, cfg->h_b);
-  LaunchFwd f{{}, make_plan(cfg, wide), stream};
+  LaunchFwd f{{}, make_plan(cfg), stream};
   ScanArgs& a = f.a;
   a.x = x; a.g = g; a.h0 = h0; a.lengths = lengths; a.h = h; a.h_last = h_last; a.ckpt = ckpt;
   a.runs = static_cast<float2*>(workspace);
   a.D = cfg->D; a.T = int32_t(cfg->T); a.batch = int32_t(cfg->batch); a.ntiles = f.p.ntiles; a.per = f.p.per;
   a.x_t = cfg->x_t; a.x_b = cfg->x_b; a.g_t = cfg->g_t; a.g_b = cfg->g_b; a.h_t = cfg->h_t; a.h_b = cfg->h_b;
-  dispatch(cfg, wide, f);
+  dispatch(cfg, f.p.vec == 2, f);
   return launched("scan forward");
 }
 
@@ -648,11 +641,7 @@ dendsn_status dendsn_scan_backward(const dendsn_scan_cfg* cfg, const void* x, co
   }
   st = check_workspace(workspace, workspace_bytes, runs_bytes(cfg), "dendsn_scan_workspace_bytes");
   if (st != DENDSN_OK) return st;
-  const bool wide = cfg->D % 2 == 0 && aligned(x, 2 * esz) && aligned(g, 2 * esz) && aligned(grad_h, 2 * esz) &&
-                    aligned(grad_x, 2 * esz) && aligned(grad_g, 2 * esz) && even(cfg->x_t, cfg->x_b) &&
-                    even(cfg->g_t, cfg->g_b) && even(cfg->grad_h_t, cfg->grad_h_b) &&
-                    even(cfg->grad_x_t, cfg->grad_x_b) && even(cfg->grad_g_t, cfg->grad_g_b);
-  LaunchBwd f{{}, make_plan(cfg, wide), stream};
+  LaunchBwd f{{}, make_plan(cfg), stream};
   ScanArgs& a = f.a;
   a.x = x; a.g = g; a.gh = grad_h; a.lengths = lengths; a.ckpt_in = ckpt; a.gh_last = grad_h_last;
   a.gx = grad_x; a.gg = grad_g; a.gh0 = grad_h0;
@@ -661,7 +650,7 @@ dendsn_status dendsn_scan_backward(const dendsn_scan_cfg* cfg, const void* x, co
   a.x_t = cfg->x_t; a.x_b = cfg->x_b; a.g_t = cfg->g_t; a.g_b = cfg->g_b;
   a.gh_t = cfg->grad_h_t; a.gh_b = cfg->grad_h_b; a.gx_t = cfg->grad_x_t; a.gx_b = cfg->grad_x_b;
   a.gg_t = cfg->grad_g_t; a.gg_b = cfg->grad_g_b;
-  dispatch(cfg, wide, f);
+  dispatch(cfg, f.p.vec == 2, f);
   return launched("scan backward");
 }
 
@@ -681,8 +670,8 @@ dendsn_status dendsn_scan_step(const dendsn_scan_cfg* cfg, const void* x, const 
   if (!aligned(slots, 4) || !aligned(state, 4)) return fail(DENDSN_E_INVALID, "slots or state misaligned");
   if (!none && !rows_apart(cfg, cfg->h_t, cfg->h_b)) return fail(DENDSN_E_INVALID, "rows of h overlap");
   if (none) return DENDSN_OK;
-  const bool wide = cfg->D % 2 == 0 && aligned(x, 2 * esz) && aligned(g, 2 * esz) && aligned(h, 2 * esz) &&
-                    aligned(state, 8) && cfg->x_b % 2 == 0 && cfg->g_b % 2 == 0 && cfg->h_b % 2 == 0;
+  // (no lane shares a channel here: its state is read and written)
+  const bool wide = cfg->D % 2 == 0;
   LaunchStep f{{x, g, slots, state, h, cfg->D, cfg->x_b, cfg->g_b, cfg->h_b, n_slots}, cfg->batch, stream};
   dispatch(cfg, wide, f);
   return launched("scan step");
