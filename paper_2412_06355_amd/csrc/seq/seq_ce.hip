@@ -59,10 +59,9 @@ __device__ __forceinline__ void store8(uint16_t* to, const uint16_t (&x)[8]) {
   *reinterpret_cast<uint4*>(to) = q;
 }
 
-// Eight values a thread; WIDE: 16-byte reads (the rows allow them).
-template <typename IO, bool WIDE>
+// Eight values a thread.
+template <typename IO>
 __global__ void __launch_bounds__(kThreads) ce_pack_kernel(PackArgs p) {
-  constexpr int E = 16 / sizeof(IO);
   const int64_t chunks = p.cols_p / 8, id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
   const int64_t row = id / chunks, d = id % chunks * 8;
   if (row >= p.rows) return;
@@ -73,21 +72,14 @@ __global__ void __launch_bounds__(kThreads) ce_pack_kernel(PackArgs p) {
   }
   const IO* src = static_cast<const IO*>(p.src) + row * p.ld + d;
   float v[8] = {};
-  if (keep) {
+  if (keep && d + 8 <= p.cols) {
+    const auto x = *reinterpret_cast<const Pack<IO, 8>*>(src);
 #pragma unroll
-    for (int e = 0; e < 8; e += E) {
-      if (WIDE) {  // (cols is a multiple of E)
-        if (d + e < p.cols) {
-          const auto x = *reinterpret_cast<const Pack<IO, E>*>(src + e);
+    for (int k = 0; k < 8; ++k) v[k] = widen(x.v[k]);
+  } else if (keep) {
 #pragma unroll
-          for (int k = 0; k < E; ++k) v[e + k] = widen(x.v[k]);
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < E; ++k)
-          if (d + e + k < p.cols) v[e + k] = widen(src[e + k]);
-      }
-    }
+    for (int k = 0; k < 8; ++k)
+      if (d + k < p.cols) v[k] = widen(src[k]);
   }
   uint16_t* dst = p.dst + row * p.cols_p + d;
   uint16_t a[8], f[8], b[8], c[8];
@@ -251,7 +243,8 @@ struct ScoreArgs {
   const void* targets;
   float2* stats;   // [M][gridDim.x]
   float* chosen;   // [M]
-  int64_t ldh, ldw, M, V, K;
+  float* z;        // as LogitArgs
+  int64_t ldh, ldw, M, V, K, zrows;
   float scale;
   int wide;
 };
@@ -283,7 +276,12 @@ __global__ void __launch_bounds__(kScoreWaves * 64) ce_score_kernel(ScoreArgs p)
   constexpr int E = 16 / sizeof(IO), L = 16 / E;  // values of a load, loads of a unit
   __shared__ f32x4 part[2][kScoreWaves][MF][64];
   const int lane = threadIdx.x & 63, w = scalar(int(threadIdx.x >> 6)), i = lane & 15, q = lane >> 4;
-  const int64_t n0 = p.V * blockIdx.x / gridDim.x, n1 = p.V * (blockIdx.x + 1) / gridDim.x;
+  int64_t n0 = p.V * blockIdx.x / gridDim.x, n1 = p.V * (blockIdx.x + 1) / gridDim.x;
+  if (p.z) {  // whole sixteens, so that a lane's four lie together in a panel
+    const int64_t units = ceil_div(p.V, 16);
+    n0 = units * blockIdx.x / gridDim.x * 16;
+    n1 = min(units * (blockIdx.x + 1) / gridDim.x * 16, p.V);
+  }
   const int k0 = w * U * kStep + q * 16;
   u32x4 hf[MF][L * U];
 #pragma unroll
@@ -332,10 +330,11 @@ __global__ void __launch_bounds__(kScoreWaves * 64) ce_score_kernel(ScoreArgs p)
 #pragma unroll
       for (int o = 1; o < kScoreWaves; ++o) z += part[buf][o][w][lane];
       float most = top;
+      if (p.z && m < p.M) *reinterpret_cast<f32x4*>(p.z + (n / kStep * p.zrows + m) * kStep + n % kStep + 4 * q) = z;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int64_t v = n + 4 * q + r;
-        if (v == target && v < n1) p.chosen[m] = z[r];  // (past n1: another block's)
+        if (p.chosen && v == target && v < n1) p.chosen[m] = z[r];  // (past n1: another block's)
         z[r] = v < n1 ? p.scale * z[r] : -INFINITY;
         most = fmaxf(most, z[r]);
       }
@@ -373,14 +372,17 @@ struct GradArgs {
   int add, keep;         // add the sum of the pieces before; keep it (else the result is whole)
 };
 
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) { return uint32_t(bf16_bits(a)) | uint32_t(bf16_bits(b)) << 16; }
+
+// Four neighbours of a row, of which those below N are there; rows of any alignment.
 __device__ __forceinline__ void store4(void* out, int io, int64_t at, int64_t n, int64_t N, f32x4 v) {
-  // rows of any alignment: element by element unless 4 fit and lie aligned
   if (io == DENDSN_IO_BF16) {
     uint16_t* o = static_cast<uint16_t*>(out) + at;
-    if (n + 4 <= N && (reinterpret_cast<uintptr_t>(o) & 7) == 0) {
-      const uint64_t q = uint64_t(bf16_bits(v[0])) | uint64_t(bf16_bits(v[1])) << 16 |
-                         uint64_t(bf16_bits(v[2])) << 32 | uint64_t(bf16_bits(v[3])) << 48;
-      *reinterpret_cast<uint64_t*>(o) = q;
+    if (n + 4 <= N) {
+      *reinterpret_cast<u32x2_any*>(o) = u32x2_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
       return;
     }
 #pragma unroll
@@ -388,8 +390,8 @@ __device__ __forceinline__ void store4(void* out, int io, int64_t at, int64_t n,
       if (n + r < N) o[r] = bf16_bits(v[r]);
   } else {
     float* o = static_cast<float*>(out) + at;
-    if (n + 4 <= N && (reinterpret_cast<uintptr_t>(o) & 15) == 0) {
-      *reinterpret_cast<f32x4*>(o) = v;
+    if (n + 4 <= N) {
+      *reinterpret_cast<f32x4_any*>(o) = v;
       return;
     }
 #pragma unroll
@@ -731,16 +733,17 @@ void finish(GemmArgs& g, int planes, int tile, int splits) {
   g.each = (g.steps + splits - 1) / splits;
 }
 
-void pack(const PackArgs& a, bool bf, bool wide, hipStream_t stream) {
+void pack(const PackArgs& a, bool bf, hipStream_t stream) {
   const dim3 g(unsigned(ceil_div(a.rows * (a.cols_p / 8), kThreads))), b(kThreads);
-  if (bf) wide ? ce_pack_kernel<bf16_t, true><<<g, b, 0, stream>>>(a) : ce_pack_kernel<bf16_t, false><<<g, b, 0, stream>>>(a);
-  else wide ? ce_pack_kernel<float, true><<<g, b, 0, stream>>>(a) : ce_pack_kernel<float, false><<<g, b, 0, stream>>>(a);
+  if (bf) ce_pack_kernel<bf16_t><<<g, b, 0, stream>>>(a);
+  else ce_pack_kernel<float><<<g, b, 0, stream>>>(a);
 }
 
 // The kernel for few rows, if one is made for these sizes: MF times sixteen rows, U units
 // of 64 k a wave, as far as the registers reach.  2048 features, 50001 classes in bf16: 8
 // rows 33 us, 32 rows 35 us; the tiles, which split no sum over k, 53 and 41 us (and fp32
-// would be laid out in planes first).
+// would be laid out in planes first).  With the logits kept for training, 64 rows of 32000
+// classes and 1024 features: 19 us against 22; 32 rows of 50000 in fp32: 70 us against 137.
 template <typename IO>
 bool launch_score(const ScoreArgs& a, unsigned grid, hipStream_t stream) {
   constexpr bool BF = sizeof(IO) == 2;
@@ -775,25 +778,25 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
   const int wide = c->index == DENDSN_INDEX_I64;
   const size_t isz = wide ? 8 : 4;
   const bool bf = c->io == DENDSN_IO_BF16;
-  if (!train && rows16(c, hidden, c->ld_hidden) && rows16(c, weight, c->ld_weight)) {
-    // at most as many blocks as there is room for statistics, a CU each
-    const int64_t blocks = ceil_div(c->V, kStep) < 256 ? ceil_div(c->V, kStep) : 256;
-    const ScoreArgs a{hidden, weight, targets, reinterpret_cast<float2*>(ws + p.stats), reinterpret_cast<float*>(ws + p.chosen),
-                      c->ld_hidden, c->ld_weight, c->N, c->V, c->D, c->logit_scale, wide};
-    if (bf ? launch_score<bf16_t>(a, unsigned(blocks), stream) : launch_score<float>(a, unsigned(blocks), stream)) {
-      LossArgs s{};
-      s.stats = a.stats; s.chosen = a.chosen; s.targets = targets; s.loss = loss; s.lse = lse;
-      s.M = c->N; s.V = c->V; s.scale = c->logit_scale; s.tiles = int(blocks); s.wide = wide;
-      ce_loss_kernel<<<dim3(unsigned(ceil_div(c->N, kThreads / 64))), dim3(kThreads), 0, stream>>>(s);
-      return launched("linear cross entropy");
-    }
-  }
+  // Few rows: at most as many blocks as there is room for statistics, a CU each.
+  const unsigned blocks = unsigned(ceil_div(c->V, kStep) < 256 ? ceil_div(c->V, kStep) : 256);
+  auto few = [&](const void* h, const void* t, int64_t M) {
+    if (!rows16(c, h, c->ld_hidden) || !rows16(c, weight, c->ld_weight)) return false;
+    const ScoreArgs a{h, weight, t, reinterpret_cast<float2*>(ws + p.stats),
+                      train ? nullptr : reinterpret_cast<float*>(ws + p.chosen),
+                      train ? reinterpret_cast<float*>(ws + p.z) : nullptr,
+                      c->ld_hidden, c->ld_weight, M, c->V, c->D, p.rows, c->logit_scale, wide};
+    return bf ? launch_score<bf16_t>(a, blocks, stream) : launch_score<float>(a, blocks, stream);
+  };
+  const bool streamed = c->N <= 64 && few(hidden, targets, c->N);
   Operand w{};
-  if (direct(c, weight, c->ld_weight)) {
+  if (streamed && !train) {
+    // (no product reads it)
+  } else if (direct(c, weight, c->ld_weight)) {
     w = Operand{static_cast<const uint16_t*>(weight), c->ld_weight, 0, 0, c->V, c->D};
   } else {
     PackArgs a{weight, reinterpret_cast<uint16_t*>(ws + p.w), nullptr, c->V, c->D, c->ld_weight, p.Dp, c->V * p.Dp, c->V, wide, p.planes};
-    pack(a, bf, rows16(c, weight, c->ld_weight), stream);
+    pack(a, bf, stream);
     w = Operand{a.dst, p.Dp, a.plane, kFinite * a.plane, c->V, p.Dp};
   }
   float* unit = nullptr;
@@ -806,11 +809,12 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     const void* hp = static_cast<const char*>(hidden) + size_t(r0) * size_t(c->ld_hidden) * esz;
     const void* tp = static_cast<const char*>(targets) + size_t(r0) * isz;
     Operand h{};
-    if (!train && direct(c, hp, c->ld_hidden)) {
+    if (streamed && !train) {
+    } else if (!train && direct(c, hp, c->ld_hidden)) {
       h = Operand{static_cast<const uint16_t*>(hp), c->ld_hidden, 0, 0, M, c->D};
     } else {
       PackArgs a{hp, reinterpret_cast<uint16_t*>(ws + p.h), tp, M, c->D, c->ld_hidden, p.Dp, M * p.Dp, c->V, wide, p.planes};
-      pack(a, bf, rows16(c, hp, c->ld_hidden), stream);
+      pack(a, bf, stream);
       h = Operand{a.dst, p.Dp, a.plane, kFinite * a.plane, M, p.Dp};
     }
     LogitArgs l{};
@@ -823,7 +827,8 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     l.chosen = train ? nullptr : reinterpret_cast<float*>(ws + p.chosen);
     l.targets = tp; l.zrows = p.rows; l.zcols = p.Vp; l.wide = wide;
     const dim3 lg(grid_of(l.g, p.logits, train));
-    if (p.logits == 256) ce_logits_kernel<256, 256, 2, 4><<<lg, dim3(512), 0, stream>>>(l);
+    if (streamed) l.g.tiles_n = int(blocks);
+    else if (p.logits == 256) ce_logits_kernel<256, 256, 2, 4><<<lg, dim3(512), 0, stream>>>(l);
     else ce_logits_kernel<128, 128, 2, 2><<<lg, dim3(256), 0, stream>>>(l);
 
     LossArgs s{};

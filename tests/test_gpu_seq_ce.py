@@ -86,6 +86,22 @@ def test_few_rows(gpu_device, N, V, D, io):
     assert torch.equal(again, loss)
 
 
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V,D", [(1, 1003, 520), (9, 700, 1024), (16, 17, 2048), (5, 1, 512), (17, 990, 504),
+                                   (33, 2001, 512), (64, 1030, 1016), (65, 1030, 256), (3, 20000, 128), (30, 97, 61)])
+def test_few_rows_trained(gpu_device, N, V, D, io):
+    """The gradients of few rows, whose logits come from one stream over the weights where the rows
+    are aligned; a row without a target holds NaN."""
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    announce(f"ce few rows trained {cfg}")
+    h, w, t, r = make(N, V, D, io, gpu_device, V)
+    check(cfg, h, w, t, r)
+    if N > 1:
+        t[N // 2] = V
+        h[N // 2] = float("nan")
+        check(cfg, h, w, t, r)
+
+
 def test_pieces_of_rows(gpu_device):
     """More rows than the scratch holds logits of: the pieces' gradients of the weights add up."""
     N, V, D = 6000, 131072, 16
