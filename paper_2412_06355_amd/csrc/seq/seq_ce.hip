@@ -372,30 +372,31 @@ struct GradArgs {
   int add, keep;         // add the sum of the pieces before; keep it (else the result is whole)
 };
 
-typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) { return uint32_t(bf16_bits(a)) | uint32_t(bf16_bits(b)) << 16; }
 
-// Four neighbours of a row, of which those below N are there; rows of any alignment.
-__device__ __forceinline__ void store4(void* out, int io, int64_t at, int64_t n, int64_t N, f32x4 v) {
+// Eight neighbours of a row, of which those below N are there; rows of any alignment.
+__device__ __forceinline__ void store8(void* out, int io, int64_t at, int64_t n, int64_t N, const float (&v)[8]) {
   if (io == DENDSN_IO_BF16) {
     uint16_t* o = static_cast<uint16_t*>(out) + at;
-    if (n + 4 <= N) {
-      *reinterpret_cast<u32x2_any*>(o) = u32x2_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+    if (n + 8 <= N) {
+      *reinterpret_cast<u32x4_any*>(o) = u32x4_any{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
       return;
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < 8; ++r)
       if (n + r < N) o[r] = bf16_bits(v[r]);
   } else {
     float* o = static_cast<float*>(out) + at;
-    if (n + 4 <= N) {
-      *reinterpret_cast<f32x4_any*>(o) = v;
+    if (n + 8 <= N) {
+      *reinterpret_cast<f32x4_any*>(o) = f32x4_any{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f32x4_any*>(o + 4) = f32x4_any{v[4], v[5], v[6], v[7]};
       return;
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < 8; ++r)
       if (n + r < N) o[r] = v[r];
   }
 }
@@ -424,7 +425,7 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs) {
     const int64_t N = p.g.N;
     const float unit = p.unit ? *p.unit * p.scale : p.scale;
     const int64_t m0 = int64_t(tm) * BM + wm * G::TM + (lane & 15);
-    const int64_t n0 = int64_t(tn) * BN + wn * G::TN + 4 * (lane >> 4);
+    const int64_t n0 = int64_t(tn) * BN + wn * G::TN + 8 * (lane >> 4);
     const int this_split = split;
     id += gridDim.x;
     if (id < units) begin(p.g, id);
@@ -440,22 +441,28 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs) {
         zero = t < 0 || t >= p.V;
       }
 #pragma unroll
-      for (int i = 0; i < G::FN; ++i) {
+      for (int i = 0; i < G::FN; i += 2) {
         const int64_t n = n0 + 16 * i;
         if (n >= N) continue;
-        f32x4 v = acc[i][j];
-        if (zero) v = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        float v[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = zero ? 0.0f : acc[i + r / 4][j][r % 4];
         if (p.g.splits > 1) {
-          store4(p.part, DENDSN_IO_F32, (int64_t(this_split) * p.g.M + m) * N + n, n, N, v);
+          store8(p.part, DENDSN_IO_F32, (int64_t(this_split) * p.g.M + m) * N + n, n, N, v);
           continue;
         }
         if (p.add) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
+          for (int r = 0; r < 8; ++r)
             if (n + r < N) v[r] += p.part[m * N + n + r];
         }
-        if (p.keep) store4(p.part, DENDSN_IO_F32, m * N + n, n, N, v);
-        else store4(p.out, p.io, m * p.ld + n, n, N, zero ? v : unit * v);
+        if (p.keep) {
+          store8(p.part, DENDSN_IO_F32, m * N + n, n, N, v);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 8; ++r) v[r] = zero ? 0.0f : unit * v[r];
+          store8(p.out, p.io, m * p.ld + n, n, N, v);
+        }
       }
     }
     if (id >= units) break;

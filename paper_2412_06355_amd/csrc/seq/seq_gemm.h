@@ -93,7 +93,8 @@ __device__ __forceinline__ const T& arguments() {
 
 // One operand's side of a block: R rows (K rows) or columns (K columns) of its stages.
 // A stage is fetched through a descriptor that stays put while a scalar offset moves.
-template <int R, int NW, bool KCOL, bool PANEL>
+// EIGHTS: as Frags.
+template <int R, int NW, bool KCOL, bool PANEL, bool EIGHTS>
 struct Side {
   static constexpr int kBytes = R * kStep * 2;
   static constexpr int kLoads = kBytes / (1024 * NW);  // DMA instructions of a wave
@@ -121,7 +122,7 @@ struct Side {
     }
   }
   static __device__ __forceinline__ int swizzle(int row) {
-    return KCOL ? 2 * ((row & 3) | ((row >> 3) & 1) << 2) : row & 7;
+    return !KCOL ? row & 7 : EIGHTS ? 4 * (row & 3) : 2 * ((row & 3) | ((row >> 3) & 1) << 2);
   }
   __device__ __forceinline__ void place() {
     const int hi = int(left >> 32);  // (a 64-bit comparison would be a vector instruction)
@@ -174,8 +175,11 @@ __device__ __forceinline__ s16x4 read_transposed(const char* __restrict__ p) {
 }
 
 // A lane's addresses of its fragments in a stage: rows (or columns) r0 + 16 f + (lane & 15),
-// k = 32 s + 8 (lane >> 4) .. + 7.
-template <int R, int F, bool KCOL>
+// k = 32 s + 8 (lane >> 4) .. + 7.  EIGHTS (K columns): two fragments together take 32
+// columns, of which fragment f has the fours of parity f & 1: a lane's results of the two
+// are eight neighbours, so that a product of few stages (64 rows, 32000 x 1024 of them
+// written in bf16: 27 us, with four neighbours 34) writes whole lines.
+template <int R, int F, bool KCOL, bool EIGHTS>
 struct Frags {
   uint32_t at[KCOL ? F : 2];
   __device__ __forceinline__ void init(int r0, int lane) {
@@ -184,7 +188,9 @@ struct Frags {
       const int k = q * 8 + (i >> 2);
       const int fp = (i >> 2) | (q & 1) << 2;
 #pragma unroll
-      for (int f = 0; f < F; ++f) at[f] = k * (R * 2) + ((r0 / 16 + f) ^ fp) * 32 + (i & 3) * 8;
+      for (int f = 0; f < F; ++f)
+        at[f] = EIGHTS ? k * (R * 2) + ((r0 / 8 + f / 2 * 4 + (i & 3)) ^ (i >> 2) * 4) * 16 + f % 2 * 8
+                       : k * (R * 2) + ((r0 / 16 + f) ^ fp) * 32 + (i & 3) * 8;
     } else {
 #pragma unroll
       for (int s = 0; s < 2; ++s) at[s] = (r0 + i) * (kStep * 2) + (((s * 4 + q) ^ (i & 7)) * 16);
@@ -227,12 +233,13 @@ __device__ __forceinline__ void planes_of(int s, int& px, int& py) {
 }
 
 // The product of one tile.  acc[i][j]: lane l holds rows m = 16 j + (l & 15) and
-// columns n = 16 i + 4 (l >> 4) + 0..3 of the wave's tile.
+// columns n = 16 i + 4 (l >> 4) + 0..3 of the wave's tile; with YCOL, in i's pairs,
+// n = 32 (i / 2) + 8 (l >> 4) + 4 (i % 2) + 0..3.
 template <int BM, int BN, int WM, int WN, bool XCOL, bool XPANEL, bool YCOL>
 struct Gemm {
   static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
-  using SX = Side<BM, NW, XCOL, XPANEL>;
-  using SY = Side<BN, NW, YCOL, false>;
+  using SX = Side<BM, NW, XCOL, XPANEL, false>;
+  using SY = Side<BN, NW, YCOL, false, YCOL>;
   static constexpr int kStage = SX::kBytes + SY::kBytes;
   static constexpr int kLoads = SX::kLoads + SY::kLoads;
   static constexpr int kNotes = WN * BM * 8;  // bytes past the stages for the kernel's own use
@@ -243,8 +250,8 @@ struct Gemm {
   int lane, w, per, s0, s1, prod, k, m0, n0;
   SX sx;
   SY sy;
-  Frags<BM, FM, XCOL> fx;
-  Frags<BN, FN, YCOL> fy;
+  Frags<BM, FM, XCOL, false> fx;
+  Frags<BN, FN, YCOL, YCOL> fy;
 
   __device__ __forceinline__ explicit Gemm(char* stages) : lds(stages) {
     const GemmArgs& g = arguments<GemmArgs>();
