@@ -21,6 +21,8 @@
  *     is used where it is there, never required.
  *   - The library allocates nothing, keeps no state between calls and never
  *     synchronises: every call enqueues kernels on the given stream and returns.
+ *   - An output, a checkpoint or a workspace may overlap neither an input nor
+ *     another of them (not checked), but for the state of dendsn_scan_step.
  *   - Outputs are overwritten, never accumulated.  Results are deterministic: the
  *     same inputs give bit-identical outputs.
  *   - Every argument check runs on the host before anything is launched; on
@@ -64,7 +66,8 @@ typedef struct dendsn_embed_cfg {
 dendsn_status dendsn_embed_forward(const dendsn_embed_cfg* cfg, const void* ids, const void* table, void* out,
                                    hipStream_t stream);
 
-/* Scratch of dendsn_embed_backward (always > 0). */
+/* Scratch of dendsn_embed_backward (always > 0).  Both refuse n * D above
+ * 2^36 (n in runs of 32, D in 64s) with DENDSN_E_UNSUPPORTED. */
 dendsn_status dendsn_embed_workspace_bytes(const dendsn_embed_cfg* cfg, size_t* bytes);
 
 /* grad_table[v] = scale * sum of grad_out[i] over the i with ids[i] = v, every

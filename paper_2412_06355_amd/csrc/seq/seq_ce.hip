@@ -15,6 +15,7 @@ namespace dendsn_seq {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kMostThreads = int64_t(1) << 31;  // of a launch (it has fewer than 2^32)
 constexpr int64_t kPieceBytes = int64_t(4) << 30;  // of the logits and their gradient of a piece
 
 __device__ __forceinline__ int64_t target_of(const void* t, int wide, int64_t i) {
@@ -30,6 +31,7 @@ struct PackArgs {
   const void* targets;  // rows without a target become zero (NULL: none)
   int64_t rows, cols, ld, cols_p, plane, V;
   int wide, planes;
+  int64_t first;  // thread of the launch's first
 };
 
 // v as three bf16 that add up to it (two for the bits below the first eight): cut off,
@@ -62,7 +64,7 @@ __device__ __forceinline__ void store8(uint16_t* to, const uint16_t (&x)[8]) {
 // Eight values a thread.
 template <typename IO>
 __global__ void __launch_bounds__(kThreads) ce_pack_kernel(PackArgs p) {
-  const int64_t chunks = p.cols_p / 8, id = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  const int64_t chunks = p.cols_p / 8, id = p.first + int64_t(blockIdx.x) * kThreads + threadIdx.x;
   const int64_t row = id / chunks, d = id % chunks * 8;
   if (row >= p.rows) return;
   bool keep = true;
@@ -624,12 +626,13 @@ __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
   }
 }
 
+// The gradient of the weights of no rows.
 __global__ void __launch_bounds__(kThreads) ce_zero_kernel(void* out, int64_t rows, int64_t cols, int64_t ld, int io) {
-  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= rows * cols) return;
-  const int64_t at = i / cols * ld + i % cols;
-  if (io == DENDSN_IO_BF16) static_cast<uint16_t*>(out)[at] = 0;
-  else static_cast<float*>(out)[at] = 0.0f;
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < rows * cols; i += int64_t(gridDim.x) * kThreads) {
+    const int64_t at = i / cols * ld + i % cols;
+    if (io == DENDSN_IO_BF16) static_cast<uint16_t*>(out)[at] = 0;
+    else static_cast<float*>(out)[at] = 0.0f;
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -740,10 +743,14 @@ void finish(GemmArgs& g, int planes, int tile, int splits) {
   g.each = (g.steps + splits - 1) / splits;
 }
 
-void pack(const PackArgs& a, bool bf, hipStream_t stream) {
-  const dim3 g(unsigned(ceil_div(a.rows * (a.cols_p / 8), kThreads))), b(kThreads);
-  if (bf) ce_pack_kernel<bf16_t><<<g, b, 0, stream>>>(a);
-  else ce_pack_kernel<float><<<g, b, 0, stream>>>(a);
+void pack(PackArgs a, bool bf, hipStream_t stream) {
+  const int64_t threads = a.rows * (a.cols_p / 8);
+  for (a.first = 0; a.first < threads; a.first += kMostThreads) {
+    const int64_t n = threads - a.first < kMostThreads ? threads - a.first : kMostThreads;
+    const dim3 g(unsigned(ceil_div(n, kThreads))), b(kThreads);
+    if (bf) ce_pack_kernel<bf16_t><<<g, b, 0, stream>>>(a);
+    else ce_pack_kernel<float><<<g, b, 0, stream>>>(a);
+  }
 }
 
 // The kernel for few rows, if one is made for these sizes: MF times sixteen rows, U units
@@ -947,8 +954,8 @@ dendsn_status dendsn_ce_train(const dendsn_ce_cfg* cfg, const void* hidden, cons
   st = check_workspace(workspace, workspace_bytes, p.total, "dendsn_ce_workspace_bytes");
   if (st != DENDSN_OK) return st;
   if (cfg->N == 0) {
-    const int64_t n = cfg->V * cfg->D;
-    ce_zero_kernel<<<dim3(unsigned(ceil_div(n, kThreads))), dim3(kThreads), 0, stream>>>(grad_weight, cfg->V, cfg->D, cfg->ld_grad_weight, cfg->io);
+    const int64_t blocks = ceil_div(cfg->V * cfg->D, kThreads);
+    ce_zero_kernel<<<dim3(unsigned(blocks < 4096 ? blocks : 4096)), dim3(kThreads), 0, stream>>>(grad_weight, cfg->V, cfg->D, cfg->ld_grad_weight, cfg->io);
     return launched("linear cross entropy");
   }
   return run(cfg, true, hidden, weight, targets, row_weight, loss, lse, grad_hidden, grad_weight,

@@ -393,6 +393,13 @@ size_t esize(const dendsn_embed_cfg* c) { return c->io == DENDSN_IO_BF16 ? 2 : 4
 // 16 bytes a lane, but for rows that are shorter.
 bool wide(const dendsn_embed_cfg* c) { return c->D >= int64_t(16 / esize(c)); }
 
+// Blocks of embed_sum_kernel: a launch has fewer than 2^32 threads.
+dendsn_status check_sums(const dendsn_embed_cfg* c) {
+  if (ceil_div(c->n, kRun) * ceil_div(c->D, 64) > (int64_t(1) << 25))
+    return fail(DENDSN_E_UNSUPPORTED, "n * D must be at most 2^36");
+  return DENDSN_OK;
+}
+
 struct Layout {
   size_t key[2], at[2], hist, part, total;
   int64_t tile, runs;
@@ -506,7 +513,8 @@ dendsn_status dendsn_embed_forward(const dendsn_embed_cfg* cfg, const void* ids,
 
 dendsn_status dendsn_embed_workspace_bytes(const dendsn_embed_cfg* cfg, size_t* bytes) {
   clear_error();
-  const dendsn_status st = check_cfg(cfg);
+  dendsn_status st = check_cfg(cfg);
+  if (st == DENDSN_OK) st = check_sums(cfg);
   if (st != DENDSN_OK) return st;
   if (!bytes) return fail(DENDSN_E_INVALID, "bytes is NULL");
   *bytes = layout(cfg).total;
@@ -518,6 +526,7 @@ dendsn_status dendsn_embed_backward(const dendsn_embed_cfg* cfg, const void* ids
                                     hipStream_t stream) {
   clear_error();
   dendsn_status st = check_cfg(cfg);
+  if (st == DENDSN_OK) st = check_sums(cfg);
   if (st != DENDSN_OK) return st;
   const bool none = cfg->V == 0 || cfg->D == 0;
   const size_t isz = cfg->index == DENDSN_INDEX_I64 ? 8 : 4, esz = esize(cfg);
@@ -530,8 +539,6 @@ dendsn_status dendsn_embed_backward(const dendsn_embed_cfg* cfg, const void* ids
   if (st != DENDSN_OK) return st;
   if (none) return DENDSN_OK;
 
-  if (l.runs * ceil_div(cfg->D, 64) > (int64_t(1) << 25))
-    return fail(DENDSN_E_UNSUPPORTED, "n * D must be below 2^36");
   char* ws = static_cast<char*>(workspace);
   int cur = 0;
   if (cfg->n > 0)

@@ -420,8 +420,8 @@ __global__ void __launch_bounds__(256) scan_step_kernel(StepArgs p) {
 
 // T = 0: the state passes through.
 __global__ void __launch_bounds__(256) scan_copy_kernel(const float* from, float* to, int64_t n) {
-  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  if (i < n) to[i] = from ? from[i] : 0.0f;
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256)
+    to[i] = from ? from[i] : 0.0f;
 }
 
 // ---------------------------------------------------------------------------
@@ -595,7 +595,7 @@ dendsn_status dendsn_scan_forward(const dendsn_scan_cfg* cfg, const void* x, con
   if (none) {
     const int64_t lanes = cfg->batch * cfg->D;
     if (h_last && lanes) {
-      scan_copy_kernel<<<dim3(unsigned(ceil_div(lanes, 256))), dim3(256), 0, stream>>>(h0, h_last, lanes);
+      scan_copy_kernel<<<dim3(unsigned(ceil_div(lanes, 256) < 4096 ? ceil_div(lanes, 256) : 4096)), dim3(256), 0, stream>>>(h0, h_last, lanes);
       return launched("scan forward");
     }
     return DENDSN_OK;
@@ -634,7 +634,7 @@ dendsn_status dendsn_scan_backward(const dendsn_scan_cfg* cfg, const void* x, co
   if (none) {
     const int64_t lanes = cfg->batch * cfg->D;
     if (grad_h0 && lanes) {
-      scan_copy_kernel<<<dim3(unsigned(ceil_div(lanes, 256))), dim3(256), 0, stream>>>(grad_h_last, grad_h0, lanes);
+      scan_copy_kernel<<<dim3(unsigned(ceil_div(lanes, 256) < 4096 ? ceil_div(lanes, 256) : 4096)), dim3(256), 0, stream>>>(grad_h_last, grad_h0, lanes);
       return launched("scan backward");
     }
     return DENDSN_OK;

@@ -92,6 +92,21 @@ def test_embed_arguments(lib):
     assert "dendsn_embed_workspace_bytes" in dendsn.dendsn_seq_last_error()
 
 
+def test_embed_gradient_too_large(lib):
+    """A gradient whose sums a launch cannot hold is refused before its scratch is asked for, the
+    lookup of the same sizes is not (it has nothing to read without ids)."""
+    D = 1 << 16
+    c, out = embed_cfg(n=1 << 25, V=10, D=D, ld_table=D, ld_out=D), ctypes.c_size_t(77)
+    assert lib.dendsn_embed_workspace_bytes(ref(c), ctypes.byref(out)) == UNSUPPORTED and out.value == 77
+    assert embed_bwd(lib, c, nbytes=(1 << 63) - 1) == UNSUPPORTED
+    assert "2^36" in dendsn.dendsn_seq_last_error()
+    assert embed_fwd(lib, c, ids=None) == INVALID and "ids" in dendsn.dendsn_seq_last_error()
+    c = embed_cfg(n=1 << 25, V=10, D=2048, ld_table=2048, ld_out=2048)   # 2^36: the most
+    assert lib.dendsn_embed_workspace_bytes(ref(c), ctypes.byref(out)) == OK and out.value > (1 << 33)
+    c = embed_cfg(n=1 << 25, V=10, D=2049, ld_table=2049, ld_out=2049)
+    assert lib.dendsn_embed_workspace_bytes(ref(c), ctypes.byref(out)) == UNSUPPORTED
+
+
 def test_embed_nothing(lib):
     assert embed_fwd(lib, embed_cfg(n=0), ids=None, table=None, out=None) == OK
     assert embed_fwd(lib, embed_cfg(D=0, ld_table=0, ld_out=0), ids=None, out=None) == OK
