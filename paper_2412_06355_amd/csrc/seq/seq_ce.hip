@@ -462,7 +462,7 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs) {
           store8(p.part, DENDSN_IO_F32, m * N + n, n, N, v);
         } else {
 #pragma unroll
-          for (int r = 0; r < 8; ++r) v[r] = zero ? 0.0f : unit * v[r];
+          for (int r = 0; r < 8; ++r) v[r] = v[r] == 0.0f ? 0.0f : unit * v[r];
           store8(p.out, p.io, m * p.ld + n, n, N, v);
         }
       }
@@ -661,7 +661,7 @@ struct Plan {
   int64_t Dp, Vp;      // rows of packed operands, of logits
   int64_t piece, pieces, rows;  // rows: of a panel
   int logits, dh_tile, dw_tile;  // tiles of the products: 256 x 256 or 128 x 128
-  int splits;                    // of dH
+  int splits, dw_splits;         // of their sums: dH, dW
   size_t h, w, stats, z, dz, chosen, lse, unit, dh, dw, total;
 };
 
@@ -685,6 +685,24 @@ int tile_for(int64_t M, int64_t N) {
   const int64_t big = ceil_div(ceil_div(M, 256) * ceil_div(N, 256), 256);
   const int64_t small = ceil_div(ceil_div(M, 128) * ceil_div(N, 128), 256);
   return 5 * big <= 2 * small ? 256 : 128;
+}
+
+// Parts of dW's sum over the rows: where larger tiles leave most CUs without one, as many
+// parts as fill them, if that saves more stages (1.6 us each on a full chip; of 128 tiles
+// 0.64 a round, 0.85 alone) than writing and joining the parts costs (their bytes at 4 TB/s,
+// and a launch).  1024 rows, 10000 x 512 weights in fp32: 85 us against 110; 8192 rows,
+// 1000 x 256 in bf16: 28 against 93; 4096 rows, 4000 x 1024 (not split): 58.
+int dw_splits(const dendsn_ce_cfg* c, const Plan& p) {
+  if (p.pieces > 1) return 1;
+  const int64_t steps = ceil_div(c->N > 0 ? c->N : 1, kStep) * (p.planes == 3 ? 6 : 1);
+  const int64_t tiles = ceil_div(c->V, 256) * ceil_div(c->D, 256);
+  const int64_t small = ceil_div(ceil_div(c->V, 128) * ceil_div(c->D, 128), 256);
+  int64_t s = 256 / tiles;
+  if (s > steps / 8) s = steps / 8;
+  if (s < 2) return 1;
+  const double one = double(steps) * (p.dw_tile == 256 ? 1.6 : small == 1 ? 0.85 : 0.64 * double(small));
+  const double split = double(ceil_div(steps, s)) * 1.6 + double(2 * s + 1) * double(c->V) * double(c->D) * 1e-6 + 5.0;
+  return split < one ? int(ceil_div(steps, ceil_div(steps, s))) : 1;
 }
 
 Plan make_plan(const dendsn_ce_cfg* c, bool train) {
@@ -715,6 +733,8 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
     p.z = cv.take(size_t(p.rows) * size_t(p.Vp) * 4);
     p.dz = p.planes == 1 ? p.z : cv.take(size_t(p.planes) * size_t(p.rows) * size_t(p.Vp) * 2);
     p.dw_tile = tile_for(c->V, c->D);
+    p.dw_splits = dw_splits(c, p);
+    if (p.dw_splits > 1) p.dw_tile = 256;
     // dH's sum over the classes is split until the chip is full, by 32 parts of eight
     // stages at most: the larger tiles where those fill it (2048 x 30000 x 512 fp32: 353 us
     // against 463; but 1024 x 10000 x 512 bf16, 152 blocks, 28 us against 25)
@@ -727,7 +747,8 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
     p.splits = s < 1 ? 1 : int(s);
     p.splits = int(ceil_div(steps, ceil_div(steps, p.splits)));
     p.dh = cv.take(p.splits > 1 ? size_t(p.splits) * size_t(p.piece) * size_t(c->D) * 4 : 0);
-    p.dw = cv.take(p.pieces > 1 ? size_t(c->V) * size_t(c->D) * 4 : 0);
+    const int dw_parts = p.dw_splits > 1 ? p.dw_splits : p.pieces > 1 ? 1 : 0;
+    p.dw = cv.take(size_t(dw_parts) * size_t(c->V) * size_t(c->D) * 4);
   }
   p.total = cv.at;
   return p;
@@ -783,6 +804,14 @@ bool launch_score(const ScoreArgs& a, unsigned grid, hipStream_t stream) {
 unsigned grid_of(const GemmArgs& g, int tile, bool all) {
   const int64_t units = int64_t(g.tiles_m) * g.tiles_n * g.splits, most = tile == 256 ? 256 : 512;
   return unsigned(all || units < most ? units : most);
+}
+
+void join_splits(const GradArgs& g, int splits, hipStream_t stream) {
+  const JoinArgs j{g.part, g.unit, g.out, g.g.M, g.g.N, g.ld, g.scale, splits, g.io};
+  const bool four = j.N % 4 == 0;
+  const dim3 grid(unsigned(ceil_div(j.M * j.N, kThreads * (four ? 4 : 1)))), b(kThreads);
+  if (four) ce_join_splits_kernel<4><<<grid, b, 0, stream>>>(j);
+  else ce_join_splits_kernel<1><<<grid, b, 0, stream>>>(j);
 }
 
 dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const void* weight, const void* targets,
@@ -874,19 +903,13 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     const dim3 hg(grid_of(gh.g, p.dh_tile, false));
     if (p.dh_tile == 256) ce_grad_kernel<256, 256, 2, 4, false><<<hg, dim3(512), 0, stream>>>(gh);
     else ce_grad_kernel<128, 128, 2, 2, false><<<hg, dim3(256), 0, stream>>>(gh);
-    if (p.splits > 1) {
-      JoinArgs j{gh.part, unit, gh.out, M, c->D, c->ld_grad_hidden, c->logit_scale, p.splits, c->io};
-      const bool four = c->D % 4 == 0;
-      const dim3 jg(unsigned(ceil_div(M * c->D, kThreads * (four ? 4 : 1))));
-      if (four) ce_join_splits_kernel<4><<<jg, dim3(kThreads), 0, stream>>>(j);
-      else ce_join_splits_kernel<1><<<jg, dim3(kThreads), 0, stream>>>(j);
-    }
+    if (p.splits > 1) join_splits(gh, p.splits, stream);
 
     GradArgs gw{};
     gw.g.x = Operand{z.dz, z.ld, z.plane, 0, M, p.Vp, p.rows};
     gw.g.y = h;
     gw.g.M = c->V; gw.g.N = c->D; gw.g.K = M;
-    finish(gw.g, p.planes, p.dw_tile, 1);
+    finish(gw.g, p.planes, p.dw_tile, p.dw_splits);
     gw.unit = unit; gw.scale = c->logit_scale;
     gw.out = grad_weight; gw.ld = c->ld_grad_weight; gw.io = c->io;
     gw.part = reinterpret_cast<float*>(ws + p.dw);
@@ -894,6 +917,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     const dim3 wg(grid_of(gw.g, p.dw_tile, false));
     if (p.dw_tile == 256) ce_grad_kernel<256, 256, 2, 4, true><<<wg, dim3(512), 0, stream>>>(gw);
     else ce_grad_kernel<128, 128, 2, 2, true><<<wg, dim3(256), 0, stream>>>(gw);
+    if (p.dw_splits > 1) join_splits(gw, p.dw_splits, stream);
   }
   return launched("linear cross entropy");
 }

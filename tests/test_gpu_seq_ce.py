@@ -102,6 +102,20 @@ def test_few_rows_trained(gpu_device, N, V, D, io):
         check(cfg, h, w, t, r)
 
 
+@pytest.mark.parametrize("N,V,D,io", [(3000, 1000, 512, "bf16"), (1025, 700, 261, "f32"), (2111, 255, 64, "f32"),
+                                      (8200, 300, 250, "bf16"), (600, 5000, 300, "f32")])
+def test_long_sums_over_rows(gpu_device, N, V, D, io):
+    """Many rows and a small matrix of weights: the sum of its gradient is cut into parts."""
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io, logit_scale=-0.5)
+    announce(f"ce long sums {cfg}")
+    h, w, t, r = make(N, V, D, io, gpu_device, V)
+    got = check(cfg, h, w, t, r)
+    # classes that no row gives a part of: +0, whatever the scale's sign
+    some = dendsn.linear_ce_train(cfg, h, w, t, torch.zeros_like(r))
+    for k in ("grad_hidden", "grad_weight"):
+        assert torch.equal(some[k], torch.zeros_like(got[k])) and not torch.signbit(some[k]).any(), k
+
+
 def test_pieces_of_rows(gpu_device):
     """More rows than the scratch holds logits of: the pieces' gradients of the weights add up."""
     N, V, D = 6000, 131072, 16
