@@ -130,7 +130,7 @@ def _expect(t, name, shape, dtype, device, optional=False, rows=False):
         if optional:
             return
         raise ValueError(f"{name} is required")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)} != {tuple(shape)}")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name}: dtype {t.dtype} != {dtype}")
@@ -200,17 +200,17 @@ def _row_stride(t, D):
 
 def embedding(cfg: EmbeddingConfig, ids, table):
     """The rows [n, D] of ``ids`` [n] (int32 or int64) in ``table`` [V, D] (rows may lie apart)."""
-    import torch
-
     dt, dev = _io_dtype(cfg.io), table.device
     _expect(ids, "ids", (cfg.n,), None, dev)
     _expect(table, "table", (cfg.V, cfg.D), dt, dev, rows=True)
     if table.shape[0] > 1 and table.stride(0) < cfg.D:
         raise ValueError("table: rows overlap")
-    out = torch.empty((cfg.n, cfg.D), dtype=dt, device=dev)
-    c = cfg.to_c()
-    c.index, c.ld_table, c.ld_out = _index_code(ids, "ids"), _row_stride(table, cfg.D), cfg.D
-    _check(seq_lib().dendsn_embed_forward(ctypes.byref(c), _ptr(ids), _ptr(table), _ptr(out), _stream(dev)))
+    # (a serving step's lookup: the struct and the output by the shortest way)
+    out = table.new_empty((cfg.n, cfg.D))
+    c = dendsn_embed_cfg(cfg.n, cfg.V, cfg.D, _row_stride(table, cfg.D), cfg.D, IO[cfg.io], _index_code(ids, "ids"),
+                         cfg.scale)
+    _check(seq_lib().dendsn_embed_forward(ctypes.byref(c), ids.data_ptr(), table.data_ptr(), out.data_ptr(),
+                                          _stream(dev)))
     return out
 
 
@@ -285,10 +285,10 @@ def dendsn_scan_backward(cfg: GatedScanConfig, x, g, lengths, ckpt, grad_h, grad
 
 def dendsn_scan_step(cfg: GatedScanConfig, x, g, slots, state, h, stream=None):
     st = stream if stream is not None else _stream(x.device)
-    c = cfg.to_c()
-    c.x_b, c.g_b, c.h_b = x.stride(0), g.stride(0), h.stride(0)
-    _check(seq_lib().dendsn_scan_step(ctypes.byref(c), _ptr(x), _ptr(g), state.shape[0], _ptr(slots), _ptr(state),
-                                      _ptr(h), st))
+    c = dendsn_scan_cfg(cfg.T, cfg.batch, cfg.D, 0, x.stride(0), 0, g.stride(0), 0, h.stride(0), 0, 0, 0, 0, 0, 0,
+                        IO[cfg.io], GATE[cfg.gate], cfg.leaky)
+    _check(seq_lib().dendsn_scan_step(ctypes.byref(c), x.data_ptr(), g.data_ptr(), state.shape[0], _ptr(slots),
+                                      state.data_ptr(), h.data_ptr(), st))
 
 
 def _check_scan(cfg, x, g, lengths):
@@ -350,12 +350,12 @@ def gated_scan_step(cfg: GatedScanConfig, x, g, state, slots=None):
     [batch, D].  A request whose slot is no row of ``state`` is idle: h is 0."""
     import torch
 
-    dt, dev = _io_dtype(cfg.io), x.device
-    _expect(x, "x", (cfg.batch, cfg.D), dt, dev, rows=True)
-    _expect(g, "g", (cfg.batch, cfg.D), dt, dev, rows=True)
+    dt, dev, shape = _io_dtype(cfg.io), x.device, (cfg.batch, cfg.D)
+    _expect(x, "x", shape, dt, dev, rows=True)
+    _expect(g, "g", shape, dt, dev, rows=True)
     _expect(state, "state", (state.shape[0], cfg.D), torch.float32, dev)
     _expect(slots, "slots", (cfg.batch,), torch.int32, dev, optional=True)
-    h = torch.empty((cfg.batch, cfg.D), dtype=dt, device=dev)
+    h = x.new_empty(shape)
     dendsn_scan_step(cfg, x, g, slots, state, h)
     return h
 
