@@ -9,6 +9,11 @@
 // joined into lse; the gradient of the logits, without the rows' common factor (see
 // ce_unit_kernel), is rounded to bf16 once and enters the two other products, dW summed
 // over the pieces in fp32.  The three products carry the time: 2 N V D operations each.
+//
+// 8192 rows, 128000 classes, 2048 features in bf16, 11.8 ms: logits 4.05 ms (1060 TF with
+// their 4.2 GB of stores; 1275 TF without), dz 1.20 ms (5.2 TB/s), dH 2.95 ms (1460 TF), dW
+// 3.5 ms (1230 TF); the card's power limit holds the clock at 1.8 to 1.95 GHz throughout.
+// A library product of 8192^3 reaches 1510 TF, of dW's form 1060.
 #include "seq_gemm.h"
 
 namespace dendsn_seq {
@@ -403,6 +408,9 @@ __device__ __forceinline__ void store8(void* out, int io, int64_t at, int64_t n,
   }
 }
 
+// dH (dz by rows, sums over the classes) or, XCOL, dW (dz by columns, sums over the rows).
+// As many blocks as the chip holds take tiles in turn: the next tile's first stages are on
+// their way while this one is written.
 template <int BM, int BN, int WM, int WN, bool XCOL>
 __global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs) {
   using G = Gemm<BM, BN, WM, WN, XCOL, true, true>;  // X: dz, in panels
@@ -471,7 +479,8 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_grad_kernel(GradArgs) {
   }
 }
 
-// The splits of a product joined, in their order.
+// The splits of a product joined, in their order.  Bound by memory (4096 x 1024 of 4 parts
+// 14 us), most of it in cache.
 struct JoinArgs {
   const float *part, *unit;
   void* out;
@@ -523,7 +532,7 @@ struct LossArgs {
   int tiles, wide;
 };
 
-// A wave a row: joins the tiles' statistics.
+// A wave a row: joins the tiles' statistics (8192 rows of 500: 19 us).
 __global__ void __launch_bounds__(kThreads) ce_loss_kernel(LossArgs p) {
   const int lane = threadIdx.x & 63;
   const int64_t m = int64_t(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
@@ -593,7 +602,7 @@ constexpr int kDzRows = 128;  // rows of a block, of one panel
 // dz = (r / unit) (exp(s z - lse) - onehot); +0 in rows without a target, past V, and in the
 // rows past M that the last stage of dW's sum reads.  In bf16 dz takes the place of the
 // logits (ld = 128: the first half of each row's 64 fp32): the eight lanes that write a
-// row are those that have read it, in one wave.
+// row are those that have read it, in one wave.  Bound by memory: 5.2 TB/s.
 __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
   const int64_t panel = blockIdx.x / p.blocks, r0 = blockIdx.x % p.blocks * kDzRows;
   const int64_t v0 = panel * kStep + threadIdx.x % 8 * 8;

@@ -8,6 +8,11 @@
 // tokens cost no more than rare ones, and the sums of ids that go on past a wave's
 // positions are joined by a second kernel.  Rows that no token names are cleared beside
 // the sums.  Both directions are bound by memory: the gradient writes all V rows.
+//
+// 32768 tokens (frequencies 1 / rank) in 50001 rows of 1024 in bf16: lookup 21 us (67 MB
+// written), sort 2 x (3 + 7) us, sums and clearing 30 us (67 MB read from cache, 102 MB
+// written), join 7 us; 87 us with the launches' gaps.  With a block a row of the table,
+// whatever its count, the sums alone took 342 us (the first token has 2700 positions).
 #include "seq_common.h"
 
 namespace dendsn_seq {
@@ -28,7 +33,8 @@ __device__ __forceinline__ uint32_t key_of(const ID* ids, int64_t i, uint32_t V)
   return id >= 0 && id < int64_t(V) ? uint32_t(id) : V;  // V: no row
 }
 
-// A wave a row: 64 lanes over its values, VEC a lane.
+// A wave a row: 64 lanes over its values, VEC a lane.  Bound by the rows' bytes, 64 rows by
+// the launch (2.7 us).
 template <typename IO, typename ID, int VEC>
 __global__ void __launch_bounds__(kThreads) embed_fwd_kernel(const ID* ids, const IO* table, IO* out, int64_t n,
                                                              uint32_t V, int64_t D, int64_t ldt, int64_t ldo,
@@ -148,6 +154,8 @@ __device__ __forceinline__ void sort_move(const SortArgs& p, SortShared& s, int6
   }
 }
 
+// A block a tile: bases from all tiles' counts, then the tile's positions moved in order.
+// Bound by latency (7 us for 32 tiles of 1024): counts, ranks and stores follow each other.
 template <typename ID, bool FIRST>
 __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(SortArgs p) {
   __shared__ SortShared s;
@@ -324,7 +332,8 @@ __global__ void __launch_bounds__(kThreads) embed_sum_kernel(SumArgs p) {
 }
 
 // Ids whose positions go on past a run: the block of the run that they begin in adds
-// the runs' sums, each of its waves a share.
+// the runs' sums, each of its waves a share.  Bound by the most frequent id (7 us for 84
+// runs), whose sums are read four at a time by each wave.
 template <typename IO, int VEC>
 __global__ void __launch_bounds__(kThreads) embed_join_kernel(SumArgs p) {
   constexpr int W = kThreads / 64, U = 4;

@@ -7,9 +7,9 @@
 // the fragments of half a stage while it reads those of the next half, and the block
 // meets once a stage, between the halves, with products on both sides of the barrier;
 // the products of a half go in rounds with its reads and fetches between them.  The
-// 16-byte chunks of a stage are permuted so that neither kind of read meets a bank
-// twice: the DMA writes LDS linearly, so each lane fetches the chunk that belongs at
-// its place.  Buffer descriptors bound every access: rows, columns and k past an
+// 16-byte chunks of a stage are permuted so that reads spread over the banks (those of K
+// columns in eights meet some twice, a quarter of their cycles: see Frags): the DMA writes
+// LDS linearly, so each lane fetches the chunk that belongs at its place.  Buffer descriptors bound every access: rows, columns and k past an
 // operand's end read as zero.
 //
 // fp32 operands come as three bf16 planes that add up to them exactly (8 bits of

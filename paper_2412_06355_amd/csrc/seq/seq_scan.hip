@@ -11,6 +11,11 @@
 // through LDS (one barrier a tile), the state carried in registers.  Every input
 // is read once.  With few channels the steps are also split over S blocks: a first
 // kernel composes each block's run, and the scan starts from the runs before it.
+//
+// Bound by memory: bytes read once, written once, and the checkpoints (1/64 of a fp32
+// state a step).  8192 steps, 8 sequences, 4096 channels in bf16: forward 344 us and
+// backward 575 us (4.7 TB/s); a copy reaches 5.2.  64 steps, 32 sequences: 13 and 23 us
+// (3.9 and 3.6 TB/s).
 #include "seq_common.h"
 
 namespace dendsn_seq {
@@ -78,7 +83,10 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // Composes the run of one block of the split: (A, B) over its steps, forward
-// (u = w x) or backward (c[t-1] = a[t] (dh[t] + c[t])).
+// (u = w x) or backward (c[t-1] = a[t] (dh[t] + c[t])).  16384 steps of 2000 channels in
+// bf16 (131 MB): 38 us forward, 32 us backward.  The scan then reads the same bytes from
+// the 256 MB cache; blocks that wait for the runs before them instead of this kernel
+// (one read of the inputs) took 83 + 140 us for both scans, against 89 + 119 with it.
 template <typename IO, int VEC, bool SIG, bool LEAKY, bool BWD>
 __global__ void __launch_bounds__(kW * 64) scan_runs_kernel(ScanArgs p) {
   __shared__ float2 sh[kW][64 * VEC];
@@ -160,6 +168,8 @@ __device__ __forceinline__ void enter(float (&carry)[VEC], const float2* runs, i
   }
 }
 
+// Two tiles' inputs are in flight while a third is worked on; a wave's eight steps are
+// composed, the eight waves' runs exchanged, and the states written from registers.
 template <typename IO, int VEC, bool SIG, bool LEAKY>
 __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
   __shared__ float2 sh[2][kW][64 * VEC];
@@ -254,6 +264,10 @@ __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
   }
 }
 
+// From the last tile to the first: the tile's states are computed again from its
+// checkpoint, so that h is not read (it would cost as much as x, and is rounded in bf16),
+// the gradient's runs are exchanged beside the states', and the next tile's inputs are in
+// flight meanwhile.
 template <typename IO, int VEC, bool SIG, bool LEAKY>
 __global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
   __shared__ float shA[2][kW][64 * VEC], shH[2][kW][64 * VEC], shC[2][kW][64 * VEC];
@@ -390,7 +404,7 @@ struct StepArgs {
 };
 
 // One token of each request: VEC channels a thread, the state read and written
-// where it lies.
+// where it lies.  64 requests of 4096 channels move 3.7 MB in 2.7 us, a launch's latency.
 template <typename IO, int VEC, bool SIG, bool LEAKY>
 __global__ void __launch_bounds__(256) scan_step_kernel(StepArgs p) {
   const int64_t d = (int64_t(blockIdx.x) * 256 + threadIdx.x) * VEC;
@@ -465,8 +479,9 @@ struct Plan {
   int ntiles, per, S;
 };
 
-// Lanes of two channels (4 or 8 bytes a lane).  With fewer
-// blocks than CUs the steps are split, to kFill blocks.
+// Lanes of two channels (4 or 8 bytes a lane).  With fewer blocks than CUs the steps are
+// split, to kFill blocks (16384 steps of 2000 channels, forward and backward with kFill of
+// 256 / 512 / 1024: 242 / 228 / 243 us).
 constexpr int64_t kCus = 256, kFill = 512;
 
 Plan make_plan(const dendsn_scan_cfg* c) {
