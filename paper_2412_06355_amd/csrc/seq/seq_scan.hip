@@ -13,9 +13,9 @@
 // kernel composes each block's run, and the scan starts from the runs before it.
 //
 // Bound by memory: bytes read once, written once, and the checkpoints (1/64 of a fp32
-// state a step).  8192 steps, 8 sequences, 4096 channels in bf16: forward 344 us and
-// backward 575 us (4.7 TB/s); a copy reaches 5.2.  64 steps, 32 sequences: 13 and 23 us
-// (3.9 and 3.6 TB/s).
+// state a step).  8192 steps, 8 sequences, 4096 channels in bf16: both together 823 us
+// (5.2 TB/s, as a copy; under a profiler 341 and 575).  64 steps, 32 sequences: 34 us, 13
+// and 23 under a profiler.
 #include "seq_common.h"
 
 namespace dendsn_seq {
