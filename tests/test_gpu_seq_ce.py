@@ -214,6 +214,29 @@ def test_rows_that_lie_apart(gpu_device, io):
             assert torch.equal(a, b)
 
 
+@pytest.mark.parametrize("N,ld", [(300, 1 << 21), (300, (1 << 21) + 8), (20, 1 << 21)])
+def test_offsets_past_32_bits(gpu_device, N, ld):
+    """Weights, and gradients of both operands, whose rows lie 2^21 elements apart (the furthest
+    that are read where they lie) and further (laid out first): the last of 2600 starts past
+    2^32 elements.  20 rows: their logits from one stream over the weights."""
+    V, D = 2600, 72
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io="bf16", ld_weight=ld, ld_grad_hidden=ld, ld_grad_weight=ld)
+    h, w, t, r = make(N, V, D, "bf16", gpu_device, 21)
+    far = lambda n: torch.empty((n - 1) * ld + D, dtype=torch.bfloat16, device=gpu_device).as_strided((n, D), (ld, 1))
+    fw, gh, gw = far(V), far(N), far(V)
+    fw.copy_(w)
+    announce(f"ce far rows {cfg}")
+    loss, lse = (torch.empty(N, device=gpu_device) for _ in range(2))
+    ws = torch.empty(dendsn.dendsn_ce_workspace_bytes(cfg, True), dtype=torch.uint8, device=gpu_device)
+    dendsn.dendsn_ce_train(cfg, h, fw, t, r, loss, lse, gh, gw, ws)
+    want = dendsn.linear_ce_train(cfg.with_(ld_weight=0, ld_grad_hidden=0, ld_grad_weight=0), h, w, t, r)
+    for k, v in dict(loss=loss, lse=lse, grad_hidden=gh, grad_weight=gw).items():
+        assert torch.equal(v.contiguous(), want[k]), k
+    alone, _ = dendsn.linear_ce(cfg.with_(ld_weight=0), h, fw, t)
+    near, _ = dendsn.linear_ce(cfg.with_(ld_weight=0), h, w, t)
+    assert torch.equal(alone, near)
+
+
 def test_gradients_with_strides(gpu_device):
     """The entry point with the C name writes gradients into slices, and nothing beside them."""
     N, V, D = 50, 70, 20
