@@ -4,14 +4,14 @@
 //
 // The gradient adds each row's positions in an order that the ids alone fix: positions
 // are sorted by id (a stable radix sort of up to 9 bits a pass), every wave sums the
-// runs of equal ids among kRun sorted positions, whatever their rows, so that frequent
+// runs of equal ids among 16 or 32 sorted positions, whatever their rows, so that frequent
 // tokens cost no more than rare ones, and the sums of ids that go on past a wave's
 // positions are joined by a second kernel.  Rows that no token names are cleared beside
 // the sums.  Both directions are bound by memory: the gradient writes all V rows.
 //
 // 32768 tokens (frequencies 1 / rank) in 50001 rows of 1024 in bf16: lookup 21 us (67 MB
-// written), sort 2 x (3 + 7) us, sums and clearing 30 us (67 MB read from cache, 102 MB
-// written), join 7 us; 87 us with the launches' gaps.  With a block a row of the table,
+// written), sort 2 x (3 + 6) us, sums and clearing 30 us (67 MB read from cache, 102 MB
+// written), join 7 us; 86 us with the launches' gaps.  With a block a row of the table,
 // whatever its count, the sums alone took 342 us (the first token has 2700 positions).
 #include "seq_common.h"
 
@@ -22,9 +22,10 @@ constexpr int kThreads = 256;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
 constexpr int kBits = 9, kRadix = 1 << kBits;  // most bits of a pass
 constexpr int kMaxTiles = 512;                 // sorting blocks, at most
-constexpr int kOneBlock = 2048;                // positions that one block sorts alone (13 us; by passes over
-                                               // blocks 18; 4096: 23)
-constexpr int kRun = 32;                       // sorted positions of a wave
+constexpr int kOneBlock = 1024;                // positions that one block sorts alone (7 us, in two launches
+                                               // 4 + 4; 2048: 12, 4.7 + 5)
+constexpr int kCountAll = 4096;                // positions that every sorting block counts for itself (a pass
+                                               // 5.8 us, with a launch that counts 2.4 + 4.8; 8192: 8.6, 3 + 5.7)
 constexpr int kRows = 32;                      // table rows of a clearing block
 
 template <typename ID>
@@ -94,22 +95,27 @@ __global__ void __launch_bounds__(kSortThreads) embed_hist_kernel(SortArgs p) {
 }
 
 struct SortShared {
-  uint32_t base[kRadix], count[kSortWaves][kRadix], sums[kRadix], part[4][2][kRadix];
+  uint32_t base[kRadix], count[kSortWaves][kRadix], sums[kRadix / 64], part[4][2][kRadix];
 };
 
 // base[d] = positions before this tile's first of digit d, from the digits' totals and
 // their counts in the tiles before.  total, before: of digit tid < kRadix.
 __device__ __forceinline__ void sort_bases(SortShared& s, uint32_t total, uint32_t before) {
-  const int tid = threadIdx.x;
-  if (tid < kRadix) s.sums[tid] = total;
-  __syncthreads();
-  for (int d = 1; d < kRadix; d <<= 1) {
-    const uint32_t add = tid < kRadix && tid >= d ? s.sums[tid - d] : 0;
-    __syncthreads();
-    if (tid < kRadix) s.sums[tid] += add;
-    __syncthreads();
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  uint32_t sum = total;  // of the wave's digits up to this one
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t add = __shfl_up(sum, d);
+    if (lane >= d) sum += add;
   }
-  if (tid < kRadix) s.base[tid] = s.sums[tid] - total + before;
+  if (lane == 63 && w < kRadix / 64) s.sums[w] = sum;
+  __syncthreads();
+  if (tid < kRadix) {
+#pragma unroll
+    for (int q = 0; q < kRadix / 64; ++q)
+      if (q < w) sum += s.sums[q];
+    s.base[tid] = sum - total + before;
+  }
 }
 
 // Moves the positions [lo, hi) to their places, in their order.
@@ -155,28 +161,41 @@ __device__ __forceinline__ void sort_move(const SortArgs& p, SortShared& s, int6
 }
 
 // A block a tile: bases from all tiles' counts, then the tile's positions moved in order.
-// Bound by latency (7 us for 32 tiles of 1024): counts, ranks and stores follow each other.
-template <typename ID, bool FIRST>
+// Bound by latency (6 us for 32 tiles of 1024): counts, ranks and stores follow each other.
+// COUNTED: embed_hist_kernel has counted the tiles; else each block counts all positions.
+template <typename ID, bool FIRST, bool COUNTED>
 __global__ void __launch_bounds__(kSortThreads) embed_scatter_kernel(SortArgs p) {
   __shared__ SortShared s;
-  const int tid = threadIdx.x, q = tid >> 8, d = (tid & 255) * 2;
-  uint2 total = make_uint2(0, 0), before = make_uint2(0, 0);
-#pragma unroll 8
-  for (uint32_t t = q; t < p.ntiles; t += 4) {
-    const uint2 c = *reinterpret_cast<const uint2*>(p.hist + int64_t(t) * kRadix + d);
-    total.x += c.x, total.y += c.y;
-    if (t < blockIdx.x) before.x += c.x, before.y += c.y;
-  }
-  *reinterpret_cast<uint2*>(&s.part[q][0][d]) = total;
-  *reinterpret_cast<uint2*>(&s.part[q][1][d]) = before;
-  __syncthreads();
+  const int tid = threadIdx.x;
+  const int64_t lo = blockIdx.x * p.tile;
   uint32_t tt = 0, bb = 0;
-  if (tid < kRadix) {
+  if (COUNTED) {
+    const int q = tid >> 8, d = (tid & 255) * 2;
+    uint2 total = make_uint2(0, 0), before = make_uint2(0, 0);
+#pragma unroll 8
+    for (uint32_t t = q; t < p.ntiles; t += 4) {
+      const uint2 c = *reinterpret_cast<const uint2*>(p.hist + int64_t(t) * kRadix + d);
+      total.x += c.x, total.y += c.y;
+      if (t < blockIdx.x) before.x += c.x, before.y += c.y;
+    }
+    *reinterpret_cast<uint2*>(&s.part[q][0][d]) = total;
+    *reinterpret_cast<uint2*>(&s.part[q][1][d]) = before;
+    __syncthreads();
+    if (tid < kRadix) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) tt += s.part[k][0][tid], bb += s.part[k][1][tid];
+      for (int k = 0; k < 4; ++k) tt += s.part[k][0][tid], bb += s.part[k][1][tid];
+    }
+  } else {
+    if (tid < kRadix) s.part[0][0][tid] = s.part[0][1][tid] = 0;
+    __syncthreads();
+    const uint32_t mask = (1u << p.bits) - 1;
+#pragma unroll 8
+    for (int64_t i = tid; i < p.n; i += kSortThreads)
+      atomicAdd(&s.part[0][i < lo][(sort_key<ID, FIRST>(p, i) >> p.shift) & mask], 1u);
+    __syncthreads();
+    if (tid < kRadix) bb = s.part[0][1][tid], tt = s.part[0][0][tid] + bb;
   }
   sort_bases(s, tt, bb);
-  const int64_t lo = blockIdx.x * p.tile;
   sort_move<ID, FIRST>(p, s, lo, min(lo + p.tile, p.n));
 }
 
@@ -218,6 +237,7 @@ struct SumArgs {
   int64_t n, D, ldg, ldt;
   int64_t runs, sum_blocks;
   int chunks;                // waves along a row
+  int log_run;               // of the sorted positions of a wave
   uint32_t V;
   float scale;
 };
@@ -248,12 +268,12 @@ __device__ __forceinline__ void store_row(const SumArgs& p, uint32_t v, int64_t 
   *reinterpret_cast<Pack<IO, VEC>*>(static_cast<IO*>(p.table) + int64_t(v) * p.ldt + d) = o;
 }
 
-// A wave: kRun sorted positions by 64 VEC values of a row.
+// A wave: a run of sorted positions by 64 VEC values of a row.
 template <typename IO, int VEC>
 __device__ __forceinline__ void sum_run(const SumArgs& p, int64_t run, int chunk, int lane) {
   constexpr int U = 8;  // loads in flight
-  const int64_t i0 = run * kRun;
-  const int count = int(min(int64_t(kRun), p.n - i0));
+  const int64_t i0 = run << p.log_run;
+  const int count = int(min(int64_t(1) << p.log_run, p.n - i0));
   const int64_t mine = i0 + min(lane, count - 1);
   const uint32_t key = p.key[mine], at = p.at[mine];
   const uint32_t prev = i0 > 0 ? p.key[i0 - 1] : ~0u, next = i0 + count < p.n ? p.key[i0 + count] : ~0u;
@@ -333,17 +353,17 @@ __global__ void __launch_bounds__(kThreads) embed_sum_kernel(SumArgs p) {
 
 // Ids whose positions go on past a run: the block of the run that they begin in adds
 // the runs' sums, each of its waves a share.  Bound by the most frequent id (7 us for 84
-// runs), whose sums are read four at a time by each wave.
+// runs), whose sums are read eight at a time by each wave.
 template <typename IO, int VEC>
 __global__ void __launch_bounds__(kThreads) embed_join_kernel(SumArgs p) {
-  constexpr int W = kThreads / 64, U = 4;
+  constexpr int W = kThreads / 64, U = 8;
   __shared__ float join[W][64 * VEC];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t run = blockIdx.x, i0 = run * kRun, i1 = i0 + kRun;  // (i1 < n: the last run has no block)
+  const int64_t run = blockIdx.x, i0 = run << p.log_run, i1 = (run + 1) << p.log_run;  // (i1 < n: the last run has no block)
   const uint32_t k = p.key[i1 - 1];
   if (k >= p.V || p.key[i1] != k || (i0 > 0 && p.key[i0 - 1] == k)) return;
   const int64_t end = lower_bound(p.key, i1, p.n - i1, k + 1, lane);
-  const int64_t runs = (end - 1) / kRun - run;  // that go on
+  const int64_t runs = ((end - 1) >> p.log_run) - run;  // that go on
   const int64_t each = ceil_div(runs, W), lo = min(run + 1 + w * each, run + 1 + runs), hi = min(lo + each, run + 1 + runs);
   const int64_t d0 = (int64_t(blockIdx.y) * 64 + lane) * VEC, d = min(d0, p.D - VEC);
   const bool on = d0 < p.D;
@@ -404,7 +424,7 @@ bool wide(const dendsn_embed_cfg* c) { return c->D >= int64_t(16 / esize(c)); }
 
 // Blocks of embed_sum_kernel: a launch has fewer than 2^32 threads.
 dendsn_status check_sums(const dendsn_embed_cfg* c) {
-  if (ceil_div(c->n, kRun) * ceil_div(c->D, 64) > (int64_t(1) << 25))
+  if (ceil_div(c->n, 32) * ceil_div(c->D, 64) > (int64_t(1) << 25))
     return fail(DENDSN_E_UNSUPPORTED, "n * D must be at most 2^36");
   return DENDSN_OK;
 }
@@ -413,7 +433,7 @@ struct Layout {
   size_t key[2], at[2], hist, part, total;
   int64_t tile, runs;
   uint32_t ntiles;
-  int bits, passes;
+  int bits, passes, log_run;
 };
 
 Layout layout(const dendsn_embed_cfg* c) {
@@ -426,7 +446,12 @@ Layout layout(const dendsn_embed_cfg* c) {
   const int64_t n = c->n > 0 ? c->n : 1;
   l.tile = round_up(ceil_div(n, kMaxTiles), kSortThreads);
   l.ntiles = uint32_t(ceil_div(n, l.tile));
-  l.runs = ceil_div(n, kRun);
+  // Runs of 32, or of 16 where those are fewer waves than four a CU: 8192 positions of 513
+  // in fp32 (768 waves) sums and join 11 + 4 us, of 16 7 + 5; 32768 of 1024 in bf16 (2048
+  // waves) 25 + 8, of 16 26 + 13.
+  const int64_t chunks = ceil_div(c->D, wide(c) ? 64 * int64_t(16 / esize(c)) : 64);
+  l.log_run = ceil_div(n, 32) * chunks < 1024 ? 4 : 5;
+  l.runs = ceil_div(n, int64_t(1) << l.log_run);
   for (int i = 0; i < 2; ++i) {
     l.key[i] = cv.take(size_t(n) * 4);
     l.at[i] = cv.take(size_t(n) * 4);
@@ -458,12 +483,15 @@ int sort(const dendsn_embed_cfg* c, const Layout& l, const void* ids, char* ws, 
     s.shift = k * l.bits;
     s.key_in = key[k & 1]; s.at_in = at[k & 1];
     s.key_out = key[~k & 1]; s.at_out = at[~k & 1];
-    if (k == 0) {
+    if (c->n <= kCountAll) {
+      if (k == 0) embed_scatter_kernel<ID, true, false><<<grid, block, 0, stream>>>(s);
+      else embed_scatter_kernel<ID, false, false><<<grid, block, 0, stream>>>(s);
+    } else if (k == 0) {
       embed_hist_kernel<ID, true><<<grid, block, 0, stream>>>(s);
-      embed_scatter_kernel<ID, true><<<grid, block, 0, stream>>>(s);
+      embed_scatter_kernel<ID, true, true><<<grid, block, 0, stream>>>(s);
     } else {
       embed_hist_kernel<ID, false><<<grid, block, 0, stream>>>(s);
-      embed_scatter_kernel<ID, false><<<grid, block, 0, stream>>>(s);
+      embed_scatter_kernel<ID, false, true><<<grid, block, 0, stream>>>(s);
     }
   }
   return l.passes & 1;
@@ -554,6 +582,7 @@ dendsn_status dendsn_embed_backward(const dendsn_embed_cfg* cfg, const void* ids
     cur = cfg->index == DENDSN_INDEX_I64 ? sort<int64_t>(cfg, l, ids, ws, stream) : sort<int32_t>(cfg, l, ids, ws, stream);
   SumArgs a{};
   a.runs = cfg->n > 0 ? l.runs : 0;
+  a.log_run = l.log_run;
   a.key = reinterpret_cast<const uint32_t*>(ws + l.key[cur]);
   a.at = reinterpret_cast<const uint32_t*>(ws + l.at[cur]);
   a.grad = grad_out; a.table = grad_table;
