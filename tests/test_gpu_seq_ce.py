@@ -64,6 +64,15 @@ def test_large_tiles(gpu_device, N, V, D, io):
     check(cfg, *make(N, V, D, io, gpu_device, N))
 
 
+@pytest.mark.parametrize("N,V,D,io", [(1000, 10007, 72, "bf16"), (1000, 10007, 40, "f32"), (700, 12001, 129, "bf16"),
+                                      (1921, 5100, 8, "bf16")])
+def test_middle_tiles(gpu_device, N, V, D, io):
+    """Counts of rows and classes that tiles of 192 rows divide among the chip best."""
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    announce(f"ce {cfg}")
+    check(cfg, *make(N, V, D, io, gpu_device, N))
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 @pytest.mark.parametrize("N,V,D", [(1, 1003, 520), (9, 700, 1024), (16, 65, 2048), (5, 517, 4096), (8, 300, 1504),
                                    (17, 999, 512), (32, 1500, 904), (25, 640, 2000), (33, 2001, 512), (64, 1030, 1016),
