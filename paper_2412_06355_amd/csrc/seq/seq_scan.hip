@@ -170,12 +170,18 @@ __device__ __forceinline__ void enter(float (&carry)[VEC], const float2* runs, i
 
 // Two tiles' inputs are in flight while a third is worked on; a wave's eight steps are
 // composed, the eight waves' runs exchanged, and the states written from registers.
-template <typename IO, int VEC, bool SIG, bool LEAKY>
-__global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
-  __shared__ float2 sh[2][kW][64 * VEC];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// W > 0: all steps are one tile of W waves, kW / W of them (of other channels) a block, and
+// nothing is in flight beside it.  With blocks of a tile, as for long sequences, 256
+// sequences of 4096 channels in bf16 took 56 us forward and 134 backward for one step, 10
+// and 14 so; 64 steps of 512 x 1000 in fp32 115 and 181, 90 and 162 so.
+template <typename IO, int VEC, bool SIG, bool LEAKY, int W>
+__global__ void __launch_bounds__(kW * 64, W ? 4 : 2) scan_fwd_kernel(ScanArgs p) {
+  constexpr bool ONE = W > 0;
+  constexpr int N = ONE ? W : kW;  // waves of a tile
+  __shared__ float2 sh[ONE ? 1 : 2][kW][64 * VEC];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave % N;
   const int b = blockIdx.y, seg = blockIdx.z;
-  const int d0 = int((blockIdx.x * 64 + lane) * VEC);
+  const int d0 = int(((blockIdx.x * (kW / N) + wave / N) * 64 + lane) * VEC);
   const bool on = d0 < p.D;
   const int d = on ? min(d0, int(p.D) - VEC) : 0;  // (an odd row's last lane shares a channel)
   const int len = seq_length(p, b);
@@ -185,9 +191,9 @@ __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
   float carry[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) carry[v] = p.h0 ? p.h0[bd + v] : 0.0f;
-  enter<VEC>(carry, p.runs + bd, lanes, 0, seg, 1);
+  if (!ONE) enter<VEC>(carry, p.runs + bd, lanes, 0, seg, 1);
 
-  const int k0 = seg * p.per, k1 = min(k0 + p.per, p.ntiles);
+  const int k0 = ONE ? 0 : seg * p.per, k1 = ONE ? 1 : min(k0 + p.per, p.ntiles);
   struct Raw {
     Pack<IO, VEC> x[kL], g[kL];
   };
@@ -220,18 +226,20 @@ __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
         H[j][v] = in ? fmaf(a, hp, LEAKY ? na * xv : xv) : hp;
       }
     }
-    fetch(raw, k + 2);
+    if (!ONE) fetch(raw, k + 2);
+    if (N > 1) {
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) sh[buf][w][v * 64 + lane] = make_float2(P[kL - 1][v], H[kL - 1][v]);
-    lds_barrier();
+      for (int v = 0; v < VEC; ++v) sh[buf][wave][v * 64 + lane] = make_float2(P[kL - 1][v], H[kL - 1][v]);
+      lds_barrier();
+    }
     float in[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       if (w == 0 && on && p.ckpt) p.ckpt[int64_t(k) * lanes + bd + v] = carry[v];
       in[v] = carry[v];
 #pragma unroll
-      for (int q = 0; q < kW; ++q) {
-        const float2 r = sh[buf][q][v * 64 + lane];
+      for (int q = 0; q < N; ++q) {
+        const float2 r = N > 1 ? sh[buf][wave - w + q][v * 64 + lane] : make_float2(P[kL - 1][v], H[kL - 1][v]);
         if (q == w) in[v] = carry[v];
         carry[v] = fmaf(r.x, carry[v], r.y);
       }
@@ -253,10 +261,14 @@ __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
   };
   Raw ra, rb;  // a tile's loads are two tiles ahead of its use
   fetch(ra, k0);
-  fetch(rb, k0 + 1);
-  for (int k = k0; k < k1; k += 2) {
-    either(ra, k, 0);
-    if (k + 1 < k1) either(rb, k + 1, 1);
+  if (ONE) {
+    either(ra, 0, 0);
+  } else {
+    fetch(rb, k0 + 1);
+    for (int k = k0; k < k1; k += 2) {
+      either(ra, k, 0);
+      if (k + 1 < k1) either(rb, k + 1, 1);
+    }
   }
   if (w == 0 && on && p.h_last && k1 == p.ntiles && k0 < k1) {
 #pragma unroll
@@ -268,12 +280,14 @@ __global__ void __launch_bounds__(kW * 64) scan_fwd_kernel(ScanArgs p) {
 // checkpoint, so that h is not read (it would cost as much as x, and is rounded in bf16),
 // the gradient's runs are exchanged beside the states', and the next tile's inputs are in
 // flight meanwhile.
-template <typename IO, int VEC, bool SIG, bool LEAKY>
-__global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
-  __shared__ float shA[2][kW][64 * VEC], shH[2][kW][64 * VEC], shC[2][kW][64 * VEC];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+template <typename IO, int VEC, bool SIG, bool LEAKY, int W>
+__global__ void __launch_bounds__(kW * 64, 2) scan_bwd_kernel(ScanArgs p) {
+  constexpr bool ONE = W > 0;  // as in the forward
+  constexpr int N = ONE ? W : kW, S = ONE ? 1 : 2;
+  __shared__ float shA[S][kW][64 * VEC], shH[S][kW][64 * VEC], shC[S][kW][64 * VEC];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave % N;
   const int b = blockIdx.y, seg = blockIdx.z;
-  const int d0 = int((blockIdx.x * 64 + lane) * VEC);
+  const int d0 = int(((blockIdx.x * (kW / N) + wave / N) * 64 + lane) * VEC);
   const bool on = d0 < p.D;
   const int d = on ? min(d0, int(p.D) - VEC) : 0;  // (an odd row's last lane shares a channel)
   const int len = seq_length(p, b);
@@ -283,9 +297,9 @@ __global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
   float carry[VEC];  // c of the tile's last step
 #pragma unroll
   for (int v = 0; v < VEC; ++v) carry[v] = p.gh_last ? p.gh_last[bd + v] : 0.0f;
-  enter<VEC>(carry, p.runs + bd, lanes, int(gridDim.z) - 1, seg, -1);
+  if (!ONE) enter<VEC>(carry, p.runs + bd, lanes, int(gridDim.z) - 1, seg, -1);
 
-  const int k0 = seg * p.per, k1 = min(k0 + p.per, p.ntiles);
+  const int k0 = ONE ? 0 : seg * p.per, k1 = ONE ? 1 : min(k0 + p.per, p.ntiles);
   struct Raw {
     Pack<IO, VEC> x[kL], g[kL], h[kL];
     float start[VEC];
@@ -336,22 +350,25 @@ __global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       hin[v] = raw.start[v];
-      shA[buf][w][v * 64 + lane] = A[v];
-      shH[buf][w][v * 64 + lane] = H[v];
-      shC[buf][w][v * 64 + lane] = C[v];
+      if (N > 1) {
+        shA[buf][wave][v * 64 + lane] = A[v];
+        shH[buf][wave][v * 64 + lane] = H[v];
+        shC[buf][wave][v * 64 + lane] = C[v];
+      }
     }
-    fetch(raw, k - 1);
-    lds_barrier();
+    if (!ONE) fetch(raw, k - 1);
+    if (N > 1) lds_barrier();
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
+      const int first = wave - w, at = v * 64 + lane;
 #pragma unroll
-      for (int q = 0; q < kW - 1; ++q)
-        if (q < w) hin[v] = fmaf(shA[buf][q][v * 64 + lane], hin[v], shH[buf][q][v * 64 + lane]);
+      for (int q = 0; q < N - 1; ++q)
+        if (q < w) hin[v] = fmaf(shA[buf][first + q][at], hin[v], shH[buf][first + q][at]);
       cin[v] = carry[v];
 #pragma unroll
-      for (int q = kW - 1; q >= 0; --q) {
+      for (int q = N - 1; q >= 0; --q) {
         if (q == w) cin[v] = carry[v];
-        carry[v] = fmaf(shA[buf][q][v * 64 + lane], carry[v], shC[buf][q][v * 64 + lane]);
+        carry[v] = fmaf(N > 1 ? shA[buf][first + q][at] : A[v], carry[v], N > 1 ? shC[buf][first + q][at] : C[v]);
       }
     }
     float before[kL][VEC];
@@ -388,7 +405,7 @@ __global__ void __launch_bounds__(kW * 64) scan_bwd_kernel(ScanArgs p) {
   };
   Raw raw;  // (two tiles ahead, as in the forward, the registers do not reach)
   fetch(raw, k1 - 1);
-  for (int k = k1 - 1; k >= k0; --k) either(raw, k, k & 1);
+  for (int k = k1 - 1; k >= k0; --k) either(raw, k, ONE ? 0 : k & 1);
   if (w == 0 && on && p.gh0 && seg == 0) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) p.gh0[bd + v] = carry[v];
@@ -477,6 +494,7 @@ struct Plan {
   int vec;
   int64_t groups;  // blocks along the channels
   int ntiles, per, S;
+  int one;         // waves of the only tile; 0: several tiles
 };
 
 // Lanes of two channels (4 or 8 bytes a lane).  With fewer blocks than CUs the steps are
@@ -489,6 +507,7 @@ Plan make_plan(const dendsn_scan_cfg* c) {
   p.vec = c->D >= 2 ? 2 : 1;
   p.groups = ceil_div(c->D, 64 * p.vec);
   p.ntiles = int(ceil_div(c->T, kTile));
+  p.one = c->T > kTile ? 0 : c->T > 4 * kL ? 8 : c->T > 2 * kL ? 4 : c->T > kL ? 2 : 1;
   const int64_t blocks = p.groups * c->batch;
   int64_t S = blocks >= kCus ? 1 : ceil_div(kFill, blocks);
   S = S < kMaxSplit ? S : kMaxSplit;
@@ -539,7 +558,12 @@ struct LaunchFwd {
     const dim3 block(kW * 64);
     if (p.S > 1)
       scan_runs_kernel<IO, V, SIG, LEAKY, false><<<dim3(unsigned(p.groups), a.batch, p.S - 1), block, 0, stream>>>(a);
-    scan_fwd_kernel<IO, V, SIG, LEAKY><<<dim3(unsigned(p.groups), a.batch, p.S), block, 0, stream>>>(a);
+    const dim3 grid(unsigned(ceil_div(p.groups, p.one ? kW / p.one : 1)), a.batch, p.S);
+    if (p.one == 1) scan_fwd_kernel<IO, V, SIG, LEAKY, 1><<<grid, block, 0, stream>>>(a);
+    else if (p.one == 2) scan_fwd_kernel<IO, V, SIG, LEAKY, 2><<<grid, block, 0, stream>>>(a);
+    else if (p.one == 4) scan_fwd_kernel<IO, V, SIG, LEAKY, 4><<<grid, block, 0, stream>>>(a);
+    else if (p.one == 8) scan_fwd_kernel<IO, V, SIG, LEAKY, 8><<<grid, block, 0, stream>>>(a);
+    else scan_fwd_kernel<IO, V, SIG, LEAKY, 0><<<grid, block, 0, stream>>>(a);
   }
 };
 
@@ -552,7 +576,12 @@ struct LaunchBwd {
     const dim3 block(kW * 64);
     if (p.S > 1)
       scan_runs_kernel<IO, V, SIG, LEAKY, true><<<dim3(unsigned(p.groups), a.batch, p.S - 1), block, 0, stream>>>(a);
-    scan_bwd_kernel<IO, V, SIG, LEAKY><<<dim3(unsigned(p.groups), a.batch, p.S), block, 0, stream>>>(a);
+    const dim3 grid(unsigned(ceil_div(p.groups, p.one ? kW / p.one : 1)), a.batch, p.S);
+    if (p.one == 1) scan_bwd_kernel<IO, V, SIG, LEAKY, 1><<<grid, block, 0, stream>>>(a);
+    else if (p.one == 2) scan_bwd_kernel<IO, V, SIG, LEAKY, 2><<<grid, block, 0, stream>>>(a);
+    else if (p.one == 4) scan_bwd_kernel<IO, V, SIG, LEAKY, 4><<<grid, block, 0, stream>>>(a);
+    else if (p.one == 8) scan_bwd_kernel<IO, V, SIG, LEAKY, 8><<<grid, block, 0, stream>>>(a);
+    else scan_bwd_kernel<IO, V, SIG, LEAKY, 0><<<grid, block, 0, stream>>>(a);
   }
 };
 

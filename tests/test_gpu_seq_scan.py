@@ -60,6 +60,18 @@ def test_against_recurrence(gpu_device, T, b, D, io):
 
 
 @pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 3, 8, 9, 16, 17, 32, 33, 64])
+@pytest.mark.parametrize("b,D", [(3, 1000), (2, 1), (1, 515)])
+def test_one_tile(gpu_device, T, b, D, io):
+    """Steps around the eight of one, two, four and eight waves, where a block's other waves have
+    other channels; rows end inside a block's share."""
+    for gate, leaky, ragged, carry in (("sigmoid", True, True, True), ("decay", False, False, False)):
+        cfg = dendsn.GatedScanConfig(T=T, batch=b, D=D, io=io, gate=gate, leaky=leaky)
+        announce(f"scan {cfg} ragged {ragged} carry {carry}")
+        check(cfg, make(T, b, D, io, gate, T + D, ragged, carry), gpu_device)
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_layouts(gpu_device, io):
     """Batch-major, side by side in one projection, odd strides and broadcast inputs give
     the contiguous call's bits."""
