@@ -664,6 +664,7 @@ dendsn_status check_cfg(const dendsn_ce_cfg* c) {
 }
 
 constexpr int kBig = 256;  // tile of a product, both ways
+constexpr int64_t kMaxParts = 128;  // of a sum over k
 
 struct Plan {
   int planes;
@@ -707,22 +708,35 @@ int logits_tile(int64_t M, int64_t V) {
   return 85 * mid < (tile == 256 ? 100 * big : 40 * small) ? 192 : tile;
 }
 
-// Parts of dW's sum over the rows: where larger tiles leave most CUs without one, as many
-// parts as fill them, if that saves more stages (1.6 us each on a full chip; of 128 tiles
-// 0.64 a round, 0.85 alone) than writing and joining the parts costs (their bytes at 4 TB/s,
-// and a launch).  1024 rows, 10000 x 512 weights in fp32: 85 us against 110; 8192 rows,
-// 1000 x 256 in bf16: 28 against 93; 4096 rows, 4000 x 1024 (not split): 58.
-int dw_splits(const dendsn_ce_cfg* c, const Plan& p) {
-  if (p.pieces > 1) return 1;
-  const int64_t steps = ceil_div(c->N > 0 ? c->N : 1, kStep) * (p.planes == 3 ? 6 : 1);
-  const int64_t tiles = ceil_div(c->V, 256) * ceil_div(c->D, 256);
-  const int64_t small = ceil_div(ceil_div(c->V, 128) * ceil_div(c->D, 128), 256);
-  int64_t s = 256 / tiles;
-  if (s > steps / 8) s = steps / 8;
-  if (s < 2) return 1;
-  const double one = double(steps) * (p.dw_tile == 256 ? 1.6 : small == 1 ? 0.85 : 0.64 * double(small));
-  const double split = double(ceil_div(steps, s)) * 1.6 + double(2 * s + 1) * double(c->V) * double(c->D) * 1e-6 + 5.0;
-  return split < one ? int(ceil_div(steps, ceil_div(steps, s))) : 1;
+// The tile of a gradient's product, and the parts that its sum of `steps` stages is cut
+// into, by an estimate in us: a stage of a full chip takes 1.6 in 256 tiles, 0.64 a round of
+// 256 tiles of 128 (0.85 where there is one round: nothing shares a CU then); parts are
+// written and joined at 4 TB/s, by a launch of 5.  At least eight stages a part.  Measured,
+// the kernel and the join: dW of 1024 rows, 10000 x 512 in fp32 in three parts 85, whole (128
+// tiles) 110; of 8192 rows, 1000 x 256 in bf16 28 and 93; dH of 64 rows, 32000 x 1024 in bf16
+// in 32 parts of 128 tiles 32; of 4096 in four of 256 254.
+struct Split {
+  int tile, parts;
+};
+
+Split split_of(int64_t M, int64_t N, int64_t steps, bool whole) {
+  Split best{};
+  double least = 0.0;
+  for (int tile : {256, 128}) {
+    const int64_t tiles = ceil_div(M, tile) * ceil_div(N, tile);
+    for (int64_t fill : {0, 256, 512}) {  // blocks
+      int64_t parts = fill / tiles;
+      if (parts > kMaxParts) parts = kMaxParts;
+      if (parts > steps / 8) parts = steps / 8;
+      if (parts < 1 || whole) parts = 1;
+      const int64_t each = ceil_div(steps, parts), rounds = ceil_div(tiles * parts, 256);
+      parts = ceil_div(steps, each);
+      double us = double(each) * (tile == 256 ? 1.6 * double(rounds) : rounds == 1 ? 0.85 : 0.64 * double(rounds));
+      if (parts > 1) us += double(2 * parts + 1) * double(M) * double(N) * 1e-6 + 5.0;
+      if (!best.tile || us < least) best = Split{tile, int(parts)}, least = us;
+    }
+  }
+  return best;
 }
 
 Plan make_plan(const dendsn_ce_cfg* c, bool train) {
@@ -753,20 +767,11 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   if (train) {
     p.z = cv.take(size_t(p.rows) * size_t(p.Vp) * 4);
     p.dz = p.planes == 1 ? p.z : cv.take(size_t(p.planes) * size_t(p.rows) * size_t(p.Vp) * 2);
-    p.dw_tile = tile_for(c->V, c->D);
-    p.dw_splits = dw_splits(c, p);
-    if (p.dw_splits > 1) p.dw_tile = 256;
-    // dH's sum over the classes is split until the chip is full, by 32 parts of eight
-    // stages at most: the larger tiles where those fill it (2048 x 30000 x 512 fp32: 353 us
-    // against 463; but 1024 x 10000 x 512 bf16, 152 blocks, 28 us against 25)
-    const int64_t steps = ceil_div(c->V, kStep) * (p.planes == 3 ? 6 : 1);
-    const int64_t parts = steps / 8 < 32 ? steps / 8 : 32;
-    p.dh_tile = ceil_div(p.piece, 256) * ceil_div(c->D, 256) * parts >= 256 ? 256 : 128;
-    const int64_t tiles = ceil_div(p.piece, p.dh_tile) * ceil_div(c->D, p.dh_tile);
-    int64_t s = (p.dh_tile == 256 ? 256 : 512) / tiles;
-    if (s > parts) s = parts;
-    p.splits = s < 1 ? 1 : int(s);
-    p.splits = int(ceil_div(steps, ceil_div(steps, p.splits)));
+    const int64_t planes = p.planes == 3 ? 6 : 1;
+    const Split dh = split_of(p.piece, c->D, ceil_div(c->V, kStep) * planes, false);
+    const Split dw = split_of(c->V, c->D, ceil_div(p.piece, kStep) * planes, p.pieces > 1);
+    p.dh_tile = dh.tile, p.splits = dh.parts;
+    p.dw_tile = dw.tile, p.dw_splits = dw.parts;
     p.dh = cv.take(p.splits > 1 ? size_t(p.splits) * size_t(p.piece) * size_t(c->D) * 4 : 0);
     const int dw_parts = p.dw_splits > 1 ? p.dw_splits : p.pieces > 1 ? 1 : 0;
     p.dw = cv.take(size_t(dw_parts) * size_t(c->V) * size_t(c->D) * 4);
