@@ -104,7 +104,7 @@ def _bytes(fn, *args) -> int:
 
 
 def _nbytes(t):
-    return ctypes.c_size_t(0 if t is None else t.numel() * t.element_size())
+    return 0 if t is None else t.nbytes
 
 
 def _io_dtype(io):
@@ -254,10 +254,12 @@ class GatedScanConfig:
     def to_c(self, x=None, g=None, h=None, grad_h=None, grad_x=None, grad_g=None) -> dendsn_scan_cfg:
         """The C struct with the strides of the given [T, batch, D] tensors (None: contiguous)."""
         dense = (self.batch * self.D, self.D)
-        s = []
-        for t in (x, g, h, grad_h, grad_x, grad_g):
-            s += dense if t is None else (t.stride(0), t.stride(1))
+        s = [v for t in (x, g, h, grad_h, grad_x, grad_g) for v in (dense if t is None else t.stride()[:2])]
         return dendsn_scan_cfg(self.T, self.batch, self.D, *s, IO[self.io], GATE[self.gate], int(self.leaky))
+
+    def ckpt_values(self) -> int:
+        """The fp32 values of the checkpoints (dendsn_scan_ckpt_bytes / 4)."""
+        return -(-self.T // SCAN_TILE) * self.batch * self.D
 
 
 def dendsn_scan_ckpt_bytes(cfg: GatedScanConfig) -> int:
@@ -310,11 +312,10 @@ def gated_scan(cfg: GatedScanConfig, x, g, h0=None, lengths=None, *, save_ckpt: 
 
     dt, dev, shape = _check_scan(cfg, x, g, lengths)
     _expect(h0, "h0", shape[1:], torch.float32, dev, optional=True)
-    h = torch.empty(shape, dtype=dt, device=dev)
+    h = x.new_empty(shape)
     h_last = torch.empty(shape[1:], dtype=torch.float32, device=dev)
     c, fn = cfg.to_c(x, g, h), seq_lib()
-    ckpt = torch.empty((_bytes(fn.dendsn_scan_ckpt_bytes, ctypes.byref(c)) // 4,), dtype=torch.float32,
-                       device=dev) if save_ckpt else None
+    ckpt = torch.empty((cfg.ckpt_values(),), dtype=torch.float32, device=dev) if save_ckpt else None
     ws = _workspace(_bytes(fn.dendsn_scan_workspace_bytes, ctypes.byref(c), 0), workspace, dev)
     _check(fn.dendsn_scan_forward(ctypes.byref(c), _ptr(x), _ptr(g), _ptr(h0), _ptr(lengths), _ptr(h), _ptr(h_last),
                                   _ptr(ckpt), _ptr(ws), _nbytes(ws), _stream(dev)))
@@ -330,10 +331,10 @@ def gated_scan_backward(cfg: GatedScanConfig, x, g, lengths, ckpt, grad_h, grad_
     _expect(grad_h, "grad_h", shape, dt, dev, rows=True)
     _expect(grad_h_last, "grad_h_last", shape[1:], torch.float32, dev, optional=True)
     fn = seq_lib()
-    out = dict(grad_x=torch.empty(shape, dtype=dt, device=dev), grad_g=torch.empty(shape, dtype=dt, device=dev),
+    out = dict(grad_x=x.new_empty(shape), grad_g=x.new_empty(shape),
                grad_h0=torch.empty(shape[1:], dtype=torch.float32, device=dev))
     c = cfg.to_c(x, g, None, grad_h, out["grad_x"], out["grad_g"])
-    need = _bytes(fn.dendsn_scan_ckpt_bytes, ctypes.byref(c))
+    need = 4 * cfg.ckpt_values()
     if need and (ckpt is None or ckpt.dtype != torch.float32 or ckpt.device != dev or not ckpt.is_contiguous()
                  or ckpt.numel() * 4 < need):
         raise ValueError(f"ckpt must be the forward's checkpoints: contiguous float32 on {dev}, {need} bytes")

@@ -306,3 +306,11 @@ def test_python_checks():
         dendsn.linear_ce_train(c, h, w, t, torch.ones(2))
     with pytest.raises(ValueError, match="overlap"):
         dendsn.linear_ce(c, torch.zeros(4).expand(3, 4), w, t)
+
+
+@pytest.mark.parametrize("T", [0, 1, 63, 64, 65, 1000, 1 << 30])
+@pytest.mark.parametrize("batch,D", [(0, 5), (1, 0), (3, 70)])
+def test_scan_checkpoint_size(lib, T, batch, D):
+    """The binding allocates the checkpoints by their description; the library asks for the same."""
+    cfg = dendsn.GatedScanConfig(T=T, batch=batch, D=D)
+    assert 4 * cfg.ckpt_values() == dendsn.dendsn_scan_ckpt_bytes(cfg)
