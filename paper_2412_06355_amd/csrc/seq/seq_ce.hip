@@ -489,15 +489,15 @@ struct JoinArgs {
   int splits, io;
 };
 
-// VEC: values of a thread (4 where N is a multiple of it).
-template <int VEC>
+// VEC: values of a thread (4 where N is a multiple of it).  U: loads in flight, 16 of many
+// splits (256 of 8 x 512: 13 us, with 8 17; but 3 of 10000 x 512 20 against 15).
+template <int VEC, int U>
 __global__ void __launch_bounds__(kThreads) ce_join_splits_kernel(JoinArgs p) {
   const int64_t at = (int64_t(blockIdx.x) * kThreads + threadIdx.x) * VEC;
   if (at >= p.M * p.N) return;
   const float unit = p.unit ? *p.unit * p.scale : p.scale;
   const float* from = p.part + at;
   float s[VEC] = {};
-  constexpr int U = 8;  // loads in flight
   for (int k0 = 0; k0 < p.splits; k0 += U) {
     Pack<float, VEC> v[U];
 #pragma unroll
@@ -635,6 +635,121 @@ __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
   }
 }
 
+// Both gradients of few rows in fp32: the weights are read, and their gradient written, once.
+struct FewArgs {
+  const void *h, *w, *targets;
+  const float *z, *lse, *row_weight;
+  float *part, *gw;  // dH: [gridDim.y][M][D], without the scale
+  int64_t ldh, ldw, ldg, M, V, D, zrows, panels, each;  // each: panels of a block
+  float scale;
+  int wide;
+};
+
+// A block takes a run of panels of 64 classes by 256 features, a wave 64 of them, four
+// neighbours a lane.  The panel's dz is formed in LDS; a wave's sixteen classes of weights
+// enter its sums for dH (over the classes: k is a class), and meet the rows of hidden, MF
+// times sixteen, that stay in registers (k is a row) for their own gradient, which is
+// written at once.  Bound by the weights' bytes and, from 32 rows on, by the fp32 matrix
+// instructions.  50000 classes, 512 features: 8 rows 38 us (205 MB, 5.4 TB/s), 32 rows 58,
+// 64 rows 130 (50 TF; a block a CU, for its registers); as planes laid out and three
+// products of tiles 220, 210 and 220.  More rows go through the tiles.
+template <int MF>
+__global__ void __launch_bounds__(256, MF == 4 ? 1 : 2) ce_few_grad_kernel(FewArgs p) {
+  __shared__ float dz[16 * MF][kStep + 4];  // (rows four banks apart)
+  const int tid = threadIdx.x, lane = tid & 63, w = scalar(tid >> 6), i = lane & 15, q = lane >> 4;
+  const int64_t d = int64_t(blockIdx.x) * 256 + w * 64 + 4 * i;
+  const bool on = d < p.D;  // (and then all four)
+  auto keeps = [&](int64_t m) {
+    const int64_t t = m < p.M ? target_of(p.targets, p.wide, m) : -1;
+    return t >= 0 && t < p.V;
+  };
+  f32x4 hf[4 * MF], acc[MF][4];
+#pragma unroll
+  for (int s = 0; s < 4 * MF; ++s) {
+    const int64_t m = 4 * s + q;
+    hf[s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (on && keeps(m)) hf[s] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.h) + m * p.ldh + d);
+  }
+#pragma unroll
+  for (int f = 0; f < MF; ++f)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[f][c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int64_t k0 = blockIdx.y * p.each, k1 = min(k0 + p.each, p.panels);
+  const int64_t end = min(k1 * kStep, p.V);
+  f32x4 wf[2][4];  // sixteen classes, and those after them
+  auto fetch = [&](f32x4 (&to)[4], int64_t v0) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int64_t v = v0 + 4 * t + q;
+      to[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      if (on && v < end) to[t] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(p.w) + v * p.ldw + d);
+    }
+  };
+  fetch(wf[0], k0 * kStep);
+  for (int64_t k = k0; k < k1; ++k) {
+    const int64_t v0 = k * kStep;
+    __syncthreads();  // (the last panel's dz is read)
+#pragma unroll
+    for (int f = 0; f < MF; ++f) {
+      const int64_t m = 16 * f + tid / 16, v = v0 + tid % 16 * 4;
+      const int64_t t = m < p.M ? target_of(p.targets, p.wide, m) : -1;
+      f32x4 g{0.0f, 0.0f, 0.0f, 0.0f};
+      if (t >= 0 && t < p.V) {
+        const f32x4 z = *reinterpret_cast<const f32x4*>(p.z + (k * p.zrows + m) * kStep + tid % 16 * 4);
+        const float lse = p.lse[m], r = p.row_weight ? p.row_weight[m] : 1.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (v + e < p.V) g[e] = r * (exp_diff(p.scale * z[e], lse) - (v + e == t ? 1.0f : 0.0f));
+      }
+      *reinterpret_cast<f32x4*>(&dz[16 * f + tid / 16][tid % 16 * 4]) = g;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      f32x4 o[4];
+      fetch(wf[~u & 1], v0 + 16 * (u + 1));
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int f = 0; f < MF; ++f) {
+          const float a = dz[16 * f + i][16 * u + 4 * t + q];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[f][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, wf[u & 1][t][c], acc[f][c], 0, 0, 0);
+        }
+#pragma unroll
+      for (int s = 0; s < 4 * MF; ++s) {
+        const float a = dz[4 * s + q][16 * u + i];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, hf[s][c], o[c], 0, 0, 0);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t v = v0 + 16 * u + 4 * q + r;
+        f32x4 g;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) g[c] = o[c][r] == 0.0f ? 0.0f : p.scale * o[c][r];
+        if (on && v < p.V) *reinterpret_cast<f32x4_any*>(p.gw + v * p.ldg + d) = g;
+      }
+      __builtin_amdgcn_sched_barrier(0);  // (no later classes' loads before: the registers do not reach)
+    }
+  }
+#pragma unroll
+  for (int f = 0; f < MF; ++f)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int64_t m = 16 * f + 4 * q + r;
+      if (!on || m >= p.M) continue;
+      f32x4 g{0.0f, 0.0f, 0.0f, 0.0f};
+      if (keeps(m)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) g[c] = acc[f][c][r];
+      }
+      *reinterpret_cast<f32x4*>(p.part + (int64_t(blockIdx.y) * p.M + m) * p.D + d) = g;
+    }
+}
+
 // The gradient of the weights of no rows.
 __global__ void __launch_bounds__(kThreads) ce_zero_kernel(void* out, int64_t rows, int64_t cols, int64_t ld, int io) {
   for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < rows * cols; i += int64_t(gridDim.x) * kThreads) {
@@ -672,6 +787,7 @@ struct Plan {
   int64_t piece, pieces, rows;  // rows: of a panel
   int logits, dh_tile, dw_tile;  // rows of the products' tiles: 256 x 256, 192 x 256, 128 x 128
   int splits, dw_splits;         // of their sums: dH, dW
+  int64_t few;                   // panels of a block of ce_few_grad_kernel
   size_t h, w, stats, z, dz, chosen, lse, unit, dh, dw, total;
 };
 
@@ -772,7 +888,14 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
     const Split dw = split_of(c->V, c->D, ceil_div(p.piece, kStep) * planes, p.pieces > 1);
     p.dh_tile = dh.tile, p.splits = dh.parts;
     p.dw_tile = dw.tile, p.dw_splits = dw.parts;
-    p.dh = cv.take(p.splits > 1 ? size_t(p.splits) * size_t(p.piece) * size_t(c->D) * 4 : 0);
+    int64_t dh_parts = p.splits > 1 ? p.splits : 0;
+    if (p.planes == 3 && c->N <= 64) {  // two blocks a CU
+      const int64_t panels = p.Vp / kStep, columns = ceil_div(c->D, 256);
+      const int64_t parts = columns < 512 ? 512 / columns : 1;
+      p.few = ceil_div(panels, parts);
+      if (ceil_div(panels, p.few) > dh_parts) dh_parts = ceil_div(panels, p.few);
+    }
+    p.dh = cv.take(size_t(dh_parts) * size_t(p.piece) * size_t(c->D) * 4);
     const int dw_parts = p.dw_splits > 1 ? p.dw_splits : p.pieces > 1 ? 1 : 0;
     p.dw = cv.take(size_t(dw_parts) * size_t(c->V) * size_t(c->D) * 4);
   }
@@ -804,7 +927,8 @@ void pack(PackArgs a, bool bf, hipStream_t stream) {
 // of 64 k a wave, as far as the registers reach.  2048 features, 50001 classes in bf16: 8
 // rows 33 us, 32 rows 35 us; the tiles, which split no sum over k, 53 and 41 us (and fp32
 // would be laid out in planes first).  With the logits kept for training, 64 rows of 32000
-// classes and 1024 features: 19 us against 22; 32 rows of 50000 in fp32: 70 us against 137.
+// classes and 1024 features: 19 us against 22; 32 rows of 50000 in fp32: 70 us against 137;
+// 32 rows of 5000 classes and 1500 features in fp32: 31 against 107, and 20 of layout.
 template <typename IO>
 bool launch_score(const ScoreArgs& a, unsigned grid, hipStream_t stream) {
   constexpr bool BF = sizeof(IO) == 2;
@@ -820,6 +944,8 @@ bool launch_score(const ScoreArgs& a, unsigned grid, hipStream_t stream) {
   DENDSN_SCORE(4, 1)
   if constexpr (BF) {
     DENDSN_SCORE(1, 8) DENDSN_SCORE(2, 4) DENDSN_SCORE(4, 2)
+  } else {
+    DENDSN_SCORE(2, 3) DENDSN_SCORE(4, 2)
   }
 #undef DENDSN_SCORE
   return false;
@@ -836,8 +962,14 @@ void join_splits(const GradArgs& g, int splits, hipStream_t stream) {
   const JoinArgs j{g.part, g.unit, g.out, g.g.M, g.g.N, g.ld, g.scale, splits, g.io};
   const bool four = j.N % 4 == 0;
   const dim3 grid(unsigned(ceil_div(j.M * j.N, kThreads * (four ? 4 : 1)))), b(kThreads);
-  if (four) ce_join_splits_kernel<4><<<grid, b, 0, stream>>>(j);
-  else ce_join_splits_kernel<1><<<grid, b, 0, stream>>>(j);
+  if (splits > 32) {
+    if (four) ce_join_splits_kernel<4, 16><<<grid, b, 0, stream>>>(j);
+    else ce_join_splits_kernel<1, 16><<<grid, b, 0, stream>>>(j);
+  } else if (four) {
+    ce_join_splits_kernel<4, 8><<<grid, b, 0, stream>>>(j);
+  } else {
+    ce_join_splits_kernel<1, 8><<<grid, b, 0, stream>>>(j);
+  }
 }
 
 dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const void* weight, const void* targets,
@@ -858,8 +990,10 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     return bf ? launch_score<bf16_t>(a, blocks, stream) : launch_score<float>(a, blocks, stream);
   };
   const bool streamed = c->N <= 64 && few(hidden, targets, c->N);
+  const bool few_back = train && p.few && rows16(c, hidden, c->ld_hidden) && rows16(c, weight, c->ld_weight);
+  const bool no_tiles = streamed && (!train || few_back);
   Operand w{};
-  if (streamed && !train) {
+  if (no_tiles) {
     // (no product reads it)
   } else if (direct(c, weight, c->ld_weight)) {
     w = Operand{static_cast<const uint16_t*>(weight), c->ld_weight, 0, 0, c->V, c->D};
@@ -869,7 +1003,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     w = Operand{a.dst, p.Dp, a.plane, kFinite * a.plane, c->V, p.Dp};
   }
   float* unit = nullptr;
-  if (train && row_weight) {
+  if (train && row_weight && !few_back) {
     unit = reinterpret_cast<float*>(ws + p.unit);
     ce_unit_kernel<<<dim3(1), dim3(1024), 0, stream>>>(UnitArgs{row_weight, targets, unit, c->N, c->V, wide});
   }
@@ -878,7 +1012,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     const void* hp = static_cast<const char*>(hidden) + size_t(r0) * size_t(c->ld_hidden) * esz;
     const void* tp = static_cast<const char*>(targets) + size_t(r0) * isz;
     Operand h{};
-    if (streamed && !train) {
+    if (no_tiles) {
     } else if (!train && direct(c, hp, c->ld_hidden)) {
       h = Operand{static_cast<const uint16_t*>(hp), c->ld_hidden, 0, 0, M, c->D};
     } else {
@@ -909,6 +1043,19 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     s.M = M; s.zrows = p.rows; s.V = c->V; s.scale = c->logit_scale; s.tiles = l.g.tiles_n; s.wide = wide;
     ce_loss_kernel<<<dim3(unsigned(ceil_div(M, kThreads / 64))), dim3(kThreads), 0, stream>>>(s);
     if (!train) continue;
+    if (few_back) {
+      FewArgs a{hidden, weight, targets, l.z, s.lse, row_weight, reinterpret_cast<float*>(ws + p.dh), static_cast<float*>(grad_weight),
+                c->ld_hidden, c->ld_weight, c->ld_grad_weight, M, c->V, c->D, p.rows, p.Vp / kStep, p.few, c->logit_scale, wide};
+      const dim3 grid(unsigned(ceil_div(c->D, 256)), unsigned(ceil_div(a.panels, a.each))), b(256);
+      if (M <= 16) ce_few_grad_kernel<1><<<grid, b, 0, stream>>>(a);
+      else if (M <= 32) ce_few_grad_kernel<2><<<grid, b, 0, stream>>>(a);
+      else ce_few_grad_kernel<4><<<grid, b, 0, stream>>>(a);
+      GradArgs g{};
+      g.g.M = M; g.g.N = c->D;
+      g.out = grad_hidden; g.part = a.part; g.scale = c->logit_scale; g.ld = c->ld_grad_hidden; g.io = c->io;
+      join_splits(g, int(grid.y), stream);
+      continue;
+    }
 
     DzArgs z{};
     z.z = l.z; z.lse = s.lse; z.row_weight = row_weight ? row_weight + r0 : nullptr;

@@ -111,6 +111,27 @@ def test_few_rows_trained(gpu_device, N, V, D, io):
         check(cfg, h, w, t, r)
 
 
+@pytest.mark.parametrize("N,V,D", [(40, 20001, 1100), (16, 40000, 64), (64, 9000, 2052), (3, 33000, 4), (33, 65, 260),
+                                   (20, 3000, 1500), (64, 4100, 1024)])
+def test_few_rows_trained_in_fp32(gpu_device, N, V, D):
+    """Blocks of several panels of classes, features past a block's and a wave's share, rows of
+    weights that lie apart, a row without a target that holds infinities."""
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, logit_scale=-0.5 if N % 2 else 1.5)
+    announce(f"ce few rows {cfg}")
+    h, w, t, r = make(N, V, D, "f32", gpu_device, V)
+    got = check(cfg, h, w, t, r)
+    wide = torch.full((V, D + 8), float("nan"), device=gpu_device)
+    wide[:, 4:D + 4] = w
+    apart = dendsn.linear_ce_train(cfg, h, wide[:, 4:D + 4], t, r)
+    for k in got:
+        assert torch.equal(got[k], apart[k]), k
+    t[0] = -1
+    h[0] = float("inf")
+    zero = dendsn.linear_ce_train(cfg, h, w, t, None)
+    assert not zero["grad_hidden"][0].view(torch.int32).any()
+    assert bool(torch.isfinite(zero["grad_hidden"]).all()) and bool(torch.isfinite(zero["grad_weight"]).all())
+
+
 @pytest.mark.parametrize("N,V,D,io", [(3000, 1000, 512, "bf16"), (1025, 700, 261, "f32"), (2111, 255, 64, "f32"),
                                       (8200, 300, 250, "bf16"), (600, 5000, 300, "f32")])
 def test_long_sums_over_rows(gpu_device, N, V, D, io):
