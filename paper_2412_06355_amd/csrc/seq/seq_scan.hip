@@ -179,9 +179,10 @@ __global__ void __launch_bounds__(kW * 64, W ? 4 : 2) scan_fwd_kernel(ScanArgs p
   constexpr bool ONE = W > 0;
   constexpr int N = ONE ? W : kW;  // waves of a tile
   __shared__ float2 sh[ONE ? 1 : 2][kW][64 * VEC];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave % N;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int w = N < kW ? wave % N : wave, first = N < kW ? wave - w : 0;  // in its tile; its tile's first
   const int b = blockIdx.y, seg = blockIdx.z;
-  const int d0 = int(((blockIdx.x * (kW / N) + wave / N) * 64 + lane) * VEC);
+  const int d0 = int(((N < kW ? blockIdx.x * (kW / N) + wave / N : blockIdx.x) * 64 + lane) * VEC);
   const bool on = d0 < p.D;
   const int d = on ? min(d0, int(p.D) - VEC) : 0;  // (an odd row's last lane shares a channel)
   const int len = seq_length(p, b);
@@ -239,7 +240,7 @@ __global__ void __launch_bounds__(kW * 64, W ? 4 : 2) scan_fwd_kernel(ScanArgs p
       in[v] = carry[v];
 #pragma unroll
       for (int q = 0; q < N; ++q) {
-        const float2 r = N > 1 ? sh[buf][wave - w + q][v * 64 + lane] : make_float2(P[kL - 1][v], H[kL - 1][v]);
+        const float2 r = N > 1 ? sh[buf][first + q][v * 64 + lane] : make_float2(P[kL - 1][v], H[kL - 1][v]);
         if (q == w) in[v] = carry[v];
         carry[v] = fmaf(r.x, carry[v], r.y);
       }
@@ -285,9 +286,10 @@ __global__ void __launch_bounds__(kW * 64, 2) scan_bwd_kernel(ScanArgs p) {
   constexpr bool ONE = W > 0;  // as in the forward
   constexpr int N = ONE ? W : kW, S = ONE ? 1 : 2;
   __shared__ float shA[S][kW][64 * VEC], shH[S][kW][64 * VEC], shC[S][kW][64 * VEC];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), w = wave % N;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int w = N < kW ? wave % N : wave, first = N < kW ? wave - w : 0;  // in its tile; its tile's first
   const int b = blockIdx.y, seg = blockIdx.z;
-  const int d0 = int(((blockIdx.x * (kW / N) + wave / N) * 64 + lane) * VEC);
+  const int d0 = int(((N < kW ? blockIdx.x * (kW / N) + wave / N : blockIdx.x) * 64 + lane) * VEC);
   const bool on = d0 < p.D;
   const int d = on ? min(d0, int(p.D) - VEC) : 0;  // (an odd row's last lane shares a channel)
   const int len = seq_length(p, b);
@@ -360,7 +362,7 @@ __global__ void __launch_bounds__(kW * 64, 2) scan_bwd_kernel(ScanArgs p) {
     if (N > 1) lds_barrier();
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      const int first = wave - w, at = v * 64 + lane;
+      const int at = v * 64 + lane;
 #pragma unroll
       for (int q = 0; q < N - 1; ++q)
         if (q < w) hin[v] = fmaf(shA[buf][first + q][at], hin[v], shH[buf][first + q][at]);
