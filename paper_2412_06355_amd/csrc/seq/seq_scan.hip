@@ -14,8 +14,8 @@
 //
 // Bound by memory: bytes read once, written once, and the checkpoints (1/64 of a fp32
 // state a step).  8192 steps, 8 sequences, 4096 channels in bf16: both together 823 us
-// (5.2 TB/s, as a copy; under a profiler 341 and 575).  64 steps, 32 sequences: 34 us, 13
-// and 23 under a profiler.
+// (5.2 TB/s, as a copy; under a profiler 341 and 575).  64 steps, 32 sequences: 33 us, 12.5
+// and 22 under a profiler.
 #include "seq_common.h"
 
 namespace dendsn_seq {
