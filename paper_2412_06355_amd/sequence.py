@@ -81,14 +81,21 @@ def _check(status: int):
 
 
 def _ptr(t):
-    return None if t is None else t.data_ptr()
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError(f"a tensor on {t.device}: the library takes GPU memory alone")
+    return t.data_ptr()
 
 
 def _stream(device):
-    """The current stream of the device: a serving step's calls are a few microseconds long, so
-    the handle is asked for without building a Stream object."""
+    """The current stream of the GPU that the tensors lie on (no other device has one): a serving
+    step's calls are a few microseconds long, so the handle is asked for without building a Stream
+    object."""
     import torch
 
+    if device.type != "cuda":
+        raise ValueError(f"tensors on {device}: the library takes GPU memory alone")
     return torch._C._cuda_getCurrentRawStream(device.index if device.index is not None else
                                               torch.cuda.current_device())
 
@@ -205,12 +212,11 @@ def embedding(cfg: EmbeddingConfig, ids, table):
     _expect(table, "table", (cfg.V, cfg.D), dt, dev, rows=True)
     if table.shape[0] > 1 and table.stride(0) < cfg.D:
         raise ValueError("table: rows overlap")
+    index, st = _index_code(ids, "ids"), _stream(dev)
     # (a serving step's lookup: the struct and the output by the shortest way)
     out = table.new_empty((cfg.n, cfg.D))
-    c = dendsn_embed_cfg(cfg.n, cfg.V, cfg.D, _row_stride(table, cfg.D), cfg.D, IO[cfg.io], _index_code(ids, "ids"),
-                         cfg.scale)
-    _check(seq_lib().dendsn_embed_forward(ctypes.byref(c), ids.data_ptr(), table.data_ptr(), out.data_ptr(),
-                                          _stream(dev)))
+    c = dendsn_embed_cfg(cfg.n, cfg.V, cfg.D, _row_stride(table, cfg.D), cfg.D, IO[cfg.io], index, cfg.scale)
+    _check(seq_lib().dendsn_embed_forward(ctypes.byref(c), ids.data_ptr(), table.data_ptr(), out.data_ptr(), st))
     return out
 
 
@@ -222,13 +228,14 @@ def embedding_backward(cfg: EmbeddingConfig, ids, grad_out, workspace=None):
     dt, dev = _io_dtype(cfg.io), grad_out.device
     _expect(ids, "ids", (cfg.n,), None, dev)
     _expect(grad_out, "grad_out", (cfg.n, cfg.D), dt, dev, rows=True)
+    index, st = _index_code(ids, "ids"), _stream(dev)
     grad_table = torch.empty((cfg.V, cfg.D), dtype=dt, device=dev)
     c = cfg.to_c()
-    c.index, c.ld_table = _index_code(ids, "ids"), cfg.D
+    c.index, c.ld_table = index, cfg.D
     c.ld_out = int(grad_out.stride(0)) if cfg.n > 1 else cfg.D
     ws = _workspace(_bytes(seq_lib().dendsn_embed_workspace_bytes, ctypes.byref(c)), workspace, dev)
     _check(seq_lib().dendsn_embed_backward(ctypes.byref(c), _ptr(ids), _ptr(grad_out), _ptr(grad_table), _ptr(ws),
-                                           _nbytes(ws), _stream(dev)))
+                                           _nbytes(ws), st))
     return grad_table
 
 
@@ -285,12 +292,15 @@ def dendsn_scan_backward(cfg: GatedScanConfig, x, g, lengths, ckpt, grad_h, grad
                                           _ptr(workspace), _nbytes(workspace), st))
 
 
+def _step_cfg(cfg, x, g, h):
+    return dendsn_scan_cfg(cfg.T, cfg.batch, cfg.D, 0, x.stride(0), 0, g.stride(0), 0, h.stride(0), 0, 0, 0, 0, 0, 0,
+                           IO[cfg.io], GATE[cfg.gate], cfg.leaky)
+
+
 def dendsn_scan_step(cfg: GatedScanConfig, x, g, slots, state, h, stream=None):
     st = stream if stream is not None else _stream(x.device)
-    c = dendsn_scan_cfg(cfg.T, cfg.batch, cfg.D, 0, x.stride(0), 0, g.stride(0), 0, h.stride(0), 0, 0, 0, 0, 0, 0,
-                        IO[cfg.io], GATE[cfg.gate], cfg.leaky)
-    _check(seq_lib().dendsn_scan_step(ctypes.byref(c), x.data_ptr(), g.data_ptr(), state.shape[0], _ptr(slots),
-                                      state.data_ptr(), h.data_ptr(), st))
+    _check(seq_lib().dendsn_scan_step(ctypes.byref(_step_cfg(cfg, x, g, h)), _ptr(x), _ptr(g), state.shape[0], _ptr(slots),
+                                      _ptr(state), _ptr(h), st))
 
 
 def _check_scan(cfg, x, g, lengths):
@@ -312,13 +322,14 @@ def gated_scan(cfg: GatedScanConfig, x, g, h0=None, lengths=None, *, save_ckpt: 
 
     dt, dev, shape = _check_scan(cfg, x, g, lengths)
     _expect(h0, "h0", shape[1:], torch.float32, dev, optional=True)
+    st = _stream(dev)
     h = x.new_empty(shape)
     h_last = torch.empty(shape[1:], dtype=torch.float32, device=dev)
     c, fn = cfg.to_c(x, g, h), seq_lib()
     ckpt = torch.empty((cfg.ckpt_values(),), dtype=torch.float32, device=dev) if save_ckpt else None
     ws = _workspace(_bytes(fn.dendsn_scan_workspace_bytes, ctypes.byref(c), 0), workspace, dev)
     _check(fn.dendsn_scan_forward(ctypes.byref(c), _ptr(x), _ptr(g), _ptr(h0), _ptr(lengths), _ptr(h), _ptr(h_last),
-                                  _ptr(ckpt), _ptr(ws), _nbytes(ws), _stream(dev)))
+                                  _ptr(ckpt), _ptr(ws), _nbytes(ws), st))
     return h, h_last, ckpt
 
 
@@ -330,18 +341,18 @@ def gated_scan_backward(cfg: GatedScanConfig, x, g, lengths, ckpt, grad_h, grad_
     dt, dev, shape = _check_scan(cfg, x, g, lengths)
     _expect(grad_h, "grad_h", shape, dt, dev, rows=True)
     _expect(grad_h_last, "grad_h_last", shape[1:], torch.float32, dev, optional=True)
-    fn = seq_lib()
-    out = dict(grad_x=x.new_empty(shape), grad_g=x.new_empty(shape),
-               grad_h0=torch.empty(shape[1:], dtype=torch.float32, device=dev))
-    c = cfg.to_c(x, g, None, grad_h, out["grad_x"], out["grad_g"])
     need = 4 * cfg.ckpt_values()
     if need and (ckpt is None or ckpt.dtype != torch.float32 or ckpt.device != dev or not ckpt.is_contiguous()
                  or ckpt.numel() * 4 < need):
         raise ValueError(f"ckpt must be the forward's checkpoints: contiguous float32 on {dev}, {need} bytes")
+    st, fn = _stream(dev), seq_lib()
+    out = dict(grad_x=x.new_empty(shape), grad_g=x.new_empty(shape),
+               grad_h0=torch.empty(shape[1:], dtype=torch.float32, device=dev))
+    c = cfg.to_c(x, g, None, grad_h, out["grad_x"], out["grad_g"])
     ws = _workspace(_bytes(fn.dendsn_scan_workspace_bytes, ctypes.byref(c), 1), workspace, dev)
     _check(fn.dendsn_scan_backward(ctypes.byref(c), _ptr(x), _ptr(g), _ptr(lengths), _ptr(ckpt), _ptr(grad_h),
                                    _ptr(grad_h_last), _ptr(out["grad_x"]), _ptr(out["grad_g"]),
-                                   _ptr(out["grad_h0"]), _ptr(ws), _nbytes(ws), _stream(dev)))
+                                   _ptr(out["grad_h0"]), _ptr(ws), _nbytes(ws), st))
     return out
 
 
@@ -356,8 +367,10 @@ def gated_scan_step(cfg: GatedScanConfig, x, g, state, slots=None):
     _expect(g, "g", shape, dt, dev, rows=True)
     _expect(state, "state", (state.shape[0], cfg.D), torch.float32, dev)
     _expect(slots, "slots", (cfg.batch,), torch.int32, dev, optional=True)
+    st = _stream(dev)
     h = x.new_empty(shape)
-    dendsn_scan_step(cfg, x, g, slots, state, h)
+    _check(seq_lib().dendsn_scan_step(ctypes.byref(_step_cfg(cfg, x, g, h)), x.data_ptr(), g.data_ptr(), state.shape[0],
+                                      _ptr(slots), state.data_ptr(), h.data_ptr(), st))
     return h
 
 
@@ -429,11 +442,12 @@ def linear_ce(cfg: LinearCEConfig, hidden, weight, targets, *, workspace=None):
     import torch
 
     _, dev, c = _check_ce(cfg, hidden, weight, targets)
+    st = _stream(dev)
     loss, lse = (torch.empty((cfg.N,), dtype=torch.float32, device=dev) for _ in range(2))
     fn = seq_lib()
     ws = _workspace(_bytes(fn.dendsn_ce_workspace_bytes, ctypes.byref(c), 0), workspace, dev)
     _check(fn.dendsn_ce_forward(ctypes.byref(c), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(loss), _ptr(lse),
-                                _ptr(ws), _nbytes(ws), _stream(dev)))
+                                _ptr(ws), _nbytes(ws), st))
     return loss, lse
 
 
@@ -444,6 +458,7 @@ def linear_ce_train(cfg: LinearCEConfig, hidden, weight, targets, row_weight=Non
 
     dt, dev, c = _check_ce(cfg, hidden, weight, targets)
     _expect(row_weight, "row_weight", (cfg.N,), torch.float32, dev, optional=True)
+    st = _stream(dev)
     out = dict(loss=torch.empty((cfg.N,), dtype=torch.float32, device=dev),
                lse=torch.empty((cfg.N,), dtype=torch.float32, device=dev),
                grad_hidden=torch.empty((cfg.N, cfg.D), dtype=dt, device=dev),
@@ -452,5 +467,5 @@ def linear_ce_train(cfg: LinearCEConfig, hidden, weight, targets, row_weight=Non
     ws = _workspace(_bytes(fn.dendsn_ce_workspace_bytes, ctypes.byref(c), 1), workspace, dev)
     _check(fn.dendsn_ce_train(ctypes.byref(c), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(row_weight),
                               _ptr(out["loss"]), _ptr(out["lse"]), _ptr(out["grad_hidden"]), _ptr(out["grad_weight"]),
-                              _ptr(ws), _nbytes(ws), _stream(dev)))
+                              _ptr(ws), _nbytes(ws), st))
     return out

@@ -314,3 +314,54 @@ def test_scan_checkpoint_size(lib, T, batch, D):
     """The binding allocates the checkpoints by their description; the library asks for the same."""
     cfg = dendsn.GatedScanConfig(T=T, batch=batch, D=D)
     assert 4 * cfg.ckpt_values() == dendsn.dendsn_scan_ckpt_bytes(cfg)
+
+
+def _cpu_calls():
+    """Every call of the binding with valid arguments, but for their place: the CPU's memory."""
+    import torch
+
+    e = dendsn.EmbeddingConfig(n=4, V=8, D=6)
+    s = dendsn.GatedScanConfig(T=3, batch=2, D=4)
+    c = dendsn.LinearCEConfig(N=3, V=5, D=4)
+    ids, table, rows = torch.zeros(4, dtype=torch.int64), torch.zeros(8, 6), torch.zeros(4, 6)
+    x, ckpt, state = torch.zeros(3, 2, 4), torch.zeros(8), torch.zeros(2, 4)
+    h, w, t, f = torch.zeros(3, 4), torch.zeros(5, 4), torch.zeros(3, dtype=torch.int32), torch.zeros(3)
+    ws, st = torch.zeros(1 << 16, dtype=torch.uint8), ctypes.c_void_p(0)
+    calls = dict(
+        embedding=lambda: dendsn.embedding(e, ids, table),
+        embedding_backward=lambda: dendsn.embedding_backward(e, ids, rows),
+        gated_scan=lambda: dendsn.gated_scan(s, x, x),
+        gated_scan_backward=lambda: dendsn.gated_scan_backward(s, x, x, None, ckpt, x),
+        gated_scan_step=lambda: dendsn.gated_scan_step(s.with_(T=1), x[0], x[0], state),
+        linear_ce=lambda: dendsn.linear_ce(c, h, w, t),
+        linear_ce_train=lambda: dendsn.linear_ce_train(c, h, w, t))
+    for k, stream in (("", None), (" on a stream", st)):
+        calls.update({
+            "dendsn_embed_forward" + k: lambda stream=stream: dendsn.dendsn_embed_forward(e, ids, table, rows, stream),
+            "dendsn_embed_backward" + k: lambda stream=stream: dendsn.dendsn_embed_backward(e, ids, rows, table, ws, stream),
+            "dendsn_scan_forward" + k: lambda stream=stream: dendsn.dendsn_scan_forward(s, x, x, None, None, x, None, ckpt, ws,
+                                                                                     stream),
+            "dendsn_scan_backward" + k: lambda stream=stream: dendsn.dendsn_scan_backward(s, x, x, None, ckpt, x, None, x, x,
+                                                                                      None, ws, stream),
+            "dendsn_scan_step" + k: lambda stream=stream: dendsn.dendsn_scan_step(s.with_(T=1), x[0], x[0], None, state, x[0],
+                                                                              stream),
+            "dendsn_ce_forward" + k: lambda stream=stream: dendsn.dendsn_ce_forward(c, h, w, t, f, None, ws, stream),
+            "dendsn_ce_train" + k: lambda stream=stream: dendsn.dendsn_ce_train(c, h, w, t, None, f, None, h, w, ws, stream)})
+    return calls
+
+
+@pytest.mark.parametrize("name", list(_cpu_calls()))
+def test_tensors_of_the_cpu_are_refused(monkeypatch, name):
+    """A host pointer would fault the GPU: the binding refuses it before any call of the library."""
+    from paper_2412_06355_amd import sequence
+
+    reached = []
+
+    class Stub:
+        def __getattr__(self, entry):
+            return lambda *a: reached.append(entry) or 0
+
+    monkeypatch.setattr(sequence, "seq_lib", Stub)
+    with pytest.raises(ValueError, match="GPU memory"):
+        _cpu_calls()[name]()
+    assert not reached
