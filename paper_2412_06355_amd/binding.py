@@ -147,9 +147,22 @@ def _ptr(t):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+def _check_device(device):
+    """Kernels are launched on the current GPU, whatever the stream (the default stream of every
+    GPU has the handle 0): tensors of another one would be worked on by the wrong device."""
+    import torch
+
+    if device.type != "cuda":
+        raise ValueError(f"tensors on {device}: the library takes GPU memory alone")
+    if device.index is not None and device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"tensors on {device}, but the current device is cuda:{torch._C._cuda_getDevice()}: "
+                         "make theirs the current one (torch.cuda.device)")
+
+
 def _stream(device):
     import torch
 
+    _check_device(device)
     return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
 
 

@@ -6,7 +6,8 @@ with its gradients.  As in the layer's binding, the functions named like the C
 entry points take the C arguments (tensors in place of pointers); ``embedding``,
 ``gated_scan``, ``linear_ce`` and their companions check shapes, allocate the
 outputs and call them.  Everything is computed by the library's HIP kernels, on
-the current stream of the tensors' device; there is no fallback.
+the current stream of the tensors' device, which has to be the current device; there is no
+fallback.
 """
 
 from __future__ import annotations
@@ -15,7 +16,7 @@ import ctypes
 import dataclasses
 from dataclasses import dataclass
 
-from .binding import IO, DendSNError
+from .binding import IO, DendSNError, _check_device
 from .binding import lib as _lib
 
 GATE = {"sigmoid": 0, "decay": 1}
@@ -89,13 +90,12 @@ def _ptr(t):
 
 
 def _stream(device):
-    """The current stream of the GPU that the tensors lie on (no other device has one): a serving
-    step's calls are a few microseconds long, so the handle is asked for without building a Stream
-    object."""
+    """The current stream of the GPU that the tensors lie on, which has to be the current one: a
+    serving step's calls are a few microseconds long, so the handle is asked for without building a
+    Stream object."""
     import torch
 
-    if device.type != "cuda":
-        raise ValueError(f"tensors on {device}: the library takes GPU memory alone")
+    _check_device(device)
     return torch._C._cuda_getCurrentRawStream(device.index if device.index is not None else
                                               torch.cuda.current_device())
 
@@ -299,8 +299,8 @@ def _step_cfg(cfg, x, g, h):
 
 def dendsn_scan_step(cfg: GatedScanConfig, x, g, slots, state, h, stream=None):
     st = stream if stream is not None else _stream(x.device)
-    _check(seq_lib().dendsn_scan_step(ctypes.byref(_step_cfg(cfg, x, g, h)), _ptr(x), _ptr(g), state.shape[0], _ptr(slots),
-                                      _ptr(state), _ptr(h), st))
+    _check(seq_lib().dendsn_scan_step(ctypes.byref(_step_cfg(cfg, x, g, h)), _ptr(x), _ptr(g), state.shape[0],
+                                      _ptr(slots), _ptr(state), _ptr(h), st))
 
 
 def _check_scan(cfg, x, g, lengths):

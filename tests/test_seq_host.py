@@ -365,3 +365,21 @@ def test_tensors_of_the_cpu_are_refused(monkeypatch, name):
     with pytest.raises(ValueError, match="GPU memory"):
         _cpu_calls()[name]()
     assert not reached
+
+
+@pytest.mark.parametrize("module", ["binding", "sequence"])
+def test_tensors_of_another_gpu_are_refused(monkeypatch, module):
+    """Every GPU's default stream has the handle 0: a launch would run on the current GPU."""
+    import importlib
+
+    import torch
+
+    m = importlib.import_module(f"paper_2412_06355_amd.{module}")
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda index: 0, raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: type("Stream", (), dict(cuda_stream=0))())
+    assert not getattr(m._stream(torch.device("cuda", 0)), "value", 0)
+    with pytest.raises(ValueError, match="current device is cuda:0"):
+        m._stream(torch.device("cuda", 1))
+    with pytest.raises(ValueError, match="GPU memory"):
+        m._stream(torch.device("cpu"))
