@@ -344,10 +344,13 @@ __global__ void __launch_bounds__(kThreads) embed_sum_kernel(SumArgs p) {
   }
   __syncthreads();
   const uint32_t have = named;
-  const float zero[VEC] = {};
+  Pack<IO, VEC> zero;  // +0, not the scale's product with it: a negative one has -0
+#pragma unroll
+  for (int k = 0; k < VEC; ++k) zero.v[k] = narrow<IO>(0.0f);
   for (uint32_t r = w; r < rows; r += kThreads / 64) {
     if (have >> r & 1) continue;
-    for (int64_t d = lane * VEC; d < p.D; d += 64 * VEC) store_row<IO, VEC>(p, v0 + r, min(d, p.D - VEC), zero);
+    IO* row = static_cast<IO*>(p.table) + int64_t(v0 + r) * p.ldt;
+    for (int64_t d = lane * VEC; d < p.D; d += 64 * VEC) *reinterpret_cast<Pack<IO, VEC>*>(row + min(d, p.D - VEC)) = zero;
   }
 }
 

@@ -121,3 +121,20 @@ def test_nothing(gpu_device):
     none = dendsn.embedding(cfg.with_(n=3, V=0), torch.zeros(3, dtype=torch.int64, device=gpu_device),
                             torch.zeros((0, 5), device=gpu_device))
     assert none.shape == (3, 5) and not none.any()
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [3, 40])
+def test_rows_without_a_token_are_plus_zero_at_any_scale(gpu_device, io, D):
+    """The product of a negative scale with no sum would be -0."""
+    n, V = 50, 70
+    ids, _, grad = make(n, V, D, io, "random", seed=D)
+    cfg = dendsn.EmbeddingConfig(n=n, V=V, D=D, io=io, scale=-2.0)
+    announce(f"embed negative scale {cfg}")
+    got = dendsn.embedding_backward(cfg, ids.to(gpu_device), grad.to(gpu_device))
+    ref, bound = seq_ref.embed_backward(ids, grad, V, -2.0, io)
+    seq_ref.assert_within(got, ref, bound, "grad_table")
+    named = torch.zeros(V, dtype=torch.bool)
+    named[ids] = True
+    assert not named.all()
+    assert not got.cpu()[~named].view(torch.int16 if io == "bf16" else torch.int32).any()
