@@ -547,7 +547,7 @@ __global__ void __launch_bounds__(kThreads) ce_loss_kernel(LossArgs p) {
   float sum = 0.0f;
   for (int i = lane; i < p.tiles; i += 64) {
     const float2 s = p.stats[m * p.tiles + i];
-    sum += s.y * exp_diff(s.x == -INFINITY ? 0.0f : s.x, ref);
+    sum += s.y * exp_diff(s.x, ref);  // (a tile at minus infinity: 0 times 0)
   }
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);

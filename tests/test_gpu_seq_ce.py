@@ -313,3 +313,23 @@ def test_nothing(gpu_device):
     got = dendsn.linear_ce_train(cfg, h, torch.ones((9, 5), device=gpu_device), t)
     assert loss.numel() == 0 and lse.numel() == 0 and got["grad_weight"].shape == (9, 5)
     assert not got["grad_weight"].view(torch.int32).any()
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [20, 100])
+def test_tiles_at_minus_infinity_beside_low_logits(gpu_device, N, io):
+    """Classes of whole tiles at minus infinity have no part in rows whose other logits are all far
+    below zero (exp(-lse) is infinite there)."""
+    V, D = 900, 64
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    h, w, t, r = make(N, V, D, io, gpu_device, 5, ignored=0.0)
+    t = t % 100
+    h[:, 0], w[:100, 0], w[100:, 0] = 1.0, -200.0, -float("inf")
+    announce(f"ce tiles at minus infinity {cfg}")
+    ref = seq_ref.ce(h, w, t, 1.0, io, train=False)
+    assert float(ref["lse"][0].max()) < -100.0
+    loss, lse = dendsn.linear_ce(cfg, h, w, t)
+    got = dendsn.linear_ce_train(cfg, h, w, t, r)
+    for k, v in dict(loss=loss, lse=lse).items():
+        seq_ref.assert_within(v, *ref[k], k)
+        seq_ref.assert_within(got[k], *ref[k], k + " of the training call")
