@@ -112,6 +112,10 @@ __device__ __forceinline__ float exp_diff(float a, float b) {
   return __builtin_amdgcn_exp2f(1.44269504f * (a - b));
 }
 
+// What the exponentials of a row are taken from: its maximum, or 0 where that is infinite (the
+// sum is then 0 or infinite, and so is what it gives).
+__device__ __forceinline__ float anchor(float top) { return fabsf(top) == INFINITY ? 0.0f : top; }
+
 struct LogitArgs {
   GemmArgs g;
   float scale;
@@ -147,7 +151,7 @@ __device__ __forceinline__ void row_statistics(const f32x4 (&acc)[FN][FM], int64
 #pragma unroll
       for (int r = 0; r < 4; ++r) top = fmaxf(top, in(i, r) ? acc[i][j][r] : -INFINITY);
     top = over_groups(top, [](float a, float b) { return fmaxf(a, b); });
-    const float ref = top == -INFINITY ? 0.0f : top;
+    const float ref = anchor(top);
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < FN; ++i)
@@ -233,7 +237,7 @@ __global__ void __launch_bounds__(WM * WN * 64) ce_logits_kernel(LogitArgs) {
 #pragma unroll
       for (int q = 1; q < WN; ++q) {
         const float2 b = part[q][r];
-        const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.0f : top;
+        const float top = fmaxf(a.x, b.x), ref = anchor(top);
         a = make_float2(top, a.y * exp_diff(a.x, ref) + b.y * exp_diff(b.x, ref));
       }
       p.stats[(m0 + r) * p.g.tiles_n + this_tn] = a;
@@ -345,7 +349,7 @@ __global__ void __launch_bounds__(kScoreWaves * 64) ce_score_kernel(ScoreArgs p)
         z[r] = v < n1 ? p.scale * z[r] : -INFINITY;
         most = fmaxf(most, z[r]);
       }
-      const float ref = most == -INFINITY ? 0.0f : most;
+      const float ref = anchor(most);
       sum *= exp_diff(top, ref);
 #pragma unroll
       for (int r = 0; r < 4; ++r) sum += exp_diff(z[r], ref);
@@ -361,7 +365,7 @@ __global__ void __launch_bounds__(kScoreWaves * 64) ce_score_kernel(ScoreArgs p)
   }
   if (w < MF) {
     const float most = over_groups(top, [](float a, float b) { return fmaxf(a, b); });
-    const float ref = most == -INFINITY ? 0.0f : most;
+    const float ref = anchor(most);
     sum = over_groups(sum * exp_diff(top, ref), [](float a, float b) { return a + b; });
     if (lane < 16 && m < p.M) p.stats[m * gridDim.x + blockIdx.x] = make_float2(most, sum);
   }
@@ -543,7 +547,7 @@ __global__ void __launch_bounds__(kThreads) ce_loss_kernel(LossArgs p) {
   for (int i = lane; i < p.tiles; i += 64) top = fmaxf(top, p.stats[m * p.tiles + i].x);
 #pragma unroll
   for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  const float ref = top == -INFINITY ? 0.0f : top;
+  const float ref = anchor(top);
   float sum = 0.0f;
   for (int i = lane; i < p.tiles; i += 64) {
     const float2 s = p.stats[m * p.tiles + i];

@@ -333,3 +333,27 @@ def test_tiles_at_minus_infinity_beside_low_logits(gpu_device, N, io):
     for k, v in dict(loss=loss, lse=lse).items():
         seq_ref.assert_within(v, *ref[k], k)
         seq_ref.assert_within(got[k], *ref[k], k + " of the training call")
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [20, 100])
+def test_logits_at_plus_infinity(gpu_device, N, io):
+    """One class that rows put at plus and at minus infinity in turn: lse and loss are infinite where
+    the definition has them so, and as ever elsewhere."""
+    V, D = 900, 64
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    h, w, t, r = make(N, V, D, io, gpu_device, 6, ignored=0.0)
+    t = t % 100
+    h[:, 0] = torch.where(torch.arange(N, device=gpu_device) % 2 == 0, 1.0, -1.0).to(h.dtype)
+    for at in (3, 500, 899):
+        wi = w.clone()
+        wi[at, 0] = float("inf")
+        to = torch.where(t == at, t + 1, t)
+        announce(f"ce logits at plus infinity {cfg} class {at}")
+        ref = seq_ref.ce(h, wi, to, 1.0, io, train=False)
+        assert bool((ref["lse"][0][::2] == float("inf")).all()) and bool(torch.isfinite(ref["lse"][0][1::2]).all())
+        loss, lse = dendsn.linear_ce(cfg, h, wi, to)
+        got = dendsn.linear_ce_train(cfg, h, wi, to, r)
+        for k, v in dict(loss=loss, lse=lse).items():
+            seq_ref.assert_within(v, *ref[k], k)
+            seq_ref.assert_within(got[k], *ref[k], k + " of the training call")
