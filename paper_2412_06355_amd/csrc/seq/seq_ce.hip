@@ -530,13 +530,16 @@ struct LossArgs {
   const float* z;       // kept logits, or
   const float* chosen;  // the target's
   const void* targets;
-  float *loss, *lse;    // lse: also what the gradient reads
+  float *loss, *lse;
+  float2* norm;         // [M] what the gradient reads: what exponentials are taken from, one over their sum (or NULL)
   int64_t M, zrows, V;
   float scale;
   int tiles, wide;
 };
 
-// A wave a row: joins the tiles' statistics (8192 rows of 500: 19 us).
+// A wave a row: joins the tiles' statistics (8192 rows of 500: 19 us).  The gradient gets the
+// maximum and the sum apart, and the loss its difference from the maximum first: in lse, their sum,
+// logits of 4e4 leave the probabilities 0.2 % of their own rounding.
 __global__ void __launch_bounds__(kThreads) ce_loss_kernel(LossArgs p) {
   const int lane = threadIdx.x & 63;
   const int64_t m = int64_t(blockIdx.x) * (kThreads / 64) + (threadIdx.x >> 6);
@@ -556,10 +559,12 @@ __global__ void __launch_bounds__(kThreads) ce_loss_kernel(LossArgs p) {
 #pragma unroll
   for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
   if (lane == 0) {
-    const float lse = ref + logf(sum);
+    const float log_sum = logf(sum);
     const float z = !keep ? 0.0f : p.scale * (p.z ? p.z[(t / kStep * p.zrows + m) * kStep + t % kStep] : p.chosen[m]);
-    p.loss[m] = keep ? lse - z : 0.0f;
-    if (p.lse) p.lse[m] = keep ? lse : 0.0f;
+    p.loss[m] = keep ? (ref - z) + log_sum : 0.0f;
+    if (p.lse) p.lse[m] = keep ? ref + log_sum : 0.0f;
+    // (a maximum of plus infinity: no other class has a part)
+    if (p.norm) p.norm[m] = top == INFINITY ? make_float2(top, 1.0f) : make_float2(ref, 1.0f / sum);
   }
 }
 
@@ -592,7 +597,8 @@ __global__ void __launch_bounds__(1024) ce_unit_kernel(UnitArgs p) {
 }
 
 struct DzArgs {
-  const float *z, *lse, *row_weight, *unit;
+  const float *z, *row_weight, *unit;
+  const float2* norm;  // as LossArgs
   const void* targets;
   uint16_t* dz;
   int64_t M, rows, blocks, plane, V;  // rows of a panel; blocks along the rows
@@ -603,7 +609,7 @@ struct DzArgs {
 
 constexpr int kDzRows = 128;  // rows of a block, of one panel
 
-// dz = (r / unit) (exp(s z - lse) - onehot); +0 in rows without a target, past V, and in the
+// dz = (r / unit) (softmax(s z) - onehot); +0 in rows without a target, past V, and in the
 // rows past M that the last stage of dW's sum reads.  In bf16 dz takes the place of the
 // logits (ld = 128: the first half of each row's 64 fp32): the eight lanes that write a
 // row are those that have read it, in one wave.  Bound by memory: 5.2 TB/s.
@@ -617,7 +623,7 @@ __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
     const int64_t t = m < p.M ? target_of(p.targets, p.wide, m) : -1;
     const bool keep = t >= 0 && t < p.V;
     const float c = keep && p.row_weight ? p.row_weight[m] / *p.unit : 1.0f;
-    const float lse = keep ? p.lse[m] : 0.0f;
+    const float2 norm = keep ? p.norm[m] : make_float2(0.0f, 0.0f);
     const int64_t row = panel * p.rows + m, at = row * p.ld + threadIdx.x % 8 * 8;
     const f32x4* z = reinterpret_cast<const f32x4*>(p.z + row * kStep + threadIdx.x % 8 * 8);
     const f32x4 za = __builtin_nontemporal_load(z), zb = __builtin_nontemporal_load(z + 1);
@@ -627,7 +633,7 @@ __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
       const float zk = k < 4 ? za[k & 3] : zb[k & 3];
       float g = 0.0f;
       if (keep && v0 + k < p.V) {
-        g = exp_diff(p.scale * zk, lse);
+        g = exp_diff(p.scale * zk, norm.x) * norm.y;
         if (v0 + k == t) g -= 1.0f;
         g *= c;
       }
@@ -642,7 +648,8 @@ __global__ void __launch_bounds__(kThreads) ce_dz_kernel(DzArgs p) {
 // Both gradients of few rows in fp32: the weights are read, and their gradient written, once.
 struct FewArgs {
   const void *h, *w, *targets;
-  const float *z, *lse, *row_weight;
+  const float *z, *row_weight;
+  const float2* norm;  // as LossArgs
   float *part, *gw;  // dH: [gridDim.y][M][D], without the scale
   int64_t ldh, ldw, ldg, M, V, D, zrows, panels, each;  // each: panels of a block
   float scale;
@@ -700,10 +707,11 @@ __global__ void __launch_bounds__(256, MF == 4 ? 1 : 2) ce_few_grad_kernel(FewAr
       f32x4 g{0.0f, 0.0f, 0.0f, 0.0f};
       if (t >= 0 && t < p.V) {
         const f32x4 z = *reinterpret_cast<const f32x4*>(p.z + (k * p.zrows + m) * kStep + tid % 16 * 4);
-        const float lse = p.lse[m], r = p.row_weight ? p.row_weight[m] : 1.0f;
+        const float2 norm = p.norm[m];
+        const float r = p.row_weight ? p.row_weight[m] : 1.0f;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (v + e < p.V) g[e] = r * (exp_diff(p.scale * z[e], lse) - (v + e == t ? 1.0f : 0.0f));
+          if (v + e < p.V) g[e] = r * (exp_diff(p.scale * z[e], norm.x) * norm.y - (v + e == t ? 1.0f : 0.0f));
       }
       *reinterpret_cast<f32x4*>(&dz[16 * f + tid / 16][tid % 16 * 4]) = g;
     }
@@ -792,7 +800,7 @@ struct Plan {
   int logits, dh_tile, dw_tile;  // rows of the products' tiles: 256 x 256, 192 x 256, 128 x 128
   int splits, dw_splits;         // of their sums: dH, dW
   int64_t few;                   // panels of a block of ce_few_grad_kernel
-  size_t h, w, stats, z, dz, chosen, lse, unit, dh, dw, total;
+  size_t h, w, stats, z, dz, chosen, norm, unit, dh, dw, total;
 };
 
 // Rows that can be read in chunks of 16 bytes, near enough for a descriptor.
@@ -880,11 +888,11 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   p.h = cv.take(size_t(p.planes == 3 ? 4 : 1) * size_t(p.piece) * size_t(p.Dp) * 2);
   p.w = cv.take(size_t(p.planes == 3 ? 4 : 1) * size_t(c->V) * size_t(p.Dp) * 2);
   p.stats = cv.take(size_t(p.piece) * size_t(ceil_div(c->V, 64)) * 8);
-  p.lse = cv.take(size_t(p.piece) * 4);
   p.chosen = cv.take(size_t(p.piece) * 4);
   p.unit = cv.take(4);
   p.splits = 1;
   if (train) {
+    p.norm = cv.take(size_t(p.piece) * 8);
     p.z = cv.take(size_t(p.rows) * size_t(p.Vp) * 4);
     p.dz = p.planes == 1 ? p.z : cv.take(size_t(p.planes) * size_t(p.rows) * size_t(p.Vp) * 2);
     const int64_t planes = p.planes == 3 ? 6 : 1;
@@ -1042,13 +1050,13 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     LossArgs s{};
     s.stats = l.stats; s.z = l.z; s.chosen = l.chosen; s.targets = tp;
     s.loss = loss + r0;
-    float* own_lse = reinterpret_cast<float*>(ws + p.lse);
-    s.lse = lse ? lse + r0 : train ? own_lse : nullptr;
+    s.lse = lse ? lse + r0 : nullptr;
+    s.norm = train ? reinterpret_cast<float2*>(ws + p.norm) : nullptr;
     s.M = M; s.zrows = p.rows; s.V = c->V; s.scale = c->logit_scale; s.tiles = l.g.tiles_n; s.wide = wide;
     ce_loss_kernel<<<dim3(unsigned(ceil_div(M, kThreads / 64))), dim3(kThreads), 0, stream>>>(s);
     if (!train) continue;
     if (few_back) {
-      FewArgs a{hidden, weight, targets, l.z, s.lse, row_weight, reinterpret_cast<float*>(ws + p.dh), static_cast<float*>(grad_weight),
+      FewArgs a{hidden, weight, targets, l.z, row_weight, s.norm, reinterpret_cast<float*>(ws + p.dh), static_cast<float*>(grad_weight),
                 c->ld_hidden, c->ld_weight, c->ld_grad_weight, M, c->V, c->D, p.rows, p.Vp / kStep, p.few, c->logit_scale, wide};
       const dim3 grid(unsigned(ceil_div(c->D, 256)), unsigned(ceil_div(a.panels, a.each))), b(256);
       if (M <= 16) ce_few_grad_kernel<1><<<grid, b, 0, stream>>>(a);
@@ -1062,7 +1070,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     }
 
     DzArgs z{};
-    z.z = l.z; z.lse = s.lse; z.row_weight = row_weight ? row_weight + r0 : nullptr;
+    z.z = l.z; z.norm = s.norm; z.row_weight = row_weight ? row_weight + r0 : nullptr;
     z.unit = unit; z.targets = tp;
     z.dz = reinterpret_cast<uint16_t*>(ws + p.dz);
     z.M = M; z.rows = p.rows; z.blocks = ceil_div(round_up(M, kStep), kDzRows);

@@ -357,3 +357,43 @@ def test_logits_at_plus_infinity(gpu_device, N, io):
         for k, v in dict(loss=loss, lse=lse).items():
             seq_ref.assert_within(v, *ref[k], k)
             seq_ref.assert_within(got[k], *ref[k], k + " of the training call")
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [20, 100])
+def test_large_logits_that_are_exact(gpu_device, N, io):
+    """Logits of 40000 that fp32 holds exactly, as it does their differences: loss and probabilities
+    are then off by the exponentials and the sums alone, not by the rounding of lse (2^-9 here)."""
+    V, D, U = 900, 16, seq_ref.U
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    dt = seq_ref.io_dtype(io)
+    n, v = torch.arange(N, device=gpu_device), torch.arange(V, device=gpu_device)
+    h = torch.zeros((N, D), device=gpu_device)
+    w = torch.zeros((V, D), device=gpu_device)
+    h[:, 0], h[:, 1], h[:, 2] = 1.0, 1.0, n % 4
+    w[:, 0], w[:, 1], w[:, 2] = 39936.0, (v * 37 % 256) / 16.0, v % 7 / 4.0
+    h, w, t = h.to(dt), w.to(dt), n * 11 % V
+    announce(f"ce exact logits {cfg}")
+    hd, wd = h.double(), w.double()
+    z = hd @ wd.t()
+    assert torch.equal(z, z.float().double())
+    top = z.max(dim=1).values[:, None]
+    log_sum = torch.exp(z - top).sum(dim=1).log()[:, None]
+    p = torch.exp(z - top - log_sum)
+    # an exponential's argument is rounded, and its result and the sum of V of them
+    e = (top - z + 8) * U
+    es = (p * e).sum(dim=1, keepdim=True) + (V / 64 + 80) * U
+    chosen = z.gather(1, t[:, None])
+    loss = top - chosen + log_sum
+    bound = es + 4 * U * (top - chosen + log_sum.abs()) + seq_ref.TINY
+    alone, _ = dendsn.linear_ce(cfg, h, w, t)
+    got = dendsn.linear_ce_train(cfg, h, w, t)
+    seq_ref.assert_within(alone, loss[:, 0], bound[:, 0], "loss")
+    seq_ref.assert_within(got["loss"], loss[:, 0], bound[:, 0], "loss of the training call")
+    onehot = torch.zeros_like(p).scatter_(1, t[:, None], 1.0)
+    dz = p - onehot
+    edz = p * (e + es) + 3 * U * (p + onehot) + (seq_ref.UB if io == "bf16" else 2 * U) * dz.abs()
+    gh, gw = dz @ wd, dz.t() @ hd
+    egh, egw = (edz + (V + 8) * U * dz.abs()) @ wd.abs(), (edz + (N + 8) * U * dz.abs()).t() @ hd.abs()
+    seq_ref.assert_within(got["grad_hidden"], gh, seq_ref.stored(gh, egh, io), "grad_hidden")
+    seq_ref.assert_within(got["grad_weight"], gw, seq_ref.stored(gw, egw, io), "grad_weight")
