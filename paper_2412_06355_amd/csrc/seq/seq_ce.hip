@@ -39,22 +39,30 @@ struct PackArgs {
   int64_t first;  // thread of the launch's first
 };
 
-// v as three bf16 that add up to it (two for the bits below the first eight): cut off,
-// not rounded, so that no part overflows.  Infinities and NaN are in the first alone, and
-// not in its finite copy.
+// The bf16 nearest to finite bits u, or the one below where that is infinite.
+__device__ __forceinline__ uint16_t nearest(uint32_t u) {
+  const uint32_t r = u + 0x7FFFu + (u >> 16 & 1);
+  return uint16_t(((r & 0x7F800000u) == 0x7F800000u ? u : r) >> 16);
+}
+
+// v as three bf16 that add up to it: each the nearest to what the ones before leave, so that
+// the second is at most 2^-8 and the third 2^-17 of v's power of two, with either sign (cut
+// off, they would be twice and four times that, all of v's sign, and so would what the
+// products of lower planes lose).  Infinities and NaN are in the first alone, and not in its
+// finite copy.
 __device__ __forceinline__ void split3(float v, uint16_t& a, uint16_t& finite, uint16_t& b, uint16_t& c) {
   const uint32_t u = __float_as_uint(v);
-  a = finite = uint16_t(u >> 16);
   if ((u & 0x7F800000u) == 0x7F800000u) {
+    a = uint16_t(u >> 16);
     if (u & 0x7FFFFFu) a |= 0x40;  // a NaN stays one without its low bits
     finite = b = c = 0;
     return;
   }
-  const float r1 = v - __uint_as_float(u & 0xFFFF0000u);
-  const uint32_t u1 = __float_as_uint(r1);
-  b = uint16_t(u1 >> 16);
-  const float r2 = r1 - __uint_as_float(u1 & 0xFFFF0000u);
-  c = uint16_t(__float_as_uint(r2) >> 16);
+  a = finite = nearest(u);
+  const float r1 = v - __uint_as_float(uint32_t(a) << 16);
+  b = nearest(__float_as_uint(r1));
+  const float r2 = r1 - __uint_as_float(uint32_t(b) << 16);
+  c = uint16_t(__float_as_uint(r2) >> 16);  // (at most eight bits are left)
 }
 
 __device__ __forceinline__ void store8(uint16_t* to, const uint16_t (&x)[8]) {

@@ -12,10 +12,10 @@
 // LDS linearly, so each lane fetches the chunk that belongs at its place.  Buffer descriptors bound every access: rows, columns and k past an
 // operand's end read as zero.
 //
-// fp32 operands come as three bf16 planes that add up to them exactly (8 bits of
-// the significand each); the six products of planes that matter at fp32 precision
-// (those of at most two steps down) run as one longer sum over k.  The products with a
-// lower plane take the first plane from a copy without infinities: a lower plane is
+// fp32 operands come as three bf16 planes that add up to them exactly, each the nearest
+// to what is left; the six products of planes of at most two steps down run as one longer
+// sum over k (the other three are at most 2^-24 of a product, with either sign).  The
+// products with a lower plane take the first plane from a copy without infinities: a lower plane is
 // often 0, and 0 times infinity is no part of the sum.
 #pragma once
 

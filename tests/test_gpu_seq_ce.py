@@ -397,3 +397,33 @@ def test_large_logits_that_are_exact(gpu_device, N, io):
     egh, egw = (edz + (V + 8) * U * dz.abs()) @ wd.abs(), (edz + (N + 8) * U * dz.abs()).t() @ hd.abs()
     seq_ref.assert_within(got["grad_hidden"], gh, seq_ref.stored(gh, egh, io), "grad_hidden")
     seq_ref.assert_within(got["grad_weight"], gw, seq_ref.stored(gw, egw, io), "grad_weight")
+
+
+@pytest.mark.parametrize("D", [1, 2, 3, 5, 66])
+def test_products_of_fp32_planes(gpu_device, D):
+    """Values whose significands leave the lower planes as much as they can, of one sign: a logit is
+    off by at most (D + 2) roundings of its products' sizes.  Two classes of opposite logits, far
+    apart: lse is the larger one.  The largest numbers do not overflow on the way."""
+    N, V, U = 3000, 2, seq_ref.U
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D)
+    gen = torch.Generator().manual_seed(D)
+    steps = torch.randint(0, 1 << 23, (N, D), generator=gen).double() * 2.0 ** -23
+    top = torch.randint(0, 128, (N, D), generator=gen).double() * 2.0 ** -7
+    low = torch.randint(0, 64, (N, D), generator=gen).double() * 2.0 ** -23
+    rows = torch.arange(N)[:, None] % 3
+    h = torch.where(rows == 0, steps, top + torch.where(rows == 1, 2.0 ** -7 - 2.0 ** -23, 2.0 ** -8) - low)
+    h = (1.0 + h).float()
+    h[0] = 1.0 + 2.0 ** -7 - 2.0 ** -23
+    t = torch.zeros(N, dtype=torch.int64, device=gpu_device)
+    for row in (0, 1, 2):
+        w = torch.stack([64.0 * h[row], -64.0 * h[row]])
+        announce(f"ce planes {cfg} row {row}")
+        _, lse = dendsn.linear_ce(cfg, h.to(gpu_device), w.to(gpu_device), t)
+        z = torch.matmul(h.double(), w[0].double())
+        assert float(z.min()) > 60.0
+        seq_ref.assert_within(lse, z, (D + 2) * U * z, "lse")
+    big = torch.full((N, D), torch.finfo(torch.float32).max)
+    w = torch.stack([torch.full((D,), 2.0 ** -20), torch.full((D,), -2.0 ** -20)])
+    _, lse = dendsn.linear_ce(cfg, big.to(gpu_device), w.to(gpu_device), t)
+    z = torch.matmul(big.double(), w[0].double())
+    seq_ref.assert_within(lse, z, (D + 2) * U * z, "lse of the largest numbers")
