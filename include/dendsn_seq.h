@@ -156,8 +156,10 @@ typedef struct dendsn_ce_cfg {
     float logit_scale;  /* finite                                              */
 } dendsn_ce_cfg;
 
-/* Scratch of the loss alone (train = 0) or of the loss with gradients (train != 0);
- * it does not grow with N beyond a bounded piece of rows. */
+/* Scratch of the loss alone (train = 0) or of the loss with gradients (train != 0).
+ * Rows go through in pieces: at most 4 GiB of logits (in fp32 with their gradient) and
+ * 4 GiB of copies of hidden are held at a time, or 256 rows' where those are more; the
+ * rest does not grow with N but for some bytes a tile of logits. */
 dendsn_status dendsn_ce_workspace_bytes(const dendsn_ce_cfg* cfg, int32_t train, size_t* bytes);
 
 /*

@@ -21,7 +21,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int64_t kMostThreads = int64_t(1) << 31;  // of a launch (it has fewer than 2^32)
-constexpr int64_t kPieceBytes = int64_t(4) << 30;  // of the logits and their gradient of a piece
+constexpr int64_t kPieceBytes = int64_t(4) << 30;  // of a piece's logits with their gradient, and of its packed rows
 
 __device__ __forceinline__ int64_t target_of(const void* t, int wide, int64_t i) {
   return wide ? static_cast<const int64_t*>(t)[i] : int64_t(static_cast<const int32_t*>(t)[i]);
@@ -881,7 +881,9 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   p.Dp = round_up(c->D, kStep);
   p.Vp = round_up(c->V, kStep);
   // a row's logits, with their gradient in their place (fp32: beside them, in planes)
-  const int64_t per_row = train ? p.Vp * (p.planes == 1 ? 4 : 10) : ceil_div(c->V, 64) * 8;
+  const int64_t logits_row = train ? p.Vp * (p.planes == 1 ? 4 : 10) : ceil_div(c->V, 64) * 8;
+  const int64_t packed_row = p.Dp * (p.planes == 1 ? 2 : 8);
+  const int64_t per_row = logits_row > packed_row ? logits_row : packed_row;
   int64_t most = kPieceBytes / per_row / kBig * kBig;
   if (most < kBig) most = kBig;
   if (most > kMaxPanelRows) most = kMaxPanelRows;

@@ -383,3 +383,19 @@ def test_tensors_of_another_gpu_are_refused(monkeypatch, module):
         m._stream(torch.device("cuda", 1))
     with pytest.raises(ValueError, match="GPU memory"):
         m._stream(torch.device("cpu"))
+
+
+@pytest.mark.parametrize("train", [0, 1])
+@pytest.mark.parametrize("V,D,io", [(32000, 4096, 0), (1000, 4096, 1), (1000, 4096, 0), (131072, 64, 1), (1, 1 << 16, 1)])
+def test_ce_scratch_is_bounded_in_every_form(lib, train, V, D, io):
+    """Whatever dominates a row (its logits, its statistics, its packed copy), the scratch of 2^20
+    rows is that of 2^22, and beside a copy of the weights below 9 GiB."""
+    size = []
+    for N in (1 << 20, 1 << 22):
+        out = ctypes.c_size_t(0)
+        assert lib.dendsn_ce_workspace_bytes(ref(ce_cfg(N=N, V=V, D=D, ld_hidden=D, ld_weight=D, ld_grad_hidden=D,
+                                                        ld_grad_weight=D, io=io)), train, ctypes.byref(out)) == OK
+        size.append(out.value)
+    padded = -(-D // 64) * 64
+    weights = V * padded * (2 if io else 8) + (V * padded * 4 if train else 0)   # laid out; their gradient's sum
+    assert max(size) - weights < 9 << 30 and size[1] <= 1.1 * size[0]
