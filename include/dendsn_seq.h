@@ -162,6 +162,12 @@ typedef struct dendsn_ce_cfg {
  * rest does not grow with N but for some bytes a tile of logits. */
 dendsn_status dendsn_ce_workspace_bytes(const dendsn_ce_cfg* cfg, int32_t train, size_t* bytes);
 
+/* The same for operands that lie at these addresses (only their alignment counts):
+ * without the copies of operands that the kernels read in place, which the query
+ * above has room for.  The calls below ask for this much. */
+dendsn_status dendsn_ce_workspace_bytes_at(const dendsn_ce_cfg* cfg, int32_t train, const void* hidden,
+                                           const void* weight, size_t* bytes);
+
 /*
  * loss[n] = lse[n] - z[n, targets[n]], lse[n] = log sum_v exp(z[n, v]).  A row
  * whose target is outside [0, V) is ignored: its loss and lse are +0, and

@@ -31,6 +31,7 @@ from .sequence import (  # noqa: F401
     dendsn_ce_forward,
     dendsn_ce_train,
     dendsn_ce_workspace_bytes,
+    dendsn_ce_workspace_bytes_at,
     dendsn_embed_backward,
     dendsn_embed_forward,
     dendsn_embed_workspace_bytes,

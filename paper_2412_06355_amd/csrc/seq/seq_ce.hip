@@ -817,9 +817,56 @@ bool rows16(const dendsn_ce_cfg* c, const void* p, int64_t ld) {
   return aligned(p, 16) && c->D % m == 0 && ld % m == 0 && ld <= kMaxLd;
 }
 
-// Operands that the DMA can take as they lie.
-bool direct(const dendsn_ce_cfg* c, const void* p, int64_t ld) {
-  return c->io == DENDSN_IO_BF16 && rows16(c, p, ld);
+// The kernel for few rows, if one is made for these sizes: MF times sixteen rows, U units
+// of 64 k a wave, as far as the registers reach.  2048 features, 50001 classes in bf16: 8
+// rows 33 us, 32 rows 35 us; the tiles, which split no sum over k, 53 and 41 us (and fp32
+// would be laid out in planes first).  With the logits kept for training, 64 rows of 32000
+// classes and 1024 features: 19 us against 22; 32 rows of 50000 in fp32: 70 us against 137;
+// 32 rows of 5000 classes and 1500 features in fp32: 31 against 107, and 20 of layout.
+// launch = false: only says whether.
+template <typename IO>
+bool launch_score(const ScoreArgs& a, bool launch, unsigned grid, hipStream_t stream) {
+  constexpr bool BF = sizeof(IO) == 2;
+  const int64_t mf = ceil_div(a.M, 16), u = ceil_div(a.K, kStep * kScoreWaves);
+  const dim3 g(grid), b(kScoreWaves * 64);
+#define DENDSN_SCORE(MF, U)                                         \
+  if (mf <= MF && u <= U) {                                         \
+    if (launch) ce_score_kernel<IO, MF, U><<<g, b, 0, stream>>>(a); \
+    return true;                                                    \
+  }
+  DENDSN_SCORE(1, 1) DENDSN_SCORE(1, 2) DENDSN_SCORE(1, 4)
+  DENDSN_SCORE(2, 1) DENDSN_SCORE(2, 2)
+  DENDSN_SCORE(4, 1)
+  if constexpr (BF) {
+    DENDSN_SCORE(1, 8) DENDSN_SCORE(2, 4) DENDSN_SCORE(4, 2)
+  } else {
+    DENDSN_SCORE(2, 3) DENDSN_SCORE(4, 2)
+  }
+#undef DENDSN_SCORE
+  return false;
+}
+
+// Which kernels read the operands, by where they lie.
+struct Route {
+  bool streamed;        // logits of few rows, from one stream over the weights
+  bool few_back;        // and their gradients, from another
+  bool pack_h, pack_w;  // operands are laid out for the products (bf16 as they lie: by the DMA)
+};
+
+Route route_of(const dendsn_ce_cfg* c, bool train, const void* hidden, const void* weight) {
+  const bool bf = c->io == DENDSN_IO_BF16, h = rows16(c, hidden, c->ld_hidden), w = rows16(c, weight, c->ld_weight);
+  Route r{};
+  if (c->N <= 64 && h && w) {
+    ScoreArgs a{};
+    a.M = c->N;
+    a.K = c->D;
+    r.streamed = bf ? launch_score<bf16_t>(a, false, 1, nullptr) : launch_score<float>(a, false, 1, nullptr);
+    r.few_back = train && !bf;
+  }
+  const bool products = !r.streamed || (train && !r.few_back);
+  r.pack_w = products && !(bf && w);
+  r.pack_h = products && !(bf && h && !train);  // (training clears the rows without a target)
+  return r;
 }
 
 // The tile of a product of M x N.  A CU works through a 256 tile at 0.6 of the time of
@@ -875,7 +922,8 @@ Split split_of(int64_t M, int64_t N, int64_t steps, bool whole) {
   return best;
 }
 
-Plan make_plan(const dendsn_ce_cfg* c, bool train) {
+// Of a route, or of all that the operands' places may lead to.
+Plan make_plan(const dendsn_ce_cfg* c, bool train, const Route* r) {
   Plan p{};
   p.planes = c->io == DENDSN_IO_BF16 ? 1 : 3;
   p.Dp = round_up(c->D, kStep);
@@ -895,8 +943,8 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   p.rows = round_up(p.piece, kBig);
   if (p.logits == 192) p.rows = round_up(p.piece, 192) > p.rows ? round_up(p.piece, 192) : p.rows;
   Carve cv;
-  p.h = cv.take(size_t(p.planes == 3 ? 4 : 1) * size_t(p.piece) * size_t(p.Dp) * 2);
-  p.w = cv.take(size_t(p.planes == 3 ? 4 : 1) * size_t(c->V) * size_t(p.Dp) * 2);
+  if (!r || r->pack_h) p.h = cv.take(size_t(p.planes == 3 ? 4 : 1) * size_t(p.piece) * size_t(p.Dp) * 2);
+  if (!r || r->pack_w) p.w = cv.take(size_t(p.planes == 3 ? 4 : 1) * size_t(c->V) * size_t(p.Dp) * 2);
   p.stats = cv.take(size_t(p.piece) * size_t(ceil_div(c->V, 64)) * 8);
   p.chosen = cv.take(size_t(p.piece) * 4);
   p.unit = cv.take(4);
@@ -904,21 +952,22 @@ Plan make_plan(const dendsn_ce_cfg* c, bool train) {
   if (train) {
     p.norm = cv.take(size_t(p.piece) * 8);
     p.z = cv.take(size_t(p.rows) * size_t(p.Vp) * 4);
-    p.dz = p.planes == 1 ? p.z : cv.take(size_t(p.planes) * size_t(p.rows) * size_t(p.Vp) * 2);
+    p.dz = p.z;
+    if (p.planes == 3 && !(r && r->few_back)) p.dz = cv.take(size_t(p.planes) * size_t(p.rows) * size_t(p.Vp) * 2);
     const int64_t planes = p.planes == 3 ? 6 : 1;
     const Split dh = split_of(p.piece, c->D, ceil_div(c->V, kStep) * planes, false);
     const Split dw = split_of(c->V, c->D, ceil_div(p.piece, kStep) * planes, p.pieces > 1);
     p.dh_tile = dh.tile, p.splits = dh.parts;
     p.dw_tile = dw.tile, p.dw_splits = dw.parts;
-    int64_t dh_parts = p.splits > 1 ? p.splits : 0;
-    if (p.planes == 3 && c->N <= 64) {  // two blocks a CU
+    int64_t dh_parts = p.splits > 1 && !(r && r->few_back) ? p.splits : 0;
+    if (r ? r->few_back : p.planes == 3 && c->N <= 64) {  // two blocks a CU
       const int64_t panels = p.Vp / kStep, columns = ceil_div(c->D, 256);
       const int64_t parts = columns < 512 ? 512 / columns : 1;
       p.few = ceil_div(panels, parts);
       if (ceil_div(panels, p.few) > dh_parts) dh_parts = ceil_div(panels, p.few);
     }
     p.dh = cv.take(size_t(dh_parts) * size_t(p.piece) * size_t(c->D) * 4);
-    const int dw_parts = p.dw_splits > 1 ? p.dw_splits : p.pieces > 1 ? 1 : 0;
+    const int dw_parts = r && r->few_back ? 0 : p.dw_splits > 1 ? p.dw_splits : p.pieces > 1 ? 1 : 0;
     p.dw = cv.take(size_t(dw_parts) * size_t(c->V) * size_t(c->D) * 4);
   }
   p.total = cv.at;
@@ -945,34 +994,6 @@ void pack(PackArgs a, bool bf, hipStream_t stream) {
   }
 }
 
-// The kernel for few rows, if one is made for these sizes: MF times sixteen rows, U units
-// of 64 k a wave, as far as the registers reach.  2048 features, 50001 classes in bf16: 8
-// rows 33 us, 32 rows 35 us; the tiles, which split no sum over k, 53 and 41 us (and fp32
-// would be laid out in planes first).  With the logits kept for training, 64 rows of 32000
-// classes and 1024 features: 19 us against 22; 32 rows of 50000 in fp32: 70 us against 137;
-// 32 rows of 5000 classes and 1500 features in fp32: 31 against 107, and 20 of layout.
-template <typename IO>
-bool launch_score(const ScoreArgs& a, unsigned grid, hipStream_t stream) {
-  constexpr bool BF = sizeof(IO) == 2;
-  const int64_t mf = ceil_div(a.M, 16), u = ceil_div(a.K, kStep * kScoreWaves);
-  const dim3 g(grid), b(kScoreWaves * 64);
-#define DENDSN_SCORE(MF, U)                                 \
-  if (mf <= MF && u <= U) {                                 \
-    ce_score_kernel<IO, MF, U><<<g, b, 0, stream>>>(a);     \
-    return true;                                            \
-  }
-  DENDSN_SCORE(1, 1) DENDSN_SCORE(1, 2) DENDSN_SCORE(1, 4)
-  DENDSN_SCORE(2, 1) DENDSN_SCORE(2, 2)
-  DENDSN_SCORE(4, 1)
-  if constexpr (BF) {
-    DENDSN_SCORE(1, 8) DENDSN_SCORE(2, 4) DENDSN_SCORE(4, 2)
-  } else {
-    DENDSN_SCORE(2, 3) DENDSN_SCORE(4, 2)
-  }
-#undef DENDSN_SCORE
-  return false;
-}
-
 // As many blocks as the 256 CUs hold at a time, a multiple of the eight XCDs: a block's
 // tiles then stay on its XCD.
 unsigned grid_of(const GemmArgs& g, int tile, bool all) {
@@ -996,36 +1017,29 @@ void join_splits(const GradArgs& g, int splits, hipStream_t stream) {
 
 dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const void* weight, const void* targets,
                   const float* row_weight, float* loss, float* lse, void* grad_hidden, void* grad_weight,
-                  char* ws, const Plan& p, hipStream_t stream) {
+                  char* ws, const Route& route, const Plan& p, hipStream_t stream) {
   const size_t esz = c->io == DENDSN_IO_BF16 ? 2 : 4;
   const int wide = c->index == DENDSN_INDEX_I64;
   const size_t isz = wide ? 8 : 4;
   const bool bf = c->io == DENDSN_IO_BF16;
   // Few rows: at most as many blocks as there is room for statistics, a CU each.
   const unsigned blocks = unsigned(ceil_div(c->V, kStep) < 256 ? ceil_div(c->V, kStep) : 256);
-  auto few = [&](const void* h, const void* t, int64_t M) {
-    if (!rows16(c, h, c->ld_hidden) || !rows16(c, weight, c->ld_weight)) return false;
-    const ScoreArgs a{h, weight, t, reinterpret_cast<float2*>(ws + p.stats),
+  if (route.streamed) {
+    const ScoreArgs a{hidden, weight, targets, reinterpret_cast<float2*>(ws + p.stats),
                       train ? nullptr : reinterpret_cast<float*>(ws + p.chosen),
                       train ? reinterpret_cast<float*>(ws + p.z) : nullptr,
-                      c->ld_hidden, c->ld_weight, M, c->V, c->D, p.rows, c->logit_scale, wide};
-    return bf ? launch_score<bf16_t>(a, blocks, stream) : launch_score<float>(a, blocks, stream);
-  };
-  const bool streamed = c->N <= 64 && few(hidden, targets, c->N);
-  const bool few_back = train && p.few && rows16(c, hidden, c->ld_hidden) && rows16(c, weight, c->ld_weight);
-  const bool no_tiles = streamed && (!train || few_back);
-  Operand w{};
-  if (no_tiles) {
-    // (no product reads it)
-  } else if (direct(c, weight, c->ld_weight)) {
-    w = Operand{static_cast<const uint16_t*>(weight), c->ld_weight, 0, 0, c->V, c->D};
-  } else {
+                      c->ld_hidden, c->ld_weight, c->N, c->V, c->D, p.rows, c->logit_scale, wide};
+    if (bf) launch_score<bf16_t>(a, true, blocks, stream);
+    else launch_score<float>(a, true, blocks, stream);
+  }
+  Operand w{static_cast<const uint16_t*>(weight), c->ld_weight, 0, 0, c->V, c->D};  // (bf16, where a product reads it)
+  if (route.pack_w) {
     PackArgs a{weight, reinterpret_cast<uint16_t*>(ws + p.w), nullptr, c->V, c->D, c->ld_weight, p.Dp, c->V * p.Dp, c->V, wide, p.planes};
     pack(a, bf, stream);
     w = Operand{a.dst, p.Dp, a.plane, kFinite * a.plane, c->V, p.Dp};
   }
   float* unit = nullptr;
-  if (train && row_weight && !few_back) {
+  if (train && row_weight && !route.few_back) {
     unit = reinterpret_cast<float*>(ws + p.unit);
     ce_unit_kernel<<<dim3(1), dim3(1024), 0, stream>>>(UnitArgs{row_weight, targets, unit, c->N, c->V, wide});
   }
@@ -1033,11 +1047,8 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     const int64_t M = c->N - r0 < p.piece ? c->N - r0 : p.piece;
     const void* hp = static_cast<const char*>(hidden) + size_t(r0) * size_t(c->ld_hidden) * esz;
     const void* tp = static_cast<const char*>(targets) + size_t(r0) * isz;
-    Operand h{};
-    if (no_tiles) {
-    } else if (!train && direct(c, hp, c->ld_hidden)) {
-      h = Operand{static_cast<const uint16_t*>(hp), c->ld_hidden, 0, 0, M, c->D};
-    } else {
+    Operand h{static_cast<const uint16_t*>(hp), c->ld_hidden, 0, 0, M, c->D};  // (as w)
+    if (route.pack_h) {
       PackArgs a{hp, reinterpret_cast<uint16_t*>(ws + p.h), tp, M, c->D, c->ld_hidden, p.Dp, M * p.Dp, c->V, wide, p.planes};
       pack(a, bf, stream);
       h = Operand{a.dst, p.Dp, a.plane, kFinite * a.plane, M, p.Dp};
@@ -1052,7 +1063,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     l.chosen = train ? nullptr : reinterpret_cast<float*>(ws + p.chosen);
     l.targets = tp; l.zrows = p.rows; l.zcols = p.Vp; l.wide = wide;
     const dim3 lg(grid_of(l.g, p.logits, train));
-    if (streamed) l.g.tiles_n = int(blocks);
+    if (route.streamed) l.g.tiles_n = int(blocks);
     else if (p.logits == 256) ce_logits_kernel<256, 256, 2, 4><<<lg, dim3(512), 0, stream>>>(l);
     else if (p.logits == 192) ce_logits_kernel<192, 256, 2, 4><<<lg, dim3(512), 0, stream>>>(l);
     else ce_logits_kernel<128, 128, 2, 2><<<lg, dim3(256), 0, stream>>>(l);
@@ -1065,7 +1076,7 @@ dendsn_status run(const dendsn_ce_cfg* c, bool train, const void* hidden, const 
     s.M = M; s.zrows = p.rows; s.V = c->V; s.scale = c->logit_scale; s.tiles = l.g.tiles_n; s.wide = wide;
     ce_loss_kernel<<<dim3(unsigned(ceil_div(M, kThreads / 64))), dim3(kThreads), 0, stream>>>(s);
     if (!train) continue;
-    if (few_back) {
+    if (route.few_back) {
       FewArgs a{hidden, weight, targets, l.z, row_weight, s.norm, reinterpret_cast<float*>(ws + p.dh), static_cast<float*>(grad_weight),
                 c->ld_hidden, c->ld_weight, c->ld_grad_weight, M, c->V, c->D, p.rows, p.Vp / kStep, p.few, c->logit_scale, wide};
       const dim3 grid(unsigned(ceil_div(c->D, 256)), unsigned(ceil_div(a.panels, a.each))), b(256);
@@ -1140,7 +1151,18 @@ dendsn_status dendsn_ce_workspace_bytes(const dendsn_ce_cfg* cfg, int32_t train,
   const dendsn_status st = check_cfg(cfg);
   if (st != DENDSN_OK) return st;
   if (!bytes) return fail(DENDSN_E_INVALID, "bytes is NULL");
-  *bytes = make_plan(cfg, train != 0).total;
+  *bytes = make_plan(cfg, train != 0, nullptr).total;
+  return DENDSN_OK;
+}
+
+dendsn_status dendsn_ce_workspace_bytes_at(const dendsn_ce_cfg* cfg, int32_t train, const void* hidden,
+                                           const void* weight, size_t* bytes) {
+  clear_error();
+  const dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  if (!bytes) return fail(DENDSN_E_INVALID, "bytes is NULL");
+  const Route r = route_of(cfg, train != 0, hidden, weight);
+  *bytes = make_plan(cfg, train != 0, &r).total;
   return DENDSN_OK;
 }
 
@@ -1151,11 +1173,12 @@ dendsn_status dendsn_ce_forward(const dendsn_ce_cfg* cfg, const void* hidden, co
   dendsn_status st = check_cfg(cfg);
   if (st == DENDSN_OK) st = check_args(cfg, hidden, weight, targets, loss, lse);
   if (st != DENDSN_OK) return st;
-  const Plan p = make_plan(cfg, false);
-  st = check_workspace(workspace, workspace_bytes, p.total, "dendsn_ce_workspace_bytes");
+  const Route r = route_of(cfg, false, hidden, weight);
+  const Plan p = make_plan(cfg, false, &r);
+  st = check_workspace(workspace, workspace_bytes, p.total, "dendsn_ce_workspace_bytes_at");
   if (st != DENDSN_OK || cfg->N == 0) return st;
   return run(cfg, false, hidden, weight, targets, nullptr, loss, lse, nullptr, nullptr, static_cast<char*>(workspace),
-             p, stream);
+             r, p, stream);
 }
 
 dendsn_status dendsn_ce_train(const dendsn_ce_cfg* cfg, const void* hidden, const void* weight,
@@ -1170,8 +1193,9 @@ dendsn_status dendsn_ce_train(const dendsn_ce_cfg* cfg, const void* hidden, cons
   if ((cfg->N > 0 && !grad_hidden) || !grad_weight) return fail(DENDSN_E_INVALID, "grad_hidden or grad_weight is NULL");
   if (!aligned(grad_hidden, esz) || !aligned(grad_weight, esz) || !aligned(row_weight, 4))
     return fail(DENDSN_E_INVALID, "grad_hidden, grad_weight or row_weight misaligned");
-  const Plan p = make_plan(cfg, true);
-  st = check_workspace(workspace, workspace_bytes, p.total, "dendsn_ce_workspace_bytes");
+  const Route r = route_of(cfg, true, hidden, weight);
+  const Plan p = make_plan(cfg, true, &r);
+  st = check_workspace(workspace, workspace_bytes, p.total, "dendsn_ce_workspace_bytes_at");
   if (st != DENDSN_OK) return st;
   if (cfg->N == 0) {
     const int64_t blocks = ceil_div(cfg->V * cfg->D, kThreads);
@@ -1179,7 +1203,7 @@ dendsn_status dendsn_ce_train(const dendsn_ce_cfg* cfg, const void* hidden, cons
     return launched("linear cross entropy");
   }
   return run(cfg, true, hidden, weight, targets, row_weight, loss, lse, grad_hidden, grad_weight,
-             static_cast<char*>(workspace), p, stream);
+             static_cast<char*>(workspace), r, p, stream);
 }
 
 }  // extern "C"

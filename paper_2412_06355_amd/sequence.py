@@ -53,6 +53,7 @@ _SIGS = {
     "dendsn_scan_backward": (ctypes.c_int, [ctypes.POINTER(dendsn_scan_cfg)] + [_P] * 10 + [_Z, _P]),
     "dendsn_scan_step": (ctypes.c_int, [ctypes.POINTER(dendsn_scan_cfg), _P, _P, ctypes.c_int64, _P, _P, _P, _P]),
     "dendsn_ce_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(dendsn_ce_cfg), ctypes.c_int32, _SIZE]),
+    "dendsn_ce_workspace_bytes_at": (ctypes.c_int, [ctypes.POINTER(dendsn_ce_cfg), ctypes.c_int32, _P, _P, _SIZE]),
     "dendsn_ce_forward": (ctypes.c_int, [ctypes.POINTER(dendsn_ce_cfg)] + [_P] * 6 + [_Z, _P]),
     "dendsn_ce_train": (ctypes.c_int, [ctypes.POINTER(dendsn_ce_cfg)] + [_P] * 9 + [_Z, _P]),
     "dendsn_seq_last_error": (ctypes.c_char_p, []),
@@ -406,6 +407,10 @@ def dendsn_ce_workspace_bytes(cfg: LinearCEConfig, train: bool) -> int:
     return _bytes(seq_lib().dendsn_ce_workspace_bytes, ctypes.byref(cfg.to_c()), int(train))
 
 
+def dendsn_ce_workspace_bytes_at(cfg: LinearCEConfig, train: bool, hidden, weight) -> int:
+    return _bytes(seq_lib().dendsn_ce_workspace_bytes_at, ctypes.byref(cfg.to_c()), int(train), _ptr(hidden), _ptr(weight))
+
+
 def dendsn_ce_forward(cfg: LinearCEConfig, hidden, weight, targets, loss, lse, workspace, stream=None):
     st = stream if stream is not None else _stream(weight.device)
     _check(seq_lib().dendsn_ce_forward(ctypes.byref(cfg.to_c()), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(loss),
@@ -445,7 +450,7 @@ def linear_ce(cfg: LinearCEConfig, hidden, weight, targets, *, workspace=None):
     st = _stream(dev)
     loss, lse = (torch.empty((cfg.N,), dtype=torch.float32, device=dev) for _ in range(2))
     fn = seq_lib()
-    ws = _workspace(_bytes(fn.dendsn_ce_workspace_bytes, ctypes.byref(c), 0), workspace, dev)
+    ws = _workspace(_bytes(fn.dendsn_ce_workspace_bytes_at, ctypes.byref(c), 0, _ptr(hidden), _ptr(weight)), workspace, dev)
     _check(fn.dendsn_ce_forward(ctypes.byref(c), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(loss), _ptr(lse),
                                 _ptr(ws), _nbytes(ws), st))
     return loss, lse
@@ -464,7 +469,7 @@ def linear_ce_train(cfg: LinearCEConfig, hidden, weight, targets, row_weight=Non
                grad_hidden=torch.empty((cfg.N, cfg.D), dtype=dt, device=dev),
                grad_weight=torch.empty((cfg.V, cfg.D), dtype=dt, device=dev))
     fn = seq_lib()
-    ws = _workspace(_bytes(fn.dendsn_ce_workspace_bytes, ctypes.byref(c), 1), workspace, dev)
+    ws = _workspace(_bytes(fn.dendsn_ce_workspace_bytes_at, ctypes.byref(c), 1, _ptr(hidden), _ptr(weight)), workspace, dev)
     _check(fn.dendsn_ce_train(ctypes.byref(c), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(row_weight),
                               _ptr(out["loss"]), _ptr(out["lse"]), _ptr(out["grad_hidden"]), _ptr(out["grad_weight"]),
                               _ptr(ws), _nbytes(ws), st))

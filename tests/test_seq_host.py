@@ -399,3 +399,35 @@ def test_ce_scratch_is_bounded_in_every_form(lib, train, V, D, io):
     padded = -(-D // 64) * 64
     weights = V * padded * (2 if io else 8) + (V * padded * 4 if train else 0)   # laid out; their gradient's sum
     assert max(size) - weights < 9 << 30 and size[1] <= 1.1 * size[0]
+
+
+@pytest.mark.parametrize("io", [0, 1])
+@pytest.mark.parametrize("N,V,D", [(8, 50001, 2048), (64, 32000, 1024), (100, 32000, 1024), (4096, 32000, 1024), (8, 5003, 515)])
+def test_ce_scratch_by_place(lib, N, V, D, io):
+    """Operands that are read where they lie take no room for copies: little beside the logits of few
+    rows, and nowhere more than for any alignment.  The calls ask for just that."""
+    c = ce_cfg(N=N, V=V, D=D, ld_hidden=D, ld_weight=D, ld_grad_hidden=D, ld_grad_weight=D, io=io)
+    weights = V * D * (2 if io else 4)
+    for train in (0, 1):
+        def at(h, w):
+            out = ctypes.c_size_t(0)
+            assert lib.dendsn_ce_workspace_bytes_at(ref(c), train, p(h), p(w), ctypes.byref(out)) == OK
+            return out.value
+
+        most = ctypes.c_size_t(0)
+        assert lib.dendsn_ce_workspace_bytes(ref(c), train, ctypes.byref(most)) == OK
+        call = ce_train if train else ce_fwd
+        for h, w in ((A, 2 * A), (A, 2 * A + 4), (A + 4, 2 * A)):
+            need = at(h, w)
+            assert 0 < need <= most.value
+            assert call(lib, c, h=h, w=w, nbytes=need - 1) == WORKSPACE
+        if D == 515:
+            assert at(A, 2 * A) > weights      # odd rows are laid out wherever they lie
+        elif N <= 64 and not train:
+            assert at(A, 2 * A) < 1 << 20 < weights < at(A, 2 * A + 4)
+        elif io:
+            assert at(A, 2 * A) <= at(A, 2 * A + 4) - weights
+    assert lib.dendsn_ce_workspace_bytes_at(ref(c), 0, p(A), p(A), None) == INVALID
+    out = ctypes.c_size_t(77)
+    assert lib.dendsn_ce_workspace_bytes_at(ref(ce_cfg(V=0)), 1, p(A), p(A), ctypes.byref(out)) == INVALID
+    assert lib.dendsn_ce_workspace_bytes_at(None, 1, p(A), p(A), ctypes.byref(out)) == INVALID and out.value == 77
