@@ -112,7 +112,12 @@ def _bytes(fn, *args) -> int:
 
 
 def _nbytes(t):
-    return 0 if t is None else t.nbytes
+    """The bytes of a workspace: as many as its elements' only where they lie one after another."""
+    if t is None:
+        return 0
+    if not t.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return t.nbytes
 
 
 def _io_dtype(io):

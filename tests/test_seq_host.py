@@ -431,3 +431,16 @@ def test_ce_scratch_by_place(lib, N, V, D, io):
     out = ctypes.c_size_t(77)
     assert lib.dendsn_ce_workspace_bytes_at(ref(ce_cfg(V=0)), 1, p(A), p(A), ctypes.byref(out)) == INVALID
     assert lib.dendsn_ce_workspace_bytes_at(None, 1, p(A), p(A), ctypes.byref(out)) == INVALID and out.value == 77
+
+
+def test_workspaces_are_contiguous():
+    """The bytes of a broadcast or strided tensor are not there: the library would write past it."""
+    import torch
+
+    from paper_2412_06355_amd import sequence
+
+    for ws in (torch.zeros(16, dtype=torch.uint8).expand(1 << 20, 16), torch.zeros(64, dtype=torch.uint8)[::2],
+               torch.zeros(4, 8).t()):
+        with pytest.raises(ValueError, match="contiguous"):
+            sequence._nbytes(ws)
+    assert sequence._nbytes(torch.zeros(4, 8)) == 128 and sequence._nbytes(None) == 0
