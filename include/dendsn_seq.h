@@ -101,7 +101,9 @@ dendsn_status dendsn_scan_ckpt_bytes(const dendsn_scan_cfg* cfg, size_t* bytes);
 dendsn_status dendsn_scan_workspace_bytes(const dendsn_scan_cfg* cfg, int32_t backward, size_t* bytes);
 
 /*
- * Forward over all steps.
+ * Forward over all steps.  Decays that are given (DENDSN_GATE_DECAY) may have any value,
+ * beyond 1 too: products of many steps' carry exponents of their own.  After an input that
+ * is not finite its channel's states are not finite either, infinite or NaN.
  *   x, g     [T,batch,D] io    required
  *   h0       [batch,D] fp32    NULL means 0
  *   lengths  [batch] int32     NULL: every sequence has T steps.  Steps at and past

@@ -32,7 +32,7 @@ struct ScanArgs {
   const int32_t* lengths;
   void *h, *gx, *gg;
   float *h_last, *ckpt, *gh0;
-  float2* runs;  // [S][batch][D] composed runs of the split
+  void* runs;  // [S][batch][D] composed runs of the split (Run)
   int64_t D, x_t, x_b, g_t, g_b, h_t, h_b, gh_t, gh_b, gx_t, gx_b, gg_t, gg_b;
   int32_t T, batch, ntiles, per;  // per: tiles of a block of the split
 };
@@ -57,6 +57,49 @@ __device__ __forceinline__ void decay(float g, float& a, float& na) {
     na = 1.0f - g;
   }
 }
+
+// A run of steps: it takes a state s to A s + b.  Sigmoid decays are at most 1, and their
+// product is a number.  Decays that are given have any size: 512 steps of 1.25, or two of
+// 1e20, would make A infinite, and A times a state of 0 NaN, where the recurrence has 0.  Their
+// product carries its exponent beside a mantissa (16384 steps of 2000 channels in bf16, forward
+// and backward: 191 us, without 184; with exponents only in tiles that need them 191 too).
+template <bool SIG>
+struct Run {
+  float a, b;
+  __device__ __forceinline__ void one() { a = 1.0f; }
+  __device__ __forceinline__ void times(float f) { a *= f; }
+  __device__ __forceinline__ void settle() {}
+  __device__ __forceinline__ void times(const Run& r) { a *= r.a; }
+  __device__ __forceinline__ float plus(float s, float add) const { return fmaf(a, s, add); }  // A s + add
+  __device__ __forceinline__ float of(float s) const { return plus(s, b); }
+};
+
+template <>
+struct Run<false> {
+  float a, b;
+  int32_t e;  // A = a 2^e
+  __device__ __forceinline__ void one() { a = 1.0f, e = 0; }
+  // (a halves with each at most: settle() after some eights of them)
+  __device__ __forceinline__ void times(float f) {
+    a *= __builtin_amdgcn_frexp_mantf(f);
+    e += __builtin_amdgcn_frexp_expf(f);
+  }
+  // (an exponent past 2^28 is no state's any more, and 32 bits would overflow)
+  __device__ __forceinline__ void settle() {
+    constexpr int32_t kMost = 1 << 28;
+    e = max(-kMost, min(kMost, e + __builtin_amdgcn_frexp_expf(a)));
+    a = __builtin_amdgcn_frexp_mantf(a);
+  }
+  __device__ __forceinline__ void times(const Run& r) {  // both settled
+    a *= r.a;
+    e += r.e;
+    settle();
+  }
+  __device__ __forceinline__ float plus(float s, float add) const {
+    return __builtin_amdgcn_ldexpf(a * __builtin_amdgcn_frexp_mantf(s), e + __builtin_amdgcn_frexp_expf(s)) + add;
+  }
+  __device__ __forceinline__ float of(float s) const { return plus(s, b); }
+};
 
 // VEC values at d of the row that starts `off` elements into an array (off is the same in
 // every lane, d a lane's).
@@ -89,7 +132,7 @@ __device__ __forceinline__ void lds_barrier() {
 // (one read of the inputs) took 83 + 140 us for both scans, against 89 + 119 with it.
 template <typename IO, int VEC, bool SIG, bool LEAKY, bool BWD>
 __global__ void __launch_bounds__(kW * 64) scan_runs_kernel(ScanArgs p) {
-  __shared__ float2 sh[kW][64 * VEC];
+  __shared__ Run<SIG> sh[kW][64 * VEC];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int b = blockIdx.y;
   const int seg = BWD ? int(blockIdx.z) + 1 : int(blockIdx.z);  // the first (last) block's run feeds nobody
@@ -104,9 +147,9 @@ __global__ void __launch_bounds__(kW * 64) scan_runs_kernel(ScanArgs p) {
   const int64_t xb = b * (BWD ? p.gh_b : p.x_b), gb = b * p.g_b;
   const void* xs = BWD ? p.gh : p.x;
   const int64_t xt = BWD ? p.gh_t : p.x_t;
-  float A[VEC], B[VEC];
+  Run<SIG> r[VEC];
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) A[v] = 1.0f, B[v] = 0.0f;
+  for (int v = 0; v < VEC; ++v) r[v].one(), r[v].b = 0.0f;
   const int n = s1 - s0;
   for (int j0 = 0; j0 < n; j0 += kL) {  // (loads further ahead than this measured no faster)
     Pack<IO, VEC> rx[kL], rg[kL];
@@ -125,35 +168,38 @@ __global__ void __launch_bounds__(kW * 64) scan_runs_kernel(ScanArgs p) {
         float a, na;
         decay<SIG>(widen(rg[j].v[v]), a, na);
         const float xv = widen(rx[j].v[v]);
-        const float next = BWD ? a * (xv + B[v]) : fmaf(a, B[v], LEAKY ? na * xv : xv);
-        B[v] = in ? next : B[v];
-        A[v] = in ? A[v] * a : A[v];
+        const float next = BWD ? a * (xv + r[v].b) : fmaf(a, r[v].b, LEAKY ? na * xv : xv);
+        r[v].b = in ? next : r[v].b;
+        r[v].times(in ? a : 1.0f);
       }
     }
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) r[v].settle();
   }
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) sh[w][v * 64 + lane] = make_float2(A[v], B[v]);
+  for (int v = 0; v < VEC; ++v) sh[w][v * 64 + lane] = r[v];
   __syncthreads();
   if (w == 0 && on) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      float2 c = sh[BWD ? kW - 1 : 0][v * 64 + lane];
+      Run<SIG> c = sh[BWD ? kW - 1 : 0][v * 64 + lane];
       for (int k = 1; k < kW; ++k) {
-        const float2 r = sh[BWD ? kW - 1 - k : k][v * 64 + lane];
-        c = make_float2(r.x * c.x, fmaf(r.x, c.y, r.y));
+        const Run<SIG> next = sh[BWD ? kW - 1 - k : k][v * 64 + lane];
+        c.b = next.of(c.b);
+        c.times(next);
       }
-      p.runs[(int64_t(seg) * p.batch + b) * p.D + d + v] = c;
+      static_cast<Run<SIG>*>(p.runs)[(int64_t(seg) * p.batch + b) * p.D + d + v] = c;
     }
   }
 }
 
 // What enters block `to` of the split, from what entered block `from`: the runs between,
-// in the order of `step`, sixteen at a time in flight.
-template <int VEC>
-__device__ __forceinline__ void enter(float (&carry)[VEC], const float2* runs, int64_t lanes, int from, int to, int step) {
-  constexpr int U = 16;
+// in the order of `step`, sixteen (of three words: eight) at a time in flight.
+template <int VEC, bool SIG>
+__device__ __forceinline__ void enter(float (&carry)[VEC], const Run<SIG>* runs, int64_t lanes, int from, int to, int step) {
+  constexpr int U = SIG ? 16 : 8;
   for (int s0 = from; s0 != to; s0 += step * min(U, (to - s0) * step)) {
-    float2 r[U][VEC];
+    Run<SIG> r[U][VEC];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int s = (to - s0) * step > u ? s0 + u * step : s0;
@@ -164,7 +210,7 @@ __device__ __forceinline__ void enter(float (&carry)[VEC], const float2* runs, i
     for (int u = 0; u < U; ++u)
       if ((to - s0) * step > u)
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) carry[v] = fmaf(r[u][v].x, carry[v], r[u][v].y);
+        for (int v = 0; v < VEC; ++v) carry[v] = r[u][v].of(carry[v]);
   }
 }
 
@@ -175,10 +221,10 @@ __device__ __forceinline__ void enter(float (&carry)[VEC], const float2* runs, i
 // sequences of 4096 channels in bf16 took 56 us forward and 134 backward for one step, 10
 // and 14 so; 64 steps of 512 x 1000 in fp32 115 and 181, 90 and 162 so.
 template <typename IO, int VEC, bool SIG, bool LEAKY, int W>
-__global__ void __launch_bounds__(kW * 64, W ? 4 : 2) scan_fwd_kernel(ScanArgs p) {
+__global__ void __launch_bounds__(kW * 64, W || sizeof(IO) == 2 ? 4 : 2) scan_fwd_kernel(ScanArgs p) {
   constexpr bool ONE = W > 0;
   constexpr int N = ONE ? W : kW;  // waves of a tile
-  __shared__ float2 sh[ONE ? 1 : 2][kW][64 * VEC];
+  __shared__ Run<SIG> sh[ONE ? 1 : 2][kW][64 * VEC];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int w = N < kW ? wave % N : wave, first = N < kW ? wave - w : 0;  // in its tile; its tile's first
   const int b = blockIdx.y, seg = blockIdx.z;
@@ -192,7 +238,7 @@ __global__ void __launch_bounds__(kW * 64, W ? 4 : 2) scan_fwd_kernel(ScanArgs p
   float carry[VEC];
 #pragma unroll
   for (int v = 0; v < VEC; ++v) carry[v] = p.h0 ? p.h0[bd + v] : 0.0f;
-  if (!ONE) enter<VEC>(carry, p.runs + bd, lanes, 0, seg, 1);
+  if (!ONE) enter<VEC, SIG>(carry, static_cast<const Run<SIG>*>(p.runs) + bd, lanes, 0, seg, 1);
 
   const int k0 = ONE ? 0 : seg * p.per, k1 = ONE ? 1 : min(k0 + p.per, p.ntiles);
   struct Raw {
@@ -213,24 +259,31 @@ __global__ void __launch_bounds__(kW * 64, W ? 4 : 2) scan_fwd_kernel(ScanArgs p
   auto tile = [&](auto whole, Raw& raw, int k, int buf) {
     constexpr bool WHOLE = decltype(whole)::value;
     const int t0 = k * kTile + w * kL;
-    float P[kL][VEC], H[kL][VEC];  // the run of the wave's first j + 1 steps
+    // what takes the state before the wave's steps to the one after step j, A s + b; where decays
+    // are given, the state before that step (the products of several may be no numbers)
+    float P[kL][VEC], H[kL][VEC];
+    Run<SIG> run[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) run[v].one(), run[v].b = 0.0f;
 #pragma unroll
     for (int j = 0; j < kL; ++j) {
       const bool in = WHOLE || t0 + j < len;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        const float pp = j ? P[j - 1][v] : 1.0f, hp = j ? H[j - 1][v] : 0.0f;
         float a, na;
         decay<SIG>(widen(raw.g[j].v[v]), a, na);
         const float xv = widen(raw.x[j].v[v]);
-        P[j][v] = in ? pp * a : pp;
-        H[j][v] = in ? fmaf(a, hp, LEAKY ? na * xv : xv) : hp;
+        const float u = LEAKY ? na * xv : xv, next = fmaf(a, run[v].b, u);
+        run[v].times(in ? a : 1.0f);
+        run[v].b = in ? next : run[v].b;
+        P[j][v] = SIG ? run[v].a : in ? a : 1.0f;
+        H[j][v] = SIG ? run[v].b : in ? u : 0.0f;
       }
     }
     if (!ONE) fetch(raw, k + 2);
     if (N > 1) {
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) sh[buf][wave][v * 64 + lane] = make_float2(P[kL - 1][v], H[kL - 1][v]);
+      for (int v = 0; v < VEC; ++v) sh[buf][wave][v * 64 + lane] = run[v];
       lds_barrier();
     }
     float in[VEC];
@@ -240,9 +293,9 @@ __global__ void __launch_bounds__(kW * 64, W ? 4 : 2) scan_fwd_kernel(ScanArgs p
       in[v] = carry[v];
 #pragma unroll
       for (int q = 0; q < N; ++q) {
-        const float2 r = N > 1 ? sh[buf][first + q][v * 64 + lane] : make_float2(P[kL - 1][v], H[kL - 1][v]);
+        const Run<SIG> r = N > 1 ? sh[buf][first + q][v * 64 + lane] : run[v];
         if (q == w) in[v] = carry[v];
-        carry[v] = fmaf(r.x, carry[v], r.y);
+        carry[v] = r.of(carry[v]);
       }
     }
     if (on) {
@@ -251,7 +304,11 @@ __global__ void __launch_bounds__(kW * 64, W ? 4 : 2) scan_fwd_kernel(ScanArgs p
         const int t = t0 + j;
         Pack<IO, VEC> o;
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) o.v[v] = narrow<IO>(WHOLE || t < len ? fmaf(P[j][v], in[v], H[j][v]) : 0.0f);
+        for (int v = 0; v < VEC; ++v) {
+          const float state = fmaf(P[j][v], in[v], H[j][v]);
+          if (!SIG) in[v] = state;
+          o.v[v] = narrow<IO>(WHOLE || t < len ? state : 0.0f);
+        }
         if (WHOLE || t < p.T) store_row<IO, VEC>(p.h, t * p.h_t + hb, d, o);
       }
     }
@@ -285,7 +342,8 @@ template <typename IO, int VEC, bool SIG, bool LEAKY, int W>
 __global__ void __launch_bounds__(kW * 64, 2) scan_bwd_kernel(ScanArgs p) {
   constexpr bool ONE = W > 0;  // as in the forward
   constexpr int N = ONE ? W : kW, S = ONE ? 1 : 2;
-  __shared__ float shA[S][kW][64 * VEC], shH[S][kW][64 * VEC], shC[S][kW][64 * VEC];
+  __shared__ Run<SIG> shH[S][kW][64 * VEC];  // the states' runs; the gradient's have their products
+  __shared__ float shC[S][kW][64 * VEC];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int w = N < kW ? wave % N : wave, first = N < kW ? wave - w : 0;  // in its tile; its tile's first
   const int b = blockIdx.y, seg = blockIdx.z;
@@ -299,7 +357,7 @@ __global__ void __launch_bounds__(kW * 64, 2) scan_bwd_kernel(ScanArgs p) {
   float carry[VEC];  // c of the tile's last step
 #pragma unroll
   for (int v = 0; v < VEC; ++v) carry[v] = p.gh_last ? p.gh_last[bd + v] : 0.0f;
-  if (!ONE) enter<VEC>(carry, p.runs + bd, lanes, int(gridDim.z) - 1, seg, -1);
+  if (!ONE) enter<VEC, SIG>(carry, static_cast<const Run<SIG>*>(p.runs) + bd, lanes, int(gridDim.z) - 1, seg, -1);
 
   const int k0 = ONE ? 0 : seg * p.per, k1 = ONE ? 1 : min(k0 + p.per, p.ntiles);
   struct Raw {
@@ -325,9 +383,10 @@ __global__ void __launch_bounds__(kW * 64, 2) scan_bwd_kernel(ScanArgs p) {
     constexpr bool WHOLE = decltype(whole)::value;
     const int t0 = k * kTile + w * kL;
     float a[kL][VEC], na[kL][VEC], x[kL][VEC], dh[kL][VEC];
-    float A[VEC], H[VEC], C[VEC];
+    Run<SIG> H[VEC];
+    float C[VEC];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) A[v] = 1.0f, H[v] = 0.0f, C[v] = 0.0f;
+    for (int v = 0; v < VEC; ++v) H[v].one(), H[v].b = 0.0f, C[v] = 0.0f;
 #pragma unroll
     for (int j = 0; j < kL; ++j) {
 #pragma unroll
@@ -339,8 +398,8 @@ __global__ void __launch_bounds__(kW * 64, 2) scan_bwd_kernel(ScanArgs p) {
         na[j][v] = in ? nav : 0.0f;
         x[j][v] = in ? widen(raw.x[j].v[v]) : 0.0f;
         dh[j][v] = in ? widen(raw.h[j].v[v]) : 0.0f;
-        A[v] *= a[j][v];
-        H[v] = fmaf(a[j][v], H[v], LEAKY ? na[j][v] * x[j][v] : x[j][v]);
+        H[v].times(a[j][v]);
+        H[v].b = fmaf(a[j][v], H[v].b, LEAKY ? na[j][v] * x[j][v] : x[j][v]);
       }
     }
 #pragma unroll
@@ -353,7 +412,6 @@ __global__ void __launch_bounds__(kW * 64, 2) scan_bwd_kernel(ScanArgs p) {
     for (int v = 0; v < VEC; ++v) {
       hin[v] = raw.start[v];
       if (N > 1) {
-        shA[buf][wave][v * 64 + lane] = A[v];
         shH[buf][wave][v * 64 + lane] = H[v];
         shC[buf][wave][v * 64 + lane] = C[v];
       }
@@ -365,12 +423,12 @@ __global__ void __launch_bounds__(kW * 64, 2) scan_bwd_kernel(ScanArgs p) {
       const int at = v * 64 + lane;
 #pragma unroll
       for (int q = 0; q < N - 1; ++q)
-        if (q < w) hin[v] = fmaf(shA[buf][first + q][at], hin[v], shH[buf][first + q][at]);
+        if (q < w) hin[v] = shH[buf][first + q][at].of(hin[v]);
       cin[v] = carry[v];
 #pragma unroll
       for (int q = N - 1; q >= 0; --q) {
         if (q == w) cin[v] = carry[v];
-        carry[v] = fmaf(N > 1 ? shA[buf][first + q][at] : A[v], carry[v], N > 1 ? shC[buf][first + q][at] : C[v]);
+        carry[v] = N > 1 ? shH[buf][first + q][at].plus(carry[v], shC[buf][first + q][at]) : H[v].plus(carry[v], C[v]);
       }
     }
     float before[kL][VEC];
@@ -523,7 +581,8 @@ Plan make_plan(const dendsn_scan_cfg* c) {
 
 size_t runs_bytes(const dendsn_scan_cfg* c) {
   const Plan p = make_plan(c);
-  return p.S > 1 ? size_t(p.S) * size_t(c->batch) * size_t(c->D) * sizeof(float2) : 0;
+  const size_t run = c->gate == DENDSN_GATE_SIGMOID ? sizeof(Run<true>) : sizeof(Run<false>);
+  return p.S > 1 ? size_t(p.S) * size_t(c->batch) * size_t(c->D) * run : 0;
 }
 
 size_t ckpt_bytes(const dendsn_scan_cfg* c) {
@@ -651,7 +710,7 @@ dendsn_status dendsn_scan_forward(const dendsn_scan_cfg* cfg, const void* x, con
   LaunchFwd f{{}, make_plan(cfg), stream};
   ScanArgs& a = f.a;
   a.x = x; a.g = g; a.h0 = h0; a.lengths = lengths; a.h = h; a.h_last = h_last; a.ckpt = ckpt;
-  a.runs = static_cast<float2*>(workspace);
+  a.runs = workspace;
   a.D = cfg->D; a.T = int32_t(cfg->T); a.batch = int32_t(cfg->batch); a.ntiles = f.p.ntiles; a.per = f.p.per;
   a.x_t = cfg->x_t; a.x_b = cfg->x_b; a.g_t = cfg->g_t; a.g_b = cfg->g_b; a.h_t = cfg->h_t; a.h_b = cfg->h_b;
   dispatch(cfg, f.p.vec == 2, f);
@@ -691,7 +750,7 @@ dendsn_status dendsn_scan_backward(const dendsn_scan_cfg* cfg, const void* x, co
   ScanArgs& a = f.a;
   a.x = x; a.g = g; a.gh = grad_h; a.lengths = lengths; a.ckpt_in = ckpt; a.gh_last = grad_h_last;
   a.gx = grad_x; a.gg = grad_g; a.gh0 = grad_h0;
-  a.runs = static_cast<float2*>(workspace);
+  a.runs = workspace;
   a.D = cfg->D; a.T = int32_t(cfg->T); a.batch = int32_t(cfg->batch); a.ntiles = f.p.ntiles; a.per = f.p.per;
   a.x_t = cfg->x_t; a.x_b = cfg->x_b; a.g_t = cfg->g_t; a.g_b = cfg->g_b;
   a.gh_t = cfg->grad_h_t; a.gh_b = cfg->grad_h_b; a.gx_t = cfg->grad_x_t; a.gx_b = cfg->grad_x_b;

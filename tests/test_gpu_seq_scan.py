@@ -252,3 +252,39 @@ def test_step(gpu_device, b, D, io):
         both = torch.cat([x[0], g[0]], dim=-1)
         h = dendsn.gated_scan_step(one, both[:, :D], both[:, D:], plain)
         seq_ref.assert_within(h, ref["h"][0][0], ref["h"][1][0], "h without slots")
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [8, 30, 64, 150, 2500])
+def test_decays_beyond_one(gpu_device, T, io):
+    """Given decays of any size: the product of many is no fp32 number, their states are.  States of
+    0 stay 0 until something comes in; a state of 2^-100 is brought up and down again; a decay of 0
+    forgets."""
+    b, D = 2, 10
+    for leaky in (False, True):
+        cfg = dendsn.GatedScanConfig(T=T, batch=b, D=D, io=io, gate="decay", leaky=leaky)
+        d = make(T, b, D, io, "decay", T, carry=True)
+        x, g, gh, h0, last = d["x"], d["g"], d["grad_h"], d["h0"], d["grad_last"]
+        t = torch.arange(T)
+        late = t >= T - T // 4
+        # growth while the state is 0: inputs come at the end, gradients at the first step
+        for i, a in enumerate((1.25, 2.0 ** 40, -1.5, 2.0 ** 120)):
+            g[:, :, i] = torch.where(late, 0.75, a)[:, None]
+            x[~late, :, i] = 0.0
+            h0[:, i] = 0.0
+            last[:, i] = 0.0
+            gh[1:, :, i] = 0.0
+        # up and down by 2^66 twice
+        for i, order in ((4, (66, 66, -66, -66)), (5, (-66, -66, 66, 66))):
+            g[:, :, i] = torch.tensor([2.0 ** order[k % 4] for k in range(T)])[:, None]
+            x[:, :, i], gh[:, :, i] = 0.0, 0.0
+            h0[:, i] = 2.0 ** (-100 if order[0] > 0 else 100)
+            # (in range on the way back, and so is its product with the state)
+            last[:, i] = 2.0 ** (-100 if order[(T - 1) % 4] > 0 else 100 if T % 4 == 0 else 30)
+        # large decays, of which one is 0
+        g[:, :, 6] = torch.where(t == T // 2, 0.0, torch.where(t < T // 2, 2.0 ** 30, 0.5))[:, None]
+        x[t < T // 2, :, 6], h0[:, 6], gh[:, :, 6], last[:, 6] = 0.0, 0.0, 0.0, 1.0
+        # decays far below one, whose product is none either
+        g[:, :, 7] = 2.0 ** -100
+        announce(f"scan decays beyond one {cfg}")
+        check(cfg, d, gpu_device)
