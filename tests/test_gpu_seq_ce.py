@@ -427,3 +427,26 @@ def test_products_of_fp32_planes(gpu_device, D):
     _, lse = dendsn.linear_ce(cfg, big.to(gpu_device), w.to(gpu_device), t)
     z = torch.matmul(big.double(), w[0].double())
     seq_ref.assert_within(lse, z, (D + 2) * U * z, "lse of the largest numbers")
+
+
+def test_pieces_of_rows_in_fp32(gpu_device):
+    """Logits of 3072 rows at a time, with their gradient's planes."""
+    N, V, D = 3400, 131072, 16
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D)
+    one = dendsn.dendsn_ce_workspace_bytes(cfg.with_(N=1700), True)
+    assert dendsn.dendsn_ce_workspace_bytes(cfg, True) < 1.5 * one
+    announce(f"ce pieces {cfg}")
+    check(cfg, *make(N, V, D, "f32", gpu_device, 14))
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V,D", [((1 << 20) + 1000, 70, 8), (3 << 19, 5, 16)])
+def test_pieces_of_rows_without_gradients(gpu_device, N, V, D, io):
+    """The loss alone of more rows than a piece has."""
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io)
+    h, w, t, _ = make(N, V, D, io, gpu_device, 15)
+    announce(f"ce pieces {cfg}")
+    ref = seq_ref.ce(h, w, t, 1.0, io, train=False)
+    loss, lse = dendsn.linear_ce(cfg, h, w, t)
+    seq_ref.assert_within(loss, *ref["loss"], "loss")
+    seq_ref.assert_within(lse, *ref["lse"], "lse")

@@ -138,3 +138,18 @@ def test_rows_without_a_token_are_plus_zero_at_any_scale(gpu_device, io, D):
     named[ids] = True
     assert not named.all()
     assert not got.cpu()[~named].view(torch.int16 if io == "bf16" else torch.int32).any()
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("n,V,D", [(33000, 5000, 520), (40001, 300, 1025), (600001, 3000, 8), (1100000, 100, 3)])
+def test_gradient_of_many_tokens(gpu_device, n, V, D, io):
+    """Runs of 32 positions and their joins; sorting blocks of two and three rounds of 1024, whose
+    bases are carried on."""
+    ids, _, grad = make(n, V, D, io, "skewed", seed=n)
+    cfg = dendsn.EmbeddingConfig(n=n, V=V, D=D, io=io, scale=0.5)
+    announce(f"embed gradient {cfg}")
+    d = [t.to(gpu_device) for t in (ids, grad)]
+    got, again = (dendsn.embedding_backward(cfg, *d) for _ in range(2))
+    ref, bound = seq_ref.embed_backward(ids, grad, V, 0.5, io)
+    seq_ref.assert_within(got, ref, bound, "grad_table")
+    assert torch.equal(got.view(torch.uint8), again.view(torch.uint8))

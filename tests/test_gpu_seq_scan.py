@@ -288,3 +288,25 @@ def test_decays_beyond_one(gpu_device, T, io):
         g[:, :, 7] = 2.0 ** -100
         announce(f"scan decays beyond one {cfg}")
         check(cfg, d, gpu_device)
+
+
+@pytest.mark.parametrize("T,b,D,io,gate,leaky,ragged", [
+    (700, 16, 2048, "bf16", "sigmoid", True, False), (700, 16, 2048, "f32", "decay", False, True),
+    (650, 129, 255, "bf16", "decay", True, True), (650, 129, 255, "f32", "sigmoid", False, False),
+    (16400, 1, 2000, "bf16", "sigmoid", True, False), (9000, 2, 1001, "f32", "decay", False, True)])
+def test_many_tiles_a_block(gpu_device, T, b, D, io, gate, leaky, ragged):
+    """Blocks that walk ten tiles of whole sequences (256 blocks and more: no split), and splits of
+    nine tiles a block: every channel is its own recurrence, and some of them are compared."""
+    cfg = dendsn.GatedScanConfig(T=T, batch=b, D=D, io=io, gate=gate, leaky=leaky)
+    d = make(T, b, D, io, gate, T + D, ragged, carry=True)
+    announce(f"scan {cfg} ragged {ragged}")
+    got, again = run(cfg, d, gpu_device), run(cfg, d, gpu_device)
+    some = torch.tensor(sorted({0, 1, 63, 64, 127, 128, 129, D // 2, D - 130, D - 2, D - 1}))
+    part = {k: v if v is None or k == "lengths" else v[..., some] for k, v in d.items()}
+    ref = seq_ref.scan(part["x"], part["g"], gate, leaky, io, part["h0"], part["lengths"], part["grad_h"],
+                       part["grad_last"])
+    for k, (value, bound) in ref.items():
+        seq_ref.assert_within(got[k].cpu()[..., some], value, bound, k)
+    for k in got:
+        assert bool(torch.isfinite(got[k]).all()), k
+        assert torch.equal(got[k].contiguous().view(torch.uint8), again[k].contiguous().view(torch.uint8)), k
