@@ -168,7 +168,8 @@ __device__ __forceinline__ void row_statistics(const f32x4 (&acc)[FN][FM], int64
         // (the difference first: see exp_diff)
         sum += in(i, r) ? __builtin_amdgcn_exp2f(c * (acc[i][j][r] - ref)) : 0.0f;
     sum = over_groups(sum, [](float a, float b) { return a + b; });
-    if (lane < 16) to[16 * j] = make_float2(scale * top, sum);
+    // (no class of its own: minus infinity at a scale of 0 too)
+    if (lane < 16) to[16 * j] = make_float2(top == -INFINITY ? top : scale * top, sum);
   }
 }
 

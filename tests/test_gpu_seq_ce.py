@@ -450,3 +450,16 @@ def test_pieces_of_rows_without_gradients(gpu_device, N, V, D, io):
     loss, lse = dendsn.linear_ce(cfg, h, w, t)
     seq_ref.assert_within(loss, *ref["loss"], "loss")
     seq_ref.assert_within(lse, *ref["lse"], "lse")
+
+
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V", [(5, 70), (100, 130), (300, 1003), (1921, 5100)])
+def test_logit_scale_of_zero(gpu_device, N, V, io):
+    """All logits are 0, also where the last classes leave part of a tile empty: lse is log V, and the
+    gradients are 0."""
+    D = 64
+    cfg = dendsn.LinearCEConfig(N=N, V=V, D=D, io=io, logit_scale=0.0)
+    h, w, t, r = make(N, V, D, io, gpu_device, 16)
+    announce(f"ce scale 0 {cfg}")
+    got = check(cfg, h, w, t, r)
+    assert not got["grad_hidden"].any() and not got["grad_weight"].any()
