@@ -96,9 +96,9 @@ def _stream(device):
     Stream object."""
     import torch
 
-    _check_device(device)
-    return torch._C._cuda_getCurrentRawStream(device.index if device.index is not None else
-                                              torch.cuda.current_device())
+    if device.type != "cuda" or device.index != torch._C._cuda_getDevice():
+        _check_device(device)  # raises
+    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def dendsn_seq_last_error() -> str:
