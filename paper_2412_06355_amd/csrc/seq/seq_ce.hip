@@ -39,12 +39,6 @@ struct PackArgs {
   int64_t first;  // thread of the launch's first
 };
 
-// The bf16 nearest to finite bits u, or the one below where that is infinite.
-__device__ __forceinline__ uint16_t nearest(uint32_t u) {
-  const uint32_t r = u + 0x7FFFu + (u >> 16 & 1);
-  return uint16_t(((r & 0x7F800000u) == 0x7F800000u ? u : r) >> 16);
-}
-
 // v as three bf16 that add up to it: each the nearest to what the ones before leave, so that
 // the second is at most 2^-8 and the third 2^-17 of v's power of two, with either sign (cut
 // off, they would be twice and four times that, all of v's sign, and so would what the
@@ -58,9 +52,10 @@ __device__ __forceinline__ void split3(float v, uint16_t& a, uint16_t& finite, u
     finite = b = c = 0;
     return;
   }
-  a = finite = nearest(u);
+  constexpr float kMost = 3.38953139e38f;  // of bf16: beyond it the nearest would be infinite
+  a = finite = bf16_bits(__builtin_amdgcn_fmed3f(v, -kMost, kMost));
   const float r1 = v - __uint_as_float(uint32_t(a) << 16);
-  b = nearest(__float_as_uint(r1));
+  b = bf16_bits(r1);
   const float r2 = r1 - __uint_as_float(uint32_t(b) << 16);
   c = uint16_t(__float_as_uint(r2) >> 16);  // (at most eight bits are left)
 }
@@ -120,9 +115,9 @@ __device__ __forceinline__ float exp_diff(float a, float b) {
   return __builtin_amdgcn_exp2f(1.44269504f * (a - b));
 }
 
-// What the exponentials of a row are taken from: its maximum, or 0 where that is infinite (the
-// sum is then 0 or infinite, and so is what it gives).
-__device__ __forceinline__ float anchor(float top) { return fabsf(top) == INFINITY ? 0.0f : top; }
+// What the exponentials of a row are taken from: its maximum, kept finite, since infinity
+// less itself is none (minus infinity then gives a sum of 0, plus infinity an infinite one).
+__device__ __forceinline__ float anchor(float top) { return __builtin_amdgcn_fmed3f(top, -3.40282347e38f, 3.40282347e38f); }
 
 struct LogitArgs {
   GemmArgs g;
@@ -168,8 +163,8 @@ __device__ __forceinline__ void row_statistics(const f32x4 (&acc)[FN][FM], int64
         // (the difference first: see exp_diff)
         sum += in(i, r) ? __builtin_amdgcn_exp2f(c * (acc[i][j][r] - ref)) : 0.0f;
     sum = over_groups(sum, [](float a, float b) { return a + b; });
-    // (no class of its own: minus infinity at a scale of 0 too)
-    if (lane < 16) to[16 * j] = make_float2(top == -INFINITY ? top : scale * top, sum);
+    // (of a finite maximum: with no class of its own and a scale of 0 the other would be NaN)
+    if (lane < 16) to[16 * j] = make_float2(scale * ref, sum);
   }
 }
 
@@ -572,8 +567,7 @@ __global__ void __launch_bounds__(kThreads) ce_loss_kernel(LossArgs p) {
     const float z = !keep ? 0.0f : p.scale * (p.z ? p.z[(t / kStep * p.zrows + m) * kStep + t % kStep] : p.chosen[m]);
     p.loss[m] = keep ? (ref - z) + log_sum : 0.0f;
     if (p.lse) p.lse[m] = keep ? ref + log_sum : 0.0f;
-    // (a maximum of plus infinity: no other class has a part)
-    if (p.norm) p.norm[m] = top == INFINITY ? make_float2(top, 1.0f) : make_float2(ref, 1.0f / sum);
+    if (p.norm) p.norm[m] = make_float2(ref, 1.0f / sum);
   }
 }
 
