@@ -12,8 +12,8 @@
  *                channel by channel, forward, backward and one token at a time
  *   linear CE    softmax cross entropy of a linear readout over a vocabulary,
  *                  z = scale * hidden weight^T,  lse = log sum_v exp(z_v),  loss = lse - z_target
- *                with the gradients of both operands; the logits of all rows are
- *                never held together
+ *                with the gradients of both operands; at most 4 GiB of logits are held
+ *                at a time (all of them where they fit), without gradients none
  *
  * Conventions (those of dendsn.h):
  *   - Every tensor pointer is a DEVICE pointer owned by the caller, aligned to
@@ -24,7 +24,9 @@
  *   - An output, a checkpoint or a workspace may overlap neither an input nor
  *     another of them (not checked), but for the state of dendsn_scan_step.
  *   - Outputs are overwritten, never accumulated.  Results are deterministic: the
- *     same inputs give bit-identical outputs.
+ *     same inputs, of the same alignment and strides (by which kernels are chosen,
+ *     whose sums run in other orders), give bit-identical outputs.
+ *   - Kernels run on the current device, whose memory and stream the arguments are.
  *   - Every argument check runs on the host before anything is launched; on
  *     failure the call writes nothing, returns a status, and
  *     dendsn_seq_last_error() on the calling thread describes the first failed

@@ -6,13 +6,13 @@
 // The rows go through in pieces whose logits fit a bounded scratch.  Of a piece, the
 // first product leaves each row's maximum and sum of exponentials over every tile of
 // the vocabulary (and, for the gradient, its fp32 logits); the tiles' statistics are
-// joined into lse; the gradient of the logits, without the rows' common factor (see
+// joined into the row's; the gradient of the logits, without the rows' common factor (see
 // ce_unit_kernel), is rounded to bf16 once and enters the two other products, dW summed
 // over the pieces in fp32.  The three products carry the time: 2 N V D operations each.
 //
-// 8192 rows, 128000 classes, 2048 features in bf16, 11.8 ms: logits 4.05 ms (1060 TF with
-// their 4.2 GB of stores; 1275 TF without), dz 1.20 ms (5.2 TB/s), dH 2.95 ms (1460 TF), dW
-// 3.5 ms (1230 TF); the card's power limit holds the clock at 1.8 to 1.95 GHz throughout.
+// 8192 rows, 128000 classes, 2048 features in bf16, 11.7 ms: logits 4.02 ms (1070 TF with
+// their 4.2 GB of stores; 1275 TF without), dz 1.21 ms (5.2 TB/s), dH 2.92 ms (1470 TF), dW
+// 3.52 ms (1220 TF); the card's power limit holds the clock at 1.8 to 1.95 GHz throughout.
 // A library product of 8192^3 reaches 1510 TF, of dW's form 1060.
 #include "seq_gemm.h"
 
@@ -110,7 +110,8 @@ __global__ void __launch_bounds__(kThreads) ce_pack_kernel(PackArgs p) {
 // The products
 // ---------------------------------------------------------------------------
 // exp(a - b): the difference first, which is exact where it matters (a scaled maximum
-// would be rounded, by hundredths for logits of 10^4).
+// would be rounded, by hundredths for logits of 10^4).  The argument of exp2 is rounded once: a
+// probability p is off by p |log p| 2^-24, at most 0.37 x 2^-24.
 __device__ __forceinline__ float exp_diff(float a, float b) {
   return __builtin_amdgcn_exp2f(1.44269504f * (a - b));
 }

@@ -4,9 +4,11 @@
 //
 // The gradient adds each row's positions in an order that the ids alone fix: positions
 // are sorted by id (a stable radix sort of up to 9 bits a pass), every wave sums the
-// runs of equal ids among 16 or 32 sorted positions, whatever their rows, so that frequent
-// tokens cost no more than rare ones, and the sums of ids that go on past a wave's
-// positions are joined by a second kernel.  Rows that no token names are cleared beside
+// runs of equal ids among 16 or 32 sorted positions, whatever their rows, and the sums of
+// ids that go on past a wave's positions are joined by a second kernel.  The sums of a
+// frequent token are so spread over the chip; its join (one block for 256 to 512 values of
+// the row, a term for every 16 or 32 positions) and the block that clears its neighbours (it
+// reads their ids once) still grow with its count.  Rows that no token names are cleared beside
 // the sums.  Both directions are bound by memory: the gradient writes all V rows.
 //
 // 32768 tokens (frequencies 1 / rank) in 50001 rows of 1024 in bf16: lookup 21 us (67 MB

@@ -13,7 +13,7 @@
 // kernel composes each block's run, and the scan starts from the runs before it.
 //
 // Bound by memory: bytes read once, written once, and the checkpoints (1/64 of a fp32
-// state a step).  8192 steps, 8 sequences, 4096 channels in bf16: both together 823 us
+// state a step).  8192 steps, 8 sequences, 4096 channels in bf16: both together 826 us
 // (5.2 TB/s, as a copy; under a profiler 341 and 575).  64 steps, 32 sequences: 33 us, 12.5
 // and 22 under a profiler.
 #include "seq_common.h"
@@ -37,7 +37,8 @@ struct ScanArgs {
   int32_t T, batch, ntiles, per;  // per: tiles of a block of the split
 };
 
-// The decay and its complement, each with full relative accuracy.
+// The decay and its complement, each to (|g| + 6) 2^-24 of itself: |g| 2^-24 is the rounding of
+// the exponential's argument, which the smaller of the two alone carries.
 template <bool SIG>
 __device__ __forceinline__ void decay(float g, float& a, float& na) {
   if (SIG) {
