@@ -430,7 +430,7 @@ def test_products_of_fp32_planes(gpu_device, D):
 
 
 def test_pieces_of_rows_in_fp32(gpu_device):
-    """Logits of 3072 rows at a time, with their gradient's planes."""
+    """The logits of 3400 rows and their gradient's planes do not fit the scratch at once: two pieces."""
     N, V, D = 3400, 131072, 16
     cfg = dendsn.LinearCEConfig(N=N, V=V, D=D)
     one = dendsn.dendsn_ce_workspace_bytes(cfg.with_(N=1700), True)
