@@ -2,8 +2,9 @@
 
 The forward temporal scan of a layer of dendritic spiking neurons and its
 surrogate-gradient backward scan, as hand-written HIP kernels behind the C ABI
-of include/dendsn.h, and the token-sequence operators around such layers behind
-that of include/dendsn_seq.h.  This package is the Python binding of that library.
+of include/dendsn.h, the token-sequence operators around such layers behind
+that of include/dendsn_seq.h, and the operators of a block of layers and of its
+training step behind that of include/dendsn_block.h.  This package is the Python binding of that library.
 """
 
 from .binding import (  # noqa: F401
@@ -22,6 +23,31 @@ from .binding import (  # noqa: F401
     dendsn_status_str,
     forward,
     lib,
+)
+from .block import (  # noqa: F401
+    BLOCK_EXPORTS,
+    AdamWConfig,
+    DeltaRuleConfig,
+    RMSNormConfig,
+    adamw,
+    adamw_states,
+    block_lib,
+    delta_rule,
+    delta_rule_backward,
+    delta_rule_step,
+    dendsn_adamw_step,
+    dendsn_delta_backward,
+    dendsn_delta_ckpt_bytes,
+    dendsn_delta_forward,
+    dendsn_delta_step,
+    dendsn_delta_workspace_bytes,
+    dendsn_norm_backward,
+    dendsn_norm_forward,
+    dendsn_norm_forward_e4m3,
+    dendsn_norm_workspace_bytes,
+    rms_norm,
+    rms_norm_backward,
+    rms_norm_e4m3,
 )
 from .sequence import (  # noqa: F401
     SEQ_EXPORTS,

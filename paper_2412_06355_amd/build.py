@@ -25,8 +25,9 @@ _BWD = ["dendsn_bwd_f32_cm.hip", "dendsn_bwd_bf16_cm.hip", "dendsn_bwd_bf16_kc.h
         "dendsn_bwd_bf16.hip", "dendsn_bwd_f32.hip"]
 _OTHER = ["dendsn_fwd_f32_cm.hip", "dendsn_fwd_bf16_cm.hip", "dendsn_fwd_f32_kc.hip", "dendsn_fwd_bf16_kc.hip",
           "dendsn_api.hip", "dendsn_fwd_f32.hip", "dendsn_fwd_bf16.hip"]
-# The token-sequence operators (csrc/seq).
-_SEQ = ["seq/seq_ce.hip", "seq/seq_scan.hip", "seq/seq_embed.hip", "seq/seq_api.hip"]
+# The token-sequence operators and those of a block (csrc/seq).
+_SEQ = ["seq/seq_delta.hip", "seq/seq_ce.hip", "seq/seq_scan.hip", "seq/seq_embed.hip", "seq/seq_norm.hip",
+        "seq/seq_adamw.hip", "seq/seq_api.hip"]
 SOURCES = [(src, [f"-DDENDSN_SG={k}", f"-DDENDSN_SL={m}"], f"{src[:-4]}_sg{k}_sl{m}.o")
            for src in _BWD for m in (0, 1) for k in (0, 1)] + \
           [(src, [], f"{os.path.basename(src)[:-4]}.o") for src in _OTHER + _SEQ]

@@ -1,0 +1,1182 @@
+// Gated delta rule: forward and backward over chunks of 64 steps, and one-token step.
+//
+// Of a head's steps i in a chunk that starts from state S, with G_i the sum of g up to i,
+// D_ij = exp(G_i - G_j) for j <= i, and u_i = b_i (v_i - a_i S[i-1]^T k_i) the values that
+// are added,
+//
+//   (I + A) U = R,  A_ij = b_i D_ij k_i.k_j (j < i),  R_i = b_i (v_i - e^G_i S^T k_i)
+//   o_i = scale e^G_i S^T q_i + sum_j P_ij u_j,       P_ij = scale D_ij q_i.k_j (j <= i)
+//   S'  = e^G_63 S + sum_i e^(G_63 - G_i) k_i u_i^T
+//
+// and back, from dS' and do, with T = (I + A)^-1,
+//
+//   dU = P^T do + e^(G_63 - G) K dS',   dR = T^T dU,   dv = b dR
+//   dS = e^G_63 dS' + Q^T (scale e^G do) - K^T (b e^G dR)
+//   dq = scale e^G do S^T + E K,        E_ij = scale D_ij do_i.u_j (j <= i)
+//   dk = b X + Y,  X = F K - e^G dR S^T,  F_ij = -D_ij dR_i.u_j (j < i)
+//   Y = e^(G_63 - G) U dS'^T + E^T Q + (b F)^T K
+//   db_i = dR_i.v_i + k_i.X_i
+//   dg_t = sum over i >= t of (q_i.dq_i + b_i k_i.X_i - k_i.Y_i)
+//          + sum over all i of e^(G_63 - G_i) k_i.(dS' u_i) + e^G_63 <S, dS'>
+//
+// where E's diagonal, which has no decay, is left out of the products (its parts of the two sums
+// would cancel) and added to dq and dk at the end, and what dS' gives is summed over i < t.
+//
+// T and P are of a chunk alone and are computed for all chunks at once (local); the states go
+// chunk by chunk, 32 columns of v a block (scan, and back: back_scan, which leaves dR and dS');
+// the gradients of q, k, g and b are again of a chunk alone (back_local).
+//
+// Products are matrix instructions of 16 x 16.  In bf16 the inputs are operands as they are;
+// everything computed on the way is the sum of two bf16 values (to 2^-17), in two or three
+// products: states and their gradients are outputs in fp32, and rounded to one bf16 they
+// would be off by 2^-9.  In fp32 the fp32 instruction is used.
+#include "dendsn_block.h"
+#include "seq_common.h"
+
+namespace dendsn_seq {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kC = 64;          // steps of a chunk
+constexpr int kBv = 32;         // columns of v of a block of the scans
+constexpr int kThreads = 256;
+constexpr double kForget = -200.0;  // exp of it is 0 in fp32
+
+struct DeltaArgs {
+  const void *q, *k, *v, *g, *beta, *go;
+  const float *s0, *gs_last, *state_in;
+  const int32_t* lengths;
+  void *o, *gq, *gk, *gv, *gg, *gbeta;
+  float *s_last, *gs0;
+  float *ck_s, *ck_u;       // [batch][H][nc]: [KP][Vp], [64][Vp]
+  float *tm, *pm, *dec;     // [batch][H][nc]: [64][64] twice, [3][64]
+  float *dr, *ds;           // as ck_u and ck_s
+  float *part_q, *part_k;   // [T][batch][H][K] where heads are shared
+  int64_t q_t, q_b, q_h, k_t, k_b, k_h, v_t, v_b, v_h, g_t, g_b, g_h, beta_t, beta_b, beta_h, o_t, o_b, o_h;
+  int64_t go_t, go_b, go_h;
+  int32_t T, batch, H, Hk, K, V, nc, Vp;
+  float scale;
+};
+
+// ---------------------------------------------------------------------------
+// Operands.  A fragment is a lane's eight values of one row (or column): row
+// lane % 16, places 8 (lane / 16) to + 7 of 32 along the sum.
+// ---------------------------------------------------------------------------
+struct F32 { using IO = float; };
+struct B16 { using IO = bf16_t; };
+
+template <class M> struct Exact;  // of inputs
+template <class M> struct Both;   // of what was computed
+template <> struct Both<F32> { f32x8 v; };
+template <> struct Exact<F32> : Both<F32> {};
+template <> struct Exact<B16> { bf16x8 h; };
+template <> struct Both<B16> { bf16x8 h, l; };
+
+__device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(f32x4& c, const Exact<B16>& a, const Exact<B16>& b) { c = mfma(a.h, b.h, c); }
+__device__ __forceinline__ void mma(f32x4& c, const Exact<B16>& a, const Both<B16>& b) {
+  c = mfma(a.h, b.l, c);
+  c = mfma(a.h, b.h, c);
+}
+__device__ __forceinline__ void mma(f32x4& c, const Both<B16>& a, const Exact<B16>& b) {
+  c = mfma(a.l, b.h, c);
+  c = mfma(a.h, b.h, c);
+}
+__device__ __forceinline__ void mma(f32x4& c, const Both<B16>& a, const Both<B16>& b) {
+  c = mfma(a.l, b.h, c);
+  c = mfma(a.h, b.l, c);
+  c = mfma(a.h, b.h, c);
+}
+__device__ __forceinline__ void mma(f32x4& c, const Both<F32>& a, const Both<F32>& b) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
+}
+
+__device__ __forceinline__ void both_of(f32x8 x, Both<F32>& f) { f.v = x; }
+__device__ __forceinline__ void both_of(f32x8 x, Both<B16>& f) {
+  f.h = __builtin_convertvector(x, bf16x8);
+  f.l = __builtin_convertvector(x - __builtin_convertvector(f.h, f32x8), bf16x8);
+}
+
+// Eight places of a row from k0 on, zeros from K on and in rows that are not there.
+template <typename IO>
+__device__ __forceinline__ Pack<IO, 8> load8(const IO* row, int k0, int K, bool ok) {
+  Pack<IO, 8> r;
+  if (ok && k0 + 8 <= K) {
+    r = *reinterpret_cast<const Pack<IO, 8>*>(row + k0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.v[j] = ok && k0 + j < K ? row[k0 + j] : IO{};
+  }
+  return r;
+}
+__device__ __forceinline__ Exact<F32> exact_of(const Pack<float, 8>& p) {
+  Exact<F32> f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f.v[j] = p.v[j];
+  return f;
+}
+__device__ __forceinline__ Exact<B16> exact_of(const Pack<bf16_t, 8>& p) {
+  Exact<B16> f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) f.h[j] = __builtin_bit_cast(__bf16, p.v[j].bits);
+  return f;
+}
+template <class M>
+__device__ __forceinline__ Both<M> load_both(const float* p) {  // 16-byte aligned
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+  Both<M> f;
+  both_of(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), f);
+  return f;
+}
+
+// Matrices in LDS, rows along the sum; padded so that a fragment's rows start on other banks.
+template <class M, int ROWS, int COLS> struct Mat;  // of computed values
+template <int ROWS, int COLS> struct Mat<F32, ROWS, COLS> {
+  static constexpr int kLd = COLS + 4;
+  float v[ROWS * kLd];
+  __device__ __forceinline__ Both<F32> frag(int row, int col) const {
+    const int lane = threadIdx.x & 63;
+    return load_both<F32>(v + (row + lane % 16) * kLd + col + lane / 16 * 8);
+  }
+  __device__ __forceinline__ void put4(int row, int col, f32x4 x) { *reinterpret_cast<f32x4*>(v + row * kLd + col) = x; }
+  __device__ __forceinline__ void put(int row, int col, float x) { v[row * kLd + col] = x; }
+};
+template <int ROWS, int COLS> struct Mat<B16, ROWS, COLS> {
+  static constexpr int kLd = COLS + 8;
+  __bf16 h[ROWS * kLd], l[ROWS * kLd];
+  __device__ __forceinline__ Both<B16> frag(int row, int col) const {
+    const int lane = threadIdx.x & 63, at = (row + lane % 16) * kLd + col + lane / 16 * 8;
+    return Both<B16>{*reinterpret_cast<const bf16x8*>(h + at), *reinterpret_cast<const bf16x8*>(l + at)};
+  }
+  __device__ __forceinline__ void put4(int row, int col, f32x4 x) {
+    const bf16x4 a = __builtin_convertvector(x, bf16x4);
+    *reinterpret_cast<bf16x4*>(h + row * kLd + col) = a;
+    *reinterpret_cast<bf16x4*>(l + row * kLd + col) = __builtin_convertvector(x - __builtin_convertvector(a, f32x4), bf16x4);
+  }
+  __device__ __forceinline__ void put(int row, int col, float x) {
+    const __bf16 a = static_cast<__bf16>(x);
+    h[row * kLd + col] = a;
+    l[row * kLd + col] = static_cast<__bf16>(x - static_cast<float>(a));
+  }
+};
+template <class M, int ROWS, int COLS> struct MatX;  // of inputs
+template <int ROWS, int COLS> struct MatX<F32, ROWS, COLS> {
+  static constexpr int kLd = COLS + 4;
+  float v[ROWS * kLd];
+  __device__ __forceinline__ Exact<F32> frag(int row, int col) const {
+    const int lane = threadIdx.x & 63;
+    Exact<F32> f;
+    f.v = load_both<F32>(v + (row + lane % 16) * kLd + col + lane / 16 * 8).v;
+    return f;
+  }
+  __device__ __forceinline__ void put4(int row, int col, float a, float b, float c, float d) {
+    *reinterpret_cast<f32x4*>(v + row * kLd + col) = f32x4{a, b, c, d};
+  }
+  __device__ __forceinline__ f32x4 get4(int row, int col) const { return *reinterpret_cast<const f32x4*>(v + row * kLd + col); }
+};
+template <int ROWS, int COLS> struct MatX<B16, ROWS, COLS> {
+  static constexpr int kLd = COLS + 8;
+  __bf16 h[ROWS * kLd];
+  __device__ __forceinline__ Exact<B16> frag(int row, int col) const {
+    const int lane = threadIdx.x & 63;
+    return Exact<B16>{*reinterpret_cast<const bf16x8*>(h + (row + lane % 16) * kLd + col + lane / 16 * 8)};
+  }
+  __device__ __forceinline__ void put4(int row, int col, bf16_t a, bf16_t b, bf16_t c, bf16_t d) {
+    *reinterpret_cast<uint2*>(h + row * kLd + col) = uint2{a.bits | uint32_t(b.bits) << 16, c.bits | uint32_t(d.bits) << 16};
+  }
+  __device__ __forceinline__ f32x4 get4(int row, int col) const {
+    return __builtin_convertvector(*reinterpret_cast<const bf16x4*>(h + row * kLd + col), f32x4);
+  }
+};
+
+// dst[d][t] = rows[t][d]: COLS steps (n of which are there), D of ROWS places.
+template <class M, int ROWS>
+__device__ __forceinline__ void fill_turned(MatX<M, ROWS, kC>& dst, const typename M::IO* rows, int64_t stride, int n, int D) {
+  using IO = typename M::IO;
+  for (int u = threadIdx.x; u < 2 * ROWS; u += kThreads) {
+    const int t = u % 16 * 4, d = u / 16 * 8;
+    Pack<IO, 8> r[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) r[x] = load8(rows + (t + x) * stride, d, D, t + x < n);
+#pragma unroll
+    for (int y = 0; y < 8; ++y) dst.put4(d + y, t, r[0].v[y], r[1].v[y], r[2].v[y], r[3].v[y]);
+  }
+}
+
+__device__ __forceinline__ int length_of(const DeltaArgs& a, int b) {
+  if (!a.lengths) return a.T;
+  const int n = a.lengths[b];
+  return n < 0 ? 0 : n > a.T ? a.T : n;
+}
+
+// exp of a difference of sums, whose rounding to fp32 would be off by more than the result's.
+__device__ __forceinline__ float exp_of(double x) {
+  const float f = float(x), e = expf(f);
+  return fmaf(e, float(x - double(f)), e);
+}
+
+// G_i of lane i's step: sums of a chunk's logarithms, in 64 bits (their differences count).
+template <typename IO>
+__device__ __forceinline__ double chunk_sum(const DeltaArgs& a, int b, int h, int t0, int n) {
+  const int i = threadIdx.x & 63;
+  double G = 0.0;
+  if (i < n) {
+    G = double(widen(static_cast<const IO*>(a.g)[int64_t(t0 + i) * a.g_t + b * a.g_b + h * a.g_h]));
+    G = G < kForget ? kForget : G;  // (NaN stays)
+  }
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    const double up = __shfl_up(G, s);
+    if (i >= s) G += up;
+  }
+  return G;
+}
+
+// ---------------------------------------------------------------------------
+// local: T and P (BACK: turned) and the decays of one chunk, one wave each.
+// ---------------------------------------------------------------------------
+template <class M, int KP, bool BACK>
+__global__ __launch_bounds__(64) void delta_local_kernel(DeltaArgs a) {
+  using IO = typename M::IO;
+  constexpr int KS = KP / 32;
+  const int lane = threadIdx.x, c = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const int t0 = c * kC, n = min(length_of(a, b) - t0, kC);
+  if (n <= 0) return;
+  __shared__ double sg[kC];
+  __shared__ float sb[kC];
+  __shared__ __align__(16) float sa[kC][kC + 4];
+  const int64_t at = (int64_t(b) * a.H + h) * a.nc + c;
+  float* pm = a.pm + at * kC * kC;
+  {
+    const double G = chunk_sum<IO>(a, b, h, t0, n);
+    const double last = __shfl(G, 63);
+    const float beta = lane < n ? widen(static_cast<const IO*>(a.beta)[int64_t(t0 + lane) * a.beta_t + b * a.beta_b + h * a.beta_h]) : 0.0f;
+    float* dec = a.dec + at * 3 * kC;
+    dec[lane] = exp_of(G);
+    dec[kC + lane] = exp_of(last - G);
+    dec[2 * kC + lane] = beta;
+    sg[lane] = G;
+    sb[lane] = beta;
+  }
+  __syncthreads();
+  const int hk = h / (a.H / a.Hk), r = lane % 16, q4 = lane / 16;
+  const IO* kp = static_cast<const IO*>(a.k) + t0 * a.k_t + b * a.k_b + hk * a.k_h;
+  const IO* qp = static_cast<const IO*>(a.q) + t0 * a.q_t + b * a.q_b + hk * a.q_h;
+  Exact<M> kf[4][KS];
+#pragma unroll
+  for (int bi = 0; bi < 4; ++bi) {
+    const int row = bi * 16 + r;
+    Exact<M> qf[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      kf[bi][s] = exact_of(load8(kp + row * a.k_t, s * 32 + q4 * 8, a.K, row < n));
+      qf[s] = exact_of(load8(qp + row * a.q_t, s * 32 + q4 * 8, a.K, row < n));
+    }
+#pragma unroll
+    for (int bj = 0; bj < 4; ++bj) {
+      f32x4 kk = {0, 0, 0, 0}, qk = {0, 0, 0, 0};
+      if (bj <= bi) {
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          mma(kk, kf[bi][s], kf[bj][s]);
+          mma(qk, qf[s], kf[bj][s]);
+        }
+      }
+      const int j = bj * 16 + r, i0 = bi * 16 + q4 * 4;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int i = i0 + x;
+        const float d = j <= i ? exp_of(sg[i] - sg[j]) : 0.0f;
+        sa[i][j] = j < i ? sb[i] * d * kk[x] : 0.0f;
+        qk[x] = j <= i ? a.scale * d * qk[x] : 0.0f;
+      }
+      if (BACK) {
+        *reinterpret_cast<f32x4*>(pm + j * kC + i0) = qk;
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) pm[(i0 + x) * kC + j] = qk[x];
+      }
+    }
+  }
+  __syncthreads();
+  // column `lane` of T, row by row
+  float t[kC];
+#pragma unroll
+  for (int i = 0; i < kC; ++i) {
+    float s = i == lane ? 1.0f : 0.0f;
+#pragma unroll
+    for (int j = 0; j < i; ++j) s = fmaf(-sa[i][j], t[j], s);
+    t[i] = s;
+  }
+  float* tm = a.tm + at * kC * kC;
+#pragma unroll
+  for (int i = 0; i < kC; i += 4) {
+    if (BACK) {
+      *reinterpret_cast<f32x4*>(tm + lane * kC + i) = f32x4{t[i], t[i + 1], t[i + 2], t[i + 3]};
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) tm[(i + x) * kC + lane] = t[i + x];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// scan: states and outputs, chunk after chunk.  Wave w has steps 16 w to + 15 of
+// the products over steps, and an eighth (K of 128) or so of the state's rows.
+// ---------------------------------------------------------------------------
+template <class M, int KP>
+struct ScanLds {
+  MatX<M, KP, kC> kt;
+  Mat<M, kBv, KP> st;
+  Mat<M, kBv, kC> rt, ut, us;
+};
+
+template <class M, int KP>
+__global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
+  using IO = typename M::IO;
+  constexpr int KS = KP / 32, MT = KP / 64;  // MT: row tiles of the state of a wave
+  extern __shared__ __align__(16) char lds[];
+  ScanLds<M, KP>& s = *reinterpret_cast<ScanLds<M, KP>*>(lds);
+  const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
+  const int v0 = blockIdx.x * kBv, h = blockIdx.y, b = blockIdx.z, hk = h / (a.H / a.Hk);
+  const int len = length_of(a, b), chunks = (len + kC - 1) / kC;
+  const int64_t bh = int64_t(b) * a.H + h;
+  const IO* kb = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
+  const IO* qb = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h;
+  const IO* vb = static_cast<const IO*>(a.v) + b * a.v_b + h * a.v_h;
+  IO* ob = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h;
+
+  // the state: rows 16 (MT w + m) + 4 q4 + x, columns 16 nt + r
+  f32x4 S[MT][2];
+  auto state_at = [&](int m, int nt, int x) { return (bh * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
+  auto state_in = [&](int m, int nt, int x) { return (MT * w + m) * 16 + q4 * 4 + x < a.K && v0 + nt * 16 + r < a.V; };
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) S[m][nt][x] = a.s0 && state_in(m, nt, x) ? a.s0[state_at(m, nt, x)] : 0.0f;
+
+  for (int c = 0; c < chunks; ++c) {
+    const int t0 = c * kC, n = min(len - t0, kC), row = 16 * w + r, i0 = 16 * w + q4 * 4;
+    const int64_t at = bh * a.nc + c;
+    const float* dec = a.dec + at * 3 * kC;
+    __syncthreads();  // the chunk before is read
+    fill_turned<M, KP>(s.kt, kb + t0 * a.k_t, a.k_t, n, a.K);
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
+        if (a.ck_s) {
+          float* to = a.ck_s + (at * KP + (MT * w + m) * 16 + q4 * 4) * a.Vp + v0 + nt * 16 + r;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = S[m][nt][x];
+        }
+      }
+    Exact<M> kf[KS], qf[KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      kf[k] = exact_of(load8(kb + (t0 + row) * a.k_t, k * 32 + q4 * 8, a.K, row < n));
+      qf[k] = exact_of(load8(qb + (t0 + row) * a.q_t, k * 32 + q4 * 8, a.K, row < n));
+    }
+    Both<M> tf[2], pf[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      tf[k] = load_both<M>(a.tm + at * kC * kC + row * kC + k * 32 + q4 * 8);
+      pf[k] = load_both<M>(a.pm + at * kC * kC + row * kC + k * 32 + q4 * 8);
+    }
+    const f32x4 eg = *reinterpret_cast<const f32x4*>(dec + i0), tail = *reinterpret_cast<const f32x4*>(dec + kC + i0),
+                beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
+    const float whole = dec[kC - 1];
+    float vv[2][4];
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        vv[nt][x] = i0 + x < n && v0 + nt * 16 + r < a.V ? widen(vb[(t0 + i0 + x) * a.v_t + v0 + nt * 16 + r]) : 0.0f;
+    __syncthreads();
+    f32x4 o[2];
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      f32x4 ks = {0, 0, 0, 0}, qs = {0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        const Both<M> f = s.st.frag(nt * 16, k * 32);
+        mma(ks, kf[k], f);
+        mma(qs, qf[k], f);
+      }
+      f32x4 R;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        R[x] = beta[x] * (vv[nt][x] - eg[x] * ks[x]);
+        o[nt][x] = a.scale * eg[x] * qs[x];
+      }
+      s.rt.put4(nt * 16 + r, i0, R);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      f32x4 U = {0, 0, 0, 0};
+      mma(U, tf[0], s.rt.frag(nt * 16, 0));
+      if (w >= 2) mma(U, tf[1], s.rt.frag(nt * 16, 32));  // T is lower
+      s.ut.put4(nt * 16 + r, i0, U);
+      s.us.put4(nt * 16 + r, i0, tail * U);
+      if (a.ck_u) {
+        float* to = a.ck_u + (at * kC + i0) * a.Vp + v0 + nt * 16 + r;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = U[x];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      mma(o[nt], pf[0], s.ut.frag(nt * 16, 0));
+      if (w >= 2) mma(o[nt], pf[1], s.ut.frag(nt * 16, 32));
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (i0 + x < n && v0 + nt * 16 + r < a.V) ob[(t0 + i0 + x) * a.o_t + v0 + nt * 16 + r] = narrow<IO>(o[nt][x]);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        S[m][nt] *= whole;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) mma(S[m][nt], s.kt.frag((MT * w + m) * 16, k * 32), s.us.frag(nt * 16, k * 32));
+      }
+    }
+  }
+  if (a.s_last) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (state_in(m, nt, x)) a.s_last[state_at(m, nt, x)] = S[m][nt][x];
+  }
+  for (int u = threadIdx.x; u < a.T - len; u += kThreads)  // steps past the end
+    for (int d = v0; d < min(v0 + kBv, a.V); ++d) ob[int64_t(len + u) * a.o_t + d] = IO{};
+}
+
+// ---------------------------------------------------------------------------
+// back_scan: the states' gradients, from the last chunk down; dR, dv.
+// ---------------------------------------------------------------------------
+template <class M, int KP>
+struct BackLds {
+  MatX<M, KP, kC> kt, qt;
+  MatX<M, kBv, kC> ot;
+  Mat<M, kBv, KP> st;
+  Mat<M, kBv, kC> os, ut, rt;
+};
+
+template <class M, int KP>
+__global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) {
+  using IO = typename M::IO;
+  constexpr int KS = KP / 32, MT = KP / 64;
+  extern __shared__ __align__(16) char lds[];
+  BackLds<M, KP>& s = *reinterpret_cast<BackLds<M, KP>*>(lds);
+  const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
+  const int v0 = blockIdx.x * kBv, h = blockIdx.y, b = blockIdx.z, hk = h / (a.H / a.Hk);
+  const int len = length_of(a, b), chunks = (len + kC - 1) / kC;
+  const int64_t bh = int64_t(b) * a.H + h;
+  const IO* kb = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
+  const IO* qb = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h;
+  const IO* gob = static_cast<const IO*>(a.go) + b * a.go_b + h * a.go_h;
+  IO* gvb = static_cast<IO*>(a.gv) + bh * a.V;
+  const int64_t gv_t = int64_t(a.batch) * a.H * a.V;
+
+  f32x4 S[MT][2];  // dS'
+  auto state_at = [&](int m, int nt, int x) { return (bh * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
+  auto state_in = [&](int m, int nt, int x) { return (MT * w + m) * 16 + q4 * 4 + x < a.K && v0 + nt * 16 + r < a.V; };
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) S[m][nt][x] = a.gs_last && state_in(m, nt, x) ? a.gs_last[state_at(m, nt, x)] : 0.0f;
+
+  for (int c = chunks - 1; c >= 0; --c) {
+    const int t0 = c * kC, n = min(len - t0, kC), row = 16 * w + r, i0 = 16 * w + q4 * 4;
+    const int64_t at = bh * a.nc + c;
+    const float* dec = a.dec + at * 3 * kC;
+    const f32x4 eg = *reinterpret_cast<const f32x4*>(dec + i0), tail = *reinterpret_cast<const f32x4*>(dec + kC + i0),
+                beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
+    const float whole = dec[kC - 1];
+    __syncthreads();
+    fill_turned<M, KP>(s.kt, kb + t0 * a.k_t, a.k_t, n, a.K);
+    fill_turned<M, KP>(s.qt, qb + t0 * a.q_t, a.q_t, n, a.K);
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      IO go[4];
+      f32x4 os;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        go[x] = i0 + x < n && v0 + nt * 16 + r < a.V ? gob[(t0 + i0 + x) * a.go_t + v0 + nt * 16 + r] : IO{};
+        os[x] = a.scale * eg[x] * widen(go[x]);
+      }
+      s.ot.put4(nt * 16 + r, i0, go[0], go[1], go[2], go[3]);
+      s.os.put4(nt * 16 + r, i0, os);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
+        float* to = a.ds + (at * KP + (MT * w + m) * 16 + q4 * 4) * a.Vp + v0 + nt * 16 + r;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = S[m][nt][x];
+      }
+    Exact<M> kf[KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) kf[k] = exact_of(load8(kb + (t0 + row) * a.k_t, k * 32 + q4 * 8, a.K, row < n));
+    Both<M> tf[2], pf[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      tf[k] = load_both<M>(a.tm + at * kC * kC + row * kC + k * 32 + q4 * 8);
+      pf[k] = load_both<M>(a.pm + at * kC * kC + row * kC + k * 32 + q4 * 8);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      f32x4 U = {0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) mma(U, kf[k], s.st.frag(nt * 16, k * 32));
+      U *= tail;
+      if (w < 2) mma(U, pf[0], s.ot.frag(nt * 16, 0));  // P turned is upper
+      mma(U, pf[1], s.ot.frag(nt * 16, 32));
+      s.ut.put4(nt * 16 + r, i0, U);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt) {
+      f32x4 R = {0, 0, 0, 0}, rs;
+      if (w < 2) mma(R, tf[0], s.ut.frag(nt * 16, 0));
+      mma(R, tf[1], s.ut.frag(nt * 16, 32));
+      float* to = a.dr + (at * kC + i0) * a.Vp + v0 + nt * 16 + r;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        to[int64_t(x) * a.Vp] = R[x];
+        const float dv = beta[x] * R[x];
+        rs[x] = -eg[x] * dv;
+        if (i0 + x < n && v0 + nt * 16 + r < a.V) gvb[(t0 + i0 + x) * gv_t + v0 + nt * 16 + r] = narrow<IO>(dv);
+      }
+      s.rt.put4(nt * 16 + r, i0, rs);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        S[m][nt] *= whole;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          mma(S[m][nt], s.qt.frag((MT * w + m) * 16, k * 32), s.os.frag(nt * 16, k * 32));
+          mma(S[m][nt], s.kt.frag((MT * w + m) * 16, k * 32), s.rt.frag(nt * 16, k * 32));
+        }
+      }
+  }
+  if (a.gs0) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (state_in(m, nt, x)) a.gs0[state_at(m, nt, x)] = S[m][nt][x];
+  }
+  for (int u = threadIdx.x; u < a.T - len; u += kThreads)
+    for (int d = v0; d < min(v0 + kBv, a.V); ++d) gvb[(len + u) * gv_t + d] = IO{};
+}
+
+// ---------------------------------------------------------------------------
+// back_local: gradients of q, k, g and beta of one chunk.
+// ---------------------------------------------------------------------------
+template <class M, int KP>
+struct LocalLds {
+  MatX<M, KP, kC> kt, qt;
+  union {
+    struct {
+      Mat<M, KP, kBv> s0, ds;
+      Mat<M, kC, kBv> u;
+    } a;
+    struct {
+      Mat<M, kC, kC> e, et, f, ft;
+    } b;
+  };
+  double g[kC];
+  float dg[kC], rv[kC], kd[kC], diag[kC], part[4];
+};
+
+template <class M, int KP>
+__global__ __launch_bounds__(kThreads) void delta_back_local_kernel(DeltaArgs a) {
+  using IO = typename M::IO;
+  constexpr int NT = KP / 16;
+  extern __shared__ __align__(16) char lds[];
+  LocalLds<M, KP>& s = *reinterpret_cast<LocalLds<M, KP>*>(lds);
+  const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
+  const int c = blockIdx.x, h = blockIdx.y, b = blockIdx.z, share = a.H / a.Hk, hk = h / share;
+  const int len = length_of(a, b), t0 = c * kC, n = min(len - t0, kC), there = min(a.T - t0, kC);
+  const int64_t bh = int64_t(b) * a.H + h, at = bh * a.nc + c;
+  // gradients are contiguous; those of shared heads are summed by a kernel of their own
+  float* part_q = share > 1 ? a.part_q + (t0 * int64_t(a.batch) * a.H + bh) * a.K : nullptr;
+  float* part_k = share > 1 ? a.part_k + (t0 * int64_t(a.batch) * a.H + bh) * a.K : nullptr;
+  const int64_t tk = int64_t(a.batch) * a.Hk, th = int64_t(a.batch) * a.H;
+  IO* gq = static_cast<IO*>(a.gq) + (t0 * tk + int64_t(b) * a.Hk + hk) * a.K;
+  IO* gk = static_cast<IO*>(a.gk) + (t0 * tk + int64_t(b) * a.Hk + hk) * a.K;
+  IO* gg = static_cast<IO*>(a.gg) + t0 * th + bh;
+  IO* gbeta = static_cast<IO*>(a.gbeta) + t0 * th + bh;
+  auto put_qk = [&](int i, int d, float q, float k) {
+    if (share > 1) {
+      part_q[i * th * a.K + d] = q;
+      part_k[i * th * a.K + d] = k;
+    } else {
+      gq[i * tk * a.K + d] = narrow<IO>(q);
+      gk[i * tk * a.K + d] = narrow<IO>(k);
+    }
+  };
+  // steps past the end
+  for (int u = threadIdx.x + max(n, 0) * a.K; u < there * a.K; u += kThreads) put_qk(u / a.K, u % a.K, 0.0f, 0.0f);
+  for (int i = threadIdx.x + max(n, 0); i < there; i += kThreads) gg[i * th] = gbeta[i * th] = IO{};
+  if (n <= 0) return;
+
+  const IO* kb = static_cast<const IO*>(a.k) + t0 * a.k_t + b * a.k_b + hk * a.k_h;
+  const IO* qb = static_cast<const IO*>(a.q) + t0 * a.q_t + b * a.q_b + hk * a.q_h;
+  const IO* vb = static_cast<const IO*>(a.v) + t0 * a.v_t + b * a.v_b + h * a.v_h;
+  const IO* gob = static_cast<const IO*>(a.go) + t0 * a.go_t + b * a.go_b + h * a.go_h;
+  const float *ck_s = a.ck_s + at * KP * a.Vp, *ds = a.ds + at * KP * a.Vp, *ck_u = a.ck_u + at * kC * a.Vp, *dr = a.dr + at * kC * a.Vp;
+  const float* dec = a.dec + at * 3 * kC;
+  const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
+  const float whole = dec[kC - 1];
+
+  const double G = chunk_sum<IO>(a, b, h, t0, n);
+  if (w == 0) s.g[lane] = G;
+  fill_turned<M, KP>(s.kt, kb, a.k_t, n, a.K);
+  fill_turned<M, KP>(s.qt, qb, a.q_t, n, a.K);
+
+  f32x4 dq[NT], X[NT], Y[NT], e[4], f[4];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) dq[t] = X[t] = Y[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+  for (int t = 0; t < 4; ++t) e[t] = f[t] = f32x4{0, 0, 0, 0};
+  float rv = 0.0f, sds = 0.0f;  // dR.v of row `row` (a quarter of it), <S, dS'>
+  for (int v0 = 0; v0 < a.Vp; v0 += kBv) {
+    __syncthreads();
+    for (int u = threadIdx.x; u < KP * kBv / 4; u += kThreads) {
+      const int d = u / (kBv / 4), v = u % (kBv / 4) * 4;
+      const f32x4 x = *reinterpret_cast<const f32x4*>(ck_s + int64_t(d) * a.Vp + v0 + v);
+      const f32x4 y = *reinterpret_cast<const f32x4*>(ds + int64_t(d) * a.Vp + v0 + v);
+      sds += (x[0] * y[0] + x[1] * y[1]) + (x[2] * y[2] + x[3] * y[3]);
+      s.a.s0.put4(d, v, x);
+      s.a.ds.put4(d, v, y);
+    }
+    for (int u = threadIdx.x; u < kC * kBv / 4; u += kThreads) {
+      const int i = u / (kBv / 4), v = u % (kBv / 4) * 4;
+      s.a.u.put4(i, v, *reinterpret_cast<const f32x4*>(ck_u + int64_t(i) * a.Vp + v0 + v));
+    }
+    const Exact<M> of = exact_of(load8(gob + row * a.go_t, v0 + q4 * 8, a.V, row < n));
+    const Pack<IO, 8> vp = load8(vb + row * a.v_t, v0 + q4 * 8, a.V, row < n);
+    const float* drp = dr + int64_t(row) * a.Vp + v0 + q4 * 8;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) rv = fmaf(drp[j], widen(vp.v[j]), rv);
+    const Both<M> rf = load_both<M>(drp);
+    __syncthreads();
+    const Both<M> uf = s.a.u.frag(16 * w, 0);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const Both<M> sf = s.a.s0.frag(t * 16, 0);
+      mma(dq[t], of, sf);
+      mma(X[t], rf, sf);
+      mma(Y[t], uf, s.a.ds.frag(t * 16, 0));
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if (t <= w) {
+        const Both<M> u2 = s.a.u.frag(t * 16, 0);
+        mma(e[t], of, u2);
+        mma(f[t], rf, u2);
+      }
+    }
+  }
+  rv += __shfl_xor(rv, 16);
+  rv += __shfl_xor(rv, 32);
+  if (q4 == 0) s.rv[row] = rv;
+#pragma unroll
+  for (int x = 32; x > 0; x /= 2) sds += __shfl_xor(sds, x);
+  const f32x4 eg = *reinterpret_cast<const f32x4*>(dec + i0), tail = *reinterpret_cast<const f32x4*>(dec + kC + i0),
+              beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
+  __syncthreads();
+  f32x4 kd = {0, 0, 0, 0}, Y2[NT];  // k.Y of dS' alone; the rest of Y
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    dq[t] *= a.scale * eg;
+    X[t] *= -eg;
+    Y[t] *= tail;
+    Y2[t] = f32x4{0, 0, 0, 0};
+    kd += s.kt.get4(t * 16 + r, i0) * Y[t];
+  }
+  if (lane == 0) s.part[w] = whole * sds;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int j = 16 * t + r;
+    f32x4 fb;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int i = i0 + x;
+      const float d = j < i ? exp_of(s.g[i] - s.g[j]) : 0.0f;
+      if (i == j) s.diag[i] = a.scale * e[t][x];
+      e[t][x] = j < i ? a.scale * d * e[t][x] : 0.0f;
+      f[t][x] = j < i ? -d * f[t][x] : 0.0f;
+      fb[x] = beta[x] * f[t][x];
+      s.b.e.put(i, j, e[t][x]);
+      s.b.f.put(i, j, f[t][x]);
+    }
+    s.b.et.put4(j, i0, e[t]);
+    s.b.ft.put4(j, i0, fb);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const Both<M> ef = s.b.e.frag(16 * w, k * 32), etf = s.b.et.frag(16 * w, k * 32), ff = s.b.f.frag(16 * w, k * 32),
+                  ftf = s.b.ft.frag(16 * w, k * 32);
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const Exact<M> kf = s.kt.frag(t * 16, k * 32);
+      mma(dq[t], ef, kf);
+      mma(X[t], ff, kf);
+      mma(Y2[t], ftf, kf);
+      mma(Y2[t], etf, s.qt.frag(t * 16, k * 32));
+    }
+  }
+  const f32x4 diag = *reinterpret_cast<const f32x4*>(s.diag + i0);
+  f32x4 dg = {0, 0, 0, 0}, kx = {0, 0, 0, 0};
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const f32x4 k = s.kt.get4(t * 16 + r, i0), q = s.qt.get4(t * 16 + r, i0);
+    dg += q * dq[t] - k * Y2[t];
+    kx += k * X[t];
+    const f32x4 gqv = dq[t] + diag * k, gkv = (beta * X[t] + Y[t]) + (Y2[t] + diag * q);
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (i0 + x < n && t * 16 + r < a.K) put_qk(i0 + x, t * 16 + r, gqv[x], gkv[x]);
+  }
+  dg += beta * kx;
+#pragma unroll
+  for (int m = 8; m > 0; m /= 2)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      dg[x] += __shfl_xor(dg[x], m);
+      kx[x] += __shfl_xor(kx[x], m);
+      kd[x] += __shfl_xor(kd[x], m);
+    }
+  if (r == 0) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      s.dg[i0 + x] = dg[x];
+      s.kd[i0 + x] = kd[x];
+      if (i0 + x < n) gbeta[(i0 + x) * th] = narrow<IO>(s.rv[i0 + x] + kx[x]);
+    }
+  }
+  __syncthreads();
+  if (w == 0) {
+    // sums from the last step down and from the first up, in 64 bits: terms cancel
+    double after = s.dg[lane], upto = s.kd[lane];
+    const double own = upto;
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) {
+      const double down = __shfl_down(after, x), up = __shfl_up(upto, x);
+      if (lane + x < 64) after += down;
+      if (lane >= x) upto += up;
+    }
+    const double held = (double(s.part[0]) + double(s.part[1])) + (double(s.part[2]) + double(s.part[3]));
+    if (lane < n) gg[lane * th] = narrow<IO>(float(after + (upto - own) + held));
+  }
+}
+
+// Gradients of heads of q and k that several heads of v share.
+template <typename IO>
+__global__ __launch_bounds__(256) void delta_join_kernel(const float* pq, const float* pk, IO* gq, IO* gk, int64_t rows, int K, int share) {
+  for (int64_t u = int64_t(blockIdx.x) * 256 + threadIdx.x; u < rows * K; u += int64_t(gridDim.x) * 256) {
+    const int64_t row = u / K, from = (row * share) * K + u % K;
+    float q = 0.0f, k = 0.0f;
+    for (int s = 0; s < share; ++s) {
+      q += pq[from + int64_t(s) * K];
+      k += pk[from + int64_t(s) * K];
+    }
+    gq[u] = narrow<IO>(q);
+    gk[u] = narrow<IO>(k);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// One token.  S^T k and S^T q come from one pass over the state, in registers:
+// o = scale (a S^T q + (q.k) u).  Bound by the state's bytes.
+// ---------------------------------------------------------------------------
+struct DeltaStepArgs {
+  const void *q, *k, *v, *g, *beta;
+  const int32_t* slots;
+  float* state;
+  void* o;
+  int64_t q_b, q_h, k_b, k_h, v_b, v_h, g_b, g_h, beta_b, beta_h, o_b, o_h, n_slots;
+  int32_t H, share, K, V;
+  float scale;
+};
+
+template <typename IO>
+__global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaStepArgs a) {
+  const int h = blockIdx.y, b = blockIdx.z, hk = h / a.share;
+  const int vl = threadIdx.x % 8 * 4, kl = threadIdx.x / 8, v = blockIdx.x * kBv + vl;
+  const int left = a.V - v;  // columns from this lane's first on
+  IO* op = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h + v;
+  const int64_t slot = a.slots ? a.slots[b] : b;
+  if (slot < 0 || slot >= a.n_slots) {
+    if (kl == 0)
+      for (int x = 0; x < 4; ++x)
+        if (x < left) op[x] = IO{};
+    return;
+  }
+  float* S = a.state + ((slot * a.H + h) * a.K) * a.V + v;
+  const IO* qp = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h;
+  const IO* kp = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
+  const float gl = widen(static_cast<const IO*>(a.g)[b * a.g_b + h * a.g_h]);
+  const float decay = expf(gl < float(kForget) ? float(kForget) : gl), beta = widen(static_cast<const IO*>(a.beta)[b * a.beta_b + h * a.beta_h]);
+  float s[4][4], kk[4];
+  float sk[4] = {0, 0, 0, 0}, sq[4] = {0, 0, 0, 0}, qk = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int d = kl + 32 * i;
+    const bool ok = d < a.K;
+    kk[i] = ok ? widen(kp[d]) : 0.0f;
+    const float q = ok ? widen(qp[d]) : 0.0f;
+    if (ok && left >= 4) {
+      const Pack<float, 4> p = *reinterpret_cast<const Pack<float, 4>*>(S + int64_t(d) * a.V);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) s[i][x] = p.v[x];
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) s[i][x] = ok && x < left ? S[int64_t(d) * a.V + x] : 0.0f;
+    }
+    qk = fmaf(q, kk[i], qk);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      s[i][x] *= decay;
+      sk[x] = fmaf(kk[i], s[i][x], sk[x]);
+      sq[x] = fmaf(q, s[i][x], sq[x]);
+    }
+  }
+#pragma unroll
+  for (int m = 8; m < 64; m *= 2) {
+    qk += __shfl_xor(qk, m);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      sk[x] += __shfl_xor(sk[x], m);
+      sq[x] += __shfl_xor(sq[x], m);
+    }
+  }
+  __shared__ float red[4][8][9];
+  const int w = threadIdx.x / 64, j = threadIdx.x % 8;
+  if ((threadIdx.x & 63) < 8) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      red[w][j][x] = sk[x];
+      red[w][j][4 + x] = sq[x];
+    }
+    red[w][j][8] = qk;
+  }
+  __syncthreads();
+  qk = (red[0][j][8] + red[1][j][8]) + (red[2][j][8] + red[3][j][8]);
+  const IO* vp = static_cast<const IO*>(a.v) + b * a.v_b + h * a.v_h + v;
+  float u[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    sk[x] = (red[0][j][x] + red[1][j][x]) + (red[2][j][x] + red[3][j][x]);
+    sq[x] = (red[0][j][4 + x] + red[1][j][4 + x]) + (red[2][j][4 + x] + red[3][j][4 + x]);
+    u[x] = x < left ? beta * (widen(vp[x]) - sk[x]) : 0.0f;
+    if (kl == 0 && x < left) op[x] = narrow<IO>(a.scale * fmaf(qk, u[x], sq[x]));
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int d = kl + 32 * i;
+    if (d >= a.K) continue;
+    Pack<float, 4> p;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) p.v[x] = fmaf(kk[i], u[x], s[i][x]);
+    if (left >= 4) {
+      *reinterpret_cast<Pack<float, 4>*>(S + int64_t(d) * a.V) = p;
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (x < left) S[int64_t(d) * a.V + x] = p.v[x];
+    }
+  }
+}
+
+__global__ __launch_bounds__(256) void delta_copy_kernel(const float* from, float* to, int64_t n) {
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256) to[i] = from ? from[i] : 0.0f;
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+bool empty(const dendsn_delta_cfg* c) { return c->T == 0 || c->batch == 0 || c->H == 0; }
+int64_t states(const dendsn_delta_cfg* c) { return c->batch * c->H * c->K * c->V; }
+int kp_of(const dendsn_delta_cfg* c) { return c->K <= 64 ? 64 : 128; }
+
+bool strides_fit(const dendsn_delta_cfg* c, int64_t t, int64_t b, int64_t h) {
+  return t >= 0 && b >= 0 && h >= 0 && small_product(c->T, t) && small_product(c->batch, b) && small_product(c->H, h);
+}
+
+dendsn_status check_cfg(const dendsn_delta_cfg* c) {
+  if (!c) return fail(DENDSN_E_INVALID, "cfg is NULL");
+  if (c->T < 0 || c->T > (int64_t(1) << 24)) return fail(DENDSN_E_INVALID, "T must be in [0, 2^24]");
+  if (c->batch < 0 || c->batch > 65535) return fail(DENDSN_E_INVALID, "batch must be in [0, 65535]");
+  if (c->H < 0 || c->H > 65535) return fail(DENDSN_E_INVALID, "H must be in [0, 65535]");
+  if (c->Hk < 1 || c->H % c->Hk) return fail(DENDSN_E_INVALID, "H must be a multiple of Hk >= 1");
+  if (c->K < 1 || c->V < 1 || c->V > 65536) return fail(DENDSN_E_INVALID, "K or V out of range");
+  if (c->K > 128) return fail(DENDSN_E_UNSUPPORTED, "K must be <= 128");
+  if (c->io != DENDSN_IO_F32 && c->io != DENDSN_IO_BF16) return fail(DENDSN_E_INVALID, "bad io");
+  if (!isfinite(c->scale)) return fail(DENDSN_E_INVALID, "scale must be finite");
+  // a chunk's states and the padding of V
+  if (!small_product(c->batch * c->H * 128, round_up(c->T + kC, kC)) ||
+      !small_product(c->batch * c->H * 128 * round_up(c->T + kC, kC) / kC * 4, round_up(c->V, kBv)))
+    return fail(DENDSN_E_INVALID, "T * batch * H * V too large");
+  const int64_t s[21] = {c->q_t, c->q_b, c->q_h, c->k_t, c->k_b, c->k_h, c->v_t, c->v_b, c->v_h, c->g_t, c->g_b, c->g_h,
+                         c->beta_t, c->beta_b, c->beta_h, c->o_t, c->o_b, c->o_h, c->grad_o_t, c->grad_o_b, c->grad_o_h};
+  for (int i = 0; i < 21; i += 3)
+    if (!strides_fit(c, s[i], s[i + 1], s[i + 2])) return fail(DENDSN_E_INVALID, "a stride is negative or too large");
+  return DENDSN_OK;
+}
+
+// Whether the rows [V] of an output at these strides lie apart: taken from the nearest to
+// the farthest, each dimension steps over all that the nearer ones span.
+bool rows_apart(const dendsn_delta_cfg* c, int64_t t, int64_t b, int64_t h) {
+  int64_t n[3] = {c->T, c->batch, c->H}, s[3] = {t, b, h}, span = c->V;
+  for (int pass = 0; pass < 3; ++pass) {
+    int least = -1;
+    for (int i = 0; i < 3; ++i)
+      if (n[i] > 1 && (least < 0 || s[i] < s[least])) least = i;
+    if (least < 0) break;
+    if (s[least] < span) return false;
+    span += s[least] * (n[least] - 1);
+    n[least] = 1;
+  }
+  return true;
+}
+
+struct DeltaPlan {
+  int64_t nc, items, Vp;
+  int KP;
+  size_t ck_u, ckpt;                               // offset of the values, whole size
+  size_t tm, pm, dec, dr, ds, part_q, part_k;      // of the scratch
+  size_t forward, backward;
+};
+
+DeltaPlan make_plan(const dendsn_delta_cfg* c) {
+  DeltaPlan p{};
+  if (empty(c)) return p;
+  p.nc = ceil_div(c->T, kC);
+  p.items = p.nc * c->batch * c->H;
+  p.Vp = round_up(c->V, kBv);
+  p.KP = kp_of(c);
+  Carve k;
+  k.take(size_t(p.items) * p.KP * p.Vp * 4);
+  p.ck_u = k.take(size_t(p.items) * kC * p.Vp * 4);
+  p.ckpt = k.at;
+  Carve w;
+  p.tm = w.take(size_t(p.items) * kC * kC * 4);
+  p.pm = w.take(size_t(p.items) * kC * kC * 4);
+  p.dec = w.take(size_t(p.items) * 3 * kC * 4);
+  p.forward = w.at;
+  p.dr = w.take(size_t(p.items) * kC * p.Vp * 4);
+  p.ds = w.take(size_t(p.items) * p.KP * p.Vp * 4);
+  if (c->H != c->Hk) {
+    p.part_q = w.take(size_t(c->T) * c->batch * c->H * c->K * 4);
+    p.part_k = w.take(size_t(c->T) * c->batch * c->H * c->K * 4);
+  }
+  p.backward = w.at;
+  return p;
+}
+
+void fill_args(const dendsn_delta_cfg* c, const DeltaPlan& p, void* workspace, DeltaArgs& a) {
+  a.q_t = c->q_t; a.q_b = c->q_b; a.q_h = c->q_h; a.k_t = c->k_t; a.k_b = c->k_b; a.k_h = c->k_h;
+  a.v_t = c->v_t; a.v_b = c->v_b; a.v_h = c->v_h; a.g_t = c->g_t; a.g_b = c->g_b; a.g_h = c->g_h;
+  a.beta_t = c->beta_t; a.beta_b = c->beta_b; a.beta_h = c->beta_h; a.o_t = c->o_t; a.o_b = c->o_b; a.o_h = c->o_h;
+  a.go_t = c->grad_o_t; a.go_b = c->grad_o_b; a.go_h = c->grad_o_h;
+  a.T = int32_t(c->T); a.batch = int32_t(c->batch); a.H = int32_t(c->H); a.Hk = int32_t(c->Hk);
+  a.K = int32_t(c->K); a.V = int32_t(c->V); a.nc = int32_t(p.nc); a.Vp = int32_t(p.Vp); a.scale = c->scale;
+  char* w = static_cast<char*>(workspace);
+  a.tm = reinterpret_cast<float*>(w + p.tm);
+  a.pm = reinterpret_cast<float*>(w + p.pm);
+  a.dec = reinterpret_cast<float*>(w + p.dec);
+  a.dr = reinterpret_cast<float*>(w + p.dr);
+  a.ds = reinterpret_cast<float*>(w + p.ds);
+  a.part_q = reinterpret_cast<float*>(w + p.part_q);
+  a.part_k = reinterpret_cast<float*>(w + p.part_k);
+}
+
+// A kernel whose LDS passes the default limit has to be told once a device; the call is cheap.
+template <typename F>
+bool allow_lds(F* kernel, size_t bytes) {
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) == hipSuccess;
+}
+
+template <class M, int KP>
+dendsn_status launch_forward(const DeltaArgs& a, hipStream_t stream) {
+  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / kBv), unsigned(a.H), unsigned(a.batch));
+  constexpr size_t bytes = sizeof(ScanLds<M, KP>);
+  static_assert(bytes <= 160 * 1024, "LDS of a CU");
+  if (!allow_lds(delta_scan_kernel<M, KP>, bytes)) return fail(DENDSN_E_HIP, "delta forward: %zu bytes of LDS refused", bytes);
+  delta_local_kernel<M, KP, false><<<heads, dim3(64), 0, stream>>>(a);
+  delta_scan_kernel<M, KP><<<cols, dim3(kThreads), bytes, stream>>>(a);
+  return launched("delta forward");
+}
+
+template <class M, int KP>
+dendsn_status launch_backward(const DeltaArgs& a, hipStream_t stream) {
+  using IO = typename M::IO;
+  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / kBv), unsigned(a.H), unsigned(a.batch));
+  constexpr size_t scan = sizeof(BackLds<M, KP>), local = sizeof(LocalLds<M, KP>);
+  static_assert(scan <= 160 * 1024 && local <= 160 * 1024, "LDS of a CU");
+  if (!allow_lds(delta_back_scan_kernel<M, KP>, scan) || !allow_lds(delta_back_local_kernel<M, KP>, local))
+    return fail(DENDSN_E_HIP, "delta backward: %zu bytes of LDS refused", scan > local ? scan : local);
+  delta_local_kernel<M, KP, true><<<heads, dim3(64), 0, stream>>>(a);
+  delta_back_scan_kernel<M, KP><<<cols, dim3(kThreads), scan, stream>>>(a);
+  delta_back_local_kernel<M, KP><<<heads, dim3(kThreads), local, stream>>>(a);
+  if (a.H != a.Hk) {
+    const int64_t rows = int64_t(a.T) * a.batch * a.Hk, blocks = ceil_div(rows * a.K, 256);
+    delta_join_kernel<IO><<<dim3(unsigned(blocks < 65536 ? blocks : 65536)), dim3(256), 0, stream>>>(
+        a.part_q, a.part_k, static_cast<IO*>(a.gq), static_cast<IO*>(a.gk), rows, a.K, a.H / a.Hk);
+  }
+  return launched("delta backward");
+}
+
+dendsn_status copy_states(const dendsn_delta_cfg* c, const float* from, float* to, hipStream_t stream, const char* what) {
+  const int64_t n = states(c), blocks = ceil_div(n, 256);
+  if (!to || n == 0) return DENDSN_OK;
+  delta_copy_kernel<<<dim3(unsigned(blocks < 4096 ? blocks : 4096)), dim3(256), 0, stream>>>(from, to, n);
+  return launched(what);
+}
+
+}  // namespace
+}  // namespace dendsn_seq
+
+using namespace dendsn_seq;
+
+extern "C" {
+
+dendsn_status dendsn_delta_ckpt_bytes(const dendsn_delta_cfg* cfg, size_t* bytes) {
+  clear_error();
+  const dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  if (!bytes) return fail(DENDSN_E_INVALID, "bytes is NULL");
+  *bytes = make_plan(cfg).ckpt;
+  return DENDSN_OK;
+}
+
+dendsn_status dendsn_delta_workspace_bytes(const dendsn_delta_cfg* cfg, int32_t backward, size_t* bytes) {
+  clear_error();
+  const dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  if (!bytes) return fail(DENDSN_E_INVALID, "bytes is NULL");
+  const DeltaPlan p = make_plan(cfg);
+  *bytes = backward ? p.backward : p.forward;
+  return DENDSN_OK;
+}
+
+dendsn_status dendsn_delta_forward(const dendsn_delta_cfg* cfg, const void* q, const void* k, const void* v,
+                                   const void* g, const void* beta, const float* s0, const int32_t* lengths, void* o,
+                                   float* s_last, void* ckpt, void* workspace, size_t workspace_bytes,
+                                   hipStream_t stream) {
+  clear_error();
+  dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
+  const bool none = empty(cfg);
+  if (!none && (!q || !k || !v || !g || !beta || !o)) return fail(DENDSN_E_INVALID, "q, k, v, g, beta or o is NULL");
+  if (!aligned(q, esz) || !aligned(k, esz) || !aligned(v, esz) || !aligned(g, esz) || !aligned(beta, esz) || !aligned(o, esz))
+    return fail(DENDSN_E_INVALID, "q, k, v, g, beta or o misaligned");
+  if (!aligned(s0, 4) || !aligned(lengths, 4) || !aligned(s_last, 4)) return fail(DENDSN_E_INVALID, "s0, lengths or s_last misaligned");
+  if (!aligned(ckpt, 16)) return fail(DENDSN_E_INVALID, "ckpt must be 16-byte aligned");
+  if (!none && !rows_apart(cfg, cfg->o_t, cfg->o_b, cfg->o_h)) return fail(DENDSN_E_INVALID, "rows of o overlap");
+  if (none) return copy_states(cfg, s0, s_last, stream, "delta forward");
+  const DeltaPlan p = make_plan(cfg);
+  st = check_workspace(workspace, workspace_bytes, p.forward, "dendsn_delta_workspace_bytes");
+  if (st != DENDSN_OK) return st;
+  DeltaArgs a{};
+  fill_args(cfg, p, workspace, a);
+  a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.s0 = s0; a.lengths = lengths; a.o = o; a.s_last = s_last;
+  if (ckpt) {
+    a.ck_s = static_cast<float*>(ckpt);
+    a.ck_u = reinterpret_cast<float*>(static_cast<char*>(ckpt) + p.ck_u);
+  }
+  if (cfg->io == DENDSN_IO_BF16) return p.KP == 64 ? launch_forward<B16, 64>(a, stream) : launch_forward<B16, 128>(a, stream);
+  return p.KP == 64 ? launch_forward<F32, 64>(a, stream) : launch_forward<F32, 128>(a, stream);
+}
+
+dendsn_status dendsn_delta_backward(const dendsn_delta_cfg* cfg, const void* q, const void* k, const void* v,
+                                    const void* g, const void* beta, const int32_t* lengths, const void* ckpt,
+                                    const void* grad_o, const float* grad_s_last, void* grad_q, void* grad_k,
+                                    void* grad_v, void* grad_g, void* grad_beta, float* grad_s0, void* workspace,
+                                    size_t workspace_bytes, hipStream_t stream) {
+  clear_error();
+  dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
+  const bool none = empty(cfg);
+  if (!none && (!q || !k || !v || !g || !beta || !grad_o)) return fail(DENDSN_E_INVALID, "q, k, v, g, beta or grad_o is NULL");
+  if (!none && (!grad_q || !grad_k || !grad_v || !grad_g || !grad_beta)) return fail(DENDSN_E_INVALID, "a gradient of an input is NULL");
+  if (!none && !ckpt) return fail(DENDSN_E_INVALID, "ckpt is NULL");
+  if (!aligned(q, esz) || !aligned(k, esz) || !aligned(v, esz) || !aligned(g, esz) || !aligned(beta, esz) || !aligned(grad_o, esz))
+    return fail(DENDSN_E_INVALID, "q, k, v, g, beta or grad_o misaligned");
+  if (!aligned(grad_q, esz) || !aligned(grad_k, esz) || !aligned(grad_v, esz) || !aligned(grad_g, esz) || !aligned(grad_beta, esz))
+    return fail(DENDSN_E_INVALID, "a gradient of an input is misaligned");
+  if (!aligned(grad_s_last, 4) || !aligned(lengths, 4) || !aligned(grad_s0, 4))
+    return fail(DENDSN_E_INVALID, "grad_s_last, lengths or grad_s0 misaligned");
+  if (!aligned(ckpt, 16)) return fail(DENDSN_E_INVALID, "ckpt must be 16-byte aligned");
+  if (none) return copy_states(cfg, grad_s_last, grad_s0, stream, "delta backward");
+  const DeltaPlan p = make_plan(cfg);
+  st = check_workspace(workspace, workspace_bytes, p.backward, "dendsn_delta_workspace_bytes");
+  if (st != DENDSN_OK) return st;
+  DeltaArgs a{};
+  fill_args(cfg, p, workspace, a);
+  a.q = q; a.k = k; a.v = v; a.g = g; a.beta = beta; a.lengths = lengths; a.go = grad_o; a.gs_last = grad_s_last;
+  a.gq = grad_q; a.gk = grad_k; a.gv = grad_v; a.gg = grad_g; a.gbeta = grad_beta; a.gs0 = grad_s0;
+  a.ck_s = static_cast<float*>(const_cast<void*>(ckpt));
+  a.ck_u = reinterpret_cast<float*>(static_cast<char*>(const_cast<void*>(ckpt)) + p.ck_u);
+  if (cfg->io == DENDSN_IO_BF16) return p.KP == 64 ? launch_backward<B16, 64>(a, stream) : launch_backward<B16, 128>(a, stream);
+  return p.KP == 64 ? launch_backward<F32, 64>(a, stream) : launch_backward<F32, 128>(a, stream);
+}
+
+dendsn_status dendsn_delta_step(const dendsn_delta_cfg* cfg, const void* q, const void* k, const void* v,
+                                const void* g, const void* beta, int64_t n_slots, const int32_t* slots, float* state,
+                                void* o, hipStream_t stream) {
+  clear_error();
+  const dendsn_status st = check_cfg(cfg);
+  if (st != DENDSN_OK) return st;
+  if (cfg->T != 1) return fail(DENDSN_E_INVALID, "T must be 1");
+  const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
+  const bool none = empty(cfg);
+  if (n_slots < 0 || !small_product(n_slots, cfg->H * cfg->K * cfg->V)) return fail(DENDSN_E_INVALID, "n_slots negative or too large");
+  if (!slots && n_slots < cfg->batch) return fail(DENDSN_E_INVALID, "without slots, n_slots must be >= batch");
+  if (!none && (!q || !k || !v || !g || !beta || !o)) return fail(DENDSN_E_INVALID, "q, k, v, g, beta or o is NULL");
+  if (!none && n_slots > 0 && !state) return fail(DENDSN_E_INVALID, "state is NULL");
+  if (!aligned(q, esz) || !aligned(k, esz) || !aligned(v, esz) || !aligned(g, esz) || !aligned(beta, esz) || !aligned(o, esz))
+    return fail(DENDSN_E_INVALID, "q, k, v, g, beta or o misaligned");
+  if (!aligned(slots, 4) || !aligned(state, 4)) return fail(DENDSN_E_INVALID, "slots or state misaligned");
+  if (!none && !rows_apart(cfg, cfg->o_t, cfg->o_b, cfg->o_h)) return fail(DENDSN_E_INVALID, "rows of o overlap");
+  if (none) return DENDSN_OK;
+  const DeltaStepArgs a{q, k, v, g, beta, slots, state, o, cfg->q_b, cfg->q_h, cfg->k_b, cfg->k_h, cfg->v_b, cfg->v_h,
+                        cfg->g_b, cfg->g_h, cfg->beta_b, cfg->beta_h, cfg->o_b, cfg->o_h, n_slots,
+                        int32_t(cfg->H), int32_t(cfg->H / cfg->Hk), int32_t(cfg->K), int32_t(cfg->V), cfg->scale};
+  const dim3 grid(unsigned(ceil_div(cfg->V, kBv)), unsigned(cfg->H), unsigned(cfg->batch));
+  if (cfg->io == DENDSN_IO_BF16) delta_step_kernel<bf16_t><<<grid, dim3(kThreads), 0, stream>>>(a);
+  else delta_step_kernel<float><<<grid, dim3(kThreads), 0, stream>>>(a);
+  return launched("delta step");
+}
+
+}  // extern "C"
