@@ -42,8 +42,11 @@ typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kC = 64;          // steps of a chunk
-constexpr int kBv = 32;         // columns of v of a block of the scans
 constexpr int kThreads = 256;
+#ifndef SCANV
+#define SCANV 32
+#endif
+constexpr int kScanV = SCANV;      // columns of v of a block of the scans
 constexpr double kForget = -200.0;  // exp of it is 0 in fp32
 
 struct DeltaArgs {
@@ -53,7 +56,8 @@ struct DeltaArgs {
   void *o, *gq, *gk, *gv, *gg, *gbeta;
   float *s_last, *gs0;
   float *ck_s, *ck_u;       // [batch][H][nc]: [KP][Vp], [64][Vp]
-  float *tm, *pm, *dec;     // [batch][H][nc]: [64][64] twice, [3][64]
+  void *tm, *pm;            // [batch][H][nc]: planes of [64][64]
+  float* dec;               // [batch][H][nc]: [3][64]
   float *dr, *ds;           // as ck_u and ck_s
   float *part_q, *part_k;   // [T][batch][H][K] where heads are shared
   int64_t q_t, q_b, q_h, k_t, k_b, k_h, v_t, v_b, v_h, g_t, g_b, g_h, beta_t, beta_b, beta_h, o_t, o_b, o_h;
@@ -66,66 +70,103 @@ struct DeltaArgs {
 // Operands.  A fragment is a lane's eight values of one row (or column): row
 // lane % 16, places 8 (lane / 16) to + 7 of 32 along the sum.
 // ---------------------------------------------------------------------------
-struct F32 { using IO = float; };
-struct B16 { using IO = bf16_t; };
+struct F32 {
+  using IO = float;
+  using Word = float;
+  static constexpr int planes = 1;
+};
+template <int P> struct Bf {
+  using IO = bf16_t;
+  using Word = __bf16;
+  static constexpr int planes = P;
+};
 
 template <class M> struct Exact;  // of inputs
-template <class M> struct Both;   // of what was computed
+template <class M> struct Both;   // of what was computed: a sum of planes
 template <> struct Both<F32> { f32x8 v; };
 template <> struct Exact<F32> : Both<F32> {};
-template <> struct Exact<B16> { bf16x8 h; };
-template <> struct Both<B16> { bf16x8 h, l; };
+template <int P> struct Exact<Bf<P>> { bf16x8 h; };
+template <int P> struct Both<Bf<P>> { bf16x8 p[P]; };
 
 __device__ __forceinline__ f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
-__device__ __forceinline__ void mma(f32x4& c, const Exact<B16>& a, const Exact<B16>& b) { c = mfma(a.h, b.h, c); }
-__device__ __forceinline__ void mma(f32x4& c, const Exact<B16>& a, const Both<B16>& b) {
-  c = mfma(a.h, b.l, c);
-  c = mfma(a.h, b.h, c);
+// The Q largest orders of planes, the smallest first; Q of 0: all.
+template <int Q = 0, int P>
+__device__ __forceinline__ void mma(f32x4& c, const Exact<Bf<P>>& a, const Exact<Bf<P>>& b) { c = mfma(a.h, b.h, c); }
+template <int Q = 0, int P>
+__device__ __forceinline__ void mma(f32x4& c, const Exact<Bf<P>>& a, const Both<Bf<P>>& b) {
+#pragma unroll
+  for (int j = (Q ? Q : P) - 1; j >= 0; --j) c = mfma(a.h, b.p[j], c);
 }
-__device__ __forceinline__ void mma(f32x4& c, const Both<B16>& a, const Exact<B16>& b) {
-  c = mfma(a.l, b.h, c);
-  c = mfma(a.h, b.h, c);
+template <int Q = 0, int P>
+__device__ __forceinline__ void mma(f32x4& c, const Both<Bf<P>>& a, const Exact<Bf<P>>& b) {
+#pragma unroll
+  for (int j = (Q ? Q : P) - 1; j >= 0; --j) c = mfma(a.p[j], b.h, c);
 }
-__device__ __forceinline__ void mma(f32x4& c, const Both<B16>& a, const Both<B16>& b) {
-  c = mfma(a.l, b.h, c);
-  c = mfma(a.h, b.l, c);
-  c = mfma(a.h, b.h, c);
+template <int Q = 0, int P>
+__device__ __forceinline__ void mma(f32x4& c, const Both<Bf<P>>& a, const Both<Bf<P>>& b) {
+#pragma unroll
+  for (int n = (Q ? Q : P) - 1; n >= 0; --n)
+#pragma unroll
+    for (int j = 0; j <= n; ++j) c = mfma(a.p[j], b.p[n - j], c);
 }
+template <int Q = 0>
 __device__ __forceinline__ void mma(f32x4& c, const Both<F32>& a, const Both<F32>& b) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[j], b.v[j], c, 0, 0, 0);
 }
 
 __device__ __forceinline__ void both_of(f32x8 x, Both<F32>& f) { f.v = x; }
-__device__ __forceinline__ void both_of(f32x8 x, Both<B16>& f) {
-  f.h = __builtin_convertvector(x, bf16x8);
-  f.l = __builtin_convertvector(x - __builtin_convertvector(f.h, f32x8), bf16x8);
+template <int P>
+__device__ __forceinline__ void both_of(f32x8 x, Both<Bf<P>>& f) {
+#pragma unroll
+  for (int j = 0; j < P; ++j) {
+    f.p[j] = __builtin_convertvector(x, bf16x8);
+    if (j + 1 < P) x -= __builtin_convertvector(f.p[j], f32x8);
+  }
 }
 
-// Eight places of a row from k0 on, zeros from K on and in rows that are not there.
+// Eight values of a row as they are stored.
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+template <typename IO> struct Eight;
+template <> struct Eight<float> {
+  typedef f32x8 Vec;
+  typedef f32x8 Any __attribute__((aligned(4)));  // anywhere in memory
+  static __device__ __forceinline__ float bits(float v) { return v; }
+  static __device__ __forceinline__ float wide(float v) { return v; }
+};
+template <> struct Eight<bf16_t> {
+  typedef u16x8 Vec;
+  typedef u16x8 Any __attribute__((aligned(2)));
+  static __device__ __forceinline__ uint16_t bits(bf16_t v) { return v.bits; }
+  static __device__ __forceinline__ float wide(uint16_t v) { return widen(bf16_t{v}); }
+};
+
+// Eight places of a row of K from k0 on, without a branch a lane: what lies past K has some
+// other value of the row.  odd (K is no multiple of 8): value by value.
 template <typename IO>
-__device__ __forceinline__ Pack<IO, 8> load8(const IO* row, int k0, int K, bool ok) {
-  Pack<IO, 8> r;
-  if (ok && k0 + 8 <= K) {
-    r = *reinterpret_cast<const Pack<IO, 8>*>(row + k0);
+__device__ __forceinline__ typename Eight<IO>::Vec load8(const IO* row, int k0, int K, bool odd) {
+  typename Eight<IO>::Vec r;
+  if (!odd) {
+    r = *reinterpret_cast<const typename Eight<IO>::Any*>(row + (k0 < K ? k0 : 0));
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) r.v[j] = ok && k0 + j < K ? row[k0 + j] : IO{};
+    for (int j = 0; j < 8; ++j) r[j] = Eight<IO>::bits(row[min(k0 + j, K - 1)]);
   }
   return r;
 }
-__device__ __forceinline__ Exact<F32> exact_of(const Pack<float, 8>& p) {
-  Exact<F32> f;
+// The same with zeros past K.
+template <typename V>
+__device__ __forceinline__ void cut8(V& r, int k0, int K) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) f.v[j] = p.v[j];
-  return f;
+  for (int j = 0; j < 8; ++j) r[j] = k0 + j < K ? r[j] : 0;
 }
-__device__ __forceinline__ Exact<B16> exact_of(const Pack<bf16_t, 8>& p) {
-  Exact<B16> f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) f.h[j] = __builtin_bit_cast(__bf16, p.v[j].bits);
+template <class M>
+__device__ __forceinline__ Exact<M> exact_of(typename Eight<typename M::IO>::Vec r) {
+  Exact<M> f;
+  if constexpr (M::planes == 1) f.v = r;
+  else f.h = __builtin_bit_cast(bf16x8, r);
   return f;
 }
 template <class M>
@@ -148,22 +189,31 @@ template <int ROWS, int COLS> struct Mat<F32, ROWS, COLS> {
   __device__ __forceinline__ void put4(int row, int col, f32x4 x) { *reinterpret_cast<f32x4*>(v + row * kLd + col) = x; }
   __device__ __forceinline__ void put(int row, int col, float x) { v[row * kLd + col] = x; }
 };
-template <int ROWS, int COLS> struct Mat<B16, ROWS, COLS> {
+template <int P, int ROWS, int COLS> struct Mat<Bf<P>, ROWS, COLS> {
   static constexpr int kLd = COLS + 8;
-  __bf16 h[ROWS * kLd], l[ROWS * kLd];
-  __device__ __forceinline__ Both<B16> frag(int row, int col) const {
+  __bf16 v[P][ROWS * kLd];
+  __device__ __forceinline__ Both<Bf<P>> frag(int row, int col) const {
     const int lane = threadIdx.x & 63, at = (row + lane % 16) * kLd + col + lane / 16 * 8;
-    return Both<B16>{*reinterpret_cast<const bf16x8*>(h + at), *reinterpret_cast<const bf16x8*>(l + at)};
+    Both<Bf<P>> f;
+#pragma unroll
+    for (int j = 0; j < P; ++j) f.p[j] = *reinterpret_cast<const bf16x8*>(v[j] + at);
+    return f;
   }
   __device__ __forceinline__ void put4(int row, int col, f32x4 x) {
-    const bf16x4 a = __builtin_convertvector(x, bf16x4);
-    *reinterpret_cast<bf16x4*>(h + row * kLd + col) = a;
-    *reinterpret_cast<bf16x4*>(l + row * kLd + col) = __builtin_convertvector(x - __builtin_convertvector(a, f32x4), bf16x4);
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const bf16x4 a = __builtin_convertvector(x, bf16x4);
+      *reinterpret_cast<bf16x4*>(v[j] + row * kLd + col) = a;
+      if (j + 1 < P) x -= __builtin_convertvector(a, f32x4);
+    }
   }
   __device__ __forceinline__ void put(int row, int col, float x) {
-    const __bf16 a = static_cast<__bf16>(x);
-    h[row * kLd + col] = a;
-    l[row * kLd + col] = static_cast<__bf16>(x - static_cast<float>(a));
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const __bf16 a = static_cast<__bf16>(x);
+      v[j][row * kLd + col] = a;
+      if (j + 1 < P) x -= static_cast<float>(a);
+    }
   }
 };
 template <class M, int ROWS, int COLS> struct MatX;  // of inputs
@@ -181,35 +231,68 @@ template <int ROWS, int COLS> struct MatX<F32, ROWS, COLS> {
   }
   __device__ __forceinline__ f32x4 get4(int row, int col) const { return *reinterpret_cast<const f32x4*>(v + row * kLd + col); }
 };
-template <int ROWS, int COLS> struct MatX<B16, ROWS, COLS> {
+template <int P, int ROWS, int COLS> struct MatX<Bf<P>, ROWS, COLS> {
   static constexpr int kLd = COLS + 8;
   __bf16 h[ROWS * kLd];
-  __device__ __forceinline__ Exact<B16> frag(int row, int col) const {
+  __device__ __forceinline__ Exact<Bf<P>> frag(int row, int col) const {
     const int lane = threadIdx.x & 63;
-    return Exact<B16>{*reinterpret_cast<const bf16x8*>(h + (row + lane % 16) * kLd + col + lane / 16 * 8)};
+    return Exact<Bf<P>>{*reinterpret_cast<const bf16x8*>(h + (row + lane % 16) * kLd + col + lane / 16 * 8)};
   }
-  __device__ __forceinline__ void put4(int row, int col, bf16_t a, bf16_t b, bf16_t c, bf16_t d) {
-    *reinterpret_cast<uint2*>(h + row * kLd + col) = uint2{a.bits | uint32_t(b.bits) << 16, c.bits | uint32_t(d.bits) << 16};
+  __device__ __forceinline__ void put4(int row, int col, uint16_t a, uint16_t b, uint16_t c, uint16_t d) {
+    *reinterpret_cast<uint2*>(h + row * kLd + col) = uint2{a | uint32_t(b) << 16, c | uint32_t(d) << 16};
   }
   __device__ __forceinline__ f32x4 get4(int row, int col) const {
     return __builtin_convertvector(*reinterpret_cast<const bf16x4*>(h + row * kLd + col), f32x4);
   }
 };
 
-// dst[d][t] = rows[t][d]: COLS steps (n of which are there), D of ROWS places.
-template <class M, int ROWS>
-__device__ __forceinline__ void fill_turned(MatX<M, ROWS, kC>& dst, const typename M::IO* rows, int64_t stride, int n, int D) {
+// dst[d][t] = rows[t][d]: 64 steps (n of which are there), D of ROWS places.  A thread has a
+// block of 4 x 8, in registers between the two.
+template <class M, int ROWS> struct Turn {
   using IO = typename M::IO;
-  for (int u = threadIdx.x; u < 2 * ROWS; u += kThreads) {
-    const int t = u % 16 * 4, d = u / 16 * 8;
-    Pack<IO, 8> r[4];
+  static constexpr bool kAll = 2 * ROWS == kThreads;  // each of 256 threads has a block
+  static_assert(2 * ROWS <= kThreads, "one block a thread");
+  __device__ __forceinline__ static int tid() { return threadIdx.x % kThreads; }
+  typename Eight<IO>::Vec r[4];
+  // steps past the n-th have the n-th's values
+  __device__ __forceinline__ void load(const IO* rows, int64_t stride, int n, int D, bool odd) {
+    const int t = tid() % 16 * 4, d = tid() / 16 * 8;
+    if (!kAll && tid() >= 2 * ROWS) return;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) r[x] = load8(rows + (t + x) * stride, d, D, t + x < n);
-#pragma unroll
-    for (int y = 0; y < 8; ++y) dst.put4(d + y, t, r[0].v[y], r[1].v[y], r[2].v[y], r[3].v[y]);
+    for (int x = 0; x < 4; ++x) r[x] = load8(rows + min(t + x, n - 1) * stride, d, D, odd);
   }
+  __device__ __forceinline__ void put(MatX<M, ROWS, kC>& dst, int D) {
+    const int t = tid() % 16 * 4, d = tid() / 16 * 8;
+    if (!kAll && tid() >= 2 * ROWS) return;
+    if (D < ROWS) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) cut8(r[x], d, D);
+    }
+#pragma unroll
+    for (int y = 0; y < 8; ++y) dst.put4(d + y, t, r[0][y], r[1][y], r[2][y], r[3][y]);
+  }
+};
+
+// A barrier for what is in LDS: loads and stores of device memory stay in flight.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+// T and P in memory: planes of [64][64], as operands of their rows.
+template <class M>
+__device__ __forceinline__ Both<M> load_planes(const typename M::Word* p, int row, int col) {
+  const int at = row * kC + col;
+  Both<M> f;
+  if constexpr (M::planes == 1) {
+    f = load_both<M>(p + at);
+  } else {
+#pragma unroll
+    for (int j = 0; j < M::planes; ++j) f.p[j] = *reinterpret_cast<const bf16x8*>(p + j * kC * kC + at);
+  }
+  return f;
+}
 __device__ __forceinline__ int length_of(const DeltaArgs& a, int b) {
   if (!a.lengths) return a.T;
   const int n = a.lengths[b];
@@ -240,21 +323,52 @@ __device__ __forceinline__ double chunk_sum(const DeltaArgs& a, int b, int h, in
 }
 
 // ---------------------------------------------------------------------------
-// local: T and P (BACK: turned) and the decays of one chunk, one wave each.
+// local: T and P (BACK: turned) and the decays of one chunk.  Wave w has steps 16 w to + 15
+// of A and P.  T by blocks of 16: those on the diagonal by substitution, a column a lane; then
+// T_ij = -T_ii sum over k from j to i - 1 of A_ik T_kj, a diagonal of blocks at a time, in fp32.
 // ---------------------------------------------------------------------------
+// Eight values of a row of T or P from LDS, as planes in memory.
+template <class M>
+__device__ __forceinline__ void store_planes8(typename M::Word* p, int row, int col, f32x8 x) {
+  if constexpr (M::planes == 1) {
+    *reinterpret_cast<f32x8*>(p + row * kC + col) = x;
+  } else {
+#pragma unroll
+    for (int j = 0; j < M::planes; ++j) {
+      const bf16x8 a = __builtin_convertvector(x, bf16x8);
+      *reinterpret_cast<bf16x8*>(p + j * kC * kC + row * kC + col) = a;
+      x -= __builtin_convertvector(a, f32x8);
+    }
+  }
+}
+
 template <class M, int KP, bool BACK>
-__global__ __launch_bounds__(64) void delta_local_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
   using IO = typename M::IO;
-  constexpr int KS = KP / 32;
-  const int lane = threadIdx.x, c = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  using Word = typename M::Word;
+  constexpr int KS = KP / 32, kLd = kC + 4;
+  const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
+  const int c = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const int t0 = c * kC, n = min(length_of(a, b) - t0, kC);
   if (n <= 0) return;
   __shared__ double sg[kC];
   __shared__ float sb[kC];
-  __shared__ __align__(16) float sa[kC][kC + 4];
+  __shared__ __align__(16) float sa[kC][kLd], st[kC][kLd], sp[kC][kLd], sm[4][16][17];
   const int64_t at = (int64_t(b) * a.H + h) * a.nc + c;
-  float* pm = a.pm + at * kC * kC;
-  {
+  const int hk = h / (a.H / a.Hk), row = 16 * w + r;
+  const IO* kp = static_cast<const IO*>(a.k) + t0 * a.k_t + b * a.k_b + hk * a.k_h;
+  const IO* qp = static_cast<const IO*>(a.q) + t0 * a.q_t + b * a.q_b + hk * a.q_h;
+  const bool odd = a.K % 8;
+  typename Eight<IO>::Vec kr[3][KS], own[KS], qr[KS];  // rows of the blocks before, of the wave's own
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    qr[s] = load8(qp + min(row, n - 1) * a.q_t, s * 32 + q4 * 8, a.K, odd);
+    own[s] = load8(kp + min(row, n - 1) * a.k_t, s * 32 + q4 * 8, a.K, odd);
+#pragma unroll
+    for (int bj = 0; bj < 3; ++bj)
+      if (bj < w) kr[bj][s] = load8(kp + min(16 * bj + r, n - 1) * a.k_t, s * 32 + q4 * 8, a.K, odd);
+  }
+  if (w == 3) {  // (the wave with the most products waits least)
     const double G = chunk_sum<IO>(a, b, h, t0, n);
     const double last = __shfl(G, 63);
     const float beta = lane < n ? widen(static_cast<const IO*>(a.beta)[int64_t(t0 + lane) * a.beta_t + b * a.beta_b + h * a.beta_h]) : 0.0f;
@@ -265,87 +379,123 @@ __global__ __launch_bounds__(64) void delta_local_kernel(DeltaArgs a) {
     sg[lane] = G;
     sb[lane] = beta;
   }
-  __syncthreads();
-  const int hk = h / (a.H / a.Hk), r = lane % 16, q4 = lane / 16;
-  const IO* kp = static_cast<const IO*>(a.k) + t0 * a.k_t + b * a.k_b + hk * a.k_h;
-  const IO* qp = static_cast<const IO*>(a.q) + t0 * a.q_t + b * a.q_b + hk * a.q_h;
-  Exact<M> kf[4][KS];
-#pragma unroll
-  for (int bi = 0; bi < 4; ++bi) {
-    const int row = bi * 16 + r;
-    Exact<M> qf[KS];
+  if (a.K < KP) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      kf[bi][s] = exact_of(load8(kp + row * a.k_t, s * 32 + q4 * 8, a.K, row < n));
-      qf[s] = exact_of(load8(qp + row * a.q_t, s * 32 + q4 * 8, a.K, row < n));
+      cut8(qr[s], s * 32 + q4 * 8, a.K);
+      cut8(own[s], s * 32 + q4 * 8, a.K);
+#pragma unroll
+      for (int bj = 0; bj < 3; ++bj)
+        if (bj < w) cut8(kr[bj][s], s * 32 + q4 * 8, a.K);
     }
+  }
+  f32x4 kk[4], qk[4];  // of the blocks before, and last of the wave's own
 #pragma unroll
-    for (int bj = 0; bj < 4; ++bj) {
-      f32x4 kk = {0, 0, 0, 0}, qk = {0, 0, 0, 0};
-      if (bj <= bi) {
+  for (int bj = 0; bj < 4; ++bj) {
+    kk[bj] = qk[bj] = f32x4{0, 0, 0, 0};
+    if (bj < w || bj == 3) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-          mma(kk, kf[bi][s], kf[bj][s]);
-          mma(qk, qf[s], kf[bj][s]);
-        }
+      for (int s = 0; s < KS; ++s) {
+        const Exact<M> f = exact_of<M>(bj < 3 ? kr[bj < 3 ? bj : 0][s] : own[s]);
+        mma(kk[bj], exact_of<M>(own[s]), f);
+        mma(qk[bj], exact_of<M>(qr[s]), f);
       }
-      const int j = bj * 16 + r, i0 = bi * 16 + q4 * 4;
+    }
+  }
+  __syncthreads();
+  const int i0 = 16 * w + q4 * 4;
+#pragma unroll
+  for (int bj = 0; bj < 4; ++bj) {
+    const int j = 16 * bj + r;
+    f32x4 A = {0, 0, 0, 0}, P = {0, 0, 0, 0};
+    if (bj <= w) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const int i = i0 + x;
         const float d = j <= i ? exp_of(sg[i] - sg[j]) : 0.0f;
-        sa[i][j] = j < i ? sb[i] * d * kk[x] : 0.0f;
-        qk[x] = j <= i ? a.scale * d * qk[x] : 0.0f;
+        A[x] = j < i ? sb[i] * d * (bj < w ? kk[bj][x] : kk[3][x]) : 0.0f;
+        P[x] = j <= i ? a.scale * d * (bj < w ? qk[bj][x] : qk[3][x]) : 0.0f;
       }
-      if (BACK) {
-        *reinterpret_cast<f32x4*>(pm + j * kC + i0) = qk;
-      } else {
+    }
+    if (BACK) *reinterpret_cast<f32x4*>(&sp[j][i0]) = P;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) pm[(i0 + x) * kC + j] = qk[x];
-      }
+    for (int x = 0; x < 4; ++x) {
+      sa[i0 + x][j] = A[x];
+      if (!BACK) sp[i0 + x][j] = P[x];
+      if (bj > w) st[i0 + x][j] = 0.0f;
     }
   }
   __syncthreads();
-  // column `lane` of T, row by row
-  float t[kC];
+  {  // the block on the diagonal: lane r has column r, each quarter of the wave writes four rows
+    float t[16];
 #pragma unroll
-  for (int i = 0; i < kC; ++i) {
-    float s = i == lane ? 1.0f : 0.0f;
+    for (int i = 0; i < 16; ++i) {
+      float s = i == r ? 1.0f : 0.0f;
 #pragma unroll
-    for (int j = 0; j < i; ++j) s = fmaf(-sa[i][j], t[j], s);
-    t[i] = s;
-  }
-  float* tm = a.tm + at * kC * kC;
-#pragma unroll
-  for (int i = 0; i < kC; i += 4) {
-    if (BACK) {
-      *reinterpret_cast<f32x4*>(tm + lane * kC + i) = f32x4{t[i], t[i + 1], t[i + 2], t[i + 3]};
-    } else {
-#pragma unroll
-      for (int x = 0; x < 4; ++x) tm[(i + x) * kC + lane] = t[i + x];
+      for (int j = 0; j < i; ++j) s = fmaf(-sa[16 * w + i][16 * w + j], t[j], s);
+      t[i] = s;
     }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i / 4 == q4) st[16 * w + i][16 * w + r] = t[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int d = 1; d < 4; ++d) {
+    if (w + d < 4) {
+      const int i = 16 * (w + d), j = 16 * w;
+      f32x4 m = {0, 0, 0, 0}, t = {0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < 16 * d; k += 4) m = __builtin_amdgcn_mfma_f32_16x16x4f32(sa[i + r][j + k + q4], st[j + k + q4][j + r], m, 0, 0, 0);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) sm[w][q4 * 4 + x][r] = m[x];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+      for (int k = 0; k < 16; k += 4) t = __builtin_amdgcn_mfma_f32_16x16x4f32(st[i + r][i + k + q4], sm[w][k + q4][r], t, 0, 0, 0);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) st[i + q4 * 4 + x][j + r] = -t[x];
+    }
+    __syncthreads();
+  }
+  Word* pm = static_cast<Word*>(a.pm) + at * M::planes * kC * kC;
+  Word* tm = static_cast<Word*>(a.tm) + at * M::planes * kC * kC;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int e = u * kThreads + threadIdx.x, i = e / 8, j = e % 8 * 8;
+    f32x8 x, y;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = BACK ? st[j + k][i] : st[i][j + k];
+      y[k] = sp[i][j + k];
+    }
+    store_planes8<M>(tm, i, j, x);
+    store_planes8<M>(pm, i, j, y);
   }
 }
 
 // ---------------------------------------------------------------------------
-// scan: states and outputs, chunk after chunk.  Wave w has steps 16 w to + 15 of
-// the products over steps, and an eighth (K of 128) or so of the state's rows.
+// scan: states and outputs, chunk after chunk, BV columns of v a block.  Wave w has steps 16 w
+// to + 15 of the products over steps, and a quarter of the state's rows, which stay in its
+// registers.  Three barriers a chunk: the state, R and U go through LDS.  What a chunk reads is
+// fetched while the one before is computed, into the registers that it no longer needs; the
+// barriers wait for LDS alone.
 // ---------------------------------------------------------------------------
-template <class M, int KP>
+template <class M, int KP, int BV>
 struct ScanLds {
-  MatX<M, KP, kC> kt;
-  Mat<M, kBv, KP> st;
-  Mat<M, kBv, kC> rt, ut, us;
+  MatX<M, KP, kC> kt[2];
+  Mat<M, BV, KP> st;
+  Mat<M, BV, kC> rt, ut, us;
 };
 
-template <class M, int KP>
+template <class M, int KP, int BV, bool ODD>
 __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
   using IO = typename M::IO;
-  constexpr int KS = KP / 32, MT = KP / 64;  // MT: row tiles of the state of a wave
+  using Word = typename M::Word;
+  constexpr int KS = KP / 32, MT = KP / 64, NV = BV / 16;  // MT: row tiles of the state of a wave
   extern __shared__ __align__(16) char lds[];
-  ScanLds<M, KP>& s = *reinterpret_cast<ScanLds<M, KP>*>(lds);
+  ScanLds<M, KP, BV>& s = *reinterpret_cast<ScanLds<M, KP, BV>*>(lds);
   const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
-  const int v0 = blockIdx.x * kBv, h = blockIdx.y, b = blockIdx.z, hk = h / (a.H / a.Hk);
+  const int v0 = blockIdx.x * BV, h = blockIdx.y, b = blockIdx.z, hk = h / (a.H / a.Hk);
   const int len = length_of(a, b), chunks = (len + kC - 1) / kC;
   const int64_t bh = int64_t(b) * a.H + h;
   const IO* kb = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
@@ -354,79 +504,119 @@ __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
   IO* ob = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h;
 
   // the state: rows 16 (MT w + m) + 4 q4 + x, columns 16 nt + r
-  f32x4 S[MT][2];
+  f32x4 S[MT][NV];
   auto state_at = [&](int m, int nt, int x) { return (bh * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
   auto state_in = [&](int m, int nt, int x) { return (MT * w + m) * 16 + q4 * 4 + x < a.K && v0 + nt * 16 + r < a.V; };
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
+    for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
       for (int x = 0; x < 4; ++x) S[m][nt][x] = a.s0 && state_in(m, nt, x) ? a.s0[state_at(m, nt, x)] : 0.0f;
 
-  for (int c = 0; c < chunks; ++c) {
-    const int t0 = c * kC, n = min(len - t0, kC), row = 16 * w + r, i0 = 16 * w + q4 * 4;
-    const int64_t at = bh * a.nc + c;
-    const float* dec = a.dec + at * 3 * kC;
-    __syncthreads();  // the chunk before is read
-    fill_turned<M, KP>(s.kt, kb + t0 * a.k_t, a.k_t, n, a.K);
+  const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
+  // Rows past the sequence's end are read as its last one, columns past K and V as some other:
+  // their betas are 0, their rows of the state stay 0 (Turn), their values are set to 0.
+  constexpr bool odd = ODD;  // K is no multiple of 8
+  int vc[NV];
+  bool vin[NV];
+#pragma unroll
+  for (int nt = 0; nt < NV; ++nt) {
+    vin[nt] = v0 + nt * 16 + r < a.V;
+    vc[nt] = vin[nt] ? v0 + nt * 16 + r : 0;
+  }
+  Turn<M, KP> turn;
+  Exact<M> kf[KS], qf[KS];
+  Both<M> tf[2], pf[2];
+  f32x4 eg, tail, beta;
+  float whole;
+  IO vv[NV][4];
+  auto load_rows = [&](int c) {
+    const int t0 = c * kC, end = len - 1;
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      kf[k] = exact_of<M>(load8(kb + min(t0 + row, end) * a.k_t, k * 32 + q4 * 8, a.K, odd));
+      qf[k] = exact_of<M>(load8(qb + min(t0 + row, end) * a.q_t, k * 32 + q4 * 8, a.K, odd));
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt) vv[nt][x] = vb[min(t0 + i0 + x, end) * a.v_t + vc[nt]];
+  };
+  auto load_turn = [&](int c) { turn.load(kb + c * kC * a.k_t, a.k_t, min(len - c * kC, kC), a.K, odd); };
+  auto load_t = [&](int c) {
+    const Word* tm = static_cast<const Word*>(a.tm) + (bh * a.nc + c) * M::planes * kC * kC;
+    tf[0] = load_planes<M>(tm, row, q4 * 8);
+    if (w >= 2) tf[1] = load_planes<M>(tm, row, 32 + q4 * 8);  // T is lower
+  };
+  auto load_p = [&](int c) {
+    const Word* pm = static_cast<const Word*>(a.pm) + (bh * a.nc + c) * M::planes * kC * kC;
+    pf[0] = load_planes<M>(pm, row, q4 * 8);
+    if (w >= 2) pf[1] = load_planes<M>(pm, row, 32 + q4 * 8);
+  };
+  auto load_dec = [&](int c) {
+    const float* dec = a.dec + (bh * a.nc + c) * 3 * kC;
+    eg = *reinterpret_cast<const f32x4*>(dec + i0);
+    tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
+    beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
+    whole = dec[kC - 1];
+  };
+  auto put_state = [&]() {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
-        if (a.ck_s) {
-          float* to = a.ck_s + (at * KP + (MT * w + m) * 16 + q4 * 4) * a.Vp + v0 + nt * 16 + r;
+      for (int nt = 0; nt < NV; ++nt) s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
+  };
+  if (chunks > 0) {
+    load_turn(0);
+    load_rows(0);
+    load_t(0);
+    load_p(0);
+    load_dec(0);
+    turn.put(s.kt[0], a.K);
+    put_state();
+    lds_barrier();
+  }
+  for (int c = 0; c < chunks; ++c) {
+    const int t0 = c * kC, n = min(len - t0, kC);
+    const int64_t at = bh * a.nc + c;
+    const bool more = c + 1 < chunks;
+    if (more) load_turn(c + 1);
+    f32x4 o[NV];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = S[m][nt][x];
-        }
-      }
-    Exact<M> kf[KS], qf[KS];
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      kf[k] = exact_of(load8(kb + (t0 + row) * a.k_t, k * 32 + q4 * 8, a.K, row < n));
-      qf[k] = exact_of(load8(qb + (t0 + row) * a.q_t, k * 32 + q4 * 8, a.K, row < n));
-    }
-    Both<M> tf[2], pf[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      tf[k] = load_both<M>(a.tm + at * kC * kC + row * kC + k * 32 + q4 * 8);
-      pf[k] = load_both<M>(a.pm + at * kC * kC + row * kC + k * 32 + q4 * 8);
-    }
-    const f32x4 eg = *reinterpret_cast<const f32x4*>(dec + i0), tail = *reinterpret_cast<const f32x4*>(dec + kC + i0),
-                beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
-    const float whole = dec[kC - 1];
-    float vv[2][4];
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-        vv[nt][x] = i0 + x < n && v0 + nt * 16 + r < a.V ? widen(vb[(t0 + i0 + x) * a.v_t + v0 + nt * 16 + r]) : 0.0f;
-    __syncthreads();
-    f32x4 o[2];
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
+    for (int nt = 0; nt < NV; ++nt) {
       f32x4 ks = {0, 0, 0, 0}, qs = {0, 0, 0, 0};
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         const Both<M> f = s.st.frag(nt * 16, k * 32);
         mma(ks, kf[k], f);
-        mma(qs, qf[k], f);
+        mma<2>(qs, qf[k], f);
       }
       f32x4 R;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        R[x] = beta[x] * (vv[nt][x] - eg[x] * ks[x]);
+        R[x] = beta[x] * ((vin[nt] ? widen(vv[nt][x]) : 0.0f) - eg[x] * ks[x]);
         o[nt][x] = a.scale * eg[x] * qs[x];
       }
       s.rt.put4(nt * 16 + r, i0, R);
     }
-    __syncthreads();
+    if (more) load_rows(c + 1);
+    if (a.ck_s) {
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt) {
+          float* to = a.ck_s + (at * KP + (MT * w + m) * 16 + q4 * 4) * a.Vp + v0 + nt * 16 + r;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = S[m][nt][x];
+        }
+    }
+    lds_barrier();
+#pragma unroll
+    for (int nt = 0; nt < NV; ++nt) {
       f32x4 U = {0, 0, 0, 0};
       mma(U, tf[0], s.rt.frag(nt * 16, 0));
-      if (w >= 2) mma(U, tf[1], s.rt.frag(nt * 16, 32));  // T is lower
+      if (w >= 2) mma(U, tf[1], s.rt.frag(nt * 16, 32));
       s.ut.put4(nt * 16 + r, i0, U);
       s.us.put4(nt * 16 + r, i0, tail * U);
       if (a.ck_u) {
@@ -435,54 +625,74 @@ __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
         for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = U[x];
       }
     }
-    __syncthreads();
+    if (more) load_t(c + 1);
+    lds_barrier();
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-      mma(o[nt], pf[0], s.ut.frag(nt * 16, 0));
-      if (w >= 2) mma(o[nt], pf[1], s.ut.frag(nt * 16, 32));
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-        if (i0 + x < n && v0 + nt * 16 + r < a.V) ob[(t0 + i0 + x) * a.o_t + v0 + nt * 16 + r] = narrow<IO>(o[nt][x]);
+    for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         S[m][nt] *= whole;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) mma(S[m][nt], s.kt.frag((MT * w + m) * 16, k * 32), s.us.frag(nt * 16, k * 32));
+        for (int k = 0; k < 2; ++k) mma(S[m][nt], s.kt[c & 1].frag((MT * w + m) * 16, k * 32), s.us.frag(nt * 16, k * 32));
       }
+    put_state();  // (all have read the one before)
+    if (more) {
+      load_dec(c + 1);
+      turn.put(s.kt[(c + 1) & 1], a.K);
     }
+#pragma unroll
+    for (int nt = 0; nt < NV; ++nt) {
+      mma<2>(o[nt], pf[0], s.ut.frag(nt * 16, 0));
+      if (w >= 2) mma<2>(o[nt], pf[1], s.ut.frag(nt * 16, 32));
+    }
+    if (more) load_p(c + 1);
+    if (n == kC && v0 + BV <= a.V) {
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) ob[(t0 + i0 + x) * a.o_t + v0 + nt * 16 + r] = narrow<IO>(o[nt][x]);
+    } else {
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (i0 + x < n && vin[nt]) ob[(t0 + i0 + x) * a.o_t + v0 + nt * 16 + r] = narrow<IO>(o[nt][x]);
+    }
+    lds_barrier();
   }
   if (a.s_last) {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+      for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           if (state_in(m, nt, x)) a.s_last[state_at(m, nt, x)] = S[m][nt][x];
   }
-  for (int u = threadIdx.x; u < a.T - len; u += kThreads)  // steps past the end
-    for (int d = v0; d < min(v0 + kBv, a.V); ++d) ob[int64_t(len + u) * a.o_t + d] = IO{};
+  for (int64_t u = threadIdx.x; u < int64_t(a.T - len) * BV; u += kThreads)  // steps past the end
+    if (v0 + u % BV < a.V) ob[(len + u / BV) * a.o_t + v0 + u % BV] = IO{};
 }
 
 // ---------------------------------------------------------------------------
-// back_scan: the states' gradients, from the last chunk down; dR, dv.
+// back_scan: the states' gradients, from the last chunk down; dR, dv.  As the scan.
 // ---------------------------------------------------------------------------
-template <class M, int KP>
+template <class M, int KP, int BV>
 struct BackLds {
   MatX<M, KP, kC> kt, qt;
-  MatX<M, kBv, kC> ot;
-  Mat<M, kBv, KP> st;
-  Mat<M, kBv, kC> os, ut, rt;
+  MatX<M, BV, kC> ot;
+  Mat<M, BV, KP> st;
+  Mat<M, BV, kC> os, ut, rt;
 };
 
-template <class M, int KP>
+template <class M, int KP, int BV, bool ODD>
 __global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) {
   using IO = typename M::IO;
-  constexpr int KS = KP / 32, MT = KP / 64;
+  using Word = typename M::Word;
+  constexpr int KS = KP / 32, MT = KP / 64, NV = BV / 16;
   extern __shared__ __align__(16) char lds[];
-  BackLds<M, KP>& s = *reinterpret_cast<BackLds<M, KP>*>(lds);
+  BackLds<M, KP, BV>& s = *reinterpret_cast<BackLds<M, KP, BV>*>(lds);
   const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
-  const int v0 = blockIdx.x * kBv, h = blockIdx.y, b = blockIdx.z, hk = h / (a.H / a.Hk);
+  const int v0 = blockIdx.x * BV, h = blockIdx.y, b = blockIdx.z, hk = h / (a.H / a.Hk);
   const int len = length_of(a, b), chunks = (len + kC - 1) / kC;
   const int64_t bh = int64_t(b) * a.H + h;
   const IO* kb = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
@@ -491,70 +701,123 @@ __global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) 
   IO* gvb = static_cast<IO*>(a.gv) + bh * a.V;
   const int64_t gv_t = int64_t(a.batch) * a.H * a.V;
 
-  f32x4 S[MT][2];  // dS'
+  f32x4 S[MT][NV];  // dS'
   auto state_at = [&](int m, int nt, int x) { return (bh * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
   auto state_in = [&](int m, int nt, int x) { return (MT * w + m) * 16 + q4 * 4 + x < a.K && v0 + nt * 16 + r < a.V; };
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
+    for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
       for (int x = 0; x < 4; ++x) S[m][nt][x] = a.gs_last && state_in(m, nt, x) ? a.gs_last[state_at(m, nt, x)] : 0.0f;
 
-  for (int c = chunks - 1; c >= 0; --c) {
-    const int t0 = c * kC, n = min(len - t0, kC), row = 16 * w + r, i0 = 16 * w + q4 * 4;
-    const int64_t at = bh * a.nc + c;
-    const float* dec = a.dec + at * 3 * kC;
-    const f32x4 eg = *reinterpret_cast<const f32x4*>(dec + i0), tail = *reinterpret_cast<const f32x4*>(dec + kC + i0),
-                beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
-    const float whole = dec[kC - 1];
-    __syncthreads();
-    fill_turned<M, KP>(s.kt, kb + t0 * a.k_t, a.k_t, n, a.K);
-    fill_turned<M, KP>(s.qt, qb + t0 * a.q_t, a.q_t, n, a.K);
+  const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
+  constexpr bool odd = ODD;  // K is no multiple of 8
+  int vc[NV];
+  bool vin[NV];
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-      IO go[4];
+  for (int nt = 0; nt < NV; ++nt) {
+    vin[nt] = v0 + nt * 16 + r < a.V;
+    vc[nt] = vin[nt] ? v0 + nt * 16 + r : 0;
+  }
+  Turn<M, KP> kturn, qturn;
+  Exact<M> kf[KS];
+  Both<M> tf[2], pf[2];
+  f32x4 eg, tail, beta;
+  float whole;
+  IO go[NV][4];
+  auto load_turn = [&](int c) {
+    kturn.load(kb + c * kC * a.k_t, a.k_t, min(len - c * kC, kC), a.K, odd);
+    qturn.load(qb + c * kC * a.q_t, a.q_t, min(len - c * kC, kC), a.K, odd);
+  };
+  auto load_rows = [&](int c) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) kf[k] = exact_of<M>(load8(kb + min(c * kC + row, len - 1) * a.k_t, k * 32 + q4 * 8, a.K, odd));
+  };
+  auto load_go = [&](int c) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt) go[nt][x] = gob[min(c * kC + i0 + x, len - 1) * a.go_t + vc[nt]];
+  };
+  auto load_t = [&](int c) {  // T and P turned are upper
+    const Word* tm = static_cast<const Word*>(a.tm) + (bh * a.nc + c) * M::planes * kC * kC;
+    if (w < 2) tf[0] = load_planes<M>(tm, row, q4 * 8);
+    tf[1] = load_planes<M>(tm, row, 32 + q4 * 8);
+  };
+  auto load_p = [&](int c) {
+    const Word* pm = static_cast<const Word*>(a.pm) + (bh * a.nc + c) * M::planes * kC * kC;
+    if (w < 2) pf[0] = load_planes<M>(pm, row, q4 * 8);
+    pf[1] = load_planes<M>(pm, row, 32 + q4 * 8);
+  };
+  auto load_dec = [&](int c) {
+    const float* dec = a.dec + (bh * a.nc + c) * 3 * kC;
+    eg = *reinterpret_cast<const f32x4*>(dec + i0);
+    tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
+    beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
+    whole = dec[kC - 1];
+  };
+  // of the next chunk down: its state's gradient and its turned inputs
+  auto put_chunk = [&](int c) {
+    kturn.put(s.kt, a.K);
+    qturn.put(s.qt, a.K);
+#pragma unroll
+    for (int nt = 0; nt < NV; ++nt) {
       f32x4 os;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        go[x] = i0 + x < n && v0 + nt * 16 + r < a.V ? gob[(t0 + i0 + x) * a.go_t + v0 + nt * 16 + r] : IO{};
-        os[x] = a.scale * eg[x] * widen(go[x]);
+        if (c * kC + i0 + x >= len || !vin[nt]) go[nt][x] = IO{};
+        os[x] = a.scale * eg[x] * widen(go[nt][x]);
       }
-      s.ot.put4(nt * 16 + r, i0, go[0], go[1], go[2], go[3]);
+      using E = Eight<IO>;
+      s.ot.put4(nt * 16 + r, i0, E::bits(go[nt][0]), E::bits(go[nt][1]), E::bits(go[nt][2]), E::bits(go[nt][3]));
       s.os.put4(nt * 16 + r, i0, os);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
+    }
+  };
+  if (chunks > 0) {
+    load_turn(chunks - 1);
+    load_go(chunks - 1);
+    load_dec(chunks - 1);
+    load_rows(chunks - 1);
+    load_t(chunks - 1);
+    load_p(chunks - 1);
+    put_chunk(chunks - 1);
+    lds_barrier();
+  }
+  for (int c = chunks - 1; c >= 0; --c) {
+    const int t0 = c * kC, n = min(len - t0, kC);
+    const int64_t at = bh * a.nc + c;
+    if (c > 0) {
+      load_turn(c - 1);
+      load_go(c - 1);
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-        s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
-        float* to = a.ds + (at * KP + (MT * w + m) * 16 + q4 * 4) * a.Vp + v0 + nt * 16 + r;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = S[m][nt][x];
-      }
-    Exact<M> kf[KS];
-#pragma unroll
-    for (int k = 0; k < KS; ++k) kf[k] = exact_of(load8(kb + (t0 + row) * a.k_t, k * 32 + q4 * 8, a.K, row < n));
-    Both<M> tf[2], pf[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      tf[k] = load_both<M>(a.tm + at * kC * kC + row * kC + k * 32 + q4 * 8);
-      pf[k] = load_both<M>(a.pm + at * kC * kC + row * kC + k * 32 + q4 * 8);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
+    for (int nt = 0; nt < NV; ++nt) {
       f32x4 U = {0, 0, 0, 0};
 #pragma unroll
       for (int k = 0; k < KS; ++k) mma(U, kf[k], s.st.frag(nt * 16, k * 32));
       U *= tail;
-      if (w < 2) mma(U, pf[0], s.ot.frag(nt * 16, 0));  // P turned is upper
+      if (w < 2) mma(U, pf[0], s.ot.frag(nt * 16, 0));
       mma(U, pf[1], s.ot.frag(nt * 16, 32));
       s.ut.put4(nt * 16 + r, i0, U);
     }
-    __syncthreads();
+    if (c > 0) {
+      load_rows(c - 1);
+      load_p(c - 1);
+    }
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt) {
+        float* to = a.ds + (at * KP + (MT * w + m) * 16 + q4 * 4) * a.Vp + v0 + nt * 16 + r;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = S[m][nt][x];
+      }
+    lds_barrier();
+#pragma unroll
+    for (int nt = 0; nt < NV; ++nt) {
       f32x4 R = {0, 0, 0, 0}, rs;
       if (w < 2) mma(R, tf[0], s.ut.frag(nt * 16, 0));
       mma(R, tf[1], s.ut.frag(nt * 16, 32));
@@ -562,73 +825,95 @@ __global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) 
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         to[int64_t(x) * a.Vp] = R[x];
-        const float dv = beta[x] * R[x];
-        rs[x] = -eg[x] * dv;
-        if (i0 + x < n && v0 + nt * 16 + r < a.V) gvb[(t0 + i0 + x) * gv_t + v0 + nt * 16 + r] = narrow<IO>(dv);
+        R[x] *= beta[x];
+        rs[x] = -eg[x] * R[x];
+      }
+      if (n == kC && v0 + BV <= a.V) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) gvb[(t0 + i0 + x) * gv_t + v0 + nt * 16 + r] = narrow<IO>(R[x]);
+      } else {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (i0 + x < n && vin[nt]) gvb[(t0 + i0 + x) * gv_t + v0 + nt * 16 + r] = narrow<IO>(R[x]);
       }
       s.rt.put4(nt * 16 + r, i0, rs);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         S[m][nt] *= whole;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          mma(S[m][nt], s.qt.frag((MT * w + m) * 16, k * 32), s.os.frag(nt * 16, k * 32));
-          mma(S[m][nt], s.kt.frag((MT * w + m) * 16, k * 32), s.rt.frag(nt * 16, k * 32));
-        }
+        for (int k = 0; k < 2; ++k) mma(S[m][nt], s.qt.frag((MT * w + m) * 16, k * 32), s.os.frag(nt * 16, k * 32));
       }
+    }
+    if (c > 0) {
+      load_t(c - 1);
+      load_dec(c - 1);
+    }
+    lds_barrier();
+#pragma unroll
+    for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) mma(S[m][nt], s.kt.frag((MT * w + m) * 16, k * 32), s.rt.frag(nt * 16, k * 32));
+    if (c > 0) {
+      lds_barrier();
+      put_chunk(c - 1);
+      lds_barrier();
+    }
   }
   if (a.gs0) {
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
+      for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           if (state_in(m, nt, x)) a.gs0[state_at(m, nt, x)] = S[m][nt][x];
   }
-  for (int u = threadIdx.x; u < a.T - len; u += kThreads)
-    for (int d = v0; d < min(v0 + kBv, a.V); ++d) gvb[(len + u) * gv_t + d] = IO{};
+  for (int64_t u = threadIdx.x; u < int64_t(a.T - len) * BV; u += kThreads)
+    if (v0 + u % BV < a.V) gvb[(len + u / BV) * gv_t + v0 + u % BV] = IO{};
 }
 
 // ---------------------------------------------------------------------------
-// back_local: gradients of q, k, g and beta of one chunk.
+// back_local: gradients of q, k, g and beta of one chunk.  Wave (w, half) has steps 16 w to + 15
+// and half of q's and k's places; sums over v go 32 columns at a time, the next ones' operands
+// on their way meanwhile.
 // ---------------------------------------------------------------------------
+constexpr int kVpad = 32;      // columns of v at a time; rows in memory are filled up to a multiple
+constexpr int kLocalThreads = 512;
+
 template <class M, int KP>
 struct LocalLds {
   MatX<M, KP, kC> kt, qt;
   union {
     struct {
-      Mat<M, KP, kBv> s0, ds;
-      Mat<M, kC, kBv> u;
+      Mat<M, KP, kVpad> s0, ds;
+      Mat<M, kC, kVpad> u;
     } a;
     struct {
       Mat<M, kC, kC> e, et, f, ft;
     } b;
   };
   double g[kC];
-  float dg[kC], rv[kC], kd[kC], diag[kC], part[4];
+  float dg[2][kC], kx[2][kC], kd[2][kC], rv[kC], diag[kC], part[8];
 };
 
 template <class M, int KP>
-__global__ __launch_bounds__(kThreads) void delta_back_local_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(kLocalThreads) void delta_back_local_kernel(DeltaArgs a) {
   using IO = typename M::IO;
-  constexpr int NT = KP / 16;
+  constexpr int NT = KP / 32, kQuads = KP * kVpad / 4 / kLocalThreads;  // tiles of a wave; f32x4 of a state a thread
   extern __shared__ __align__(16) char lds[];
   LocalLds<M, KP>& s = *reinterpret_cast<LocalLds<M, KP>*>(lds);
-  const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, w = wave % 4, half = wave / 4, r = lane % 16, q4 = lane / 16;
   const int c = blockIdx.x, h = blockIdx.y, b = blockIdx.z, share = a.H / a.Hk, hk = h / share;
   const int len = length_of(a, b), t0 = c * kC, n = min(len - t0, kC), there = min(a.T - t0, kC);
   const int64_t bh = int64_t(b) * a.H + h, at = bh * a.nc + c;
   // gradients are contiguous; those of shared heads are summed by a kernel of their own
-  float* part_q = share > 1 ? a.part_q + (t0 * int64_t(a.batch) * a.H + bh) * a.K : nullptr;
-  float* part_k = share > 1 ? a.part_k + (t0 * int64_t(a.batch) * a.H + bh) * a.K : nullptr;
-  const int64_t tk = int64_t(a.batch) * a.Hk, th = int64_t(a.batch) * a.H;
-  IO* gq = static_cast<IO*>(a.gq) + (t0 * tk + int64_t(b) * a.Hk + hk) * a.K;
-  IO* gk = static_cast<IO*>(a.gk) + (t0 * tk + int64_t(b) * a.Hk + hk) * a.K;
+  const int64_t tk = int64_t(a.batch) * a.Hk * a.K, th = int64_t(a.batch) * a.H;
+  float* part_q = share > 1 ? a.part_q + (t0 * th + bh) * a.K : nullptr;
+  float* part_k = share > 1 ? a.part_k + (t0 * th + bh) * a.K : nullptr;
+  IO* gq = static_cast<IO*>(a.gq) + t0 * tk + (int64_t(b) * a.Hk + hk) * a.K;
+  IO* gk = static_cast<IO*>(a.gk) + t0 * tk + (int64_t(b) * a.Hk + hk) * a.K;
   IO* gg = static_cast<IO*>(a.gg) + t0 * th + bh;
   IO* gbeta = static_cast<IO*>(a.gbeta) + t0 * th + bh;
   auto put_qk = [&](int i, int d, float q, float k) {
@@ -636,13 +921,13 @@ __global__ __launch_bounds__(kThreads) void delta_back_local_kernel(DeltaArgs a)
       part_q[i * th * a.K + d] = q;
       part_k[i * th * a.K + d] = k;
     } else {
-      gq[i * tk * a.K + d] = narrow<IO>(q);
-      gk[i * tk * a.K + d] = narrow<IO>(k);
+      gq[i * tk + d] = narrow<IO>(q);
+      gk[i * tk + d] = narrow<IO>(k);
     }
   };
   // steps past the end
-  for (int u = threadIdx.x + max(n, 0) * a.K; u < there * a.K; u += kThreads) put_qk(u / a.K, u % a.K, 0.0f, 0.0f);
-  for (int i = threadIdx.x + max(n, 0); i < there; i += kThreads) gg[i * th] = gbeta[i * th] = IO{};
+  for (int u = threadIdx.x + max(n, 0) * a.K; u < there * a.K; u += kLocalThreads) put_qk(u / a.K, u % a.K, 0.0f, 0.0f);
+  for (int i = threadIdx.x + max(n, 0); i < there; i += kLocalThreads) gg[i * th] = gbeta[i * th] = IO{};
   if (n <= 0) return;
 
   const IO* kb = static_cast<const IO*>(a.k) + t0 * a.k_t + b * a.k_b + hk * a.k_h;
@@ -654,50 +939,71 @@ __global__ __launch_bounds__(kThreads) void delta_back_local_kernel(DeltaArgs a)
   const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
   const float whole = dec[kC - 1];
 
-  const double G = chunk_sum<IO>(a, b, h, t0, n);
-  if (w == 0) s.g[lane] = G;
-  fill_turned<M, KP>(s.kt, kb, a.k_t, n, a.K);
-  fill_turned<M, KP>(s.qt, qb, a.q_t, n, a.K);
+  // what 32 columns of v need, in registers
+  f32x4 ps[kQuads], pd[kQuads], pu;
+  typename Eight<IO>::Vec po, pv;
+  f32x8 pr;
+  auto load = [&](int v0) {
+#pragma unroll
+    for (int u = 0; u < kQuads; ++u) {
+      const int e = u * kLocalThreads + threadIdx.x, d = e / 8, v = v0 + e % 8 * 4;
+      ps[u] = *reinterpret_cast<const f32x4*>(ck_s + int64_t(d) * a.Vp + v);
+      pd[u] = *reinterpret_cast<const f32x4*>(ds + int64_t(d) * a.Vp + v);
+    }
+    pu = *reinterpret_cast<const f32x4*>(ck_u + int64_t(threadIdx.x / 8) * a.Vp + v0 + threadIdx.x % 8 * 4);
+    // (values past V meet zeros, of U, S and dR; rows past the end are the last one's, but for do)
+    po = load8(gob + min(row, n - 1) * a.go_t, v0 + q4 * 8, a.V, a.V % 8);
+    if (half == 0) pv = load8(vb + min(row, n - 1) * a.v_t, v0 + q4 * 8, a.V, a.V % 8);
+    pr = *reinterpret_cast<const f32x8*>(dr + int64_t(row) * a.Vp + v0 + q4 * 8);
+  };
+  {
+    Turn<M, KP> turn;
+    if (half == 0) turn.load(kb, a.k_t, n, a.K, a.K % 8);
+    else turn.load(qb, a.q_t, n, a.K, a.K % 8);
+    load(0);
+    const double G = chunk_sum<IO>(a, b, h, t0, n);
+    if (wave == 0) s.g[lane] = G;
+    turn.put(half == 0 ? s.kt : s.qt, a.K);
+  }
 
-  f32x4 dq[NT], X[NT], Y[NT], e[4], f[4];
+  f32x4 dq[NT], X[NT], Y[NT], e[2], f[2];
 #pragma unroll
   for (int t = 0; t < NT; ++t) dq[t] = X[t] = Y[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int t = 0; t < 4; ++t) e[t] = f[t] = f32x4{0, 0, 0, 0};
+  for (int t = 0; t < 2; ++t) e[t] = f[t] = f32x4{0, 0, 0, 0};
   float rv = 0.0f, sds = 0.0f;  // dR.v of row `row` (a quarter of it), <S, dS'>
-  for (int v0 = 0; v0 < a.Vp; v0 += kBv) {
-    __syncthreads();
-    for (int u = threadIdx.x; u < KP * kBv / 4; u += kThreads) {
-      const int d = u / (kBv / 4), v = u % (kBv / 4) * 4;
-      const f32x4 x = *reinterpret_cast<const f32x4*>(ck_s + int64_t(d) * a.Vp + v0 + v);
-      const f32x4 y = *reinterpret_cast<const f32x4*>(ds + int64_t(d) * a.Vp + v0 + v);
-      sds += (x[0] * y[0] + x[1] * y[1]) + (x[2] * y[2] + x[3] * y[3]);
-      s.a.s0.put4(d, v, x);
-      s.a.ds.put4(d, v, y);
-    }
-    for (int u = threadIdx.x; u < kC * kBv / 4; u += kThreads) {
-      const int i = u / (kBv / 4), v = u % (kBv / 4) * 4;
-      s.a.u.put4(i, v, *reinterpret_cast<const f32x4*>(ck_u + int64_t(i) * a.Vp + v0 + v));
-    }
-    const Exact<M> of = exact_of(load8(gob + row * a.go_t, v0 + q4 * 8, a.V, row < n));
-    const Pack<IO, 8> vp = load8(vb + row * a.v_t, v0 + q4 * 8, a.V, row < n);
-    const float* drp = dr + int64_t(row) * a.Vp + v0 + q4 * 8;
+  for (int v0 = 0; v0 < a.Vp; v0 += kVpad) {
+    if (v0 > 0) lds_barrier();
 #pragma unroll
-    for (int j = 0; j < 8; ++j) rv = fmaf(drp[j], widen(vp.v[j]), rv);
-    const Both<M> rf = load_both<M>(drp);
-    __syncthreads();
+    for (int u = 0; u < kQuads; ++u) {
+      const int e1 = u * kLocalThreads + threadIdx.x, d = e1 / 8, v = e1 % 8 * 4;
+      sds += (ps[u][0] * pd[u][0] + ps[u][1] * pd[u][1]) + (ps[u][2] * pd[u][2] + ps[u][3] * pd[u][3]);
+      s.a.s0.put4(d, v, ps[u]);
+      s.a.ds.put4(d, v, pd[u]);
+    }
+    s.a.u.put4(threadIdx.x / 8, threadIdx.x % 8 * 4, pu);
+    if (row >= n) po = 0;
+    const Exact<M> of = exact_of<M>(po);
+    if (half == 0) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) rv = fmaf(pr[j], Eight<IO>::wide(pv[j]), rv);
+    }
+    Both<M> rf;
+    both_of(pr, rf);
+    if (v0 + kVpad < a.Vp) load(v0 + kVpad);
+    lds_barrier();
     const Both<M> uf = s.a.u.frag(16 * w, 0);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const Both<M> sf = s.a.s0.frag(t * 16, 0);
+      const Both<M> sf = s.a.s0.frag((half * NT + t) * 16, 0);
       mma(dq[t], of, sf);
       mma(X[t], rf, sf);
-      mma(Y[t], uf, s.a.ds.frag(t * 16, 0));
+      mma(Y[t], uf, s.a.ds.frag((half * NT + t) * 16, 0));
     }
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      if (t <= w) {
-        const Both<M> u2 = s.a.u.frag(t * 16, 0);
+    for (int t = 0; t < 2; ++t) {
+      if (2 * half + t <= w) {
+        const Both<M> u2 = s.a.u.frag((2 * half + t) * 16, 0);
         mma(e[t], of, u2);
         mma(f[t], rf, u2);
       }
@@ -705,12 +1011,13 @@ __global__ __launch_bounds__(kThreads) void delta_back_local_kernel(DeltaArgs a)
   }
   rv += __shfl_xor(rv, 16);
   rv += __shfl_xor(rv, 32);
-  if (q4 == 0) s.rv[row] = rv;
+  if (half == 0 && q4 == 0) s.rv[row] = rv;
 #pragma unroll
   for (int x = 32; x > 0; x /= 2) sds += __shfl_xor(sds, x);
+  if (lane == 0) s.part[wave] = whole * sds;
   const f32x4 eg = *reinterpret_cast<const f32x4*>(dec + i0), tail = *reinterpret_cast<const f32x4*>(dec + kC + i0),
               beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
-  __syncthreads();
+  lds_barrier();
   f32x4 kd = {0, 0, 0, 0}, Y2[NT];  // k.Y of dS' alone; the rest of Y
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
@@ -718,12 +1025,11 @@ __global__ __launch_bounds__(kThreads) void delta_back_local_kernel(DeltaArgs a)
     X[t] *= -eg;
     Y[t] *= tail;
     Y2[t] = f32x4{0, 0, 0, 0};
-    kd += s.kt.get4(t * 16 + r, i0) * Y[t];
+    kd += s.kt.get4((half * NT + t) * 16 + r, i0) * Y[t];
   }
-  if (lane == 0) s.part[w] = whole * sds;
 #pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int j = 16 * t + r;
+  for (int t = 0; t < 2; ++t) {
+    const int j = 16 * (2 * half + t) + r;
     f32x4 fb;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -739,31 +1045,41 @@ __global__ __launch_bounds__(kThreads) void delta_back_local_kernel(DeltaArgs a)
     s.b.et.put4(j, i0, e[t]);
     s.b.ft.put4(j, i0, fb);
   }
-  __syncthreads();
+  lds_barrier();
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const Both<M> ef = s.b.e.frag(16 * w, k * 32), etf = s.b.et.frag(16 * w, k * 32), ff = s.b.f.frag(16 * w, k * 32),
                   ftf = s.b.ft.frag(16 * w, k * 32);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const Exact<M> kf = s.kt.frag(t * 16, k * 32);
+      const Exact<M> kf = s.kt.frag((half * NT + t) * 16, k * 32);
       mma(dq[t], ef, kf);
       mma(X[t], ff, kf);
       mma(Y2[t], ftf, kf);
-      mma(Y2[t], etf, s.qt.frag(t * 16, k * 32));
+      mma(Y2[t], etf, s.qt.frag((half * NT + t) * 16, k * 32));
     }
   }
   const f32x4 diag = *reinterpret_cast<const f32x4*>(s.diag + i0);
   f32x4 dg = {0, 0, 0, 0}, kx = {0, 0, 0, 0};
+  const bool full = n == kC && a.K == KP && share == 1;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const f32x4 k = s.kt.get4(t * 16 + r, i0), q = s.qt.get4(t * 16 + r, i0);
+    const int d = (half * NT + t) * 16 + r;
+    const f32x4 k = s.kt.get4(d, i0), q = s.qt.get4(d, i0);
     dg += q * dq[t] - k * Y2[t];
     kx += k * X[t];
     const f32x4 gqv = dq[t] + diag * k, gkv = (beta * X[t] + Y[t]) + (Y2[t] + diag * q);
+    if (full) {
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-      if (i0 + x < n && t * 16 + r < a.K) put_qk(i0 + x, t * 16 + r, gqv[x], gkv[x]);
+      for (int x = 0; x < 4; ++x) {
+        gq[(i0 + x) * tk + d] = narrow<IO>(gqv[x]);
+        gk[(i0 + x) * tk + d] = narrow<IO>(gkv[x]);
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (i0 + x < n && d < a.K) put_qk(i0 + x, d, gqv[x], gkv[x]);
+    }
   }
   dg += beta * kx;
 #pragma unroll
@@ -775,17 +1091,14 @@ __global__ __launch_bounds__(kThreads) void delta_back_local_kernel(DeltaArgs a)
       kd[x] += __shfl_xor(kd[x], m);
     }
   if (r == 0) {
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      s.dg[i0 + x] = dg[x];
-      s.kd[i0 + x] = kd[x];
-      if (i0 + x < n) gbeta[(i0 + x) * th] = narrow<IO>(s.rv[i0 + x] + kx[x]);
-    }
+    *reinterpret_cast<f32x4*>(&s.dg[half][i0]) = dg;
+    *reinterpret_cast<f32x4*>(&s.kx[half][i0]) = kx;
+    *reinterpret_cast<f32x4*>(&s.kd[half][i0]) = kd;
   }
-  __syncthreads();
-  if (w == 0) {
+  lds_barrier();
+  if (wave == 0) {
     // sums from the last step down and from the first up, in 64 bits: terms cancel
-    double after = s.dg[lane], upto = s.kd[lane];
+    double after = double(s.dg[0][lane]) + double(s.dg[1][lane]), upto = double(s.kd[0][lane]) + double(s.kd[1][lane]), held = 0.0;
     const double own = upto;
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) {
@@ -793,8 +1106,12 @@ __global__ __launch_bounds__(kThreads) void delta_back_local_kernel(DeltaArgs a)
       if (lane + x < 64) after += down;
       if (lane >= x) upto += up;
     }
-    const double held = (double(s.part[0]) + double(s.part[1])) + (double(s.part[2]) + double(s.part[3]));
-    if (lane < n) gg[lane * th] = narrow<IO>(float(after + (upto - own) + held));
+#pragma unroll
+    for (int x = 0; x < 8; ++x) held += double(s.part[x]);
+    if (lane < n) {
+      gg[lane * th] = narrow<IO>(float(after + (upto - own) + held));
+      gbeta[lane * th] = narrow<IO>(s.rv[lane] + (s.kx[0][lane] + s.kx[1][lane]));
+    }
   }
 }
 
@@ -817,6 +1134,8 @@ __global__ __launch_bounds__(256) void delta_join_kernel(const float* pq, const 
 // One token.  S^T k and S^T q come from one pass over the state, in registers:
 // o = scale (a S^T q + (q.k) u).  Bound by the state's bytes.
 // ---------------------------------------------------------------------------
+constexpr int kStepV = 32;  // columns of a block
+
 struct DeltaStepArgs {
   const void *q, *k, *v, *g, *beta;
   const int32_t* slots;
@@ -830,7 +1149,7 @@ struct DeltaStepArgs {
 template <typename IO>
 __global__ __launch_bounds__(kThreads) void delta_step_kernel(DeltaStepArgs a) {
   const int h = blockIdx.y, b = blockIdx.z, hk = h / a.share;
-  const int vl = threadIdx.x % 8 * 4, kl = threadIdx.x / 8, v = blockIdx.x * kBv + vl;
+  const int vl = threadIdx.x % 8 * 4, kl = threadIdx.x / 8, v = blockIdx.x * kStepV + vl;
   const int left = a.V - v;  // columns from this lane's first on
   IO* op = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h + v;
   const int64_t slot = a.slots ? a.slots[b] : b;
@@ -943,7 +1262,7 @@ dendsn_status check_cfg(const dendsn_delta_cfg* c) {
   if (!isfinite(c->scale)) return fail(DENDSN_E_INVALID, "scale must be finite");
   // a chunk's states and the padding of V
   if (!small_product(c->batch * c->H * 128, round_up(c->T + kC, kC)) ||
-      !small_product(c->batch * c->H * 128 * round_up(c->T + kC, kC) / kC * 4, round_up(c->V, kBv)))
+      !small_product(c->batch * c->H * 128 * round_up(c->T + kC, kC) / kC * 4, round_up(c->V, kVpad)))
     return fail(DENDSN_E_INVALID, "T * batch * H * V too large");
   const int64_t s[21] = {c->q_t, c->q_b, c->q_h, c->k_t, c->k_b, c->k_h, c->v_t, c->v_b, c->v_h, c->g_t, c->g_b, c->g_h,
                          c->beta_t, c->beta_b, c->beta_h, c->o_t, c->o_b, c->o_h, c->grad_o_t, c->grad_o_b, c->grad_o_h};
@@ -976,20 +1295,24 @@ struct DeltaPlan {
   size_t forward, backward;
 };
 
+using Wide = Bf<3>;    // of the scans: their states are outputs in fp32
+using Narrow = Bf<2>;  // of what ends in bf16
+
 DeltaPlan make_plan(const dendsn_delta_cfg* c) {
   DeltaPlan p{};
   if (empty(c)) return p;
   p.nc = ceil_div(c->T, kC);
   p.items = p.nc * c->batch * c->H;
-  p.Vp = round_up(c->V, kBv);
+  p.Vp = round_up(c->V, kVpad);
   p.KP = kp_of(c);
   Carve k;
   k.take(size_t(p.items) * p.KP * p.Vp * 4);
   p.ck_u = k.take(size_t(p.items) * kC * p.Vp * 4);
   p.ckpt = k.at;
   Carve w;
-  p.tm = w.take(size_t(p.items) * kC * kC * 4);
-  p.pm = w.take(size_t(p.items) * kC * kC * 4);
+  const size_t square = size_t(kC) * kC * (c->io == DENDSN_IO_BF16 ? 2 * Wide::planes : 4);
+  p.tm = w.take(size_t(p.items) * square);
+  p.pm = w.take(size_t(p.items) * square);
   p.dec = w.take(size_t(p.items) * 3 * kC * 4);
   p.forward = w.at;
   p.dr = w.take(size_t(p.items) * kC * p.Vp * 4);
@@ -1010,8 +1333,8 @@ void fill_args(const dendsn_delta_cfg* c, const DeltaPlan& p, void* workspace, D
   a.T = int32_t(c->T); a.batch = int32_t(c->batch); a.H = int32_t(c->H); a.Hk = int32_t(c->Hk);
   a.K = int32_t(c->K); a.V = int32_t(c->V); a.nc = int32_t(p.nc); a.Vp = int32_t(p.Vp); a.scale = c->scale;
   char* w = static_cast<char*>(workspace);
-  a.tm = reinterpret_cast<float*>(w + p.tm);
-  a.pm = reinterpret_cast<float*>(w + p.pm);
+  a.tm = w + p.tm;
+  a.pm = w + p.pm;
   a.dec = reinterpret_cast<float*>(w + p.dec);
   a.dr = reinterpret_cast<float*>(w + p.dr);
   a.ds = reinterpret_cast<float*>(w + p.ds);
@@ -1025,34 +1348,57 @@ bool allow_lds(F* kernel, size_t bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) == hipSuccess;
 }
 
-template <class M, int KP>
-dendsn_status launch_forward(const DeltaArgs& a, hipStream_t stream) {
-  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / kBv), unsigned(a.H), unsigned(a.batch));
-  constexpr size_t bytes = sizeof(ScanLds<M, KP>);
+template <class M, int KP, int BV, bool ODD>
+dendsn_status launch_scan(const DeltaArgs& a, hipStream_t stream) {
+  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / BV), unsigned(a.H), unsigned(a.batch));
+  constexpr size_t bytes = sizeof(ScanLds<M, KP, BV>);
   static_assert(bytes <= 160 * 1024, "LDS of a CU");
-  if (!allow_lds(delta_scan_kernel<M, KP>, bytes)) return fail(DENDSN_E_HIP, "delta forward: %zu bytes of LDS refused", bytes);
-  delta_local_kernel<M, KP, false><<<heads, dim3(64), 0, stream>>>(a);
-  delta_scan_kernel<M, KP><<<cols, dim3(kThreads), bytes, stream>>>(a);
+  if (!allow_lds(delta_scan_kernel<M, KP, BV, ODD>, bytes)) return fail(DENDSN_E_HIP, "delta forward: %zu bytes of LDS refused", bytes);
+  delta_local_kernel<M, KP, false><<<heads, dim3(kThreads), 0, stream>>>(a);
+  delta_scan_kernel<M, KP, BV, ODD><<<cols, dim3(kThreads), bytes, stream>>>(a);
   return launched("delta forward");
 }
 
+template <class M, int KP, int BV, bool ODD>
+dendsn_status launch_back_scan(const DeltaArgs& a, hipStream_t stream) {
+  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / BV), unsigned(a.H), unsigned(a.batch));
+  constexpr size_t bytes = sizeof(BackLds<M, KP, BV>);
+  static_assert(bytes <= 160 * 1024, "LDS of a CU");
+  if (!allow_lds(delta_back_scan_kernel<M, KP, BV, ODD>, bytes)) return fail(DENDSN_E_HIP, "delta backward: %zu bytes of LDS refused", bytes);
+  delta_local_kernel<M, KP, true><<<heads, dim3(kThreads), 0, stream>>>(a);
+  delta_back_scan_kernel<M, KP, BV, ODD><<<cols, dim3(kThreads), bytes, stream>>>(a);
+  return launched("delta backward");
+}
+
 template <class M, int KP>
-dendsn_status launch_backward(const DeltaArgs& a, hipStream_t stream) {
+dendsn_status launch_back_local(const DeltaArgs& a, hipStream_t stream) {
   using IO = typename M::IO;
-  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / kBv), unsigned(a.H), unsigned(a.batch));
-  constexpr size_t scan = sizeof(BackLds<M, KP>), local = sizeof(LocalLds<M, KP>);
-  static_assert(scan <= 160 * 1024 && local <= 160 * 1024, "LDS of a CU");
-  if (!allow_lds(delta_back_scan_kernel<M, KP>, scan) || !allow_lds(delta_back_local_kernel<M, KP>, local))
-    return fail(DENDSN_E_HIP, "delta backward: %zu bytes of LDS refused", scan > local ? scan : local);
-  delta_local_kernel<M, KP, true><<<heads, dim3(64), 0, stream>>>(a);
-  delta_back_scan_kernel<M, KP><<<cols, dim3(kThreads), scan, stream>>>(a);
-  delta_back_local_kernel<M, KP><<<heads, dim3(kThreads), local, stream>>>(a);
+  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch));
+  constexpr size_t bytes = sizeof(LocalLds<M, KP>);
+  static_assert(bytes <= 160 * 1024, "LDS of a CU");
+  if (!allow_lds(delta_back_local_kernel<M, KP>, bytes)) return fail(DENDSN_E_HIP, "delta backward: %zu bytes of LDS refused", bytes);
+  delta_back_local_kernel<M, KP><<<heads, dim3(kLocalThreads), bytes, stream>>>(a);
   if (a.H != a.Hk) {
     const int64_t rows = int64_t(a.T) * a.batch * a.Hk, blocks = ceil_div(rows * a.K, 256);
     delta_join_kernel<IO><<<dim3(unsigned(blocks < 65536 ? blocks : 65536)), dim3(256), 0, stream>>>(
         a.part_q, a.part_k, static_cast<IO*>(a.gq), static_cast<IO*>(a.gk), rows, a.K, a.H / a.Hk);
   }
   return launched("delta backward");
+}
+
+template <class M, class L, int KP>
+dendsn_status launch(const DeltaArgs& a, bool back, hipStream_t stream) {
+  constexpr int BV = kScanV;
+  const bool odd = a.K % 8;
+  if (!back) return odd ? launch_scan<M, KP, BV, true>(a, stream) : launch_scan<M, KP, BV, false>(a, stream);
+  const dendsn_status st = odd ? launch_back_scan<M, KP, BV, true>(a, stream) : launch_back_scan<M, KP, BV, false>(a, stream);
+  return st != DENDSN_OK ? st : launch_back_local<L, KP>(a, stream);
+}
+
+dendsn_status launch(const dendsn_delta_cfg* c, const DeltaArgs& a, bool back, hipStream_t stream) {
+  if (c->io == DENDSN_IO_BF16)
+    return kp_of(c) == 64 ? launch<Wide, Narrow, 64>(a, back, stream) : launch<Wide, Narrow, 128>(a, back, stream);
+  return kp_of(c) == 64 ? launch<F32, F32, 64>(a, back, stream) : launch<F32, F32, 128>(a, back, stream);
 }
 
 dendsn_status copy_states(const dendsn_delta_cfg* c, const float* from, float* to, hipStream_t stream, const char* what) {
@@ -1114,8 +1460,7 @@ dendsn_status dendsn_delta_forward(const dendsn_delta_cfg* cfg, const void* q, c
     a.ck_s = static_cast<float*>(ckpt);
     a.ck_u = reinterpret_cast<float*>(static_cast<char*>(ckpt) + p.ck_u);
   }
-  if (cfg->io == DENDSN_IO_BF16) return p.KP == 64 ? launch_forward<B16, 64>(a, stream) : launch_forward<B16, 128>(a, stream);
-  return p.KP == 64 ? launch_forward<F32, 64>(a, stream) : launch_forward<F32, 128>(a, stream);
+  return launch(cfg, a, false, stream);
 }
 
 dendsn_status dendsn_delta_backward(const dendsn_delta_cfg* cfg, const void* q, const void* k, const void* v,
@@ -1148,8 +1493,7 @@ dendsn_status dendsn_delta_backward(const dendsn_delta_cfg* cfg, const void* q, 
   a.gq = grad_q; a.gk = grad_k; a.gv = grad_v; a.gg = grad_g; a.gbeta = grad_beta; a.gs0 = grad_s0;
   a.ck_s = static_cast<float*>(const_cast<void*>(ckpt));
   a.ck_u = reinterpret_cast<float*>(static_cast<char*>(const_cast<void*>(ckpt)) + p.ck_u);
-  if (cfg->io == DENDSN_IO_BF16) return p.KP == 64 ? launch_backward<B16, 64>(a, stream) : launch_backward<B16, 128>(a, stream);
-  return p.KP == 64 ? launch_backward<F32, 64>(a, stream) : launch_backward<F32, 128>(a, stream);
+  return launch(cfg, a, true, stream);
 }
 
 dendsn_status dendsn_delta_step(const dendsn_delta_cfg* cfg, const void* q, const void* k, const void* v,
@@ -1173,7 +1517,7 @@ dendsn_status dendsn_delta_step(const dendsn_delta_cfg* cfg, const void* q, cons
   const DeltaStepArgs a{q, k, v, g, beta, slots, state, o, cfg->q_b, cfg->q_h, cfg->k_b, cfg->k_h, cfg->v_b, cfg->v_h,
                         cfg->g_b, cfg->g_h, cfg->beta_b, cfg->beta_h, cfg->o_b, cfg->o_h, n_slots,
                         int32_t(cfg->H), int32_t(cfg->H / cfg->Hk), int32_t(cfg->K), int32_t(cfg->V), cfg->scale};
-  const dim3 grid(unsigned(ceil_div(cfg->V, kBv)), unsigned(cfg->H), unsigned(cfg->batch));
+  const dim3 grid(unsigned(ceil_div(cfg->V, kStepV)), unsigned(cfg->H), unsigned(cfg->batch));
   if (cfg->io == DENDSN_IO_BF16) delta_step_kernel<bf16_t><<<grid, dim3(kThreads), 0, stream>>>(a);
   else delta_step_kernel<float><<<grid, dim3(kThreads), 0, stream>>>(a);
   return launched("delta step");
