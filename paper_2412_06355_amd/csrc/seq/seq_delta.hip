@@ -143,16 +143,28 @@ template <> struct Eight<bf16_t> {
   static __device__ __forceinline__ float wide(uint16_t v) { return widen(bf16_t{v}); }
 };
 
-// Eight places of a row of K from k0 on, without a branch a lane: what lies past K has some
-// other value of the row.  odd (K is no multiple of 8): value by value.
+// The value `at` places behind a base that is the same in all lanes: 64 steps of a tensor span
+// less than 2^32 bytes, and addresses are a scalar and 32 bits.
+template <typename T>
+__device__ __forceinline__ const T& behind(const T* base, uint32_t at) {
+  return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + uint32_t(at * uint32_t(sizeof(T))));
+}
+template <typename T>
+__device__ __forceinline__ T& behind(T* base, uint32_t at) {
+  return *reinterpret_cast<T*>(reinterpret_cast<char*>(base) + uint32_t(at * uint32_t(sizeof(T))));
+}
+
+// Eight places from k0 on of the row of K that starts `row` places behind base, without a branch a
+// lane: what lies past K has some other value of the row.  odd (K is no multiple of 8): value
+// by value.
 template <typename IO>
-__device__ __forceinline__ typename Eight<IO>::Vec load8(const IO* row, int k0, int K, bool odd) {
+__device__ __forceinline__ typename Eight<IO>::Vec load8(const IO* base, uint32_t row, int k0, int K, bool odd) {
   typename Eight<IO>::Vec r;
   if (!odd) {
-    r = *reinterpret_cast<const typename Eight<IO>::Any*>(row + (k0 < K ? k0 : 0));
+    r = *reinterpret_cast<const typename Eight<IO>::Any*>(&behind(base, row + (k0 < K ? k0 : 0)));
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) r[j] = Eight<IO>::bits(row[min(k0 + j, K - 1)]);
+    for (int j = 0; j < 8; ++j) r[j] = Eight<IO>::bits(behind(base, row + min(k0 + j, K - 1)));
   }
   return r;
 }
@@ -255,11 +267,11 @@ template <class M, int ROWS> struct Turn {
   __device__ __forceinline__ static int tid() { return threadIdx.x % kThreads; }
   typename Eight<IO>::Vec r[4];
   // steps past the n-th have the n-th's values
-  __device__ __forceinline__ void load(const IO* rows, int64_t stride, int n, int D, bool odd) {
+  __device__ __forceinline__ void load(const IO* rows, uint32_t stride, int n, int D, bool odd) {
     const int t = tid() % 16 * 4, d = tid() / 16 * 8;
     if (!kAll && tid() >= 2 * ROWS) return;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) r[x] = load8(rows + min(t + x, n - 1) * stride, d, D, odd);
+    for (int x = 0; x < 4; ++x) r[x] = load8(rows, uint32_t(min(t + x, n - 1)) * stride, d, D, odd);
   }
   __device__ __forceinline__ void put(MatX<M, ROWS, kC>& dst, int D) {
     const int t = tid() % 16 * 4, d = tid() / 16 * 8;
@@ -362,11 +374,11 @@ __global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
   typename Eight<IO>::Vec kr[3][KS], own[KS], qr[KS];  // rows of the blocks before, of the wave's own
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
-    qr[s] = load8(qp + min(row, n - 1) * a.q_t, s * 32 + q4 * 8, a.K, odd);
-    own[s] = load8(kp + min(row, n - 1) * a.k_t, s * 32 + q4 * 8, a.K, odd);
+    qr[s] = load8(qp, uint32_t(min(row, n - 1)) * uint32_t(a.q_t), s * 32 + q4 * 8, a.K, odd);
+    own[s] = load8(kp, uint32_t(min(row, n - 1)) * uint32_t(a.k_t), s * 32 + q4 * 8, a.K, odd);
 #pragma unroll
     for (int bj = 0; bj < 3; ++bj)
-      if (bj < w) kr[bj][s] = load8(kp + min(16 * bj + r, n - 1) * a.k_t, s * 32 + q4 * 8, a.K, odd);
+      if (bj < w) kr[bj][s] = load8(kp, uint32_t(min(16 * bj + r, n - 1)) * uint32_t(a.k_t), s * 32 + q4 * 8, a.K, odd);
   }
   if (w == 3) {  // (the wave with the most products waits least)
     const double G = chunk_sum<IO>(a, b, h, t0, n);
@@ -480,6 +492,16 @@ __global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
 // fetched while the one before is computed, into the registers that it no longer needs; the
 // barriers wait for LDS alone.
 // ---------------------------------------------------------------------------
+// Blocks go to the eight XCDs in turn, each of which has a cache of its own: the blocks of one
+// head, which read the same q, k, T and P, are eight apart.
+struct ScanBlock {
+  int v0, bh;
+};
+__device__ __forceinline__ ScanBlock scan_block(const DeltaArgs& a, int BV) {
+  const int cols = a.Vp / BV, m = blockIdx.x / 8, bh = m / cols * 8 + blockIdx.x % 8;
+  return {m % cols * BV, bh < a.batch * a.H ? bh : -1};
+}
+
 template <class M, int KP, int BV>
 struct ScanLds {
   MatX<M, KP, kC> kt[2];
@@ -495,9 +517,11 @@ __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
   extern __shared__ __align__(16) char lds[];
   ScanLds<M, KP, BV>& s = *reinterpret_cast<ScanLds<M, KP, BV>*>(lds);
   const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
-  const int v0 = blockIdx.x * BV, h = blockIdx.y, b = blockIdx.z, hk = h / (a.H / a.Hk);
-  const int len = length_of(a, b), chunks = (len + kC - 1) / kC;
-  const int64_t bh = int64_t(b) * a.H + h;
+  const ScanBlock at_block = scan_block(a, BV);
+  const int v0 = at_block.v0, bh = at_block.bh;
+  if (bh < 0) return;
+  const int b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
+  const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), chunks = (len + kC - 1) / kC;
   const IO* kb = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
   const IO* qb = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h;
   const IO* vb = static_cast<const IO*>(a.v) + b * a.v_b + h * a.v_h;
@@ -505,7 +529,7 @@ __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
 
   // the state: rows 16 (MT w + m) + 4 q4 + x, columns 16 nt + r
   f32x4 S[MT][NV];
-  auto state_at = [&](int m, int nt, int x) { return (bh * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
+  auto state_at = [&](int m, int nt, int x) { return (int64_t(bh) * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
   auto state_in = [&](int m, int nt, int x) { return (MT * w + m) * 16 + q4 * 4 + x < a.K && v0 + nt * 16 + r < a.V; };
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -518,12 +542,12 @@ __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
   // Rows past the sequence's end are read as its last one, columns past K and V as some other:
   // their betas are 0, their rows of the state stay 0 (Turn), their values are set to 0.
   constexpr bool odd = ODD;  // K is no multiple of 8
-  int vc[NV];
+  uint32_t vat[NV];
   bool vin[NV];
 #pragma unroll
   for (int nt = 0; nt < NV; ++nt) {
     vin[nt] = v0 + nt * 16 + r < a.V;
-    vc[nt] = vin[nt] ? v0 + nt * 16 + r : 0;
+    vat[nt] = vin[nt] ? v0 + nt * 16 + r : 0;
   }
   Turn<M, KP> turn;
   Exact<M> kf[KS], qf[KS];
@@ -532,30 +556,32 @@ __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
   float whole;
   IO vv[NV][4];
   auto load_rows = [&](int c) {
-    const int t0 = c * kC, end = len - 1;
+    const int t0 = c * kC, end = min(len - t0, kC) - 1;
+    const uint32_t at = min(row, end);
+    const IO *kc = kb + t0 * a.k_t, *qc = qb + t0 * a.q_t, *vc = vb + t0 * a.v_t;
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
-      kf[k] = exact_of<M>(load8(kb + min(t0 + row, end) * a.k_t, k * 32 + q4 * 8, a.K, odd));
-      qf[k] = exact_of<M>(load8(qb + min(t0 + row, end) * a.q_t, k * 32 + q4 * 8, a.K, odd));
+      kf[k] = exact_of<M>(load8(kc, at * uint32_t(a.k_t), k * 32 + q4 * 8, a.K, odd));
+      qf[k] = exact_of<M>(load8(qc, at * uint32_t(a.q_t), k * 32 + q4 * 8, a.K, odd));
     }
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
-      for (int nt = 0; nt < NV; ++nt) vv[nt][x] = vb[min(t0 + i0 + x, end) * a.v_t + vc[nt]];
+      for (int nt = 0; nt < NV; ++nt) vv[nt][x] = behind(vc, uint32_t(min(i0 + x, end)) * uint32_t(a.v_t) + vat[nt]);
   };
   auto load_turn = [&](int c) { turn.load(kb + c * kC * a.k_t, a.k_t, min(len - c * kC, kC), a.K, odd); };
   auto load_t = [&](int c) {
-    const Word* tm = static_cast<const Word*>(a.tm) + (bh * a.nc + c) * M::planes * kC * kC;
+    const Word* tm = static_cast<const Word*>(a.tm) + (int64_t(bh) * a.nc + c) * M::planes * kC * kC;
     tf[0] = load_planes<M>(tm, row, q4 * 8);
     if (w >= 2) tf[1] = load_planes<M>(tm, row, 32 + q4 * 8);  // T is lower
   };
   auto load_p = [&](int c) {
-    const Word* pm = static_cast<const Word*>(a.pm) + (bh * a.nc + c) * M::planes * kC * kC;
+    const Word* pm = static_cast<const Word*>(a.pm) + (int64_t(bh) * a.nc + c) * M::planes * kC * kC;
     pf[0] = load_planes<M>(pm, row, q4 * 8);
     if (w >= 2) pf[1] = load_planes<M>(pm, row, 32 + q4 * 8);
   };
   auto load_dec = [&](int c) {
-    const float* dec = a.dec + (bh * a.nc + c) * 3 * kC;
+    const float* dec = a.dec + (int64_t(bh) * a.nc + c) * 3 * kC;
     eg = *reinterpret_cast<const f32x4*>(dec + i0);
     tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
     beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
@@ -579,7 +605,7 @@ __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
   }
   for (int c = 0; c < chunks; ++c) {
     const int t0 = c * kC, n = min(len - t0, kC);
-    const int64_t at = bh * a.nc + c;
+    const int64_t at = int64_t(bh) * a.nc + c;
     const bool more = c + 1 < chunks;
     if (more) load_turn(c + 1);
     f32x4 o[NV];
@@ -606,9 +632,9 @@ __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int nt = 0; nt < NV; ++nt) {
-          float* to = a.ck_s + (at * KP + (MT * w + m) * 16 + q4 * 4) * a.Vp + v0 + nt * 16 + r;
 #pragma unroll
-          for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = S[m][nt][x];
+          for (int x = 0; x < 4; ++x)
+            behind(a.ck_s + at * KP * a.Vp, uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = S[m][nt][x];
         }
     }
     lds_barrier();
@@ -620,9 +646,8 @@ __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
       s.ut.put4(nt * 16 + r, i0, U);
       s.us.put4(nt * 16 + r, i0, tail * U);
       if (a.ck_u) {
-        float* to = a.ck_u + (at * kC + i0) * a.Vp + v0 + nt * 16 + r;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = U[x];
+        for (int x = 0; x < 4; ++x) behind(a.ck_u + at * kC * a.Vp, uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = U[x];
       }
     }
     if (more) load_t(c + 1);
@@ -646,17 +671,18 @@ __global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
       if (w >= 2) mma<2>(o[nt], pf[1], s.ut.frag(nt * 16, 32));
     }
     if (more) load_p(c + 1);
+    IO* oc = ob + t0 * a.o_t;
     if (n == kC && v0 + BV <= a.V) {
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) ob[(t0 + i0 + x) * a.o_t + v0 + nt * 16 + r] = narrow<IO>(o[nt][x]);
+        for (int x = 0; x < 4; ++x) behind(oc, uint32_t(i0 + x) * uint32_t(a.o_t) + vat[nt]) = narrow<IO>(o[nt][x]);
     } else {
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          if (i0 + x < n && vin[nt]) ob[(t0 + i0 + x) * a.o_t + v0 + nt * 16 + r] = narrow<IO>(o[nt][x]);
+          if (i0 + x < n && vin[nt]) behind(oc, uint32_t(i0 + x) * uint32_t(a.o_t) + vat[nt]) = narrow<IO>(o[nt][x]);
     }
     lds_barrier();
   }
@@ -692,17 +718,19 @@ __global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) 
   extern __shared__ __align__(16) char lds[];
   BackLds<M, KP, BV>& s = *reinterpret_cast<BackLds<M, KP, BV>*>(lds);
   const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
-  const int v0 = blockIdx.x * BV, h = blockIdx.y, b = blockIdx.z, hk = h / (a.H / a.Hk);
-  const int len = length_of(a, b), chunks = (len + kC - 1) / kC;
-  const int64_t bh = int64_t(b) * a.H + h;
+  const ScanBlock at_block = scan_block(a, BV);
+  const int v0 = at_block.v0, bh = at_block.bh;
+  if (bh < 0) return;
+  const int b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
+  const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), chunks = (len + kC - 1) / kC;
   const IO* kb = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
   const IO* qb = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h;
   const IO* gob = static_cast<const IO*>(a.go) + b * a.go_b + h * a.go_h;
-  IO* gvb = static_cast<IO*>(a.gv) + bh * a.V;
+  IO* gvb = static_cast<IO*>(a.gv) + int64_t(bh) * a.V;
   const int64_t gv_t = int64_t(a.batch) * a.H * a.V;
 
   f32x4 S[MT][NV];  // dS'
-  auto state_at = [&](int m, int nt, int x) { return (bh * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
+  auto state_at = [&](int m, int nt, int x) { return (int64_t(bh) * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
   auto state_in = [&](int m, int nt, int x) { return (MT * w + m) * 16 + q4 * 4 + x < a.K && v0 + nt * 16 + r < a.V; };
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -713,12 +741,12 @@ __global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) 
 
   const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
   constexpr bool odd = ODD;  // K is no multiple of 8
-  int vc[NV];
+  uint32_t vat[NV];
   bool vin[NV];
 #pragma unroll
   for (int nt = 0; nt < NV; ++nt) {
     vin[nt] = v0 + nt * 16 + r < a.V;
-    vc[nt] = vin[nt] ? v0 + nt * 16 + r : 0;
+    vat[nt] = vin[nt] ? v0 + nt * 16 + r : 0;
   }
   Turn<M, KP> kturn, qturn;
   Exact<M> kf[KS];
@@ -732,26 +760,28 @@ __global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) 
   };
   auto load_rows = [&](int c) {
 #pragma unroll
-    for (int k = 0; k < KS; ++k) kf[k] = exact_of<M>(load8(kb + min(c * kC + row, len - 1) * a.k_t, k * 32 + q4 * 8, a.K, odd));
+    for (int k = 0; k < KS; ++k)
+      kf[k] = exact_of<M>(load8(kb + c * kC * a.k_t, uint32_t(min(row, len - c * kC - 1)) * uint32_t(a.k_t), k * 32 + q4 * 8, a.K, odd));
   };
   auto load_go = [&](int c) {
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
-      for (int nt = 0; nt < NV; ++nt) go[nt][x] = gob[min(c * kC + i0 + x, len - 1) * a.go_t + vc[nt]];
+      for (int nt = 0; nt < NV; ++nt)
+        go[nt][x] = behind(gob + c * kC * a.go_t, uint32_t(min(i0 + x, len - c * kC - 1)) * uint32_t(a.go_t) + vat[nt]);
   };
   auto load_t = [&](int c) {  // T and P turned are upper
-    const Word* tm = static_cast<const Word*>(a.tm) + (bh * a.nc + c) * M::planes * kC * kC;
+    const Word* tm = static_cast<const Word*>(a.tm) + (int64_t(bh) * a.nc + c) * M::planes * kC * kC;
     if (w < 2) tf[0] = load_planes<M>(tm, row, q4 * 8);
     tf[1] = load_planes<M>(tm, row, 32 + q4 * 8);
   };
   auto load_p = [&](int c) {
-    const Word* pm = static_cast<const Word*>(a.pm) + (bh * a.nc + c) * M::planes * kC * kC;
+    const Word* pm = static_cast<const Word*>(a.pm) + (int64_t(bh) * a.nc + c) * M::planes * kC * kC;
     if (w < 2) pf[0] = load_planes<M>(pm, row, q4 * 8);
     pf[1] = load_planes<M>(pm, row, 32 + q4 * 8);
   };
   auto load_dec = [&](int c) {
-    const float* dec = a.dec + (bh * a.nc + c) * 3 * kC;
+    const float* dec = a.dec + (int64_t(bh) * a.nc + c) * 3 * kC;
     eg = *reinterpret_cast<const f32x4*>(dec + i0);
     tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
     beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
@@ -788,7 +818,7 @@ __global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) 
   }
   for (int c = chunks - 1; c >= 0; --c) {
     const int t0 = c * kC, n = min(len - t0, kC);
-    const int64_t at = bh * a.nc + c;
+    const int64_t at = int64_t(bh) * a.nc + c;
     if (c > 0) {
       load_turn(c - 1);
       load_go(c - 1);
@@ -811,9 +841,9 @@ __global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) 
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) {
-        float* to = a.ds + (at * KP + (MT * w + m) * 16 + q4 * 4) * a.Vp + v0 + nt * 16 + r;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) to[int64_t(x) * a.Vp] = S[m][nt][x];
+        for (int x = 0; x < 4; ++x)
+          behind(a.ds + at * KP * a.Vp, uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = S[m][nt][x];
       }
     lds_barrier();
 #pragma unroll
@@ -821,20 +851,20 @@ __global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) 
       f32x4 R = {0, 0, 0, 0}, rs;
       if (w < 2) mma(R, tf[0], s.ut.frag(nt * 16, 0));
       mma(R, tf[1], s.ut.frag(nt * 16, 32));
-      float* to = a.dr + (at * kC + i0) * a.Vp + v0 + nt * 16 + r;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        to[int64_t(x) * a.Vp] = R[x];
+        behind(a.dr + at * kC * a.Vp, uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = R[x];
         R[x] *= beta[x];
         rs[x] = -eg[x] * R[x];
       }
+      IO* gvc = gvb + t0 * gv_t;
       if (n == kC && v0 + BV <= a.V) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) gvb[(t0 + i0 + x) * gv_t + v0 + nt * 16 + r] = narrow<IO>(R[x]);
+        for (int x = 0; x < 4; ++x) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[x]);
       } else {
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          if (i0 + x < n && vin[nt]) gvb[(t0 + i0 + x) * gv_t + v0 + nt * 16 + r] = narrow<IO>(R[x]);
+          if (i0 + x < n && vin[nt]) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[x]);
       }
       s.rt.put4(nt * 16 + r, i0, rs);
 #pragma unroll
@@ -952,8 +982,8 @@ __global__ __launch_bounds__(kLocalThreads) void delta_back_local_kernel(DeltaAr
     }
     pu = *reinterpret_cast<const f32x4*>(ck_u + int64_t(threadIdx.x / 8) * a.Vp + v0 + threadIdx.x % 8 * 4);
     // (values past V meet zeros, of U, S and dR; rows past the end are the last one's, but for do)
-    po = load8(gob + min(row, n - 1) * a.go_t, v0 + q4 * 8, a.V, a.V % 8);
-    if (half == 0) pv = load8(vb + min(row, n - 1) * a.v_t, v0 + q4 * 8, a.V, a.V % 8);
+    po = load8(gob, uint32_t(min(row, n - 1)) * uint32_t(a.go_t), v0 + q4 * 8, a.V, a.V % 8);
+    if (half == 0) pv = load8(vb, uint32_t(min(row, n - 1)) * uint32_t(a.v_t), v0 + q4 * 8, a.V, a.V % 8);
     pr = *reinterpret_cast<const f32x8*>(dr + int64_t(row) * a.Vp + v0 + q4 * 8);
   };
   {
@@ -1264,10 +1294,18 @@ dendsn_status check_cfg(const dendsn_delta_cfg* c) {
   if (!small_product(c->batch * c->H * 128, round_up(c->T + kC, kC)) ||
       !small_product(c->batch * c->H * 128 * round_up(c->T + kC, kC) / kC * 4, round_up(c->V, kVpad)))
     return fail(DENDSN_E_INVALID, "T * batch * H * V too large");
+  // a launch has fewer than 2^32 threads: blocks of 256, 16 columns of v or more
+  if (round_up(c->batch * c->H, 8) > (int64_t(1) << 23) / (round_up(c->V, kVpad) / 16))
+    return fail(DENDSN_E_UNSUPPORTED, "batch * H * V too large");
   const int64_t s[21] = {c->q_t, c->q_b, c->q_h, c->k_t, c->k_b, c->k_h, c->v_t, c->v_b, c->v_h, c->g_t, c->g_b, c->g_h,
                          c->beta_t, c->beta_b, c->beta_h, c->o_t, c->o_b, c->o_h, c->grad_o_t, c->grad_o_b, c->grad_o_h};
   for (int i = 0; i < 21; i += 3)
     if (!strides_fit(c, s[i], s[i + 1], s[i + 2])) return fail(DENDSN_E_INVALID, "a stride is negative or too large");
+  // 64 steps of a tensor lie within 2^32 bytes (gradients are contiguous)
+  int64_t most = c->batch * c->H * (c->V > c->K ? c->V : c->K);
+  for (int i = 0; i < 21; i += 3) most = s[i] > most ? s[i] : most;
+  if (c->T > 1 && most >= (int64_t(1) << 32) / kC / (c->io == DENDSN_IO_BF16 ? 2 : 4))
+    return fail(DENDSN_E_UNSUPPORTED, "64 steps of a tensor span 2^32 bytes or more");
   return DENDSN_OK;
 }
 
@@ -1350,7 +1388,7 @@ bool allow_lds(F* kernel, size_t bytes) {
 
 template <class M, int KP, int BV, bool ODD>
 dendsn_status launch_scan(const DeltaArgs& a, hipStream_t stream) {
-  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / BV), unsigned(a.H), unsigned(a.batch));
+  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / BV * round_up(int64_t(a.batch) * a.H, 8)));
   constexpr size_t bytes = sizeof(ScanLds<M, KP, BV>);
   static_assert(bytes <= 160 * 1024, "LDS of a CU");
   if (!allow_lds(delta_scan_kernel<M, KP, BV, ODD>, bytes)) return fail(DENDSN_E_HIP, "delta forward: %zu bytes of LDS refused", bytes);
@@ -1361,7 +1399,7 @@ dendsn_status launch_scan(const DeltaArgs& a, hipStream_t stream) {
 
 template <class M, int KP, int BV, bool ODD>
 dendsn_status launch_back_scan(const DeltaArgs& a, hipStream_t stream) {
-  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / BV), unsigned(a.H), unsigned(a.batch));
+  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / BV * round_up(int64_t(a.batch) * a.H, 8)));
   constexpr size_t bytes = sizeof(BackLds<M, KP, BV>);
   static_assert(bytes <= 160 * 1024, "LDS of a CU");
   if (!allow_lds(delta_back_scan_kernel<M, KP, BV, ODD>, bytes)) return fail(DENDSN_E_HIP, "delta backward: %zu bytes of LDS refused", bytes);

@@ -88,6 +88,10 @@ def test_delta_unsupported(lib):
     c = delta_cfg(K=129)
     assert delta_fwd(lib, c) == UNSUPPORTED and delta_bwd(lib, c) == UNSUPPORTED
     assert delta_step(lib, delta_cfg(K=129, T=1)) == UNSUPPORTED
+    # steps that lie too far apart, more blocks than a launch has
+    for kw in (dict(k_t=1 << 24), dict(io=1, grad_o_t=1 << 25), dict(batch=65535, H=64, Hk=2, V=128, T=2),
+               dict(batch=65535, H=256, Hk=2, K=1, V=1, T=1)):
+        assert delta_fwd(lib, delta_cfg(**kw)) == UNSUPPORTED, kw
 
 
 def test_delta_arguments(lib):
