@@ -266,12 +266,16 @@ template <class M, int ROWS> struct Turn {
   static_assert(2 * ROWS <= kThreads, "one block a thread");
   __device__ __forceinline__ static int tid() { return threadIdx.x % kThreads; }
   typename Eight<IO>::Vec r[4];
+  uint32_t at[4];  // the four rows
   // steps past the n-th have the n-th's values
-  __device__ __forceinline__ void load(const IO* rows, uint32_t stride, int n, int D, bool odd) {
-    const int t = tid() % 16 * 4, d = tid() / 16 * 8;
+  __device__ __forceinline__ void place(uint32_t stride, int n) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x) at[x] = uint32_t(min(tid() % 16 * 4 + x, n - 1)) * stride;
+  }
+  __device__ __forceinline__ void load(const IO* rows, int D, bool odd) {
     if (!kAll && tid() >= 2 * ROWS) return;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) r[x] = load8(rows, uint32_t(min(t + x, n - 1)) * stride, d, D, odd);
+    for (int x = 0; x < 4; ++x) r[x] = load8(rows, at[x], tid() / 16 * 8, D, odd);
   }
   __device__ __forceinline__ void put(MatX<M, ROWS, kC>& dst, int D) {
     const int t = tid() % 16 * 4, d = tid() / 16 * 8;
@@ -486,12 +490,15 @@ __global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// scan: states and outputs, chunk after chunk, BV columns of v a block.  Wave w has steps 16 w
-// to + 15 of the products over steps, and a quarter of the state's rows, which stay in its
-// registers.  Three barriers a chunk: the state, R and U go through LDS.  What a chunk reads is
-// fetched while the one before is computed, into the registers that it no longer needs; the
-// barriers wait for LDS alone.
+// scan: states and outputs, chunk after chunk, BV columns of v a block of two groups of four
+// waves.  The first has the chain: wave w has steps 16 w to + 15 of R and U, and a quarter of the
+// state's rows, which stay in its registers.  The second has q's products, the outputs, and
+// turns the next chunk's k over.  Three barriers a chunk: the state, R and U go through LDS.
+// What a chunk reads is fetched while the one before is computed, into the registers that it
+// no longer needs; the barriers wait for LDS alone.
 // ---------------------------------------------------------------------------
+constexpr int kScanThreads = 512;
+
 // Blocks go to the eight XCDs in turn, each of which has a cache of its own: the blocks of one
 // head, which read the same q, k, T and P, are eight apart.
 struct ScanBlock {
@@ -510,398 +517,518 @@ struct ScanLds {
 };
 
 template <class M, int KP, int BV, bool ODD>
-__global__ __launch_bounds__(kThreads) void delta_scan_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
   using IO = typename M::IO;
   using Word = typename M::Word;
+  using E = Eight<IO>;
   constexpr int KS = KP / 32, MT = KP / 64, NV = BV / 16;  // MT: row tiles of the state of a wave
   extern __shared__ __align__(16) char lds[];
   ScanLds<M, KP, BV>& s = *reinterpret_cast<ScanLds<M, KP, BV>*>(lds);
-  const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, w = wave % 4, r = lane % 16, q4 = lane / 16;
+  const bool chain = wave < 4;
   const ScanBlock at_block = scan_block(a, BV);
   const int v0 = at_block.v0, bh = at_block.bh;
   if (bh < 0) return;
   const int b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
   const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), chunks = (len + kC - 1) / kC;
-  const IO* kb = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
-  const IO* qb = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h;
-  const IO* vb = static_cast<const IO*>(a.v) + b * a.v_b + h * a.v_h;
-  IO* ob = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h;
-
-  // the state: rows 16 (MT w + m) + 4 q4 + x, columns 16 nt + r
-  f32x4 S[MT][NV];
-  auto state_at = [&](int m, int nt, int x) { return (int64_t(bh) * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
-  auto state_in = [&](int m, int nt, int x) { return (MT * w + m) * 16 + q4 * 4 + x < a.K && v0 + nt * 16 + r < a.V; };
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int nt = 0; nt < NV; ++nt)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) S[m][nt][x] = a.s0 && state_in(m, nt, x) ? a.s0[state_at(m, nt, x)] : 0.0f;
-
   const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
-  // Rows past the sequence's end are read as its last one, columns past K and V as some other:
-  // their betas are 0, their rows of the state stay 0 (Turn), their values are set to 0.
-  constexpr bool odd = ODD;  // K is no multiple of 8
+  // the next chunk's, in turn
+  const IO* kc = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
+  const IO* qc = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h;
+  const IO* vc = static_cast<const IO*>(a.v) + b * a.v_b + h * a.v_h;
+  const Word* tm = static_cast<const Word*>(a.tm) + int64_t(bh) * a.nc * M::planes * kC * kC;
+  const Word* pm = static_cast<const Word*>(a.pm) + int64_t(bh) * a.nc * M::planes * kC * kC;
+  const float* dec = a.dec + int64_t(bh) * a.nc * 3 * kC;
+  // this chunk's
+  IO* oc = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h;
+  float* ck_s = a.ck_s ? a.ck_s + int64_t(bh) * a.nc * KP * a.Vp : nullptr;
+  float* ck_u = a.ck_s ? a.ck_u + int64_t(bh) * a.nc * kC * a.Vp : nullptr;
+
+  // Rows past the sequence's end are read as its last one, columns past K and V as some other: their
+  // betas are 0, their rows of the state stay 0 (Turn), their values are set to 0.  Where K is no
+  // multiple of 8, eight values may reach into the row behind, if there is one, and are cut off.
   uint32_t vat[NV];
-  bool vin[NV];
+  bool vin[NV], step_by_step = false;
 #pragma unroll
   for (int nt = 0; nt < NV; ++nt) {
     vin[nt] = v0 + nt * 16 + r < a.V;
     vat[nt] = vin[nt] ? v0 + nt * 16 + r : 0;
   }
+  uint32_t at_k, at_q, at_v[4];
   Turn<M, KP> turn;
+  auto place = [&](int c) {  // where the rows of chunk c lie: of all but the last the same
+    const int n = min(len - c * kC, kC);
+    at_k = uint32_t(min(row, n - 1)) * uint32_t(a.k_t);
+    at_q = uint32_t(min(row, n - 1)) * uint32_t(a.q_t);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) at_v[x] = uint32_t(min(i0 + x, n - 1)) * uint32_t(a.v_t);
+    turn.place(a.k_t, n);
+    if (ODD) step_by_step = c + 1 >= chunks || a.k_t < a.K + 8 || a.q_t < a.K + 8;
+  };
   Exact<M> kf[KS], qf[KS];
   Both<M> tf[2], pf[2];
   f32x4 eg, tail, beta;
   float whole;
   IO vv[NV][4];
-  auto load_rows = [&](int c) {
-    const int t0 = c * kC, end = min(len - t0, kC) - 1;
-    const uint32_t at = min(row, end);
-    const IO *kc = kb + t0 * a.k_t, *qc = qb + t0 * a.q_t, *vc = vb + t0 * a.v_t;
-#pragma unroll
-    for (int k = 0; k < KS; ++k) {
-      kf[k] = exact_of<M>(load8(kc, at * uint32_t(a.k_t), k * 32 + q4 * 8, a.K, odd));
-      qf[k] = exact_of<M>(load8(qc, at * uint32_t(a.q_t), k * 32 + q4 * 8, a.K, odd));
+  auto row8 = [&](const IO* base, uint32_t at, int k) { return load8(base, at, k * 32 + q4 * 8, a.K, ODD && step_by_step); };
+  auto cut = [&](Exact<M>& f, int k) {
+    if (ODD) {
+      typename E::Vec x = __builtin_bit_cast(typename E::Vec, f);
+      cut8(x, k * 32 + q4 * 8, a.K);
+      f = exact_of<M>(x);
     }
+  };
+  auto load_k = [&]() {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) kf[k] = exact_of<M>(row8(kc, at_k, k));
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
-      for (int nt = 0; nt < NV; ++nt) vv[nt][x] = behind(vc, uint32_t(min(i0 + x, end)) * uint32_t(a.v_t) + vat[nt]);
+      for (int nt = 0; nt < NV; ++nt) vv[nt][x] = behind(vc, at_v[x] + vat[nt]);
   };
-  auto load_turn = [&](int c) { turn.load(kb + c * kC * a.k_t, a.k_t, min(len - c * kC, kC), a.K, odd); };
-  auto load_t = [&](int c) {
-    const Word* tm = static_cast<const Word*>(a.tm) + (int64_t(bh) * a.nc + c) * M::planes * kC * kC;
-    tf[0] = load_planes<M>(tm, row, q4 * 8);
-    if (w >= 2) tf[1] = load_planes<M>(tm, row, 32 + q4 * 8);  // T is lower
+  auto load_q = [&]() {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) qf[k] = exact_of<M>(row8(qc, at_q, k));
   };
-  auto load_p = [&](int c) {
-    const Word* pm = static_cast<const Word*>(a.pm) + (int64_t(bh) * a.nc + c) * M::planes * kC * kC;
-    pf[0] = load_planes<M>(pm, row, q4 * 8);
-    if (w >= 2) pf[1] = load_planes<M>(pm, row, 32 + q4 * 8);
+  auto load_square = [&](Both<M>(&f)[2], const Word* m) {  // rows of T or P, which are lower
+    f[0] = load_planes<M>(m, row, q4 * 8);
+    if (w >= 2) f[1] = load_planes<M>(m, row, 32 + q4 * 8);
   };
-  auto load_dec = [&](int c) {
-    const float* dec = a.dec + (int64_t(bh) * a.nc + c) * 3 * kC;
+  auto load_dec = [&]() {
     eg = *reinterpret_cast<const f32x4*>(dec + i0);
-    tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
-    beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
-    whole = dec[kC - 1];
+    if (chain) {
+      tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
+      beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
+      whole = dec[kC - 1];
+    }
   };
-  auto put_state = [&]() {
+  auto next = [&](int c) {  // what is loaded from now on is of chunk c
+    kc += kC * a.k_t;
+    qc += kC * a.q_t;
+    vc += kC * a.v_t;
+    tm += M::planes * kC * kC;
+    pm += M::planes * kC * kC;
+    dec += 3 * kC;
+    if (c + 1 == chunks) place(c);
+  };
+
+  if (chain) {
+    // the state: rows 16 (MT w + m) + 4 q4 + x, columns 16 nt + r
+    f32x4 S[MT][NV];
+    auto state_at = [&](int m, int nt, int x) { return (int64_t(bh) * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
+    auto state_in = [&](int m, int nt, int x) { return (MT * w + m) * 16 + q4 * 4 + x < a.K && vin[nt]; };
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int nt = 0; nt < NV; ++nt) s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
-  };
-  if (chunks > 0) {
-    load_turn(0);
-    load_rows(0);
-    load_t(0);
-    load_p(0);
-    load_dec(0);
-    turn.put(s.kt[0], a.K);
-    put_state();
-    lds_barrier();
-  }
-  for (int c = 0; c < chunks; ++c) {
-    const int t0 = c * kC, n = min(len - t0, kC);
-    const int64_t at = int64_t(bh) * a.nc + c;
-    const bool more = c + 1 < chunks;
-    if (more) load_turn(c + 1);
-    f32x4 o[NV];
+      for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
-    for (int nt = 0; nt < NV; ++nt) {
-      f32x4 ks = {0, 0, 0, 0}, qs = {0, 0, 0, 0};
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const Both<M> f = s.st.frag(nt * 16, k * 32);
-        mma(ks, kf[k], f);
-        mma<2>(qs, qf[k], f);
-      }
-      f32x4 R;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        R[x] = beta[x] * ((vin[nt] ? widen(vv[nt][x]) : 0.0f) - eg[x] * ks[x]);
-        o[nt][x] = a.scale * eg[x] * qs[x];
-      }
-      s.rt.put4(nt * 16 + r, i0, R);
-    }
-    if (more) load_rows(c + 1);
-    if (a.ck_s) {
+        for (int x = 0; x < 4; ++x) S[m][nt][x] = a.s0 && state_in(m, nt, x) ? a.s0[state_at(m, nt, x)] : 0.0f;
+    auto put_state = [&]() {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
+        for (int nt = 0; nt < NV; ++nt) s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
+    };
+    if (chunks > 0) {
+      place(0);
+      load_k();
+      load_square(tf, tm);
+      load_dec();
+      put_state();
+    }
+    lds_barrier();
+    for (int c = 0; c < chunks; ++c) {
+      const bool more = c + 1 < chunks;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) cut(kf[k], k);
+      if (more) next(c + 1);
+      f32x4 ks[NV];
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt) ks[nt] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt) mma(ks[nt], kf[k], s.st.frag(nt * 16, k * 32));
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt) {
+        f32x4 R;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) R[x] = beta[x] * ((vin[nt] ? widen(vv[nt][x]) : 0.0f) - eg[x] * ks[nt][x]);
+        s.rt.put4(nt * 16 + r, i0, R);
+      }
+      if (more) load_k();
+      if (ck_s) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              behind(ck_s, uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = S[m][nt][x];
+        ck_s += KP * a.Vp;
+      }
+      lds_barrier();
+      f32x4 U[NV];
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt) {
+        U[nt] = f32x4{0, 0, 0, 0};
+        mma(U[nt], tf[0], s.rt.frag(nt * 16, 0));
+        if (w >= 2) mma(U[nt], tf[1], s.rt.frag(nt * 16, 32));
+        s.us.put4(nt * 16 + r, i0, tail * U[nt]);
+        s.ut.put4(nt * 16 + r, i0, U[nt]);
+      }
+      if (more) load_square(tf, tm);
+      if (ck_s) {
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) behind(ck_u, uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = U[nt][x];
+        ck_u += kC * a.Vp;
+      }
+      lds_barrier();
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) S[m][nt] *= whole;
+      if (more) load_dec();
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
         for (int nt = 0; nt < NV; ++nt) {
+          const Both<M> f = s.us.frag(nt * 16, k * 32);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) mma(S[m][nt], s.kt[c & 1].frag((MT * w + m) * 16, k * 32), f);
+        }
+      put_state();  // (all have read the one before)
+      lds_barrier();
+    }
+    if (a.s_last) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            behind(a.ck_s + at * KP * a.Vp, uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = S[m][nt][x];
-        }
+            if (state_in(m, nt, x)) a.s_last[state_at(m, nt, x)] = S[m][nt][x];
+    }
+  } else {
+    if (chunks > 0) {
+      place(0);
+      turn.load(kc, a.K, ODD && step_by_step);
+      load_q();
+      load_square(pf, pm);
+      load_dec();
+      turn.put(s.kt[0], a.K);
     }
     lds_barrier();
+    for (int c = 0; c < chunks; ++c) {
+      const int n = min(len - c * kC, kC);
+      const bool more = c + 1 < chunks;
 #pragma unroll
-    for (int nt = 0; nt < NV; ++nt) {
-      f32x4 U = {0, 0, 0, 0};
-      mma(U, tf[0], s.rt.frag(nt * 16, 0));
-      if (w >= 2) mma(U, tf[1], s.rt.frag(nt * 16, 32));
-      s.ut.put4(nt * 16 + r, i0, U);
-      s.us.put4(nt * 16 + r, i0, tail * U);
-      if (a.ck_u) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) behind(a.ck_u + at * kC * a.Vp, uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = U[x];
+      for (int k = 0; k < KS; ++k) cut(qf[k], k);
+      if (more) {
+        next(c + 1);
+        turn.load(kc, a.K, ODD && step_by_step);
       }
-    }
-    if (more) load_t(c + 1);
-    lds_barrier();
+      f32x4 o[NV];
 #pragma unroll
-    for (int nt = 0; nt < NV; ++nt)
+      for (int nt = 0; nt < NV; ++nt) o[nt] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        S[m][nt] *= whole;
+      for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) mma(S[m][nt], s.kt[c & 1].frag((MT * w + m) * 16, k * 32), s.us.frag(nt * 16, k * 32));
+        for (int nt = 0; nt < NV; ++nt) mma<2>(o[nt], qf[k], s.st.frag(nt * 16, k * 32));
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt) o[nt] *= a.scale * eg;
+      if (more) {
+        load_q();
+        load_dec();
       }
-    put_state();  // (all have read the one before)
-    if (more) {
-      load_dec(c + 1);
-      turn.put(s.kt[(c + 1) & 1], a.K);
+      lds_barrier();
+      if (more) turn.put(s.kt[(c + 1) & 1], a.K);
+      lds_barrier();
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt) {
+        mma<2>(o[nt], pf[0], s.ut.frag(nt * 16, 0));
+        if (w >= 2) mma<2>(o[nt], pf[1], s.ut.frag(nt * 16, 32));
+      }
+      if (more) load_square(pf, pm);
+      if (n == kC && v0 + BV <= a.V) {
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) behind(oc, uint32_t(i0 + x) * uint32_t(a.o_t) + vat[nt]) = narrow<IO>(o[nt][x]);
+      } else {
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (i0 + x < n && vin[nt]) behind(oc, uint32_t(i0 + x) * uint32_t(a.o_t) + vat[nt]) = narrow<IO>(o[nt][x]);
+      }
+      oc += kC * a.o_t;
+      lds_barrier();
     }
-#pragma unroll
-    for (int nt = 0; nt < NV; ++nt) {
-      mma<2>(o[nt], pf[0], s.ut.frag(nt * 16, 0));
-      if (w >= 2) mma<2>(o[nt], pf[1], s.ut.frag(nt * 16, 32));
-    }
-    if (more) load_p(c + 1);
-    IO* oc = ob + t0 * a.o_t;
-    if (n == kC && v0 + BV <= a.V) {
-#pragma unroll
-      for (int nt = 0; nt < NV; ++nt)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) behind(oc, uint32_t(i0 + x) * uint32_t(a.o_t) + vat[nt]) = narrow<IO>(o[nt][x]);
-    } else {
-#pragma unroll
-      for (int nt = 0; nt < NV; ++nt)
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          if (i0 + x < n && vin[nt]) behind(oc, uint32_t(i0 + x) * uint32_t(a.o_t) + vat[nt]) = narrow<IO>(o[nt][x]);
-    }
-    lds_barrier();
+    // steps past the end
+    IO* ob = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h;
+    for (int64_t u = threadIdx.x - kThreads; u < int64_t(a.T - len) * BV; u += kThreads)
+      if (v0 + u % BV < a.V) ob[(len + u / BV) * a.o_t + v0 + u % BV] = IO{};
   }
-  if (a.s_last) {
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int nt = 0; nt < NV; ++nt)
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          if (state_in(m, nt, x)) a.s_last[state_at(m, nt, x)] = S[m][nt][x];
-  }
-  for (int64_t u = threadIdx.x; u < int64_t(a.T - len) * BV; u += kThreads)  // steps past the end
-    if (v0 + u % BV < a.V) ob[(len + u / BV) * a.o_t + v0 + u % BV] = IO{};
 }
 
 // ---------------------------------------------------------------------------
-// back_scan: the states' gradients, from the last chunk down; dR, dv.  As the scan.
+// back_scan: the states' gradients, from the last chunk down; dR, dv.  As the scan; here the
+// first group has dU and dR, the second the state's gradient and the turned q and k.
 // ---------------------------------------------------------------------------
 template <class M, int KP, int BV>
 struct BackLds {
-  MatX<M, KP, kC> kt, qt;
+  MatX<M, KP, kC> kt[2], qt;
   MatX<M, BV, kC> ot;
   Mat<M, BV, KP> st;
   Mat<M, BV, kC> os, ut, rt;
 };
 
 template <class M, int KP, int BV, bool ODD>
-__global__ __launch_bounds__(kThreads) void delta_back_scan_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs a) {
   using IO = typename M::IO;
   using Word = typename M::Word;
+  using E = Eight<IO>;
   constexpr int KS = KP / 32, MT = KP / 64, NV = BV / 16;
   extern __shared__ __align__(16) char lds[];
   BackLds<M, KP, BV>& s = *reinterpret_cast<BackLds<M, KP, BV>*>(lds);
-  const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, w = wave % 4, r = lane % 16, q4 = lane / 16;
   const ScanBlock at_block = scan_block(a, BV);
   const int v0 = at_block.v0, bh = at_block.bh;
   if (bh < 0) return;
   const int b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
-  const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), chunks = (len + kC - 1) / kC;
-  const IO* kb = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
-  const IO* qb = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h;
-  const IO* gob = static_cast<const IO*>(a.go) + b * a.go_b + h * a.go_h;
-  IO* gvb = static_cast<IO*>(a.gv) + int64_t(bh) * a.V;
-  const int64_t gv_t = int64_t(a.batch) * a.H * a.V;
-
-  f32x4 S[MT][NV];  // dS'
-  auto state_at = [&](int m, int nt, int x) { return (int64_t(bh) * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
-  auto state_in = [&](int m, int nt, int x) { return (MT * w + m) * 16 + q4 * 4 + x < a.K && v0 + nt * 16 + r < a.V; };
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int nt = 0; nt < NV; ++nt)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) S[m][nt][x] = a.gs_last && state_in(m, nt, x) ? a.gs_last[state_at(m, nt, x)] : 0.0f;
-
+  const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), chunks = (len + kC - 1) / kC, end = max(chunks - 1, 0);
   const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
-  constexpr bool odd = ODD;  // K is no multiple of 8
+  const int64_t gv_t = int64_t(a.batch) * a.H * a.V, top = int64_t(bh) * a.nc + end;
+  // of the chunk that is loaded next
+  const IO* kc = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h + end * kC * a.k_t;
+  const IO* qc = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h + end * kC * a.q_t;
+  const IO* goc = static_cast<const IO*>(a.go) + b * a.go_b + h * a.go_h + end * kC * a.go_t;
+  const Word* tm = static_cast<const Word*>(a.tm) + top * M::planes * kC * kC;
+  const Word* pm = static_cast<const Word*>(a.pm) + top * M::planes * kC * kC;
+  const float* dec = a.dec + top * 3 * kC;
   uint32_t vat[NV];
-  bool vin[NV];
+  bool vin[NV], step_by_step = false;
 #pragma unroll
   for (int nt = 0; nt < NV; ++nt) {
     vin[nt] = v0 + nt * 16 + r < a.V;
     vat[nt] = vin[nt] ? v0 + nt * 16 + r : 0;
   }
+  uint32_t at_k, at_go[4];
   Turn<M, KP> kturn, qturn;
-  Exact<M> kf[KS];
-  Both<M> tf[2], pf[2];
-  f32x4 eg, tail, beta;
-  float whole;
-  IO go[NV][4];
-  auto load_turn = [&](int c) {
-    kturn.load(kb + c * kC * a.k_t, a.k_t, min(len - c * kC, kC), a.K, odd);
-    qturn.load(qb + c * kC * a.q_t, a.q_t, min(len - c * kC, kC), a.K, odd);
-  };
-  auto load_rows = [&](int c) {
+  auto place = [&](int c) {  // of all but the last, which comes first, the same
+    const int n = min(len - c * kC, kC);
+    at_k = uint32_t(min(row, n - 1)) * uint32_t(a.k_t);
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
-      kf[k] = exact_of<M>(load8(kb + c * kC * a.k_t, uint32_t(min(row, len - c * kC - 1)) * uint32_t(a.k_t), k * 32 + q4 * 8, a.K, odd));
+    for (int x = 0; x < 4; ++x) at_go[x] = uint32_t(min(i0 + x, n - 1)) * uint32_t(a.go_t);
+    kturn.place(a.k_t, n);
+    qturn.place(a.q_t, n);
+    if (ODD) step_by_step = c + 1 >= chunks || a.k_t < a.K + 8 || a.q_t < a.K + 8;
   };
-  auto load_go = [&](int c) {
+  auto next = [&](int c) {
+    kc -= kC * a.k_t;
+    qc -= kC * a.q_t;
+    goc -= kC * a.go_t;
+    tm -= M::planes * kC * kC;
+    pm -= M::planes * kC * kC;
+    dec -= 3 * kC;
+    if (c + 2 == chunks) place(c);
+  };
+  if (chunks > 0) place(end);
+
+  if (wave < 4) {
+    Exact<M> kf[KS];
+    Both<M> tf[2], pf[2];
+    f32x4 eg, tail, beta;
+    IO go[NV][4];
+    IO* gvc = static_cast<IO*>(a.gv) + int64_t(bh) * a.V + end * kC * gv_t;
+    float* drc = a.dr + top * kC * a.Vp;
+    auto load_k = [&]() {
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+      for (int k = 0; k < KS; ++k) kf[k] = exact_of<M>(load8(kc, at_k, k * 32 + q4 * 8, a.K, ODD && step_by_step));
+    };
+    auto load_go = [&]() {
 #pragma unroll
-      for (int nt = 0; nt < NV; ++nt)
-        go[nt][x] = behind(gob + c * kC * a.go_t, uint32_t(min(i0 + x, len - c * kC - 1)) * uint32_t(a.go_t) + vat[nt]);
-  };
-  auto load_t = [&](int c) {  // T and P turned are upper
-    const Word* tm = static_cast<const Word*>(a.tm) + (int64_t(bh) * a.nc + c) * M::planes * kC * kC;
-    if (w < 2) tf[0] = load_planes<M>(tm, row, q4 * 8);
-    tf[1] = load_planes<M>(tm, row, 32 + q4 * 8);
-  };
-  auto load_p = [&](int c) {
-    const Word* pm = static_cast<const Word*>(a.pm) + (int64_t(bh) * a.nc + c) * M::planes * kC * kC;
-    if (w < 2) pf[0] = load_planes<M>(pm, row, q4 * 8);
-    pf[1] = load_planes<M>(pm, row, 32 + q4 * 8);
-  };
-  auto load_dec = [&](int c) {
-    const float* dec = a.dec + (int64_t(bh) * a.nc + c) * 3 * kC;
-    eg = *reinterpret_cast<const f32x4*>(dec + i0);
-    tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
-    beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
-    whole = dec[kC - 1];
-  };
-  // of the next chunk down: its state's gradient and its turned inputs
-  auto put_chunk = [&](int c) {
-    kturn.put(s.kt, a.K);
-    qturn.put(s.qt, a.K);
+      for (int x = 0; x < 4; ++x)
 #pragma unroll
-    for (int nt = 0; nt < NV; ++nt) {
-      f32x4 os;
+        for (int nt = 0; nt < NV; ++nt) go[nt][x] = behind(goc, at_go[x] + vat[nt]);
+    };
+    auto load_square = [&](Both<M>(&f)[2], const Word* m) {  // rows of T or P turned, which are upper
+      if (w < 2) f[0] = load_planes<M>(m, row, q4 * 8);
+      f[1] = load_planes<M>(m, row, 32 + q4 * 8);
+    };
+    auto load_dec = [&]() {
+      eg = *reinterpret_cast<const f32x4*>(dec + i0);
+      tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
+      beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
+    };
+    auto put_go = [&](int c) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if (c * kC + i0 + x >= len || !vin[nt]) go[nt][x] = IO{};
-        os[x] = a.scale * eg[x] * widen(go[nt][x]);
+      for (int nt = 0; nt < NV; ++nt) {
+        f32x4 os;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          if (c * kC + i0 + x >= len || !vin[nt]) go[nt][x] = IO{};
+          os[x] = a.scale * eg[x] * widen(go[nt][x]);
+        }
+        s.ot.put4(nt * 16 + r, i0, E::bits(go[nt][0]), E::bits(go[nt][1]), E::bits(go[nt][2]), E::bits(go[nt][3]));
+        s.os.put4(nt * 16 + r, i0, os);
       }
-      using E = Eight<IO>;
-      s.ot.put4(nt * 16 + r, i0, E::bits(go[nt][0]), E::bits(go[nt][1]), E::bits(go[nt][2]), E::bits(go[nt][3]));
-      s.os.put4(nt * 16 + r, i0, os);
-#pragma unroll
-      for (int m = 0; m < MT; ++m) s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
+    };
+    if (chunks > 0) {
+      load_go();
+      load_dec();
+      load_k();
+      load_square(pf, pm);
+      load_square(tf, tm);
+      put_go(end);
     }
-  };
-  if (chunks > 0) {
-    load_turn(chunks - 1);
-    load_go(chunks - 1);
-    load_dec(chunks - 1);
-    load_rows(chunks - 1);
-    load_t(chunks - 1);
-    load_p(chunks - 1);
-    put_chunk(chunks - 1);
     lds_barrier();
-  }
-  for (int c = chunks - 1; c >= 0; --c) {
-    const int t0 = c * kC, n = min(len - t0, kC);
-    const int64_t at = int64_t(bh) * a.nc + c;
-    if (c > 0) {
-      load_turn(c - 1);
-      load_go(c - 1);
-    }
+    for (int c = end; c >= 0 && chunks > 0; --c) {
+      const int n = min(len - c * kC, kC);
+      if (ODD) {
 #pragma unroll
-    for (int nt = 0; nt < NV; ++nt) {
-      f32x4 U = {0, 0, 0, 0};
+        for (int k = 0; k < KS; ++k) {
+          typename E::Vec x = __builtin_bit_cast(typename E::Vec, kf[k]);
+          cut8(x, k * 32 + q4 * 8, a.K);
+          kf[k] = exact_of<M>(x);
+        }
+      }
+      if (c > 0) {
+        next(c - 1);
+        load_go();
+      }
+      f32x4 U[NV];
 #pragma unroll
-      for (int k = 0; k < KS; ++k) mma(U, kf[k], s.st.frag(nt * 16, k * 32));
-      U *= tail;
-      if (w < 2) mma(U, pf[0], s.ot.frag(nt * 16, 0));
-      mma(U, pf[1], s.ot.frag(nt * 16, 32));
-      s.ut.put4(nt * 16 + r, i0, U);
+      for (int nt = 0; nt < NV; ++nt) U[nt] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt) mma(U[nt], kf[k], s.st.frag(nt * 16, k * 32));
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt) {
+        U[nt] *= tail;
+        if (w < 2) mma(U[nt], pf[0], s.ot.frag(nt * 16, 0));
+        mma(U[nt], pf[1], s.ot.frag(nt * 16, 32));
+        s.ut.put4(nt * 16 + r, i0, U[nt]);
+      }
+      if (c > 0) {
+        load_k();
+        load_square(pf, pm);
+      }
+      lds_barrier();
+#pragma unroll
+      for (int nt = 0; nt < NV; ++nt) {
+        f32x4 R = {0, 0, 0, 0};
+        if (w < 2) mma(R, tf[0], s.ut.frag(nt * 16, 0));
+        mma(R, tf[1], s.ut.frag(nt * 16, 32));
+        s.rt.put4(nt * 16 + r, i0, -eg * beta * R);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) behind(drc, uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = R[x];
+        R *= beta;
+        if (n == kC && v0 + BV <= a.V) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[x]);
+        } else {
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (i0 + x < n && vin[nt]) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[x]);
+        }
+      }
+      gvc -= kC * gv_t;
+      drc -= kC * a.Vp;
+      if (c > 0) {
+        load_square(tf, tm);
+        load_dec();
+      }
+      lds_barrier();
+      if (c > 0) put_go(c - 1);
+      lds_barrier();
     }
-    if (c > 0) {
-      load_rows(c - 1);
-      load_p(c - 1);
-    }
+    IO* gvb = static_cast<IO*>(a.gv) + int64_t(bh) * a.V;
+    for (int64_t u = threadIdx.x; u < int64_t(a.T - len) * BV; u += kThreads)  // steps past the end
+      if (v0 + u % BV < a.V) gvb[(len + u / BV) * gv_t + v0 + u % BV] = IO{};
+  } else {
+    f32x4 S[MT][NV];  // dS'
+    auto state_at = [&](int m, int nt, int x) { return (int64_t(bh) * a.K + (MT * w + m) * 16 + q4 * 4 + x) * a.V + v0 + nt * 16 + r; };
+    auto state_in = [&](int m, int nt, int x) { return (MT * w + m) * 16 + q4 * 4 + x < a.K && vin[nt]; };
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int nt = 0; nt < NV; ++nt) {
+      for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          behind(a.ds + at * KP * a.Vp, uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = S[m][nt][x];
-      }
-    lds_barrier();
-#pragma unroll
-    for (int nt = 0; nt < NV; ++nt) {
-      f32x4 R = {0, 0, 0, 0}, rs;
-      if (w < 2) mma(R, tf[0], s.ut.frag(nt * 16, 0));
-      mma(R, tf[1], s.ut.frag(nt * 16, 32));
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        behind(a.dr + at * kC * a.Vp, uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = R[x];
-        R[x] *= beta[x];
-        rs[x] = -eg[x] * R[x];
-      }
-      IO* gvc = gvb + t0 * gv_t;
-      if (n == kC && v0 + BV <= a.V) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[x]);
-      } else {
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          if (i0 + x < n && vin[nt]) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[x]);
-      }
-      s.rt.put4(nt * 16 + r, i0, rs);
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        S[m][nt] *= whole;
-#pragma unroll
-        for (int k = 0; k < 2; ++k) mma(S[m][nt], s.qt.frag((MT * w + m) * 16, k * 32), s.os.frag(nt * 16, k * 32));
-      }
-    }
-    if (c > 0) {
-      load_t(c - 1);
-      load_dec(c - 1);
-    }
-    lds_barrier();
-#pragma unroll
-    for (int nt = 0; nt < NV; ++nt)
+        for (int x = 0; x < 4; ++x) S[m][nt][x] = a.gs_last && state_in(m, nt, x) ? a.gs_last[state_at(m, nt, x)] : 0.0f;
+    auto put_state = [&]() {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int k = 0; k < 2; ++k) mma(S[m][nt], s.kt.frag((MT * w + m) * 16, k * 32), s.rt.frag(nt * 16, k * 32));
-    if (c > 0) {
+        for (int nt = 0; nt < NV; ++nt) s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
+    };
+    float whole = 0.0f;
+    float* dsc = a.ds + top * KP * a.Vp;
+    if (chunks > 0) {
+      kturn.load(kc, a.K, ODD && step_by_step);
+      qturn.load(qc, a.K, ODD && step_by_step);
+      whole = dec[kC - 1];
+      put_state();
+      kturn.put(s.kt[end & 1], a.K);
+      qturn.put(s.qt, a.K);
+    }
+    lds_barrier();
+    for (int c = end; c >= 0 && chunks > 0; --c) {
+      if (c > 0) {
+        next(c - 1);
+        kturn.load(kc, a.K, ODD && step_by_step);
+        qturn.load(qc, a.K, ODD && step_by_step);
+      }
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            behind(dsc, uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = S[m][nt][x];
+          S[m][nt] *= whole;
+        }
+      dsc -= KP * a.Vp;
+      if (c > 0) whole = dec[kC - 1];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt) {
+          const Both<M> f = s.os.frag(nt * 16, k * 32);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) mma(S[m][nt], s.qt.frag((MT * w + m) * 16, k * 32), f);
+        }
       lds_barrier();
-      put_chunk(c - 1);
+      if (c > 0) {  // (q's products are done; k's of this chunk are not)
+        kturn.put(s.kt[(c - 1) & 1], a.K);
+        qturn.put(s.qt, a.K);
+      }
+      lds_barrier();
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt) {
+          const Both<M> f = s.rt.frag(nt * 16, k * 32);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) mma(S[m][nt], s.kt[c & 1].frag((MT * w + m) * 16, k * 32), f);
+        }
+      put_state();
       lds_barrier();
     }
+    if (a.gs0) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (state_in(m, nt, x)) a.gs0[state_at(m, nt, x)] = S[m][nt][x];
+    }
   }
-  if (a.gs0) {
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int nt = 0; nt < NV; ++nt)
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          if (state_in(m, nt, x)) a.gs0[state_at(m, nt, x)] = S[m][nt][x];
-  }
-  for (int64_t u = threadIdx.x; u < int64_t(a.T - len) * BV; u += kThreads)
-    if (v0 + u % BV < a.V) gvb[(len + u / BV) * gv_t + v0 + u % BV] = IO{};
 }
 
 // ---------------------------------------------------------------------------
@@ -988,8 +1115,8 @@ __global__ __launch_bounds__(kLocalThreads) void delta_back_local_kernel(DeltaAr
   };
   {
     Turn<M, KP> turn;
-    if (half == 0) turn.load(kb, a.k_t, n, a.K, a.K % 8);
-    else turn.load(qb, a.q_t, n, a.K, a.K % 8);
+    turn.place(half == 0 ? a.k_t : a.q_t, n);
+    turn.load(half == 0 ? kb : qb, a.K, a.K % 8);
     load(0);
     const double G = chunk_sum<IO>(a, b, h, t0, n);
     if (wave == 0) s.g[lane] = G;
@@ -1294,8 +1421,8 @@ dendsn_status check_cfg(const dendsn_delta_cfg* c) {
   if (!small_product(c->batch * c->H * 128, round_up(c->T + kC, kC)) ||
       !small_product(c->batch * c->H * 128 * round_up(c->T + kC, kC) / kC * 4, round_up(c->V, kVpad)))
     return fail(DENDSN_E_INVALID, "T * batch * H * V too large");
-  // a launch has fewer than 2^32 threads: blocks of 256, 16 columns of v or more
-  if (round_up(c->batch * c->H, 8) > (int64_t(1) << 23) / (round_up(c->V, kVpad) / 16))
+  // a launch has fewer than 2^32 threads: blocks of 512, 16 columns of v or more
+  if (round_up(c->batch * c->H, 8) > (int64_t(1) << 22) / (round_up(c->V, kVpad) / 16))
     return fail(DENDSN_E_UNSUPPORTED, "batch * H * V too large");
   const int64_t s[21] = {c->q_t, c->q_b, c->q_h, c->k_t, c->k_b, c->k_h, c->v_t, c->v_b, c->v_h, c->g_t, c->g_b, c->g_h,
                          c->beta_t, c->beta_b, c->beta_h, c->o_t, c->o_b, c->o_h, c->grad_o_t, c->grad_o_b, c->grad_o_h};
@@ -1393,7 +1520,7 @@ dendsn_status launch_scan(const DeltaArgs& a, hipStream_t stream) {
   static_assert(bytes <= 160 * 1024, "LDS of a CU");
   if (!allow_lds(delta_scan_kernel<M, KP, BV, ODD>, bytes)) return fail(DENDSN_E_HIP, "delta forward: %zu bytes of LDS refused", bytes);
   delta_local_kernel<M, KP, false><<<heads, dim3(kThreads), 0, stream>>>(a);
-  delta_scan_kernel<M, KP, BV, ODD><<<cols, dim3(kThreads), bytes, stream>>>(a);
+  delta_scan_kernel<M, KP, BV, ODD><<<cols, dim3(kScanThreads), bytes, stream>>>(a);
   return launched("delta forward");
 }
 
@@ -1404,7 +1531,7 @@ dendsn_status launch_back_scan(const DeltaArgs& a, hipStream_t stream) {
   static_assert(bytes <= 160 * 1024, "LDS of a CU");
   if (!allow_lds(delta_back_scan_kernel<M, KP, BV, ODD>, bytes)) return fail(DENDSN_E_HIP, "delta backward: %zu bytes of LDS refused", bytes);
   delta_local_kernel<M, KP, true><<<heads, dim3(kThreads), 0, stream>>>(a);
-  delta_back_scan_kernel<M, KP, BV, ODD><<<cols, dim3(kThreads), bytes, stream>>>(a);
+  delta_back_scan_kernel<M, KP, BV, ODD><<<cols, dim3(kScanThreads), bytes, stream>>>(a);
   return launched("delta backward");
 }
 
