@@ -297,7 +297,7 @@ __device__ __forceinline__ void lds_barrier() {
 }
 
 // T and P in memory: planes of [64][64], as operands of their rows.
-template <class M>
+template <class M, int Q = M::planes>
 __device__ __forceinline__ Both<M> load_planes(const typename M::Word* p, int row, int col) {
   const int at = row * kC + col;
   Both<M> f;
@@ -305,7 +305,7 @@ __device__ __forceinline__ Both<M> load_planes(const typename M::Word* p, int ro
     f = load_both<M>(p + at);
   } else {
 #pragma unroll
-    for (int j = 0; j < M::planes; ++j) f.p[j] = *reinterpret_cast<const bf16x8*>(p + j * kC * kC + at);
+    for (int j = 0; j < Q; ++j) f.p[j] = *reinterpret_cast<const bf16x8*>(p + j * kC * kC + at);
   }
   return f;
 }
@@ -494,8 +494,8 @@ __global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
 // waves.  The first has the chain: wave w has steps 16 w to + 15 of R and U, and a quarter of the
 // state's rows, which stay in its registers.  The second has q's products, the outputs, and
 // turns the next chunk's k over.  Three barriers a chunk: the state, R and U go through LDS.
-// What a chunk reads is fetched while the one before is computed, into the registers that it
-// no longer needs; the barriers wait for LDS alone.
+// What a chunk reads is fetched two chunks ahead, into the registers that are free again; the
+// barriers wait for LDS alone.
 // ---------------------------------------------------------------------------
 constexpr int kScanThreads = 512;
 
@@ -565,43 +565,14 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
     turn.place(a.k_t, n);
     if (ODD) step_by_step = c + 1 >= chunks || a.k_t < a.K + 8 || a.q_t < a.K + 8;
   };
-  Exact<M> kf[KS], qf[KS];
-  Both<M> tf[2], pf[2];
-  f32x4 eg, tail, beta;
-  float whole;
-  IO vv[NV][4];
   auto row8 = [&](const IO* base, uint32_t at, int k) { return load8(base, at, k * 32 + q4 * 8, a.K, ODD && step_by_step); };
-  auto cut = [&](Exact<M>& f, int k) {
-    if (ODD) {
-      typename E::Vec x = __builtin_bit_cast(typename E::Vec, f);
-      cut8(x, k * 32 + q4 * 8, a.K);
-      f = exact_of<M>(x);
-    }
+  auto load_square = [&](Both<M>(&f)[2], const Word* m, auto planes) {  // rows of T or P, which are lower
+    constexpr int Q = decltype(planes)::value;
+    f[0] = load_planes<M, Q>(m, row, q4 * 8);
+    if (w >= 2) f[1] = load_planes<M, Q>(m, row, 32 + q4 * 8);
   };
-  auto load_k = [&]() {
-#pragma unroll
-    for (int k = 0; k < KS; ++k) kf[k] = exact_of<M>(row8(kc, at_k, k));
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int nt = 0; nt < NV; ++nt) vv[nt][x] = behind(vc, at_v[x] + vat[nt]);
-  };
-  auto load_q = [&]() {
-#pragma unroll
-    for (int k = 0; k < KS; ++k) qf[k] = exact_of<M>(row8(qc, at_q, k));
-  };
-  auto load_square = [&](Both<M>(&f)[2], const Word* m) {  // rows of T or P, which are lower
-    f[0] = load_planes<M>(m, row, q4 * 8);
-    if (w >= 2) f[1] = load_planes<M>(m, row, 32 + q4 * 8);
-  };
-  auto load_dec = [&]() {
-    eg = *reinterpret_cast<const f32x4*>(dec + i0);
-    if (chain) {
-      tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
-      beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
-      whole = dec[kC - 1];
-    }
-  };
+  constexpr std::integral_constant<int, M::planes> kAll{};
+  constexpr std::integral_constant<int, M::planes < 2 ? 1 : 2> kTwo{};  // of what enters o alone
   auto next = [&](int c) {  // what is loaded from now on is of chunk c
     kc += kC * a.k_t;
     qc += kC * a.q_t;
@@ -610,6 +581,19 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
     pm += M::planes * kC * kC;
     dec += 3 * kC;
     if (c + 1 == chunks) place(c);
+  };
+  auto two_by_two = [&](auto&& step) {  // (buffers are registers: which one has to be known when it is compiled)
+    for (int c = 0; c < chunks; c += 2) {
+      step(std::integral_constant<int, 0>{}, c);
+      if (c + 1 < chunks) step(std::integral_constant<int, 1>{}, c + 1);
+    }
+  };
+  auto cut = [&](Exact<M>& f, int k) {
+    if (ODD) {
+      typename E::Vec x = __builtin_bit_cast(typename E::Vec, f);
+      cut8(x, k * 32 + q4 * 8, a.K);
+      f = exact_of<M>(x);
+    }
   };
 
   if (chain) {
@@ -629,34 +613,62 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
 #pragma unroll
         for (int nt = 0; nt < NV; ++nt) s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
     };
+    struct Chunk {
+      Exact<M> kf[KS];
+      Both<M> tf[2];
+      f32x4 eg, tail, beta;
+      float whole;
+      IO vv[NV][4];
+    } in[2];
+    auto load_k = [&](Chunk& n) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) n.kf[k] = exact_of<M>(row8(kc, at_k, k));
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt) n.vv[nt][x] = behind(vc, at_v[x] + vat[nt]);
+    };
+    auto load_dec = [&](Chunk& n) {
+      n.eg = *reinterpret_cast<const f32x4*>(dec + i0);
+      n.tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
+      n.beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
+      n.whole = dec[kC - 1];
+    };
     if (chunks > 0) {
       place(0);
-      load_k();
-      load_square(tf, tm);
-      load_dec();
+      load_k(in[0]);
+      load_square(in[0].tf, tm, kAll);
+      load_dec(in[0]);
+      if (chunks > 1) {
+        next(1);
+        load_k(in[1]);
+        load_square(in[1].tf, tm, kAll);
+        load_dec(in[1]);
+      }
       put_state();
     }
     lds_barrier();
-    for (int c = 0; c < chunks; ++c) {
-      const bool more = c + 1 < chunks;
+    two_by_two([&](auto buffer, int c) {
+      Chunk& n = in[decltype(buffer)::value];
+      const bool more = c + 2 < chunks;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) cut(kf[k], k);
-      if (more) next(c + 1);
+      for (int k = 0; k < KS; ++k) cut(n.kf[k], k);
+      if (more) next(c + 2);
       f32x4 ks[NV];
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) ks[nt] = f32x4{0, 0, 0, 0};
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int nt = 0; nt < NV; ++nt) mma(ks[nt], kf[k], s.st.frag(nt * 16, k * 32));
+        for (int nt = 0; nt < NV; ++nt) mma(ks[nt], n.kf[k], s.st.frag(nt * 16, k * 32));
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) {
         f32x4 R;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) R[x] = beta[x] * ((vin[nt] ? widen(vv[nt][x]) : 0.0f) - eg[x] * ks[nt][x]);
+        for (int x = 0; x < 4; ++x) R[x] = n.beta[x] * ((vin[nt] ? widen(n.vv[nt][x]) : 0.0f) - n.eg[x] * ks[nt][x]);
         s.rt.put4(nt * 16 + r, i0, R);
       }
-      if (more) load_k();
+      if (more) load_k(n);
       if (ck_s) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -672,12 +684,12 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) {
         U[nt] = f32x4{0, 0, 0, 0};
-        mma(U[nt], tf[0], s.rt.frag(nt * 16, 0));
-        if (w >= 2) mma(U[nt], tf[1], s.rt.frag(nt * 16, 32));
-        s.us.put4(nt * 16 + r, i0, tail * U[nt]);
+        mma(U[nt], n.tf[0], s.rt.frag(nt * 16, 0));
+        if (w >= 2) mma(U[nt], n.tf[1], s.rt.frag(nt * 16, 32));
+        s.us.put4(nt * 16 + r, i0, n.tail * U[nt]);
         s.ut.put4(nt * 16 + r, i0, U[nt]);
       }
-      if (more) load_square(tf, tm);
+      if (more) load_square(n.tf, tm, kAll);
       if (ck_s) {
 #pragma unroll
         for (int nt = 0; nt < NV; ++nt)
@@ -689,19 +701,19 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) S[m][nt] *= whole;
-      if (more) load_dec();
+        for (int m = 0; m < MT; ++m) S[m][nt] *= n.whole;
+      if (more) load_dec(n);
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int nt = 0; nt < NV; ++nt) {
           const Both<M> f = s.us.frag(nt * 16, k * 32);
 #pragma unroll
-          for (int m = 0; m < MT; ++m) mma(S[m][nt], s.kt[c & 1].frag((MT * w + m) * 16, k * 32), f);
+          for (int m = 0; m < MT; ++m) mma(S[m][nt], s.kt[decltype(buffer)::value].frag((MT * w + m) * 16, k * 32), f);
         }
       put_state();  // (all have read the one before)
       lds_barrier();
-    }
+    });
     if (a.s_last) {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
@@ -712,46 +724,57 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
             if (state_in(m, nt, x)) a.s_last[state_at(m, nt, x)] = S[m][nt][x];
     }
   } else {
+    struct Chunk {
+      Exact<M> qf[KS];
+      Both<M> pf[2];
+      f32x4 eg;
+    } in[2];
+    auto load_q = [&](Chunk& n) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) n.qf[k] = exact_of<M>(row8(qc, at_q, k));
+      n.eg = *reinterpret_cast<const f32x4*>(dec + i0);
+    };
     if (chunks > 0) {
       place(0);
       turn.load(kc, a.K, ODD && step_by_step);
-      load_q();
-      load_square(pf, pm);
-      load_dec();
+      load_q(in[0]);
+      load_square(in[0].pf, pm, kTwo);
       turn.put(s.kt[0], a.K);
+      if (chunks > 1) {
+        next(1);
+        turn.load(kc, a.K, ODD && step_by_step);
+        load_q(in[1]);
+        load_square(in[1].pf, pm, kTwo);
+      }
     }
     lds_barrier();
-    for (int c = 0; c < chunks; ++c) {
+    two_by_two([&](auto buffer, int c) {
+      Chunk& m = in[decltype(buffer)::value];
       const int n = min(len - c * kC, kC);
-      const bool more = c + 1 < chunks;
+      const bool more = c + 2 < chunks;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) cut(qf[k], k);
-      if (more) {
-        next(c + 1);
-        turn.load(kc, a.K, ODD && step_by_step);
-      }
+      for (int k = 0; k < KS; ++k) cut(m.qf[k], k);
+      if (more) next(c + 2);
       f32x4 o[NV];
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) o[nt] = f32x4{0, 0, 0, 0};
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int nt = 0; nt < NV; ++nt) mma<2>(o[nt], qf[k], s.st.frag(nt * 16, k * 32));
+        for (int nt = 0; nt < NV; ++nt) mma<2>(o[nt], m.qf[k], s.st.frag(nt * 16, k * 32));
 #pragma unroll
-      for (int nt = 0; nt < NV; ++nt) o[nt] *= a.scale * eg;
-      if (more) {
-        load_q();
-        load_dec();
-      }
+      for (int nt = 0; nt < NV; ++nt) o[nt] *= a.scale * m.eg;
+      if (more) load_q(m);
       lds_barrier();
-      if (more) turn.put(s.kt[(c + 1) & 1], a.K);
+      if (c + 1 < chunks) turn.put(s.kt[1 - decltype(buffer)::value], a.K);
+      if (more) turn.load(kc, a.K, ODD && step_by_step);
       lds_barrier();
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) {
-        mma<2>(o[nt], pf[0], s.ut.frag(nt * 16, 0));
-        if (w >= 2) mma<2>(o[nt], pf[1], s.ut.frag(nt * 16, 32));
+        mma<2>(o[nt], m.pf[0], s.ut.frag(nt * 16, 0));
+        if (w >= 2) mma<2>(o[nt], m.pf[1], s.ut.frag(nt * 16, 32));
       }
-      if (more) load_square(pf, pm);
+      if (more) load_square(m.pf, pm, kTwo);
       if (n == kC && v0 + BV <= a.V) {
 #pragma unroll
         for (int nt = 0; nt < NV; ++nt)
@@ -766,7 +789,7 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
       }
       oc += kC * a.o_t;
       lds_barrier();
-    }
+    });
     // steps past the end
     IO* ob = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h;
     for (int64_t u = threadIdx.x - kThreads; u < int64_t(a.T - len) * BV; u += kThreads)
@@ -837,17 +860,25 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
     if (c + 2 == chunks) place(c);
   };
   if (chunks > 0) place(end);
+  auto two_by_two = [&](auto&& step) {
+    for (int c = chunks - 1; c >= 0; c -= 2) {
+      step(std::integral_constant<int, 0>{}, c);
+      if (c > 0) step(std::integral_constant<int, 1>{}, c - 1);
+    }
+  };
 
   if (wave < 4) {
-    Exact<M> kf[KS];
-    Both<M> tf[2], pf[2];
-    f32x4 eg, tail, beta;
+    struct Chunk {
+      Exact<M> kf[KS];
+      Both<M> tf[2], pf[2];
+      f32x4 eg, tail, beta;
+    } in[2];
     IO go[NV][4];
     IO* gvc = static_cast<IO*>(a.gv) + int64_t(bh) * a.V + end * kC * gv_t;
     float* drc = a.dr + top * kC * a.Vp;
-    auto load_k = [&]() {
+    auto load_k = [&](Chunk& n) {
 #pragma unroll
-      for (int k = 0; k < KS; ++k) kf[k] = exact_of<M>(load8(kc, at_k, k * 32 + q4 * 8, a.K, ODD && step_by_step));
+      for (int k = 0; k < KS; ++k) n.kf[k] = exact_of<M>(load8(kc, at_k, k * 32 + q4 * 8, a.K, ODD && step_by_step));
     };
     auto load_go = [&]() {
 #pragma unroll
@@ -859,19 +890,19 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
       if (w < 2) f[0] = load_planes<M>(m, row, q4 * 8);
       f[1] = load_planes<M>(m, row, 32 + q4 * 8);
     };
-    auto load_dec = [&]() {
-      eg = *reinterpret_cast<const f32x4*>(dec + i0);
-      tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
-      beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
+    auto load_dec = [&](Chunk& n) {
+      n.eg = *reinterpret_cast<const f32x4*>(dec + i0);
+      n.tail = *reinterpret_cast<const f32x4*>(dec + kC + i0);
+      n.beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
     };
-    auto put_go = [&](int c) {
+    auto put_go = [&](const Chunk& n, int c) {
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) {
         f32x4 os;
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           if (c * kC + i0 + x >= len || !vin[nt]) go[nt][x] = IO{};
-          os[x] = a.scale * eg[x] * widen(go[nt][x]);
+          os[x] = a.scale * n.eg[x] * widen(go[nt][x]);
         }
         s.ot.put4(nt * 16 + r, i0, E::bits(go[nt][0]), E::bits(go[nt][1]), E::bits(go[nt][2]), E::bits(go[nt][3]));
         s.os.put4(nt * 16 + r, i0, os);
@@ -879,74 +910,84 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
     };
     if (chunks > 0) {
       load_go();
-      load_dec();
-      load_k();
-      load_square(pf, pm);
-      load_square(tf, tm);
-      put_go(end);
+      load_dec(in[0]);
+      load_k(in[0]);
+      load_square(in[0].pf, pm);
+      load_square(in[0].tf, tm);
+      put_go(in[0], end);
+      if (chunks > 1) {
+        next(end - 1);
+        load_go();
+        load_dec(in[1]);
+        load_k(in[1]);
+        load_square(in[1].pf, pm);
+        load_square(in[1].tf, tm);
+      }
     }
     lds_barrier();
-    for (int c = end; c >= 0 && chunks > 0; --c) {
+    two_by_two([&](auto buffer, int c) {
+      Chunk& m = in[decltype(buffer)::value];
       const int n = min(len - c * kC, kC);
+      const bool more = c > 1;
       if (ODD) {
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-          typename E::Vec x = __builtin_bit_cast(typename E::Vec, kf[k]);
+          typename E::Vec x = __builtin_bit_cast(typename E::Vec, m.kf[k]);
           cut8(x, k * 32 + q4 * 8, a.K);
-          kf[k] = exact_of<M>(x);
+          m.kf[k] = exact_of<M>(x);
         }
       }
-      if (c > 0) {
-        next(c - 1);
-        load_go();
-      }
+      if (more) next(c - 2);
       f32x4 U[NV];
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) U[nt] = f32x4{0, 0, 0, 0};
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int nt = 0; nt < NV; ++nt) mma(U[nt], kf[k], s.st.frag(nt * 16, k * 32));
+        for (int nt = 0; nt < NV; ++nt) mma(U[nt], m.kf[k], s.st.frag(nt * 16, k * 32));
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) {
-        U[nt] *= tail;
-        if (w < 2) mma(U[nt], pf[0], s.ot.frag(nt * 16, 0));
-        mma(U[nt], pf[1], s.ot.frag(nt * 16, 32));
+        U[nt] *= m.tail;
+        if (w < 2) mma(U[nt], m.pf[0], s.ot.frag(nt * 16, 0));
+        mma(U[nt], m.pf[1], s.ot.frag(nt * 16, 32));
         s.ut.put4(nt * 16 + r, i0, U[nt]);
       }
-      if (c > 0) {
-        load_k();
-        load_square(pf, pm);
+      if (more) {
+        load_k(m);
+        load_square(m.pf, pm);
       }
       lds_barrier();
+      f32x4 R[NV];
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) {
-        f32x4 R = {0, 0, 0, 0};
-        if (w < 2) mma(R, tf[0], s.ut.frag(nt * 16, 0));
-        mma(R, tf[1], s.ut.frag(nt * 16, 32));
-        s.rt.put4(nt * 16 + r, i0, -eg * beta * R);
+        R[nt] = f32x4{0, 0, 0, 0};
+        if (w < 2) mma(R[nt], m.tf[0], s.ut.frag(nt * 16, 0));
+        mma(R[nt], m.tf[1], s.ut.frag(nt * 16, 32));
+        s.rt.put4(nt * 16 + r, i0, -m.eg * m.beta * R[nt]);
+      }
+      if (more) load_square(m.tf, tm);
 #pragma unroll
-        for (int x = 0; x < 4; ++x) behind(drc, uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = R[x];
-        R *= beta;
+      for (int nt = 0; nt < NV; ++nt) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) behind(drc, uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = R[nt][x];
+        R[nt] *= m.beta;
         if (n == kC && v0 + BV <= a.V) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[x]);
+          for (int x = 0; x < 4; ++x) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[nt][x]);
         } else {
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            if (i0 + x < n && vin[nt]) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[x]);
+            if (i0 + x < n && vin[nt]) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[nt][x]);
         }
       }
       gvc -= kC * gv_t;
       drc -= kC * a.Vp;
-      if (c > 0) {
-        load_square(tf, tm);
-        load_dec();
-      }
+      if (more) load_dec(m);
       lds_barrier();
-      if (c > 0) put_go(c - 1);
+      if (c > 0) put_go(in[1 - decltype(buffer)::value], c - 1);
+      if (more) load_go();
       lds_barrier();
-    }
+    });
     IO* gvb = static_cast<IO*>(a.gv) + int64_t(bh) * a.V;
     for (int64_t u = threadIdx.x; u < int64_t(a.T - len) * BV; u += kThreads)  // steps past the end
       if (v0 + u % BV < a.V) gvb[(len + u / BV) * gv_t + v0 + u % BV] = IO{};
@@ -966,23 +1007,27 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
 #pragma unroll
         for (int nt = 0; nt < NV; ++nt) s.st.put4(nt * 16 + r, (MT * w + m) * 16 + q4 * 4, S[m][nt]);
     };
-    float whole = 0.0f;
+    float whole[2] = {0.0f, 0.0f};
     float* dsc = a.ds + top * KP * a.Vp;
     if (chunks > 0) {
       kturn.load(kc, a.K, ODD && step_by_step);
       qturn.load(qc, a.K, ODD && step_by_step);
-      whole = dec[kC - 1];
+      whole[0] = dec[kC - 1];
       put_state();
-      kturn.put(s.kt[end & 1], a.K);
+      kturn.put(s.kt[0], a.K);
       qturn.put(s.qt, a.K);
-    }
-    lds_barrier();
-    for (int c = end; c >= 0 && chunks > 0; --c) {
-      if (c > 0) {
-        next(c - 1);
+      if (chunks > 1) {
+        next(end - 1);
         kturn.load(kc, a.K, ODD && step_by_step);
         qturn.load(qc, a.K, ODD && step_by_step);
+        whole[1] = dec[kC - 1];
       }
+    }
+    lds_barrier();
+    two_by_two([&](auto buffer, int c) {
+      constexpr int kNow = decltype(buffer)::value;
+      const bool more = c > 1;
+      if (more) next(c - 2);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -990,10 +1035,10 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
 #pragma unroll
           for (int x = 0; x < 4; ++x)
             behind(dsc, uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = S[m][nt][x];
-          S[m][nt] *= whole;
+          S[m][nt] *= whole[kNow];
         }
       dsc -= KP * a.Vp;
-      if (c > 0) whole = dec[kC - 1];
+      if (more) whole[kNow] = dec[kC - 1];
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -1004,8 +1049,12 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
         }
       lds_barrier();
       if (c > 0) {  // (q's products are done; k's of this chunk are not)
-        kturn.put(s.kt[(c - 1) & 1], a.K);
+        kturn.put(s.kt[1 - kNow], a.K);
         qturn.put(s.qt, a.K);
+      }
+      if (more) {
+        kturn.load(kc, a.K, ODD && step_by_step);
+        qturn.load(qc, a.K, ODD && step_by_step);
       }
       lds_barrier();
 #pragma unroll
@@ -1014,11 +1063,11 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
         for (int nt = 0; nt < NV; ++nt) {
           const Both<M> f = s.rt.frag(nt * 16, k * 32);
 #pragma unroll
-          for (int m = 0; m < MT; ++m) mma(S[m][nt], s.kt[c & 1].frag((MT * w + m) * 16, k * 32), f);
+          for (int m = 0; m < MT; ++m) mma(S[m][nt], s.kt[kNow].frag((MT * w + m) * 16, k * 32), f);
         }
       put_state();
       lds_barrier();
-    }
+    });
     if (a.gs0) {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
