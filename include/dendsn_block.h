@@ -43,7 +43,7 @@ typedef struct dendsn_delta_cfg {
     /* Strides of step, sequence and head: element (t, b, h, d) of q lies at
      * t * q_t + b * q_b + h * q_h + d, and so on (g and beta: without d).  Those of
      * inputs may be 0 (broadcast); rows of outputs may not overlap; 64 steps of a tensor,
-     * gradients among them, span less than 2^32 bytes (or T is 1). */
+     * gradients among them, span less than 2^31 bytes (or T is 1). */
     int64_t q_t, q_b, q_h, k_t, k_b, k_h, v_t, v_b, v_h, g_t, g_b, g_h, beta_t, beta_b, beta_h, o_t, o_b, o_h;
     int64_t grad_o_t, grad_o_b, grad_o_h;                    /* backward             */
     int32_t io;         /* dendsn_io of q, k, v, g, beta, o and their gradients */

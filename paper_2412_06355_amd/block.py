@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import struct
 from dataclasses import dataclass
 
 from .binding import IO
@@ -366,7 +367,7 @@ class AdamWConfig:
 
 
 def dendsn_adamw_step(cfg: AdamWConfig, tensors, count: int, step: int, step_dev, grad_scale, seed: int, stream):
-    """``tensors``: a ctypes array of dendsn_adamw_tensor."""
+    """``tensors``: a ctypes array of dendsn_adamw_tensor, or its bytes."""
     _check(block_lib().dendsn_adamw_step(ctypes.byref(cfg.to_c()), ctypes.cast(tensors, _P), count, step,
                                          _ptr(step_dev), _ptr(grad_scale), seed, stream))
 
@@ -403,35 +404,42 @@ def adamw(cfg: AdamWConfig, params, grads, states, step, *, copies=None, grad_sc
     dev = params[0].device
     f32, bf16, f8 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
     eight = STATE[cfg.state] == 1
-    array = (dendsn_adamw_tensor * count)()
-    for i in range(count):
-        p, g, s = params[i], grads[i], states[i]
-        shape, n = p.shape, p.numel()
-        _expect(p, "param", shape, f32, dev)
-        if g is None or g.dtype not in (f32, bf16):
-            raise ValueError("grad: expected torch.float32 or torch.bfloat16")
-        _expect(g, "grad", shape, None, dev)
-        if len(s) != (4 if eight else 2):
-            raise ValueError(f"states: {len(s)} tensors, expected {4 if eight else 2}")
-        c = copies[i] if copies is not None else None
-        _expect(c, "copy", shape, bf16, dev, optional=True)
+    state_type, parts = (f8, 4) if eight else (f32, 2)
+
+    pack = struct.Struct("@q7Pi4x").pack_into
+    array = bytearray(ctypes.sizeof(dendsn_adamw_tensor) * count)
+    gpu, here, ms, vs, c, at = dev.type == "cuda", params[0].get_device(), 0, 0, 0, 0
+    for i, (p, g, s) in enumerate(zip(params, grads, states)):
+        if len(s) != parts:
+            raise ValueError(f"states of tensor {i}: {len(s)} tensors, expected {parts}")
+        if g is None:
+            raise ValueError(f"grad of tensor {i} is required")
+        m, v, shape = s[0], s[parts // 2], p.shape
+        # of hundreds of tensors: in few steps whether all is well, else what is not
+        if not (gpu and p.dtype is f32 and p.is_contiguous() and p.get_device() == here
+                and g.is_contiguous() and g.get_device() == here and g.shape == shape
+                and m.dtype is state_type and m.is_contiguous() and m.get_device() == here and m.shape == shape
+                and v.dtype is state_type and v.is_contiguous() and v.get_device() == here and v.shape == shape):
+            for t, name, dtype in ((p, "param", f32), (g, "grad", None), (m, "m", state_type),
+                                   (v, "root" if eight else "v", state_type)):
+                _expect(t, f"{name} of tensor {i}", shape, dtype, dev)
+        half = g.dtype is bf16
+        if not half and g.dtype is not f32:
+            raise ValueError(f"grad of tensor {i}: expected torch.float32 or torch.bfloat16")
+        n = p.numel()
         if eight:
-            blocks = (-(-n // STATE_BLOCK),)
-            _expect(s[0], "m", shape, f8, dev)
-            _expect(s[1], "m_scale", blocks, f32, dev)
-            _expect(s[2], "root", shape, f8, dev)
-            _expect(s[3], "root_scale", blocks, f32, dev)
-            m, v, ms, vs = s[0], s[2], s[1].data_ptr(), s[3].data_ptr()
-        else:
-            m, v = s
-            _expect(m, "m", shape, f32, dev)
-            _expect(v, "v", shape, f32, dev)
-            ms = vs = None
-        array[i] = (n, p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), ms, vs,
-                    None if c is None else c.data_ptr(), 1 if g.dtype == bf16 else 0)
+            for t, name in ((s[1], "m_scale"), (s[3], "root_scale")):
+                _expect(t, f"{name} of tensor {i}", (-(-n // STATE_BLOCK),), f32, dev)
+            ms, vs = s[1].data_ptr(), s[3].data_ptr()
+        if copies is not None:
+            c = copies[i]
+            _expect(c, f"copy of tensor {i}", shape, bf16, dev, optional=True)
+            c = 0 if c is None else c.data_ptr()
+        pack(array, at, n, p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), ms, vs, c, half)
+        at += 72
     step_dev = None
     if isinstance(step, torch.Tensor):
         _expect(step, "step", (1,), torch.int32, dev)
         step, step_dev = 1, step
     _expect(grad_scale, "grad_scale", (1,), f32, dev, optional=True)
-    dendsn_adamw_step(cfg, array, count, int(step), step_dev, grad_scale, seed, _stream(dev))
+    dendsn_adamw_step(cfg, (ctypes.c_char * len(array)).from_buffer(array), count, int(step), step_dev, grad_scale, seed, _stream(dev))

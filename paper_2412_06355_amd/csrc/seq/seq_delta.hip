@@ -43,10 +43,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kC = 64;          // steps of a chunk
 constexpr int kThreads = 256;
-#ifndef SCANV
-#define SCANV 32
-#endif
-constexpr int kScanV = SCANV;      // columns of v of a block of the scans
+
 constexpr double kForget = -200.0;  // exp of it is 0 in fp32
 
 struct DeltaArgs {
@@ -62,9 +59,16 @@ struct DeltaArgs {
   float *part_q, *part_k;   // [T][batch][H][K] where heads are shared
   int64_t q_t, q_b, q_h, k_t, k_b, k_h, v_t, v_b, v_h, g_t, g_b, g_h, beta_t, beta_b, beta_h, o_t, o_b, o_h;
   int64_t go_t, go_b, go_h;
+  float *maps, *seg_in;     // [batch][H][segs]: [KP][Vp + KP], [KP][Vp]
   int32_t T, batch, H, Hk, K, V, nc, Vp;
+  int32_t segs, per, pass;  // segments of the steps, chunks of one, and what a scan does (Pass)
   float scale;
 };
+
+// A long sequence of few heads is cut into segments that go at once: the first pass starts each
+// from S = 0 beside K columns of the identity, which gives it as a map S -> M S + N of what enters
+// it; the maps are composed (delta_join_states); the second pass starts from the states.
+enum Pass { kWhole, kMaps, kStates };
 
 // ---------------------------------------------------------------------------
 // Operands.  A fragment is a lane's eight values of one row (or column): row
@@ -144,7 +148,7 @@ template <> struct Eight<bf16_t> {
 };
 
 // The value `at` places behind a base that is the same in all lanes: 64 steps of a tensor span
-// less than 2^32 bytes, and addresses are a scalar and 32 bits.
+// less than 2^31 bytes, and addresses are a scalar and 32 bits.
 template <typename T>
 __device__ __forceinline__ const T& behind(const T* base, uint32_t at) {
   return *reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + uint32_t(at * uint32_t(sizeof(T))));
@@ -152,6 +156,20 @@ __device__ __forceinline__ const T& behind(const T* base, uint32_t at) {
 template <typename T>
 __device__ __forceinline__ T& behind(T* base, uint32_t at) {
   return *reinterpret_cast<T*>(reinterpret_cast<char*>(base) + uint32_t(at * uint32_t(sizeof(T))));
+}
+
+// Stores by a descriptor drop what lies at 2^31 and beyond: a condition is an offset, and no branch
+// comes between the stores and what they are counted with.
+typedef __amdgpu_buffer_rsrc_t rsrc_t;
+constexpr uint32_t kNowhere = 0x80000000u;
+__device__ __forceinline__ rsrc_t stores_to(void* base, bool there = true) {
+  return __builtin_amdgcn_make_buffer_rsrc(base, 0, there ? int(kNowhere) : 0, 0x00020000);
+}
+__device__ __forceinline__ void put_at(rsrc_t to, uint32_t at, float v, float) {
+  __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), to, at, 0, 0);
+}
+__device__ __forceinline__ void put_at(rsrc_t to, uint32_t at, float v, bf16_t) {
+  __builtin_amdgcn_raw_buffer_store_b16(bf16_bits(v), to, at, 0, 0);
 }
 
 // Eight places from k0 on of the row of K that starts `row` places behind base, without a branch a
@@ -262,9 +280,9 @@ template <int P, int ROWS, int COLS> struct MatX<Bf<P>, ROWS, COLS> {
 // block of 4 x 8, in registers between the two.
 template <class M, int ROWS> struct Turn {
   using IO = typename M::IO;
-  static constexpr bool kAll = 2 * ROWS == kThreads;  // each of 256 threads has a block
   static_assert(2 * ROWS <= kThreads, "one block a thread");
-  __device__ __forceinline__ static int tid() { return threadIdx.x % kThreads; }
+  // (with fewer blocks than 256 threads several have the same one)
+  __device__ __forceinline__ static int tid() { return threadIdx.x % (2 * ROWS); }
   typename Eight<IO>::Vec r[4];
   uint32_t at[4];  // the four rows
   // steps past the n-th have the n-th's values
@@ -273,13 +291,11 @@ template <class M, int ROWS> struct Turn {
     for (int x = 0; x < 4; ++x) at[x] = uint32_t(min(tid() % 16 * 4 + x, n - 1)) * stride;
   }
   __device__ __forceinline__ void load(const IO* rows, int D, bool odd) {
-    if (!kAll && tid() >= 2 * ROWS) return;
 #pragma unroll
     for (int x = 0; x < 4; ++x) r[x] = load8(rows, at[x], tid() / 16 * 8, D, odd);
   }
   __device__ __forceinline__ void put(MatX<M, ROWS, kC>& dst, int D) {
     const int t = tid() % 16 * 4, d = tid() / 16 * 8;
-    if (!kAll && tid() >= 2 * ROWS) return;
     if (D < ROWS) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) cut8(r[x], d, D);
@@ -495,7 +511,9 @@ __global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
 // state's rows, which stay in its registers.  The second has q's products, the outputs, and
 // turns the next chunk's k over.  Three barriers a chunk: the state, R and U go through LDS.
 // What a chunk reads is fetched two chunks ahead, into the registers that are free again; the
-// barriers wait for LDS alone.
+// barriers wait for LDS alone.  A wave waits for a load by the number of loads and stores behind it,
+// on the path that has the fewest: so each is issued in every chunk (past the end the last one's
+// again), and stores that are not wanted go nowhere.
 // ---------------------------------------------------------------------------
 constexpr int kScanThreads = 512;
 
@@ -504,8 +522,8 @@ constexpr int kScanThreads = 512;
 struct ScanBlock {
   int v0, bh;
 };
-__device__ __forceinline__ ScanBlock scan_block(const DeltaArgs& a, int BV) {
-  const int cols = a.Vp / BV, m = blockIdx.x / 8, bh = m / cols * 8 + blockIdx.x % 8;
+__device__ __forceinline__ ScanBlock scan_block(const DeltaArgs& a, int KP, int BV) {
+  const int cols = (a.Vp + (a.pass == kMaps ? KP : 0)) / BV, m = blockIdx.x / 8, bh = m / cols * 8 + blockIdx.x % 8;
   return {m % cols * BV, bh < a.batch * a.H ? bh : -1};
 }
 
@@ -524,25 +542,29 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
   constexpr int KS = KP / 32, MT = KP / 64, NV = BV / 16;  // MT: row tiles of the state of a wave
   extern __shared__ __align__(16) char lds[];
   ScanLds<M, KP, BV>& s = *reinterpret_cast<ScanLds<M, KP, BV>*>(lds);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, w = wave % 4, r = lane % 16, q4 = lane / 16;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), w = wave % 4, r = lane % 16, q4 = lane / 16;
   const bool chain = wave < 4;
-  const ScanBlock at_block = scan_block(a, BV);
+  const ScanBlock at_block = scan_block(a, KP, BV);
   const int v0 = at_block.v0, bh = at_block.bh;
   if (bh < 0) return;
   const int b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
   const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), chunks = (len + kC - 1) / kC;
   const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
+  const bool maps = a.pass == kMaps;
+  const int c0 = blockIdx.y * a.per, c1 = min(chunks, c0 + a.per);  // the segment's chunks
+  const int64_t first = int64_t(bh) * a.nc + c0, seg = int64_t(bh) * a.segs + blockIdx.y;
   // the next chunk's, in turn
-  const IO* kc = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h;
-  const IO* qc = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h;
-  const IO* vc = static_cast<const IO*>(a.v) + b * a.v_b + h * a.v_h;
-  const Word* tm = static_cast<const Word*>(a.tm) + int64_t(bh) * a.nc * M::planes * kC * kC;
-  const Word* pm = static_cast<const Word*>(a.pm) + int64_t(bh) * a.nc * M::planes * kC * kC;
-  const float* dec = a.dec + int64_t(bh) * a.nc * 3 * kC;
+  const IO* kc = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h + c0 * kC * a.k_t;
+  const IO* qc = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h + c0 * kC * a.q_t;
+  const IO* vc = static_cast<const IO*>(a.v) + b * a.v_b + h * a.v_h + c0 * kC * a.v_t;
+  const Word* tm = static_cast<const Word*>(a.tm) + first * M::planes * kC * kC;
+  const Word* pm = static_cast<const Word*>(a.pm) + first * M::planes * kC * kC;
+  const float* dec = a.dec + first * 3 * kC;
   // this chunk's
-  IO* oc = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h;
-  float* ck_s = a.ck_s ? a.ck_s + int64_t(bh) * a.nc * KP * a.Vp : nullptr;
-  float* ck_u = a.ck_s ? a.ck_u + int64_t(bh) * a.nc * kC * a.Vp : nullptr;
+  IO* oc = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h + c0 * kC * a.o_t;
+  const bool keep = a.ck_s && !maps;
+  float* ck_s = a.ck_s + first * KP * a.Vp;
+  float* ck_u = a.ck_u + first * kC * a.Vp;
 
   // Rows past the sequence's end are read as its last one, columns past K and V as some other: their
   // betas are 0, their rows of the state stay 0 (Turn), their values are set to 0.  Where K is no
@@ -583,9 +605,9 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
     if (c + 1 == chunks) place(c);
   };
   auto two_by_two = [&](auto&& step) {  // (buffers are registers: which one has to be known when it is compiled)
-    for (int c = 0; c < chunks; c += 2) {
+    for (int c = c0; c < c1; c += 2) {
       step(std::integral_constant<int, 0>{}, c);
-      if (c + 1 < chunks) step(std::integral_constant<int, 1>{}, c + 1);
+      if (c + 1 < c1) step(std::integral_constant<int, 1>{}, c + 1);
     }
   };
   auto cut = [&](Exact<M>& f, int k) {
@@ -606,7 +628,12 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) S[m][nt][x] = a.s0 && state_in(m, nt, x) ? a.s0[state_at(m, nt, x)] : 0.0f;
+        for (int x = 0; x < 4; ++x) {
+          const int d = (MT * w + m) * 16 + q4 * 4 + x, v = v0 + nt * 16 + r;
+          if (maps) S[m][nt][x] = d == v - a.Vp ? 1.0f : 0.0f;
+          else if (a.pass == kStates && blockIdx.y > 0) S[m][nt][x] = a.seg_in[(seg * KP + d) * a.Vp + v];
+          else S[m][nt][x] = a.s0 && state_in(m, nt, x) ? a.s0[state_at(m, nt, x)] : 0.0f;
+        }
     auto put_state = [&]() {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
@@ -634,23 +661,21 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
       n.beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
       n.whole = dec[kC - 1];
     };
-    if (chunks > 0) {
-      place(0);
+    if (c0 < c1) {
+      place(c0);
       load_k(in[0]);
       load_square(in[0].tf, tm, kAll);
       load_dec(in[0]);
-      if (chunks > 1) {
-        next(1);
-        load_k(in[1]);
-        load_square(in[1].tf, tm, kAll);
-        load_dec(in[1]);
-      }
+      if (c0 + 1 < c1) next(c0 + 1);
+      load_k(in[1]);
+      load_square(in[1].tf, tm, kAll);
+      load_dec(in[1]);
       put_state();
     }
     lds_barrier();
     two_by_two([&](auto buffer, int c) {
       Chunk& n = in[decltype(buffer)::value];
-      const bool more = c + 2 < chunks;
+      const bool more = c + 2 < c1;
 #pragma unroll
       for (int k = 0; k < KS; ++k) cut(n.kf[k], k);
       if (more) next(c + 2);
@@ -668,15 +693,16 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
         for (int x = 0; x < 4; ++x) R[x] = n.beta[x] * ((vin[nt] ? widen(n.vv[nt][x]) : 0.0f) - n.eg[x] * ks[nt][x]);
         s.rt.put4(nt * 16 + r, i0, R);
       }
-      if (more) load_k(n);
-      if (ck_s) {
+      load_k(n);
+      {
+        const rsrc_t to = stores_to(ck_s, keep);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
           for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
             for (int x = 0; x < 4; ++x)
-              behind(ck_s, uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = S[m][nt][x];
+              put_at(to, 4 * (uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r), S[m][nt][x], 0.0f);
         ck_s += KP * a.Vp;
       }
       lds_barrier();
@@ -689,12 +715,13 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
         s.us.put4(nt * 16 + r, i0, n.tail * U[nt]);
         s.ut.put4(nt * 16 + r, i0, U[nt]);
       }
-      if (more) load_square(n.tf, tm, kAll);
-      if (ck_s) {
+      load_square(n.tf, tm, kAll);
+      {
+        const rsrc_t to = stores_to(ck_u, keep);
 #pragma unroll
         for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) behind(ck_u, uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = U[nt][x];
+          for (int x = 0; x < 4; ++x) put_at(to, 4 * (uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r), U[nt][x], 0.0f);
         ck_u += kC * a.Vp;
       }
       lds_barrier();
@@ -702,7 +729,7 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
       for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
         for (int m = 0; m < MT; ++m) S[m][nt] *= n.whole;
-      if (more) load_dec(n);
+      load_dec(n);
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -714,7 +741,15 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
       put_state();  // (all have read the one before)
       lds_barrier();
     });
-    if (a.s_last) {
+    if (maps) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            a.maps[(seg * KP + (MT * w + m) * 16 + q4 * 4 + x) * (a.Vp + KP) + v0 + nt * 16 + r] = S[m][nt][x];
+    } else if (a.s_last && (c0 < c1 ? c1 == chunks : c0 == 0)) {  // the segment with the sequence's end
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -723,6 +758,23 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
           for (int x = 0; x < 4; ++x)
             if (state_in(m, nt, x)) a.s_last[state_at(m, nt, x)] = S[m][nt][x];
     }
+  } else if (maps) {
+    if (c0 < c1) {
+      place(c0);
+      turn.load(kc, a.K, ODD && step_by_step);
+      turn.put(s.kt[0], a.K);
+      if (c0 + 1 < c1) next(c0 + 1);
+      turn.load(kc, a.K, ODD && step_by_step);
+    }
+    lds_barrier();
+    two_by_two([&](auto buffer, int c) {
+      if (c + 2 < c1) next(c + 2);
+      lds_barrier();
+      turn.put(s.kt[1 - decltype(buffer)::value], a.K);
+      turn.load(kc, a.K, ODD && step_by_step);
+      lds_barrier();
+      lds_barrier();
+    });
   } else {
     struct Chunk {
       Exact<M> qf[KS];
@@ -734,24 +786,22 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
       for (int k = 0; k < KS; ++k) n.qf[k] = exact_of<M>(row8(qc, at_q, k));
       n.eg = *reinterpret_cast<const f32x4*>(dec + i0);
     };
-    if (chunks > 0) {
-      place(0);
+    if (c0 < c1) {
+      place(c0);
       turn.load(kc, a.K, ODD && step_by_step);
       load_q(in[0]);
       load_square(in[0].pf, pm, kTwo);
       turn.put(s.kt[0], a.K);
-      if (chunks > 1) {
-        next(1);
-        turn.load(kc, a.K, ODD && step_by_step);
-        load_q(in[1]);
-        load_square(in[1].pf, pm, kTwo);
-      }
+      if (c0 + 1 < c1) next(c0 + 1);
+      turn.load(kc, a.K, ODD && step_by_step);
+      load_q(in[1]);
+      load_square(in[1].pf, pm, kTwo);
     }
     lds_barrier();
     two_by_two([&](auto buffer, int c) {
       Chunk& m = in[decltype(buffer)::value];
       const int n = min(len - c * kC, kC);
-      const bool more = c + 2 < chunks;
+      const bool more = c + 2 < c1;
 #pragma unroll
       for (int k = 0; k < KS; ++k) cut(m.qf[k], k);
       if (more) next(c + 2);
@@ -764,33 +814,28 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
         for (int nt = 0; nt < NV; ++nt) mma<2>(o[nt], m.qf[k], s.st.frag(nt * 16, k * 32));
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) o[nt] *= a.scale * m.eg;
-      if (more) load_q(m);
+      load_q(m);
       lds_barrier();
-      if (c + 1 < chunks) turn.put(s.kt[1 - decltype(buffer)::value], a.K);
-      if (more) turn.load(kc, a.K, ODD && step_by_step);
+      turn.put(s.kt[1 - decltype(buffer)::value], a.K);
+      turn.load(kc, a.K, ODD && step_by_step);
       lds_barrier();
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt) {
         mma<2>(o[nt], m.pf[0], s.ut.frag(nt * 16, 0));
         if (w >= 2) mma<2>(o[nt], m.pf[1], s.ut.frag(nt * 16, 32));
       }
-      if (more) load_square(m.pf, pm, kTwo);
-      if (n == kC && v0 + BV <= a.V) {
+      load_square(m.pf, pm, kTwo);
+      const rsrc_t to = stores_to(oc);
 #pragma unroll
-        for (int nt = 0; nt < NV; ++nt)
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t at = i0 + x < n ? uint32_t(i0 + x) * uint32_t(a.o_t * sizeof(IO)) : kNowhere;
 #pragma unroll
-          for (int x = 0; x < 4; ++x) behind(oc, uint32_t(i0 + x) * uint32_t(a.o_t) + vat[nt]) = narrow<IO>(o[nt][x]);
-      } else {
-#pragma unroll
-        for (int nt = 0; nt < NV; ++nt)
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-            if (i0 + x < n && vin[nt]) behind(oc, uint32_t(i0 + x) * uint32_t(a.o_t) + vat[nt]) = narrow<IO>(o[nt][x]);
+        for (int nt = 0; nt < NV; ++nt) put_at(to, vin[nt] ? at + vat[nt] * uint32_t(sizeof(IO)) : kNowhere, o[nt][x], IO{});
       }
       oc += kC * a.o_t;
       lds_barrier();
     });
-    // steps past the end
+    if (blockIdx.y > 0) return;  // steps past the end
     IO* ob = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h;
     for (int64_t u = threadIdx.x - kThreads; u < int64_t(a.T - len) * BV; u += kThreads)
       if (v0 + u % BV < a.V) ob[(len + u / BV) * a.o_t + v0 + u % BV] = IO{};
@@ -817,14 +862,16 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
   constexpr int KS = KP / 32, MT = KP / 64, NV = BV / 16;
   extern __shared__ __align__(16) char lds[];
   BackLds<M, KP, BV>& s = *reinterpret_cast<BackLds<M, KP, BV>*>(lds);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, w = wave % 4, r = lane % 16, q4 = lane / 16;
-  const ScanBlock at_block = scan_block(a, BV);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), w = wave % 4, r = lane % 16, q4 = lane / 16;
+  const ScanBlock at_block = scan_block(a, KP, BV);
   const int v0 = at_block.v0, bh = at_block.bh;
   if (bh < 0) return;
   const int b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
-  const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), chunks = (len + kC - 1) / kC, end = max(chunks - 1, 0);
+  const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), chunks = (len + kC - 1) / kC;
+  const bool maps = a.pass == kMaps;
+  const int c0 = blockIdx.y * a.per, c1 = min(chunks, c0 + a.per), end = max(c1 - 1, 0);  // the segment's chunks
   const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
-  const int64_t gv_t = int64_t(a.batch) * a.H * a.V, top = int64_t(bh) * a.nc + end;
+  const int64_t gv_t = int64_t(a.batch) * a.H * a.V, top = int64_t(bh) * a.nc + end, seg = int64_t(bh) * a.segs + blockIdx.y;
   // of the chunk that is loaded next
   const IO* kc = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h + end * kC * a.k_t;
   const IO* qc = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h + end * kC * a.q_t;
@@ -857,13 +904,13 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
     tm -= M::planes * kC * kC;
     pm -= M::planes * kC * kC;
     dec -= 3 * kC;
-    if (c + 2 == chunks) place(c);
+    if (c + 2 == c1) place(c);
   };
-  if (chunks > 0) place(end);
+  if (c0 < c1) place(end);
   auto two_by_two = [&](auto&& step) {
-    for (int c = chunks - 1; c >= 0; c -= 2) {
+    for (int c = c1 - 1; c >= c0; c -= 2) {
       step(std::integral_constant<int, 0>{}, c);
-      if (c > 0) step(std::integral_constant<int, 1>{}, c - 1);
+      if (c > c0) step(std::integral_constant<int, 1>{}, c - 1);
     }
   };
 
@@ -908,27 +955,25 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
         s.os.put4(nt * 16 + r, i0, os);
       }
     };
-    if (chunks > 0) {
+    if (c0 < c1) {
       load_go();
       load_dec(in[0]);
       load_k(in[0]);
       load_square(in[0].pf, pm);
       load_square(in[0].tf, tm);
       put_go(in[0], end);
-      if (chunks > 1) {
-        next(end - 1);
-        load_go();
-        load_dec(in[1]);
-        load_k(in[1]);
-        load_square(in[1].pf, pm);
-        load_square(in[1].tf, tm);
-      }
+      if (c0 + 1 < c1) next(end - 1);
+      load_go();
+      load_dec(in[1]);
+      load_k(in[1]);
+      load_square(in[1].pf, pm);
+      load_square(in[1].tf, tm);
     }
     lds_barrier();
     two_by_two([&](auto buffer, int c) {
       Chunk& m = in[decltype(buffer)::value];
       const int n = min(len - c * kC, kC);
-      const bool more = c > 1;
+      const bool more = c > c0 + 1;
       if (ODD) {
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
@@ -952,10 +997,8 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
         mma(U[nt], m.pf[1], s.ot.frag(nt * 16, 32));
         s.ut.put4(nt * 16 + r, i0, U[nt]);
       }
-      if (more) {
-        load_k(m);
-        load_square(m.pf, pm);
-      }
+      load_k(m);
+      load_square(m.pf, pm);
       lds_barrier();
       f32x4 R[NV];
 #pragma unroll
@@ -965,29 +1008,26 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
         mma(R[nt], m.tf[1], s.ut.frag(nt * 16, 32));
         s.rt.put4(nt * 16 + r, i0, -m.eg * m.beta * R[nt]);
       }
-      if (more) load_square(m.tf, tm);
+      load_square(m.tf, tm);
+      const rsrc_t to_dr = stores_to(drc, !maps), to_gv = stores_to(gvc, !maps);
 #pragma unroll
-      for (int nt = 0; nt < NV; ++nt) {
+      for (int x = 0; x < 4; ++x) {
+        const uint32_t at = i0 + x < n ? uint32_t(i0 + x) * uint32_t(gv_t * sizeof(IO)) : kNowhere;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) behind(drc, uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = R[nt][x];
-        R[nt] *= m.beta;
-        if (n == kC && v0 + BV <= a.V) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[nt][x]);
-        } else {
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-            if (i0 + x < n && vin[nt]) behind(gvc, uint32_t(i0 + x) * uint32_t(gv_t) + vat[nt]) = narrow<IO>(R[nt][x]);
+        for (int nt = 0; nt < NV; ++nt) {
+          put_at(to_dr, 4 * (uint32_t(i0 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r), R[nt][x], 0.0f);
+          put_at(to_gv, vin[nt] ? at + vat[nt] * uint32_t(sizeof(IO)) : kNowhere, m.beta[x] * R[nt][x], IO{});
         }
       }
       gvc -= kC * gv_t;
       drc -= kC * a.Vp;
-      if (more) load_dec(m);
+      load_dec(m);
       lds_barrier();
-      if (c > 0) put_go(in[1 - decltype(buffer)::value], c - 1);
-      if (more) load_go();
+      put_go(in[1 - decltype(buffer)::value], c - 1);
+      load_go();
       lds_barrier();
     });
+    if (maps || blockIdx.y > 0) return;
     IO* gvb = static_cast<IO*>(a.gv) + int64_t(bh) * a.V;
     for (int64_t u = threadIdx.x; u < int64_t(a.T - len) * BV; u += kThreads)  // steps past the end
       if (v0 + u % BV < a.V) gvb[(len + u / BV) * gv_t + v0 + u % BV] = IO{};
@@ -1000,7 +1040,12 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
 #pragma unroll
       for (int nt = 0; nt < NV; ++nt)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) S[m][nt][x] = a.gs_last && state_in(m, nt, x) ? a.gs_last[state_at(m, nt, x)] : 0.0f;
+        for (int x = 0; x < 4; ++x) {
+          const int d = (MT * w + m) * 16 + q4 * 4 + x, v = v0 + nt * 16 + r;
+          if (maps) S[m][nt][x] = d == v - a.Vp ? 1.0f : 0.0f;
+          else if (a.pass == kStates && int(blockIdx.y) + 1 < a.segs) S[m][nt][x] = a.seg_in[(seg * KP + d) * a.Vp + v];
+          else S[m][nt][x] = a.gs_last && state_in(m, nt, x) ? a.gs_last[state_at(m, nt, x)] : 0.0f;
+        }
     auto put_state = [&]() {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
@@ -1009,36 +1054,35 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
     };
     float whole[2] = {0.0f, 0.0f};
     float* dsc = a.ds + top * KP * a.Vp;
-    if (chunks > 0) {
+    if (c0 < c1) {
       kturn.load(kc, a.K, ODD && step_by_step);
       qturn.load(qc, a.K, ODD && step_by_step);
       whole[0] = dec[kC - 1];
       put_state();
       kturn.put(s.kt[0], a.K);
       qturn.put(s.qt, a.K);
-      if (chunks > 1) {
-        next(end - 1);
-        kturn.load(kc, a.K, ODD && step_by_step);
-        qturn.load(qc, a.K, ODD && step_by_step);
-        whole[1] = dec[kC - 1];
-      }
+      if (c0 + 1 < c1) next(end - 1);
+      kturn.load(kc, a.K, ODD && step_by_step);
+      qturn.load(qc, a.K, ODD && step_by_step);
+      whole[1] = dec[kC - 1];
     }
     lds_barrier();
     two_by_two([&](auto buffer, int c) {
       constexpr int kNow = decltype(buffer)::value;
-      const bool more = c > 1;
+      const bool more = c > c0 + 1;
       if (more) next(c - 2);
+      const rsrc_t to = stores_to(dsc, !maps);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int nt = 0; nt < NV; ++nt) {
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            behind(dsc, uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r) = S[m][nt][x];
+            put_at(to, 4 * (uint32_t((MT * w + m) * 16 + q4 * 4 + x) * uint32_t(a.Vp) + v0 + nt * 16 + r), S[m][nt][x], 0.0f);
           S[m][nt] *= whole[kNow];
         }
       dsc -= KP * a.Vp;
-      if (more) whole[kNow] = dec[kC - 1];
+      whole[kNow] = dec[kC - 1];
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -1048,14 +1092,11 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
           for (int m = 0; m < MT; ++m) mma(S[m][nt], s.qt.frag((MT * w + m) * 16, k * 32), f);
         }
       lds_barrier();
-      if (c > 0) {  // (q's products are done; k's of this chunk are not)
-        kturn.put(s.kt[1 - kNow], a.K);
-        qturn.put(s.qt, a.K);
-      }
-      if (more) {
-        kturn.load(kc, a.K, ODD && step_by_step);
-        qturn.load(qc, a.K, ODD && step_by_step);
-      }
+      // (q's products are done; k's of this chunk are not)
+      kturn.put(s.kt[1 - kNow], a.K);
+      qturn.put(s.qt, a.K);
+      kturn.load(kc, a.K, ODD && step_by_step);
+      qturn.load(qc, a.K, ODD && step_by_step);
       lds_barrier();
 #pragma unroll
       for (int k = 0; k < 2; ++k)
@@ -1068,7 +1109,15 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
       put_state();
       lds_barrier();
     });
-    if (a.gs0) {
+    if (maps) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int nt = 0; nt < NV; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            a.maps[(seg * KP + (MT * w + m) * 16 + q4 * 4 + x) * (a.Vp + KP) + v0 + nt * 16 + r] = S[m][nt][x];
+    } else if (a.gs0 && blockIdx.y == 0) {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -1077,6 +1126,60 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
           for (int x = 0; x < 4; ++x)
             if (state_in(m, nt, x)) a.gs0[state_at(m, nt, x)] = S[m][nt][x];
     }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// join_states: the states that enter the segments, S = M S + N from one to the next (back: from
+// the last down), 16 columns of v a block, in fp32.  A wave has a quarter of the rows; the next
+// segment's map is on its way meanwhile.
+// ---------------------------------------------------------------------------
+template <int KP>
+__global__ __launch_bounds__(kThreads) void delta_join_states_kernel(DeltaArgs a, const float* from, bool back) {
+  constexpr int KS = KP / 32, MT = KP / 64;
+  __shared__ __align__(16) Mat<F32, 16, KP> st;
+  const int lane = threadIdx.x & 63, w = threadIdx.x / 64, r = lane % 16, q4 = lane / 16;
+  const int v = blockIdx.x * 16 + r, bh = blockIdx.y, ld = a.Vp + KP;
+  auto map_of = [&](int n) { return a.maps + (int64_t(bh) * a.segs + (back ? a.segs - 1 - n : n)) * KP * ld; };
+  f32x4 S[MT], N[MT];
+  Both<F32> mf[MT][KS];
+  auto load = [&](int n) {
+    const float* map = map_of(n);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) mf[m][k] = load_both<F32>(map + int64_t((MT * w + m) * 16 + r) * ld + a.Vp + k * 32 + q4 * 8);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) N[m][x] = map[int64_t((MT * w + m) * 16 + q4 * 4 + x) * ld + v];
+    }
+  };
+  load(0);
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int d = (MT * w + m) * 16 + q4 * 4 + x;
+      S[m][x] = from && d < a.K && v < a.V ? from[(int64_t(bh) * a.K + d) * a.V + v] : 0.0f;
+    }
+  for (int n = 0; n + 1 < a.segs; ++n) {
+#pragma unroll
+    for (int m = 0; m < MT; ++m) st.put4(r, (MT * w + m) * 16 + q4 * 4, S[m]);
+    lds_barrier();
+#pragma unroll
+    for (int m = 0; m < MT; ++m) S[m] = N[m];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+      const Both<F32> f = st.frag(0, k * 32);
+#pragma unroll
+      for (int m = 0; m < MT; ++m) mma(S[m], mf[m][k], f);
+    }
+    load(n + 2 < a.segs ? n + 1 : n);
+    float* to = a.seg_in + (int64_t(bh) * a.segs + (back ? a.segs - 2 - n : n + 1)) * KP * a.Vp;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) to[int64_t((MT * w + m) * 16 + q4 * 4 + x) * a.Vp + v] = S[m][x];
+    lds_barrier();
   }
 }
 
@@ -1477,11 +1580,11 @@ dendsn_status check_cfg(const dendsn_delta_cfg* c) {
                          c->beta_t, c->beta_b, c->beta_h, c->o_t, c->o_b, c->o_h, c->grad_o_t, c->grad_o_b, c->grad_o_h};
   for (int i = 0; i < 21; i += 3)
     if (!strides_fit(c, s[i], s[i + 1], s[i + 2])) return fail(DENDSN_E_INVALID, "a stride is negative or too large");
-  // 64 steps of a tensor lie within 2^32 bytes (gradients are contiguous)
+  // 64 steps of a tensor lie within 2^31 bytes (gradients are contiguous)
   int64_t most = c->batch * c->H * (c->V > c->K ? c->V : c->K);
   for (int i = 0; i < 21; i += 3) most = s[i] > most ? s[i] : most;
-  if (c->T > 1 && most >= (int64_t(1) << 32) / kC / (c->io == DENDSN_IO_BF16 ? 2 : 4))
-    return fail(DENDSN_E_UNSUPPORTED, "64 steps of a tensor span 2^32 bytes or more");
+  if (c->T > 1 && most >= (int64_t(1) << 31) / kC / (c->io == DENDSN_IO_BF16 ? 2 : 4))
+    return fail(DENDSN_E_UNSUPPORTED, "64 steps of a tensor span 2^31 bytes or more");
   return DENDSN_OK;
 }
 
@@ -1505,10 +1608,12 @@ struct DeltaPlan {
   int64_t nc, items, Vp;
   int KP;
   size_t ck_u, ckpt;                               // offset of the values, whole size
-  size_t tm, pm, dec, dr, ds, part_q, part_k;      // of the scratch
+  int segs, per;                                   // of the steps, and chunks of one
+  size_t tm, pm, dec, maps, seg_in, dr, ds, part_q, part_k;  // of the scratch
   size_t forward, backward;
 };
 
+constexpr int64_t kCus = 256;
 using Wide = Bf<3>;    // of the scans: their states are outputs in fp32
 using Narrow = Bf<2>;  // of what ends in bf16
 
@@ -1528,6 +1633,21 @@ DeltaPlan make_plan(const dendsn_delta_cfg* c) {
   p.tm = w.take(size_t(p.items) * square);
   p.pm = w.take(size_t(p.items) * square);
   p.dec = w.take(size_t(p.items) * 3 * kC * 4);
+  // With few heads the steps are cut into segments: the number that takes the fewest rounds of chunks,
+  // a CU having one block at a time, where each chunk goes through both passes and a join takes about
+  // a chunk's time (16384 steps of 4 heads, bf16, forward: 626 us whole).
+  const int64_t heads = c->batch * c->H, states = p.Vp / 16 * heads, maps = (p.Vp + p.KP) / 16 * heads;
+  int64_t segs = 1, least = p.nc * ceil_div(states, kCus);
+  for (int64_t n = 2; n <= 64 && 4 * n <= p.nc; ++n) {
+    const int64_t rounds = ceil_div(p.nc, n) * (ceil_div(states * n, kCus) + ceil_div(maps * n, kCus)) + n;
+    if (rounds < least) segs = n, least = rounds;
+  }
+  p.per = int(ceil_div(p.nc, segs));
+  p.segs = int(ceil_div(p.nc, p.per));
+  if (p.segs > 1) {
+    p.maps = w.take(size_t(c->batch) * c->H * p.segs * p.KP * (p.Vp + p.KP) * 4);
+    p.seg_in = w.take(size_t(c->batch) * c->H * p.segs * p.KP * p.Vp * 4);
+  }
   p.forward = w.at;
   p.dr = w.take(size_t(p.items) * kC * p.Vp * 4);
   p.ds = w.take(size_t(p.items) * p.KP * p.Vp * 4);
@@ -1550,6 +1670,9 @@ void fill_args(const dendsn_delta_cfg* c, const DeltaPlan& p, void* workspace, D
   a.tm = w + p.tm;
   a.pm = w + p.pm;
   a.dec = reinterpret_cast<float*>(w + p.dec);
+  a.maps = reinterpret_cast<float*>(w + p.maps);
+  a.seg_in = reinterpret_cast<float*>(w + p.seg_in);
+  a.segs = p.segs; a.per = p.per;
   a.dr = reinterpret_cast<float*>(w + p.dr);
   a.ds = reinterpret_cast<float*>(w + p.ds);
   a.part_q = reinterpret_cast<float*>(w + p.part_q);
@@ -1562,25 +1685,40 @@ bool allow_lds(F* kernel, size_t bytes) {
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(bytes)) == hipSuccess;
 }
 
+// A scan over the steps at once, or over segments of them: their maps, the states that enter, the rest.
+template <int KP, typename K>
+void scan_passes(K kernel, size_t bytes, int BV, DeltaArgs a, const float* from, bool back, hipStream_t stream) {
+  const int64_t heads = int64_t(a.batch) * a.H;
+  auto grid = [&](int64_t cols) { return dim3(unsigned(cols / BV * round_up(heads, 8)), unsigned(a.segs)); };
+  a.pass = kWhole;
+  if (a.segs > 1) {
+    a.pass = kMaps;
+    kernel<<<grid(a.Vp + KP), dim3(kScanThreads), bytes, stream>>>(a);
+    delta_join_states_kernel<KP><<<dim3(unsigned(a.Vp / 16), unsigned(heads)), dim3(kThreads), 0, stream>>>(a, from, back);
+    a.pass = kStates;
+  }
+  kernel<<<grid(a.Vp), dim3(kScanThreads), bytes, stream>>>(a);
+}
+
 template <class M, int KP, int BV, bool ODD>
 dendsn_status launch_scan(const DeltaArgs& a, hipStream_t stream) {
-  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / BV * round_up(int64_t(a.batch) * a.H, 8)));
+  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch));
   constexpr size_t bytes = sizeof(ScanLds<M, KP, BV>);
   static_assert(bytes <= 160 * 1024, "LDS of a CU");
   if (!allow_lds(delta_scan_kernel<M, KP, BV, ODD>, bytes)) return fail(DENDSN_E_HIP, "delta forward: %zu bytes of LDS refused", bytes);
   delta_local_kernel<M, KP, false><<<heads, dim3(kThreads), 0, stream>>>(a);
-  delta_scan_kernel<M, KP, BV, ODD><<<cols, dim3(kScanThreads), bytes, stream>>>(a);
+  scan_passes<KP>(delta_scan_kernel<M, KP, BV, ODD>, bytes, BV, a, a.s0, false, stream);
   return launched("delta forward");
 }
 
 template <class M, int KP, int BV, bool ODD>
 dendsn_status launch_back_scan(const DeltaArgs& a, hipStream_t stream) {
-  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch)), cols(unsigned(a.Vp / BV * round_up(int64_t(a.batch) * a.H, 8)));
+  const dim3 heads(unsigned(a.nc), unsigned(a.H), unsigned(a.batch));
   constexpr size_t bytes = sizeof(BackLds<M, KP, BV>);
   static_assert(bytes <= 160 * 1024, "LDS of a CU");
   if (!allow_lds(delta_back_scan_kernel<M, KP, BV, ODD>, bytes)) return fail(DENDSN_E_HIP, "delta backward: %zu bytes of LDS refused", bytes);
   delta_local_kernel<M, KP, true><<<heads, dim3(kThreads), 0, stream>>>(a);
-  delta_back_scan_kernel<M, KP, BV, ODD><<<cols, dim3(kScanThreads), bytes, stream>>>(a);
+  scan_passes<KP>(delta_back_scan_kernel<M, KP, BV, ODD>, bytes, BV, a, a.gs_last, true, stream);
   return launched("delta backward");
 }
 
@@ -1600,19 +1738,26 @@ dendsn_status launch_back_local(const DeltaArgs& a, hipStream_t stream) {
   return launched("delta backward");
 }
 
-template <class M, class L, int KP>
+// 32 columns of v a block where that gives each CU one, else 16: what a chunk reads of q, k, T and P
+// is half as much a column, but a block's chunk takes longer (16 and 32, forward and back, bf16, heads
+// of 128 x 128: 32 heads of 2048 steps 102 + 116 and 129 + 155 us, 64 of 8192 steps 955 + 1023 and
+// 646 + 741).
+template <class M, class L, int KP, bool ODD>
 dendsn_status launch(const DeltaArgs& a, bool back, hipStream_t stream) {
-  constexpr int BV = kScanV;
-  const bool odd = a.K % 8;
-  if (!back) return odd ? launch_scan<M, KP, BV, true>(a, stream) : launch_scan<M, KP, BV, false>(a, stream);
-  const dendsn_status st = odd ? launch_back_scan<M, KP, BV, true>(a, stream) : launch_back_scan<M, KP, BV, false>(a, stream);
+  const bool wide = int64_t(a.Vp / 32) * a.batch * a.H >= 256;
+  if (!back) return wide ? launch_scan<M, KP, 32, ODD>(a, stream) : launch_scan<M, KP, 16, ODD>(a, stream);
+  const dendsn_status st = wide ? launch_back_scan<M, KP, 32, ODD>(a, stream) : launch_back_scan<M, KP, 16, ODD>(a, stream);
   return st != DENDSN_OK ? st : launch_back_local<L, KP>(a, stream);
 }
 
+template <class M, class L>
+dendsn_status launch(const DeltaArgs& a, bool back, hipStream_t stream) {
+  if (a.K % 8) return a.K <= 64 ? launch<M, L, 64, true>(a, back, stream) : launch<M, L, 128, true>(a, back, stream);
+  return a.K <= 64 ? launch<M, L, 64, false>(a, back, stream) : launch<M, L, 128, false>(a, back, stream);
+}
+
 dendsn_status launch(const dendsn_delta_cfg* c, const DeltaArgs& a, bool back, hipStream_t stream) {
-  if (c->io == DENDSN_IO_BF16)
-    return kp_of(c) == 64 ? launch<Wide, Narrow, 64>(a, back, stream) : launch<Wide, Narrow, 128>(a, back, stream);
-  return kp_of(c) == 64 ? launch<F32, F32, 64>(a, back, stream) : launch<F32, F32, 128>(a, back, stream);
+  return c->io == DENDSN_IO_BF16 ? launch<Wide, Narrow>(a, back, stream) : launch<F32, F32>(a, back, stream);
 }
 
 dendsn_status copy_states(const dendsn_delta_cfg* c, const float* from, float* to, hipStream_t stream, const char* what) {

@@ -15,7 +15,7 @@
 namespace dendsn_seq {
 namespace {
 
-constexpr int kE = 4;  // packs of a lane kept in registers
+constexpr int kMost = 4;  // packs of a lane that may be kept in registers
 constexpr float kTop = 448.0f;  // the largest e4m3 value
 
 template <typename IO> constexpr int kV = 16 / int(sizeof(IO));
@@ -102,7 +102,7 @@ __device__ __forceinline__ void store_e4m3(uint8_t* row, int base, int D, const 
   }
 }
 
-template <typename IO, int TPR, bool E4M3>
+template <typename IO, int TPR, int kE, bool E4M3>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_kernel(NormArgs a) {
   constexpr int V = kV<IO>, kBlock = TPR > 256 ? TPR : 256;
   __shared__ float red[TPR > 64 ? TPR / 64 : 1];
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_kernel(NormArg
   }
 }
 
-template <typename IO, int TPR, bool W>
+template <typename IO, int TPR, int kE, bool W>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(NormArgs a) {
   constexpr int V = kV<IO>, kBlock = TPR > 256 ? TPR : 256, kRows = kBlock / TPR;
   __shared__ float red[TPR > 64 ? TPR / 64 : 1];
@@ -353,35 +353,49 @@ dendsn_status check_cfg(const dendsn_norm_cfg* c) {
   return DENDSN_OK;
 }
 
-int lanes_of(const dendsn_norm_cfg* c) {  // of a row
-  const int64_t packs = ceil_div(c->D, c->io == DENDSN_IO_BF16 ? 8 : 4);
-  return packs <= 16 * kE ? 16 : packs <= 64 * kE ? 64 : packs <= 256 * kE ? 256 : 1024;
+struct Shape {
+  int lanes, packs;  // of a row, of a lane
+};
+Shape shape_of(const dendsn_norm_cfg* c) {
+  const int64_t n = ceil_div(c->D, c->io == DENDSN_IO_BF16 ? 8 : 4);
+  const int lanes = n <= 16 * kMost ? 16 : n <= 64 * kMost ? 64 : n <= 256 * kMost ? 256 : 1024;
+  return {lanes, n <= lanes ? 1 : n <= 2 * lanes ? 2 : kMost};
 }
 
 // Blocks of the backward: four of 256 threads a CU, or one of 1024.
 int64_t parts_of(const dendsn_norm_cfg* c) {
-  const int lanes = lanes_of(c), rows = lanes < 256 ? 256 / lanes : 1;
+  const int lanes = shape_of(c).lanes, rows = lanes < 256 ? 256 / lanes : 1;
   const int64_t blocks = ceil_div(c->N, rows), most = lanes == 1024 ? 256 : 1024;
   return blocks < most ? blocks : most;
 }
 
+template <typename F>
+void dispatch(Shape s, F&& f) {
+  auto packs = [&](auto lanes) {
+    if (s.packs == 1) f(lanes, std::integral_constant<int, 1>{});
+    else if (s.packs == 2) f(lanes, std::integral_constant<int, 2>{});
+    else f(lanes, std::integral_constant<int, kMost>{});
+  };
+  if (s.lanes == 16) packs(std::integral_constant<int, 16>{});
+  else if (s.lanes == 64) packs(std::integral_constant<int, 64>{});
+  else if (s.lanes == 256) packs(std::integral_constant<int, 256>{});
+  else packs(std::integral_constant<int, 1024>{});
+}
+
 template <typename IO, bool E4M3>
-void launch_forward(const NormArgs& a, int lanes, hipStream_t stream) {
-  const int rows = lanes < 256 ? 256 / lanes : 1;
-  const dim3 grid(unsigned(ceil_div(a.N, rows))), block(lanes > 256 ? lanes : 256);
-  if (lanes == 16) norm_fwd_kernel<IO, 16, E4M3><<<grid, block, 0, stream>>>(a);
-  else if (lanes == 64) norm_fwd_kernel<IO, 64, E4M3><<<grid, block, 0, stream>>>(a);
-  else if (lanes == 256) norm_fwd_kernel<IO, 256, E4M3><<<grid, block, 0, stream>>>(a);
-  else norm_fwd_kernel<IO, 1024, E4M3><<<grid, block, 0, stream>>>(a);
+void launch_forward(const NormArgs& a, Shape s, hipStream_t stream) {
+  const dim3 grid(unsigned(ceil_div(a.N, s.lanes < 256 ? 256 / s.lanes : 1))), block(s.lanes > 256 ? s.lanes : 256);
+  dispatch(s, [&](auto lanes, auto packs) {
+    norm_fwd_kernel<IO, decltype(lanes)::value, decltype(packs)::value, E4M3><<<grid, block, 0, stream>>>(a);
+  });
 }
 
 template <typename IO, bool W>
-void launch_backward(const NormArgs& a, int lanes, int64_t blocks, hipStream_t stream) {
-  const dim3 grid{unsigned(blocks)}, block(lanes > 256 ? lanes : 256);
-  if (lanes == 16) norm_bwd_kernel<IO, 16, W><<<grid, block, 0, stream>>>(a);
-  else if (lanes == 64) norm_bwd_kernel<IO, 64, W><<<grid, block, 0, stream>>>(a);
-  else if (lanes == 256) norm_bwd_kernel<IO, 256, W><<<grid, block, 0, stream>>>(a);
-  else norm_bwd_kernel<IO, 1024, W><<<grid, block, 0, stream>>>(a);
+void launch_backward(const NormArgs& a, Shape s, int64_t blocks, hipStream_t stream) {
+  const dim3 grid{unsigned(blocks)}, block(s.lanes > 256 ? s.lanes : 256);
+  dispatch(s, [&](auto lanes, auto packs) {
+    norm_bwd_kernel<IO, decltype(lanes)::value, decltype(packs)::value, W><<<grid, block, 0, stream>>>(a);
+  });
 }
 
 dendsn_status forward(const dendsn_norm_cfg* cfg, const void* x, const void* residual, const void* weight, void* y,
@@ -391,7 +405,7 @@ dendsn_status forward(const dendsn_norm_cfg* cfg, const void* x, const void* res
   if (st != DENDSN_OK) return st;
   const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
   // a row has a block at least, of up to 1024 threads: a launch has fewer than 2^32
-  if (cfg->N > (int64_t(1) << 23) && lanes_of(cfg) >= 256) return fail(DENDSN_E_UNSUPPORTED, "more than 2^23 rows of this length");
+  if (cfg->N > (int64_t(1) << 23) && shape_of(cfg).lanes >= 256) return fail(DENDSN_E_UNSUPPORTED, "more than 2^23 rows of this length");
   if (cfg->N > 0 && (!x || !y || (e4m3 && !scale))) return fail(DENDSN_E_INVALID, e4m3 ? "x, y or scale is NULL" : "x or y is NULL");
   if (!aligned(x, esz) || !aligned(residual, esz) || !aligned(weight, esz) || !aligned(sum, esz) || (!e4m3 && !aligned(y, esz)))
     return fail(DENDSN_E_INVALID, "x, residual, weight, y or sum misaligned");
@@ -401,9 +415,9 @@ dendsn_status forward(const dendsn_norm_cfg* cfg, const void* x, const void* res
   a.x = x; a.residual = residual; a.w = weight; a.y = y; a.sum = sum; a.rstd = rstd; a.scale = scale;
   a.ld_x = cfg->ld_x; a.ld_residual = cfg->ld_residual; a.ld_y = cfg->ld_y; a.ld_sum = cfg->ld_sum;
   a.N = int32_t(cfg->N); a.D = int32_t(cfg->D); a.eps = cfg->eps;
-  const int lanes = lanes_of(cfg);
-  if (cfg->io == DENDSN_IO_BF16) e4m3 ? launch_forward<bf16_t, true>(a, lanes, stream) : launch_forward<bf16_t, false>(a, lanes, stream);
-  else e4m3 ? launch_forward<float, true>(a, lanes, stream) : launch_forward<float, false>(a, lanes, stream);
+  const Shape shape = shape_of(cfg);
+  if (cfg->io == DENDSN_IO_BF16) e4m3 ? launch_forward<bf16_t, true>(a, shape, stream) : launch_forward<bf16_t, false>(a, shape, stream);
+  else e4m3 ? launch_forward<float, true>(a, shape, stream) : launch_forward<float, false>(a, shape, stream);
   return launched("norm forward");
 }
 
@@ -457,12 +471,12 @@ dendsn_status dendsn_norm_backward(const dendsn_norm_cfg* cfg, const void* x, co
   a.part = static_cast<float*>(workspace);
   a.ld_x = cfg->ld_x; a.ld_gy = cfg->ld_grad_y; a.ld_gsum = cfg->ld_grad_sum; a.ld_gx = cfg->ld_grad_x;
   a.N = int32_t(cfg->N); a.D = int32_t(cfg->D);
-  const int lanes = lanes_of(cfg);
+  const Shape shape = shape_of(cfg);
   const int64_t parts = parts_of(cfg);
   const bool bf16 = cfg->io == DENDSN_IO_BF16;
   if (parts) {
-    if (weight) bf16 ? launch_backward<bf16_t, true>(a, lanes, parts, stream) : launch_backward<float, true>(a, lanes, parts, stream);
-    else bf16 ? launch_backward<bf16_t, false>(a, lanes, parts, stream) : launch_backward<float, false>(a, lanes, parts, stream);
+    if (weight) bf16 ? launch_backward<bf16_t, true>(a, shape, parts, stream) : launch_backward<float, true>(a, shape, parts, stream);
+    else bf16 ? launch_backward<bf16_t, false>(a, shape, parts, stream) : launch_backward<float, false>(a, shape, parts, stream);
   }
   if (weight) {  // of no rows: +0
     const dim3 grid(unsigned(ceil_div(cfg->D, 32)));

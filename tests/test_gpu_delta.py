@@ -76,6 +76,19 @@ def test_against_recurrence(gpu_device, T, b, H, Hk, K, V, io):
         check(cfg, make(cfg, T + K, ragged, carry, layout), gpu_device)
 
 
+# few heads and so many steps that they are cut into segments; ends inside, at and between them
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("T,b,H,Hk,K,V", [(1100, 1, 1, 0, 16, 20), (1537, 3, 2, 1, 36, 33), (700, 4, 1, 0, 128, 17)])
+def test_segments(gpu_device, T, b, H, Hk, K, V, io):
+    for ragged, carry, layout in ((False, True, "time"), (True, True, "fused"), (False, False, "batch")):
+        cfg = dendsn.DeltaRuleConfig(T=T, batch=b, H=H, Hk=Hk, K=K, V=V, io=io)
+        announce(f"delta segments {cfg} ragged {ragged} carry {carry} {layout}")
+        d = make(cfg, T + K, ragged, carry, layout, decay=0.02)
+        if ragged and b > 2:
+            d["lengths"][1] = 256
+        check(cfg, d, gpu_device)
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_scale_and_decays(gpu_device, io):
     """Decays of 1, decays that forget all (minus infinity among them), betas of 0 and 1, a scale."""
