@@ -375,7 +375,7 @@ __device__ __forceinline__ void store_planes8(typename M::Word* p, int row, int 
 }
 
 template <class M, int KP, bool BACK>
-__global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(kThreads, M::planes == 1 && KP > 64 ? 2 : 3) void delta_local_kernel(DeltaArgs a) {
   using IO = typename M::IO;
   using Word = typename M::Word;
   constexpr int KS = KP / 32, kLd = kC + 4;
@@ -385,7 +385,7 @@ __global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
   if (n <= 0) return;
   __shared__ double sg[kC];
   __shared__ float sb[kC];
-  __shared__ __align__(16) float sa[kC][kLd], st[kC][kLd], sp[kC][kLd], sm[4][16][17];
+  __shared__ __align__(16) float sa[kC][kLd], st[kC][kLd], sm[4][16][17];  // A and later P, T
   const int64_t at = (int64_t(b) * a.H + h) * a.nc + c;
   const int hk = h / (a.H / a.Hk), row = 16 * w + r;
   const IO* kp = static_cast<const IO*>(a.k) + t0 * a.k_t + b * a.k_b + hk * a.k_h;
@@ -436,24 +436,24 @@ __global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
   }
   __syncthreads();
   const int i0 = 16 * w + q4 * 4;
+  f32x4 P[4];
 #pragma unroll
   for (int bj = 0; bj < 4; ++bj) {
     const int j = 16 * bj + r;
-    f32x4 A = {0, 0, 0, 0}, P = {0, 0, 0, 0};
+    f32x4 A = {0, 0, 0, 0};
+    P[bj] = f32x4{0, 0, 0, 0};
     if (bj <= w) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const int i = i0 + x;
         const float d = j <= i ? exp_of(sg[i] - sg[j]) : 0.0f;
         A[x] = j < i ? sb[i] * d * (bj < w ? kk[bj][x] : kk[3][x]) : 0.0f;
-        P[x] = j <= i ? a.scale * d * (bj < w ? qk[bj][x] : qk[3][x]) : 0.0f;
+        P[bj][x] = j <= i ? a.scale * d * (bj < w ? qk[bj][x] : qk[3][x]) : 0.0f;
       }
     }
-    if (BACK) *reinterpret_cast<f32x4*>(&sp[j][i0]) = P;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       sa[i0 + x][j] = A[x];
-      if (!BACK) sp[i0 + x][j] = P[x];
       if (bj > w) st[i0 + x][j] = 0.0f;
     }
   }
@@ -489,6 +489,15 @@ __global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
     }
     __syncthreads();
   }
+#pragma unroll
+  for (int bj = 0; bj < 4; ++bj) {
+    const int j = 16 * bj + r;
+    if (BACK) *reinterpret_cast<f32x4*>(&sa[j][i0]) = P[bj];
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if (!BACK) sa[i0 + x][j] = P[bj][x];
+  }
+  __syncthreads();
   Word* pm = static_cast<Word*>(a.pm) + at * M::planes * kC * kC;
   Word* tm = static_cast<Word*>(a.tm) + at * M::planes * kC * kC;
 #pragma unroll
@@ -498,7 +507,7 @@ __global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       x[k] = BACK ? st[j + k][i] : st[i][j + k];
-      y[k] = sp[i][j + k];
+      y[k] = sa[i][j + k];
     }
     store_planes8<M>(tm, i, j, x);
     store_planes8<M>(pm, i, j, y);
@@ -518,13 +527,14 @@ __global__ __launch_bounds__(kThreads) void delta_local_kernel(DeltaArgs a) {
 constexpr int kScanThreads = 512;
 
 // Blocks go to the eight XCDs in turn, each of which has a cache of its own: the blocks of one
-// head, which read the same q, k, T and P, are eight apart.
+// head (and segment), which read the same q, k, T and P, are eight apart.
 struct ScanBlock {
-  int v0, bh;
+  int v0, bh, seg;
 };
 __device__ __forceinline__ ScanBlock scan_block(const DeltaArgs& a, int KP, int BV) {
-  const int cols = (a.Vp + (a.pass == kMaps ? KP : 0)) / BV, m = blockIdx.x / 8, bh = m / cols * 8 + blockIdx.x % 8;
-  return {m % cols * BV, bh < a.batch * a.H ? bh : -1};
+  const int cols = (a.Vp + (a.pass == kMaps ? KP : 0)) / BV, m = blockIdx.x / 8, heads = a.batch * a.H;
+  const int group = m / cols * 8 + blockIdx.x % 8, seg = group / heads;
+  return {m % cols * BV, seg < a.segs ? group - seg * heads : -1, seg};
 }
 
 template <class M, int KP, int BV>
@@ -545,14 +555,14 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), w = wave % 4, r = lane % 16, q4 = lane / 16;
   const bool chain = wave < 4;
   const ScanBlock at_block = scan_block(a, KP, BV);
-  const int v0 = at_block.v0, bh = at_block.bh;
+  const int v0 = at_block.v0, bh = at_block.bh, part = at_block.seg;
   if (bh < 0) return;
   const int b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
   const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), chunks = (len + kC - 1) / kC;
   const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
   const bool maps = a.pass == kMaps;
-  const int c0 = blockIdx.y * a.per, c1 = min(chunks, c0 + a.per);  // the segment's chunks
-  const int64_t first = int64_t(bh) * a.nc + c0, seg = int64_t(bh) * a.segs + blockIdx.y;
+  const int c0 = part * a.per, c1 = min(chunks, c0 + a.per);  // the segment's chunks
+  const int64_t first = int64_t(bh) * a.nc + c0, seg = int64_t(bh) * a.segs + part;
   // the next chunk's, in turn
   const IO* kc = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h + c0 * kC * a.k_t;
   const IO* qc = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h + c0 * kC * a.q_t;
@@ -631,7 +641,7 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
         for (int x = 0; x < 4; ++x) {
           const int d = (MT * w + m) * 16 + q4 * 4 + x, v = v0 + nt * 16 + r;
           if (maps) S[m][nt][x] = d == v - a.Vp ? 1.0f : 0.0f;
-          else if (a.pass == kStates && blockIdx.y > 0) S[m][nt][x] = a.seg_in[(seg * KP + d) * a.Vp + v];
+          else if (a.pass == kStates && part > 0) S[m][nt][x] = a.seg_in[(seg * KP + d) * a.Vp + v];
           else S[m][nt][x] = a.s0 && state_in(m, nt, x) ? a.s0[state_at(m, nt, x)] : 0.0f;
         }
     auto put_state = [&]() {
@@ -835,7 +845,7 @@ __global__ __launch_bounds__(kScanThreads) void delta_scan_kernel(DeltaArgs a) {
       oc += kC * a.o_t;
       lds_barrier();
     });
-    if (blockIdx.y > 0) return;  // steps past the end
+    if (part > 0) return;  // steps past the end
     IO* ob = static_cast<IO*>(a.o) + b * a.o_b + h * a.o_h;
     for (int64_t u = threadIdx.x - kThreads; u < int64_t(a.T - len) * BV; u += kThreads)
       if (v0 + u % BV < a.V) ob[(len + u / BV) * a.o_t + v0 + u % BV] = IO{};
@@ -864,14 +874,14 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
   BackLds<M, KP, BV>& s = *reinterpret_cast<BackLds<M, KP, BV>*>(lds);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), w = wave % 4, r = lane % 16, q4 = lane / 16;
   const ScanBlock at_block = scan_block(a, KP, BV);
-  const int v0 = at_block.v0, bh = at_block.bh;
+  const int v0 = at_block.v0, bh = at_block.bh, part = at_block.seg;
   if (bh < 0) return;
   const int b = bh / a.H, h = bh - b * a.H, hk = h / (a.H / a.Hk);
   const int len = __builtin_amdgcn_readfirstlane(length_of(a, b)), chunks = (len + kC - 1) / kC;
   const bool maps = a.pass == kMaps;
-  const int c0 = blockIdx.y * a.per, c1 = min(chunks, c0 + a.per), end = max(c1 - 1, 0);  // the segment's chunks
+  const int c0 = part * a.per, c1 = min(chunks, c0 + a.per), end = max(c1 - 1, 0);  // the segment's chunks
   const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
-  const int64_t gv_t = int64_t(a.batch) * a.H * a.V, top = int64_t(bh) * a.nc + end, seg = int64_t(bh) * a.segs + blockIdx.y;
+  const int64_t gv_t = int64_t(a.batch) * a.H * a.V, top = int64_t(bh) * a.nc + end, seg = int64_t(bh) * a.segs + part;
   // of the chunk that is loaded next
   const IO* kc = static_cast<const IO*>(a.k) + b * a.k_b + hk * a.k_h + end * kC * a.k_t;
   const IO* qc = static_cast<const IO*>(a.q) + b * a.q_b + hk * a.q_h + end * kC * a.q_t;
@@ -1027,7 +1037,7 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
       load_go();
       lds_barrier();
     });
-    if (maps || blockIdx.y > 0) return;
+    if (maps || part > 0) return;
     IO* gvb = static_cast<IO*>(a.gv) + int64_t(bh) * a.V;
     for (int64_t u = threadIdx.x; u < int64_t(a.T - len) * BV; u += kThreads)  // steps past the end
       if (v0 + u % BV < a.V) gvb[(len + u / BV) * gv_t + v0 + u % BV] = IO{};
@@ -1043,7 +1053,7 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
         for (int x = 0; x < 4; ++x) {
           const int d = (MT * w + m) * 16 + q4 * 4 + x, v = v0 + nt * 16 + r;
           if (maps) S[m][nt][x] = d == v - a.Vp ? 1.0f : 0.0f;
-          else if (a.pass == kStates && int(blockIdx.y) + 1 < a.segs) S[m][nt][x] = a.seg_in[(seg * KP + d) * a.Vp + v];
+          else if (a.pass == kStates && part + 1 < a.segs) S[m][nt][x] = a.seg_in[(seg * KP + d) * a.Vp + v];
           else S[m][nt][x] = a.gs_last && state_in(m, nt, x) ? a.gs_last[state_at(m, nt, x)] : 0.0f;
         }
     auto put_state = [&]() {
@@ -1117,7 +1127,7 @@ __global__ __launch_bounds__(kScanThreads) void delta_back_scan_kernel(DeltaArgs
 #pragma unroll
           for (int x = 0; x < 4; ++x)
             a.maps[(seg * KP + (MT * w + m) * 16 + q4 * 4 + x) * (a.Vp + KP) + v0 + nt * 16 + r] = S[m][nt][x];
-    } else if (a.gs0 && blockIdx.y == 0) {
+    } else if (a.gs0 && part == 0) {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -1184,36 +1194,36 @@ __global__ __launch_bounds__(kThreads) void delta_join_states_kernel(DeltaArgs a
 }
 
 // ---------------------------------------------------------------------------
-// back_local: gradients of q, k, g and beta of one chunk.  Wave (w, half) has steps 16 w to + 15
-// and half of q's and k's places; sums over v go 32 columns at a time, the next ones' operands
-// on their way meanwhile.
+// back_local: gradients of q, k, g and beta of one chunk.  Wave w has steps 16 w to + 15; sums over v
+// go 32 columns at a time, through LDS, whose place E, then F, and the turned q and k take
+// afterwards: two blocks a CU, one of which computes while the other waits for memory.
 // ---------------------------------------------------------------------------
 constexpr int kVpad = 32;      // columns of v at a time; rows in memory are filled up to a multiple
-constexpr int kLocalThreads = 512;
+constexpr int kLocalThreads = 256;
 
 template <class M, int KP>
 struct LocalLds {
-  MatX<M, KP, kC> kt, qt;
   union {
     struct {
       Mat<M, KP, kVpad> s0, ds;
       Mat<M, kC, kVpad> u;
     } a;
     struct {
-      Mat<M, kC, kC> e, et, f, ft;
+      MatX<M, KP, kC> kt, qt;
+      Mat<M, kC, kC> e, et;  // later F and b F
     } b;
   };
   double g[kC];
-  float dg[2][kC], kx[2][kC], kd[2][kC], rv[kC], diag[kC], part[8];
+  float dg[kC], kx[kC], kd[kC], rv[kC], diag[kC], part[4];
 };
 
 template <class M, int KP>
-__global__ __launch_bounds__(kLocalThreads) void delta_back_local_kernel(DeltaArgs a) {
+__global__ __launch_bounds__(kLocalThreads, M::planes == 1 ? 1 : 2) void delta_back_local_kernel(DeltaArgs a) {
   using IO = typename M::IO;
-  constexpr int NT = KP / 32, kQuads = KP * kVpad / 4 / kLocalThreads;  // tiles of a wave; f32x4 of a state a thread
+  constexpr int NT = KP / 16, kQuads = KP * kVpad / 4 / kLocalThreads;  // f32x4 of a state a thread
   extern __shared__ __align__(16) char lds[];
   LocalLds<M, KP>& s = *reinterpret_cast<LocalLds<M, KP>*>(lds);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, w = wave % 4, half = wave / 4, r = lane % 16, q4 = lane / 16;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, q4 = lane / 16;
   const int c = blockIdx.x, h = blockIdx.y, b = blockIdx.z, share = a.H / a.Hk, hk = h / share;
   const int len = length_of(a, b), t0 = c * kC, n = min(len - t0, kC), there = min(a.T - t0, kC);
   const int64_t bh = int64_t(b) * a.H + h, at = bh * a.nc + c;
@@ -1248,84 +1258,100 @@ __global__ __launch_bounds__(kLocalThreads) void delta_back_local_kernel(DeltaAr
   const int row = 16 * w + r, i0 = 16 * w + q4 * 4;
   const float whole = dec[kC - 1];
 
-  // what 32 columns of v need, in registers
-  f32x4 ps[kQuads], pd[kQuads], pu;
-  typename Eight<IO>::Vec po, pv;
-  f32x8 pr;
-  auto load = [&](int v0) {
-#pragma unroll
-    for (int u = 0; u < kQuads; ++u) {
-      const int e = u * kLocalThreads + threadIdx.x, d = e / 8, v = v0 + e % 8 * 4;
-      ps[u] = *reinterpret_cast<const f32x4*>(ck_s + int64_t(d) * a.Vp + v);
-      pd[u] = *reinterpret_cast<const f32x4*>(ds + int64_t(d) * a.Vp + v);
-    }
-    pu = *reinterpret_cast<const f32x4*>(ck_u + int64_t(threadIdx.x / 8) * a.Vp + v0 + threadIdx.x % 8 * 4);
-    // (values past V meet zeros, of U, S and dR; rows past the end are the last one's, but for do)
-    po = load8(gob, uint32_t(min(row, n - 1)) * uint32_t(a.go_t), v0 + q4 * 8, a.V, a.V % 8);
-    if (half == 0) pv = load8(vb, uint32_t(min(row, n - 1)) * uint32_t(a.v_t), v0 + q4 * 8, a.V, a.V % 8);
-    pr = *reinterpret_cast<const f32x8*>(dr + int64_t(row) * a.Vp + v0 + q4 * 8);
-  };
   {
-    Turn<M, KP> turn;
-    turn.place(half == 0 ? a.k_t : a.q_t, n);
-    turn.load(half == 0 ? kb : qb, a.K, a.K % 8);
-    load(0);
     const double G = chunk_sum<IO>(a, b, h, t0, n);
-    if (wave == 0) s.g[lane] = G;
-    turn.put(half == 0 ? s.kt : s.qt, a.K);
+    if (w == 0) s.g[lane] = G;
   }
-
-  f32x4 dq[NT], X[NT], Y[NT], e[2], f[2];
+  f32x4 dq[NT], X[NT], Y[NT], e[4], f[4];
 #pragma unroll
   for (int t = 0; t < NT; ++t) dq[t] = X[t] = Y[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-  for (int t = 0; t < 2; ++t) e[t] = f[t] = f32x4{0, 0, 0, 0};
+  for (int t = 0; t < 4; ++t) e[t] = f[t] = f32x4{0, 0, 0, 0};
   float rv = 0.0f, sds = 0.0f;  // dR.v of row `row` (a quarter of it), <S, dS'>
   for (int v0 = 0; v0 < a.Vp; v0 += kVpad) {
+    f32x4 ps[kQuads], pd[kQuads], pu[2];
+#pragma unroll
+    for (int u = 0; u < kQuads; ++u) {
+      const uint32_t i = u * kLocalThreads + threadIdx.x, from = i / 8 * uint32_t(a.Vp) + v0 + i % 8 * 4;
+      ps[u] = *reinterpret_cast<const f32x4*>(&behind(ck_s, from));
+      pd[u] = *reinterpret_cast<const f32x4*>(&behind(ds, from));
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint32_t i = u * kLocalThreads + threadIdx.x;
+      pu[u] = *reinterpret_cast<const f32x4*>(&behind(ck_u, i / 8 * uint32_t(a.Vp) + v0 + i % 8 * 4));
+    }
+    // (values past V meet zeros, of U, S and dR; rows past the end are the last one's, but for do)
+    typename Eight<IO>::Vec po = load8(gob, uint32_t(min(row, n - 1)) * uint32_t(a.go_t), v0 + q4 * 8, a.V, a.V % 8);
+    const typename Eight<IO>::Vec pv = load8(vb, uint32_t(min(row, n - 1)) * uint32_t(a.v_t), v0 + q4 * 8, a.V, a.V % 8);
+    const f32x8 pr = *reinterpret_cast<const f32x8*>(&behind(dr, uint32_t(row) * uint32_t(a.Vp) + v0 + q4 * 8));
     if (v0 > 0) lds_barrier();
 #pragma unroll
     for (int u = 0; u < kQuads; ++u) {
-      const int e1 = u * kLocalThreads + threadIdx.x, d = e1 / 8, v = e1 % 8 * 4;
+      const int i = u * kLocalThreads + threadIdx.x;
       sds += (ps[u][0] * pd[u][0] + ps[u][1] * pd[u][1]) + (ps[u][2] * pd[u][2] + ps[u][3] * pd[u][3]);
-      s.a.s0.put4(d, v, ps[u]);
-      s.a.ds.put4(d, v, pd[u]);
+      s.a.s0.put4(i / 8, i % 8 * 4, ps[u]);
+      s.a.ds.put4(i / 8, i % 8 * 4, pd[u]);
     }
-    s.a.u.put4(threadIdx.x / 8, threadIdx.x % 8 * 4, pu);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int i = u * kLocalThreads + threadIdx.x;
+      s.a.u.put4(i / 8, i % 8 * 4, pu[u]);
+    }
     if (row >= n) po = 0;
     const Exact<M> of = exact_of<M>(po);
-    if (half == 0) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) rv = fmaf(pr[j], Eight<IO>::wide(pv[j]), rv);
-    }
+    for (int j = 0; j < 8; ++j) rv = fmaf(pr[j], Eight<IO>::wide(pv[j]), rv);
     Both<M> rf;
     both_of(pr, rf);
-    if (v0 + kVpad < a.Vp) load(v0 + kVpad);
     lds_barrier();
     const Both<M> uf = s.a.u.frag(16 * w, 0);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const Both<M> sf = s.a.s0.frag((half * NT + t) * 16, 0);
+      const Both<M> sf = s.a.s0.frag(t * 16, 0);
       mma(dq[t], of, sf);
       mma(X[t], rf, sf);
-      mma(Y[t], uf, s.a.ds.frag((half * NT + t) * 16, 0));
+      mma(Y[t], uf, s.a.ds.frag(t * 16, 0));
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (2 * half + t <= w) {
-        const Both<M> u2 = s.a.u.frag((2 * half + t) * 16, 0);
+    for (int t = 0; t < 4; ++t) {
+      if (t <= w) {
+        const Both<M> u2 = s.a.u.frag(t * 16, 0);
         mma(e[t], of, u2);
         mma(f[t], rf, u2);
       }
     }
   }
+  Turn<M, KP> kturn, qturn;
+  kturn.place(a.k_t, n);
+  kturn.load(kb, a.K, a.K % 8);
+  qturn.place(a.q_t, n);
+  qturn.load(qb, a.K, a.K % 8);
   rv += __shfl_xor(rv, 16);
   rv += __shfl_xor(rv, 32);
-  if (half == 0 && q4 == 0) s.rv[row] = rv;
+  if (q4 == 0) s.rv[row] = rv;
 #pragma unroll
   for (int x = 32; x > 0; x /= 2) sds += __shfl_xor(sds, x);
-  if (lane == 0) s.part[wave] = whole * sds;
+  if (lane == 0) s.part[w] = whole * sds;
   const f32x4 eg = *reinterpret_cast<const f32x4*>(dec + i0), tail = *reinterpret_cast<const f32x4*>(dec + kC + i0),
               beta = *reinterpret_cast<const f32x4*>(dec + 2 * kC + i0);
+  lds_barrier();
+  kturn.put(s.b.kt, a.K);
+  qturn.put(s.b.qt, a.K);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int j = 16 * t + r;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int i = i0 + x;
+      const float d = j < i ? exp_of(s.g[i] - s.g[j]) : 0.0f;
+      if (i == j) s.diag[i] = a.scale * e[t][x];
+      e[t][x] = j < i ? a.scale * d * e[t][x] : 0.0f;
+      f[t][x] = j < i ? -d * f[t][x] : 0.0f;
+      s.b.e.put(i, j, e[t][x]);
+    }
+    s.b.et.put4(j, i0, e[t]);
+  }
   lds_barrier();
   f32x4 kd = {0, 0, 0, 0}, Y2[NT];  // k.Y of dS' alone; the rest of Y
 #pragma unroll
@@ -1334,38 +1360,34 @@ __global__ __launch_bounds__(kLocalThreads) void delta_back_local_kernel(DeltaAr
     X[t] *= -eg;
     Y[t] *= tail;
     Y2[t] = f32x4{0, 0, 0, 0};
-    kd += s.kt.get4((half * NT + t) * 16 + r, i0) * Y[t];
+    kd += s.b.kt.get4(t * 16 + r, i0) * Y[t];
   }
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const int j = 16 * (2 * half + t) + r;
-    f32x4 fb;
+  for (int k = 0; k < 2; ++k) {
+    const Both<M> ef = s.b.e.frag(16 * w, k * 32), etf = s.b.et.frag(16 * w, k * 32);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const int i = i0 + x;
-      const float d = j < i ? exp_of(s.g[i] - s.g[j]) : 0.0f;
-      if (i == j) s.diag[i] = a.scale * e[t][x];
-      e[t][x] = j < i ? a.scale * d * e[t][x] : 0.0f;
-      f[t][x] = j < i ? -d * f[t][x] : 0.0f;
-      fb[x] = beta[x] * f[t][x];
-      s.b.e.put(i, j, e[t][x]);
-      s.b.f.put(i, j, f[t][x]);
+    for (int t = 0; t < NT; ++t) {
+      mma(dq[t], ef, s.b.kt.frag(t * 16, k * 32));
+      mma(Y2[t], etf, s.b.qt.frag(t * 16, k * 32));
     }
-    s.b.et.put4(j, i0, e[t]);
-    s.b.ft.put4(j, i0, fb);
+  }
+  lds_barrier();
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int j = 16 * t + r;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) s.b.e.put(i0 + x, j, f[t][x]);
+    s.b.et.put4(j, i0, beta * f[t]);
   }
   lds_barrier();
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const Both<M> ef = s.b.e.frag(16 * w, k * 32), etf = s.b.et.frag(16 * w, k * 32), ff = s.b.f.frag(16 * w, k * 32),
-                  ftf = s.b.ft.frag(16 * w, k * 32);
+    const Both<M> ff = s.b.e.frag(16 * w, k * 32), ftf = s.b.et.frag(16 * w, k * 32);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const Exact<M> kf = s.kt.frag((half * NT + t) * 16, k * 32);
-      mma(dq[t], ef, kf);
+      const Exact<M> kf = s.b.kt.frag(t * 16, k * 32);
       mma(X[t], ff, kf);
       mma(Y2[t], ftf, kf);
-      mma(Y2[t], etf, s.qt.frag((half * NT + t) * 16, k * 32));
     }
   }
   const f32x4 diag = *reinterpret_cast<const f32x4*>(s.diag + i0);
@@ -1373,16 +1395,16 @@ __global__ __launch_bounds__(kLocalThreads) void delta_back_local_kernel(DeltaAr
   const bool full = n == kC && a.K == KP && share == 1;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int d = (half * NT + t) * 16 + r;
-    const f32x4 k = s.kt.get4(d, i0), q = s.qt.get4(d, i0);
+    const int d = t * 16 + r;
+    const f32x4 k = s.b.kt.get4(d, i0), q = s.b.qt.get4(d, i0);
     dg += q * dq[t] - k * Y2[t];
     kx += k * X[t];
     const f32x4 gqv = dq[t] + diag * k, gkv = (beta * X[t] + Y[t]) + (Y2[t] + diag * q);
     if (full) {
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        gq[(i0 + x) * tk + d] = narrow<IO>(gqv[x]);
-        gk[(i0 + x) * tk + d] = narrow<IO>(gkv[x]);
+        behind(gq, uint32_t(i0 + x) * uint32_t(tk) + d) = narrow<IO>(gqv[x]);
+        behind(gk, uint32_t(i0 + x) * uint32_t(tk) + d) = narrow<IO>(gkv[x]);
       }
     } else {
 #pragma unroll
@@ -1400,14 +1422,14 @@ __global__ __launch_bounds__(kLocalThreads) void delta_back_local_kernel(DeltaAr
       kd[x] += __shfl_xor(kd[x], m);
     }
   if (r == 0) {
-    *reinterpret_cast<f32x4*>(&s.dg[half][i0]) = dg;
-    *reinterpret_cast<f32x4*>(&s.kx[half][i0]) = kx;
-    *reinterpret_cast<f32x4*>(&s.kd[half][i0]) = kd;
+    *reinterpret_cast<f32x4*>(&s.dg[i0]) = dg;
+    *reinterpret_cast<f32x4*>(&s.kx[i0]) = kx;
+    *reinterpret_cast<f32x4*>(&s.kd[i0]) = kd;
   }
   lds_barrier();
-  if (wave == 0) {
+  if (w == 0) {
     // sums from the last step down and from the first up, in 64 bits: terms cancel
-    double after = double(s.dg[0][lane]) + double(s.dg[1][lane]), upto = double(s.kd[0][lane]) + double(s.kd[1][lane]), held = 0.0;
+    double after = s.dg[lane], upto = s.kd[lane];
     const double own = upto;
 #pragma unroll
     for (int x = 1; x < 64; x *= 2) {
@@ -1415,11 +1437,10 @@ __global__ __launch_bounds__(kLocalThreads) void delta_back_local_kernel(DeltaAr
       if (lane + x < 64) after += down;
       if (lane >= x) upto += up;
     }
-#pragma unroll
-    for (int x = 0; x < 8; ++x) held += double(s.part[x]);
+    const double held = (double(s.part[0]) + double(s.part[1])) + (double(s.part[2]) + double(s.part[3]));
     if (lane < n) {
       gg[lane * th] = narrow<IO>(float(after + (upto - own) + held));
-      gbeta[lane * th] = narrow<IO>(s.rv[lane] + (s.kx[0][lane] + s.kx[1][lane]));
+      gbeta[lane * th] = narrow<IO>(s.rv[lane] + s.kx[lane]);
     }
   }
 }
@@ -1689,7 +1710,7 @@ bool allow_lds(F* kernel, size_t bytes) {
 template <int KP, typename K>
 void scan_passes(K kernel, size_t bytes, int BV, DeltaArgs a, const float* from, bool back, hipStream_t stream) {
   const int64_t heads = int64_t(a.batch) * a.H;
-  auto grid = [&](int64_t cols) { return dim3(unsigned(cols / BV * round_up(heads, 8)), unsigned(a.segs)); };
+  auto grid = [&](int64_t cols) { return dim3(unsigned(cols / BV * round_up(heads * a.segs, 8))); };
   a.pass = kWhole;
   if (a.segs > 1) {
     a.pass = kMaps;
