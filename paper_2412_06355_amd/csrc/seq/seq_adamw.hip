@@ -86,10 +86,11 @@ __device__ __forceinline__ float over_wave(float v) {
   return v;
 }
 
-template <typename T, int V>
+// V values of which `left` are there; FULL: all.
+template <bool FULL, typename T, int V>
 __device__ __forceinline__ Pack<T, V> load_some(const T* p, int left) {
   Pack<T, V> r{};
-  if (left >= V) {
+  if (FULL || left >= V) {
     r = *reinterpret_cast<const Pack<T, V>*>(p);
   } else {
 #pragma unroll
@@ -98,9 +99,9 @@ __device__ __forceinline__ Pack<T, V> load_some(const T* p, int left) {
   }
   return r;
 }
-template <typename T, int V>
+template <bool FULL, typename T, int V>
 __device__ __forceinline__ void store_some(T* p, int left, const Pack<T, V>& r) {
-  if (left >= V) {
+  if (FULL || left >= V) {
     *reinterpret_cast<Pack<T, V>*>(p) = r;
   } else {
 #pragma unroll
@@ -141,38 +142,55 @@ __global__ __launch_bounds__(kWaves * 64) void adamw_kernel(const Batch a) {
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
   const uint32_t key = mix(a.seed_lo ^ mix(a.seed_hi ^ mix(step ^ mix(uint32_t(a.base + at) + 1u))));
   const int64_t from = int64_t(blockIdx.x - t.first) * (kGroup * kGroups);
-  for (int r = threadIdx.x / 64; r < kGroups; r += kWaves) {
+  // a lane's four values of a round
+  struct Values {
+    Pack<float, 4> p, m, v, g;
+    Pack<bf16_t, 4> gh;
+    Pack<uint8_t, 4> cm, cv;
+    float ms, vs;
+  };
+  auto left_of = [&](int64_t i) { return int(n - i < 4 ? n - i < 0 ? 0 : n - i : 4); };
+  auto load = [&](auto full, int r) {
+    constexpr bool F = decltype(full)::value;
+    Values x;
     const int64_t g0 = from + r * kGroup, i = g0 + lane * 4;
-    if (g0 >= n) break;
-    const int left = int(n - i < 4 ? n - i < 0 ? 0 : n - i : 4);
-    const Pack<float, 4> p = load_some<float, 4>(t.p + i, left);
-    float g[4], m[4], v[4];
-    if (t.bf16) {
-      const Pack<bf16_t, 4> x = load_some<bf16_t, 4>(static_cast<const bf16_t*>(t.g) + i, left);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) g[j] = widen(x.v[j]) * gs;
-    } else {
-      const Pack<float, 4> x = load_some<float, 4>(static_cast<const float*>(t.g) + i, left);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) g[j] = x.v[j] * gs;
-    }
+    const int left = F ? 4 : left_of(i);
+    x.p = load_some<F, float, 4>(t.p + i, left);
+    if (t.bf16) x.gh = load_some<F, bf16_t, 4>(static_cast<const bf16_t*>(t.g) + i, left);
+    else x.g = load_some<F, float, 4>(static_cast<const float*>(t.g) + i, left);
     if (E4M3) {
-      codes_of(load_some<uint8_t, 4>(static_cast<const uint8_t*>(t.m) + i, left), m);
-      codes_of(load_some<uint8_t, 4>(static_cast<const uint8_t*>(t.v) + i, left), v);
-      const float ms = t.ms[g0 / kGroup], vs = t.vs[g0 / kGroup];
+      x.cm = load_some<F, uint8_t, 4>(static_cast<const uint8_t*>(t.m) + i, left);
+      x.cv = load_some<F, uint8_t, 4>(static_cast<const uint8_t*>(t.v) + i, left);
+      x.ms = t.ms[g0 / kGroup];
+      x.vs = t.vs[g0 / kGroup];
+    } else {
+      x.m = load_some<F, float, 4>(static_cast<const float*>(t.m) + i, left);
+      x.v = load_some<F, float, 4>(static_cast<const float*>(t.v) + i, left);
+    }
+    return x;
+  };
+  auto compute = [&](auto full, int r, const Values& x) {
+    constexpr bool F = decltype(full)::value;
+    const int64_t g0 = from + r * kGroup, i = g0 + lane * 4;
+    const int left = F ? 4 : left_of(i);
+    const Pack<float, 4> p = x.p;
+    float g[4], m[4], v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g[j] = (t.bf16 ? widen(x.gh.v[j]) : x.g.v[j]) * gs;
+    if (E4M3) {
+      codes_of(x.cm, m);
+      codes_of(x.cv, v);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        m[j] *= ms;
-        v[j] *= vs;
+        m[j] *= x.ms;
+        v[j] *= x.vs;
         v[j] *= v[j];
       }
     } else {
-      const Pack<float, 4> x = load_some<float, 4>(static_cast<const float*>(t.m) + i, left);
-      const Pack<float, 4> y = load_some<float, 4>(static_cast<const float*>(t.v) + i, left);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        m[j] = x.v[j];
-        v[j] = y.v[j];
+        m[j] = x.m.v[j];
+        v[j] = x.v.v[j];
       }
     }
     Pack<float, 4> np;
@@ -185,8 +203,8 @@ __global__ __launch_bounds__(kWaves * 64) void adamw_kernel(const Batch a) {
       np.v[j] = p.v[j] - a.lr * fmaf(a.wd, p.v[j], to);
       copy.v[j] = narrow<bf16_t>(np.v[j]);
     }
-    store_some<float, 4>(t.p + i, left, np);
-    if (t.copy) store_some<bf16_t, 4>(t.copy + i, left, copy);
+    store_some<F, float, 4>(t.p + i, left, np);
+    if (t.copy) store_some<F, bf16_t, 4>(t.copy + i, left, copy);
     if (E4M3) {
       float tm = 0.0f, tv = 0.0f;
 #pragma unroll
@@ -200,25 +218,32 @@ __global__ __launch_bounds__(kWaves * 64) void adamw_kernel(const Batch a) {
       for (int j = 0; j < 4; ++j) {
         const uint32_t bits = mix(uint32_t(i + j) ^ (key + uint32_t(uint64_t(i + j) >> 32)));
         // (comparisons, so that NaN stays)
-        float x = in_units(fabsf(m[j]), sm), y = in_units(v[j], sv);
-        x = x > kTop ? kTop : x;
-        y = y > kTop ? kTop : y;
+        float um = in_units(fabsf(m[j]), sm), uv = in_units(v[j], sv);
+        um = um > kTop ? kTop : um;
+        uv = uv > kTop ? kTop : uv;
         const float u1 = float(bits & 0xffffu) * 0x1p-16f, u2 = float(bits >> 16) * 0x1p-16f;
-        const float cm = round_at(x, u1), cv = round_at(y, u2);
+        const float cm = round_at(um, u1), cv = round_at(uv, u2);
         m[j] = copysignf(cm, m[j]);
-        v[j] = y > 0.0f && cv < 0x1p-9f ? 0x1p-9f : cv;
+        v[j] = uv > 0.0f && cv < 0x1p-9f ? 0x1p-9f : cv;
       }
-      store_some<uint8_t, 4>(static_cast<uint8_t*>(t.m) + i, left, codes(m));
-      store_some<uint8_t, 4>(static_cast<uint8_t*>(t.v) + i, left, codes(v));
+      store_some<F, uint8_t, 4>(static_cast<uint8_t*>(t.m) + i, left, codes(m));
+      store_some<F, uint8_t, 4>(static_cast<uint8_t*>(t.v) + i, left, codes(v));
       if (lane == 0) {
         t.ms[g0 / kGroup] = sm.scale;
         t.vs[g0 / kGroup] = sv.scale;
       }
     } else {
-      store_some<float, 4>(static_cast<float*>(t.m) + i, left, Pack<float, 4>{{m[0], m[1], m[2], m[3]}});
-      store_some<float, 4>(static_cast<float*>(t.v) + i, left, Pack<float, 4>{{v[0], v[1], v[2], v[3]}});
+      store_some<F, float, 4>(static_cast<float*>(t.m) + i, left, Pack<float, 4>{{m[0], m[1], m[2], m[3]}});
+      store_some<F, float, 4>(static_cast<float*>(t.v) + i, left, Pack<float, 4>{{v[0], v[1], v[2], v[3]}});
     }
+  };
+  int r = threadIdx.x / 64;
+  for (; r + kWaves < kGroups && from + (r + kWaves + 1) * kGroup <= n; r += 2 * kWaves) {  // two rounds' loads at once
+    const Values x = load(std::true_type{}, r), y = load(std::true_type{}, r + kWaves);
+    compute(std::true_type{}, r, x);
+    compute(std::true_type{}, r + kWaves, y);
   }
+  for (; r < kGroups && from + r * kGroup < n; r += kWaves) compute(std::false_type{}, r, load(std::false_type{}, r));
 }
 
 dendsn_status check_tensor(const dendsn_adamw_cfg* c, const dendsn_adamw_tensor& t, int64_t i) {
