@@ -42,8 +42,9 @@ typedef struct dendsn_delta_cfg {
     int64_t V;          /* values of v and o, 1 <= V <= 65536                  */
     /* Strides of step, sequence and head: element (t, b, h, d) of q lies at
      * t * q_t + b * q_b + h * q_h + d, and so on (g and beta: without d).  Those of
-     * inputs may be 0 (broadcast); rows of outputs may not overlap; 64 steps of a tensor,
-     * gradients among them, span less than 2^31 bytes (or T is 1). */
+     * inputs may be 0 (broadcast); rows of outputs may not overlap.  Over whole sequences
+     * 64 steps of a tensor, gradients among them, span less than 2^31 bytes (or T is 1), and
+     * batch * H * V is at most 2^26 (V in 32s). */
     int64_t q_t, q_b, q_h, k_t, k_b, k_h, v_t, v_b, v_h, g_t, g_b, g_h, beta_t, beta_b, beta_h, o_t, o_b, o_h;
     int64_t grad_o_t, grad_o_b, grad_o_h;                    /* backward             */
     int32_t io;         /* dendsn_io of q, k, v, g, beta, o and their gradients */
@@ -70,8 +71,10 @@ dendsn_status dendsn_delta_workspace_bytes(const dendsn_delta_cfg* cfg, int32_t 
  *   o        [T,batch,H,V] io    required output
  *   s_last   [batch,H,K,V] fp32  optional output: the state after the sequence's last step
  *   ckpt     dendsn_delta_ckpt_bytes bytes, optional output (needed by the backward)
- * In bf16 what is neither an input nor an output enters the products as the sum of two
- * bf16 values, to 2^-17 of itself.
+ * Steps go in chunks of 64: an input that is not finite may leave its whole chunk's outputs,
+ * the steps before it among them, and all later ones not finite.  In bf16 what is neither an
+ * input nor an output enters the products as the sum of three bf16 values where s_last and
+ * grad_s0 hang on it (fp32's own rounding), of two (to 2^-17) where only outputs in bf16 do.
  */
 dendsn_status dendsn_delta_forward(const dendsn_delta_cfg* cfg, const void* q, const void* k, const void* v,
                                    const void* g, const void* beta, const float* s0, const int32_t* lengths, void* o,

@@ -406,6 +406,8 @@ def adamw(cfg: AdamWConfig, params, grads, states, step, *, copies=None, grad_sc
     eight = STATE[cfg.state] == 1
     state_type, parts = (f8, 4) if eight else (f32, 2)
 
+    if len({p.data_ptr() for p in params if p.numel()}) != sum(1 for p in params if p.numel()):
+        raise ValueError("params: a tensor appears twice")
     pack = struct.Struct("@q7Pi4x").pack_into
     array = bytearray(ctypes.sizeof(dendsn_adamw_tensor) * count)
     gpu, here, ms, vs, c, at = dev.type == "cuda", params[0].get_device(), 0, 0, 0, 0

@@ -1585,7 +1585,8 @@ dendsn_status check_cfg(const dendsn_delta_cfg* c) {
   if (c->T < 0 || c->T > (int64_t(1) << 24)) return fail(DENDSN_E_INVALID, "T must be in [0, 2^24]");
   if (c->batch < 0 || c->batch > 65535) return fail(DENDSN_E_INVALID, "batch must be in [0, 65535]");
   if (c->H < 0 || c->H > 65535) return fail(DENDSN_E_INVALID, "H must be in [0, 65535]");
-  if (c->Hk < 1 || c->H % c->Hk) return fail(DENDSN_E_INVALID, "H must be a multiple of Hk >= 1");
+  if (c->Hk < 0 || (c->H > 0 && (c->Hk < 1 || c->H % c->Hk)))
+    return fail(DENDSN_E_INVALID, "H must be a multiple of Hk >= 1");
   if (c->K < 1 || c->V < 1 || c->V > 65536) return fail(DENDSN_E_INVALID, "K or V out of range");
   if (c->K > 128) return fail(DENDSN_E_UNSUPPORTED, "K must be <= 128");
   if (c->io != DENDSN_IO_F32 && c->io != DENDSN_IO_BF16) return fail(DENDSN_E_INVALID, "bad io");
@@ -1594,16 +1595,24 @@ dendsn_status check_cfg(const dendsn_delta_cfg* c) {
   if (!small_product(c->batch * c->H * 128, round_up(c->T + kC, kC)) ||
       !small_product(c->batch * c->H * 128 * round_up(c->T + kC, kC) / kC * 4, round_up(c->V, kVpad)))
     return fail(DENDSN_E_INVALID, "T * batch * H * V too large");
-  // a launch has fewer than 2^32 threads: blocks of 512, 16 columns of v or more
-  if (round_up(c->batch * c->H, 8) > (int64_t(1) << 22) / (round_up(c->V, kVpad) / 16))
-    return fail(DENDSN_E_UNSUPPORTED, "batch * H * V too large");
   const int64_t s[21] = {c->q_t, c->q_b, c->q_h, c->k_t, c->k_b, c->k_h, c->v_t, c->v_b, c->v_h, c->g_t, c->g_b, c->g_h,
                          c->beta_t, c->beta_b, c->beta_h, c->o_t, c->o_b, c->o_h, c->grad_o_t, c->grad_o_b, c->grad_o_h};
   for (int i = 0; i < 21; i += 3)
     if (!strides_fit(c, s[i], s[i + 1], s[i + 2])) return fail(DENDSN_E_INVALID, "a stride is negative or too large");
+  return DENDSN_OK;
+}
+
+// What holds for whole sequences besides.
+dendsn_status check_sequences(const dendsn_delta_cfg* c) {
+  const dendsn_status st = check_cfg(c);
+  if (st != DENDSN_OK) return st;
+  // a launch has fewer than 2^32 threads: blocks of 512, 16 columns of v or more
+  if (round_up(c->batch * c->H, 8) > (int64_t(1) << 22) / (round_up(c->V, kVpad) / 16))
+    return fail(DENDSN_E_UNSUPPORTED, "batch * H * V too large");
   // 64 steps of a tensor lie within 2^31 bytes (gradients are contiguous)
+  const int64_t s[7] = {c->q_t, c->k_t, c->v_t, c->g_t, c->beta_t, c->o_t, c->grad_o_t};
   int64_t most = c->batch * c->H * (c->V > c->K ? c->V : c->K);
-  for (int i = 0; i < 21; i += 3) most = s[i] > most ? s[i] : most;
+  for (int64_t t : s) most = t > most ? t : most;
   if (c->T > 1 && most >= (int64_t(1) << 31) / kC / (c->io == DENDSN_IO_BF16 ? 2 : 4))
     return fail(DENDSN_E_UNSUPPORTED, "64 steps of a tensor span 2^31 bytes or more");
   return DENDSN_OK;
@@ -1797,7 +1806,7 @@ extern "C" {
 
 dendsn_status dendsn_delta_ckpt_bytes(const dendsn_delta_cfg* cfg, size_t* bytes) {
   clear_error();
-  const dendsn_status st = check_cfg(cfg);
+  const dendsn_status st = check_sequences(cfg);
   if (st != DENDSN_OK) return st;
   if (!bytes) return fail(DENDSN_E_INVALID, "bytes is NULL");
   *bytes = make_plan(cfg).ckpt;
@@ -1806,7 +1815,7 @@ dendsn_status dendsn_delta_ckpt_bytes(const dendsn_delta_cfg* cfg, size_t* bytes
 
 dendsn_status dendsn_delta_workspace_bytes(const dendsn_delta_cfg* cfg, int32_t backward, size_t* bytes) {
   clear_error();
-  const dendsn_status st = check_cfg(cfg);
+  const dendsn_status st = check_sequences(cfg);
   if (st != DENDSN_OK) return st;
   if (!bytes) return fail(DENDSN_E_INVALID, "bytes is NULL");
   const DeltaPlan p = make_plan(cfg);
@@ -1819,7 +1828,7 @@ dendsn_status dendsn_delta_forward(const dendsn_delta_cfg* cfg, const void* q, c
                                    float* s_last, void* ckpt, void* workspace, size_t workspace_bytes,
                                    hipStream_t stream) {
   clear_error();
-  dendsn_status st = check_cfg(cfg);
+  dendsn_status st = check_sequences(cfg);
   if (st != DENDSN_OK) return st;
   const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
   const bool none = empty(cfg);
@@ -1849,7 +1858,7 @@ dendsn_status dendsn_delta_backward(const dendsn_delta_cfg* cfg, const void* q, 
                                     void* grad_v, void* grad_g, void* grad_beta, float* grad_s0, void* workspace,
                                     size_t workspace_bytes, hipStream_t stream) {
   clear_error();
-  dendsn_status st = check_cfg(cfg);
+  dendsn_status st = check_sequences(cfg);
   if (st != DENDSN_OK) return st;
   const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
   const bool none = empty(cfg);

@@ -88,7 +88,8 @@ def test_delta_unsupported(lib):
     c = delta_cfg(K=129)
     assert delta_fwd(lib, c) == UNSUPPORTED and delta_bwd(lib, c) == UNSUPPORTED
     assert delta_step(lib, delta_cfg(K=129, T=1)) == UNSUPPORTED
-    # steps that lie too far apart, more blocks than a launch has
+    # steps that lie too far apart, more blocks than a launch has (a step has its own)
+    assert delta_step(lib, delta_cfg(batch=65535, H=256, Hk=2, K=1, V=1, T=1), slots=None) == INVALID
     for kw in (dict(k_t=1 << 24), dict(io=1, grad_o_t=1 << 25), dict(batch=65535, H=64, Hk=2, V=128, T=2),
                dict(batch=65535, H=256, Hk=2, K=1, V=1, T=1)):
         assert delta_fwd(lib, delta_cfg(**kw)) == UNSUPPORTED, kw
@@ -138,6 +139,7 @@ def test_delta_empty_needs_nothing(lib):
         assert lib.dendsn_delta_ckpt_bytes(ref(c), ctypes.byref(out)) == OK and out.value == 0
         none = {k: None for k in ("q", "k", "v", "g", "beta")}
         assert delta_fwd(lib, c, nbytes=0, ws=None, o=None, **none) == OK
+        assert delta_fwd(lib, delta_cfg(H=0, Hk=0), nbytes=0, ws=None, o=None, **none) == OK
         assert delta_bwd(lib, c, nbytes=0, ws=None, ckpt=None, grad_o=None, gq=None, gk=None, gv=None, gg=None, gbeta=None, **none) == OK
 
 
@@ -264,4 +266,6 @@ def test_binding_refuses():
                  (one, [z(4, dt=torch.float16)], state), (one, [z(8)[::2]], state), (one, one, state)):
         with pytest.raises(ValueError):
             dendsn.adamw(a, *args, 1)
+    with pytest.raises(ValueError, match="twice"):
+        dendsn.adamw(a, one * 2, [z(4), z(4)], state * 2, 1)
     dendsn.adamw(a, [], [], [], 1)

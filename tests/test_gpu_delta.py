@@ -89,6 +89,15 @@ def test_segments(gpu_device, T, b, H, Hk, K, V, io):
         check(cfg, d, gpu_device)
 
 
+# so many heads that a block takes 32 columns of v; of both widths, of K that is a multiple of 8 and not
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("K", [16, 21, 72, 69])
+def test_many_heads(gpu_device, K, io):
+    cfg = dendsn.DeltaRuleConfig(T=70, batch=8, H=32, Hk=16, K=K, V=32 if K != 21 else 31, io=io)
+    announce(f"delta many heads {cfg}")
+    check(cfg, make(cfg, K, True, True, "fused"), gpu_device)
+
+
 @pytest.mark.parametrize("io", ["f32", "bf16"])
 def test_scale_and_decays(gpu_device, io):
     """Decays of 1, decays that forget all (minus infinity among them), betas of 0 and 1, a scale."""
