@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kWaves * 64) void adamw_kernel(const Batch a) {
     fix1 = float(-expm1(double(step) * a.log_b1));
     fix2 = float(-expm1(double(step) * a.log_b2));
   }
-  const float inv1 = 1.0f / fix1, inv2 = 1.0f / fix2;
+  const float inv1 = 1.0f / fix1, inv_root = sqrtf(1.0f / fix2);
   const float gs = a.grad_scale ? *a.grad_scale : 1.0f;
   const uint32_t key = mix(a.seed_lo ^ mix(a.seed_hi ^ mix(step ^ mix(uint32_t(a.base + at) + 1u))));
   const int64_t from = int64_t(blockIdx.x - t.first) * (kGroup * kGroups);
@@ -194,12 +194,15 @@ __global__ __launch_bounds__(kWaves * 64) void adamw_kernel(const Batch a) {
       }
     }
     Pack<float, 4> np;
+    float root[4];
     Pack<bf16_t, 4> copy;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       m[j] = a.b1 * m[j] + a.c1 * g[j];
       v[j] = a.b2 * v[j] + a.c2 * g[j] * g[j];
-      const float to = (m[j] * inv1) / (sqrtf(v[j] * inv2) + a.eps);
+      // (the update needs no last bit: the root of v is taken once, the quotient is a reciprocal's)
+      root[j] = sqrtf(v[j]);
+      const float to = (m[j] * inv1) * __builtin_amdgcn_rcpf(fmaf(root[j], inv_root, a.eps));
       np.v[j] = p.v[j] - a.lr * fmaf(a.wd, p.v[j], to);
       copy.v[j] = narrow<bf16_t>(np.v[j]);
     }
@@ -209,7 +212,7 @@ __global__ __launch_bounds__(kWaves * 64) void adamw_kernel(const Batch a) {
       float tm = 0.0f, tv = 0.0f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        v[j] = sqrtf(v[j]);
+        v[j] = root[j];
         tm = fmaxf(tm, fabsf(m[j]));
         tv = fmaxf(tv, v[j]);
       }
