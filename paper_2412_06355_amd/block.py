@@ -406,11 +406,9 @@ def adamw(cfg: AdamWConfig, params, grads, states, step, *, copies=None, grad_sc
     eight = STATE[cfg.state] == 1
     state_type, parts = (f8, 4) if eight else (f32, 2)
 
-    if len({p.data_ptr() for p in params if p.numel()}) != sum(1 for p in params if p.numel()):
-        raise ValueError("params: a tensor appears twice")
     pack = struct.Struct("@q7Pi4x").pack_into
     array = bytearray(ctypes.sizeof(dendsn_adamw_tensor) * count)
-    gpu, here, ms, vs, c, at = dev.type == "cuda", params[0].get_device(), 0, 0, 0, 0
+    gpu, here, ms, vs, c, at, seen = dev.type == "cuda", params[0].get_device(), 0, 0, 0, 0, []
     for i, (p, g, s) in enumerate(zip(params, grads, states)):
         if len(s) != parts:
             raise ValueError(f"states of tensor {i}: {len(s)} tensors, expected {parts}")
@@ -437,8 +435,13 @@ def adamw(cfg: AdamWConfig, params, grads, states, step, *, copies=None, grad_sc
             c = copies[i]
             _expect(c, f"copy of tensor {i}", shape, bf16, dev, optional=True)
             c = 0 if c is None else c.data_ptr()
-        pack(array, at, n, p.data_ptr(), g.data_ptr(), m.data_ptr(), v.data_ptr(), ms, vs, c, half)
+        where = p.data_ptr()
+        if n:
+            seen.append(where)
+        pack(array, at, n, where, g.data_ptr(), m.data_ptr(), v.data_ptr(), ms, vs, c, half)
         at += 72
+    if len(set(seen)) != len(seen):
+        raise ValueError("params: a tensor appears twice")
     step_dev = None
     if isinstance(step, torch.Tensor):
         _expect(step, "step", (1,), torch.int32, dev)

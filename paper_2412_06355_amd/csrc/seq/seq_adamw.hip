@@ -7,7 +7,12 @@
 // states in 8 bits.  The tensors' pointers are kernel arguments, 40 tensors a launch: nothing
 // is copied to the device, and a captured step holds them.  A block has 8192 values of one
 // tensor, a wave 256 at a time, which is also the block of values that share a scale in 8 bits:
-// its largest magnitude is found within the wave.
+// its largest magnitude is found within the wave.  Two rounds' loads are issued together, without
+// conditions where a round is whole (1683 -> 1589 us below).
+//
+// 292M values in 122 tensors, bf16 gradients and copies: 1589 us with fp32 states (5.15 TB/s, a copy's
+// rate), 961 us in 8 bits (4.9 TB/s; its 70 vector instructions a value take nearly as long:
+// with a second root and a division 1056).
 //
 // In 8 bits a value is rounded down or up at random, so that its mean is kept.  v changes by a
 // thousandth a step, e4m3 values lie an eighth to a sixteenth apart: rounded to the nearest, v
