@@ -386,12 +386,26 @@ void dispatch(Shape s, F&& f) {
   else packs(std::integral_constant<int, 1024>{});
 }
 
+// A launch has at most 2^31 threads: with more rows there are several.
 template <typename IO, bool E4M3>
-void launch_forward(const NormArgs& a, Shape s, hipStream_t stream) {
-  const dim3 grid(unsigned(ceil_div(a.N, s.lanes < 256 ? 256 / s.lanes : 1))), block(s.lanes > 256 ? s.lanes : 256);
-  dispatch(s, [&](auto lanes, auto packs) {
-    norm_fwd_kernel<IO, decltype(lanes)::value, decltype(packs)::value, E4M3><<<grid, block, 0, stream>>>(a);
-  });
+void launch_forward(const NormArgs& whole, Shape s, hipStream_t stream) {
+  const int threads = s.lanes > 256 ? s.lanes : 256, rows = threads / s.lanes;
+  const int64_t most = (int64_t(1) << 31) / threads * rows;
+  auto from = [](auto* p, int64_t at) { return p ? p + at : p; };
+  for (int64_t n0 = 0; n0 < whole.N; n0 += most) {
+    NormArgs a = whole;
+    a.N = int32_t(whole.N - n0 < most ? whole.N - n0 : most);
+    a.x = static_cast<const IO*>(a.x) + n0 * a.ld_x;
+    a.residual = from(static_cast<const IO*>(a.residual), n0 * a.ld_residual);
+    a.y = static_cast<char*>(a.y) + n0 * a.ld_y * (E4M3 ? 1 : int64_t(sizeof(IO)));
+    a.sum = from(static_cast<IO*>(a.sum), n0 * a.ld_sum);
+    a.rstd = from(a.rstd, n0);
+    a.scale = from(a.scale, n0);
+    const dim3 grid(unsigned(ceil_div(a.N, rows))), block(threads);
+    dispatch(s, [&](auto lanes, auto packs) {
+      norm_fwd_kernel<IO, decltype(lanes)::value, decltype(packs)::value, E4M3><<<grid, block, 0, stream>>>(a);
+    });
+  }
 }
 
 template <typename IO, bool W>
@@ -408,8 +422,8 @@ dendsn_status forward(const dendsn_norm_cfg* cfg, const void* x, const void* res
   const dendsn_status st = check_cfg(cfg);
   if (st != DENDSN_OK) return st;
   const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
-  // a row has a block at least, of up to 1024 threads: a launch has fewer than 2^32
-  if (cfg->N > (int64_t(1) << 23) && shape_of(cfg).lanes >= 256) return fail(DENDSN_E_UNSUPPORTED, "more than 2^23 rows of this length");
+  // (x and y would not be in memory together)
+  if (cfg->N > (int64_t(1) << 23) && shape_of(cfg).lanes == 1024) return fail(DENDSN_E_UNSUPPORTED, "more than 2^23 rows of this length");
   if (cfg->N > 0 && (!x || !y || (e4m3 && !scale))) return fail(DENDSN_E_INVALID, e4m3 ? "x, y or scale is NULL" : "x or y is NULL");
   if (!aligned(x, esz) || !aligned(residual, esz) || !aligned(weight, esz) || !aligned(sum, esz) || (!e4m3 && !aligned(y, esz)))
     return fail(DENDSN_E_INVALID, "x, residual, weight, y or sum misaligned");

@@ -28,6 +28,27 @@ def test_norm_rows_far_apart(gpu_device):
     seq_ref.assert_within(back["grad_x"][some], *ref["grad_x"], "grad_x")
 
 
+def test_norm_more_rows_than_a_launch_has(gpu_device):
+    n, D = (1 << 28) + 5, 8  # 16 rows are a block of 256 threads: 2^32 and some
+    one = torch.tensor([1.0, -2.0, 0.5, 4.0, -1.0, 0.25, 3.0, -0.125], dtype=torch.bfloat16, device=gpu_device)
+    x = (torch.arange(n, device=gpu_device, dtype=torch.int32) % 7 + 1).to(torch.bfloat16)[:, None] * one
+    some = torch.tensor([0, 1, (1 << 27) - 1, 1 << 27, (1 << 27) + 1, (1 << 28) - 1, 1 << 28, n - 1], device=gpu_device)
+    residual = one.view(1, D).expand(n, D)
+    cfg = dendsn.RMSNormConfig(N=n, D=D, io="bf16")
+    ref = block_ref.norm(x[some], one, residual[some], 1e-6, "bf16", x[some])
+    announce("norm of many rows")
+    y, rstd, total = dendsn.rms_norm(cfg, x, one, residual)
+    for k, got in (("y", y), ("rstd", rstd), ("sum", total)):
+        seq_ref.assert_within(got[some], *ref[k], k)
+    del y
+    announce("norm of many rows, e4m3")
+    y8, scale, rstd8, total8 = dendsn.rms_norm_e4m3(cfg, x, one, residual)
+    few = cfg.with_(N=len(some))
+    want = dendsn.rms_norm_e4m3(few, x[some], one, residual[some])
+    for got, w in zip((y8.view(torch.uint8), scale, rstd8, total8), (want[0].view(torch.uint8), *want[1:])):
+        assert torch.equal(got[some], w)
+
+
 def test_adamw_value_numbers_past_32_bits(gpu_device):
     n = (1 << 32) + 777  # 17 GB of parameters, 8-bit states
     p = torch.zeros((n,), device=gpu_device)
