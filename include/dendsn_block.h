@@ -190,6 +190,8 @@ typedef struct dendsn_adamw_tensor {
  * to the nearest v could not fall by less than a sixteenth, and would not fall at all.  A v
  * that is not 0 is kept above 0.  The random bits are a hash of seed, the step, the tensor's
  * place in the list and the value's place in the tensor.
+ * A gradient that is not finite makes its own states and parameter not finite; an infinite one
+ * does so, in 8 bits, to the states of its block of 256.
  * Tensors may not overlap; none may appear twice.
  */
 dendsn_status dendsn_adamw_step(const dendsn_adamw_cfg* cfg, const dendsn_adamw_tensor* tensors, int64_t count,

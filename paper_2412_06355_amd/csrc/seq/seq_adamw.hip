@@ -20,6 +20,8 @@
 // that is not 0 stays at least at the smallest code, so that m / root stays bounded.  Whether a
 // value goes down or up hangs on its last bit, so what decides it is computed as it is written:
 // products and sums rounded one by one, quotients to the nearest.
+#include <cfloat>
+
 #include "dendsn_block.h"
 #include "seq_common.h"
 
@@ -294,7 +296,9 @@ extern "C" dendsn_status dendsn_adamw_step(const dendsn_adamw_cfg* cfg, const de
   Batch a{};
   a.b1 = float(cfg->beta1); a.c1 = float(1.0 - cfg->beta1);
   a.b2 = float(cfg->beta2); a.c2 = float(1.0 - cfg->beta2);
-  a.lr = float(cfg->lr); a.eps = float(cfg->eps); a.wd = float(cfg->weight_decay);
+  a.lr = float(cfg->lr); a.wd = float(cfg->weight_decay);
+  // (the reciprocal takes what is below the normal numbers for 0: an eps that is not 0 stays one of them)
+  a.eps = cfg->eps > 0.0 && cfg->eps < FLT_MIN ? FLT_MIN : float(cfg->eps);
   a.log_b1 = log(cfg->beta1); a.log_b2 = log(cfg->beta2);
   a.fix1 = float(-expm1(double(step) * a.log_b1)); a.fix2 = float(-expm1(double(step) * a.log_b2));
   a.step = uint32_t(step); a.seed_lo = uint32_t(seed); a.seed_hi = uint32_t(seed >> 32);

@@ -136,3 +136,47 @@ def test_seeds_differ_and_repeat(gpu_device):
     a, b, c = once(1), once(1), once(1 + (1 << 40))
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
     assert not torch.equal(a[0], c[0]) and not torch.equal(a[0], a[1])
+
+
+@pytest.mark.parametrize("eps", [1e-40, 1e-300])
+def test_eps_below_the_normal_numbers(gpu_device, eps):
+    """Values that have had no gradient stay as they are: 0 / (0 + eps) is 0."""
+    p, g, m, v = make([600], 8, gpu_device)
+    for t in (g[0], m[0], v[0]):
+        t[:300] = 0
+    before = p[0].clone()
+    cfg = dendsn.AdamWConfig(lr=1e-3, eps=eps, weight_decay=0.0)
+    want = block_ref.adamw(before, g[0], m[0], v[0], 3, lr=1e-3, eps=eps, wd=0.0)
+    announce(f"adamw eps {eps}")
+    dendsn.adamw(cfg, p, g, [(m[0], v[0])], 3)
+    assert torch.equal(p[0][:300], before[:300])
+    seq_ref.assert_within(p[0][300:], *(x[300:] for x in want["p"]), "p")
+
+
+@pytest.mark.parametrize("state", ["f32", "e4m3"])
+def test_gradients_that_are_not_finite(gpu_device, state):
+    """NaN stays with its value; infinity does too, but for 8-bit states, whose block it takes."""
+    cfg = dendsn.AdamWConfig(state=state)
+
+    def once(at):
+        p, g, _, _ = make([1100], 9, gpu_device)
+        g[0][[300, 600]] = 0.0
+        for i, x in at:
+            g[0][i] = x
+        states = dendsn.adamw_states(cfg, p)
+        dendsn.adamw(cfg, p, g, states, 1, seed=5)
+        return [p[0]] + [t.view(torch.uint8) if t.dtype == torch.float8_e4m3fn else t for t in states[0]], states[0]
+
+    announce(f"adamw not finite {state}")
+    (want, _), (got, held) = once([]), once([(300, float("nan")), (600, float("inf"))])
+    place = torch.arange(1100, device=gpu_device)
+    own, block = (place == 300) | (place == 600), (place == 300) | (place // 256 == 2)
+    assert not got[0][own].isfinite().any() and torch.equal(got[0][~own], want[0][~own])
+    codes = (1, 2) if state == "f32" else (1, 3)
+    for i in codes:
+        spared = ~own if state == "f32" else ~block
+        assert torch.equal(got[i][spared], want[i][spared])
+        assert not held[i - 1].float()[own].isfinite().any()
+    if state == "e4m3":
+        for i in (2, 4):
+            assert torch.equal(got[i][[0, 1, 3, 4]], want[i][[0, 1, 3, 4]])
