@@ -192,7 +192,8 @@ typedef struct dendsn_adamw_tensor {
  * place in the list and the value's place in the tensor.
  * A gradient that is not finite makes its own states and parameter not finite; an infinite one
  * does so, in 8 bits, to the states of its block of 256.
- * Tensors may not overlap; none may appear twice.
+ * Arrays that are written (param, m, v, scales, copy) may not overlap, within a tensor or between two
+ * (not checked); grad is read alone and may be shared.
  */
 dendsn_status dendsn_adamw_step(const dendsn_adamw_cfg* cfg, const dendsn_adamw_tensor* tensors, int64_t count,
                                 int64_t step, const int32_t* step_dev, const float* grad_scale, uint64_t seed,

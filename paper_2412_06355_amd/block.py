@@ -392,7 +392,8 @@ def adamw(cfg: AdamWConfig, params, grads, states, step, *, copies=None, grad_sc
     shapes, ``states`` as ``adamw_states`` gives them; all contiguous.  ``step`` is its number from 1
     on, an int or an int32 tensor [1] on the GPU; ``copies``, a list of bf16 tensors (or None in a
     place), receive the new parameters rounded; ``grad_scale`` [1] fp32 multiplies the gradients;
-    ``seed`` is that of the random rounding of 8-bit states.  A tensor may appear once."""
+    ``seed`` is that of the random rounding of 8-bit states.  What is written (params, states, scales,
+    copies) may appear once, and may not overlap otherwise (not checked); a gradient may be shared."""
     import torch
 
     count = len(params)
@@ -408,7 +409,7 @@ def adamw(cfg: AdamWConfig, params, grads, states, step, *, copies=None, grad_sc
 
     pack = struct.Struct("@q7Pi4x").pack_into
     array = bytearray(ctypes.sizeof(dendsn_adamw_tensor) * count)
-    gpu, here, ms, vs, c, at, seen = dev.type == "cuda", params[0].get_device(), 0, 0, 0, 0, []
+    gpu, here, ms, vs, c, at, written = dev.type == "cuda", params[0].get_device(), 0, 0, 0, 0, []
     for i, (p, g, s) in enumerate(zip(params, grads, states)):
         if len(s) != parts:
             raise ValueError(f"states of tensor {i}: {len(s)} tensors, expected {parts}")
@@ -431,17 +432,19 @@ def adamw(cfg: AdamWConfig, params, grads, states, step, *, copies=None, grad_sc
             for t, name in ((s[1], "m_scale"), (s[3], "root_scale")):
                 _expect(t, f"{name} of tensor {i}", (-(-n // STATE_BLOCK),), f32, dev)
             ms, vs = s[1].data_ptr(), s[3].data_ptr()
+            written += (ms, vs)
         if copies is not None:
             c = copies[i]
             _expect(c, f"copy of tensor {i}", shape, bf16, dev, optional=True)
             c = 0 if c is None else c.data_ptr()
-        where = p.data_ptr()
-        if n:
-            seen.append(where)
-        pack(array, at, n, where, g.data_ptr(), m.data_ptr(), v.data_ptr(), ms, vs, c, half)
+            written.append(c)
+        pa, ma, va = p.data_ptr(), m.data_ptr(), v.data_ptr()
+        written += (pa, ma, va)
+        pack(array, at, n, pa, g.data_ptr(), ma, va, ms, vs, c, half)
         at += 72
-    if len(set(seen)) != len(seen):
-        raise ValueError("params: a tensor appears twice")
+    # two blocks of a launch would race on an array that is written and there twice (0: empty)
+    if len(set(written)) != len(written) and len(set(written) - {0}) != len(written) - written.count(0):
+        raise ValueError("params, states, copies: an array that is written appears twice")
     step_dev = None
     if isinstance(step, torch.Tensor):
         _expect(step, "step", (1,), torch.int32, dev)

@@ -1,0 +1,65 @@
+"""Refusals of the block operators' binding that need no GPU: the tensors are of the CPU, so that a
+call that is not refused for its arguments is refused for where they lie."""
+
+import pytest
+import torch
+
+import paper_2412_06355_amd as dendsn
+
+
+def adamw_lists(state, copies=True):
+    n = (300, 5)
+    cfg = dendsn.AdamWConfig(state=state)
+    params = [torch.zeros(k) for k in n]
+    return cfg, dict(params=params, grads=[torch.zeros(k) for k in n], states=dendsn.adamw_states(cfg, params),
+                     copies=[torch.zeros(k, dtype=torch.bfloat16) for k in n] if copies else None)
+
+
+def refusal(cfg, lists):
+    with pytest.raises(ValueError) as e:
+        dendsn.adamw(cfg, lists["params"], lists["grads"], lists["states"], 1, copies=lists["copies"])
+    return str(e.value)
+
+
+@pytest.mark.parametrize("state,part", [("f32", 0), ("f32", 1), ("e4m3", 0), ("e4m3", 1), ("e4m3", 2), ("e4m3", 3)])
+def test_a_state_that_two_tensors_share(state, part):
+    """Each part of a state, of two tensors of one size: two blocks of one launch would write it."""
+    cfg, x = adamw_lists(state)
+    x.update({k: [v[0], v[0].clone()] if k in ("params", "grads", "copies") else v for k, v in x.items()})
+    one = [t.clone() for t in x["states"][0]]
+    two = [t.clone() for t in one]
+    x["states"] = [one, two]
+    assert "twice" not in refusal(cfg, x)
+    two[part] = one[part]
+    assert "twice" in refusal(cfg, x)
+
+
+@pytest.mark.parametrize("state", ["f32", "e4m3"])
+def test_arrays_of_one_tensor_that_are_one(state):
+    cfg, x = adamw_lists(state)
+    assert "twice" not in refusal(cfg, x)
+    s = x["states"][0]
+    half = len(s) // 2
+    x["states"][0] = (*s[:half], *s[:half])  # v is m, and with it its scale
+    assert "twice" in refusal(cfg, x)
+
+
+def test_copies_and_parameters():
+    cfg, x = adamw_lists("f32")
+    x["params"][1] = torch.zeros(300)
+    x["grads"][1] = x["grads"][0]        # read alone: may be shared
+    x["states"][1] = tuple(torch.zeros(300) for _ in range(2))
+    x["copies"][1] = torch.zeros(300, dtype=torch.bfloat16)
+    assert "twice" not in refusal(cfg, x)
+    assert "twice" in refusal(cfg, dict(x, copies=[x["copies"][0]] * 2))
+    assert "twice" in refusal(cfg, dict(x, copies=[x["params"][0].view(torch.bfloat16)[:300], None]))
+    assert "twice" in refusal(cfg, dict(x, states=[(x["params"][1], torch.zeros(300)), x["states"][1]]))
+    assert "twice" in refusal(cfg, dict(x, params=[x["params"][0]] * 2))
+
+
+def test_empty_tensors_are_no_arrays():
+    cfg, x = adamw_lists("f32", copies=False)
+    for k in ("params", "grads"):
+        x[k] += [torch.zeros(0)] * 2
+    x["states"] += [(torch.zeros(0), torch.zeros(0))] * 2
+    assert "twice" not in refusal(cfg, x)
