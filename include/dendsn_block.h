@@ -112,8 +112,8 @@ dendsn_status dendsn_delta_step(const dendsn_delta_cfg* cfg, const void* q, cons
 /* Root-mean-square norm                                                      */
 /* ------------------------------------------------------------------------- */
 typedef struct dendsn_norm_cfg {
-    int64_t N;          /* rows, 0 <= N <= 2^31 - 1; forward: 2^23 at most of rows of more than
-                         * 16 KiB                                              */
+    int64_t N;          /* rows, 0 <= N <= 2^31 - 1; forward: x and y of 2^39 bytes at most
+                         * together, which is more than a card's memory       */
     int64_t D;          /* values of a row, 1 <= D <= 2^22                     */
     int64_t ld_x, ld_residual, ld_y, ld_sum;                 /* forward              */
     int64_t ld_grad_y, ld_grad_sum, ld_grad_x;               /* backward             */

@@ -422,8 +422,10 @@ dendsn_status forward(const dendsn_norm_cfg* cfg, const void* x, const void* res
   const dendsn_status st = check_cfg(cfg);
   if (st != DENDSN_OK) return st;
   const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
-  // (x and y would not be in memory together)
-  if (cfg->N > (int64_t(1) << 23) && shape_of(cfg).lanes == 1024) return fail(DENDSN_E_UNSUPPORTED, "more than 2^23 rows of this length");
+  // (x's rows may be one, or overlap)
+  const int64_t x_bytes = ((cfg->N - 1) * cfg->ld_x + cfg->D) * int64_t(esz), y_bytes = cfg->N * cfg->D * (e4m3 ? 1 : int64_t(esz));
+  if (cfg->N > 0 && x_bytes + y_bytes > (int64_t(1) << 39))
+    return fail(DENDSN_E_UNSUPPORTED, "x and y of more than 2^39 bytes");
   if (cfg->N > 0 && (!x || !y || (e4m3 && !scale))) return fail(DENDSN_E_INVALID, e4m3 ? "x, y or scale is NULL" : "x or y is NULL");
   if (!aligned(x, esz) || !aligned(residual, esz) || !aligned(weight, esz) || !aligned(sum, esz) || (!e4m3 && !aligned(y, esz)))
     return fail(DENDSN_E_INVALID, "x, residual, weight, y or sum misaligned");

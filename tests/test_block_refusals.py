@@ -1,10 +1,14 @@
-"""Refusals of the block operators' binding that need no GPU: the tensors are of the CPU, so that a
-call that is not refused for its arguments is refused for where they lie."""
+"""What the block operators refuse, and what they do not, without a GPU: the binding's tensors are of the
+CPU, so that a call that is not refused for its arguments is refused for where they lie; a C call that
+is not refused for its sizes is for an address."""
+
+import ctypes
 
 import pytest
 import torch
 
 import paper_2412_06355_amd as dendsn
+from paper_2412_06355_amd.block import dendsn_norm_cfg
 
 
 def adamw_lists(state, copies=True):
@@ -63,3 +67,28 @@ def test_empty_tensors_are_no_arrays():
         x[k] += [torch.zeros(0)] * 2
     x["states"] += [(torch.zeros(0), torch.zeros(0))] * 2
     assert "twice" not in refusal(cfg, x)
+
+
+def norm_call(e4m3=False, x=0x10001, **kw):
+    """The status of a norm's forward whose x is misaligned (INVALID), if its size is not refused before."""
+    c = dict(N=10, D=64, io=0, eps=1e-6)
+    c.update(kw)
+    for k in ("ld_x", "ld_residual", "ld_y", "ld_sum", "ld_grad_y", "ld_grad_sum", "ld_grad_x"):
+        c.setdefault(k, c["D"])
+    call = dendsn.block_lib().dendsn_norm_forward_e4m3 if e4m3 else dendsn.block_lib().dendsn_norm_forward
+    at = [ctypes.c_void_p(a) for a in (x, 0x20000, 0x30000, 0x40000, 0x50000, 0x60000, 0x70000)[:7 if e4m3 else 6]]
+    return call(ctypes.byref(dendsn_norm_cfg(**c)), *at, None)
+
+
+def test_norm_rows_that_memory_holds_are_not_refused():
+    """Many long rows: in 8 bits, or of an x whose rows are one or overlap.  What x and y span together
+    is the limit, whatever a row's length."""
+    INVALID, UNSUPPORTED, many = 1, 2, (1 << 23) + 1
+    assert norm_call(e4m3=True, N=many, D=8200, io=1) == INVALID              # 128 + 64 GiB
+    assert norm_call(e4m3=True, N=many, D=16384, io=1, ld_x=0) == INVALID     # 128 GiB of y
+    assert norm_call(N=many, D=8200, io=1, ld_x=1) == INVALID
+    assert norm_call(N=1 << 24, D=4096) == INVALID                            # 2^39 bytes, all of them
+    assert norm_call(N=1 << 23, D=8192) == INVALID
+    assert norm_call(N=many, D=8192) == UNSUPPORTED
+    assert norm_call(N=(1 << 24) + 1, D=4096) == UNSUPPORTED
+    assert norm_call(N=0, D=1 << 22) == INVALID
