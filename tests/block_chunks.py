@@ -152,9 +152,11 @@ def bounds(ref, K, io, segments=False):
     out = {}
     for name, x in ref.items():
         size = over_head(name, x)
-        if name == "grad_g":
+        if name in ("s_last", "grad_s0"):
+            out[name] = state * size
+        elif name == "grad_g":
             out[name] = kept * size + 2 * one * (64 / K) ** 0.5 * over_head(name, ref["terms"])
-        elif name not in ("terms", "s_last", "grad_s0"):
+        elif name != "terms":
             out[name] = (kept + (one if name == "o" else 2 * one)) * size
     return {name: x + TINY for name, x in out.items()}
 

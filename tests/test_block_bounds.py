@@ -39,3 +39,17 @@ def test_a_term_left_out_of_the_decays_gradient_shows(case):
             without = block_chunks.delta(d, cfg.K ** -0.5, leave_out=(name,))
             over = (block_chunks.off(without["grad_g"], ref, "grad_g") / bound)[long]
             assert float(over.min()) > 1 and float(over.median()) > 10, (io, name, float(over.min()))
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_states_of_two_bf16_values_show(case):
+    """Three bf16 values an operand are within the states' bound, two are not."""
+    cfg, d, segments = case_of(case, "bf16")
+    ref = block_chunks.delta(d, cfg.K ** -0.5)
+    bound = block_chunks.bounds(ref, cfg.K, "bf16", segments)
+    three, two = (block_chunks.delta(d, cfg.K ** -0.5, planes=n) for n in (3, 2))
+    ran = torch.full((cfg.batch,), True) if d["lengths"] is None else d["lengths"] > block_chunks.CHUNK
+    for name in ("s_last", "grad_s0"):
+        assert bool((block_chunks.off(three[name], ref, name) <= bound[name]).all()), name
+        away = block_chunks.off(two[name], ref, name)
+        assert bool((away[ran] > bound[name][ran]).all()), (name, float((away / bound[name])[ran].min()))
