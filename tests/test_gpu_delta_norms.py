@@ -13,6 +13,11 @@ from tests.test_gpu_delta import make, run
 CASES = [
     (300, 2, 3, 1, 128, 48, False, 0.3, False),
     (200, 3, 2, 0, 60, 33, True, 0.05, False),
+    # blocks of 32 columns, several a head, five and six chunks: all lengths around the chunks' ends
+    (330, 8, 16, 8, 128, 64, True, 0.1, False),
+    (330, 8, 16, 0, 69, 40, True, 0.1, False),
+    (300, 8, 11, 0, 64, 96, True, 0.1, False),
+    (300, 8, 16, 0, 21, 33, True, 0.1, False),
     # segments
     (1537, 3, 2, 1, 36, 33, True, 0.02, True),
     (2100, 1, 2, 0, 128, 64, False, 0.02, True),
