@@ -144,7 +144,9 @@ dendsn_status dendsn_norm_workspace_bytes(const dendsn_norm_cfg* cfg, size_t* by
 
 /*
  * Gradients of sum(grad_y * y) + sum(grad_sum * sum); that of x is also the residual's.
- *   x           [N,D] io    the forward's x, or its sum where it had a residual (ld_x)
+ *   x           [N,D] io    the forward's x, or its sum where it had a residual (ld_x): what is
+ *                           differentiated is the norm of this row.  In bf16 the sum's rounding moves
+ *                           grad_weight by as much as grad_weight's own
  *   rstd        [N] fp32    the forward's
  *   grad_y      [N,D] io    required
  *   grad_sum    [N,D] io    NULL means 0
@@ -154,6 +156,13 @@ dendsn_status dendsn_norm_workspace_bytes(const dendsn_norm_cfg* cfg, size_t* by
 dendsn_status dendsn_norm_backward(const dendsn_norm_cfg* cfg, const void* x, const void* weight, const float* rstd,
                                    const void* grad_y, const void* grad_sum, void* grad_x, void* grad_weight,
                                    void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The same from the forward's x and residual [N,D] io (ld_residual; NULL: as above), whose sum is formed
+ * again in fp32: gradients of what y is the norm of, for one more array read. */
+dendsn_status dendsn_norm_backward_residual(const dendsn_norm_cfg* cfg, const void* x, const void* residual,
+                                            const void* weight, const float* rstd, const void* grad_y,
+                                            const void* grad_sum, void* grad_x, void* grad_weight, void* workspace,
+                                            size_t workspace_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------- */
 /* AdamW                                                                      */

@@ -42,6 +42,7 @@ from .block import (  # noqa: F401
     dendsn_delta_step,
     dendsn_delta_workspace_bytes,
     dendsn_norm_backward,
+    dendsn_norm_backward_residual,
     dendsn_norm_forward,
     dendsn_norm_forward_e4m3,
     dendsn_norm_workspace_bytes,

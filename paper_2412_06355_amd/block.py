@@ -63,6 +63,7 @@ _SIGS = {
     "dendsn_norm_forward_e4m3": (ctypes.c_int, [_NORM] + [_P] * 8),
     "dendsn_norm_workspace_bytes": (ctypes.c_int, [_NORM, _SIZE]),
     "dendsn_norm_backward": (ctypes.c_int, [_NORM] + [_P] * 8 + [_Z, _P]),
+    "dendsn_norm_backward_residual": (ctypes.c_int, [_NORM] + [_P] * 9 + [_Z, _P]),
     "dendsn_adamw_step": (ctypes.c_int, [_ADAMW, _P, _I64, _I64, _P, _P, ctypes.c_uint64, _P]),
 }
 
@@ -284,6 +285,15 @@ def dendsn_norm_backward(cfg: RMSNormConfig, x, weight, rstd, grad_y, grad_sum, 
                                             _nbytes(workspace), st))
 
 
+def dendsn_norm_backward_residual(cfg: RMSNormConfig, x, residual, weight, rstd, grad_y, grad_sum, grad_x, grad_weight,
+                                  workspace, stream=None):
+    st = stream if stream is not None else _stream(x.device)
+    c = cfg.to_c(x, residual, None, None, grad_y, grad_sum, grad_x)
+    _check(block_lib().dendsn_norm_backward_residual(ctypes.byref(c), _ptr(x), _ptr(residual), _ptr(weight), _ptr(rstd),
+                                                     _ptr(grad_y), _ptr(grad_sum), _ptr(grad_x), _ptr(grad_weight),
+                                                     _ptr(workspace), _nbytes(workspace), st))
+
+
 def _check_norm(cfg, x, weight, residual):
     dt, dev = _io_dtype(cfg.io), x.device
     _expect(x, "x", (cfg.N, cfg.D), dt, dev, rows=True)
@@ -322,25 +332,27 @@ def rms_norm_e4m3(cfg: RMSNormConfig, x, weight=None, residual=None):
     return y, scale, rstd, summed
 
 
-def rms_norm_backward(cfg: RMSNormConfig, x, weight, rstd, grad_y, grad_sum=None, *, workspace=None):
+def rms_norm_backward(cfg: RMSNormConfig, x, weight, rstd, grad_y, grad_sum=None, *, residual=None, workspace=None):
     """Returns a dict with grad_x [N, D] io (also the residual's) and, where there is a ``weight``,
     grad_weight [D] io: the gradients of sum(grad_y * y) + sum(grad_sum * sum).  ``x`` is the
-    forward's, or the sum that it gave."""
+    forward's, or the sum that it gave, which has io's bits; with the forward's ``residual`` beside its
+    x their sum is formed again in fp32, as y had it, for one more array read."""
     import torch
 
-    dt, dev = _check_norm(cfg, x, weight, None)
+    dt, dev = _check_norm(cfg, x, weight, residual)
     _expect(rstd, "rstd", (cfg.N,), torch.float32, dev)
     _expect(grad_y, "grad_y", (cfg.N, cfg.D), dt, dev, rows=True)
     _expect(grad_sum, "grad_sum", (cfg.N, cfg.D), dt, dev, optional=True, rows=True)
     st, fn = _stream(dev), block_lib()
     out = dict(grad_x=x.new_empty((cfg.N, cfg.D)))
-    c = cfg.to_c(x, None, None, None, grad_y, grad_sum)
+    c = cfg.to_c(x, residual, None, None, grad_y, grad_sum)
     ws = None
     if weight is not None:
         out["grad_weight"] = x.new_empty((cfg.D,))
         ws = _workspace(_bytes(fn.dendsn_norm_workspace_bytes, ctypes.byref(c)), workspace, dev)
-    _check(fn.dendsn_norm_backward(ctypes.byref(c), _ptr(x), _ptr(weight), _ptr(rstd), _ptr(grad_y), _ptr(grad_sum),
-                                   _ptr(out["grad_x"]), _ptr(out.get("grad_weight")), _ptr(ws), _nbytes(ws), st))
+    _check(fn.dendsn_norm_backward_residual(ctypes.byref(c), _ptr(x), _ptr(residual), _ptr(weight), _ptr(rstd), _ptr(grad_y),
+                                            _ptr(grad_sum), _ptr(out["grad_x"]), _ptr(out.get("grad_weight")), _ptr(ws),
+                                            _nbytes(ws), st))
     return out
 
 

@@ -213,7 +213,12 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_kernel(NormArg
   }
 }
 
-template <typename IO, int TPR, int kE, bool W>
+// hat is of the row that is given: of the sum that the forward stored, which has io's bits, or (RES) of
+// x + residual, formed again as the forward had it, for one more row read.  What y and rstd are the norm
+// of is the second; in bf16 the first moves every hat by up to 2^-8 of itself, and grad_weight by about as
+// much as its own rounding does (off by 2.4e-3 in norm, not 1.7e-3).  The choice is the caller's: 16384
+// rows of 4096 in bf16 take 120 us the first way, 146 the second.
+template <typename IO, int TPR, int kE, bool W, bool RES>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(NormArgs a) {
   constexpr int V = kV<IO>, kBlock = TPR > 256 ? TPR : 256, kRows = kBlock / TPR;
   __shared__ float red[TPR > 64 ? TPR / 64 : 1];
@@ -229,6 +234,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(NormArg
   bool first = true;
   for (int64_t n = int64_t(blockIdx.x) * kRows + sub; n < a.N; n += int64_t(gridDim.x) * kRows) {
     const IO* x = static_cast<const IO*>(a.x) + n * a.ld_x;
+    const IO* res = RES ? static_cast<const IO*>(a.residual) + n * a.ld_residual : nullptr;
     const IO* gy = static_cast<const IO*>(a.gy) + n * a.ld_gy;
     const IO* gs = a.gsum ? static_cast<const IO*>(a.gsum) + n * a.ld_gsum : nullptr;
     IO* gx = static_cast<IO*>(a.gx) + n * a.ld_gx;
@@ -237,6 +243,12 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(NormArg
     auto pack_of = [&](int base, float (&hat)[V], float (&g)[V], float (&d)[V]) {
       load_row<IO, V>(x, base, a.D, hat);
       load_row<IO, V>(gy, base, a.D, g);
+      if (RES) {
+        float r[V];
+        load_row<IO, V>(res, base, a.D, r);
+#pragma unroll
+        for (int j = 0; j < V; ++j) hat[j] += r[j];
+      }
       float ww[V];
       if (W) load_row<IO, V>(w, base, a.D, ww);
 #pragma unroll
@@ -412,7 +424,8 @@ template <typename IO, bool W>
 void launch_backward(const NormArgs& a, Shape s, int64_t blocks, hipStream_t stream) {
   const dim3 grid{unsigned(blocks)}, block(s.lanes > 256 ? s.lanes : 256);
   dispatch(s, [&](auto lanes, auto packs) {
-    norm_bwd_kernel<IO, decltype(lanes)::value, decltype(packs)::value, W><<<grid, block, 0, stream>>>(a);
+    if (a.residual) norm_bwd_kernel<IO, decltype(lanes)::value, decltype(packs)::value, W, true><<<grid, block, 0, stream>>>(a);
+    else norm_bwd_kernel<IO, decltype(lanes)::value, decltype(packs)::value, W, false><<<grid, block, 0, stream>>>(a);
   });
 }
 
@@ -471,15 +484,23 @@ dendsn_status dendsn_norm_workspace_bytes(const dendsn_norm_cfg* cfg, size_t* by
 dendsn_status dendsn_norm_backward(const dendsn_norm_cfg* cfg, const void* x, const void* weight, const float* rstd,
                                    const void* grad_y, const void* grad_sum, void* grad_x, void* grad_weight,
                                    void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  return dendsn_norm_backward_residual(cfg, x, nullptr, weight, rstd, grad_y, grad_sum, grad_x, grad_weight, workspace,
+                                       workspace_bytes, stream);
+}
+
+dendsn_status dendsn_norm_backward_residual(const dendsn_norm_cfg* cfg, const void* x, const void* residual,
+                                            const void* weight, const float* rstd, const void* grad_y,
+                                            const void* grad_sum, void* grad_x, void* grad_weight, void* workspace,
+                                            size_t workspace_bytes, hipStream_t stream) {
   clear_error();
   dendsn_status st = check_cfg(cfg);
   if (st != DENDSN_OK) return st;
   const size_t esz = cfg->io == DENDSN_IO_BF16 ? 2 : 4;
   if (cfg->N > 0 && (!x || !rstd || !grad_y || !grad_x)) return fail(DENDSN_E_INVALID, "x, rstd, grad_y or grad_x is NULL");
   if (weight && !grad_weight) return fail(DENDSN_E_INVALID, "grad_weight is NULL");
-  if (!aligned(x, esz) || !aligned(weight, esz) || !aligned(grad_y, esz) || !aligned(grad_sum, esz) ||
-      !aligned(grad_x, esz) || !aligned(grad_weight, esz) || !aligned(rstd, 4))
-    return fail(DENDSN_E_INVALID, "x, weight, rstd, grad_y, grad_sum, grad_x or grad_weight misaligned");
+  if (!aligned(x, esz) || !aligned(residual, esz) || !aligned(weight, esz) || !aligned(grad_y, esz) ||
+      !aligned(grad_sum, esz) || !aligned(grad_x, esz) || !aligned(grad_weight, esz) || !aligned(rstd, 4))
+    return fail(DENDSN_E_INVALID, "x, residual, weight, rstd, grad_y, grad_sum, grad_x or grad_weight misaligned");
   if (weight) {
     st = check_workspace(workspace, workspace_bytes, size_t(parts_of(cfg)) * size_t(cfg->D) * sizeof(float),
                          "dendsn_norm_workspace_bytes");
@@ -487,9 +508,9 @@ dendsn_status dendsn_norm_backward(const dendsn_norm_cfg* cfg, const void* x, co
   }
   if (cfg->N == 0 && !weight) return DENDSN_OK;
   NormArgs a{};
-  a.x = x; a.w = weight; a.rstd_in = rstd; a.gy = grad_y; a.gsum = grad_sum; a.gx = grad_x;
+  a.x = x; a.residual = residual; a.w = weight; a.rstd_in = rstd; a.gy = grad_y; a.gsum = grad_sum; a.gx = grad_x;
   a.part = static_cast<float*>(workspace);
-  a.ld_x = cfg->ld_x; a.ld_gy = cfg->ld_grad_y; a.ld_gsum = cfg->ld_grad_sum; a.ld_gx = cfg->ld_grad_x;
+  a.ld_x = cfg->ld_x; a.ld_residual = cfg->ld_residual; a.ld_gy = cfg->ld_grad_y; a.ld_gsum = cfg->ld_grad_sum; a.ld_gx = cfg->ld_grad_x;
   a.N = int32_t(cfg->N); a.D = int32_t(cfg->D);
   const Shape shape = shape_of(cfg);
   const int64_t parts = parts_of(cfg);

@@ -92,3 +92,22 @@ def test_norm_rows_that_memory_holds_are_not_refused():
     assert norm_call(N=many, D=8192) == UNSUPPORTED
     assert norm_call(N=(1 << 24) + 1, D=4096) == UNSUPPORTED
     assert norm_call(N=0, D=1 << 22) == INVALID
+
+
+def test_norm_backward_of_a_residual():
+    c = dict(N=10, D=64, io=0, eps=1e-6, **{k: 64 for k in ("ld_x", "ld_residual", "ld_y", "ld_sum", "ld_grad_y", "ld_grad_sum",
+                                                            "ld_grad_x")})
+
+    def call(ws=0x90000, nbytes=1 << 40, n=10, **kw):
+        at = dict(x=0x10000, residual=0x20000, weight=0x30000, rstd=0x40000, grad_y=0x50000, grad_sum=None, grad_x=0x60000,
+                  grad_weight=0x70000)
+        at.update(kw)
+        return dendsn.block_lib().dendsn_norm_backward_residual(
+            ctypes.byref(dendsn_norm_cfg(**dict(c, N=n))), *(ctypes.c_void_p(a) for a in at.values()), ctypes.c_void_p(ws), nbytes, None)
+
+    for k in ("x", "rstd", "grad_y", "grad_x", "grad_weight"):
+        assert call(**{k: None}) == 1, k
+    for k in ("x", "residual", "weight", "rstd", "grad_y", "grad_sum", "grad_x", "grad_weight"):
+        assert call(**{k: 0x10002}) == 1, k
+    assert call(ws=None) == 3 and call(nbytes=4) == 3 and call(ws=0x90008) == 3
+    assert call(n=0, weight=None, grad_weight=None, ws=None, nbytes=0) == 0
