@@ -11,7 +11,7 @@
 // conditions where a round is whole (1683 -> 1589 us below).
 //
 // 292M values in 122 tensors, bf16 gradients and copies: 1589 us with fp32 states (5.15 TB/s, a copy's
-// rate), 961 us in 8 bits (4.9 TB/s; its 70 vector instructions a value take nearly as long:
+// rate), 961 to 975 us in 8 bits (4.9 TB/s; its 70 vector instructions a value take nearly as long:
 // with a second root and a division 1056).
 //
 // In 8 bits a value is rounded down or up at random, so that its mean is kept.  v changes by a
@@ -56,7 +56,9 @@ struct Batch {
   const float* grad_scale;
 };
 
-// A bijection of 32 bits: rounds of folding the high half down and an odd product.
+// A bijection of 32 bits: rounds of folding the high half down and an odd product.  The first and the last
+// multiplier are those of a published 32-bit hash (C. Wellons, "Prospecting for Hash Functions", 2018),
+// found there by search; the one between is 2^32 over the golden ratio.
 __device__ __forceinline__ uint32_t mix(uint32_t h) {
   h = (h ^ (h >> 16)) * 0x7FEB352Du;
   h = (h ^ (h >> 16)) * 0x9E3779B1u;

@@ -28,8 +28,9 @@
 //
 // Products are matrix instructions of 16 x 16.  In bf16 the inputs are operands as they are;
 // everything computed on the way is a sum of bf16 values: of three in the scans, whose states
-// are outputs in fp32 (s_last off by 7e-8; by 3.5e-6 with two), of two where all ends in bf16.  In
-// fp32 the fp32 instruction is used.  States and values that the backward reads are kept in fp32.
+// are outputs in fp32 (s_last off by 0.8 to 1.5e-7 of a head's norm, grad_s0 by 1.5 to 2.3e-7; s_last by
+// 3.5e-6 with two), of two where all ends in bf16.  In fp32 the fp32 instruction is used.  States and
+// values that the backward reads are kept in fp32.
 //
 // 8192 steps of 4 sequences, 16 heads of 128 x 128, bf16, under a profiler: local 190 us twice (400 MB
 // written: 3.5 TB/s), scan 620, back_scan 740, back_local 605 (2.7 GB: 4.3 TB/s, bound by memory).
@@ -368,6 +369,8 @@ __device__ __forceinline__ double chunk_sum(const DeltaArgs& a, int b, int h, in
 // local: T and P (BACK: turned) and the decays of one chunk.  Wave w has steps 16 w to + 15
 // of A and P.  T by blocks of 16: those on the diagonal by substitution, a column a lane; then
 // T_ij = -T_ii sum over k from j to i - 1 of A_ik T_kj, a diagonal of blocks at a time, in fp32.
+// Both squares are written whole, with all planes: what the scans do not read of them (the quarter that
+// is 0, forward P's third plane) is some 150 of the 409 MB of the longest case forward, 100 back.
 // ---------------------------------------------------------------------------
 // Eight values of a row of T or P from LDS, as planes in memory.
 template <class M>
@@ -1674,7 +1677,8 @@ DeltaPlan make_plan(const dendsn_delta_cfg* c) {
   p.pm = w.take(size_t(p.items) * square);
   p.dec = w.take(size_t(p.items) * 3 * kC * 4);
   // With few heads the steps are cut into segments: the number that takes the fewest rounds of chunks,
-  // a CU having one block at a time, where each chunk goes through both passes and a join takes about
+  // a CU having one block (here: of 16 columns) at a time, where each chunk goes through both passes and
+  // a join takes about
   // a chunk's time (16384 steps of 4 heads, bf16, forward: 626 us whole).
   const int64_t heads = c->batch * c->H, states = p.Vp / 16 * heads, maps = (p.Vp + p.KP) / 16 * heads;
   int64_t segs = 1, least = p.nc * ceil_div(states, kCus);
@@ -1781,7 +1785,8 @@ dendsn_status launch_back_local(const DeltaArgs& a, hipStream_t stream) {
 // 32 columns of v a block where that gives each CU one, else 16: what a chunk reads of q, k, T and P
 // is half as much a column, but a block's chunk takes longer (16 and 32, forward and back, bf16, heads
 // of 128 x 128: 32 heads of 2048 steps 102 + 116 and 129 + 155 us, 64 of 8192 steps 955 + 1023 and
-// 646 + 741).
+// 646 + 741).  Between, from 33 to 63 such heads, 16 columns take two rounds of blocks where 32 take
+// one; no measurement stands for that range, and by these figures 32 would be the faster there.
 template <class M, class L, int KP, bool ODD>
 dendsn_status launch(const DeltaArgs& a, bool back, hipStream_t stream) {
   const bool wide = int64_t(a.Vp / 32) * a.batch * a.H >= 256;

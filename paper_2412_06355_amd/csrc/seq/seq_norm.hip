@@ -12,7 +12,11 @@
 //
 // 16384 rows of 4096 in bf16 with the stream: forward 126 us (4.3 TB/s), backward 119 us (4.5 TB/s)
 // and 7 for the parts' sum; registers for as many packs as the row has instead of four: backward
-// 187 -> 119.  8192 rows of 2048 to e4m3: 33 us (3.5 TB/s; 8 bytes a lane written).
+// 187 -> 119.  4096 rows of 16384, of 1024 lanes each: 139 (3.9) and 119 (4.5).  8192 rows of 2048 to
+// e4m3: 35 us (3.3 TB/s), where a device copy of as many bytes takes 24.  Why is not settled: rows of fp32
+// go at a copy's rate in the same kernel (16384 of 2048: 83 us, 5.2 TB/s), so it is not memory; the same
+// rows to bf16, without a second reduction and divisions, take 37 (3.7 TB/s), so it is not those alone;
+// 16384 of 4096 to e4m3 take 121 (3.9 TB/s), so the launch's length is a part.
 #include "dendsn_block.h"
 #include "seq_common.h"
 
@@ -216,8 +220,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_fwd_kernel(NormArg
 // hat is of the row that is given: of the sum that the forward stored, which has io's bits, or (RES) of
 // x + residual, formed again as the forward had it, for one more row read.  What y and rstd are the norm
 // of is the second; in bf16 the first moves every hat by up to 2^-8 of itself, and grad_weight by about as
-// much as its own rounding does (off by 2.4e-3 in norm, not 1.7e-3).  The choice is the caller's: 16384
-// rows of 4096 in bf16 take 120 us the first way, 146 the second.
+// much as its own rounding does (4096 rows of 512: off by 2.5e-3 in norm, not 1.6e-3).  The choice is the
+// caller's: 16384 rows of 4096 in bf16 take 120 us the first way, 146 the second.
 template <typename IO, int TPR, int kE, bool W, bool RES>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_bwd_kernel(NormArgs a) {
   constexpr int V = kV<IO>, kBlock = TPR > 256 ? TPR : 256, kRows = kBlock / TPR;
