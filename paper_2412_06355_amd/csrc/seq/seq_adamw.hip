@@ -76,11 +76,10 @@ __device__ __forceinline__ float round_at(float size, float u) {
 struct Scale {
   float scale, inv;
 };
-// Of values whose largest magnitude is top: its 448th part, as a quotient (448 is no power of two: the
-// product with its rounded reciprocal is another number for half of all blocks).  Scales stay normal
-// numbers, so that they can be inverted: values below 2^-117 are of no account.
+// Of values whose largest magnitude is top.  Scales stay normal numbers, so that they can be
+// inverted: values below 2^-117 are of no account.
 __device__ __forceinline__ Scale scale_of(float top) {
-  const float s = top > 0.0f ? fmaxf(top / kTop, 0x1p-126f) : 1.0f;
+  const float s = top > 0.0f ? fmaxf(top * (1.0f / kTop), 0x1p-126f) : 1.0f;
   return {s, 1.0f / s};
 }
 
