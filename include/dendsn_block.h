@@ -194,7 +194,7 @@ typedef struct dendsn_adamw_tensor {
  *   grad_scale [1] fp32 on the device, optional: gradients are multiplied by it first
  *   seed       of the random bits of 8-bit states
  * 8-bit states hold m and the root of v in blocks of 256 values, each value an e4m3 number
- * times its block's scale (the 448th part of the block's largest magnitude).  A value is
+ * times its block's scale (the block's largest magnitude times 1/448 rounded to fp32).  A value is
  * rounded to one of its two neighbours at random, so that its mean is kept: with rounding
  * to the nearest v could not fall by less than a sixteenth, and would not fall at all.  A v
  * that is not 0 is kept above 0.  The random bits are a hash of seed, the step, the tensor's

@@ -19,7 +19,7 @@
 // would never move.  What is held is the root of v, whose range is half v's in binades; one
 // that is not 0 stays at least at the smallest code, so that m / root stays bounded.  Whether a
 // value goes down or up hangs on its last bit, so what decides it is computed as it is written:
-// products and sums rounded one by one, quotients to the nearest.
+// products and sums rounded one by one, a value over its scale to the nearest.
 #include <cfloat>
 
 #include "dendsn_block.h"
@@ -76,7 +76,9 @@ __device__ __forceinline__ float round_at(float size, float u) {
 struct Scale {
   float scale, inv;
 };
-// Of values whose largest magnitude is top.  Scales stay normal numbers, so that they can be
+// Of values whose largest magnitude is top: that times 1 / 448 as fp32 has it.  (So does torch divide by a
+// number on the GPU; the quotient, which is another number for half of all blocks, would decide other
+// roundings than those formulas in torch do.)  Scales stay normal numbers, so that they can be
 // inverted: values below 2^-117 are of no account.
 __device__ __forceinline__ Scale scale_of(float top) {
   const float s = top > 0.0f ? fmaxf(top * (1.0f / kTop), 0x1p-126f) : 1.0f;
