@@ -128,7 +128,8 @@ typedef struct dendsn_norm_cfg {
  *   y        [N,D] io
  *   sum      [N,D] io   optional output: s, as the backward and the next layer read it
  *   rstd     [N] fp32   optional output
- * The statistics and y are of s before its rounding to io.
+ * The statistics and y are of s before its rounding to io.  Squares are summed in fp32 as they are: a row
+ * with values past some 10^19 has rstd 0, and a y of 0.
  */
 dendsn_status dendsn_norm_forward(const dendsn_norm_cfg* cfg, const void* x, const void* residual, const void* weight,
                                   void* y, void* sum, float* rstd, hipStream_t stream);

@@ -68,3 +68,17 @@ def test_a_row_for_all_and_empty(gpu_device):
     assert got["grad_x"].shape == (0, 40) and not got["grad_weight"].any()
     with pytest.raises(ValueError):
         dendsn.rms_norm_backward(cfg, m["x"], m["weight"], rstd, m["grad_y"], residual=one[:8])
+
+
+def test_squares_past_fp32(gpu_device):
+    """As documented: a row whose squares' sum passes fp32 has an rstd and a y of 0, the others their own."""
+    d = make(4, 96, "f32", 7)
+    d["x"][2] = 1e20
+    m = on(d, gpu_device)
+    announce("norm of squares past fp32")
+    cfg = dendsn.RMSNormConfig(N=4, D=96)
+    y, rstd, _ = dendsn.rms_norm(cfg, m["x"], m["weight"])
+    assert float(rstd[2]) == 0 and not y[2].any()
+    ref = block_ref.norm(d["x"], d["weight"], None, 1e-6, "f32")["y"]
+    keep = [0, 1, 3]
+    seq_ref.assert_within(y[keep], ref[0][keep], ref[1][keep], "y")
